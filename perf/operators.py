@@ -262,7 +262,7 @@ def _plain_logp(s, c):
     e = (z - m).exp()
     total = e.sum(1, keepdim=True)
     lse = m + total.log()
-    logp = torch.where(tok < 0, 0.0, (z.gather(1, tok.clamp_min(0)[:, None]) - lse)[:, 0])
+    logp = torch.where(tok < 0, 0.0, (z.gather(1, tok.clamp_min(0)[:, None]) - m - total.log())[:, 0])
     p = e / total
     entropy = -torch.where(p > 0, p * (z - lse), 0.0).sum(1)
     out = [logp, lse[:, 0], entropy]
@@ -272,7 +272,7 @@ def _plain_logp(s, c):
         order = torch.where(bits < 0, -(bits & 0x7FFFFFFF), bits)
         key = order * (1 << 20) - torch.arange(z.shape[1], device=z.device)
         ids = z.shape[1] - 1 - (key.topk(k, dim=1).values + z.shape[1] - 1) % (1 << 20)
-        out += [ids.to(s["tokens"].dtype), z.gather(1, ids) - lse]
+        out += [ids.to(s["tokens"].dtype), z.gather(1, ids) - m - total.log()]
     return out
 
 
@@ -324,8 +324,9 @@ def _plain_distill(s, c):
     loss = torch.where(q > 0, q * (logq - logp), 0.0).sum(1)
     out, p_tail = [lse[:, 0]], None
     if c["tail"]:
-        rest = torch.where(_member(s["ids"], z.shape[1]), 0.0, e).sum(1)
-        log_tail = rest.log() - total[:, 0].log()
+        # log of the share outside the ids, from both sums: near 1 the difference of two logs would cancel
+        named = _member(s["ids"], z.shape[1])
+        log_tail = -torch.log1p(torch.where(named, e, 0.0).sum(1) / torch.where(named, 0.0, e).sum(1))
         p_tail = log_tail.exp()
         loss = loss + torch.where(q_tail > 0, q_tail * (q_tail.log() - log_tail), 0.0)
         out.append(log_tail)
