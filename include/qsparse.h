@@ -60,7 +60,8 @@ enum {
     QS_NONFINITE = -5,   /* an inf or NaN reached the compressor (device status)       */
     QS_STATE = -6,       /* call out of order (no buffers bound, nothing compressed)   */
     QS_TIMEOUT = -7,     /* a bounded device-side wait ran out (device status)         */
-    QS_TOO_LARGE = -8    /* d beyond QS_STATIC_MAX_D (qs_unpack_accumulate_static only) */
+    QS_TOO_LARGE = -8    /* d beyond QS_STATIC_MAX_D (qs_unpack_accumulate_static), or a size beyond
+                            the limits of the language-model operators                   */
 };
 
 /* Sparsifiers of Section 2.2. */
@@ -381,6 +382,124 @@ int qs_unpack_accumulate_static(int R, int64_t d, int64_t k, int s, int quantize
 
 /* Frees the scratch and the context (NULL is allowed). */
 void qs_destroy(qs_ctx* ctx);
+
+/*
+ * Language-model operators: the two ends of a language model's local step, whose gradients
+ * qs_local_step and qs_sync_round_step take.  (The paper trains classifiers; these have no
+ * counterpart there.)  They take no context, allocate nothing and keep nothing between calls: the
+ * work goes on cuda_stream of the current device, scratch is the caller's.
+ *   - Element types QS_F32, QS_BF16, QS_F16; sums, norms and statistics are held in fp32 and
+ *     results rounded once.  Ids are QS_I32 or QS_I64.
+ *   - A negative id names nothing (padding); an id past the last row or column names nothing
+ *     either, makes what depends on it NaN where the call says so, and puts QS_INVALID_ARG into
+ *     *status (device, one int the caller has set to 0, or NULL).
+ *   - Pointers are aligned to their element type; strides are counted in elements.  16-byte
+ *     aligned rows of equal phase are the fast case; every other one is correct.
+ *   - Results do not depend on the order in which blocks run.
+ */
+enum { QS_F32 = 0, QS_BF16 = 1, QS_F16 = 2 };
+enum { QS_I32 = 0, QS_I64 = 1 };
+
+/*
+ * qs_embed — rows of the workers' embedding tables: out[r N + n, :] = scale * table_r[t, :] with
+ * t = tokens[r N + n], one product in fp32.
+ *   R <= 32 workers, N tokens each, tables of V rows of D; tokens R x N.
+ *   table + r * worker_stride is worker r's table (0: all workers read one), rows row_stride >= D
+ *   apart; out: R N rows, out_stride >= D apart.
+ *   A negative token gives a row of zeros, one >= V a row of NaN.
+ * R N, V, D <= 2^30, else QS_TOO_LARGE.
+ */
+int qs_embed(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int token_type,
+             const void* table, int table_type, int64_t worker_stride, int64_t row_stride,
+             float scale, void* out, int out_type, int64_t out_stride, int* status,
+             void* cuda_stream);
+
+/*
+ * qs_embed_grad — gradient of qs_embed with respect to the tables:
+ *   grad_table_r[v, :] = scale * sum of grad_out[r N + n, :] over the n with tokens[r N + n] = v
+ * (accumulate != 0: that much is added, and rows no token names are neither read nor written;
+ * otherwise those rows become zero).  The places are sorted by token, equal tokens in order, and
+ * each row's sum is taken in an order that depends on the tokens alone: the same call gives the
+ * same bits.  Tokens that name no row add nothing.
+ *   grad_out: R N rows, grad_stride >= D apart.  grad_table: fp32, worker_stride and row_stride as
+ *   in qs_embed (so that it can be a stretch of the R x d gradient of qs_local_step); the workers'
+ *   tables must not overlap.
+ *   work: device, 16-byte aligned, qs_embed_grad_bytes(R, N, V, D) bytes, else QS_CAPACITY.
+ */
+int64_t qs_embed_grad_bytes(int R, int64_t N, int64_t V, int64_t D);
+int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int token_type,
+                  const void* grad_out, int grad_type, int64_t grad_stride, float scale,
+                  int accumulate, float* grad_table, int64_t worker_stride, int64_t row_stride,
+                  void* work, int64_t work_bytes, int* status, void* cuda_stream);
+
+/*
+ * qs_token_logp — for N rows of V logits, with y = scale * logits (scale > 0, one over the
+ * temperature) and p = softmax(y):
+ *   lse = log sum exp y;  logp = y_t - lse of the given token t;  entropy = - sum p log p;
+ *   top_ids, top_logp (N x top, top <= QS_MAX_TOP and <= V): the columns of the largest logits,
+ *   largest first, equal logits by lower index, and their log probabilities.
+ * Any of logp (then tokens may be NULL), lse, entropy may be NULL; top = 0 takes no alternatives.
+ * top_ids are of token_type.
+ *   A column at -inf has p = 0 and is no alternative: places left over hold id -1 and -inf.  A row
+ *   of nothing else has lse = logp = -inf and entropy 0.  A NaN or +inf in a row makes its lse,
+ *   logp, entropy and top_logp NaN and its top_ids -1.
+ *   A negative token gives logp = 0, one >= V gives NaN.
+ * logits: rows row_stride >= V apart.  N, V <= 2^30, else QS_TOO_LARGE.
+ */
+#define QS_MAX_TOP 128
+int qs_token_logp(int64_t N, int64_t V, const void* logits, int type, int64_t row_stride,
+                  const void* tokens, int token_type, float scale, int top, float* logp,
+                  float* lse, float* entropy, void* top_ids, float* top_logp, int* status,
+                  void* cuda_stream);
+
+/*
+ * qs_token_logp_grad — gradient of sum_n (grad_logp[n] logp[n] + grad_entropy[n] entropy[n]) with
+ * respect to the logits, in their type, from the lse (and entropy) that qs_token_logp gave:
+ *   scale * ( g (1[v = t] - p_v) - h p_v (log p_v + entropy) ),   0 where p_v = 0 and v != t.
+ *   grad_logp NULL: grad_logp_all for every row.  grad_entropy NULL: none (entropy is not read).
+ *   tokens NULL or a negative token: no part from logp; one >= V: a row of NaN.
+ *   A row whose lse is -inf gets zeros.
+ *   grad: rows grad_stride >= V apart; it may be the logits themselves (same stride), any other
+ *   overlap is QS_INVALID_ARG.
+ */
+int qs_token_logp_grad(int64_t N, int64_t V, const void* logits, int type, int64_t row_stride,
+                       const void* tokens, int token_type, float scale, const float* lse,
+                       const float* entropy, const float* grad_logp, float grad_logp_all,
+                       const float* grad_entropy, void* grad, int64_t grad_stride, int* status,
+                       void* cuda_stream);
+
+/*
+ * qs_distill — distillation from a teacher's top logits.  Row n has K <= QS_MAX_TOP entries (id,
+ * teacher's value u; negative ids are padding) and w_k = exp(teacher_scale * u_k); with y, lse, p
+ * as in qs_token_logp (the student):
+ *   tail == 0   q_k = w_k / sum w                       the teacher's top, renormalised
+ *   tail != 0   q_k = w_k (u are log probabilities), and all other columns form one more class
+ *               with q_T = max(0, 1 - sum q) and p_T = the student's mass outside the ids
+ *   loss = sum_k q_k (log q_k - log p_k) [+ q_T (log q_T - log p_T)],   0 log 0 = 0
+ * and, when grad is given, in the same pass over the logits the gradient of
+ * sum_n weight[n] loss[n] (weight NULL: weight_all for every row) in their type:
+ *   weight scale ( p_v (Q + q_T) - [v outside the ids] p_v q_T / p_T - q_v ),   Q = sum q.
+ * ids, teacher: N x K, contiguous; an id given twice counts as two entries of one class.
+ *   loss, lse, log_tail (log p_T; written when tail != 0), each N or NULL.
+ *   A row without entries (tail == 0) has loss 0 and gradient 0; q_k > 0 on a column at -inf gives
+ *   loss +inf; a row of logits at -inf has gradient 0.  An id >= V makes the row's loss and
+ *   gradient NaN.  grad and its overlap as in qs_token_logp_grad.
+ */
+int qs_distill(int64_t N, int64_t V, int K, const void* logits, int type, int64_t row_stride,
+               const void* ids, int id_type, const void* teacher, int teacher_type, float scale,
+               float teacher_scale, int tail, float* loss, float* lse, float* log_tail,
+               const float* weight, float weight_all, void* grad, int64_t grad_stride, int* status,
+               void* cuda_stream);
+
+/*
+ * qs_distill_grad — the same gradient on its own, from the lse (and, for tail != 0, log_tail) that
+ * qs_distill gave, for weights that are known only after the loss.
+ */
+int qs_distill_grad(int64_t N, int64_t V, int K, const void* logits, int type, int64_t row_stride,
+                    const void* ids, int id_type, const void* teacher, int teacher_type,
+                    float scale, float teacher_scale, int tail, const float* lse,
+                    const float* log_tail, const float* weight, float weight_all, void* grad,
+                    int64_t grad_stride, int* status, void* cuda_stream);
 
 #ifdef __cplusplus
 }

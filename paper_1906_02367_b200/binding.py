@@ -19,6 +19,9 @@ QS_STATIC_MAX_D = 1 << 20
 QS_TOPK, QS_RANDK = 0, 1
 QS_QSGD, QS_QSGD_SCALED, QS_SIGN_L1, QS_NONE, QS_SIGN_L2, QS_MINMAX = 0, 1, 2, 3, 4, 5
 QS_ROUND_AUTO = 2**64 - 1
+QS_F32, QS_BF16, QS_F16 = 0, 1, 2
+QS_I32, QS_I64 = 0, 1
+QS_MAX_TOP = 128
 
 EXPORTS = [
     "qs_init", "qs_set_segments", "qs_set_sharding", "qs_bind", "qs_local_step", "qs_local_step_momentum", "qs_sync_round_step",
@@ -27,6 +30,7 @@ EXPORTS = [
     "qs_record_bits", "qs_total_k", "qs_sync_status", "qs_last_error", "qs_get_round", "qs_set_round",
     "qs_get_stats", "qs_enable_phase_timing", "qs_get_phase_timing", "qs_get_stage_trace", "qs_unpack_accumulate_static",
     "qs_gap_words", "qs_recode_gaps", "qs_decode_gaps", "qs_destroy",
+    "qs_embed", "qs_embed_grad", "qs_embed_grad_bytes", "qs_token_logp", "qs_token_logp_grad", "qs_distill", "qs_distill_grad",
 ]
 
 _lib = None
@@ -79,6 +83,15 @@ def lib():
         L.qs_get_phase_timing.argtypes = [vp, vp, C.c_int]
         L.qs_get_stage_trace.argtypes = [vp, vp, C.c_int]
         L.qs_unpack_accumulate_static.argtypes = [C.c_int, i64, i64, C.c_int, C.c_int, vp, vp, i64, vp, vp]
+        i32, f32 = C.c_int, C.c_float
+        L.qs_embed.argtypes = [i32, i64, i64, i64, vp, i32, vp, i32, i64, i64, f32, vp, i32, i64, vp, vp]
+        L.qs_embed_grad_bytes.argtypes = [i32, i64, i64, i64]
+        L.qs_embed_grad_bytes.restype = i64
+        L.qs_embed_grad.argtypes = [i32, i64, i64, i64, vp, i32, vp, i32, i64, f32, i32, vp, i64, i64, vp, i64, vp, vp]
+        L.qs_token_logp.argtypes = [i64, i64, vp, i32, i64, vp, i32, f32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.qs_token_logp_grad.argtypes = [i64, i64, vp, i32, i64, vp, i32, f32, vp, vp, vp, f32, vp, vp, i64, vp, vp]
+        L.qs_distill.argtypes = [i64, i64, i32, vp, i32, i64, vp, i32, vp, i32, f32, f32, i32, vp, vp, vp, vp, f32, vp, i64, vp, vp]
+        L.qs_distill_grad.argtypes = [i64, i64, i32, vp, i32, i64, vp, i32, vp, i32, f32, f32, i32, vp, vp, vp, f32, vp, i64, vp, vp]
         L.qs_destroy.argtypes = [vp]
         L.qs_destroy.restype = None
         _lib = L

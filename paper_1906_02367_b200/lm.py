@@ -1,0 +1,288 @@
+"""Language-model operators on torch tensors: embedding rows and their gradient, log probabilities of
+given tokens, distillation from a teacher's top logits.
+
+Argument checks and marshalling for the qs_embed, qs_token_logp and qs_distill families of
+include/qsparse.h, which says what each computes; the arithmetic is in the CUDA library.  Everything is
+enqueued on `stream` (default: the current stream of the tensors' device, which must be the current
+device) and nothing waits for the GPU.  Tensors made on other streams are the caller's to order, as with any
+torch call.  `status`, where taken, is an int32 CUDA tensor of one element, zero before the call, that receives
+QS_INVALID_ARG if an id lies past the last row or column.
+"""
+import contextlib
+from collections import namedtuple
+
+import torch
+
+from .binding import QS_BF16, QS_F16, QS_F32, QS_I32, QS_I64, QS_MAX_TOP, QsError, lib
+
+TokenLogp = namedtuple("TokenLogp", "logp lse entropy top_ids top_logp")
+Distill = namedtuple("Distill", "loss lse log_tail grad")
+
+_TYPE = {torch.float32: QS_F32, torch.bfloat16: QS_BF16, torch.float16: QS_F16}
+_ID = {torch.int32: QS_I32, torch.int64: QS_I64}
+_HERE = contextlib.nullcontext()
+
+
+def _type(t, what, table=_TYPE):
+    code = table.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: {t.dtype} is not one of {', '.join(str(d) for d in table)}")
+    return code
+
+
+def _on(first, *rest):
+    """All tensors on the current CUDA device."""
+    dev = first.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current CUDA device, not on {dev}")
+    for t in rest:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+
+
+def _stream(stream):
+    """(stream handle, context in which results are allocated so that they belong to that stream)."""
+    cur = torch.cuda.current_stream()
+    if stream is None or stream == cur:
+        return cur.cuda_stream, _HERE
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _done(rc, what):
+    if rc < 0:
+        raise QsError(rc, what + (": arguments refused" if rc == -1 else " failed"))
+
+
+def _rows(t, what):
+    """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one."""
+    if t.dim() < 2 or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{what} needs rows with unit stride")
+    step = t.stride(-2)
+    for i in range(t.dim() - 3, -1, -1):
+        if t.shape[i] > 1 and t.stride(i) != _step_of(t, i):
+            raise ValueError(f"{what}: leading dimensions must flatten into rows of one stride")
+    return step if t.shape[-2] > 1 or t.dim() > 2 else max(step, t.shape[-1])
+
+
+def _step_of(t, i):
+    return t.stride(i + 1) * t.shape[i + 1]
+
+
+def _vector(t, n, what, dtype=torch.float32):
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{what} needs {n} contiguous elements of {dtype}")
+
+
+def _result(out, shape, dtype, device, what):
+    """`out` checked, or a new tensor."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if out.shape != torch.Size(shape) or out.dtype != dtype:
+        raise ValueError(f"{what} must be {tuple(shape)} of {dtype}")
+    return out
+
+
+def _table(t, R, what):
+    """(vocabulary, width, worker stride, row stride) of a (V, D) or (R, V, D) table."""
+    if t.dim() not in (2, 3) or (t.dim() == 3 and t.shape[0] != R):
+        raise ValueError(f"{what} must be (V, D), or (R, V, D) for R workers' tokens")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what} needs rows with unit stride")
+    V, D = t.shape[-2], t.shape[-1]
+    row = t.stride(-2) if V > 1 else max(t.stride(-2), D)
+    return V, D, (t.stride(0) if t.dim() == 3 and R > 1 else 0), row
+
+
+def _tokens(tokens, workers):
+    """(R, N) of tokens: with a table per worker the first dimension counts the workers."""
+    if not tokens.is_contiguous():
+        raise ValueError("tokens must be contiguous")
+    if workers:
+        if tokens.dim() < 2:
+            raise ValueError("a table per worker needs tokens (R, ..)")
+        R = tokens.shape[0]
+        return R, tokens.numel() // R if R else 0
+    return 1, tokens.numel()
+
+
+def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=None):
+    """scale * table[tokens] (qs_embed): tokens (.., N) with a (V, D) table, or (R, .., N) with (R, V, D), one table
+    per worker.  Negative tokens give zeros.  Returns tokens.shape + (D,) in `dtype` (default the table's)."""
+    _on(tokens, table, out, status)
+    R, N = _tokens(tokens, table.dim() == 3)
+    V, D, ws, rs = _table(table, R, "table")
+    st, where = _stream(stream)
+    with where:
+        out = _result(out, (*tokens.shape, D), dtype or (out.dtype if out is not None else table.dtype), table.device, "out")
+    os_ = _rows(out, "out") if out.dim() > 1 else D
+    _done(lib().qs_embed(R, N, V, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), table.data_ptr(), _type(table, "table"), ws, rs,
+                         scale, out.data_ptr(), _type(out, "out"), os_, _ptr(status), st), "qs_embed")
+    return out
+
+
+def embed_grad_work(workers, tokens, vocab, width, device=None):
+    """Scratch of embed_grad for `tokens` tokens per worker."""
+    n = lib().qs_embed_grad_bytes(workers, tokens, vocab, width)
+    _done(min(n, 0), "qs_embed_grad_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device or "cuda")
+
+
+def embed_grad(tokens, grad_out, vocab, scale=1.0, workers=None, accumulate=False, out=None, work=None, status=None, stream=None):
+    """Gradient of embed with respect to the table(s) (qs_embed_grad), fp32.  grad_out: tokens.shape + (D,).
+    workers (default: tokens have more than one dimension, or out has three): a table per entry of the tokens' first
+    dimension, result (R, vocab, D); otherwise one table, (vocab, D).  `out` may be a strided view, a stretch of
+    the rows of a gradient batch; with accumulate it is added to and rows no token names stay untouched."""
+    _on(tokens, grad_out, out, work, status)
+    if workers is None:
+        workers = out.dim() == 3 if out is not None else tokens.dim() > 1
+    R, N = _tokens(tokens, workers)
+    D = grad_out.shape[-1]
+    if grad_out.shape[:-1] != tokens.shape:
+        raise ValueError(f"grad_out {tuple(grad_out.shape)} does not belong to tokens {tuple(tokens.shape)}")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    st, where = _stream(stream)
+    with where:
+        out = _result(out, (R, vocab, D) if workers else (vocab, D), torch.float32, grad_out.device, "out")
+        if work is None:
+            work = embed_grad_work(R, N, vocab, D, grad_out.device)
+    _, _, ws, rs = _table(out, R, "out")
+    _done(lib().qs_embed_grad(R, N, vocab, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), grad_out.data_ptr(),
+                              _type(grad_out, "grad_out"), _rows(grad_out, "grad_out"), scale, int(accumulate), out.data_ptr(), ws, rs,
+                              work.data_ptr(), work.numel() * work.element_size(), _ptr(status), st), "qs_embed_grad")
+    return out
+
+
+def _logits(logits):
+    if logits.dim() != 2:
+        raise ValueError("logits must be (N, V)")
+    return logits.shape[0], logits.shape[1], _rows(logits, "logits")
+
+
+def token_logp(logits, tokens=None, scale=1.0, top=0, status=None, stream=None):
+    """Log probabilities of `tokens` (N) under softmax(scale * logits) (qs_token_logp), with the log of the sum, the
+    entropy, and the `top` largest logits' columns and log probabilities (equal logits: lower index first).
+    tokens None: no logp, and top_ids are int64.  Returns TokenLogp; fields not asked for are None."""
+    _on(logits, tokens, status)
+    N, V, step = _logits(logits)
+    if not 0 <= top <= min(QS_MAX_TOP, V):
+        raise ValueError(f"top must be between 0 and {min(QS_MAX_TOP, V)}")
+    id_type = torch.int64
+    if tokens is not None:
+        id_type = tokens.dtype
+        _type(tokens, "tokens", _ID)
+        _vector(tokens, N, "tokens", id_type)
+    st, where = _stream(stream)
+    dev = logits.device
+    with where:
+        stats = torch.empty((3, N), dtype=torch.float32, device=dev)
+        ids = torch.empty((N, top), dtype=id_type, device=dev) if top else None
+        top_logp = torch.empty((N, top), dtype=torch.float32, device=dev) if top else None
+    base = stats.data_ptr()
+    _done(lib().qs_token_logp(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens), _ID[id_type], scale, top,
+                              base if tokens is not None else None, base + 4 * N, base + 8 * N, _ptr(ids), _ptr(top_logp), _ptr(status), st),
+          "qs_token_logp")
+    logp, lse, entropy = stats.unbind(0)
+    return TokenLogp(logp if tokens is not None else None, lse, entropy, ids, top_logp)
+
+
+def _gradient(logits, out):
+    """Stride of the result's rows."""
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    return _rows(out, "out")
+
+
+def _weights(w, n, what):
+    """(pointer, number) of a weight per row or one for all."""
+    if isinstance(w, torch.Tensor):
+        _vector(w, n, what)
+        return w.data_ptr(), 0.0
+    return None, float(w)
+
+
+def token_logp_grad(logits, tokens, lse, grad_logp=1.0, scale=1.0, entropy=None, grad_entropy=None, out=None, status=None, stream=None):
+    """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits (qs_token_logp_grad).
+    grad_logp: (N) or a number; grad_entropy: (N) or None.  out may be the logits themselves."""
+    _on(logits, tokens, lse, entropy, grad_entropy, out, status)
+    N, V, step = _logits(logits)
+    if tokens is not None:
+        _vector(tokens, N, "tokens", tokens.dtype)
+    if grad_entropy is not None and entropy is None:
+        raise ValueError("grad_entropy needs the entropy")
+    for t, what in ((lse, "lse"), (entropy, "entropy"), (grad_entropy, "grad_entropy")):
+        _vector(t, N, what)
+    if isinstance(grad_logp, torch.Tensor):
+        _on(logits, grad_logp)
+    g, g_all = _weights(grad_logp, N, "grad_logp")
+    st, where = _stream(stream)
+    with where:
+        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    _done(lib().qs_token_logp_grad(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens),
+                                   _type(tokens, "tokens", _ID) if tokens is not None else QS_I64, scale, lse.data_ptr(), _ptr(entropy), g, g_all,
+                                   _ptr(grad_entropy), out.data_ptr(), _gradient(logits, out), _ptr(status), st), "qs_token_logp_grad")
+    return out
+
+
+def _entries(ids, teacher, N):
+    """K of the teacher's entries."""
+    if ids.dim() != 2 or ids.shape[0] != N or ids.shape != teacher.shape or not ids.is_contiguous() or not teacher.is_contiguous():
+        raise ValueError("ids and teacher must be contiguous (N, K)")
+    if not 1 <= ids.shape[1] <= QS_MAX_TOP:
+        raise ValueError(f"between 1 and {QS_MAX_TOP} entries per row")
+    return ids.shape[1]
+
+
+def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weight=None, out=None, status=None, stream=None):
+    """Loss of softmax(scale * logits) against a teacher's top entries (qs_distill): ids (N, K) and the teacher's logits
+    there, renormalised, or with `tail` its log probabilities and the rest of its mass as one more class.  token_logp's
+    top_ids and top_logp are such entries.  weight (N) or a number: the gradient of sum(weight * loss) with
+    respect to the logits as well, from the same pass; out receives it and may be the logits themselves."""
+    _on(logits, ids, teacher, out, status)
+    N, V, step = _logits(logits)
+    K = _entries(ids, teacher, N)
+    w, w_all = None, 0.0
+    if weight is not None:
+        if isinstance(weight, torch.Tensor):
+            _on(logits, weight)
+        w, w_all = _weights(weight, N, "weight")
+    elif out is not None:
+        raise ValueError("a gradient needs weight")
+    st, where = _stream(stream)
+    with where:
+        stats = torch.empty((3 if tail else 2, N), dtype=torch.float32, device=logits.device)
+        if weight is not None and out is None:
+            out = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    base = stats.data_ptr()
+    _done(lib().qs_distill(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
+                           teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), base, base + 4 * N,
+                           base + 8 * N if tail else None, w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _ptr(status),
+                           st), "qs_distill")
+    parts = stats.unbind(0)
+    return Distill(parts[0], parts[1], parts[2] if tail else None, out)
+
+
+def distill_grad(logits, ids, teacher, lse, weight, scale=1.0, teacher_scale=1.0, tail=False, log_tail=None, out=None, status=None,
+                 stream=None):
+    """Gradient of sum(weight * loss) on its own (qs_distill_grad), from what distill returned."""
+    _on(logits, ids, teacher, lse, log_tail, out, status)
+    N, V, step = _logits(logits)
+    K = _entries(ids, teacher, N)
+    _vector(lse, N, "lse")
+    if tail and log_tail is None:
+        raise ValueError("tail needs log_tail")
+    _vector(log_tail, N, "log_tail")
+    if isinstance(weight, torch.Tensor):
+        _on(logits, weight)
+    w, w_all = _weights(weight, N, "weight")
+    st, where = _stream(stream)
+    with where:
+        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    _done(lib().qs_distill_grad(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
+                                teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), lse.data_ptr(), _ptr(log_tail),
+                                w, w_all, out.data_ptr(), _gradient(logits, out), _ptr(status), st), "qs_distill_grad")
+    return out
