@@ -1,5 +1,6 @@
 // Shared pieces of the language-model operators: element types, token ids, warp and block sums.
 #pragma once
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cuda_bf16.h>

@@ -364,6 +364,24 @@ def test_token_logp_gradient(N, V, type_, ids):
     _near_logp_grad(same, z, tok, 1.3, gl, torch.zeros(N))
 
 
+@pytest.mark.parametrize("type_,V", [(F32, 131073), (F32, 262200), (BF16, 262145), (F16, 300007)])
+def test_rows_beyond_the_registers_of_a_cluster(type_, V):
+    N, K = 2, 40
+    g = gen(V)
+    z = _logits("plain", N, V, type_, g)
+    z[1, V - 3000:] = z[1, 0] + 20.0             # ties that defeat the bound, in the last block
+    tok = torch.tensor([V - 1, 0])
+    zd = z.cuda()
+    _check_logp(zd, z, tok, 1.0, K)
+    ids, w = torch.randperm(V, generator=g)[: 2 * K].view(N, K).contiguous(), torch.rand(N, generator=g)
+    for tail in (False, True):
+        u = torch.log_softmax(torch.randn((N, K), generator=g), 1) - 0.3
+        got = lm().distill(zd, ids.cuda(), u.cuda(), tail=tail, weight=w.cuda())
+        _near_distill(got, z, ids, u, 1.0, 1.0, tail, w)
+        place = zd.clone()
+        assert torch.equal(lm().distill(place, ids.cuda(), u.cuda(), tail=tail, weight=w.cuda(), out=place).grad, got.grad)
+
+
 @pytest.mark.parametrize("kind", ["masked", "equal", "few"])
 @pytest.mark.parametrize("type_", [F32, BF16])
 def test_token_logp_gradient_under_masks(kind, type_):
