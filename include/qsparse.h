@@ -407,7 +407,7 @@ enum { QS_I32 = 0, QS_I64 = 1 };
  *   table + r * worker_stride is worker r's table (0: all workers read one), rows row_stride >= D
  *   apart; out: R N rows, out_stride >= D apart.
  *   A negative token gives a row of zeros, one >= V a row of NaN.
- * R N, V, D <= 2^30, else QS_TOO_LARGE.
+ * R N, V, D <= 2^30 and R N D <= 2^41, else QS_TOO_LARGE.
  */
 int qs_embed(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int token_type,
              const void* table, int table_type, int64_t worker_stride, int64_t row_stride,

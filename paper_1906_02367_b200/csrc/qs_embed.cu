@@ -4,14 +4,50 @@
 //   gradient   grad[r][v, :] = scale * sum over the places n with tok[r, n] = v of g[r, n, :]
 //
 // for R workers at once, each with its own table (a stretch of its row of the R x d batch) or a
-// shared one.  The gradient is formed without atomic additions: the places are sorted by token
-// (stable, so equal tokens stay in the order of their places) and each run is summed in that order.
+// shared one.  Both are bound by memory: the forward pass by the rows it reads and writes, the
+// gradient by g and by the whole table that it writes, most of it zeros.
+//
+// The gradient is formed without atomic additions.  The places are sorted by token (a stable radix
+// sort, so equal tokens stay in the order of their places), the sorted list is cut into chunks of
+// equal length whatever the lengths of the runs, and a warp sums a chunk's runs for 256 columns.  A
+// run that crosses chunks (a frequent token's) leaves one partial sum per chunk, and these are
+// joined in order.  The rows that no token names are known after the first look at the tokens (a bit
+// per row), so they are set to zero by blocks that run beside the sort's, which is bound by latency.
 #include "qs_lm.cuh"
 
 namespace {
 
 using namespace qs;
 
+constexpr int COLS = 256;                  // columns a warp handles at a time, 8 per lane
+
+// columns of lane `lane` in a 256-column tile: WIDE, 16 bytes at a time (8 of a 2-byte type side by side, twice 4 of a
+// 4-byte type); else 32 apart, so that a warp's single-element accesses lie side by side
+template <int SIZE, bool WIDE>
+__device__ __forceinline__ int col_of(int lane, int j) {
+    if (!WIDE) return lane + 32 * j;
+    return SIZE == 2 ? lane * 8 + j : (j >> 2) * 128 + lane * 4 + (j & 3);
+}
+
+__device__ __forceinline__ void widen(const uint4& q, float* f, __nv_bfloat16) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void widen(const uint4& q, float* f, __half) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        f[2 * i] = p.x;
+        f[2 * i + 1] = p.y;
+    }
+}
+
+// ------------------------------------------------------------------ forward
 struct EmbedArgs {
     long long N, V, D;
     Ids tok;
@@ -22,32 +58,127 @@ struct EmbedArgs {
     long long out_stride;
     int* status;
     long long rows;                        // R x N
+    uint32_t units;                        // 8-column units per row (wide), 256-column tiles per row (else)
 };
 
+// where a place's row comes from; null: it names none
+template <class TW>
+__device__ __forceinline__ const TW* source_row(const EmbedArgs& a, long long row, long long t) {
+    const long long r = a.rows == a.N ? 0 : row / a.N;
+    return t >= 0 && t < a.V ? static_cast<const TW*>(a.table) + r * a.worker_stride + t * a.row_stride : nullptr;
+}
+
+template <class T> struct Eight {              // eight neighbours of a type
+    uint4 q[sizeof(T) / 2];
+};
+template <class T> __device__ __forceinline__ void eight_to_float(const Eight<T>& e, float* f) { widen(e.q[0], f, T()); }
+template <> __device__ __forceinline__ void eight_to_float<float>(const Eight<float>& e, float* f) {
+    const uint32_t w[8] = {e.q[0].x, e.q[0].y, e.q[0].z, e.q[0].w, e.q[1].x, e.q[1].y, e.q[1].z, e.q[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ uint32_t two(float a, float b, __nv_bfloat16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t two(float a, float b, __half) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <class T> __device__ __forceinline__ void store_eight(T* p, const float* f) {
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(two(f[0], f[1], T()), two(f[2], f[3], T()), two(f[4], f[5], T()), two(f[6], f[7], T())));
+}
+template <> __device__ __forceinline__ void store_eight<float>(float* p, const float* f) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(f[0], f[1], f[2], f[3]));
+    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
+}
+
+constexpr int UNITS = 4;                       // units per thread, their loads in flight together
+
+// rows 16-byte aligned on both sides
 template <class TW, class TO>
-__global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
-    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const long long r = row / a.N, t = a.tok.at(row);
-        TO* out = static_cast<TO*>(a.out) + row * a.out_stride;
-        const bool named = t >= 0 && t < a.V;
-        if (t >= a.V && threadIdx.x == 0) flag_status(a.status, QS_INVALID_ARG);
-        const TW* src = static_cast<const TW*>(a.table) + r * a.worker_stride + (named ? t : 0) * a.row_stride;
-        const float other = t < 0 ? 0.0f : quiet_nan();
-        for (long long i = threadIdx.x; i < a.D; i += 256)
-            out[i] = from_float<TO>(named ? a.scale * to_float(src[i]) : other);
+__global__ void __launch_bounds__(256) embed_wide_kernel(const EmbedArgs a) {
+    const unsigned long long total = (unsigned long long)a.rows * a.units, first = (unsigned long long)blockIdx.x * (256 * UNITS) + threadIdx.x;
+    long long row[UNITS], col[UNITS], t[UNITS];
+    Eight<TW> e[UNITS];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        const unsigned long long id = first + 256 * i;
+        row[i] = -1;
+        if (id >= total) continue;
+        // (a 64-bit division costs several 32-bit ones)
+        row[i] = total >> 32 ? (long long)(id / a.units) : (long long)((uint32_t)id / a.units);
+        col[i] = (long long)(id - (unsigned long long)row[i] * a.units) * 8;
+        t[i] = a.tok.at(row[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        if (row[i] < 0) continue;
+        const TW* src = source_row<TW>(a, row[i], t[i]);
+        if (src && col[i] + 8 <= a.D) {
+            const uint4* p = reinterpret_cast<const uint4*>(src + col[i]);
+#pragma unroll
+            for (int w = 0; w < (int)sizeof(TW) / 2; ++w) e[i].q[w] = __ldg(p + w);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+        if (row[i] < 0) continue;
+        TO* out = static_cast<TO*>(a.out) + row[i] * a.out_stride + col[i];
+        const TW* src = source_row<TW>(a, row[i], t[i]);
+        const float none = t[i] < 0 ? 0.0f : quiet_nan();
+        if (t[i] >= a.V && col[i] == 0) flag_status(a.status, QS_INVALID_ARG);
+        if (col[i] + 8 <= a.D) {
+            float f[8];
+            eight_to_float<TW>(e[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = src ? f[j] * a.scale : none;
+            store_eight<TO>(out, f);
+        } else {
+            for (int j = 0; j < (int)(a.D - col[i]); ++j) out[j] = from_float<TO>(src ? to_float(src[col[i] + j]) * a.scale : none);
+        }
     }
 }
 
-template <class TW>
-void launch_embed_to(const EmbedArgs& a, int out_type, int grid, cudaStream_t st) {
-    if (out_type == QS_F32) embed_kernel<TW, float><<<grid, 256, 0, st>>>(a);
-    else if (out_type == QS_BF16) embed_kernel<TW, __nv_bfloat16><<<grid, 256, 0, st>>>(a);
-    else embed_kernel<TW, __half><<<grid, 256, 0, st>>>(a);
+// rows of any alignment: a warp per row and 256 columns
+template <class TW, class TO>
+__global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
+    const int lane = threadIdx.x & 31;
+    const unsigned long long total = (unsigned long long)a.rows * a.units, id = (unsigned long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (id >= total) return;
+    const long long row = (long long)(id / a.units), c0 = (long long)(id - (unsigned long long)row * a.units) * COLS, t = a.tok.at(row);
+    const TW* src = source_row<TW>(a, row, t);
+    const float none = t < 0 ? 0.0f : quiet_nan();
+    if (t >= a.V && c0 == 0 && lane == 0) flag_status(a.status, QS_INVALID_ARG);
+    TO* out = static_cast<TO*>(a.out) + row * a.out_stride;
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const long long c = c0 + lane + 32 * j;
+        f[j] = c < a.D && src ? to_float(src[c]) * a.scale : none;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const long long c = c0 + lane + 32 * j;
+        if (c < a.D) out[c] = from_float<TO>(f[j]);
+    }
+}
+
+template <class TW, class TO>
+void launch_embed(EmbedArgs a, bool wide, cudaStream_t st) {
+    const long long per = wide ? 256 * UNITS : 8;
+    a.units = (uint32_t)((a.D + (wide ? 7 : COLS - 1)) / (wide ? 8 : COLS));
+    const unsigned grid = (unsigned)((a.rows * a.units + per - 1) / per);
+    if (wide) embed_wide_kernel<TW, TO><<<grid, 256, 0, st>>>(a);
+    else embed_kernel<TW, TO><<<grid, 256, 0, st>>>(a);
 }
 
 // ------------------------------------------------------------------ gradient: sort by token
-constexpr int SORT_TILE = 1024;            // places per block, one per thread
+constexpr int SORT_THREADS = 1024;
 constexpr int SORT_MAX_BITS = 9;
+constexpr int SORT_MAX_ITEMS = 8;          // places per thread and tile
+constexpr int ONE_TILE = 4096;             // places per worker that one block sorts in its shared memory
+constexpr int WARPS = SORT_THREADS / 32;
 
 struct GradArgs {
     int R;
@@ -60,11 +191,17 @@ struct GradArgs {
     float* grad;
     long long worker_stride, row_stride;
     int* status;
-    // workspace: keys and places, two of each (R x N), and the digit counts (R x bins x tiles)
-    uint32_t* key[2];
+    // workspace
+    uint32_t* key[2];                      // sorted tokens and their places, two of each for the passes
     uint32_t* pos[2];
-    uint32_t* count;
-    int tiles, bits;                       // tiles per worker, bits per digit
+    uint32_t* count[4];                    // per pass: R x tiles x bins
+    uint32_t* named;                       // R x ceil(V / 32): a bit per row that some token names
+    uint32_t* joins;                       // [0] runs that cross chunks, then the chunk each of them starts in
+    float* part;                           // R x chunks x 2 x padded D: partial sums of such runs
+    int passes, bits, tiles, items, tile;  // bits per digit, tiles per worker, places per thread, places per tile
+    int chunk, chunks;                     // places per chunk, chunks per worker
+    int col_tiles;
+    int side;                              // where the sorted list ends up
 };
 
 __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
@@ -72,100 +209,391 @@ __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
     if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
     return (uint32_t)(t < 0 || t >= a.V ? a.V : t);      // places that name no row sort behind all rows
 }
+__device__ __forceinline__ void mark_row(const GradArgs& a, int r, uint32_t k) {
+    if (k >= a.V) return;
+    uint32_t* w = a.named + (long long)r * ((a.V + 31) / 32) + (k >> 5);
+    const uint32_t bit = 1u << (k & 31);
+    if (!(*w & bit)) atomicOr(w, bit);                   // frequent tokens find their bit set
+}
 
-__global__ void __launch_bounds__(SORT_TILE) digit_count_kernel(const GradArgs a, int pass) {
+// Rows that no token names, part `part` of `parts` of them, by `blocks` blocks of which this is number `block`: a warp
+// takes 32 rows at a time and writes those whose bit is 0
+__device__ void zero_rows(const GradArgs& a, int part, int parts, long long block, long long blocks) {
+    const int lane = threadIdx.x & 31;
+    const long long words = (a.V + 31) / 32, all = words * a.R, lo = all * part / parts, hi = all * (part + 1) / parts;
+    const long long warps = blocks * (blockDim.x >> 5);
+    for (long long w = lo + block * (blockDim.x >> 5) + (threadIdx.x >> 5); w < hi; w += warps) {
+        const long long r = w / words, v0 = (w - r * words) * 32;
+        uint32_t left = ~a.named[w];
+        if (a.V - v0 < 32) left &= (1u << (a.V - v0)) - 1u;
+        while (left) {
+            const int b = __ffs(left) - 1;
+            left &= left - 1;
+            float* dst = a.grad + r * a.worker_stride + (v0 + b) * a.row_stride;
+            const long long head = min((long long)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / 4, a.D);
+            const long long quads = (a.D - head) / 4, tail = head + quads * 4;
+            if (lane < head) dst[lane] = 0.0f;
+            float4* p = reinterpret_cast<float4*>(dst + head);
+            for (long long i = lane; i < quads; i += 32) __stcs(p + i, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+            if (tail + lane < a.D) dst[tail + lane] = 0.0f;
+        }
+    }
+}
+
+// counts of the first digit per tile; which rows are named
+__global__ void __launch_bounds__(SORT_THREADS) sort_count_kernel(const GradArgs a) {
     __shared__ uint32_t hist[1 << SORT_MAX_BITS];
     const int r = blockIdx.y, bins = 1 << a.bits;
-    for (int b = threadIdx.x; b < bins; b += SORT_TILE) hist[b] = 0;
+    for (int b = threadIdx.x; b < bins; b += SORT_THREADS) hist[b] = 0;
     __syncthreads();
-    const long long n = (long long)blockIdx.x * SORT_TILE + threadIdx.x;
-    if (n < a.N) {
-        const uint32_t k = pass == 0 ? key_of(a, r * a.N + n) : a.key[pass & 1][r * a.N + n];
-        atomicAdd(&hist[(k >> (pass * a.bits)) & (bins - 1)], 1u);
+    for (int i = 0; i < a.items; ++i) {
+        const long long n = (long long)blockIdx.x * a.tile + i * SORT_THREADS + threadIdx.x;
+        if (n >= a.N) break;
+        const uint32_t k = key_of(a, r * a.N + n);
+        atomicAdd(&hist[k & (bins - 1)], 1u);
+        if (!a.accumulate) mark_row(a, r, k);
     }
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += SORT_TILE) a.count[((long long)r * bins + b) * a.tiles + blockIdx.x] = hist[b];
+    uint32_t* out = a.count[0] + ((long long)r * a.tiles + blockIdx.x) * bins;
+    for (int b = threadIdx.x; b < bins; b += SORT_THREADS) out[b] = hist[b];
 }
 
-// exclusive sums over (digit, tile), one block per worker
-__global__ void __launch_bounds__(1024) digit_scan_kernel(const GradArgs a) {
-    __shared__ uint32_t part[1024];
-    const long long len = (long long)(1 << a.bits) * a.tiles;
-    uint32_t* c = a.count + blockIdx.x * len;
-    const long long per = (len + 1023) / 1024, lo = threadIdx.x * per, hi = lo + per < len ? lo + per : len;
-    uint32_t sum = 0;
-    for (long long i = lo; i < hi; ++i) sum += c[i];
-    part[threadIdx.x] = sum;
+struct SortShared {
+    uint16_t warp_count[WARPS << SORT_MAX_BITS];
+    uint32_t base[1 << SORT_MAX_BITS], total[1 << SORT_MAX_BITS];
+    uint32_t sums[WARPS];
+};
+
+// exclusive sums of v over the block's threads
+__device__ uint32_t block_scan(uint32_t v, uint32_t* sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(~0u, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) sums[warp] = x;
     __syncthreads();
-    for (int o = 1; o < 1024; o <<= 1) {
-        const uint32_t v = threadIdx.x >= o ? part[threadIdx.x - o] : 0u;
-        __syncthreads();
-        part[threadIdx.x] += v;
-        __syncthreads();
+    if (warp == 0) {
+        uint32_t s = lane < WARPS ? sums[lane] : 0u;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t y = __shfl_up_sync(~0u, s, o);
+            if (lane >= o) s += y;
+        }
+        if (lane < WARPS) sums[lane] = s;
     }
-    uint32_t run = threadIdx.x ? part[threadIdx.x - 1] : 0u;
-    for (long long i = lo; i < hi; ++i) {
-        const uint32_t v = c[i];
-        c[i] = run;
-        run += v;
-    }
+    __syncthreads();
+    return x - v + (warp ? sums[warp - 1] : 0u);
 }
 
-__global__ void __launch_bounds__(SORT_TILE) digit_scatter_kernel(const GradArgs a, int pass) {
-    extern __shared__ uint16_t warp_count[];             // 32 x bins
-    const int r = blockIdx.y, bins = 1 << a.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int b = threadIdx.x; b < 32 * bins; b += SORT_TILE) warp_count[b] = 0;
+// Rank of this thread's element among the block's elements of digit d (bins: none), in thread order, past what base
+// says; base then moves on past the block's elements
+__device__ uint32_t stable_place(SortShared& s, uint32_t d, int bins) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int b = threadIdx.x; b < WARPS * bins / 2; b += SORT_THREADS) reinterpret_cast<uint32_t*>(s.warp_count)[b] = 0;
     __syncthreads();
-    const long long n = (long long)blockIdx.x * SORT_TILE + threadIdx.x;
-    const bool in = n < a.N;
-    uint32_t k = 0, p = 0, d = (uint32_t)bins;
-    if (in) {
-        k = pass == 0 ? key_of(a, r * a.N + n) : a.key[pass & 1][r * a.N + n];
-        p = pass == 0 ? (uint32_t)n : a.pos[pass & 1][r * a.N + n];
-        d = (k >> (pass * a.bits)) & (bins - 1);
-    }
     const uint32_t same = __match_any_sync(0xffffffffu, d);
     const int rank = __popc(same & ((1u << lane) - 1u));
-    if (in && rank == 0) warp_count[warp * bins + d] = (uint16_t)__popc(same);
+    if (d < (uint32_t)bins && rank == 0) s.warp_count[warp * bins + d] = (uint16_t)__popc(same);
     __syncthreads();
-    for (int b = threadIdx.x; b < bins; b += SORT_TILE) {
+    for (int b = threadIdx.x; b < bins; b += SORT_THREADS) {
         uint32_t run = 0;
-        for (int w = 0; w < 32; ++w) {
-            const uint32_t v = warp_count[w * bins + b];
-            warp_count[w * bins + b] = (uint16_t)run;
+        for (int w = 0; w < WARPS; ++w) {
+            const uint32_t v = s.warp_count[w * bins + b];
+            s.warp_count[w * bins + b] = (uint16_t)run;
             run += v;
         }
+        s.total[b] = run;
     }
     __syncthreads();
-    if (in) {
-        const uint32_t to = a.count[((long long)r * bins + d) * a.tiles + blockIdx.x] + warp_count[warp * bins + d] + rank;
-        a.key[(pass + 1) & 1][r * a.N + to] = k;
-        a.pos[(pass + 1) & 1][r * a.N + to] = p;
-    }
+    const uint32_t to = d < (uint32_t)bins ? s.base[d] + s.warp_count[warp * bins + d] + rank : 0u;
+    __syncthreads();
+    for (int b = threadIdx.x; b < bins; b += SORT_THREADS) s.base[b] += s.total[b];
+    return to;
 }
 
-__global__ void __launch_bounds__(256) zero_rows_kernel(const GradArgs a) {
-    for (long long row = blockIdx.x; row < a.R * a.V; row += gridDim.x) {
-        float* dst = a.grad + (row / a.V) * a.worker_stride + (row % a.V) * a.row_stride;
-        for (long long i = threadIdx.x; i < a.D; i += 256) dst[i] = 0.0f;
+// One pass of the sort: blocks [0, R x tiles) scatter a tile each, the others set rows to zero meanwhile
+__global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const GradArgs a, int pass) {
+    __shared__ SortShared s;
+    const int sorters = a.R * a.tiles;
+    if ((int)blockIdx.x >= sorters) {
+        zero_rows(a, pass, a.passes, blockIdx.x - sorters, gridDim.x - sorters);
+        return;
     }
-}
-
-// one block per place of the sorted list; the first place of a run sums the whole run
-template <class TG>
-__global__ void __launch_bounds__(256) run_sum_kernel(const GradArgs a, int side) {
-    for (long long i = blockIdx.x; i < a.R * a.N; i += gridDim.x) {
-        const long long r = i / a.N, first = r * a.N, end = first + a.N;
-        const uint32_t k = a.key[side][i];
-        if (k >= a.V || (i > first && a.key[side][i - 1] == k)) continue;
-        float* dst = a.grad + r * a.worker_stride + (long long)k * a.row_stride;
-        for (long long c = threadIdx.x; c < a.D; c += 256) {
-            float sum = 0.0f;
-            for (long long j = i; j < end && a.key[side][j] == k; ++j)
-                sum += to_float(static_cast<const TG*>(a.g)[(first + a.pos[side][j]) * a.g_stride + c]);
-            dst[c] = a.accumulate ? fmaf(a.scale, sum, dst[c]) : a.scale * sum;
+    const int r = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, bins = 1 << a.bits, shift = pass * a.bits;
+    const uint32_t* count = a.count[pass] + (long long)r * a.tiles * bins;
+    // places before this tile's elements of a digit: all smaller digits, and the same digit in earlier tiles
+    uint32_t all = 0, before = 0;
+    if ((int)threadIdx.x < bins) {
+#pragma unroll 8
+        for (int i = 0; i < a.tiles; ++i) {
+            const uint32_t c = count[(long long)i * bins + threadIdx.x];
+            all += c;
+            before += i < tile ? c : 0u;
         }
     }
+    const uint32_t smaller = block_scan(all, s.sums);
+    if ((int)threadIdx.x < bins) s.base[threadIdx.x] = smaller + before;
+    const uint32_t* key = a.key[pass & 1] + r * a.N;
+    const uint32_t* pos = a.pos[pass & 1] + r * a.N;
+    uint32_t* key_to = a.key[(pass + 1) & 1] + r * a.N;
+    uint32_t* pos_to = a.pos[(pass + 1) & 1] + r * a.N;
+    for (int i = 0; i < a.items; ++i) {
+        const long long n = (long long)tile * a.tile + i * SORT_THREADS + threadIdx.x;
+        const bool in = n < a.N;
+        uint32_t k = 0, p = 0;
+        if (in) {
+            k = pass == 0 ? key_of(a, r * a.N + n) : key[n];
+            p = pass == 0 ? (uint32_t)n : pos[n];
+        }
+        const uint32_t to = stable_place(s, in ? (k >> shift) & (bins - 1) : (uint32_t)bins, bins);
+        if (!in) continue;
+        key_to[to] = k;
+        pos_to[to] = p;
+        if (pass + 1 < a.passes)
+            atomicAdd(a.count[pass + 1] + ((long long)r * a.tiles + to / a.tile) * bins + ((k >> (shift + a.bits)) & (bins - 1)), 1u);
+    }
+}
+
+// A worker's whole sort in one block
+__global__ void __launch_bounds__(SORT_THREADS) sort_one_tile_kernel(const GradArgs a) {
+    extern __shared__ __align__(16) uint32_t list[];     // keys, places, twice
+    __shared__ SortShared s;
+    const int r = blockIdx.x, bins = 1 << a.bits, n = (int)a.N;
+    uint32_t* key[2] = {list, list + 2 * n};
+    uint32_t* pos[2] = {list + n, list + 3 * n};
+    for (int i = threadIdx.x; i < n; i += SORT_THREADS) {
+        const uint32_t k = key_of(a, r * a.N + i);
+        key[0][i] = k;
+        pos[0][i] = i;
+        if (!a.accumulate) mark_row(a, r, k);
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int from = pass & 1, shift = pass * a.bits;
+        for (int b = threadIdx.x; b < bins; b += SORT_THREADS) s.total[b] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += SORT_THREADS) atomicAdd(&s.total[(key[from][i] >> shift) & (bins - 1)], 1u);
+        __syncthreads();
+        const uint32_t base = block_scan((int)threadIdx.x < bins ? s.total[threadIdx.x] : 0u, s.sums);
+        if ((int)threadIdx.x < bins) s.base[threadIdx.x] = base;
+        for (int i0 = 0; i0 < n; i0 += SORT_THREADS) {
+            const int i = i0 + threadIdx.x;
+            const uint32_t k = i < n ? key[from][i] : 0u, p = i < n ? pos[from][i] : 0u;
+            const uint32_t to = stable_place(s, i < n ? (k >> shift) & (bins - 1) : (uint32_t)bins, bins);
+            if (i < n) {
+                key[from ^ 1][to] = k;
+                pos[from ^ 1][to] = p;
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += SORT_THREADS) {
+        a.key[a.side][r * a.N + i] = key[a.passes & 1][i];
+        a.pos[a.side][r * a.N + i] = pos[a.passes & 1][i];
+    }
+}
+
+// ------------------------------------------------------------------ gradient: sums of the runs
+template <bool WIDE, int SIZE>
+__device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0, const float (&sum)[8]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int c = c0 + col_of<SIZE, WIDE>(lane, 4 * h);
+        if (WIDE && c + 4 <= a.D) {
+            float4* p = reinterpret_cast<float4*>(dst + c);
+            float4 v = make_float4(a.scale * sum[4 * h], a.scale * sum[4 * h + 1], a.scale * sum[4 * h + 2], a.scale * sum[4 * h + 3]);
+            if (a.accumulate) {
+                const float4 o = *p;
+                v = make_float4(fmaf(a.scale, sum[4 * h], o.x), fmaf(a.scale, sum[4 * h + 1], o.y), fmaf(a.scale, sum[4 * h + 2], o.z),
+                                fmaf(a.scale, sum[4 * h + 3], o.w));
+            }
+            __stcs(p, v);
+        } else {
+#pragma unroll
+            for (int j = 4 * h; j < 4 * h + 4; ++j) {
+                const int x = c0 + col_of<SIZE, WIDE>(lane, j);
+                if (x < a.D) dst[x] = a.accumulate ? fmaf(a.scale, sum[j], dst[x]) : a.scale * sum[j];
+            }
+        }
+    }
+}
+
+template <class T, bool WIDE>
+struct Piece {                             // a lane's 8 columns of one row of g
+    uint4 q[sizeof(T) / 2];
+    float f[WIDE ? 1 : 8];
+
+    __device__ __forceinline__ void load(const GradArgs& a, const T* row, int c0, bool on) {
+        const int lane = threadIdx.x & 31;
+        if (WIDE) {
+            constexpr int E = 16 / sizeof(T);
+#pragma unroll
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+                const int c = c0 + col_of<sizeof(T), true>(lane, h * E);
+                q[h] = make_uint4(0, 0, 0, 0);
+                if (on && c + E <= a.D) q[h] = __ldcs(reinterpret_cast<const uint4*>(row + c));
+                else if (on && c < a.D) {                  // the last columns
+                    uint32_t* w = &q[h].x;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        if (c + j >= a.D) continue;
+                        if (sizeof(T) == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[c + j];
+                        else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[c + j] << (16 * (j & 1));
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = c0 + lane + 32 * j;
+                f[WIDE ? 0 : j] = on && c < a.D ? to_float(row[c]) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
+        if (WIDE) {
+            float x[8];
+            if (sizeof(T) == 4) {
+                const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[sizeof(T) / 2 - 1].x, q[sizeof(T) / 2 - 1].y, q[sizeof(T) / 2 - 1].z, q[sizeof(T) / 2 - 1].w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+            } else {
+                widen_if(x);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += x[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += f[WIDE ? 0 : j];
+        }
+    }
+    __device__ __forceinline__ void widen_if(float* x) const;
+};
+template <class T, bool WIDE> __device__ __forceinline__ void Piece<T, WIDE>::widen_if(float* x) const { widen(q[0], x, T()); }
+template <> __device__ __forceinline__ void Piece<float, true>::widen_if(float*) const {}
+template <> __device__ __forceinline__ void Piece<float, false>::widen_if(float*) const {}
+
+// A warp per chunk and 256 columns; blocks past those set rows to zero (one-tile sorts: nothing ran beside them)
+template <class T, bool WIDE>
+__global__ void __launch_bounds__(256) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
+    constexpr int AHEAD = sizeof(T) == 4 && WIDE ? 4 : 8;          // rows in flight
+    if (blockIdx.x >= sum_blocks) {
+        zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    const long long id = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (id >= (long long)a.R * a.chunks * a.col_tiles) return;
+    const long long ch = id / a.col_tiles;
+    const int c0 = (int)(id - ch * a.col_tiles) * COLS;
+    const long long r = ch / a.chunks, i0 = (ch - r * a.chunks) * a.chunk;
+    const int n = (int)min((long long)a.chunk, a.N - i0);
+    const uint32_t* key = a.key[a.side] + r * a.N + i0;
+    const uint32_t* pos = a.pos[a.side] + r * a.N + i0;
+    const T* g = static_cast<const T*>(a.g) + r * a.N * a.g_stride;
+    const uint32_t none = 0xffffffffu, V = (uint32_t)a.V;
+    const uint32_t prev = i0 > 0 ? key[-1] : none, next = i0 + n < a.N ? key[n] : none;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    uint32_t cur = key[0];
+    bool first = true;
+    auto flush = [&](bool last) {
+        if (cur >= V) return;
+        const bool from = first && cur == prev, on = last && cur == next;
+        if (!from && !on) {
+            write_sum<WIDE, sizeof(T)>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+        } else {                                   // part of a run that crosses chunks
+            float* p = a.part + (ch * 2 + (from ? 0 : 1)) * ((long long)a.col_tiles * COLS) + c0 + lane * 8;
+            reinterpret_cast<float4*>(p)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            if (!from && c0 == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1u)] = (uint32_t)ch;
+        }
+    };
+    for (int b = 0; b < n; b += 32) {
+        const int left = min(32, n - b);
+        const uint32_t k = lane < left ? key[b + lane] : none, p = lane < left ? pos[b + lane] : 0u;
+        if (__all_sync(~0u, k >= V) && cur >= V) break;            // only places that name no row are left
+        for (int i = 0; i < left; i += AHEAD) {
+            Piece<T, WIDE> row[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31), pu = __shfl_sync(~0u, p, (i + u) & 31);
+                row[u].load(a, g + (long long)pu * a.g_stride, c0, i + u < left && ku < V);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31);
+                if (i + u < left) {
+                    if (ku != cur) {
+                        flush(false);
+                        first = false;
+                        cur = ku;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+                    }
+                    row[u].add_to(sum);
+                }
+            }
+        }
+    }
+    flush(true);
+}
+
+// Runs that cross chunks: a block per run and 256 columns adds the partial sums in order, each warp a stretch of them
+template <int SIZE, bool WIDE>
+__global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
+    __shared__ float sums[8][COLS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long all = (long long)a.joins[0] * a.col_tiles, width = (long long)a.col_tiles * COLS;
+    for (long long id = blockIdx.x; id < all; id += gridDim.x) {
+        const long long at = id / a.col_tiles;
+        const int c0 = (int)(id - at * a.col_tiles) * COLS;
+        const long long ch = a.joins[1 + at], r = ch / a.chunks, c = ch - r * a.chunks;
+        const uint32_t* key = a.key[a.side] + r * a.N;
+        const uint32_t cur = key[(c + 1) * a.chunk - 1];
+        long long m = 0;                           // chunks the run goes on in
+        for (;;) {
+            const long long j = c + 1 + m + lane;
+            const uint32_t same = __ballot_sync(~0u, j < a.chunks && key[j * a.chunk] == cur);
+            m += same == ~0u ? 32 : __ffs(~same) - 1;
+            if (same != ~0u) break;
+        }
+        const long long per = (m + 1 + 7) / 8, lo = warp * per, hi = min(lo + per, m + 1);
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+#pragma unroll 4
+        for (long long i = lo; i < hi; ++i) {      // the run's first chunk left its sum in slot 1, the others in slot 0
+            const float4* p = reinterpret_cast<const float4*>(a.part + ((ch + i) * 2 + (i == 0)) * width + c0 + lane * 8);
+            const float4 x = p[0], y = p[1];
+            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+            sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = sum[j];
+        __syncthreads();
+        if (warp == 0) {
+            for (int w = 1; w < 8; ++w)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += sums[w][lane + 32 * j];
+            write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+        }
+    }
+}
+
+// rows of zeros alone (no tokens)
+__global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_rows(a, 0, 1, blockIdx.x, gridDim.x); }
+
+template <class T, bool WIDE>
+void launch_sums(const GradArgs& a, bool zero_here, int sms, cudaStream_t st) {
+    const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + 7) / 8);
+    run_sum_kernel<T, WIDE><<<sum_blocks + (zero_here ? sms * 4 : 0), 256, 0, st>>>(a, sum_blocks);
+    run_join_kernel<sizeof(T), WIDE><<<sms * 4, 256, 0, st>>>(a);
 }
 
 int bits_for(long long v) {
@@ -174,23 +602,51 @@ int bits_for(long long v) {
     return b;
 }
 
+// Sizes and the places of the workspace's parts, in 32-bit words
 struct SortPlan {
-    int passes, bits, tiles;
-    int64_t words;
+    int passes, bits, tiles, items, chunk, chunks, col_tiles;
+    bool one_tile;
+    int64_t count, named, joins, zeroed, part, words;    // first words; [count, zeroed) starts at zero
 };
-SortPlan sort_plan(int R, int64_t N, int64_t V) {
+SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     SortPlan s;
     const int total = bits_for(V + 1);                   // keys 0 .. V
     s.passes = (total + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
     s.bits = (total + s.passes - 1) / s.passes;
-    s.tiles = (int)((N + SORT_TILE - 1) / SORT_TILE);
-    s.words = 4 * (int64_t)R * N + (int64_t)R * (1 << s.bits) * s.tiles;
+    s.one_tile = N <= ONE_TILE;
+    s.items = 1;                                         // tiles of 1024 places while 64 of them cover the list: every block reads all tiles' counts
+    while (s.items < SORT_MAX_ITEMS && N > 64ll * SORT_THREADS * s.items) s.items *= 2;
+    const int64_t tile = (int64_t)s.items * SORT_THREADS;
+    s.tiles = (int)((N + tile - 1) / tile);
+    s.col_tiles = (int)((D + COLS - 1) / COLS);
+    // chunks as long as 128 places while they give every SM some 16 warps
+    s.chunk = 16;
+    while (s.chunk < 128 && R * N / (2 * s.chunk) * s.col_tiles >= 148 * 16) s.chunk *= 2;
+    s.chunks = (int)((N + s.chunk - 1) / s.chunk);
+    s.count = 4 * R * N;
+    s.named = s.count + (s.one_tile ? 0 : (int64_t)s.passes * R * s.tiles << s.bits);
+    s.joins = s.named + R * ((V + 31) / 32);
+    s.zeroed = s.joins + 1;
+    s.part = (s.zeroed + (int64_t)R * s.chunks + 3) / 4 * 4;
+    s.words = s.part + (int64_t)R * s.chunks * 2 * s.col_tiles * COLS;
     return s;
+}
+
+template <class TW>
+void launch_embed_to(const EmbedArgs& a, int out_type, cudaStream_t st) {
+    const int out_size = out_type == QS_F32 ? 4 : 2, size = (int)sizeof(TW);
+    // 16-byte accesses need every row on a 16-byte boundary
+    const bool wide = aligned_to(a.table, 16) && a.row_stride * size % 16 == 0 && a.worker_stride * size % 16 == 0 && aligned_to(a.out, 16) &&
+                      a.out_stride * out_size % 16 == 0;
+    if (out_type == QS_F32) launch_embed<TW, float>(a, wide, st);
+    else if (out_type == QS_BF16) launch_embed<TW, __nv_bfloat16>(a, wide, st);
+    else launch_embed<TW, __half>(a, wide, st);
 }
 
 bool bad_shape(int R, int64_t N, int64_t V, int64_t D) { return R < 1 || R > 32 || N < 0 || V < 1 || D < 1; }
 bool too_large(int R, int64_t N, int64_t V, int64_t D) {
-    return V > (1ll << 30) || N > (1ll << 30) / R || D > (1ll << 30);
+    // (the last: what a grid can count)
+    return V > (1ll << 30) || N > (1ll << 30) / R || D > (1ll << 30) || R * N * ((D + 255) / 256) > (1ll << 33);
 }
 
 }  // namespace
@@ -206,19 +662,18 @@ int qs_embed(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int tok
     if (N == 0) return QS_OK;
     if (!tokens || !table || !out || !aligned_to(tokens, token_type == QS_I64 ? 8 : 4) || !aligned_to(table, size_of_type(table_type)) ||
         !aligned_to(out, size_of_type(out_type)) || !aligned_to(status, 4)) return QS_INVALID_ARG;
-    EmbedArgs a{N, V, D, Ids{tokens, token_type == QS_I64}, table, worker_stride, row_stride, scale, out, out_stride, status, R * N};
-    const int grid = (int)(a.rows < 65536 ? a.rows : 65536);
+    EmbedArgs a{N, V, D, Ids{tokens, token_type == QS_I64}, table, worker_stride, row_stride, scale, out, out_stride, status, R * N, 0};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (table_type == QS_F32) launch_embed_to<float>(a, out_type, grid, st);
-    else if (table_type == QS_BF16) launch_embed_to<__nv_bfloat16>(a, out_type, grid, st);
-    else launch_embed_to<__half>(a, out_type, grid, st);
+    if (table_type == QS_F32) launch_embed_to<float>(a, out_type, st);
+    else if (table_type == QS_BF16) launch_embed_to<__nv_bfloat16>(a, out_type, st);
+    else launch_embed_to<__half>(a, out_type, st);
     return launch_status();
 }
 
 int64_t qs_embed_grad_bytes(int R, int64_t N, int64_t V, int64_t D) {
     if (bad_shape(R, N, V, D)) return QS_INVALID_ARG;
     if (too_large(R, N, V, D)) return QS_TOO_LARGE;
-    return 4 * sort_plan(R, N, V).words;
+    return 4 * sort_plan(R, N, V, D).words;
 }
 
 int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int token_type, const void* grad_out, int grad_type,
@@ -230,30 +685,53 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     if (grad_stride < D || row_stride < D || (R > 1 && worker_stride < (V - 1) * row_stride + D &&
                                               (worker_stride < D || row_stride < (R - 1) * worker_stride + D))) return QS_INVALID_ARG;
     if (!grad_table || !aligned_to(grad_table, 4) || !aligned_to(status, 4)) return QS_INVALID_ARG;
-    const SortPlan p = sort_plan(R, N, V);
-    if (N > 0 && (!tokens || !grad_out || !work || !aligned_to(tokens, token_type == QS_I64 ? 8 : 4) ||
-                  !aligned_to(grad_out, size_of_type(grad_type)) || !aligned_to(work, 16))) return QS_INVALID_ARG;
+    const SortPlan p = sort_plan(R, N, V, D);
+    if (!work || !aligned_to(work, 16)) return QS_INVALID_ARG;
+    if (N > 0 && (!tokens || !grad_out || !aligned_to(tokens, token_type == QS_I64 ? 8 : 4) || !aligned_to(grad_out, size_of_type(grad_type))))
+        return QS_INVALID_ARG;
     if (work_bytes < 4 * p.words) return QS_CAPACITY;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cudaGetLastError();
+        return QS_CUDA;
+    }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     uint32_t* w = static_cast<uint32_t*>(work);
     const int64_t m = R * N;
-    GradArgs a{R, N, V, D, Ids{tokens, token_type == QS_I64}, grad_out, grad_stride, scale, accumulate, grad_table, worker_stride,
-               row_stride, status, {w, w + m}, {w + 2 * m, w + 3 * m}, w + 4 * m, p.tiles, p.bits};
-    const int64_t rows = R * V;
-    if (!accumulate) zero_rows_kernel<<<(int)(rows < 65536 ? rows : 65536), 256, 0, st>>>(a);
-    if (N > 0) {
-        const dim3 grid(p.tiles, R);
-        const size_t smem = sizeof(uint16_t) * 32 * (1 << p.bits);
-        for (int pass = 0; pass < p.passes; ++pass) {
-            digit_count_kernel<<<grid, SORT_TILE, 0, st>>>(a, pass);
-            digit_scan_kernel<<<R, 1024, 0, st>>>(a);
-            digit_scatter_kernel<<<grid, SORT_TILE, smem, st>>>(a, pass);
-        }
-        const int side = p.passes & 1, blocks = (int)(m < 65536 ? m : 65536);
-        if (grad_type == QS_F32) run_sum_kernel<float><<<blocks, 256, 0, st>>>(a, side);
-        else if (grad_type == QS_BF16) run_sum_kernel<__nv_bfloat16><<<blocks, 256, 0, st>>>(a, side);
-        else run_sum_kernel<__half><<<blocks, 256, 0, st>>>(a, side);
+    GradArgs a{};
+    a.R = R; a.N = N; a.V = V; a.D = D; a.tok = Ids{tokens, token_type == QS_I64};
+    a.g = grad_out; a.g_stride = grad_stride; a.scale = scale; a.accumulate = accumulate; a.grad = grad_table;
+    a.worker_stride = worker_stride; a.row_stride = row_stride; a.status = status;
+    a.key[0] = w; a.key[1] = w + m; a.pos[0] = w + 2 * m; a.pos[1] = w + 3 * m;
+    for (int i = 0; i < p.passes; ++i) a.count[i] = w + p.count + ((int64_t)i * R * p.tiles << p.bits);
+    a.named = w + p.named; a.joins = w + p.joins; a.part = reinterpret_cast<float*>(w + p.part);
+    a.passes = p.passes; a.bits = p.bits; a.tiles = p.tiles; a.items = p.items; a.tile = p.items * SORT_THREADS;
+    a.chunk = p.chunk; a.chunks = p.chunks; a.col_tiles = p.col_tiles; a.side = p.passes & 1;
+    if (N == 0 && accumulate) return QS_OK;
+    if (cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
+    if (N == 0) {
+        zero_all_kernel<<<sms * 8, 256, 0, st>>>(a);
+        return launch_status();
     }
+    if (p.one_tile) {
+        const int smem = (int)(16 * N);
+        if (cudaFuncSetAttribute(sort_one_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16 * ONE_TILE) != cudaSuccess) {
+            cudaGetLastError();
+            return QS_CUDA;
+        }
+        sort_one_tile_kernel<<<R, SORT_THREADS, smem, st>>>(a);
+    } else {
+        sort_count_kernel<<<dim3(p.tiles, R), SORT_THREADS, 0, st>>>(a);
+        for (int pass = 0; pass < p.passes; ++pass)
+            sort_scatter_kernel<<<R * p.tiles + (accumulate ? 0 : 2 * sms), SORT_THREADS, 0, st>>>(a, pass);
+    }
+    const int size = size_of_type(grad_type);
+    const bool zero_here = p.one_tile && !accumulate;
+    // 16-byte accesses need every row on a 16-byte boundary
+    const bool wide = aligned_to(grad_out, 16) && grad_stride * size % 16 == 0 && aligned_to(grad_table, 16) && row_stride % 4 == 0 && worker_stride % 4 == 0;
+    if (grad_type == QS_F32) wide ? launch_sums<float, true>(a, zero_here, sms, st) : launch_sums<float, false>(a, zero_here, sms, st);
+    else if (grad_type == QS_BF16) wide ? launch_sums<__nv_bfloat16, true>(a, zero_here, sms, st) : launch_sums<__nv_bfloat16, false>(a, zero_here, sms, st);
+    else wide ? launch_sums<__half, true>(a, zero_here, sms, st) : launch_sums<__half, false>(a, zero_here, sms, st);
     return launch_status();
 }
 
