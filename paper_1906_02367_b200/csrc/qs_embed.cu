@@ -11,7 +11,7 @@
 // sort, so equal tokens stay in the order of their places), the sorted list is cut into chunks of
 // equal length whatever the lengths of the runs, and a warp sums a chunk's runs for 256 columns.  A
 // run that crosses chunks (a frequent token's) leaves one partial sum per chunk, and these are
-// joined in order.  The rows that no token names are known after the first look at the tokens (a bit
+// joined in order.  The rows that no token names are known after the first look at the tokens (a byte
 // per row), so they are set to zero by blocks that run beside the sort's, which is bound by latency.
 #include "qs_lm.cuh"
 
@@ -177,7 +177,7 @@ void launch_embed(EmbedArgs a, bool wide, cudaStream_t st) {
 constexpr int SORT_THREADS = 1024;
 constexpr int SORT_MAX_BITS = 9;
 constexpr int SORT_MAX_ITEMS = 8;          // places per thread and tile
-constexpr int ONE_TILE = 4096;             // places per worker that one block sorts in its shared memory
+constexpr int ONE_TILE = 1024;             // places per worker that one block sorts in its shared memory
 constexpr int WARPS = SORT_THREADS / 32;
 
 struct GradArgs {
@@ -195,13 +195,15 @@ struct GradArgs {
     uint32_t* key[2];                      // sorted tokens and their places, two of each for the passes
     uint32_t* pos[2];
     uint32_t* count[4];                    // per pass: R x tiles x bins
-    uint32_t* named;                       // R x ceil(V / 32): a bit per row that some token names
+    uint8_t* named;                        // R x padded: 1 for a row that some token names
+    long long padded;                      // V up to a multiple of 32
     uint32_t* joins;                       // [0] runs that cross chunks, then the chunk each of them starts in
     float* part;                           // R x chunks x 2 x padded D: partial sums of such runs
     int passes, bits, tiles, items, tile;  // bits per digit, tiles per worker, places per thread, places per tile
     int chunk, chunks;                     // places per chunk, chunks per worker
     int col_tiles;
     int side;                              // where the sorted list ends up
+    int unit;                              // rows a warp sets to zero at a time
 };
 
 __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
@@ -209,49 +211,65 @@ __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
     if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
     return (uint32_t)(t < 0 || t >= a.V ? a.V : t);      // places that name no row sort behind all rows
 }
+// a byte per row: a plain store, which frequent tokens may repeat (an atomic on a bit made them wait in line: 22 us for
+// 65536 tokens, 6 us this way)
 __device__ __forceinline__ void mark_row(const GradArgs& a, int r, uint32_t k) {
-    if (k >= a.V) return;
-    uint32_t* w = a.named + (long long)r * ((a.V + 31) / 32) + (k >> 5);
-    const uint32_t bit = 1u << (k & 31);
-    if (!(*w & bit)) atomicOr(w, bit);                   // frequent tokens find their bit set
+    if (k < a.V) a.named[r * a.padded + k] = 1;
 }
 
-// Rows that no token names, part `part` of `parts` of them, by `blocks` blocks of which this is number `block`: a warp
-// takes 32 rows at a time and writes those whose bit is 0
-__device__ void zero_rows(const GradArgs& a, int part, int parts, long long block, long long blocks) {
+// `n` floats of zeros, a warp's work; dst on a 4-byte boundary
+__device__ __forceinline__ void warp_zero(float* dst, long long n) {
     const int lane = threadIdx.x & 31;
-    const long long words = (a.V + 31) / 32, all = words * a.R, lo = all * part / parts, hi = all * (part + 1) / parts;
+    const long long head = min((long long)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / 4, n), quads = (n - head) / 4;
+    float4* p = reinterpret_cast<float4*>(dst + head);
+#pragma unroll 4
+    for (long long i = lane; i < quads; i += 32) __stcs(p + i, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+    if (lane < head) dst[lane] = 0.0f;
+    const long long tail = head + quads * 4;
+    if (tail + lane < n) dst[tail + lane] = 0.0f;
+}
+
+// Rows that no token names, part `part` of `parts` of them, by `blocks` blocks of which this is number `block`.  A warp
+// takes `unit` rows at a time (a power of two up to 32, about 8 KB: short enough to spread the work evenly);
+// neighbours without a name are one stretch where rows lie side by side
+__device__ void zero_rows(const GradArgs& a, int part, int parts, long long block, long long blocks) {
+    const int unit = a.unit, lane = threadIdx.x & 31;
+    const long long per = a.padded / unit, all = per * a.R, lo = all * part / parts, hi = all * (part + 1) / parts;
     const long long warps = blocks * (blockDim.x >> 5);
-    for (long long w = lo + block * (blockDim.x >> 5) + (threadIdx.x >> 5); w < hi; w += warps) {
-        const long long r = w / words, v0 = (w - r * words) * 32;
-        uint32_t left = ~a.named[w];
-        if (a.V - v0 < 32) left &= (1u << (a.V - v0)) - 1u;
+    const bool side_by_side = a.row_stride == a.D;
+    for (long long i = lo + block * (blockDim.x >> 5) + (threadIdx.x >> 5); i < hi; i += warps) {
+        const long long r = i / per, v0 = (i - r * per) * unit;
+        uint32_t left = ~__ballot_sync(~0u, lane < unit && a.named[r * a.padded + v0 + lane]);
+        const long long rows = min((long long)unit, a.V - v0);
+        if (rows <= 0) continue;
+        if (rows < 32) left &= (1u << rows) - 1u;
+        float* base = a.grad + r * a.worker_stride + v0 * a.row_stride;
         while (left) {
             const int b = __ffs(left) - 1;
-            left &= left - 1;
-            float* dst = a.grad + r * a.worker_stride + (v0 + b) * a.row_stride;
-            const long long head = min((long long)((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / 4, a.D);
-            const long long quads = (a.D - head) / 4, tail = head + quads * 4;
-            if (lane < head) dst[lane] = 0.0f;
-            float4* p = reinterpret_cast<float4*>(dst + head);
-            for (long long i = lane; i < quads; i += 32) __stcs(p + i, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-            if (tail + lane < a.D) dst[tail + lane] = 0.0f;
+            const uint32_t up = ~(left >> b);              // zeros where the stretch goes on
+            const int len = !side_by_side ? 1 : up ? __ffs(up) - 1 : 32;
+            warp_zero(base + b * a.row_stride, len * a.D);
+            left &= b + len >= 32 ? 0u : ~0u << (b + len);
         }
     }
 }
 
+constexpr int SEEN = 2048;
+
 // counts of the first digit per tile; which rows are named
 __global__ void __launch_bounds__(SORT_THREADS) sort_count_kernel(const GradArgs a) {
     __shared__ uint32_t hist[1 << SORT_MAX_BITS];
+    __shared__ uint32_t seen[SEEN];                      // tokens the block has marked, by their low bits
     const int r = blockIdx.y, bins = 1 << a.bits;
     for (int b = threadIdx.x; b < bins; b += SORT_THREADS) hist[b] = 0;
+    for (int b = threadIdx.x; b < SEEN; b += SORT_THREADS) seen[b] = 0;
     __syncthreads();
     for (int i = 0; i < a.items; ++i) {
         const long long n = (long long)blockIdx.x * a.tile + i * SORT_THREADS + threadIdx.x;
         if (n >= a.N) break;
         const uint32_t k = key_of(a, r * a.N + n);
         atomicAdd(&hist[k & (bins - 1)], 1u);
-        if (!a.accumulate) mark_row(a, r, k);
+        if (!a.accumulate && atomicExch(&seen[k % SEEN], k + 1) != k + 1) mark_row(a, r, k);
     }
     __syncthreads();
     uint32_t* out = a.count[0] + ((long long)r * a.tiles + blockIdx.x) * bins;
@@ -359,41 +377,40 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const GradAr
 
 // A worker's whole sort in one block
 __global__ void __launch_bounds__(SORT_THREADS) sort_one_tile_kernel(const GradArgs a) {
-    extern __shared__ __align__(16) uint32_t list[];     // keys, places, twice
+    __shared__ uint32_t key[ONE_TILE], pos[ONE_TILE];
     __shared__ SortShared s;
-    const int r = blockIdx.x, bins = 1 << a.bits, n = (int)a.N;
-    uint32_t* key[2] = {list, list + 2 * n};
-    uint32_t* pos[2] = {list + n, list + 3 * n};
-    for (int i = threadIdx.x; i < n; i += SORT_THREADS) {
-        const uint32_t k = key_of(a, r * a.N + i);
-        key[0][i] = k;
-        pos[0][i] = i;
+    const int r = blockIdx.x, bins = 1 << a.bits, i = threadIdx.x;
+    const bool in = i < a.N;
+    uint32_t k = 0, p = i;
+    if (in) {
+        k = key_of(a, r * a.N + i);
         if (!a.accumulate) mark_row(a, r, k);
     }
     for (int pass = 0; pass < a.passes; ++pass) {
-        const int from = pass & 1, shift = pass * a.bits;
-        for (int b = threadIdx.x; b < bins; b += SORT_THREADS) s.total[b] = 0;
+        const uint32_t d = in ? (k >> (pass * a.bits)) & (bins - 1) : (uint32_t)bins;
+        for (int b = i; b < bins; b += SORT_THREADS) s.total[b] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += SORT_THREADS) atomicAdd(&s.total[(key[from][i] >> shift) & (bins - 1)], 1u);
+        if (in) atomicAdd(&s.total[d], 1u);
         __syncthreads();
-        const uint32_t base = block_scan((int)threadIdx.x < bins ? s.total[threadIdx.x] : 0u, s.sums);
-        if ((int)threadIdx.x < bins) s.base[threadIdx.x] = base;
-        for (int i0 = 0; i0 < n; i0 += SORT_THREADS) {
-            const int i = i0 + threadIdx.x;
-            const uint32_t k = i < n ? key[from][i] : 0u, p = i < n ? pos[from][i] : 0u;
-            const uint32_t to = stable_place(s, i < n ? (k >> shift) & (bins - 1) : (uint32_t)bins, bins);
-            if (i < n) {
-                key[from ^ 1][to] = k;
-                pos[from ^ 1][to] = p;
-            }
+        const uint32_t base = block_scan(i < bins ? s.total[i] : 0u, s.sums);
+        if (i < bins) s.base[i] = base;
+        const uint32_t to = stable_place(s, d, bins);
+        if (in) {
+            key[to] = k;
+            pos[to] = p;
         }
         __syncthreads();
+        if (in) {
+            k = key[i];
+            p = pos[i];
+        }
     }
-    for (int i = threadIdx.x; i < n; i += SORT_THREADS) {
-        a.key[a.side][r * a.N + i] = key[a.passes & 1][i];
-        a.pos[a.side][r * a.N + i] = pos[a.passes & 1][i];
+    if (in) {
+        a.key[a.side][r * a.N + i] = k;
+        a.pos[a.side][r * a.N + i] = p;
     }
 }
+static_assert(ONE_TILE <= SORT_THREADS, "one place per thread");
 
 // ------------------------------------------------------------------ gradient: sums of the runs
 template <bool WIDE, int SIZE>
@@ -476,16 +493,18 @@ template <class T, bool WIDE> __device__ __forceinline__ void Piece<T, WIDE>::wi
 template <> __device__ __forceinline__ void Piece<float, true>::widen_if(float*) const {}
 template <> __device__ __forceinline__ void Piece<float, false>::widen_if(float*) const {}
 
+constexpr int SUM_THREADS = 128;
+
 // A warp per chunk and 256 columns; blocks past those set rows to zero (one-tile sorts: nothing ran beside them)
 template <class T, bool WIDE>
-__global__ void __launch_bounds__(256) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
-    constexpr int AHEAD = sizeof(T) == 4 && WIDE ? 4 : 8;          // rows in flight
+__global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
+    constexpr int AHEAD = sizeof(T) == 4 || !WIDE ? 2 : 4;         // rows in a batch; two batches are in flight
     if (blockIdx.x >= sum_blocks) {
         zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
         return;
     }
     const int lane = threadIdx.x & 31;
-    const long long id = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const long long id = (long long)blockIdx.x * (SUM_THREADS / 32) + (threadIdx.x >> 5);
     if (id >= (long long)a.R * a.chunks * a.col_tiles) return;
     const long long ch = id / a.col_tiles;
     const int c0 = (int)(id - ch * a.col_tiles) * COLS;
@@ -517,13 +536,15 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const GradArgs a, unsigned
         const int left = min(32, n - b);
         const uint32_t k = lane < left ? key[b + lane] : none, p = lane < left ? pos[b + lane] : 0u;
         if (__all_sync(~0u, k >= V) && cur >= V) break;            // only places that name no row are left
-        for (int i = 0; i < left; i += AHEAD) {
-            Piece<T, WIDE> row[AHEAD];
+        Piece<T, WIDE> row[2][AHEAD];
+        auto fetch = [&](Piece<T, WIDE> (&to)[AHEAD], int i) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31), pu = __shfl_sync(~0u, p, (i + u) & 31);
-                row[u].load(a, g + (long long)pu * a.g_stride, c0, i + u < left && ku < V);
+                to[u].load(a, g + (long long)pu * a.g_stride, c0, i + u < left && ku < V);
             }
+        };
+        auto add = [&](const Piece<T, WIDE> (&from)[AHEAD], int i) {
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31);
@@ -535,54 +556,94 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const GradArgs a, unsigned
 #pragma unroll
                         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
                     }
-                    row[u].add_to(sum);
+                    from[u].add_to(sum);
                 }
             }
+        };
+        fetch(row[0], 0);
+        for (int i = 0; i < left; i += 2 * AHEAD) {
+            if (i + AHEAD < left) fetch(row[1], i + AHEAD);
+            add(row[0], i);
+            if (i + AHEAD >= left) break;
+            if (i + 2 * AHEAD < left) fetch(row[0], i + 2 * AHEAD);
+            add(row[1], i + AHEAD);
         }
     }
     flush(true);
 }
 
-// Runs that cross chunks: a block per run and 256 columns adds the partial sums in order, each warp a stretch of them
+// Runs that cross chunks: their partial sums are added in order.  A warp per run and 256 columns; a run of more than
+// JOIN_ALONE chunks takes the whole block, each warp a stretch of it
+constexpr int JOIN_ALONE = 12;
+
+// adds partial sums [lo, hi) of the run that starts in chunk ch: the first chunk left its sum in slot 1, the others in 0
+__device__ __forceinline__ void add_parts(const GradArgs& a, long long ch, int c0, long long lo, long long hi, float (&sum)[8]) {
+    const long long width = (long long)a.col_tiles * COLS;
+    const float* base = a.part + ch * 2 * width + c0 + (threadIdx.x & 31) * 8;
+#pragma unroll 4
+    for (long long i = lo; i < hi; ++i) {
+        const float4* p = reinterpret_cast<const float4*>(base + (i * 2 + (i == 0)) * width);
+        const float4 x = p[0], y = p[1];
+        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+        sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+    }
+}
+
 template <int SIZE, bool WIDE>
 __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
     __shared__ float sums[8][COLS];
+    __shared__ long long length[8];                // chunks of the long runs met in this round
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long all = (long long)a.joins[0] * a.col_tiles, width = (long long)a.col_tiles * COLS;
-    for (long long id = blockIdx.x; id < all; id += gridDim.x) {
-        const long long at = id / a.col_tiles;
-        const int c0 = (int)(id - at * a.col_tiles) * COLS;
-        const long long ch = a.joins[1 + at], r = ch / a.chunks, c = ch - r * a.chunks;
-        const uint32_t* key = a.key[a.side] + r * a.N;
-        const uint32_t cur = key[(c + 1) * a.chunk - 1];
-        long long m = 0;                           // chunks the run goes on in
-        for (;;) {
-            const long long j = c + 1 + m + lane;
-            const uint32_t same = __ballot_sync(~0u, j < a.chunks && key[j * a.chunk] == cur);
-            m += same == ~0u ? 32 : __ffs(~same) - 1;
-            if (same != ~0u) break;
-        }
-        const long long per = (m + 1 + 7) / 8, lo = warp * per, hi = min(lo + per, m + 1);
+    const long long all = (long long)a.joins[0] * a.col_tiles;
+    // a run's column tiles follow one another: neighbours go to different blocks, so that a long run's do not queue up in one
+    for (long long id0 = blockIdx.x; id0 < all; id0 += (long long)gridDim.x * 8) {
+        const long long id = id0 + (long long)warp * gridDim.x;
         float sum[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-#pragma unroll 4
-        for (long long i = lo; i < hi; ++i) {      // the run's first chunk left its sum in slot 1, the others in slot 0
-            const float4* p = reinterpret_cast<const float4*>(a.part + ((ch + i) * 2 + (i == 0)) * width + c0 + lane * 8);
-            const float4 x = p[0], y = p[1];
-            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-            sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+        long long n = 0;
+        if (id < all) {
+            const long long at = id / a.col_tiles, ch = a.joins[1 + at], r = ch / a.chunks, c = ch - r * a.chunks;
+            const uint32_t* key = a.key[a.side] + r * a.N;
+            const uint32_t cur = key[(c + 1) * a.chunk - 1];
+            n = 1;
+            for (;;) {                             // chunks the run goes on in
+                const long long j = c + n + lane;
+                const uint32_t same = __ballot_sync(~0u, j < a.chunks && key[j * a.chunk] == cur);
+                n += same == ~0u ? 32 : __ffs(~same) - 1;
+                if (same != ~0u) break;
+            }
+            if (n <= JOIN_ALONE) {
+                const int c0 = (int)(id - at * a.col_tiles) * COLS;
+                add_parts(a, ch, c0, 0, n, sum);
+                write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+                n = 0;
+            }
         }
+        if (lane == 0) length[warp] = n;
         __syncthreads();
+        for (int w = 0; w < 8; ++w) {
+            const long long m = length[w];
+            if (m == 0) continue;
+            const long long of = id0 + (long long)w * gridDim.x, at = of / a.col_tiles, ch = a.joins[1 + at], r = ch / a.chunks, c = ch - r * a.chunks;
+            const int c0 = (int)(of - at * a.col_tiles) * COLS;
+            const long long per = (m + 7) / 8, lo = min(warp * per, m), hi = min(lo + per, m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = sum[j];
-        __syncthreads();
-        if (warp == 0) {
-            for (int w = 1; w < 8; ++w)
+            for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+            add_parts(a, ch, c0, lo, hi, sum);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += sums[w][lane + 32 * j];
-            write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+            for (int j = 0; j < 8; ++j) sums[warp][lane + 32 * j] = sum[j];
+            __syncthreads();
+            if (warp == 0) {
+                for (int x = 1; x < 8; ++x)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += sums[x][lane + 32 * j];
+                const uint32_t cur = a.key[a.side][r * a.N + (c + 1) * a.chunk - 1];
+                write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+            }
+            __syncthreads();
         }
+        __syncthreads();                           // `length` is written again
     }
 }
 
@@ -591,8 +652,8 @@ __global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_
 
 template <class T, bool WIDE>
 void launch_sums(const GradArgs& a, bool zero_here, int sms, cudaStream_t st) {
-    const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + 7) / 8);
-    run_sum_kernel<T, WIDE><<<sum_blocks + (zero_here ? sms * 4 : 0), 256, 0, st>>>(a, sum_blocks);
+    const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + SUM_THREADS / 32 - 1) / (SUM_THREADS / 32));
+    run_sum_kernel<T, WIDE><<<sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, 0, st>>>(a, sum_blocks);
     run_join_kernel<sizeof(T), WIDE><<<sms * 4, 256, 0, st>>>(a);
 }
 
@@ -619,13 +680,13 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     const int64_t tile = (int64_t)s.items * SORT_THREADS;
     s.tiles = (int)((N + tile - 1) / tile);
     s.col_tiles = (int)((D + COLS - 1) / COLS);
-    // chunks as long as 128 places while they give every SM some 16 warps
+    // chunks as long as 64 places while they give every SM some 16 warps
     s.chunk = 16;
-    while (s.chunk < 128 && R * N / (2 * s.chunk) * s.col_tiles >= 148 * 16) s.chunk *= 2;
+    while (s.chunk < 64 && R * N / (2 * s.chunk) * s.col_tiles >= 148 * 16) s.chunk *= 2;
     s.chunks = (int)((N + s.chunk - 1) / s.chunk);
     s.count = 4 * R * N;
     s.named = s.count + (s.one_tile ? 0 : (int64_t)s.passes * R * s.tiles << s.bits);
-    s.joins = s.named + R * ((V + 31) / 32);
+    s.joins = s.named + R * ((V + 31) / 32 * 32) / 4;
     s.zeroed = s.joins + 1;
     s.part = (s.zeroed + (int64_t)R * s.chunks + 3) / 4 * 4;
     s.words = s.part + (int64_t)R * s.chunks * 2 * s.col_tiles * COLS;
@@ -704,9 +765,11 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     a.worker_stride = worker_stride; a.row_stride = row_stride; a.status = status;
     a.key[0] = w; a.key[1] = w + m; a.pos[0] = w + 2 * m; a.pos[1] = w + 3 * m;
     for (int i = 0; i < p.passes; ++i) a.count[i] = w + p.count + ((int64_t)i * R * p.tiles << p.bits);
-    a.named = w + p.named; a.joins = w + p.joins; a.part = reinterpret_cast<float*>(w + p.part);
+    a.named = reinterpret_cast<uint8_t*>(w + p.named); a.padded = (V + 31) / 32 * 32; a.joins = w + p.joins; a.part = reinterpret_cast<float*>(w + p.part);
     a.passes = p.passes; a.bits = p.bits; a.tiles = p.tiles; a.items = p.items; a.tile = p.items * SORT_THREADS;
     a.chunk = p.chunk; a.chunks = p.chunks; a.col_tiles = p.col_tiles; a.side = p.passes & 1;
+    a.unit = 32;
+    while (a.unit > 1 && a.unit * D > 2048) a.unit /= 2;
     if (N == 0 && accumulate) return QS_OK;
     if (cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
     if (N == 0) {
@@ -714,16 +777,13 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
         return launch_status();
     }
     if (p.one_tile) {
-        const int smem = (int)(16 * N);
-        if (cudaFuncSetAttribute(sort_one_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16 * ONE_TILE) != cudaSuccess) {
-            cudaGetLastError();
-            return QS_CUDA;
-        }
-        sort_one_tile_kernel<<<R, SORT_THREADS, smem, st>>>(a);
+        sort_one_tile_kernel<<<R, SORT_THREADS, 0, st>>>(a);
     } else {
         sort_count_kernel<<<dim3(p.tiles, R), SORT_THREADS, 0, st>>>(a);
+        // as many blocks as fit beside the sort's two to an SM, so that none of them starts late with a full share
+        const int zero_blocks = accumulate ? 0 : R * p.tiles < sms ? 2 * sms - R * p.tiles : sms;
         for (int pass = 0; pass < p.passes; ++pass)
-            sort_scatter_kernel<<<R * p.tiles + (accumulate ? 0 : 2 * sms), SORT_THREADS, 0, st>>>(a, pass);
+            sort_scatter_kernel<<<R * p.tiles + zero_blocks, SORT_THREADS, 0, st>>>(a, pass);
     }
     const int size = size_of_type(grad_type);
     const bool zero_here = p.one_tile && !accumulate;
