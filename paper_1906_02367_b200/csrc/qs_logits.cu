@@ -10,9 +10,10 @@
 // A column at -inf has p = 0 and adds nothing; a row without any other column has lse = -inf.
 //
 // All of these are bound by the memory that holds the logits: each must read the row, and the gradients write
-// one.  So a row is read once.  A cluster of up to 8 blocks holds it in registers (qs_rows.cuh); the blocks put
-// their statistics into one another's shared memory, and the same registers then give the gradient or the
-// alternatives.  The backward calls, which start from a saved lse, need no cluster.
+// one.  So a row is read once, through a ring in shared memory that stays full (qs_rows.cuh).  Statistics and
+// alternatives are taken as the chunks come by; the loss that also gives its gradient keeps the row's chunks in the
+// shared memory of a cluster until the statistics are joined, and each chunk's slot takes the next row's chunk as
+// soon as its gradient is written.  The backward calls, which start from a saved lse, are one pass per vector.
 #include "qs_rows.cuh"
 
 namespace {
@@ -20,12 +21,11 @@ namespace {
 using namespace qs;
 
 constexpr int MAX_BLOCKS = 8;              // blocks of a row's cluster
-constexpr int MAX_WARPS = 16;              // warps of a block
-constexpr int MAX_THREADS = 32 * MAX_WARPS;
+constexpr int MAX_THREADS = 256;
+constexpr int MAX_WARPS = MAX_THREADS / 32;
 constexpr int PARTS = MAX_BLOCKS * MAX_WARPS;
-constexpr int MAX_GROUPS = 1024;           // maxima that bound the K-th alternative
-constexpr int CANDS = 1024;                // candidates a row's blocks may send, CANDS / blocks each (>= QS_MAX_TOP)
-constexpr int RANK_MOST = 256;             // candidates ranked against one another without a further cut (>= QS_MAX_TOP)
+constexpr int VPT = 4;                     // vectors per thread and chunk
+constexpr int CANDS = 1024;                // candidates a block keeps, and a row's blocks send in all (>= MAX_BLOCKS QS_MAX_TOP)
 
 struct RowArgs {
     long long N, V, row0;
@@ -45,10 +45,21 @@ struct RowArgs {
     float g_all;                           // where g1 is null
     void* grad; long long grad_stride;
     int wide;                              // the gradient's rows lie like the logits' rows within 16 bytes
-    int blocks;                            // blocks per row
+    int blocks;                            // blocks per row (backward calls)
     int groups;                            // maxima per warp that bound the K-th alternative
     int* status;
 };
+
+// barriers of the ring, and its first chunks on their way
+template <class T>
+__device__ __forceinline__ void start_feed(Feed<T>& feed) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < feed.f.slots; ++i) mbar_init(&feed.full[i], 1);
+        fence_async_smem();
+        for (int i = 0; i < feed.f.slots; ++i) feed.issue();
+    }
+    __syncthreads();
+}
 
 // ------------------------------------------------------------------ log probabilities
 // Places that a cut takes: key above the cut's, or equal to it with a column at or below the cut's
@@ -95,34 +106,16 @@ __device__ Cut find_cut(int K, int most, uint32_t lo, uint32_t columns, Count co
     return Cut{lo, b};
 }
 
-// calls f(key, column) for the elements of the share
-template <class T, int VPT, bool ONE, class F>
-__device__ __forceinline__ void each_element(const Share<T>& r, uint4 (&q)[VPT], F f) {
-    const int nt = blockDim.x;
-    for (int base = r.v0; base < r.v1; base += nt * VPT) {
-        if (!ONE) load_share<T, VPT>(r, base, nt, q);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int e0 = r.first(base + j * nt + (int)threadIdx.x);
-#pragma unroll
-            for (int i = 0; i < Vec<T>::E / 2; ++i) {
-                const float2 p = parts(Vec<T>::pair(q[j], i));
-                f(p.x, (uint32_t)(e0 + 2 * i));
-                f(p.y, (uint32_t)(e0 + 2 * i + 1));
-            }
-        }
-    }
-}
-
 struct TopShared {
-    uint32_t group[MAX_GROUPS];            // keys of the group maxima of the whole row
-    unsigned long long cand[CANDS];        // (key, ~column); block b's at b * CANDS / blocks
+    uint32_t group[32 * MAX_WARPS];        // keys of the block's group maxima so far
+    unsigned long long list[CANDS];        // candidates (key, ~column) of the block's share
+    unsigned long long merged[CANDS];      // of a cluster's blocks, block b's at b * CANDS / blocks (first block)
     int count[MAX_BLOCKS];                 // of which there are
-    int mine, sums[MAX_WARPS];
-    uint32_t bound;
+    int n, kept, sums[MAX_WARPS];          // candidates in the list, and before the current chunk
+    uint32_t bound, reached;               // keys below `bound` are no alternatives; K elements so far reach `reached`
 };
 
-// The largest key found that at least K of the row's group maxima reach: no alternative lies below it.  One warp
+// The largest key found that at least K of the n group maxima reach, KEY_LOWEST - 1 if fewer are above -inf.  One warp
 __device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, int K) {
     const int lane = threadIdx.x & 31;
     uint32_t top = 0;
@@ -132,7 +125,7 @@ __device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, in
         live += group[i] >= KEY_LOWEST;
     }
     top = __reduce_max_sync(~0u, top);
-    if (__reduce_add_sync(~0u, live) < K) return KEY_LOWEST;
+    if (__reduce_add_sync(~0u, live) < K) return KEY_LOWEST - 1;
     uint32_t lo = KEY_LOWEST, hi = top + 1;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
@@ -149,176 +142,219 @@ __device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, in
     return lo;
 }
 
-template <class T, int VPT, bool ONE, bool TOP>
-__global__ void __launch_bounds__(MAX_THREADS) token_logp_kernel(const RowArgs a) {
+// calls f(z, column) for the elements of a chunk's vectors that reach `bound`
+template <class T, class F>
+__device__ __forceinline__ void each_above(const uint4 (&q)[VPT], int e0, int step, float bound, F f) {
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        if (!(Vec<T>::top(max_of_words<T>(q[j])) >= bound)) continue;
+        const int e = e0 + j * step;
+#pragma unroll
+        for (int i = 0; i < Vec<T>::E / 2; ++i) {
+            const float2 p = parts(Vec<T>::pair(q[j], i));
+            if (p.x >= bound) f(p.x, (uint32_t)(e + 2 * i));
+            if (p.y >= bound) f(p.y, (uint32_t)(e + 2 * i + 1));
+        }
+    }
+}
+
+__device__ __forceinline__ unsigned long long entry_of(float z, uint32_t col) { return ((unsigned long long)key_of(z) << 32) | (uint32_t)~col; }
+__device__ __forceinline__ bool takes(Cut c, unsigned long long e) { return takes(c, (uint32_t)(e >> 32), ~(uint32_t)e); }
+
+// More elements of this chunk pass the bound than the list holds (ties, or an order that defeats the bound): the list is
+// made anew from the entries before the chunk and the chunk's elements that an exact cut takes.  All threads
+template <class T>
+__device__ void rebuild_list(TopShared& t, const uint4 (&q)[VPT], int e0, int step, int K, uint32_t columns) {
+    const int nt = blockDim.x, kept = t.kept;
+    const float bound = value_of(t.bound);
+    const Cut cut = find_cut(K, CANDS / 2, KEY_LOWEST - 1, columns, [&](Cut c) {
+        int k = 0;
+        for (int i = threadIdx.x; i < kept; i += nt) k += takes(c, t.list[i]);
+        each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) { k += takes(c, key_of(z), col); });
+        return block_count(k, t.sums);
+    });
+    unsigned long long mine[CANDS / 128];          // (128 threads or more)
+#pragma unroll
+    for (int x = 0; x < CANDS / 128; ++x) {
+        const int i = threadIdx.x + x * nt;
+        mine[x] = i < kept && takes(cut, t.list[i]) ? t.list[i] : 0ull;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) t.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < CANDS / 128; ++x)
+        if (mine[x]) t.list[atomicAdd(&t.n, 1)] = mine[x];
+    each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) {
+        if (takes(cut, key_of(z), col)) t.list[atomicAdd(&t.n, 1)] = entry_of(z, col);
+    });
+    // K entries reach cut.key, all in earlier columns than what is still to come
+    if (threadIdx.x == 0) t.bound = max(t.bound, cut.key + 1);
+    __syncthreads();
+}
+
+// Statistics of the row, and with TOP its alternatives, in one pass.  Candidates are the elements that reach a bound
+// below which no alternative can lie: the K-th largest of group maxima over the chunks so far (a group is 32 / groups
+// lanes' share of the row), taken anew after chunks 1, 2, 4, 8, ..
+template <class T, bool TOP>
+__global__ void __launch_bounds__(MAX_THREADS, 3) token_logp_kernel(const RowArgs a, const FeedArgs f) {
+    extern __shared__ __align__(128) uint4 ring[];
+    __shared__ uint64_t full[MAX_SLOTS];
     __shared__ float4 part[PARTS];
     __shared__ float row_m, row_ls, row_lse;
     __shared__ TopShared top[1];                   // (no room where it is not used)
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = f.blocks;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-    const long long n = a.row0 + blockIdx.x / blocks;
     const float c2 = a.scale * LOG2E;
-    if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
-    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
-    uint4 q[VPT];
-    Stat st{neg_inf(), 0.0f, 0.0f};
-    float mine = neg_inf();
-    if (ONE) {
-        load_share<T, VPT>(r, r.v0, nt, q);
-        mine = thread_max_of<T, VPT>(q);
-        st = warp_stat<T, VPT, true>(q, mine, c2);
-    } else {
-        for (int base = r.v0; base < r.v1; base += nt * VPT) {
-            load_share<T, VPT>(r, base, nt, q);
-            const float tm = thread_max_of<T, VPT>(q);
-            const Stat now = warp_stat<T, VPT, true>(q, tm, c2);
-            const float m = fmaxf(st.m, now.m);
-            const Stat x = rescale(st, m, c2), y = rescale(now, m, c2);
-            st = Stat{m, x.s + y.s, x.u + y.u};
-            mine = fmaxf(mine, tm);
+    const long long first_row = blockIdx.x / blocks;
+    Feed<T> feed(a.logits, a.stride, a.N, a.V, f, ring, full, rank, first_row);
+    start_feed(feed);
+    if (TOP && threadIdx.x == 0) { top->n = top->kept = 0; top->bound = KEY_LOWEST; }
+    for (long long n = first_row; n < a.N; n += f.clusters) {
+        const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+        Stat st{neg_inf(), 0.0f, 0.0f};
+        long long t = -1;
+        float zt = 0.0f;
+        if (rank == 0 && threadIdx.x == nt - 1 && a.logp) {
+            t = a.tok.at(n);
+            if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
+            else if (t >= 0) zt = to_float(r.z[t]);
         }
-    }
-    long long t = -1;
-    float zt = 0.0f;
-    if (rank == 0 && threadIdx.x == 32 && a.logp) {
-        t = a.tok.at(n);
-        if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
-        else if (t >= 0) zt = to_float(r.z[t]);
-    }
-    if (blocks > 1) cluster_wait();
-    const float4 sent = make_float4(st.m, st.s, st.u, 0.0f);
-    if (blocks == 1) {
-        if (lane == 0) part[warp] = sent;
-    } else if (lane < (TOP ? blocks : 1)) {
-        remote_store(remote_addr(&part[rank * warps + warp], lane), sent);
-    }
-    if (TOP) {
-        const int width = 32 / a.groups;
-        float g = mine;
-        for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-        const int at = (rank * warps + warp) * a.groups + lane / width;
-        if (lane % width == 0) {
-            if (blocks == 1) top->group[at] = key_of(g);
-            else
-                for (int b = 0; b < blocks; ++b) remote_store(remote_addr(&top->group[at], b), key_of(g));
+        for (int c = 0; c < f.chunks; ++c) {
+            uint4 q[VPT];
+            const bool ok = feed.wait();
+            feed.template read<VPT>(r, c, feed.at, q);
+            feed.next();
+            if (__syncthreads_or(!ok)) {           // a copy never came
+                if (threadIdx.x == 0) feed.give_up(a.status);
+                return;
+            }
+            if (threadIdx.x == 0) feed.issue();
+            take_chunk<T, VPT, true>(st, q, c2);
+            if (!TOP) continue;
+            const int e0 = r.first(r.v0 + c * f.chunk + (int)threadIdx.x), step = nt * Vec<T>::E;
+            const bool renew = (c & (c + 1)) == 0 && c + 1 < 2 * f.chunks;     // after chunks 1, 2, 4, ..
+            if (renew) {
+                const int width = 32 / a.groups;
+                float g = st.m;
+                for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+                if (lane % width == 0) top->group[warp * a.groups + lane / width] = key_of(g);
+                __syncthreads();
+                if (warp == 0) {
+                    const uint32_t b = group_bound(top->group, warps * a.groups, a.K);
+                    if (lane == 0) {
+                        top->reached = b;
+                        top->bound = max(top->bound, b);
+                    }
+                }
+                __syncthreads();
+            }
+            const float bound = value_of(top->bound);
+            if (st.m >= bound)
+                each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) {
+                    const int at = atomicAdd(&top->n, 1);
+                    if (at < CANDS) top->list[at] = entry_of(z, col);
+                });
+            __syncthreads();
+            if (top->n > CANDS) rebuild_list<T>(*top, q, e0, step, a.K, (uint32_t)a.V);
+            else if (renew && threadIdx.x == 0 && top->reached >= KEY_LOWEST) top->bound = max(top->bound, top->reached + 1);
+            if (threadIdx.x == 0) top->kept = top->n;
+            // (the next chunk's first barrier orders these before they are read; what equals `reached` in a later column
+            // comes after the K that reached it)
         }
-    }
-    if (blocks == 1) {
-        __syncthreads();
-    } else {
-        cluster_arrive();
-        if (!TOP && rank != 0) return;             // nothing is written into this block's memory
-        cluster_wait();
-    }
-    if (rank == 0 && warp == 1) {
-        const Stat v = join_parts(part, warps * blocks, c2);
-        const bool empty = v.m == neg_inf() && v.s == 0.0f;
-        const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
-        if (lane == 0) {
-            if (a.lse) a.lse[n] = lse;
-            if (a.entropy) a.entropy[n] = empty ? 0.0f : ls - LN2 * (v.u / v.s);
-            if (a.logp) a.logp[n] = t >= a.V ? quiet_nan() : t < 0 ? 0.0f : empty ? neg_inf() : fmaf(zt - v.m, a.scale, -ls);
-            row_m = v.m; row_ls = ls; row_lse = lse;
+        const Stat w = join_warp<true>(st, c2);
+        const float4 sent = make_float4(w.m, w.s, w.u, 0.0f);
+        if (blocks == 1) {
+            if (lane == 0) part[warp] = sent;
+            __syncthreads();
+        } else {
+            if (TOP) {
+                const int room = CANDS / blocks;
+                __syncthreads();
+                const int have = top->n;
+                Cut cut{0, 0xffffffffu};
+                if (have > room)
+                    cut = find_cut(a.K, room, KEY_LOWEST - 1, (uint32_t)a.V, [&](Cut c) {
+                        int k = 0;
+                        for (int i = threadIdx.x; i < have; i += nt) k += takes(c, top->list[i]);
+                        return block_count(k, top->sums);
+                    });
+                __syncthreads();
+                if (threadIdx.x == 0) top->n = 0;
+                cluster_arrive();                  // the first block has done with the row before
+                cluster_wait();
+                for (int i = threadIdx.x; i < have; i += nt)
+                    if (takes(cut, top->list[i])) remote_store(remote_addr(&top->merged[rank * room + atomicAdd(&top->n, 1)], 0), top->list[i]);
+                __syncthreads();
+                if (threadIdx.x == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->n);
+            } else {
+                cluster_arrive();
+                cluster_wait();
+            }
+            if (lane == 0) remote_store(remote_addr(&part[rank * warps + warp], 0), sent);
+            cluster_arrive();
+            cluster_wait();
         }
-    }
-    if (!TOP) return;
-
-    if (warp == 0) {
-        const uint32_t b = group_bound(top->group, warps * blocks * a.groups, a.K);
-        if (lane == 0) { top->bound = b; top->mine = 0; }
-    }
-    __syncthreads();
-    const int room = CANDS / blocks;
-    const float bound = value_of(top->bound);
-    auto send = [&](float z, uint32_t col) {
-        const int slot = atomicAdd(&top->mine, 1);
-        if (slot >= room) return;
-        const unsigned long long v = ((unsigned long long)key_of(z) << 32) | (uint32_t)~col;
-        if (blocks == 1) top->cand[slot] = v;
-        else remote_store(remote_addr(&top->cand[rank * room + slot], 0), v);
-    };
-    if (mine >= bound) {
-        for (int base = r.v0; base < r.v1; base += nt * VPT) {
-            if (!ONE) load_share<T, VPT>(r, base, nt, q);
-#pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                if (!(Vec<T>::top(max_of_words<T>(q[j])) >= bound)) continue;
-                const int e0 = r.first(base + j * nt + (int)threadIdx.x);
-#pragma unroll
-                for (int i = 0; i < Vec<T>::E / 2; ++i) {
-                    const float2 p = parts(Vec<T>::pair(q[j], i));
-                    if (p.x >= bound) send(p.x, (uint32_t)(e0 + 2 * i));
-                    if (p.y >= bound) send(p.y, (uint32_t)(e0 + 2 * i + 1));
+        if (rank == 0) {
+            if (warp == warps - 1) {
+                const Stat v = join_parts(part, warps * blocks, c2);
+                const bool empty = v.m == neg_inf() && v.s == 0.0f;
+                const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
+                if (lane == 31) {                  // the thread that holds the token
+                    if (a.lse) a.lse[n] = lse;
+                    if (a.entropy) a.entropy[n] = empty ? 0.0f : ls - LN2 * (v.u / v.s);
+                    if (a.logp) a.logp[n] = t >= a.V ? quiet_nan() : t < 0 ? 0.0f : empty ? neg_inf() : fmaf(zt - v.m, a.scale, -ls);
+                    row_m = v.m; row_ls = ls; row_lse = lse;
                 }
             }
+            if (TOP) {
+                // rank the candidates; far more than K are cut first, since each is compared with all others
+                const int room = CANDS / blocks;
+                const unsigned long long* list = blocks == 1 ? top->list : top->merged;
+                if (blocks == 1 && threadIdx.x == 0) top->count[0] = top->n;
+                __syncthreads();
+                int total = 0;
+                for (int b = 0; b < blocks; ++b) total += top->count[b];
+                const int most = a.K + a.K / 4 + 16;
+                Cut cut{0, 0xffffffffu};
+                if (total > most)
+                    cut = find_cut(a.K, most, KEY_LOWEST - 1, (uint32_t)a.V, [&](Cut c) {
+                        int k = 0;
+                        for (int b = 0; b < blocks; ++b)
+                            for (int i = threadIdx.x; i < top->count[b]; i += nt) k += takes(c, list[b * room + i]);
+                        return block_count(k, top->sums);
+                    });
+                const float lse = row_lse, ls = row_ls, m = row_m;
+                const bool broken = !(lse == lse);
+                auto put = [&](int at, long long id, float lp) {
+                    if (a.tok.wide) static_cast<long long*>(a.top_ids)[n * a.K + at] = id;
+                    else static_cast<int*>(a.top_ids)[n * a.K + at] = (int)id;
+                    a.top_logp[n * a.K + at] = lp;
+                };
+                for (int b = 0; b < blocks && !broken; ++b)
+                    for (int i = threadIdx.x; i < top->count[b]; i += nt) {
+                        const unsigned long long v = list[b * room + i];
+                        if (!takes(cut, v)) continue;
+                        int place = 0;
+                        for (int d = 0; d < blocks; ++d)
+                            for (int x = 0; x < top->count[d]; ++x) place += list[d * room + x] > v;
+                        if (place < a.K) put(place, ~(uint32_t)v, fmaf(value_of((uint32_t)(v >> 32)) - m, a.scale, -ls));
+                    }
+                for (int k = (broken ? 0 : total) + (int)threadIdx.x; k < a.K; k += nt) put(k, -1, broken ? lse : neg_inf());
+            }
         }
+        __syncthreads();
+        if (TOP && threadIdx.x == 0) { top->n = top->kept = 0; top->bound = KEY_LOWEST; }
     }
-    __syncthreads();
-    if (top->mine > room) {                        // a mask, ties or an order that defeats the bound: cut exactly
-        const Cut cut = find_cut(a.K, room, top->bound, (uint32_t)a.V, [&](Cut c) {
-            int k = 0;
-            each_element<T, VPT, ONE>(r, q, [&](float z, uint32_t col) { k += z > neg_inf() && takes(c, key_of(z), col); });
-            return block_count(k, top->sums);
-        });
-        __syncthreads();
-        if (threadIdx.x == 0) top->mine = 0;
-        __syncthreads();
-        each_element<T, VPT, ONE>(r, q, [&](float z, uint32_t col) {
-            if (z > neg_inf() && takes(cut, key_of(z), col)) send(z, col);
-        });
-        __syncthreads();
-    }
-    if (blocks == 1) {
-        if (threadIdx.x == 0) top->count[0] = top->mine;
-        __syncthreads();
-    } else {
-        if (threadIdx.x == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->mine);
-        cluster_arrive();
-        if (rank != 0) return;
-        cluster_wait();
-    }
-
-    // the row's first block ranks the candidates
-    int total = 0;
-    for (int b = 0; b < blocks; ++b) total += top->count[b];
-    const float lse = row_lse, ls = row_ls, m = row_m;
-    const bool broken = !(lse == lse);
-    Cut cut{0, 0xffffffffu};
-    if (total > RANK_MOST)
-        cut = find_cut(a.K, RANK_MOST, KEY_LOWEST - 1, (uint32_t)a.V, [&](Cut c) {
-            int k = 0;
-            for (int b = 0; b < blocks; ++b)
-                for (int i = threadIdx.x; i < top->count[b]; i += nt) {
-                    const unsigned long long v = top->cand[b * room + i];
-                    k += takes(c, (uint32_t)(v >> 32), ~(uint32_t)v);
-                }
-            return block_count(k, top->sums);
-        });
-    auto put = [&](int at, long long id, float lp) {
-        if (a.tok.wide) static_cast<long long*>(a.top_ids)[n * a.K + at] = id;
-        else static_cast<int*>(a.top_ids)[n * a.K + at] = (int)id;
-        a.top_logp[n * a.K + at] = lp;
-    };
-    for (int b = 0; b < blocks && !broken; ++b)
-        for (int i = threadIdx.x; i < top->count[b]; i += nt) {
-            const unsigned long long v = top->cand[b * room + i];
-            const uint32_t key = (uint32_t)(v >> 32), col = ~(uint32_t)v;
-            if (!takes(cut, key, col)) continue;
-            int place = 0;
-            for (int d = 0; d < blocks; ++d)
-                for (int x = 0; x < top->count[d]; ++x) place += top->cand[d * room + x] > v;
-            if (place < a.K) put(place, col, fmaf(value_of(key) - m, a.scale, -ls));
-        }
-    for (int k = (broken ? 0 : total) + (int)threadIdx.x; k < a.K; k += nt) put(k, -1, broken ? lse : neg_inf());
 }
 
-template <class T, int VPT, bool ENT>
+template <class T, int VG, bool ENT>
 __global__ void __launch_bounds__(256) token_logp_grad_kernel(const RowArgs a) {
     const int nt = blockDim.x;
     const long long n = a.row0 + blockIdx.x / a.blocks;
     const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
-    uint4 q[VPT];
-    load_share<T, VPT>(r, r.v0, nt, q);
+    uint4 q[VG];
+    load_share<T, VG>(r, r.v0, nt, q);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const long long t = a.tok.p ? a.tok.at(n) : -1;
     const float lse = a.in_lse[n];
@@ -337,7 +373,7 @@ __global__ void __launch_bounds__(256) token_logp_grad_kernel(const RowArgs a) {
     const int hot = t >= 0 && t < a.V ? (int)((t + r.head) / Vec<T>::E) : -1;
     const float hot_g = g * a.scale;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
+    for (int j = 0; j < VG; ++j) {
         const int vec = r.v0 + j * nt + (int)threadIdx.x;
         if (vec >= r.v1) continue;
         f2 d[Vec<T>::E / 2];
@@ -376,58 +412,69 @@ __device__ __forceinline__ float teacher_at(const RowArgs& a, long long i) {
                                      : to_float(static_cast<const __half*>(a.teacher)[i]);
 }
 
-// One warp: the row's entries, their probabilities, and the logits at those ids that are in the share (`all`: at all)
-template <class T, bool TAIL>
-__device__ void load_teacher(const RowArgs& a, long long n, const Share<T>& r, bool all, TeacherShared& s) {
-    constexpr int PER = QS_MAX_TOP / 32;
-    const int lane = threadIdx.x & 31;
+// One warp's view of a row's entries, as they come from memory: entry lane + 32 i
+struct Entries {
+    static constexpr int PER = QS_MAX_TOP / 32;
+    long long id[PER];
     float u[PER];
-    bool bad = false;
-    float m = neg_inf();
+
+    __device__ __forceinline__ void load(const RowArgs& a, long long n) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int k = lane + 32 * i;
-        u[i] = neg_inf();
-        if (k >= a.K) continue;
-        const long long id = a.tok.at(n * a.K + k);
-        const bool named = id >= 0 && id < a.V;
-        bad |= id >= a.V;
-        s.id[k] = named ? (uint32_t)id : NO_ID;
-        if (!named) continue;
-        u[i] = teacher_at(a, n * a.K + k) * a.teacher_scale;
-        if (all || r.holds((int)id)) s.z[k] = to_float(r.z[id]);
-        m = fmaxf(m, u[i]);
-    }
-    bad = __any_sync(~0u, bad);
-    m = TAIL ? 0.0f : shift_of(warp_max(m));
-    float e[PER], total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        e[i] = ex2((u[i] - m) * LOG2E);
-        total += e[i];
-    }
-    total = warp_sum(total);
-    const float lt = TAIL || total == 0.0f ? 0.0f : logf(total), by = TAIL || total == 0.0f ? 1.0f : 1.0f / total;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int k = lane + 32 * i;
-        const float q = e[i] * by;
-        if (k < a.K) {
-            s.q[k] = q;
-            s.logq[k] = u[i] - m - lt;
+        for (int i = 0; i < PER; ++i) {
+            const int k = (int)(threadIdx.x & 31) + 32 * i;
+            id[i] = -1;
+            u[i] = 0.0f;
+            if (k >= a.K || n >= a.N) continue;
+            id[i] = a.tok.at(n * a.K + k);
+            u[i] = teacher_at(a, n * a.K + k);
         }
-        sum += q;
     }
-    sum = warp_sum(sum);
-    if (lane == 0) {
-        s.Q = sum;
-        s.rest = !TAIL ? 0.0f : sum == sum ? fmaxf(0.0f, 1.0f - sum) : sum;
-        s.bad = bad;
-        if (bad && r.v0 == 0) flag_status(a.status, QS_INVALID_ARG);
+    // the row's probabilities into shared memory
+    template <bool TAIL>
+    __device__ void finish(const RowArgs& a, TeacherShared& s, bool tell) {
+        const int lane = threadIdx.x & 31;
+        bool bad = false;
+        float m = neg_inf();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = lane + 32 * i;
+            const bool named = id[i] >= 0 && id[i] < a.V;
+            bad |= id[i] >= a.V;
+            u[i] = named ? u[i] * a.teacher_scale : neg_inf();
+            if (k < a.K) s.id[k] = named ? (uint32_t)id[i] : NO_ID;
+            m = fmaxf(m, u[i]);
+        }
+        bad = __any_sync(~0u, bad);
+        m = TAIL ? 0.0f : shift_of(warp_max(m));
+        float e[PER], total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            e[i] = ex2((u[i] - m) * LOG2E);
+            total += e[i];
+        }
+        total = warp_sum(total);
+        const float lt = TAIL || total == 0.0f ? 0.0f : logf(total), by = TAIL || total == 0.0f ? 1.0f : 1.0f / total;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = lane + 32 * i;
+            const float q = e[i] * by;
+            if (k < a.K) {
+                s.q[k] = q;
+                s.logq[k] = u[i] - m - lt;
+            }
+            sum += q;
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) {
+            s.Q = sum;
+            s.rest = !TAIL ? 0.0f : sum == sum ? fmaxf(0.0f, 1.0f - sum) : sum;
+            s.bad = bad;
+            if (bad && tell) flag_status(a.status, QS_INVALID_ARG);
+        }
+        __syncwarp();
     }
-    __syncwarp();
-}
+};
 
 // What turns a row's probabilities into its gradient: outside the ids f p with f = w (Q + q_T - q_T / p_T), or, where
 // p_T is too small for the quotient, w p (Q + q_T) - w q_T exp(log p - log p_T)
@@ -477,168 +524,232 @@ __device__ __forceinline__ uint4 slope_vec(const f2* d, const Slope& s, float no
     return Vec<T>::pack(g);
 }
 
-template <class T, int VPT, bool ONE, bool TAIL>
-__global__ void __launch_bounds__(MAX_THREADS) distill_kernel(const RowArgs a) {
+// Loss and, with a.grad, its gradient.  KEEP: the share's chunks stay in the ring until their gradient is written
+// (ring of at least one share); otherwise they come by twice
+template <class T, bool KEEP, bool TAIL>
+__global__ void __launch_bounds__(MAX_THREADS, 3) distill_kernel(const RowArgs a, const FeedArgs f) {
     constexpr int E = Vec<T>::E;
-    __shared__ float4 part[PARTS];
-    __shared__ float4 in_part[MAX_BLOCKS];         // tail: the statistics of the ids' own columns, block by block
+    extern __shared__ __align__(128) uint4 ring[];
+    __shared__ uint64_t full[MAX_SLOTS];
+    __shared__ float4 part[2][PARTS];              // two rows' worth: the other blocks may be a row ahead
+    __shared__ float4 in_part[2][MAX_BLOCKS];      // tail: the statistics of the ids' own columns, block by block
+    __shared__ float z_at[2][QS_MAX_TOP];          // first block: logits at the ids
     __shared__ TeacherShared t;
     __shared__ float row_m, row_by;                // maximum, one over the sum
     __shared__ Slope row;
-    __shared__ __align__(16) uint8_t named[TAIL ? MAX_THREADS * VPT : 1];      // per vector of the round: places that an id names
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = f.blocks;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-    const long long n = a.row0 + blockIdx.x / blocks;
     const float c2 = a.scale * LOG2E;
+    const long long first_row = blockIdx.x / blocks;
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
-    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
-    uint4 q[VPT];
-    if (ONE) load_share<T, VPT>(r, r.v0, nt, q);
-    if (warp == 0) load_teacher<T, TAIL>(a, n, r, rank == 0, t);
-    Stat st{neg_inf(), 0.0f, 0.0f};
-    if (TAIL) __syncthreads();
-    for (int base = r.v0; base < r.v1; base += nt * VPT) {
-        if (!ONE) load_share<T, VPT>(r, base, nt, q);
-        if (TAIL) {                                // the ids' columns leave the sum: their own statistics join later
-            uint32_t* words = reinterpret_cast<uint32_t*>(named);
-            for (int i = threadIdx.x; i < nt * VPT / 4; i += nt) words[i] = 0;
-            __syncthreads();
-            for (int k = threadIdx.x; k < a.K; k += nt) {
-                if (t.id[k] == NO_ID) continue;
-                const int place = (int)t.id[k] + r.head, at = place / E - base;
-                if (at >= 0 && at < nt * VPT && place / E < r.v1) atomicOr(&words[at >> 2], 1u << ((at & 3) * 8 + place % E));
+    Feed<T> feed(a.logits, a.stride, a.N, a.V, f, ring, full, rank, first_row);
+    start_feed(feed);
+    Entries next;
+    if (warp == 0) next.load(a, first_row);
+    if (blocks > 1) cluster_wait();
+    int odd = 0;
+    bool ok = true;
+    for (long long n = first_row; n < a.N; n += f.clusters, odd ^= 1) {
+        const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+        if (warp == 0) {
+            next.finish<TAIL>(a, t, rank == 0);
+            next.load(a, n + f.clusters);          // in flight during this row
+        }
+        __syncthreads();
+        const int kept_at = feed.at;               // KEEP: slot of the share's first chunk
+        Stat st{neg_inf(), 0.0f, 0.0f};
+        float z_in[(QS_MAX_TOP + 127) / 128];      // this thread's entries (k = thread + i nt) that the share holds
+#pragma unroll
+        for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) z_in[i] = neg_inf();
+        for (int c = 0; c < f.chunks; ++c) {
+            uint4 q[VPT];
+            ok &= feed.wait();
+            // logits at the ids of this chunk; with the tail their places leave the sum, their own statistics join later
+            const int v0 = r.v0 + c * f.chunk, v1 = min(v0 + f.chunk, r.v1);
+            T* slot = reinterpret_cast<T*>(ring + feed.at * f.chunk);
+            bool mine = false;
+#pragma unroll
+            for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) {
+                const int k = (int)threadIdx.x + i * nt;
+                if (k >= a.K || t.id[k] == NO_ID) continue;
+                const int place = (int)t.id[k] + r.head, vec = place / E;
+                if (vec < v0 || vec >= v1) continue;
+                z_in[i] = feed.inside(r, vec) ? to_float(slot[place - v0 * E]) : to_float(r.z[t.id[k]]);
+                t.z[k] = z_in[i];
+                mine = true;
+                if (rank != 0) remote_store(remote_addr(&z_at[odd][k], 0), __float_as_uint(z_in[i]));
+                else z_at[odd][k] = z_in[i];
             }
+            if (TAIL) {
+                __syncthreads();                   // an id given twice is read twice
+                if (mine) {
+#pragma unroll
+                    for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) {
+                        const int k = (int)threadIdx.x + i * nt;
+                        if (k >= a.K || t.id[k] == NO_ID) continue;
+                        const int place = (int)t.id[k] + r.head, vec = place / E;
+                        if (vec >= v0 && vec < v1 && feed.inside(r, vec)) slot[place - v0 * E] = from_float<T>(neg_inf());
+                    }
+                    fence_async_smem();            // the slot's next copy comes by the other proxy
+                }
+                __syncthreads();
+            }
+            feed.template read<VPT>(r, c, feed.at, q);
+            if (TAIL && (v0 == 0 || v1 * E - r.head > r.V)) {      // vectors that were not copied: the tensor's first and last
+#pragma unroll
+                for (int j = 0; j < VPT; ++j) {
+                    const int vec = v0 + j * nt + (int)threadIdx.x;
+                    if (j * nt + (int)threadIdx.x >= f.chunk || vec >= v1 || feed.inside(r, vec)) continue;
+                    for (int k = 0; k < a.K; ++k)
+                        if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
+                }
+            }
+            feed.next();
+            if (!KEEP) {
+                __syncthreads();
+                if (threadIdx.x == 0) feed.issue();
+            }
+            take_chunk<T, VPT, false>(st, q, c2);
+        }
+        const int readers = a.grad ? blocks : 1;   // blocks that need the row's statistics
+        const Stat w = join_warp<false>(st, c2);
+        const float4 sent = make_float4(w.m, w.s, 0.0f, 0.0f);
+        if (blocks == 1) {
+            if (lane == 0) part[odd][warp] = sent;
+        } else if (lane < readers) {
+            remote_store(remote_addr(&part[odd][rank * warps + warp], lane), sent);
+        }
+        if (TAIL) {
+            // an id given twice is one column
             __syncthreads();
+            if (warp == 0) {
+                float z[Entries::PER], m = neg_inf(), s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < Entries::PER; ++i) {
+                    const int k = lane + 32 * i;
+                    z[i] = neg_inf();
+                    if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
+                    bool first = true;
+                    for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
+                    if (first) z[i] = t.z[k];
+                    m = fmaxf(m, z[i]);
+                }
+                m = warp_max(m);
+#pragma unroll
+                for (int i = 0; i < Entries::PER; ++i) s += ex2((z[i] - shift_of(m)) * c2);
+                s = warp_sum(s);
+                const float4 v = make_float4(m, s, 0.0f, 0.0f);
+                if (blocks == 1) {
+                    if (lane == 0) in_part[odd][0] = v;
+                } else if (lane < readers) {
+                    remote_store(remote_addr(&in_part[odd][rank], lane), v);
+                }
+            }
+        }
+        if (__syncthreads_or(!ok)) {               // a copy never came
+            if (threadIdx.x == 0) feed.give_up(a.status);
+            return;
+        }
+        if (blocks > 1) {
+            cluster_arrive();
+            cluster_wait();
+        }
+        if (warp == 0 && (a.grad || rank == 0)) {
+            Stat v = join_parts(part[odd], warps * blocks, c2);
+            float log_tail = 0.0f;
+            if (TAIL) {
+                const Stat in = join_parts(in_part[odd], blocks, c2);
+                const float m = fmaxf(v.m, in.m);
+                const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
+                const float s = x.s + y.s;
+                // log of the share outside: near 1 the difference of two logs would cancel
+                log_tail = v.m == neg_inf() && v.s == 0.0f ? neg_inf() : fmaf(v.m - m, a.scale, logf(v.s) - logf(s));
+                if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
+                v = Stat{m, s, 0.0f};
+            }
+            const bool empty = v.m == neg_inf() && v.s == 0.0f;
+            const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
+            const Slope s = slope_of<TAIL>(a, n, t, lse, log_tail);
+            if (lane == 0) {
+                row_m = shift_of(v.m);
+                row_by = empty ? 0.0f : 1.0f / v.s;
+                row = s;
+            }
+            if (rank == 0) {
+                float loss = 0.0f;
+                bool beyond = false;               // an entry where the student has no mass at all
+                for (int k = lane; k < a.K; k += 32) {
+                    if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
+                    const float lp = empty ? neg_inf() : fmaf(z_at[odd][k] - v.m, a.scale, -ls);
+                    beyond |= lp == neg_inf();
+                    loss = fmaf(t.q[k], t.logq[k] - lp, loss);
+                }
+                loss = warp_sum(loss);
+                // a mean of log p at a mask of the lowest value: only its rounding passes the largest number
+                if (!__any_sync(~0u, beyond) && loss == -neg_inf()) loss = FLT_MAX;
+                if (TAIL && t.rest != 0.0f) loss = fmaf(t.rest, logf(t.rest) - log_tail, loss);
+                if (lane == 0) {
+                    if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
+                    if (a.lse) a.lse[n] = lse;
+                    if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
+                }
+            }
+        }
+        __syncthreads();
+        if (!a.grad) continue;                     // (without a gradient nothing is kept)
+        const Slope s = row;
+        const float m = row_m, by = row_by;
+        T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
+        const f2 minus = make_f2(-m, -m), c2s = make_f2(c2, c2);
+        int at = kept_at;
+        for (int c = 0; c < f.chunks; ++c) {
+            uint4 q[VPT];
+            if (!KEEP) {
+                ok &= feed.wait();                 // (looked at with the next row's)
+                at = feed.at;
+                feed.next();
+            }
+            feed.template read<VPT>(r, c, at, q);
+            const int v0 = r.v0 + c * f.chunk, v1 = min(v0 + f.chunk, r.v1);
+            __syncthreads();                       // all have read the slot
+            if (threadIdx.x == 0) feed.issue();
+            if (KEEP && ++at == f.slots) at = 0;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
-                const uint32_t bits = named[j * nt + threadIdx.x];
-                if (bits)
-                    for (int i = 0; i < E; ++i)
-                        if (bits >> i & 1) drop<T>(q[j], i);
+                const int vec = v0 + j * nt + (int)threadIdx.x;
+                if (j * nt + (int)threadIdx.x >= f.chunk || vec >= v1) continue;
+                f2 d[E / 2];
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) d[i] = mul2(add2(Vec<T>::pair(q[j], i), minus), c2s);
+                store_vec(r, out, vec, slope_vec<T, TAIL>(d, s, by), a.wide);
             }
         }
-        const Stat now = warp_stat<T, VPT, false>(q, thread_max_of<T, VPT>(q), c2);
-        if (ONE) {
-            st = now;
-        } else {
-            const float m = fmaxf(st.m, now.m);
-            st = Stat{m, rescale(st, m, c2).s + rescale(now, m, c2).s, 0.0f};
-            if (TAIL) __syncthreads();
-        }
+        __syncthreads();                           // the ids' places are written last
+        for (int k = threadIdx.x; k < a.K; k += nt)
+            if (t.id[k] != NO_ID && r.holds((int)t.id[k]))
+                out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2((t.z[k] - m) * c2) * by));
+        __syncthreads();                           // the entries are written anew
     }
-    const int readers = a.grad ? blocks : 1;       // blocks that need the row's statistics
-    if (blocks > 1) cluster_wait();
-    const float4 sent = make_float4(st.m, st.s, 0.0f, 0.0f);
-    if (blocks == 1) {
-        if (lane == 0) part[warp] = sent;
-    } else if (lane < readers) {
-        remote_store(remote_addr(&part[rank * warps + warp], lane), sent);
-    }
-    if (TAIL && warp == 0) {
-        float z[QS_MAX_TOP / 32], m = neg_inf(), s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < QS_MAX_TOP / 32; ++i) {
-            const int k = lane + 32 * i;
-            z[i] = neg_inf();
-            if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
-            bool first = true;                     // an id given twice is one column
-            for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
-            if (first) z[i] = t.z[k];
-            m = fmaxf(m, z[i]);
-        }
-        m = warp_max(m);
-#pragma unroll
-        for (int i = 0; i < QS_MAX_TOP / 32; ++i) s += ex2((z[i] - shift_of(m)) * c2);
-        s = warp_sum(s);
-        const float4 v = make_float4(m, s, 0.0f, 0.0f);
-        if (blocks == 1) {
-            if (lane == 0) in_part[0] = v;
-        } else if (lane < readers) {
-            remote_store(remote_addr(&in_part[rank], lane), v);
-        }
-    }
-    if (blocks == 1) {
-        __syncthreads();
-    } else {
-        cluster_arrive();
-        if (!a.grad && rank != 0) return;          // nothing is written into this block's memory
-        cluster_wait();
-    }
-    if (warp == 0) {
-        Stat v = join_parts(part, warps * blocks, c2);
-        float log_tail = 0.0f;
-        if (TAIL) {
-            const Stat in = join_parts(in_part, blocks, c2);
-            const float m = fmaxf(v.m, in.m);
-            const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
-            const float s = x.s + y.s;
-            // log of the share outside: near 1 the difference of two logs would cancel
-            log_tail = v.m == neg_inf() && v.s == 0.0f ? neg_inf() : fmaf(v.m - m, a.scale, logf(v.s) - logf(s));
-            if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
-            v = Stat{m, s, 0.0f};
-        }
-        const bool empty = v.m == neg_inf() && v.s == 0.0f;
-        const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
-        const Slope s = slope_of<TAIL>(a, n, t, lse, log_tail);
-        if (lane == 0) {
-            row_m = shift_of(v.m);
-            row_by = empty ? 0.0f : 1.0f / v.s;
-            row = s;
-        }
-        if (rank == 0) {
-            float loss = 0.0f;
-            bool beyond = false;                   // an entry where the student has no mass at all
-            for (int k = lane; k < a.K; k += 32) {
-                if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
-                const float lp = empty ? neg_inf() : fmaf(t.z[k] - v.m, a.scale, -ls);
-                beyond |= lp == neg_inf();
-                loss = fmaf(t.q[k], t.logq[k] - lp, loss);
-            }
-            loss = warp_sum(loss);
-            // a mean of log p at a mask of the lowest value: only its rounding passes the largest number
-            if (!__any_sync(~0u, beyond) && loss == -neg_inf()) loss = FLT_MAX;
-            if (TAIL && t.rest != 0.0f) loss = fmaf(t.rest, logf(t.rest) - log_tail, loss);
-            if (lane == 0) {
-                if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
-                if (a.lse) a.lse[n] = lse;
-                if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
-            }
-        }
-    }
-    if (!a.grad) return;
-    __syncthreads();
-    const Slope s = row;
-    const float m = row_m, by = row_by;
-    T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
-    const f2 minus = make_f2(-m, -m), c = make_f2(c2, c2);
-    for (int base = r.v0; base < r.v1; base += nt * VPT) {
-        if (!ONE) load_share<T, VPT>(r, base, nt, q);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int vec = base + j * nt + (int)threadIdx.x;
-            if (vec >= r.v1) continue;
-            f2 d[E / 2];
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) d[i] = mul2(add2(Vec<T>::pair(q[j], i), minus), c);
-            store_vec(r, out, vec, slope_vec<T, TAIL>(d, s, by), a.wide);
-        }
-    }
-    __syncthreads();                               // the ids' places are written last
-    for (int k = threadIdx.x; k < a.K; k += nt)
-        if (t.id[k] != NO_ID && r.holds((int)t.id[k]))
-            out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2((t.z[k] - m) * c2) * by));
+    if (__syncthreads_or(!ok) && threadIdx.x == 0) feed.give_up(a.status);
 }
 
-template <class T, int VPT, bool TAIL>
+template <class T, int VG, bool TAIL>
 __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
     constexpr int E = Vec<T>::E;
     __shared__ TeacherShared t;
     const int nt = blockDim.x;
     const long long n = a.row0 + blockIdx.x / a.blocks;
     const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
-    uint4 q[VPT];
-    load_share<T, VPT>(r, r.v0, nt, q);
-    if (threadIdx.x < 32) load_teacher<T, TAIL>(a, n, r, false, t);
+    uint4 q[VG];
+    load_share<T, VG>(r, r.v0, nt, q);
+    if (threadIdx.x < 32) {
+        Entries e;
+        e.load(a, n);
+        e.finish<TAIL>(a, t, r.v0 == 0);
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.K; k += nt)
+        if (t.id[k] != NO_ID && r.holds((int)t.id[k])) t.z[k] = to_float(r.z[t.id[k]]);
     const float lse = a.in_lse[n], log_tail = TAIL ? a.in_log_tail[n] : 0.0f;
     __syncthreads();
     const Slope s = slope_of<TAIL>(a, n, t, lse, log_tail);
@@ -646,7 +757,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
     const float shift = s.empty ? LOW_EXP : -lse;
     const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
+    for (int j = 0; j < VG; ++j) {
         const int vec = r.v0 + j * nt + (int)threadIdx.x;
         if (vec >= r.v1) continue;
         f2 d[E / 2];
@@ -661,86 +772,109 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
 }
 
 // ------------------------------------------------------------------ launches
-// Threads per block, vectors per thread and blocks per row
-struct Shape { int nt, vpt, blocks; bool one; };
-
 // most vectors of a row of V, whatever its alignment
 long long most_vectors(int64_t V, int size) { return (V + 2 * (16 / size - 1)) / (16 / size); }
 
-// A row in the registers of one cluster if it fits, else in rounds
-Shape row_shape(int64_t V, int size) {
-    const long long n = most_vectors(V, size);
-    if (n <= 128 * 2) return Shape{128, 2, 1, true};
-    if (n <= 128 * 8) return Shape{128, 8, 1, true};
-    if (n <= 256 * 8 * MAX_BLOCKS) return Shape{256, 8, (int)((n + 256 * 8 - 1) / (256 * 8)), true};
-    if (n <= 512 * 8 * MAX_BLOCKS) return Shape{512, 8, (int)((n + 512 * 8 - 1) / (512 * 8)), true};
-    return Shape{512, 8, MAX_BLOCKS, false};
-}
-// independent blocks, each with one round of its row
-Shape grad_shape(int64_t V, int size) {
-    const long long n = most_vectors(V, size);
-    if (n <= 128 * 2) return Shape{128, 2, 1, true};
-    if (n <= 128 * 4) return Shape{128, 4, 1, true};
-    return Shape{256, 4, (int)((n + 256 * 4 - 1) / (256 * 4)), true};
+constexpr int SMS = 148;
+constexpr int RING_BYTES = 64 * 1024;      // ring of a 256-thread block: three to an SM
+constexpr int TOP_RING_BYTES = 48 * 1024;  // beside the lists of candidates
+
+struct Shape { int nt; FeedArgs f; int grid; size_t smem; bool keep; };
+
+// Blocks and chunks for rows of `vectors`.  `keep`: the share has to fit the ring
+Shape row_shape(int64_t N, long long vectors, bool keep, int ring_bytes) {
+    Shape s;
+    s.nt = vectors <= 128 * VPT ? 128 : MAX_THREADS;
+    const long long ring = ring_bytes / (s.nt == 128 ? 32 : 16);                 // vectors of a ring
+    const int chunk = s.nt * VPT;
+    const long long chunks = (vectors + chunk - 1) / chunk;                      // of a whole row
+    // few rows: as many blocks per row as fill the SMs, each with a chunk at least
+    long long blocks = 1;
+    while (blocks < MAX_BLOCKS && N * blocks * 2 <= 2 * SMS && blocks * 2 <= chunks) blocks *= 2;
+    if (keep)
+        while (blocks < MAX_BLOCKS && (vectors + blocks - 1) / blocks > ring) ++blocks;
+    const long long share = (vectors + blocks - 1) / blocks;
+    s.keep = keep && share <= ring;
+    s.f.blocks = (int)blocks;
+    s.f.chunks = (int)((share + chunk - 1) / chunk);
+    s.f.chunk = s.f.chunks == 1 ? (int)share : chunk;
+    const long long fit = ring / s.f.chunk;
+    s.f.slots = (int)(fit < MAX_SLOTS ? fit : MAX_SLOTS);
+    s.f.passes = keep && !s.keep ? 2 : 1;
+    s.smem = (size_t)16 * s.f.slots * s.f.chunk;
+    const int resident = s.nt == 128 ? 6 : 3;                                    // blocks per SM
+    const long long clusters = (long long)SMS * resident / blocks;
+    s.f.clusters = N < clusters ? N : clusters;
+    s.grid = (int)(s.f.clusters * blocks);
+    return s;
 }
 
 template <class K>
-cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaStream_t st) {
+cudaError_t launch_stream(K kernel, const Shape& s, const RowArgs& a, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)s.grid);
+    cfg.blockDim = dim3((unsigned)s.nt);
+    cfg.dynamicSmemBytes = s.smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)s.f.blocks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = s.f.blocks > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a, s.f);
+}
+
+// the backward calls: independent blocks, each with up to VG vectors per thread of its row
+struct GradShape { int nt, vg, blocks; };
+GradShape grad_shape(int64_t V, int size) {
+    const long long n = most_vectors(V, size);
+    if (n <= 128 * 2) return GradShape{128, 2, 1};
+    if (n <= 128 * 4) return GradShape{128, 4, 1};
+    return GradShape{256, 4, (int)((n + 256 * 4 - 1) / (256 * 4))};
+}
+template <class K>
+cudaError_t launch_grad(K kernel, const GradShape& s, RowArgs a, cudaStream_t st) {
     a.blocks = s.blocks;
     const long long most = 0x7fffffffll / s.blocks;              // rows per launch
     for (a.row0 = 0; a.row0 < a.N; a.row0 += most) {
         const long long rows = a.N - a.row0 < most ? a.N - a.row0 : most;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(rows * s.blocks));
-        cfg.blockDim = dim3((unsigned)s.nt);
-        cfg.stream = st;
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = (unsigned)s.blocks;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = cluster && s.blocks > 1 ? 1 : 0;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+        kernel<<<(unsigned)(rows * s.blocks), s.nt, 0, st>>>(a);
+        const cudaError_t e = cudaPeekAtLastError();
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
 template <class T>
-cudaError_t launch_token_logp(const RowArgs& a, cudaStream_t st) {
-    const Shape s = row_shape(a.V, sizeof(T));
-    const bool top = a.K > 0;
-    if (s.vpt == 2) return launch_rows(top ? token_logp_kernel<T, 2, true, true> : token_logp_kernel<T, 2, true, false>, s, a, true, st);
-    if (s.one) return launch_rows(top ? token_logp_kernel<T, 8, true, true> : token_logp_kernel<T, 8, true, false>, s, a, true, st);
-    return launch_rows(top ? token_logp_kernel<T, 8, false, true> : token_logp_kernel<T, 8, false, false>, s, a, true, st);
+cudaError_t launch_token_logp(RowArgs a, cudaStream_t st) {
+    const Shape s = row_shape(a.N, most_vectors(a.V, sizeof(T)), false, a.K > 0 ? TOP_RING_BYTES : RING_BYTES);
+    // maxima per warp that bound the K-th alternative: about four for each alternative asked for
+    a.groups = 1;
+    while (a.groups < 32 && s.nt / 32 * a.groups < 4 * a.K) a.groups *= 2;
+    return launch_stream(a.K > 0 ? token_logp_kernel<T, true> : token_logp_kernel<T, false>, s, a, st);
 }
 template <class T>
 cudaError_t launch_token_logp_grad(const RowArgs& a, cudaStream_t st) {
-    const Shape s = grad_shape(a.V, sizeof(T));
+    const GradShape s = grad_shape(a.V, sizeof(T));
     const bool ent = a.g2 != nullptr;
-    if (s.vpt == 2) return launch_rows(ent ? token_logp_grad_kernel<T, 2, true> : token_logp_grad_kernel<T, 2, false>, s, a, false, st);
-    return launch_rows(ent ? token_logp_grad_kernel<T, 4, true> : token_logp_grad_kernel<T, 4, false>, s, a, false, st);
+    if (s.vg == 2) return launch_grad(ent ? token_logp_grad_kernel<T, 2, true> : token_logp_grad_kernel<T, 2, false>, s, a, st);
+    return launch_grad(ent ? token_logp_grad_kernel<T, 4, true> : token_logp_grad_kernel<T, 4, false>, s, a, st);
 }
 template <class T>
 cudaError_t launch_distill(const RowArgs& a, bool tail, cudaStream_t st) {
-    const Shape s = row_shape(a.V, sizeof(T));
-    if (s.vpt == 2) return launch_rows(tail ? distill_kernel<T, 2, true, true> : distill_kernel<T, 2, true, false>, s, a, true, st);
-    if (s.one) return launch_rows(tail ? distill_kernel<T, 8, true, true> : distill_kernel<T, 8, true, false>, s, a, true, st);
-    return launch_rows(tail ? distill_kernel<T, 8, false, true> : distill_kernel<T, 8, false, false>, s, a, true, st);
+    const Shape s = row_shape(a.N, most_vectors(a.V, sizeof(T)), a.grad != nullptr, RING_BYTES);
+    // without a gradient nothing is kept and nothing comes by twice
+    if (s.keep) return launch_stream(tail ? distill_kernel<T, true, true> : distill_kernel<T, true, false>, s, a, st);
+    return launch_stream(tail ? distill_kernel<T, false, true> : distill_kernel<T, false, false>, s, a, st);
 }
 template <class T>
 cudaError_t launch_distill_grad(const RowArgs& a, bool tail, cudaStream_t st) {
-    const Shape s = grad_shape(a.V, sizeof(T));
-    if (s.vpt == 2) return launch_rows(tail ? distill_grad_kernel<T, 2, true> : distill_grad_kernel<T, 2, false>, s, a, false, st);
-    return launch_rows(tail ? distill_grad_kernel<T, 4, true> : distill_grad_kernel<T, 4, false>, s, a, false, st);
-}
-
-// how many maxima per warp bound the K-th alternative: about four for each alternative asked for
-int groups_for(int K, const Shape& s) {
-    const int warps = s.nt / 32 * s.blocks;
-    int g = 1;
-    while (g < 32 && warps * g < 4 * K && warps * g * 2 <= MAX_GROUPS) g *= 2;
-    return g;
+    const GradShape s = grad_shape(a.V, sizeof(T));
+    if (s.vg == 2) return launch_grad(tail ? distill_grad_kernel<T, 2, true> : distill_grad_kernel<T, 2, false>, s, a, st);
+    return launch_grad(tail ? distill_grad_kernel<T, 4, true> : distill_grad_kernel<T, 4, false>, s, a, st);
 }
 
 int status_of(cudaError_t e) {
@@ -788,7 +922,6 @@ int qs_token_logp(int64_t N, int64_t V, const void* logits, int type, int64_t ro
     a.N = N; a.V = V; a.logits = logits; a.stride = row_stride; a.scale = scale;
     a.tok = Ids{tokens, token_type == QS_I64}; a.K = top;
     a.logp = logp; a.lse = lse; a.entropy = entropy; a.top_ids = top_ids; a.top_logp = top_logp; a.status = status;
-    a.groups = groups_for(top, row_shape(V, size_of_type(type)));
     return QS_BY_TYPE(launch_token_logp, type, a, static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -1,14 +1,17 @@
-// A row of logits in the registers of one thread block, or of a cluster of blocks.
+// Rows of logits as streams of 16-byte vectors.
 //
 // A row is cut into 16-byte vectors counted from the 16-byte boundary at or before its first element, so that
-// rows of any alignment are read with wide loads; the first and the last vector hold fewer elements of the
-// row and are read one by one (places outside the row count as -inf).  Block b of the row's cluster takes a
-// contiguous share of the vectors, thread t of it the vectors t, t + NT, t + 2 NT, .. of the share.
+// rows of any alignment are read with wide accesses; places of the first and the last vector outside the row
+// count as -inf.  A row belongs to one block or to a cluster of blocks, each with a contiguous share of the
+// vectors; blocks stay and take row after row.  A Feed brings a block's shares through a ring of chunks in
+// shared memory with bulk copies, several chunks ahead and across rows, so that the memory never waits
+// for a row's last steps.
 //
 // Statistics: with y = scale * z, a part of a row is held as (m, s, u): m = max z, s = sum e and
 // u = sum e * d with d = (z - m) * scale * log2(e) and e = 2^d.  Parts join exactly up to rounding; the
 // difference z - m is formed first, so that a row at the type's lowest value loses nothing.
 #pragma once
+#include "qs_bulk.cuh"
 #include "qs_lm.cuh"
 
 namespace qs {
@@ -207,6 +210,115 @@ __device__ __forceinline__ void store_vec(const Share<T>& r, T* out, int vec, co
     }
 }
 
+// ------------------------------------------------------------------ chunks of rows through shared memory
+struct FeedArgs {
+    int blocks;                // of a row's cluster
+    int chunks;                // per share
+    int chunk;                 // vectors per chunk
+    int slots;                 // chunks the ring holds
+    int passes;                // times a share is read
+    long long clusters;        // rows row, row + clusters, .. are one cluster's
+};
+constexpr int MAX_SLOTS = 8;
+
+template <class T>
+struct Feed {
+    const void* logits;
+    long long stride, N, V;
+    FeedArgs f;
+    uint4* ring;
+    uint64_t* full;
+    int rank;
+    // what is issued next (one thread), and the slot that is read next
+    long long row;
+    int pass, chunk, slot;
+    long long issued, taken;
+    int at;
+    uint32_t parity;
+
+    __device__ __forceinline__ Feed(const void* z, long long st, long long n, long long v, const FeedArgs& fa, uint4* r, uint64_t* bars, int rk,
+                                    long long first)
+        : logits(z), stride(st), N(n), V(v), f(fa), ring(r), full(bars), rank(rk), row(first), pass(0), chunk(0), slot(0), issued(0), taken(0), at(0), parity(0) {}
+
+    // whether a vector's 16 bytes all belong to the tensor (its first and last vector may not)
+    __device__ __forceinline__ bool inside(const Share<T>& r, int vec) const {
+        const T* p = r.z + r.first(vec);
+        return p >= static_cast<const T*>(logits) && p + Vec<T>::E <= static_cast<const T*>(logits) + (N - 1) * stride + V;
+    }
+    // the next chunk of the sequence into the next slot
+    __device__ void issue() {
+        if (row >= N) return;
+        const Share<T> r(logits, stride, row, V, rank, f.blocks);
+        const int first = r.v0 + chunk * f.chunk;
+        int lo = first, hi = min(first + f.chunk, r.v1);
+        if (lo < hi && !inside(r, lo)) ++lo;
+        if (lo < hi && !inside(r, hi - 1)) --hi;
+        const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16u : 0u;
+        ++issued;
+        mbar_expect(&full[slot], bytes);
+        if (bytes) bulk_load(ring + slot * f.chunk + (lo - first), reinterpret_cast<const uint4*>(r.z - r.head) + lo, bytes, &full[slot]);
+        if (++slot == f.slots) slot = 0;
+        if (++chunk < f.chunks) return;
+        chunk = 0;
+        if (++pass < f.passes) return;
+        pass = 0;
+        row += f.clusters;
+    }
+    __device__ __forceinline__ bool wait() const { return mbar_wait(&full[at], parity); }
+    // the thread that issues, after a wait that ran out: says so, and lets the copies under way arrive (each wait is
+    // bounded) before the block's memory goes to another
+    __device__ void give_up(int* status) {
+        flag_status(status, QS_TIMEOUT);
+        for (; taken < issued; next()) wait();
+    }
+    __device__ __forceinline__ void next() {
+        ++taken;
+        if (++at == f.slots) {
+            at = 0;
+            parity ^= 1u;
+        }
+    }
+    // this thread's vectors of a landed chunk; places outside the row are -inf
+    template <int VPT>
+    __device__ __forceinline__ void read(const Share<T>& r, int c, int slot_at, uint4 (&q)[VPT]) const {
+        const int first = r.v0 + c * f.chunk, end = min(first + f.chunk, r.v1), nt = blockDim.x;
+        const uint4* p = ring + slot_at * f.chunk;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int i = j * nt + (int)threadIdx.x;
+            q[j] = all_lowest<T>();
+            if (i < f.chunk && first + i < end) q[j] = p[i];
+        }
+        // only a row's first and last vector: a look at the share's ends tells whether the chunk can hold them
+        if (first != 0 && end * Vec<T>::E - r.head <= r.V) return;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int i = j * nt + (int)threadIdx.x, vec = first + i, e0 = r.first(vec);
+            if (i >= f.chunk || vec >= end || r.whole(vec)) continue;
+            if (!inside(r, vec)) q[j] = edge_vec(r, vec);
+            else
+                for (int e = 0; e < Vec<T>::E; ++e)
+                    if (e0 + e < 0 || e0 + e >= r.V) drop<T>(q[j], e);
+        }
+    }
+    // a vector that is not whole, element by element
+    static __device__ uint4 edge_vec(const Share<T>& r, int vec) {
+        uint4 q = all_lowest<T>();
+        uint32_t* w = &q.x;
+        const int e0 = r.first(vec);
+#pragma unroll
+        for (int i = 0; i < Vec<T>::E; ++i) {
+            if (e0 + i < 0 || e0 + i >= r.V) continue;
+            if (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(r.z)[e0 + i];
+            else {
+                const uint32_t h = reinterpret_cast<const uint16_t*>(r.z)[e0 + i];
+                w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (h << 16) : (w[i / 2] & 0xffff0000u) | h;
+            }
+        }
+        return q;
+    }
+};
+
 // ------------------------------------------------------------------ statistics
 struct Stat { float m, s, u; };
 
@@ -246,22 +358,32 @@ __device__ __forceinline__ Stat rescale(Stat a, float m, float c2) {
     return Stat{m, a.s * w, w * fmaf(a.s, d, a.u)};
 }
 
-// every warp's statistics of the share; lane 0's are the warp's
-template <class T, int VPT, bool ENT>
-__device__ __forceinline__ Stat warp_stat(const uint4 (&q)[VPT], float thread_max, float c2) {
-    const float m = warp_max(thread_max);
-    f2 s = make_f2(0.0f, 0.0f), u = s;
-    add_exps<T, VPT, ENT>(q, m, c2, s, u);
-    const float2 ps = parts(s), pu = parts(u);
-    return Stat{m, warp_sum(ps.x + ps.y), ENT ? warp_sum(pu.x + pu.y) : 0.0f};
-}
-
 template <class T, int VPT>
 __device__ __forceinline__ float thread_max_of(const uint4 (&q)[VPT]) {
     uint32_t m = max_of_words<T>(q[0]);
 #pragma unroll
     for (int j = 1; j < VPT; ++j) m = Vec<T>::max_word(m, max_of_words<T>(q[j]));
     return Vec<T>::top(m);
+}
+
+// a thread's running statistics take in the vectors of a chunk
+template <class T, int VPT, bool ENT>
+__device__ __forceinline__ void take_chunk(Stat& st, const uint4 (&q)[VPT], float c2) {
+    const float m = fmaxf(st.m, thread_max_of<T, VPT>(q));
+    if (m > st.m) st = rescale(st, m, c2);
+    f2 s = make_f2(st.s, 0.0f), u = make_f2(st.u, 0.0f);
+    add_exps<T, VPT, ENT>(q, m, c2, s, u);
+    const float2 ps = parts(s), pu = parts(u);
+    st.s = ps.x + ps.y;
+    if (ENT) st.u = pu.x + pu.y;
+}
+
+// the warp's statistics from its threads'
+template <bool ENT>
+__device__ __forceinline__ Stat join_warp(Stat st, float c2) {
+    const float m = warp_max(st.m);
+    const Stat r = rescale(st, m, c2);
+    return Stat{m, warp_sum(r.s), ENT ? warp_sum(r.u) : 0.0f};
 }
 
 // one warp joins n parts
