@@ -10,10 +10,11 @@
 // A column at -inf has p = 0 and adds nothing; a row without any other column has lse = -inf.
 //
 // All of these are bound by the memory that holds the logits: each must read the row, and the gradients write
-// one.  So a row is read once, through a ring in shared memory that stays full (qs_rows.cuh).  Statistics and
-// alternatives are taken as the chunks come by; the loss that also gives its gradient keeps the row's chunks in the
-// shared memory of a cluster until the statistics are joined, and each chunk's slot takes the next row's chunk as
-// soon as its gradient is written.  The backward calls, which start from a saved lse, are one pass per vector.
+// one.  So a row is read once.  Statistics and alternatives are taken as the vectors come by, with plain loads of
+// many resident warps (64 warps of 32 registers read 6.8 TB/s with all the arithmetic; the same loop behind a ring of
+// bulk copies and 24 warps, 4.5).  The loss that also gives its gradient keeps the row in the shared memory of a cluster's
+// blocks, one bulk copy each, until the statistics are joined.  The backward calls, which start from a saved lse,
+// are one pass per vector.
 #include "qs_rows.cuh"
 
 namespace {
@@ -24,7 +25,8 @@ constexpr int MAX_BLOCKS = 8;              // blocks of a row's cluster
 constexpr int MAX_THREADS = 256;
 constexpr int MAX_WARPS = MAX_THREADS / 32;
 constexpr int PARTS = MAX_BLOCKS * MAX_WARPS;
-constexpr int VPT = 4;                     // vectors per thread and chunk
+constexpr int VPT = 4;                     // vectors per thread and batch
+constexpr int MOST = QS_MAX_TOP + QS_MAX_TOP / 4 + 16;      // candidates ranked against one another
 constexpr int CANDS = 1024;                // candidates a block keeps, and a row's blocks send in all (>= MAX_BLOCKS QS_MAX_TOP)
 
 struct RowArgs {
@@ -45,26 +47,17 @@ struct RowArgs {
     float g_all;                           // where g1 is null
     void* grad; long long grad_stride;
     int wide;                              // the gradient's rows lie like the logits' rows within 16 bytes
-    int blocks;                            // blocks per row (backward calls)
+    int blocks;                            // blocks per row
     int groups;                            // maxima per warp that bound the K-th alternative
     int* status;
 };
-
-// barriers of the ring, and its first chunks on their way
-template <class T>
-__device__ __forceinline__ void start_feed(Feed<T>& feed) {
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < feed.f.slots; ++i) mbar_init(&feed.full[i], 1);
-        fence_async_smem();
-        for (int i = 0; i < feed.f.slots; ++i) feed.issue();
-    }
-    __syncthreads();
-}
 
 // ------------------------------------------------------------------ log probabilities
 // Places that a cut takes: key above the cut's, or equal to it with a column at or below the cut's
 struct Cut { uint32_t key, idx; };
 __device__ __forceinline__ bool takes(Cut c, uint32_t key, uint32_t idx) { return key > c.key || (key == c.key && idx <= c.idx); }
+
+__device__ __forceinline__ bool takes(Cut c, unsigned long long e) { return takes(c, (uint32_t)(e >> 32), ~(uint32_t)e); }
 
 // a sum over the block's threads
 __device__ __forceinline__ int block_count(int mine, int* sums) {
@@ -108,12 +101,65 @@ __device__ Cut find_cut(int K, int most, uint32_t lo, uint32_t columns, Count co
 
 struct TopShared {
     uint32_t group[32 * MAX_WARPS];        // keys of the block's group maxima so far
-    unsigned long long list[CANDS];        // candidates (key, ~column) of the block's share
-    unsigned long long merged[CANDS];      // of a cluster's blocks, block b's at b * CANDS / blocks (first block)
-    int count[MAX_BLOCKS];                 // of which there are
-    int n, kept, sums[MAX_WARPS];          // candidates in the list, and before the current chunk
-    uint32_t bound, reached;               // keys below `bound` are no alternatives; K elements so far reach `reached`
+    unsigned long long list[CANDS];        // candidates (key, ~column) of the block's share, then of the cluster's
+    unsigned long long merged[CANDS];      // what the cluster's blocks have left, block b's at b * CANDS / blocks (first block)
+    int count[MAX_BLOCKS];
+    unsigned long long last[MOST];         // what is left of the list for the ranking
+    int n, left, sums[MAX_WARPS];          // candidates in the list; entries in `last`
+    uint32_t bound;                        // keys below it are no alternatives
 };
+
+// One warp: between K and `most` (<= MOST) of the list's n entries, the largest, into `last`; all if there are no more than
+// that.  Bisection over the keys, then, where equal keys alone are more, over the columns
+__device__ void shrink_list(const unsigned long long* list, int n, int K, int most, uint32_t columns, unsigned long long* last, int* left) {
+    const int lane = threadIdx.x & 31;
+    Cut cut{0, 0xffffffffu};
+    if (n > most) {
+        uint32_t lo = 0xffffffffu, hi = 0;
+        for (int i = lane; i < n; i += 32) {
+            const uint32_t k = (uint32_t)(list[i] >> 32);
+            lo = min(lo, k);
+            hi = max(hi, k);
+        }
+        lo = __reduce_min_sync(~0u, lo);
+        hi = __reduce_max_sync(~0u, hi) + 1;
+        bool done = false;
+        auto count = [&](Cut c) {
+            int k = 0;
+            for (int i = lane; i < n; i += 32) k += takes(c, list[i]);
+            return __reduce_add_sync(~0u, k);
+        };
+        while (hi - lo > 1 && !done) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            const int c = count(Cut{mid, 0xffffffffu});
+            if (c >= K) {
+                lo = mid;
+                done = c <= most;
+            } else {
+                hi = mid;
+            }
+        }
+        cut = Cut{lo, 0xffffffffu};
+        if (!done && count(cut) > most) {
+            uint32_t a = 0, b = columns - 1;
+            while (a < b) {
+                const uint32_t mid = a + (b - a) / 2;
+                if (count(Cut{lo, mid}) >= K) b = mid;
+                else a = mid + 1;
+            }
+            cut.idx = b;
+        }
+    }
+    int at = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const unsigned long long e = i0 + lane < n ? list[i0 + lane] : 0ull;
+        const bool in = i0 + lane < n && takes(cut, e);
+        const uint32_t who = __ballot_sync(~0u, in);
+        if (in) last[at + __popc(who & ((1u << lane) - 1u))] = e;
+        at += __popc(who);
+    }
+    if (lane == 0) *left = at;
+}
 
 // The largest key found that at least K of the n group maxima reach, KEY_LOWEST - 1 if fewer are above -inf.  One warp
 __device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, int K) {
@@ -142,210 +188,188 @@ __device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, in
     return lo;
 }
 
-// calls f(z, column) for the elements of a chunk's vectors that reach `bound`
+// calls f(z, column) for the elements of a vector that reach `bound`
 template <class T, class F>
-__device__ __forceinline__ void each_above(const uint4 (&q)[VPT], int e0, int step, float bound, F f) {
+__device__ __forceinline__ void each_above(const uint4& q, int e0, float bound, F f) {
+    if (!(Vec<T>::top(max_of_words<T>(q)) >= bound)) return;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-        if (!(Vec<T>::top(max_of_words<T>(q[j])) >= bound)) continue;
-        const int e = e0 + j * step;
-#pragma unroll
-        for (int i = 0; i < Vec<T>::E / 2; ++i) {
-            const float2 p = parts(Vec<T>::pair(q[j], i));
-            if (p.x >= bound) f(p.x, (uint32_t)(e + 2 * i));
-            if (p.y >= bound) f(p.y, (uint32_t)(e + 2 * i + 1));
-        }
+    for (int i = 0; i < Vec<T>::E / 2; ++i) {
+        const float2 p = parts(Vec<T>::pair(q, i));
+        if (p.x >= bound) f(p.x, (uint32_t)(e0 + 2 * i));
+        if (p.y >= bound) f(p.y, (uint32_t)(e0 + 2 * i + 1));
     }
+}
+// the same for the vectors [v0, v1) of a row, read anew
+template <class T, class F>
+__device__ __forceinline__ void each_of_row(const Share<T>& r, int v0, int v1, float bound, F f) {
+    for (int vec = v0 + (int)threadIdx.x; vec < v1; vec += blockDim.x)
+        each_above<T>(vec >= r.w0 && vec < r.w1 ? r.vectors()[vec] : r.edge(vec), r.first(vec), bound, f);
 }
 
 __device__ __forceinline__ unsigned long long entry_of(float z, uint32_t col) { return ((unsigned long long)key_of(z) << 32) | (uint32_t)~col; }
-__device__ __forceinline__ bool takes(Cut c, unsigned long long e) { return takes(c, (uint32_t)(e >> 32), ~(uint32_t)e); }
 
-// More elements of this chunk pass the bound than the list holds (ties, or an order that defeats the bound): the list is
-// made anew from the entries before the chunk and the chunk's elements that an exact cut takes.  All threads
+// More elements of the vectors [v0, v1) reach the bound than the list holds (ties, a mask, or an order that defeats the
+// bound): the list is made anew with what an exact cut takes of them, reading them once per step of a bisection
 template <class T>
-__device__ void rebuild_list(TopShared& t, const uint4 (&q)[VPT], int e0, int step, int K, uint32_t columns) {
-    const int nt = blockDim.x, kept = t.kept;
+__device__ __noinline__ void cut_exactly(TopShared& t, const Share<T>& r, int v0, int v1, int K) {
     const float bound = value_of(t.bound);
-    const Cut cut = find_cut(K, CANDS / 2, KEY_LOWEST - 1, columns, [&](Cut c) {
+    const Cut cut = find_cut(K, CANDS / 2, t.bound - 1, (uint32_t)r.V, [&](Cut c) {
         int k = 0;
-        for (int i = threadIdx.x; i < kept; i += nt) k += takes(c, t.list[i]);
-        each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) { k += takes(c, key_of(z), col); });
+        each_of_row<T>(r, v0, v1, bound, [&](float z, uint32_t col) { k += takes(c, key_of(z), col); });
         return block_count(k, t.sums);
     });
-    unsigned long long mine[CANDS / 128];          // (128 threads or more)
-#pragma unroll
-    for (int x = 0; x < CANDS / 128; ++x) {
-        const int i = threadIdx.x + x * nt;
-        mine[x] = i < kept && takes(cut, t.list[i]) ? t.list[i] : 0ull;
-    }
     __syncthreads();
     if (threadIdx.x == 0) t.n = 0;
     __syncthreads();
-#pragma unroll
-    for (int x = 0; x < CANDS / 128; ++x)
-        if (mine[x]) t.list[atomicAdd(&t.n, 1)] = mine[x];
-    each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) {
+    each_of_row<T>(r, v0, v1, bound, [&](float z, uint32_t col) {
         if (takes(cut, key_of(z), col)) t.list[atomicAdd(&t.n, 1)] = entry_of(z, col);
     });
-    // K entries reach cut.key, all in earlier columns than what is still to come
+    // K elements reach cut.key, all in earlier columns than what is still to come
     if (threadIdx.x == 0) t.bound = max(t.bound, cut.key + 1);
     __syncthreads();
 }
 
 // Statistics of the row, and with TOP its alternatives, in one pass.  Candidates are the elements that reach a bound
-// below which no alternative can lie: the K-th largest of group maxima over the chunks so far (a group is 32 / groups
-// lanes' share of the row), taken anew after chunks 1, 2, 4, 8, ..
+// below which no alternative can lie: the K-th largest of group maxima so far (a group is 32 / groups lanes' share of
+// the row).  It is taken after the first batch, and again after 2, 4, 8, .. without a barrier: maxima that are late
+// or early only make it lower.
 template <class T, bool TOP>
-__global__ void __launch_bounds__(MAX_THREADS, 3) token_logp_kernel(const RowArgs a, const FeedArgs f) {
-    extern __shared__ __align__(128) uint4 ring[];
-    __shared__ uint64_t full[MAX_SLOTS];
+__global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(const RowArgs a) {
     __shared__ float4 part[PARTS];
     __shared__ float row_m, row_ls, row_lse;
     __shared__ TopShared top[1];                   // (no room where it is not used)
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = f.blocks;
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
+    const long long n = a.row0 + blockIdx.x / blocks;
     const float c2 = a.scale * LOG2E;
-    const long long first_row = blockIdx.x / blocks;
-    Feed<T> feed(a.logits, a.stride, a.N, a.V, f, ring, full, rank, first_row);
-    start_feed(feed);
-    if (TOP && threadIdx.x == 0) { top->n = top->kept = 0; top->bound = KEY_LOWEST; }
-    for (long long n = first_row; n < a.N; n += f.clusters) {
-        const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
-        Stat st{neg_inf(), 0.0f, 0.0f};
-        long long t = -1;
-        float zt = 0.0f;
-        if (rank == 0 && threadIdx.x == nt - 1 && a.logp) {
-            t = a.tok.at(n);
-            if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
-            else if (t >= 0) zt = to_float(r.z[t]);
+    if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+    if (TOP && threadIdx.x == 0) { top->n = 0; top->bound = KEY_LOWEST; }
+    Stat st{neg_inf(), 0.0f, 0.0f};
+    float mine = neg_inf();                        // the thread's largest
+    int batch = 0;
+    for (int base = r.v0; base < r.v1; base += nt * VPT, ++batch) {
+        uint4 q[VPT];
+        if (base >= r.w0 && base + nt * VPT <= r.w1) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) q[j] = __ldcs(r.vectors() + base + j * nt + threadIdx.x);
+        } else {
+            load_share<T, VPT>(r, base, nt, q);
         }
-        for (int c = 0; c < f.chunks; ++c) {
-            uint4 q[VPT];
-            const bool ok = feed.wait();
-            feed.template read<VPT>(r, c, feed.at, q);
-            feed.next();
-            if (__syncthreads_or(!ok)) {           // a copy never came
-                if (threadIdx.x == 0) feed.give_up(a.status);
-                return;
+        const float m = thread_max_of<T, VPT>(q);
+        take<T, VPT, true>(st, q, m, c2);
+        mine = fmaxf(mine, m);
+        if (!TOP) continue;
+        const bool renew = (batch & (batch + 1)) == 0;
+        if (renew) {
+            const int width = 32 / a.groups;
+            float g = mine;
+            for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+            if (lane % width == 0) top->group[warp * a.groups + lane / width] = key_of(g);
+            if (batch == 0) __syncthreads();
+            else __syncwarp();
+            if (warp == (batch == 0 ? 0 : warps - 1)) {
+                const uint32_t b = group_bound(top->group, warps * a.groups, a.K);
+                if (lane == 0) atomicMax(&top->bound, b);
             }
-            if (threadIdx.x == 0) feed.issue();
-            take_chunk<T, VPT, true>(st, q, c2);
-            if (!TOP) continue;
-            const int e0 = r.first(r.v0 + c * f.chunk + (int)threadIdx.x), step = nt * Vec<T>::E;
-            const bool renew = (c & (c + 1)) == 0 && c + 1 < 2 * f.chunks;     // after chunks 1, 2, 4, ..
-            if (renew) {
-                const int width = 32 / a.groups;
-                float g = st.m;
-                for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-                if (lane % width == 0) top->group[warp * a.groups + lane / width] = key_of(g);
-                __syncthreads();
-                if (warp == 0) {
-                    const uint32_t b = group_bound(top->group, warps * a.groups, a.K);
-                    if (lane == 0) {
-                        top->reached = b;
-                        top->bound = max(top->bound, b);
-                    }
-                }
-                __syncthreads();
-            }
-            const float bound = value_of(top->bound);
-            if (st.m >= bound)
-                each_above<T>(q, e0, step, bound, [&](float z, uint32_t col) {
+            if (batch == 0) __syncthreads();
+        }
+        const float bound = value_of(*reinterpret_cast<volatile uint32_t*>(&top->bound));
+        if (m >= bound) {
+            const int e0 = r.first(base + (int)threadIdx.x), step = nt * Vec<T>::E;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+                each_above<T>(q[j], e0 + j * step, bound, [&](float z, uint32_t col) {
                     const int at = atomicAdd(&top->n, 1);
                     if (at < CANDS) top->list[at] = entry_of(z, col);
                 });
-            __syncthreads();
-            if (top->n > CANDS) rebuild_list<T>(*top, q, e0, step, a.K, (uint32_t)a.V);
-            else if (renew && threadIdx.x == 0 && top->reached >= KEY_LOWEST) top->bound = max(top->bound, top->reached + 1);
-            if (threadIdx.x == 0) top->kept = top->n;
-            // (the next chunk's first barrier orders these before they are read; what equals `reached` in a later column
-            // comes after the K that reached it)
         }
-        const Stat w = join_warp<true>(st, c2);
-        const float4 sent = make_float4(w.m, w.s, w.u, 0.0f);
-        if (blocks == 1) {
-            if (lane == 0) part[warp] = sent;
+        if (batch == 0) {
+            // what equals the bound in a later batch, thus in a later column, comes after the K that reach it
             __syncthreads();
-        } else {
-            if (TOP) {
-                const int room = CANDS / blocks;
-                __syncthreads();
-                const int have = top->n;
-                Cut cut{0, 0xffffffffu};
-                if (have > room)
-                    cut = find_cut(a.K, room, KEY_LOWEST - 1, (uint32_t)a.V, [&](Cut c) {
-                        int k = 0;
-                        for (int i = threadIdx.x; i < have; i += nt) k += takes(c, top->list[i]);
-                        return block_count(k, top->sums);
-                    });
-                __syncthreads();
-                if (threadIdx.x == 0) top->n = 0;
-                cluster_arrive();                  // the first block has done with the row before
-                cluster_wait();
-                for (int i = threadIdx.x; i < have; i += nt)
-                    if (takes(cut, top->list[i])) remote_store(remote_addr(&top->merged[rank * room + atomicAdd(&top->n, 1)], 0), top->list[i]);
-                __syncthreads();
-                if (threadIdx.x == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->n);
+            const uint32_t b = top->bound;
+            if (top->n > CANDS) {
+                cut_exactly<T>(*top, r, r.v0, min(r.v0 + nt * VPT, r.v1), a.K);
             } else {
-                cluster_arrive();
-                cluster_wait();
-            }
-            if (lane == 0) remote_store(remote_addr(&part[rank * warps + warp], 0), sent);
-            cluster_arrive();
-            cluster_wait();
-        }
-        if (rank == 0) {
-            if (warp == warps - 1) {
-                const Stat v = join_parts(part, warps * blocks, c2);
-                const bool empty = v.m == neg_inf() && v.s == 0.0f;
-                const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
-                if (lane == 31) {                  // the thread that holds the token
-                    if (a.lse) a.lse[n] = lse;
-                    if (a.entropy) a.entropy[n] = empty ? 0.0f : ls - LN2 * (v.u / v.s);
-                    if (a.logp) a.logp[n] = t >= a.V ? quiet_nan() : t < 0 ? 0.0f : empty ? neg_inf() : fmaf(zt - v.m, a.scale, -ls);
-                    row_m = v.m; row_ls = ls; row_lse = lse;
-                }
-            }
-            if (TOP) {
-                // rank the candidates; far more than K are cut first, since each is compared with all others
-                const int room = CANDS / blocks;
-                const unsigned long long* list = blocks == 1 ? top->list : top->merged;
-                if (blocks == 1 && threadIdx.x == 0) top->count[0] = top->n;
                 __syncthreads();
-                int total = 0;
-                for (int b = 0; b < blocks; ++b) total += top->count[b];
-                const int most = a.K + a.K / 4 + 16;
-                Cut cut{0, 0xffffffffu};
-                if (total > most)
-                    cut = find_cut(a.K, most, KEY_LOWEST - 1, (uint32_t)a.V, [&](Cut c) {
-                        int k = 0;
-                        for (int b = 0; b < blocks; ++b)
-                            for (int i = threadIdx.x; i < top->count[b]; i += nt) k += takes(c, list[b * room + i]);
-                        return block_count(k, top->sums);
-                    });
-                const float lse = row_lse, ls = row_ls, m = row_m;
-                const bool broken = !(lse == lse);
-                auto put = [&](int at, long long id, float lp) {
-                    if (a.tok.wide) static_cast<long long*>(a.top_ids)[n * a.K + at] = id;
-                    else static_cast<int*>(a.top_ids)[n * a.K + at] = (int)id;
-                    a.top_logp[n * a.K + at] = lp;
-                };
-                for (int b = 0; b < blocks && !broken; ++b)
-                    for (int i = threadIdx.x; i < top->count[b]; i += nt) {
-                        const unsigned long long v = list[b * room + i];
-                        if (!takes(cut, v)) continue;
-                        int place = 0;
-                        for (int d = 0; d < blocks; ++d)
-                            for (int x = 0; x < top->count[d]; ++x) place += list[d * room + x] > v;
-                        if (place < a.K) put(place, ~(uint32_t)v, fmaf(value_of((uint32_t)(v >> 32)) - m, a.scale, -ls));
-                    }
-                for (int k = (broken ? 0 : total) + (int)threadIdx.x; k < a.K; k += nt) put(k, -1, broken ? lse : neg_inf());
+                if (threadIdx.x == 0 && b > KEY_LOWEST) top->bound = b + 1;
+                __syncthreads();
             }
+        }
+    }
+    long long t = -1;
+    float zt = 0.0f;
+    if (rank == 0 && threadIdx.x == nt - 1 && a.logp) {
+        t = a.tok.at(n);
+        if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
+        else if (t >= 0) zt = to_float(r.z[t]);
+    }
+    if (TOP) {
+        __syncthreads();
+        if (top->n > CANDS) {
+            if (threadIdx.x == 0) top->bound = KEY_LOWEST;
+            __syncthreads();
+            cut_exactly<T>(*top, r, r.v0, r.v1, a.K);
+        }
+    }
+    const int most = min(a.K + a.K / 4 + 16, nt);  // candidates that are ranked, a thread each
+    const Stat w = join_warp<true>(st, mine, c2);
+    const float4 sent = make_float4(w.m, w.s, w.u, 0.0f);
+    if (blocks == 1) {
+        if (lane == 0) part[warp] = sent;
+        __syncthreads();
+    } else {
+        cluster_wait();
+        if (TOP && warp == 0) {
+            shrink_list(top->list, top->n, a.K, min(most, CANDS / blocks), (uint32_t)a.V, top->last, &top->left);
+            __syncwarp();
+            for (int i = lane; i < top->left; i += 32) remote_store(remote_addr(&top->merged[rank * (CANDS / blocks) + i], 0), top->last[i]);
+            if (lane == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->left);
+        }
+        if (lane == 0) remote_store(remote_addr(&part[rank * warps + warp], 0), sent);
+        cluster_arrive();
+        if (rank != 0) return;                     // nothing is written into this block's memory
+        cluster_wait();
+    }
+    if (warp == warps - 1) {
+        const Stat v = join_parts(part, warps * blocks, c2);
+        const bool empty = v.m == neg_inf() && v.s == 0.0f;
+        const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
+        if (lane == 31) {                          // the thread that holds the token
+            if (a.lse) a.lse[n] = lse;
+            if (a.entropy) a.entropy[n] = empty ? 0.0f : ls - LN2 * (v.u / v.s);
+            if (a.logp) a.logp[n] = t >= a.V ? quiet_nan() : t < 0 ? 0.0f : empty ? neg_inf() : fmaf(zt - v.m, a.scale, -ls);
+            row_m = v.m; row_ls = ls; row_lse = lse;
+        }
+    }
+    if (!TOP) return;
+    int n_list = top->n;
+    if (blocks > 1) {
+        n_list = 0;
+        for (int b = 0; b < blocks; ++b) {
+            for (int i = threadIdx.x; i < top->count[b]; i += nt) top->list[n_list + i] = top->merged[b * (CANDS / blocks) + i];
+            n_list += top->count[b];
         }
         __syncthreads();
-        if (TOP && threadIdx.x == 0) { top->n = top->kept = 0; top->bound = KEY_LOWEST; }
     }
+    if (warp == 0) shrink_list(top->list, n_list, a.K, most, (uint32_t)a.V, top->last, &top->left);
+    __syncthreads();
+    const float lse = row_lse, ls = row_ls, m = row_m;
+    const bool broken = !(lse == lse);
+    auto put = [&](int at, long long id, float lp) {
+        if (a.tok.wide) static_cast<long long*>(a.top_ids)[n * a.K + at] = id;
+        else static_cast<int*>(a.top_ids)[n * a.K + at] = (int)id;
+        a.top_logp[n * a.K + at] = lp;
+    };
+    const int left = top->left;
+    if ((int)threadIdx.x < left && !broken) {
+        const unsigned long long v = top->last[threadIdx.x];
+        int place = 0;
+#pragma unroll 4
+        for (int x = 0; x < left; ++x) place += top->last[x] > v;
+        if (place < a.K) put(place, ~(uint32_t)v, fmaf(value_of((uint32_t)(v >> 32)) - m, a.scale, -ls));
+    }
+    for (int k = (broken ? 0 : left) + (int)threadIdx.x; k < a.K; k += nt) put(k, -1, broken ? lse : neg_inf());
 }
 
 template <class T, int VG, bool ENT>
@@ -403,6 +427,7 @@ struct TeacherShared {
     float q[QS_MAX_TOP], logq[QS_MAX_TOP], z[QS_MAX_TOP];
     uint32_t id[QS_MAX_TOP];
     float Q, rest;                         // sum of q, mass left to the other columns (tail)
+    float w;                               // weight * scale
     int bad;                               // an id past the last column
 };
 
@@ -416,9 +441,10 @@ __device__ __forceinline__ float teacher_at(const RowArgs& a, long long i) {
 struct Entries {
     static constexpr int PER = QS_MAX_TOP / 32;
     long long id[PER];
-    float u[PER];
+    float u[PER], w;
 
     __device__ __forceinline__ void load(const RowArgs& a, long long n) {
+        w = n < a.N && a.g1 ? a.g1[n] : a.g_all;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = (int)(threadIdx.x & 31) + 32 * i;
@@ -467,6 +493,7 @@ struct Entries {
         }
         sum = warp_sum(sum);
         if (lane == 0) {
+            s.w = w * a.scale;
             s.Q = sum;
             s.rest = !TAIL ? 0.0f : sum == sum ? fmaxf(0.0f, 1.0f - sum) : sum;
             s.bad = bad;
@@ -484,9 +511,9 @@ struct Slope {
     int thin, empty;
 };
 template <bool TAIL>
-__device__ __forceinline__ Slope slope_of(const RowArgs& a, long long n, const TeacherShared& t, float lse, float log_tail) {
+__device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, float lse, float log_tail) {
     Slope s;
-    s.w = (a.g1 ? a.g1[n] : a.g_all) * a.scale;
+    s.w = w;
     s.in = t.bad ? quiet_nan() : t.Q + t.rest;
     s.rest = t.rest;
     s.log_tail = log_tail;
@@ -524,213 +551,212 @@ __device__ __forceinline__ uint4 slope_vec(const f2* d, const Slope& s, float no
     return Vec<T>::pack(g);
 }
 
-// Loss and, with a.grad, its gradient.  KEEP: the share's chunks stay in the ring until their gradient is written
-// (ring of at least one share); otherwise they come by twice
+// Loss and, with a.grad, its gradient.  KEEP: the share lies in shared memory from one bulk copy until its gradient is
+// written; otherwise (rows beyond a cluster's shared memory) it is read twice
 template <class T, bool KEEP, bool TAIL>
-__global__ void __launch_bounds__(MAX_THREADS, 3) distill_kernel(const RowArgs a, const FeedArgs f) {
-    constexpr int E = Vec<T>::E;
-    extern __shared__ __align__(128) uint4 ring[];
-    __shared__ uint64_t full[MAX_SLOTS];
-    __shared__ float4 part[2][PARTS];              // two rows' worth: the other blocks may be a row ahead
-    __shared__ float4 in_part[2][MAX_BLOCKS];      // tail: the statistics of the ids' own columns, block by block
-    __shared__ float z_at[2][QS_MAX_TOP];          // first block: logits at the ids
+__global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a) {
+    constexpr int E = Vec<T>::E, PER = (QS_MAX_TOP + 127) / 128;
+    extern __shared__ __align__(128) uint4 kept[];
+    __shared__ uint64_t landed;
+    __shared__ float4 part[PARTS];
+    __shared__ float4 in_part[MAX_BLOCKS];         // tail: the statistics of the ids' own columns, block by block
+    __shared__ float z_at[QS_MAX_TOP];             // first block: logits at the ids
     __shared__ TeacherShared t;
     __shared__ float row_m, row_by;                // maximum, one over the sum
     __shared__ Slope row;
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = f.blocks;
+    __shared__ uint32_t marks[KEEP || !TAIL ? 1 : 256];        // vectors that an id may name, by their low bits
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
+    const long long n = a.row0 + blockIdx.x / blocks;
     const float c2 = a.scale * LOG2E;
-    const long long first_row = blockIdx.x / blocks;
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
-    Feed<T> feed(a.logits, a.stride, a.N, a.V, f, ring, full, rank, first_row);
-    start_feed(feed);
-    Entries next;
-    if (warp == 0) next.load(a, first_row);
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+    if (KEEP) {
+        if (threadIdx.x == 0) {
+            const uint32_t bytes = r.w1 > r.w0 ? (uint32_t)(r.w1 - r.w0) * 16u : 0u;
+            mbar_init(&landed, 1);
+            fence_async_smem();
+            mbar_expect(&landed, bytes);
+            if (bytes) bulk_load(kept + (r.w0 - r.v0), r.vectors() + r.w0, bytes, &landed);
+        }
+        if ((int)threadIdx.x == nt - 1 && r.w0 > r.v0) kept[0] = r.edge(r.v0);
+        if ((int)threadIdx.x == nt - 2 && r.w1 < r.v1) kept[r.w1 - r.v0] = r.edge(r.w1);
+    }
+    if (!KEEP && TAIL)
+        for (int i = threadIdx.x; i < 256; i += nt) marks[i] = 0;
+    if (warp == 0) {
+        Entries e;
+        e.load(a, n);
+        e.finish<TAIL>(a, t, rank == 0);
+    }
+    __syncthreads();
     if (blocks > 1) cluster_wait();
-    int odd = 0;
     bool ok = true;
-    for (long long n = first_row; n < a.N; n += f.clusters, odd ^= 1) {
-        const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
-        if (warp == 0) {
-            next.finish<TAIL>(a, t, rank == 0);
-            next.load(a, n + f.clusters);          // in flight during this row
-        }
-        __syncthreads();
-        const int kept_at = feed.at;               // KEEP: slot of the share's first chunk
-        Stat st{neg_inf(), 0.0f, 0.0f};
-        float z_in[(QS_MAX_TOP + 127) / 128];      // this thread's entries (k = thread + i nt) that the share holds
+    if (KEEP) ok = mbar_wait(&landed, 0);
+    // logits at the ids of the share
+    T* flat = reinterpret_cast<T*>(kept);
+    bool named[PER];
 #pragma unroll
-        for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) z_in[i] = neg_inf();
-        for (int c = 0; c < f.chunks; ++c) {
-            uint4 q[VPT];
-            ok &= feed.wait();
-            // logits at the ids of this chunk; with the tail their places leave the sum, their own statistics join later
-            const int v0 = r.v0 + c * f.chunk, v1 = min(v0 + f.chunk, r.v1);
-            T* slot = reinterpret_cast<T*>(ring + feed.at * f.chunk);
-            bool mine = false;
+    for (int i = 0; i < PER; ++i) {
+        const int k = (int)threadIdx.x + i * nt;
+        named[i] = k < a.K && t.id[k] != NO_ID && r.holds((int)t.id[k]);
+        if (!named[i]) continue;
+        const int place = (int)t.id[k] + r.head;
+        const float z = to_float(KEEP ? flat[place - r.v0 * E] : r.z[t.id[k]]);
+        t.z[k] = z;
+        if (rank != 0) remote_store(remote_addr(&z_at[k], 0), __float_as_uint(z));
+        else z_at[k] = z;
+        if (!KEEP && TAIL) atomicOr(&marks[(place / E & 8191) >> 5], 1u << (place / E & 31));
+    }
+    if (TAIL) {                                    // these places leave the sum; their own statistics join later
+        __syncthreads();                           // (an id given twice is read twice)
+        if (KEEP) {
 #pragma unroll
-            for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) {
-                const int k = (int)threadIdx.x + i * nt;
-                if (k >= a.K || t.id[k] == NO_ID) continue;
-                const int place = (int)t.id[k] + r.head, vec = place / E;
-                if (vec < v0 || vec >= v1) continue;
-                z_in[i] = feed.inside(r, vec) ? to_float(slot[place - v0 * E]) : to_float(r.z[t.id[k]]);
-                t.z[k] = z_in[i];
-                mine = true;
-                if (rank != 0) remote_store(remote_addr(&z_at[odd][k], 0), __float_as_uint(z_in[i]));
-                else z_at[odd][k] = z_in[i];
-            }
-            if (TAIL) {
-                __syncthreads();                   // an id given twice is read twice
-                if (mine) {
-#pragma unroll
-                    for (int i = 0; i < (QS_MAX_TOP + 127) / 128; ++i) {
-                        const int k = (int)threadIdx.x + i * nt;
-                        if (k >= a.K || t.id[k] == NO_ID) continue;
-                        const int place = (int)t.id[k] + r.head, vec = place / E;
-                        if (vec >= v0 && vec < v1 && feed.inside(r, vec)) slot[place - v0 * E] = from_float<T>(neg_inf());
-                    }
-                    fence_async_smem();            // the slot's next copy comes by the other proxy
-                }
-                __syncthreads();
-            }
-            feed.template read<VPT>(r, c, feed.at, q);
-            if (TAIL && (v0 == 0 || v1 * E - r.head > r.V)) {      // vectors that were not copied: the tensor's first and last
-#pragma unroll
-                for (int j = 0; j < VPT; ++j) {
-                    const int vec = v0 + j * nt + (int)threadIdx.x;
-                    if (j * nt + (int)threadIdx.x >= f.chunk || vec >= v1 || feed.inside(r, vec)) continue;
-                    for (int k = 0; k < a.K; ++k)
-                        if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
-                }
-            }
-            feed.next();
-            if (!KEEP) {
-                __syncthreads();
-                if (threadIdx.x == 0) feed.issue();
-            }
-            take_chunk<T, VPT, false>(st, q, c2);
-        }
-        const int readers = a.grad ? blocks : 1;   // blocks that need the row's statistics
-        const Stat w = join_warp<false>(st, c2);
-        const float4 sent = make_float4(w.m, w.s, 0.0f, 0.0f);
-        if (blocks == 1) {
-            if (lane == 0) part[odd][warp] = sent;
-        } else if (lane < readers) {
-            remote_store(remote_addr(&part[odd][rank * warps + warp], lane), sent);
-        }
-        if (TAIL) {
-            // an id given twice is one column
+            for (int i = 0; i < PER; ++i)
+                if (named[i]) flat[(int)t.id[threadIdx.x + i * nt] + r.head - r.v0 * E] = from_float<T>(neg_inf());
             __syncthreads();
-            if (warp == 0) {
-                float z[Entries::PER], m = neg_inf(), s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < Entries::PER; ++i) {
-                    const int k = lane + 32 * i;
-                    z[i] = neg_inf();
-                    if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
-                    bool first = true;
-                    for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
-                    if (first) z[i] = t.z[k];
-                    m = fmaxf(m, z[i]);
-                }
-                m = warp_max(m);
-#pragma unroll
-                for (int i = 0; i < Entries::PER; ++i) s += ex2((z[i] - shift_of(m)) * c2);
-                s = warp_sum(s);
-                const float4 v = make_float4(m, s, 0.0f, 0.0f);
-                if (blocks == 1) {
-                    if (lane == 0) in_part[odd][0] = v;
-                } else if (lane < readers) {
-                    remote_store(remote_addr(&in_part[odd][rank], lane), v);
-                }
-            }
         }
-        if (__syncthreads_or(!ok)) {               // a copy never came
-            if (threadIdx.x == 0) feed.give_up(a.status);
-            return;
-        }
-        if (blocks > 1) {
-            cluster_arrive();
-            cluster_wait();
-        }
-        if (warp == 0 && (a.grad || rank == 0)) {
-            Stat v = join_parts(part[odd], warps * blocks, c2);
-            float log_tail = 0.0f;
-            if (TAIL) {
-                const Stat in = join_parts(in_part[odd], blocks, c2);
-                const float m = fmaxf(v.m, in.m);
-                const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
-                const float s = x.s + y.s;
-                // log of the share outside: near 1 the difference of two logs would cancel
-                log_tail = v.m == neg_inf() && v.s == 0.0f ? neg_inf() : fmaf(v.m - m, a.scale, logf(v.s) - logf(s));
-                if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
-                v = Stat{m, s, 0.0f};
-            }
-            const bool empty = v.m == neg_inf() && v.s == 0.0f;
-            const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
-            const Slope s = slope_of<TAIL>(a, n, t, lse, log_tail);
-            if (lane == 0) {
-                row_m = shift_of(v.m);
-                row_by = empty ? 0.0f : 1.0f / v.s;
-                row = s;
-            }
-            if (rank == 0) {
-                float loss = 0.0f;
-                bool beyond = false;               // an entry where the student has no mass at all
-                for (int k = lane; k < a.K; k += 32) {
-                    if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
-                    const float lp = empty ? neg_inf() : fmaf(z_at[odd][k] - v.m, a.scale, -ls);
-                    beyond |= lp == neg_inf();
-                    loss = fmaf(t.q[k], t.logq[k] - lp, loss);
-                }
-                loss = warp_sum(loss);
-                // a mean of log p at a mask of the lowest value: only its rounding passes the largest number
-                if (!__any_sync(~0u, beyond) && loss == -neg_inf()) loss = FLT_MAX;
-                if (TAIL && t.rest != 0.0f) loss = fmaf(t.rest, logf(t.rest) - log_tail, loss);
-                if (lane == 0) {
-                    if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
-                    if (a.lse) a.lse[n] = lse;
-                    if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
-                }
-            }
-        }
-        __syncthreads();
-        if (!a.grad) continue;                     // (without a gradient nothing is kept)
-        const Slope s = row;
-        const float m = row_m, by = row_by;
-        T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
-        const f2 minus = make_f2(-m, -m), c2s = make_f2(c2, c2);
-        int at = kept_at;
-        for (int c = 0; c < f.chunks; ++c) {
-            uint4 q[VPT];
-            if (!KEEP) {
-                ok &= feed.wait();                 // (looked at with the next row's)
-                at = feed.at;
-                feed.next();
-            }
-            feed.template read<VPT>(r, c, at, q);
-            const int v0 = r.v0 + c * f.chunk, v1 = min(v0 + f.chunk, r.v1);
-            __syncthreads();                       // all have read the slot
-            if (threadIdx.x == 0) feed.issue();
-            if (KEEP && ++at == f.slots) at = 0;
+    }
+    Stat st{neg_inf(), 0.0f, 0.0f};
+    float largest = neg_inf();
+    for (int base = r.v0; base < r.v1; base += nt * VPT) {
+        uint4 q[VPT];
+        if (KEEP) {
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
-                const int vec = v0 + j * nt + (int)threadIdx.x;
-                if (j * nt + (int)threadIdx.x >= f.chunk || vec >= v1) continue;
-                f2 d[E / 2];
-#pragma unroll
-                for (int i = 0; i < E / 2; ++i) d[i] = mul2(add2(Vec<T>::pair(q[j], i), minus), c2s);
-                store_vec(r, out, vec, slope_vec<T, TAIL>(d, s, by), a.wide);
+                const int vec = base + j * nt + (int)threadIdx.x;
+                q[j] = all_lowest<T>();
+                if (vec < r.v1) q[j] = kept[vec - r.v0];
             }
+        } else {
+            load_share<T, VPT>(r, base, nt, q);
+            if (TAIL)
+#pragma unroll
+                for (int j = 0; j < VPT; ++j) {
+                    const int vec = base + j * nt + (int)threadIdx.x;
+                    if (vec < r.v1 && marks[(vec & 8191) >> 5] >> (vec & 31) & 1)
+                        for (int k = 0; k < a.K; ++k)
+                            if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
+                }
         }
-        __syncthreads();                           // the ids' places are written last
-        for (int k = threadIdx.x; k < a.K; k += nt)
-            if (t.id[k] != NO_ID && r.holds((int)t.id[k]))
-                out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2((t.z[k] - m) * c2) * by));
-        __syncthreads();                           // the entries are written anew
+        const float most = thread_max_of<T, VPT>(q);
+        take<T, VPT, false>(st, q, most, c2);
+        largest = fmaxf(largest, most);
     }
-    if (__syncthreads_or(!ok) && threadIdx.x == 0) feed.give_up(a.status);
+    const int readers = a.grad ? blocks : 1;       // blocks that need the row's statistics
+    const Stat w = join_warp<false>(st, largest, c2);
+    const float4 sent = make_float4(w.m, w.s, 0.0f, 0.0f);
+    if (blocks == 1) {
+        if (lane == 0) part[warp] = sent;
+    } else if (lane < readers) {
+        remote_store(remote_addr(&part[rank * warps + warp], lane), sent);
+    }
+    if (TAIL && warp == 0) {
+        float z[Entries::PER], m = neg_inf(), s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Entries::PER; ++i) {
+            const int k = lane + 32 * i;
+            z[i] = neg_inf();
+            if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
+            bool first = true;                     // an id given twice is one column
+            for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
+            if (first) z[i] = t.z[k];
+            m = fmaxf(m, z[i]);
+        }
+        m = warp_max(m);
+#pragma unroll
+        for (int i = 0; i < Entries::PER; ++i) s += ex2((z[i] - shift_of(m)) * c2);
+        s = warp_sum(s);
+        const float4 v = make_float4(m, s, 0.0f, 0.0f);
+        if (blocks == 1) {
+            if (lane == 0) in_part[0] = v;
+        } else if (lane < readers) {
+            remote_store(remote_addr(&in_part[rank], lane), v);
+        }
+    }
+    if (!ok) {                                     // the copy never came (2 s): the row's results are void
+        flag_status(a.status, QS_TIMEOUT);
+        mbar_wait(&landed, 0);                     // once more, before the memory goes to another block
+    }
+    if (blocks == 1) {
+        __syncthreads();
+    } else {
+        cluster_arrive();
+        if (!a.grad && rank != 0) return;          // nothing is written into this block's memory
+        cluster_wait();
+    }
+    Stat v{};
+    float log_tail = 0.0f, lse = 0.0f, ls = 0.0f;
+    if (warp == 0) {
+        v = join_parts(part, warps * blocks, c2);
+        if (TAIL) {
+            const Stat in = join_parts(in_part, blocks, c2);
+            const float m = fmaxf(v.m, in.m);
+            const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
+            const float s = x.s + y.s;
+            // log of the share outside: near 1 the difference of two logs would cancel
+            log_tail = v.m == neg_inf() && v.s == 0.0f ? neg_inf() : fmaf(v.m - m, a.scale, logf(v.s) - logf(s));
+            if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
+            v = Stat{m, s, 0.0f};
+        }
+        const bool empty = v.m == neg_inf() && v.s == 0.0f;
+        ls = logf(v.s);
+        lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
+        const Slope s = slope_of<TAIL>(t.w, t, lse, log_tail);
+        if (lane == 0) {
+            row_m = shift_of(v.m);
+            row_by = empty ? 0.0f : 1.0f / v.s;
+            row = s;
+        }
+    }
+    if (a.grad) __syncthreads();
+    if (warp == 0 && rank == 0) {                  // while the other warps go on
+        float loss = 0.0f;
+        bool beyond = false;                       // an entry where the student has no mass at all
+        for (int k = lane; k < a.K; k += 32) {
+            if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
+            const float lp = lse == neg_inf() ? neg_inf() : fmaf(z_at[k] - v.m, a.scale, -ls);
+            beyond |= lp == neg_inf();
+            loss = fmaf(t.q[k], t.logq[k] - lp, loss);
+        }
+        loss = warp_sum(loss);
+        // a mean of log p at a mask of the lowest value: only its rounding passes the largest number
+        if (!__any_sync(~0u, beyond) && loss == -neg_inf()) loss = FLT_MAX;
+        if (TAIL && t.rest != 0.0f) loss = fmaf(t.rest, logf(t.rest) - log_tail, loss);
+        if (lane == 0) {
+            if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
+            if (a.lse) a.lse[n] = lse;
+            if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
+        }
+    }
+    if (!a.grad) return;
+    const Slope s = row;
+    const float m = row_m, by = row_by;
+    T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
+    uint4* to = reinterpret_cast<uint4*>(out - r.head);
+    const f2 minus = make_f2(-m, -m), c2s = make_f2(c2, c2);
+    for (int base = r.v0; base < r.v1; base += nt * VPT) {
+        uint4 q[VPT];
+        if (!KEEP) load_share<T, VPT>(r, base, nt, q);
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int vec = base + j * nt + (int)threadIdx.x;
+            if (vec >= r.v1) continue;
+            if (KEEP) q[j] = kept[vec - r.v0];
+            f2 d[E / 2];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) d[i] = mul2(add2(Vec<T>::pair(q[j], i), minus), c2s);
+            const uint4 g = slope_vec<T, TAIL>(d, s, by);
+            if (a.wide && vec >= r.w0 && vec < r.w1) __stcs(to + vec, g);
+            else store_vec(r, out, vec, g, false);
+        }
+    }
+    __syncthreads();                               // the ids' places are written last
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = (int)threadIdx.x + i * nt;
+        if (named[i]) out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2((t.z[k] - m) * c2) * by));
+    }
 }
 
 template <class T, int VG, bool TAIL>
@@ -752,7 +778,7 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
         if (t.id[k] != NO_ID && r.holds((int)t.id[k])) t.z[k] = to_float(r.z[t.id[k]]);
     const float lse = a.in_lse[n], log_tail = TAIL ? a.in_log_tail[n] : 0.0f;
     __syncthreads();
-    const Slope s = slope_of<TAIL>(a, n, t, lse, log_tail);
+    const Slope s = slope_of<TAIL>((a.g1 ? a.g1[n] : a.g_all) * a.scale, t, lse, log_tail);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const float shift = s.empty ? LOW_EXP : -lse;
     const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);
@@ -776,55 +802,57 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
 long long most_vectors(int64_t V, int size) { return (V + 2 * (16 / size - 1)) / (16 / size); }
 
 constexpr int SMS = 148;
-constexpr int RING_BYTES = 64 * 1024;      // ring of a 256-thread block: three to an SM
-constexpr int TOP_RING_BYTES = 48 * 1024;  // beside the lists of candidates
 
-struct Shape { int nt; FeedArgs f; int grid; size_t smem; bool keep; };
+struct Shape { int nt, blocks; size_t smem; bool keep; };
 
-// Blocks and chunks for rows of `vectors`.  `keep`: the share has to fit the ring
-Shape row_shape(int64_t N, long long vectors, bool keep, int ring_bytes) {
-    Shape s;
-    s.nt = vectors <= 128 * VPT ? 128 : MAX_THREADS;
-    const long long ring = ring_bytes / (s.nt == 128 ? 32 : 16);                 // vectors of a ring
-    const int chunk = s.nt * VPT;
-    const long long chunks = (vectors + chunk - 1) / chunk;                      // of a whole row
-    // few rows: as many blocks per row as fill the SMs, each with a chunk at least
-    long long blocks = 1;
-    while (blocks < MAX_BLOCKS && N * blocks * 2 <= 2 * SMS && blocks * 2 <= chunks) blocks *= 2;
-    if (keep)
-        while (blocks < MAX_BLOCKS && (vectors + blocks - 1) / blocks > ring) ++blocks;
-    const long long share = (vectors + blocks - 1) / blocks;
-    s.keep = keep && share <= ring;
-    s.f.blocks = (int)blocks;
-    s.f.chunks = (int)((share + chunk - 1) / chunk);
-    s.f.chunk = s.f.chunks == 1 ? (int)share : chunk;
-    const long long fit = ring / s.f.chunk;
-    s.f.slots = (int)(fit < MAX_SLOTS ? fit : MAX_SLOTS);
-    s.f.passes = keep && !s.keep ? 2 : 1;
-    s.smem = (size_t)16 * s.f.slots * s.f.chunk;
-    const int resident = s.nt == 128 ? 6 : 3;                                    // blocks per SM
-    const long long clusters = (long long)SMS * resident / blocks;
-    s.f.clusters = N < clusters ? N : clusters;
-    s.grid = (int)(s.f.clusters * blocks);
+// threads for a row of `vectors`: a batch of four vectors each
+int threads_for(long long vectors) { return vectors <= 128 * VPT ? 128 : MAX_THREADS; }
+
+// Statistics and alternatives: a block per row; few rows are split over a cluster until the blocks fill the SMs six
+// times over, each with a batch at least
+Shape stream_shape(int64_t N, long long vectors) {
+    Shape s{threads_for(vectors), 1, 0, false};
+    while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * VPT < vectors) s.blocks *= 2;
+    return s;
+}
+// The loss with its gradient: shares of 32 KB, so that seven blocks' fit an SM, or as long as 8 blocks make necessary.
+// Few rows are split further, down to a batch per block
+constexpr int SHARE = 32 * 1024 / 16, SHARE_MOST = 200 * 1024 / 16;
+Shape keep_shape(int64_t N, long long vectors) {
+    Shape s{threads_for(vectors), 1, 0, true};
+    while (s.blocks < MAX_BLOCKS && ((vectors + s.blocks - 1) / s.blocks > SHARE ||
+                                     (N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * VPT < vectors))) ++s.blocks;
+    const long long share = (vectors + s.blocks - 1) / s.blocks;
+    s.keep = share <= SHARE_MOST;
+    s.smem = s.keep ? 16 * (size_t)share : 0;
     return s;
 }
 
 template <class K>
-cudaError_t launch_stream(K kernel, const Shape& s, const RowArgs& a, cudaStream_t st) {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)s.grid);
-    cfg.blockDim = dim3((unsigned)s.nt);
-    cfg.dynamicSmemBytes = s.smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)s.f.blocks;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = s.f.blocks > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, a, s.f);
+cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, cudaStream_t st) {
+    a.blocks = s.blocks;
+    if (s.smem > 32 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
+        if (e != cudaSuccess) return e;
+    }
+    const long long most = 0x7fffffffll / s.blocks;              // rows per launch
+    for (a.row0 = 0; a.row0 < a.N; a.row0 += most) {
+        const long long rows = a.N - a.row0 < most ? a.N - a.row0 : most;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(rows * s.blocks));
+        cfg.blockDim = dim3((unsigned)s.nt);
+        cfg.dynamicSmemBytes = s.smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)s.blocks;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = s.blocks > 1 ? 1 : 0;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 // the backward calls: independent blocks, each with up to VG vectors per thread of its row
@@ -850,11 +878,11 @@ cudaError_t launch_grad(K kernel, const GradShape& s, RowArgs a, cudaStream_t st
 
 template <class T>
 cudaError_t launch_token_logp(RowArgs a, cudaStream_t st) {
-    const Shape s = row_shape(a.N, most_vectors(a.V, sizeof(T)), false, a.K > 0 ? TOP_RING_BYTES : RING_BYTES);
+    const Shape s = stream_shape(a.N, most_vectors(a.V, sizeof(T)));
     // maxima per warp that bound the K-th alternative: about four for each alternative asked for
     a.groups = 1;
     while (a.groups < 32 && s.nt / 32 * a.groups < 4 * a.K) a.groups *= 2;
-    return launch_stream(a.K > 0 ? token_logp_kernel<T, true> : token_logp_kernel<T, false>, s, a, st);
+    return launch_rows(a.K > 0 ? token_logp_kernel<T, true> : token_logp_kernel<T, false>, s, a, st);
 }
 template <class T>
 cudaError_t launch_token_logp_grad(const RowArgs& a, cudaStream_t st) {
@@ -865,10 +893,9 @@ cudaError_t launch_token_logp_grad(const RowArgs& a, cudaStream_t st) {
 }
 template <class T>
 cudaError_t launch_distill(const RowArgs& a, bool tail, cudaStream_t st) {
-    const Shape s = row_shape(a.N, most_vectors(a.V, sizeof(T)), a.grad != nullptr, RING_BYTES);
-    // without a gradient nothing is kept and nothing comes by twice
-    if (s.keep) return launch_stream(tail ? distill_kernel<T, true, true> : distill_kernel<T, true, false>, s, a, st);
-    return launch_stream(tail ? distill_kernel<T, false, true> : distill_kernel<T, false, false>, s, a, st);
+    const Shape s = keep_shape(a.N, most_vectors(a.V, sizeof(T)));
+    if (s.keep) return launch_rows(tail ? distill_kernel<T, true, true> : distill_kernel<T, true, false>, s, a, st);
+    return launch_rows(tail ? distill_kernel<T, false, true> : distill_kernel<T, false, false>, s, a, st);
 }
 template <class T>
 cudaError_t launch_distill_grad(const RowArgs& a, bool tail, cudaStream_t st) {

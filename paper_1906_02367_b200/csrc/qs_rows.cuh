@@ -1,11 +1,9 @@
-// Rows of logits as streams of 16-byte vectors.
+// Rows of logits as 16-byte vectors.
 //
 // A row is cut into 16-byte vectors counted from the 16-byte boundary at or before its first element, so that
-// rows of any alignment are read with wide accesses; places of the first and the last vector outside the row
-// count as -inf.  A row belongs to one block or to a cluster of blocks, each with a contiguous share of the
-// vectors; blocks stay and take row after row.  A Feed brings a block's shares through a ring of chunks in
-// shared memory with bulk copies, several chunks ahead and across rows, so that the memory never waits
-// for a row's last steps.
+// rows of any alignment are read with wide accesses; the first and the last vector may hold only some elements of
+// the row and are read one by one, their other places counting as -inf.  A row belongs to one block or to a cluster
+// of blocks, each with a contiguous share of the vectors.
 //
 // Statistics: with y = scale * z, a part of a row is held as (m, s, u): m = max z, s = sum e and
 // u = sum e * d with d = (z - m) * scale * log2(e) and e = 2^d.  Parts join exactly up to rounding; the
@@ -146,6 +144,7 @@ struct Share {
     const T* z;                // the row's first element
     int V, head;               // elements; places between the 16-byte boundary and the first
     int v0, v1;                // the block's vectors
+    int w0, w1;                // those of them that are whole
 
     __device__ __forceinline__ Share(const void* logits, long long stride, long long n, long long len, int part, int nparts) {
         z = static_cast<const T*>(logits) + n * stride;
@@ -154,6 +153,27 @@ struct Share {
         const int nvec = (V + head + Vec<T>::E - 1) / Vec<T>::E, per = (nvec + nparts - 1) / nparts;
         v0 = min(part * per, nvec);
         v1 = min(v0 + per, nvec);
+        w0 = v0 < v1 && !whole(v0) ? v0 + 1 : v0;
+        w1 = w0 < v1 && !whole(v1 - 1) ? v1 - 1 : v1;
+    }
+    __device__ __forceinline__ const uint4* vectors() const { return reinterpret_cast<const uint4*>(z - head); }
+    // a vector that is not whole, element by element
+    __device__ __noinline__ uint4 edge(int vec) const {
+        uint32_t w[4];
+        constexpr uint32_t low = Vec<T>::LOWEST;
+        const int e0 = first(vec);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = low;
+#pragma unroll
+        for (int i = 0; i < Vec<T>::E; ++i) {
+            if (e0 + i < 0 || e0 + i >= V) continue;
+            if (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(z)[e0 + i];
+            else {
+                const uint32_t h = reinterpret_cast<const uint16_t*>(z)[e0 + i];
+                w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (h << 16) : (w[i / 2] & 0xffff0000u) | h;
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ __forceinline__ int first(int vec) const { return vec * Vec<T>::E - head; }      // element of place 0, may be < 0
     __device__ __forceinline__ bool whole(int vec) const { return first(vec) >= 0 && first(vec) <= V - Vec<T>::E; }
@@ -163,33 +183,21 @@ struct Share {
     }
 };
 
-// vectors base + j NT + t of the share, j < VPT; what is not there is -inf.  Read past the L1, evicted first:
-// nothing reads them again through the caches unless the share takes more than one round
+// vectors base + j NT + t of the share, j < VPT; what is not there is -inf.  Read past the L1, evicted first
 template <class T, int VPT>
 __device__ __forceinline__ void load_share(const Share<T>& r, int base, int nt, uint4 (&q)[VPT]) {
-    const uint4* p = reinterpret_cast<const uint4*>(r.z - r.head);
+    const uint4* p = r.vectors();
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int vec = base + j * nt + (int)threadIdx.x;
         q[j] = all_lowest<T>();
-        if (vec < r.v1 && r.whole(vec)) q[j] = __ldcs(p + vec);
+        if (vec >= r.w0 && vec < r.w1) q[j] = __ldcs(p + vec);
     }
+    if (r.w0 == r.v0 && r.w1 == r.v1) return;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int vec = base + j * nt + (int)threadIdx.x;
-        if (vec < r.v1 && !r.whole(vec)) {
-            const int e0 = r.first(vec);
-            uint32_t* w = &q[j].x;
-#pragma unroll
-            for (int i = 0; i < Vec<T>::E; ++i) {
-                if (e0 + i < 0 || e0 + i >= r.V) continue;
-                if (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(r.z)[e0 + i];
-                else {
-                    const uint32_t h = reinterpret_cast<const uint16_t*>(r.z)[e0 + i];
-                    w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (h << 16) : (w[i / 2] & 0xffff0000u) | h;
-                }
-            }
-        }
+        if (vec < r.v1 && (vec < r.w0 || vec >= r.w1)) q[j] = r.edge(vec);
     }
 }
 
@@ -210,115 +218,6 @@ __device__ __forceinline__ void store_vec(const Share<T>& r, T* out, int vec, co
     }
 }
 
-// ------------------------------------------------------------------ chunks of rows through shared memory
-struct FeedArgs {
-    int blocks;                // of a row's cluster
-    int chunks;                // per share
-    int chunk;                 // vectors per chunk
-    int slots;                 // chunks the ring holds
-    int passes;                // times a share is read
-    long long clusters;        // rows row, row + clusters, .. are one cluster's
-};
-constexpr int MAX_SLOTS = 8;
-
-template <class T>
-struct Feed {
-    const void* logits;
-    long long stride, N, V;
-    FeedArgs f;
-    uint4* ring;
-    uint64_t* full;
-    int rank;
-    // what is issued next (one thread), and the slot that is read next
-    long long row;
-    int pass, chunk, slot;
-    long long issued, taken;
-    int at;
-    uint32_t parity;
-
-    __device__ __forceinline__ Feed(const void* z, long long st, long long n, long long v, const FeedArgs& fa, uint4* r, uint64_t* bars, int rk,
-                                    long long first)
-        : logits(z), stride(st), N(n), V(v), f(fa), ring(r), full(bars), rank(rk), row(first), pass(0), chunk(0), slot(0), issued(0), taken(0), at(0), parity(0) {}
-
-    // whether a vector's 16 bytes all belong to the tensor (its first and last vector may not)
-    __device__ __forceinline__ bool inside(const Share<T>& r, int vec) const {
-        const T* p = r.z + r.first(vec);
-        return p >= static_cast<const T*>(logits) && p + Vec<T>::E <= static_cast<const T*>(logits) + (N - 1) * stride + V;
-    }
-    // the next chunk of the sequence into the next slot
-    __device__ void issue() {
-        if (row >= N) return;
-        const Share<T> r(logits, stride, row, V, rank, f.blocks);
-        const int first = r.v0 + chunk * f.chunk;
-        int lo = first, hi = min(first + f.chunk, r.v1);
-        if (lo < hi && !inside(r, lo)) ++lo;
-        if (lo < hi && !inside(r, hi - 1)) --hi;
-        const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16u : 0u;
-        ++issued;
-        mbar_expect(&full[slot], bytes);
-        if (bytes) bulk_load(ring + slot * f.chunk + (lo - first), reinterpret_cast<const uint4*>(r.z - r.head) + lo, bytes, &full[slot]);
-        if (++slot == f.slots) slot = 0;
-        if (++chunk < f.chunks) return;
-        chunk = 0;
-        if (++pass < f.passes) return;
-        pass = 0;
-        row += f.clusters;
-    }
-    __device__ __forceinline__ bool wait() const { return mbar_wait(&full[at], parity); }
-    // the thread that issues, after a wait that ran out: says so, and lets the copies under way arrive (each wait is
-    // bounded) before the block's memory goes to another
-    __device__ void give_up(int* status) {
-        flag_status(status, QS_TIMEOUT);
-        for (; taken < issued; next()) wait();
-    }
-    __device__ __forceinline__ void next() {
-        ++taken;
-        if (++at == f.slots) {
-            at = 0;
-            parity ^= 1u;
-        }
-    }
-    // this thread's vectors of a landed chunk; places outside the row are -inf
-    template <int VPT>
-    __device__ __forceinline__ void read(const Share<T>& r, int c, int slot_at, uint4 (&q)[VPT]) const {
-        const int first = r.v0 + c * f.chunk, end = min(first + f.chunk, r.v1), nt = blockDim.x;
-        const uint4* p = ring + slot_at * f.chunk;
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int i = j * nt + (int)threadIdx.x;
-            q[j] = all_lowest<T>();
-            if (i < f.chunk && first + i < end) q[j] = p[i];
-        }
-        // only a row's first and last vector: a look at the share's ends tells whether the chunk can hold them
-        if (first != 0 && end * Vec<T>::E - r.head <= r.V) return;
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int i = j * nt + (int)threadIdx.x, vec = first + i, e0 = r.first(vec);
-            if (i >= f.chunk || vec >= end || r.whole(vec)) continue;
-            if (!inside(r, vec)) q[j] = edge_vec(r, vec);
-            else
-                for (int e = 0; e < Vec<T>::E; ++e)
-                    if (e0 + e < 0 || e0 + e >= r.V) drop<T>(q[j], e);
-        }
-    }
-    // a vector that is not whole, element by element
-    static __device__ uint4 edge_vec(const Share<T>& r, int vec) {
-        uint4 q = all_lowest<T>();
-        uint32_t* w = &q.x;
-        const int e0 = r.first(vec);
-#pragma unroll
-        for (int i = 0; i < Vec<T>::E; ++i) {
-            if (e0 + i < 0 || e0 + i >= r.V) continue;
-            if (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(r.z)[e0 + i];
-            else {
-                const uint32_t h = reinterpret_cast<const uint16_t*>(r.z)[e0 + i];
-                w[i / 2] = i & 1 ? (w[i / 2] & 0xffffu) | (h << 16) : (w[i / 2] & 0xffff0000u) | h;
-            }
-        }
-        return q;
-    }
-};
-
 // ------------------------------------------------------------------ statistics
 struct Stat { float m, s, u; };
 
@@ -335,20 +234,44 @@ __device__ __forceinline__ float warp_sum(float v) {
 // the shift that a part's exponents take: its maximum, or 0 where everything is masked
 __device__ __forceinline__ float shift_of(float m) { return m == neg_inf() ? 0.0f : m; }
 
+// The exponentials of a batch of vectors relative to m: s += sum e, u += sum e d.  One multiply-add per pair gives
+// d + delta = z c2 - fl(m c2); the rounding error delta of m c2 is the same in all places and is taken out of the
+// sums.  False where this form does not serve: u turns to NaN where a place is masked (0 times -inf), and m c2 may be
+// out of range
 template <class T, int VPT, bool ENT>
-__device__ __forceinline__ void add_exps(const uint4 (&q)[VPT], float m, float c2, f2& s, f2& u) {
-    const float sh = shift_of(m);
-    const f2 minus = make_f2(-sh, -sh), c = make_f2(c2, c2);
+__device__ __forceinline__ bool add_exps(const uint4 (&q)[VPT], float m, float c2, float& s_all, float& u_all) {
+    const float ref = m * c2;
+    const f2 minus = make_f2(-ref, -ref), c = make_f2(c2, c2);
+    f2 s = make_f2(0.0f, 0.0f), u = s;
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int i = 0; i < Vec<T>::E / 2; ++i) {
-            f2 d = mul2(add2(Vec<T>::pair(q[j], i), minus), c);
-            if (ENT) d = floor2(d);
-            const f2 e = ex2_2(d);
+            const f2 d = fma2(Vec<T>::pair(q[j], i), c, minus), e = ex2_2(d);
             s = add2(s, e);
             if (ENT) u = fma2(e, d, u);
         }
+    const float2 ps = parts(s), pu = parts(u);
+    const float delta = fmaf(m, c2, -ref), w = ex2(-delta);
+    const float sum = (ps.x + ps.y) * w, sum_d = ENT ? fmaf(-delta, sum, (pu.x + pu.y) * w) : 0.0f;
+    if (!(fabsf(ref) < 65536.0f) || (ENT && !(sum_d == sum_d))) return false;
+    s_all += sum;
+    if (ENT) u_all += sum_d;
+    return true;
+}
+// the same for one vector in a form that serves always: z - m first, masked places and overflow made finite
+template <class T>
+__device__ __noinline__ float2 add_exps_exact(uint4 q, float m, float c2) {
+    const f2 minus = make_f2(-m, -m), c = make_f2(c2, c2);
+    f2 s = make_f2(0.0f, 0.0f), u = s;
+#pragma unroll
+    for (int i = 0; i < Vec<T>::E / 2; ++i) {
+        const f2 d = floor2(mul2(add2(Vec<T>::pair(q, i), minus), c)), e = ex2_2(d);
+        s = add2(s, e);
+        u = fma2(e, d, u);
+    }
+    const float2 ps = parts(s), pu = parts(u);
+    return make_float2(ps.x + ps.y, pu.x + pu.y);
 }
 
 // the larger maximum takes over
@@ -366,22 +289,27 @@ __device__ __forceinline__ float thread_max_of(const uint4 (&q)[VPT]) {
     return Vec<T>::top(m);
 }
 
-// a thread's running statistics take in the vectors of a chunk
+// A thread's running statistics take in a batch of vectors, of which m is the largest value.  Their reference st.m
+// moves when the exponents would pass 2^REACH, so that most batches need no new scale; the reach is small because the
+// entropy's u loses REACH units in the last place when it moves on to the row's maximum at the end
+constexpr float REACH = 3.0f;
 template <class T, int VPT, bool ENT>
-__device__ __forceinline__ void take_chunk(Stat& st, const uint4 (&q)[VPT], float c2) {
-    const float m = fmaxf(st.m, thread_max_of<T, VPT>(q));
-    if (m > st.m) st = rescale(st, m, c2);
-    f2 s = make_f2(st.s, 0.0f), u = make_f2(st.u, 0.0f);
-    add_exps<T, VPT, ENT>(q, m, c2, s, u);
-    const float2 ps = parts(s), pu = parts(u);
-    st.s = ps.x + ps.y;
-    if (ENT) st.u = pu.x + pu.y;
+__device__ __forceinline__ void take(Stat& st, const uint4 (&q)[VPT], float m, float c2) {
+    if (!((m - st.m) * c2 <= REACH) && m > st.m) st = rescale(st, m, c2);
+    const float ref = shift_of(st.m);
+    if (add_exps<T, VPT, ENT>(q, ref, c2, st.s, st.u)) return;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const float2 x = add_exps_exact<T>(q[j], ref, c2);
+        st.s += x.x;
+        if (ENT) st.u += x.y;
+    }
 }
 
-// the warp's statistics from its threads'
+// the warp's statistics from its threads'; `largest` is the thread's largest value
 template <bool ENT>
-__device__ __forceinline__ Stat join_warp(Stat st, float c2) {
-    const float m = warp_max(st.m);
+__device__ __forceinline__ Stat join_warp(Stat st, float largest, float c2) {
+    const float m = warp_max(largest);
     const Stat r = rescale(st, m, c2);
     return Stat{m, warp_sum(r.s), ENT ? warp_sum(r.u) : 0.0f};
 }
