@@ -26,6 +26,9 @@ constexpr int MAX_THREADS = 256;
 constexpr int MAX_WARPS = MAX_THREADS / 32;
 constexpr int PARTS = MAX_BLOCKS * MAX_WARPS;
 constexpr int VPT = 4;                     // vectors per thread and batch
+constexpr int VK = 8;                      // the same where the row is kept: 128 threads and 8 vectors take a tenth less than 256 and 4
+constexpr int SLOTS = 16;                  // stretches of a thread's share whose largest elements are kept apart
+constexpr int PAIRS = 512;                 // such stretches that are looked through again
 constexpr int MOST = QS_MAX_TOP + QS_MAX_TOP / 4 + 16;      // candidates ranked against one another
 constexpr int CANDS = 1024;                // candidates a block keeps, and a row's blocks send in all (>= MAX_BLOCKS QS_MAX_TOP)
 
@@ -48,7 +51,7 @@ struct RowArgs {
     void* grad; long long grad_stride;
     int wide;                              // the gradient's rows lie like the logits' rows within 16 bytes
     int blocks;                            // blocks per row
-    int groups;                            // maxima per warp that bound the K-th alternative
+    int per;                               // batches per stretch whose maximum is kept
     int* status;
 };
 
@@ -70,11 +73,11 @@ __device__ __forceinline__ int block_count(int mine, int* sums) {
     return total;
 }
 
-// A cut that takes between K and `most` places, by bisection over the keys and then, where equal keys alone are more
-// than that, over the columns.  `count(cut)` is the number of places a cut takes; Cut{lo, ~0} takes more than `most`
+// A cut that takes between K and `most` places, by bisection over the keys in [lo, hi) and then, where equal keys alone
+// are more than that, over the columns.  `count(cut)` is the number of places a cut takes, the same in all threads;
+// Cut{lo, ~0} takes more than `most`, Cut{hi, ~0} none
 template <class Count>
-__device__ Cut find_cut(int K, int most, uint32_t lo, uint32_t columns, Count count) {
-    uint32_t hi = 0xffffffffu;
+__device__ __forceinline__ Cut find_cut(int K, int most, uint32_t lo, uint32_t hi, uint32_t columns, Count count) {
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
         const int c = count(Cut{mid, 0xffffffffu});
@@ -100,92 +103,71 @@ __device__ Cut find_cut(int K, int most, uint32_t lo, uint32_t columns, Count co
 }
 
 struct TopShared {
-    uint32_t group[32 * MAX_WARPS];        // keys of the block's group maxima so far
     unsigned long long list[CANDS];        // candidates (key, ~column) of the block's share, then of the cluster's
-    unsigned long long merged[CANDS];      // what the cluster's blocks have left, block b's at b * CANDS / blocks (first block)
     int count[MAX_BLOCKS];
     unsigned long long last[MOST];         // what is left of the list for the ranking
     int n, left, sums[MAX_WARPS];          // candidates in the list; entries in `last`
-    uint32_t bound;                        // keys below it are no alternatives
+    int pairs;                             // (slot, thread) pairs whose largest element reaches the bound
+    uint16_t pair[PAIRS];
+    uint32_t low[MAX_WARPS], high[MAX_WARPS];
 };
 
-// One warp: between K and `most` (<= MOST) of the list's n entries, the largest, into `last`; all if there are no more than
-// that.  Bisection over the keys, then, where equal keys alone are more, over the columns
-__device__ void shrink_list(const unsigned long long* list, int n, int K, int most, uint32_t columns, unsigned long long* last, int* left) {
-    const int lane = threadIdx.x & 31;
-    Cut cut{0, 0xffffffffu};
-    if (n > most) {
-        uint32_t lo = 0xffffffffu, hi = 0;
-        for (int i = lane; i < n; i += 32) {
-            const uint32_t k = (uint32_t)(list[i] >> 32);
-            lo = min(lo, k);
-            hi = max(hi, k);
-        }
-        lo = __reduce_min_sync(~0u, lo);
-        hi = __reduce_max_sync(~0u, hi) + 1;
-        bool done = false;
-        auto count = [&](Cut c) {
-            int k = 0;
-            for (int i = lane; i < n; i += 32) k += takes(c, list[i]);
-            return __reduce_add_sync(~0u, k);
-        };
-        while (hi - lo > 1 && !done) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            const int c = count(Cut{mid, 0xffffffffu});
-            if (c >= K) {
-                lo = mid;
-                done = c <= most;
-            } else {
-                hi = mid;
-            }
-        }
-        cut = Cut{lo, 0xffffffffu};
-        if (!done && count(cut) > most) {
-            uint32_t a = 0, b = columns - 1;
-            while (a < b) {
-                const uint32_t mid = a + (b - a) / 2;
-                if (count(Cut{lo, mid}) >= K) b = mid;
-                else a = mid + 1;
-            }
-            cut.idx = b;
-        }
+// smallest and largest key of the block's threads
+__device__ __forceinline__ uint2 block_range(uint32_t low, uint32_t high, TopShared& t) {
+    const uint32_t a = __reduce_min_sync(~0u, low), b = __reduce_max_sync(~0u, high);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) {
+        t.low[threadIdx.x >> 5] = a;
+        t.high[threadIdx.x >> 5] = b;
     }
-    int at = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const unsigned long long e = i0 + lane < n ? list[i0 + lane] : 0ull;
-        const bool in = i0 + lane < n && takes(cut, e);
-        const uint32_t who = __ballot_sync(~0u, in);
-        if (in) last[at + __popc(who & ((1u << lane) - 1u))] = e;
-        at += __popc(who);
-    }
-    if (lane == 0) *left = at;
+    __syncthreads();
+    uint2 r = make_uint2(t.low[0], t.high[0]);
+    for (int i = 1; i < (int)(blockDim.x >> 5); ++i) r = make_uint2(min(r.x, t.low[i]), max(r.y, t.high[i]));
+    return r;
 }
 
-// The largest key found that at least K of the n group maxima reach, KEY_LOWEST - 1 if fewer are above -inf.  One warp
-__device__ __forceinline__ uint32_t group_bound(const uint32_t* group, int n, int K) {
-    const int lane = threadIdx.x & 31;
-    uint32_t top = 0;
-    int live = 0;
-    for (int i = lane; i < n; i += 32) {
-        top = max(top, group[i]);
-        live += group[i] >= KEY_LOWEST;
-    }
-    top = __reduce_max_sync(~0u, top);
-    if (__reduce_add_sync(~0u, live) < K) return KEY_LOWEST - 1;
-    uint32_t lo = KEY_LOWEST, hi = top + 1;
+// The largest key found that at least K of the threads' maxima reach (a few more may), 0 if fewer are above -inf
+__device__ uint32_t maxima_bound(uint32_t mine, int K, TopShared& t) {
+    const int live = __syncthreads_count(mine >= KEY_LOWEST);
+    if (live < K) return 0;
+    const uint2 range = block_range(mine >= KEY_LOWEST ? mine : 0xffffffffu, mine, t);
+    uint32_t lo = range.x, hi = range.y + 1;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
-        int c = 0;
-        for (int i = lane; i < n; i += 32) c += group[i] >= mid;
-        c = __reduce_add_sync(~0u, c);
+        const int c = __syncthreads_count(mine >= mid);
         if (c >= K) {
             lo = mid;
-            if (c <= K + K / 4 + 1) break;
+            if (c <= K + K / 8 + 1) break;
         } else {
             hi = mid;
         }
     }
     return lo;
+}
+
+// Between K and `most` (<= MOST) of the list's n entries, the largest, into `last`; all if there are no more than that
+__device__ void shrink_list(TopShared& t, int n, int K, int most, uint32_t columns) {
+    const int nt = blockDim.x;
+    Cut cut{0, 0xffffffffu};
+    if (n > most) {
+        uint32_t low = 0xffffffffu, high = 0;
+        for (int i = threadIdx.x; i < n; i += nt) {
+            low = min(low, (uint32_t)(t.list[i] >> 32));
+            high = max(high, (uint32_t)(t.list[i] >> 32));
+        }
+        const uint2 range = block_range(low, high, t);
+        cut = find_cut(K, most, range.x, range.y + 1, columns, [&](Cut c) {
+            int k = 0;
+            for (int i = threadIdx.x; i - (int)threadIdx.x < n; i += nt) k += __syncthreads_count(i < n && takes(c, t.list[i]));
+            return k;
+        });
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) t.left = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += nt)
+        if (takes(cut, t.list[i])) t.last[atomicAdd(&t.left, 1)] = t.list[i];
+    __syncthreads();
 }
 
 // calls f(z, column) for the elements of a vector that reach `bound`
@@ -208,111 +190,145 @@ __device__ __forceinline__ void each_of_row(const Share<T>& r, int v0, int v1, f
 
 __device__ __forceinline__ unsigned long long entry_of(float z, uint32_t col) { return ((unsigned long long)key_of(z) << 32) | (uint32_t)~col; }
 
-// More elements of the vectors [v0, v1) reach the bound than the list holds (ties, a mask, or an order that defeats the
-// bound): the list is made anew with what an exact cut takes of them, reading them once per step of a bisection
-template <class T>
-__device__ __noinline__ void cut_exactly(TopShared& t, const Share<T>& r, int v0, int v1, int K) {
-    const float bound = value_of(t.bound);
-    const Cut cut = find_cut(K, CANDS / 2, t.bound - 1, (uint32_t)r.V, [&](Cut c) {
-        int k = 0;
-        each_of_row<T>(r, v0, v1, bound, [&](float z, uint32_t col) { k += takes(c, key_of(z), col); });
-        return block_count(k, t.sums);
-    });
-    __syncthreads();
-    if (threadIdx.x == 0) t.n = 0;
-    __syncthreads();
-    each_of_row<T>(r, v0, v1, bound, [&](float z, uint32_t col) {
-        if (takes(cut, key_of(z), col)) t.list[atomicAdd(&t.n, 1)] = entry_of(z, col);
-    });
-    // K elements reach cut.key, all in earlier columns than what is still to come
-    if (threadIdx.x == 0) t.bound = max(t.bound, cut.key + 1);
-    __syncthreads();
+__device__ __forceinline__ void put_candidate(TopShared& t, float z, uint32_t col) {
+    const int at = atomicAdd(&t.n, 1);
+    if (at < CANDS) t.list[at] = entry_of(z, col);
 }
 
-// Statistics of the row, and with TOP its alternatives, in one pass.  Candidates are the elements that reach a bound
-// below which no alternative can lie: the K-th largest of group maxima so far (a group is 32 / groups lanes' share of
-// the row).  It is taken after the first batch, and again after 2, 4, 8, .. without a barrier: maxima that are late
-// or early only make it lower.
+// The elements of the share that reach the bound, from the stretches whose largest does; false (and no list) if there are
+// too many.  All threads
+template <class T>
+__device__ bool collect(TopShared& t, const Share<T>& r, const float* slot_max, int slots, int per, float bound) {
+    const int nt = blockDim.x;
+    __syncthreads();
+    if (threadIdx.x == 0) t.n = t.pairs = 0;
+    __syncthreads();
+    for (int i = 0; i < slots; ++i)
+        if (slot_max[i * nt + threadIdx.x] >= bound) {
+            const int at = atomicAdd(&t.pairs, 1);
+            if (at < PAIRS) t.pair[at] = (uint16_t)(i * nt + threadIdx.x);
+        }
+    __syncthreads();
+    if (t.pairs > PAIRS) return false;
+    auto put = [&](float z, uint32_t col) { put_candidate(t, z, col); };
+    const int each = per * VPT, all = t.pairs * each;
+    for (int i = threadIdx.x; i < all; i += nt) {
+        const int pair = t.pair[i / each], vec = r.w0 + (pair / nt * each + i % each) * nt + pair % nt;
+        if (vec < r.w1) each_above<T>(r.vectors()[vec], r.first(vec), bound, put);
+    }
+    if (threadIdx.x == 0 && r.w0 > r.v0) each_above<T>(r.edge(r.v0), r.first(r.v0), bound, put);
+    if ((int)threadIdx.x == nt - 1 && r.w1 < r.v1) each_above<T>(r.edge(r.w1), r.first(r.w1), bound, put);
+    __syncthreads();
+    return t.n <= CANDS;
+}
+
+// Too many elements reach the bound: equal ones, as a rule (a mask of the lowest value).  What lies above it, and of the
+// equal ones the first that make it K, stretch of columns by stretch; an order that defeats the bound itself
+// is cut exactly, reading the row once per step of a bisection
+template <class T>
+__device__ __noinline__ void collect_hard(TopShared& t, const Share<T>& r, const float* slot_max, int slots, int per, int K, uint32_t bound) {
+    const int nt = blockDim.x;
+    if (!collect<T>(t, r, slot_max, slots, per, value_of(bound + 1))) {
+        const Cut cut = find_cut(K, CANDS / 2, bound - 1, 0xff800001u, (uint32_t)r.V, [&](Cut c) {
+            int k = 0;
+            each_of_row<T>(r, r.v0, r.v1, value_of(bound), [&](float z, uint32_t col) { k += takes(c, key_of(z), col); });
+            return block_count(k, t.sums);
+        });
+        __syncthreads();
+        if (threadIdx.x == 0) t.n = 0;
+        __syncthreads();
+        each_of_row<T>(r, r.v0, r.v1, value_of(bound), [&](float z, uint32_t col) {
+            if (takes(cut, key_of(z), col)) put_candidate(t, z, col);
+        });
+        __syncthreads();
+        return;
+    }
+    const float tie = value_of(bound);
+    int have = t.n;
+    for (int v0 = r.v0; v0 < r.v1 && have < K; v0 += nt * VPT) {
+        const int v1 = min(v0 + nt * VPT, r.v1);
+        auto count = [&](uint32_t col_most) {
+            int k = 0;
+            each_of_row<T>(r, v0, v1, tie, [&](float z, uint32_t col) { k += key_of(z) == bound && col <= col_most; });
+            return block_count(k, t.sums);
+        };
+        uint32_t to = 0xffffffffu;
+        if (count(to) > CANDS - have) {            // a column that leaves enough of them, and few enough
+            uint32_t a = (uint32_t)max(r.first(v0), 0), b = (uint32_t)r.first(v1);
+            while (a < b) {
+                const uint32_t mid = a + (b - a) / 2;
+                const int c = count(mid);
+                if (c >= K - have) {
+                    b = mid;
+                    if (c <= CANDS - have) break;
+                } else {
+                    a = mid + 1;
+                }
+            }
+            to = b;
+        }
+        __syncthreads();
+        each_of_row<T>(r, v0, v1, tie, [&](float z, uint32_t col) {
+            if (key_of(z) == bound && col <= to) put_candidate(t, z, col);
+        });
+        __syncthreads();
+        have = t.n;
+        __syncthreads();
+    }
+}
+
+// Statistics of the row, and with TOP its alternatives.  While the row comes by, each thread keeps the largest element of
+// each of up to 16 stretches of its share; the K-th largest of the threads' maxima is a bound below which no alternative
+// can lie, and the few stretches that reach it (about K) are read again, from the L2.
 template <class T, bool TOP>
-__global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(const RowArgs a) {
+__global__ void __launch_bounds__(MAX_THREADS, TOP ? 5 : 6) token_logp_kernel(const RowArgs a) {
     __shared__ float4 part[PARTS];
     __shared__ float row_m, row_ls, row_lse;
     __shared__ TopShared top[1];                   // (no room where it is not used)
+    // TOP: the stretches' maxima (slots x threads), and what a cluster's blocks have left, block b's at b * CANDS / blocks
+    extern __shared__ unsigned long long merged[];
     const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
     const long long n = a.row0 + blockIdx.x / blocks;
     const float c2 = a.scale * LOG2E;
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
     const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
-    if (TOP && threadIdx.x == 0) { top->n = 0; top->bound = KEY_LOWEST; }
     Stat st{neg_inf(), 0.0f, 0.0f};
     float mine = neg_inf();                        // the thread's largest
-    int batch = 0;
-    for (int base = r.v0; base < r.v1; base += nt * VPT, ++batch) {
-        uint4 q[VPT];
-        if (base >= r.w0 && base + nt * VPT <= r.w1) {
-#pragma unroll
-            for (int j = 0; j < VPT; ++j) q[j] = __ldcs(r.vectors() + base + j * nt + threadIdx.x);
-        } else {
-            load_share<T, VPT>(r, base, nt, q);
-        }
-        const float m = thread_max_of<T, VPT>(q);
-        take<T, VPT, true>(st, q, m, c2);
+    float* slot_max = reinterpret_cast<float*>(merged + (blocks > 1 ? CANDS : 0)) + threadIdx.x;
+    float stretch = neg_inf();
+    int batch = 0, slot = 0;
+    each_batch<T, VPT>(r, [&](auto& q, int vec, auto more) {
+        constexpr int P = sizeof(q) / sizeof(uint4);
+        const float m = thread_max_of<T, P>(q);
+        take<T, P, true, decltype(more)::value>(st, q, m, c2);
         mine = fmaxf(mine, m);
-        if (!TOP) continue;
-        const bool renew = (batch & (batch + 1)) == 0;
-        if (renew) {
-            const int width = 32 / a.groups;
-            float g = mine;
-            for (int o = 1; o < width; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-            if (lane % width == 0) top->group[warp * a.groups + lane / width] = key_of(g);
-            if (batch == 0) __syncthreads();
-            else __syncwarp();
-            if (warp == (batch == 0 ? 0 : warps - 1)) {
-                const uint32_t b = group_bound(top->group, warps * a.groups, a.K);
-                if (lane == 0) atomicMax(&top->bound, b);
-            }
-            if (batch == 0) __syncthreads();
-        }
-        const float bound = value_of(*reinterpret_cast<volatile uint32_t*>(&top->bound));
-        if (m >= bound) {
-            const int e0 = r.first(base + (int)threadIdx.x), step = nt * Vec<T>::E;
-#pragma unroll
-            for (int j = 0; j < VPT; ++j)
-                each_above<T>(q[j], e0 + j * step, bound, [&](float z, uint32_t col) {
-                    const int at = atomicAdd(&top->n, 1);
-                    if (at < CANDS) top->list[at] = entry_of(z, col);
-                });
-        }
-        if (batch == 0) {
-            // what equals the bound in a later batch, thus in a later column, comes after the K that reach it
-            __syncthreads();
-            const uint32_t b = top->bound;
-            if (top->n > CANDS) {
-                cut_exactly<T>(*top, r, r.v0, min(r.v0 + nt * VPT, r.v1), a.K);
-            } else {
-                __syncthreads();
-                if (threadIdx.x == 0 && b > KEY_LOWEST) top->bound = b + 1;
-                __syncthreads();
+        if (TOP) {
+            if (vec < r.w0 || vec >= r.w1) return; // (vectors that are not whole are looked through in any case)
+            stretch = fmaxf(stretch, m);
+            slot_max[slot * nt] = stretch;
+            if (++batch == a.per) {
+                batch = 0;
+                ++slot;
+                stretch = neg_inf();
             }
         }
+    });
+    if (TOP) {
+        if (batch == 0) slot_max[slot * nt] = neg_inf();       // (a thread without a vector in the last batch)
+        const int slots = (r.w1 - r.w0 + nt * VPT * a.per - 1) / (nt * VPT * a.per);
+        const uint32_t key = max(maxima_bound(key_of(mine), a.K, *top), KEY_LOWEST);
+        if (!collect<T>(*top, r, slot_max - threadIdx.x, slots, a.per, value_of(key)))
+            collect_hard<T>(*top, r, slot_max - threadIdx.x, slots, a.per, a.K, key);
     }
     long long t = -1;
     float zt = 0.0f;
-    if (rank == 0 && threadIdx.x == nt - 1 && a.logp) {
+    if (rank == 0 && (int)threadIdx.x == nt - 1 && a.logp) {
         t = a.tok.at(n);
         if (t >= a.V) flag_status(a.status, QS_INVALID_ARG);
         else if (t >= 0) zt = to_float(r.z[t]);
     }
-    if (TOP) {
-        __syncthreads();
-        if (top->n > CANDS) {
-            if (threadIdx.x == 0) top->bound = KEY_LOWEST;
-            __syncthreads();
-            cut_exactly<T>(*top, r, r.v0, r.v1, a.K);
-        }
-    }
-    const int most = min(a.K + a.K / 4 + 16, nt);  // candidates that are ranked, a thread each
+    const int most = min(max(a.K + a.K / 4 + 16, 96), nt);       // candidates that are ranked, a thread or more each
     const Stat w = join_warp<true>(st, mine, c2);
     const float4 sent = make_float4(w.m, w.s, w.u, 0.0f);
     if (blocks == 1) {
@@ -320,11 +336,10 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(co
         __syncthreads();
     } else {
         cluster_wait();
-        if (TOP && warp == 0) {
-            shrink_list(top->list, top->n, a.K, min(most, CANDS / blocks), (uint32_t)a.V, top->last, &top->left);
-            __syncwarp();
-            for (int i = lane; i < top->left; i += 32) remote_store(remote_addr(&top->merged[rank * (CANDS / blocks) + i], 0), top->last[i]);
-            if (lane == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->left);
+        if (TOP) {
+            shrink_list(*top, top->n, a.K, min(most, CANDS / blocks), (uint32_t)a.V);
+            for (int i = threadIdx.x; i < top->left; i += nt) remote_store(remote_addr(&merged[rank * (CANDS / blocks) + i], 0), top->last[i]);
+            if (threadIdx.x == 0) remote_store(remote_addr(&top->count[rank], 0), (uint32_t)top->left);
         }
         if (lane == 0) remote_store(remote_addr(&part[rank * warps + warp], 0), sent);
         cluster_arrive();
@@ -332,7 +347,7 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(co
         cluster_wait();
     }
     if (warp == warps - 1) {
-        const Stat v = join_parts(part, warps * blocks, c2);
+        const Stat v = final_stat(join_parts(part, warps * blocks, c2), c2);
         const bool empty = v.m == neg_inf() && v.s == 0.0f;
         const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
         if (lane == 31) {                          // the thread that holds the token
@@ -347,13 +362,12 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(co
     if (blocks > 1) {
         n_list = 0;
         for (int b = 0; b < blocks; ++b) {
-            for (int i = threadIdx.x; i < top->count[b]; i += nt) top->list[n_list + i] = top->merged[b * (CANDS / blocks) + i];
+            for (int i = threadIdx.x; i < top->count[b]; i += nt) top->list[n_list + i] = merged[b * (CANDS / blocks) + i];
             n_list += top->count[b];
         }
         __syncthreads();
     }
-    if (warp == 0) shrink_list(top->list, n_list, a.K, most, (uint32_t)a.V, top->last, &top->left);
-    __syncthreads();
+    shrink_list(*top, n_list, a.K, most, (uint32_t)a.V);         // (its barriers publish row_m and the others, too)
     const float lse = row_lse, ls = row_ls, m = row_m;
     const bool broken = !(lse == lse);
     auto put = [&](int at, long long id, float lp) {
@@ -361,24 +375,48 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 4 : 6) token_logp_kernel(co
         else static_cast<int*>(a.top_ids)[n * a.K + at] = (int)id;
         a.top_logp[n * a.K + at] = lp;
     };
+    // places by comparison with all others, each entry by as many threads of a warp as there are
     const int left = top->left;
-    if ((int)threadIdx.x < left && !broken) {
-        const unsigned long long v = top->last[threadIdx.x];
-        int place = 0;
-#pragma unroll 4
-        for (int x = 0; x < left; ++x) place += top->last[x] > v;
-        if (place < a.K) put(place, ~(uint32_t)v, fmaf(value_of((uint32_t)(v >> 32)) - m, a.scale, -ls));
-    }
+    int split = 1;
+    while (split < 32 && left * split * 2 <= nt) split *= 2;
+    const int of = (int)threadIdx.x / split, share = (int)threadIdx.x % split;
+    const unsigned long long v = of < left ? top->last[of] : 0ull;
+    int place = 0;
+    for (int x = share; x < left; x += split) place += top->last[x] > v;
+    for (int o = 1; o < split; o <<= 1) place += __shfl_xor_sync(~0u, place, o);
+    if (of < left && share == 0 && place < a.K && !broken) put(place, ~(uint32_t)v, fmaf(value_of((uint32_t)(v >> 32)) - m, a.scale, -ls));
     for (int k = (broken ? 0 : left) + (int)threadIdx.x; k < a.K; k += nt) put(k, -1, broken ? lse : neg_inf());
 }
 
-template <class T, int VG, bool ENT>
-__global__ void __launch_bounds__(256) token_logp_grad_kernel(const RowArgs a) {
+// One pass over the row: f(q) turns a vector of logits into its gradient.  Four loads in flight; each vector is read and
+// written by one thread, so that the gradient may take the logits' place
+template <class T, class F>
+__device__ __forceinline__ void map_row(const Share<T>& r, T* out, bool wide, F f) {
     const int nt = blockDim.x;
+    const uint4* p = r.vectors();
+    uint4* to = reinterpret_cast<uint4*>(out - r.head);
+    if (wide) {
+        int vec = r.w0 + (int)threadIdx.x;
+        for (; vec + 3 * nt < r.w1; vec += 4 * nt) {
+            uint4 q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[j] = __ldcs(p + vec + j * nt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) __stcs(to + vec + j * nt, f(q[j], vec + j * nt));
+        }
+        for (; vec < r.w1; vec += nt) __stcs(to + vec, f(__ldcs(p + vec), vec));
+        if (threadIdx.x == 0 && r.w0 > r.v0) store_edge(r, out, r.v0, f(r.edge(r.v0), r.v0));
+        if ((int)threadIdx.x == nt - 1 && r.w1 < r.v1) store_edge(r, out, r.w1, f(r.edge(r.w1), r.w1));
+    } else {
+        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt)
+            store_edge(r, out, vec, f(vec >= r.w0 && vec < r.w1 ? __ldcs(p + vec) : r.edge(vec), vec));
+    }
+}
+
+template <class T, bool ENT>
+__global__ void __launch_bounds__(MAX_THREADS) token_logp_grad_kernel(const RowArgs a) {
     const long long n = a.row0 + blockIdx.x / a.blocks;
     const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
-    uint4 q[VG];
-    load_share<T, VG>(r, r.v0, nt, q);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const long long t = a.tok.p ? a.tok.at(n) : -1;
     const float lse = a.in_lse[n];
@@ -396,15 +434,12 @@ __global__ void __launch_bounds__(256) token_logp_grad_kernel(const RowArgs a) {
     const f2 slope = make_f2(-h * a.scale, -h * a.scale), offset = make_f2(-at_one, -at_one);
     const int hot = t >= 0 && t < a.V ? (int)((t + r.head) / Vec<T>::E) : -1;
     const float hot_g = g * a.scale;
-#pragma unroll
-    for (int j = 0; j < VG; ++j) {
-        const int vec = r.v0 + j * nt + (int)threadIdx.x;
-        if (vec >= r.v1) continue;
+    map_row<T>(r, out, a.wide, [&](const uint4& q, int vec) {
         f2 d[Vec<T>::E / 2];
 #pragma unroll
         for (int i = 0; i < Vec<T>::E / 2; ++i) {
             // log p; p times minus (g + h (log p + entropy))
-            f2 lp = fma2(Vec<T>::pair(q[j], i), scale, minus);
+            f2 lp = fma2(Vec<T>::pair(q, i), scale, minus);
             if (ENT) lp = floor2(lp);
             d[i] = mul2(ex2_2(mul2(lp, l2e)), ENT ? fma2(lp, slope, offset) : offset);
         }
@@ -416,8 +451,8 @@ __global__ void __launch_bounds__(256) token_logp_grad_kernel(const RowArgs a) {
                 d[i] = make_f2(2 * i == e ? p.x + hot_g : p.x, 2 * i + 1 == e ? p.y + hot_g : p.y);
             }
         }
-        store_vec(r, out, vec, Vec<T>::pack(d), a.wide);
-    }
+        return Vec<T>::pack(d);
+    });
 }
 
 // ------------------------------------------------------------------ distillation
@@ -530,32 +565,54 @@ __device__ __forceinline__ float at_id(const TeacherShared& t, int K, int k, con
     return s.empty ? (t.bad ? s.in : 0.0f) : s.w * fmaf(p, s.in, -q);
 }
 
-// the gradient of one vector outside the ids, from d = log2 of p up to the factor 1 / norm
-template <class T, bool TAIL>
-__device__ __forceinline__ uint4 slope_vec(const f2* d, const Slope& s, float norm) {
+// The factor that turns 2^d into the gradient outside the ids; norm: 1 over the sum of the row's 2^d
+__device__ __forceinline__ float factor(const Slope& s, float norm) {
+    return s.empty ? (s.in == s.in ? 0.0f : s.in) : s.w * s.out * norm;
+}
+// rows whose p_T is too small for a quotient: what is left of the gradient, exponents first
+template <class T>
+__device__ __noinline__ uint4 thin_vec(const f2* d, const Slope& s, float norm) {
     constexpr int P = Vec<T>::E / 2;
     f2 g[P];
-    const float f = s.empty ? (s.in == s.in ? 0.0f : s.in) : s.w * s.out * norm;
-    const f2 ff = make_f2(f, f);
+    const float f = factor(s, norm), sub = s.log_tail * LOG2E - log2f(norm), c = s.log_tail > neg_inf() ? -s.w * s.rest : 0.0f;
 #pragma unroll
-    for (int i = 0; i < P; ++i) g[i] = mul2(ex2_2(d[i]), ff);
-    if (TAIL && s.thin && !s.empty && s.log_tail > neg_inf()) {
-        // 2^d norm / p_T, exponents first: norm is 1 / sum of the row's exponentials, or 1
-        const float sub = s.log_tail * LOG2E - log2f(norm), c = -s.w * s.rest;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const float2 x = parts(d[i]), y = parts(g[i]);
-            g[i] = make_f2(fmaf(c, ex2(x.x - sub), y.x), fmaf(c, ex2(x.y - sub), y.y));
-        }
+    for (int i = 0; i < P; ++i) {
+        const float2 x = parts(d[i]);
+        const float a = c == 0.0f ? 0.0f : c * ex2(x.x - sub), b = c == 0.0f ? 0.0f : c * ex2(x.y - sub);
+        g[i] = make_f2(fmaf(f, ex2(x.x), a), fmaf(f, ex2(x.y), b));
     }
     return Vec<T>::pack(g);
+}
+// the gradient of one vector outside the ids, from d = log2 of p times the sum
+template <class T>
+__device__ __forceinline__ uint4 slope_vec(const f2* d, float f) {
+    f2 g[Vec<T>::E / 2];
+    const f2 ff = make_f2(f, f);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::E / 2; ++i) g[i] = mul2(ex2_2(d[i]), ff);
+    return Vec<T>::pack(g);
+}
+
+// vectors base + j nt + t of the share, from where it is kept or from memory
+template <class T, bool KEEP>
+__device__ __forceinline__ void load_kept(const Share<T>& r, const uint4* kept, int base, uint4 (&q)[VK]) {
+    if (!KEEP) {
+        load_share<T, VK>(r, base, blockDim.x, q);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < VK; ++j) {
+        const int vec = base + j * (int)blockDim.x + (int)threadIdx.x;
+        q[j] = all_lowest<T>();
+        if (vec < r.v1) q[j] = kept[vec - r.v0];
+    }
 }
 
 // Loss and, with a.grad, its gradient.  KEEP: the share lies in shared memory from one bulk copy until its gradient is
 // written; otherwise (rows beyond a cluster's shared memory) it is read twice
 template <class T, bool KEEP, bool TAIL>
-__global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a) {
-    constexpr int E = Vec<T>::E, PER = (QS_MAX_TOP + 127) / 128;
+__global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a) {
+    constexpr int E = Vec<T>::E, PER = (QS_MAX_TOP + 31) / 32;
     extern __shared__ __align__(128) uint4 kept[];
     __shared__ uint64_t landed;
     __shared__ float4 part[PARTS];
@@ -619,28 +676,21 @@ __global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a
     }
     Stat st{neg_inf(), 0.0f, 0.0f};
     float largest = neg_inf();
-    for (int base = r.v0; base < r.v1; base += nt * VPT) {
-        uint4 q[VPT];
-        if (KEEP) {
+    // (one loop for all vectors: a second copy of its body for the rest costs more in instruction misses than it saves)
+    for (int base = r.v0; base < r.v1; base += nt * VK) {
+        uint4 q[VK];
+        load_kept<T, KEEP>(r, kept, base, q);
+        if (!KEEP && TAIL) {
 #pragma unroll
-            for (int j = 0; j < VPT; ++j) {
+            for (int j = 0; j < VK; ++j) {
                 const int vec = base + j * nt + (int)threadIdx.x;
-                q[j] = all_lowest<T>();
-                if (vec < r.v1) q[j] = kept[vec - r.v0];
+                if (vec < r.v1 && marks[(vec & 8191) >> 5] >> (vec & 31) & 1)
+                    for (int k = 0; k < a.K; ++k)
+                        if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
             }
-        } else {
-            load_share<T, VPT>(r, base, nt, q);
-            if (TAIL)
-#pragma unroll
-                for (int j = 0; j < VPT; ++j) {
-                    const int vec = base + j * nt + (int)threadIdx.x;
-                    if (vec < r.v1 && marks[(vec & 8191) >> 5] >> (vec & 31) & 1)
-                        for (int k = 0; k < a.K; ++k)
-                            if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
-                }
         }
-        const float most = thread_max_of<T, VPT>(q);
-        take<T, VPT, false>(st, q, most, c2);
+        const float most = thread_max_of<T, VK>(q);
+        take<T, VK, false, false>(st, q, most, c2);
         largest = fmaxf(largest, most);
     }
     const int readers = a.grad ? blocks : 1;       // blocks that need the row's statistics
@@ -665,7 +715,10 @@ __global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a
         }
         m = warp_max(m);
 #pragma unroll
-        for (int i = 0; i < Entries::PER; ++i) s += ex2((z[i] - shift_of(m)) * c2);
+        for (int i = 0; i < Entries::PER; ++i) {
+            const float at = shift_of(m);
+            s += ex2(in_range(at, c2) ? fmaf(z[i], c2, -(at * c2)) : (z[i] - at) * c2);
+        }
         s = warp_sum(s);
         const float4 v = make_float4(m, s, 0.0f, 0.0f);
         if (blocks == 1) {
@@ -695,9 +748,14 @@ __global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a
             const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
             const float s = x.s + y.s;
             // log of the share outside: near 1 the difference of two logs would cancel
-            log_tail = v.m == neg_inf() && v.s == 0.0f ? neg_inf() : fmaf(v.m - m, a.scale, logf(v.s) - logf(s));
+            const float out_s = final_stat(v, c2).s;
+            const bool none = v.m == neg_inf() && v.s == 0.0f;
+            const float out_m = v.m;
+            v = final_stat(Stat{m, s, 0.0f}, c2);
+            log_tail = none ? neg_inf() : fmaf(out_m - m, a.scale, logf(out_s) - logf(v.s));
             if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
-            v = Stat{m, s, 0.0f};
+        } else {
+            v = final_stat(v, c2);
         }
         const bool empty = v.m == neg_inf() && v.s == 0.0f;
         ls = logf(v.s);
@@ -734,21 +792,37 @@ __global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a
     const float m = row_m, by = row_by;
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     uint4* to = reinterpret_cast<uint4*>(out - r.head);
-    const f2 minus = make_f2(-m, -m), c2s = make_f2(c2, c2);
-    for (int base = r.v0; base < r.v1; base += nt * VPT) {
-        uint4 q[VPT];
-        if (!KEEP) load_share<T, VPT>(r, base, nt, q);
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int vec = base + j * nt + (int)threadIdx.x;
-            if (vec >= r.v1) continue;
-            if (KEEP) q[j] = kept[vec - r.v0];
+    // exponents as in the sums: one multiply-add where the reference allows it
+    const bool far = !in_range(m, c2), thin = TAIL && s.thin && !s.empty;
+    const float ref = m * c2, norm = far ? by : by * ex2(-fmaf(m, c2, -ref)), f = factor(s, norm);
+    const f2 c2s = make_f2(c2, c2);
+    if (KEEP && a.wide && !far && !thin) {
+        const f2 minus = make_f2(-ref, -ref);
+        auto grad_of = [&](const uint4& q) {
             f2 d[E / 2];
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) d[i] = mul2(add2(Vec<T>::pair(q[j], i), minus), c2s);
-            const uint4 g = slope_vec<T, TAIL>(d, s, by);
-            if (a.wide && vec >= r.w0 && vec < r.w1) __stcs(to + vec, g);
-            else store_vec(r, out, vec, g, false);
+            for (int i = 0; i < E / 2; ++i) d[i] = fma2(Vec<T>::pair(q, i), c2s, minus);
+            return slope_vec<T>(d, f);
+        };
+#pragma unroll 4
+        for (int vec = r.w0 + (int)threadIdx.x; vec < r.w1; vec += nt) __stcs(to + vec, grad_of(kept[vec - r.v0]));
+        if ((int)threadIdx.x == nt - 1 && r.w0 > r.v0) store_edge(r, out, r.v0, grad_of(kept[0]));
+        if ((int)threadIdx.x == nt - 2 && r.w1 < r.v1) store_edge(r, out, r.w1, grad_of(kept[r.w1 - r.v0]));
+    } else {
+        const f2 minus = far ? make_f2(-m, -m) : make_f2(-ref, -ref);
+#pragma unroll 1
+        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt) {
+            const bool whole = vec >= r.w0 && vec < r.w1;
+            const uint4 q = KEEP ? kept[vec - r.v0] : whole ? __ldcs(r.vectors() + vec) : r.edge(vec);
+            f2 d[E / 2];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                const f2 z = Vec<T>::pair(q, i);
+                d[i] = far ? mul2(add2(z, minus), c2s) : fma2(z, c2s, minus);
+            }
+            const uint4 g = thin ? thin_vec<T>(d, s, norm) : slope_vec<T>(d, f);
+            if (a.wide && whole) __stcs(to + vec, g);
+            else store_edge(r, out, vec, g);
         }
     }
     __syncthreads();                               // the ids' places are written last
@@ -759,15 +833,14 @@ __global__ void __launch_bounds__(MAX_THREADS, 6) distill_kernel(const RowArgs a
     }
 }
 
-template <class T, int VG, bool TAIL>
-__global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
+template <class T, bool TAIL>
+__global__ void __launch_bounds__(MAX_THREADS) distill_grad_kernel(const RowArgs a) {
     constexpr int E = Vec<T>::E;
     __shared__ TeacherShared t;
     const int nt = blockDim.x;
     const long long n = a.row0 + blockIdx.x / a.blocks;
     const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
-    uint4 q[VG];
-    load_share<T, VG>(r, r.v0, nt, q);
+    const float lse = a.in_lse[n], log_tail = TAIL ? a.in_log_tail[n] : 0.0f;
     if (threadIdx.x < 32) {
         Entries e;
         e.load(a, n);
@@ -776,20 +849,28 @@ __global__ void __launch_bounds__(256) distill_grad_kernel(const RowArgs a) {
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += nt)
         if (t.id[k] != NO_ID && r.holds((int)t.id[k])) t.z[k] = to_float(r.z[t.id[k]]);
-    const float lse = a.in_lse[n], log_tail = TAIL ? a.in_log_tail[n] : 0.0f;
-    __syncthreads();
-    const Slope s = slope_of<TAIL>((a.g1 ? a.g1[n] : a.g_all) * a.scale, t, lse, log_tail);
+    __syncthreads();                               // the gradient may take the logits' place
+    const Slope s = slope_of<TAIL>(t.w, t, lse, log_tail);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
-    const float shift = s.empty ? LOW_EXP : -lse;
+    const float shift = s.empty ? LOW_EXP : -lse, f = factor(s, 1.0f);
     const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);
+    auto exponents = [&](const uint4& q, f2* d) {
 #pragma unroll
-    for (int j = 0; j < VG; ++j) {
-        const int vec = r.v0 + j * nt + (int)threadIdx.x;
-        if (vec >= r.v1) continue;
-        f2 d[E / 2];
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) d[i] = mul2(fma2(Vec<T>::pair(q[j], i), scale, minus), l2e);
-        store_vec(r, out, vec, slope_vec<T, TAIL>(d, s, 1.0f), a.wide);
+        for (int i = 0; i < E / 2; ++i) d[i] = mul2(fma2(Vec<T>::pair(q, i), scale, minus), l2e);
+    };
+    if (TAIL && s.thin && !s.empty) {
+#pragma unroll 1
+        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt) {
+            f2 d[E / 2];
+            exponents(vec >= r.w0 && vec < r.w1 ? __ldcs(r.vectors() + vec) : r.edge(vec), d);
+            store_edge(r, out, vec, thin_vec<T>(d, s, 1.0f));
+        }
+    } else {
+        map_row<T>(r, out, a.wide, [&](const uint4& q, int) {
+            f2 d[E / 2];
+            exponents(q, d);
+            return slope_vec<T>(d, f);
+        });
     }
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += nt)
@@ -805,31 +886,47 @@ constexpr int SMS = 148;
 
 struct Shape { int nt, blocks; size_t smem; bool keep; };
 
-// threads for a row of `vectors`: a batch of four vectors each
-int threads_for(long long vectors) { return vectors <= 128 * VPT ? 128 : MAX_THREADS; }
+// Threads of a row's block: few enough that a thread has some eight vectors at least (its share of the row's last steps is
+// dear: 65536 rows of 1000 take 102 us with 128 threads, 55 with 32), and as many as bound the K-th alternative well
+int threads_for(long long vectors, int K) {
+    const int least = K == 0 ? 32 : K <= 20 ? 64 : K <= 64 ? 128 : MAX_THREADS;
+    int nt = MAX_THREADS;
+    while (nt > least && vectors <= nt * 8) nt /= 2;
+    return nt;
+}
 
 // Statistics and alternatives: a block per row; few rows are split over a cluster until the blocks fill the SMs six
 // times over, each with a batch at least
-Shape stream_shape(int64_t N, long long vectors) {
-    Shape s{threads_for(vectors), 1, 0, false};
+Shape stream_shape(int64_t N, long long vectors, int K) {
+    Shape s{threads_for(vectors, K), 1, 0, false};
     while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * VPT < vectors) s.blocks *= 2;
     return s;
 }
-// The loss with its gradient: shares of 32 KB, so that seven blocks' fit an SM, or as long as 8 blocks make necessary.
-// Few rows are split further, down to a batch per block
-constexpr int SHARE = 32 * 1024 / 16, SHARE_MOST = 200 * 1024 / 16;
+// The loss with its gradient: the row is cut into as many shares as leave the most of an SM's shared memory in use by
+// resident blocks (2 shares of 50 KB for a row of 100 KB, four blocks to an SM: 184 us where 3 shares take 199; 8 of 32 KB
+// for one of 256 KB: 227 us, with 4 shares 244).  Few rows are split further, down to a batch per block
+constexpr int SHARE_MOST = 200 * 1024 / 16;
 Shape keep_shape(int64_t N, long long vectors) {
-    Shape s{threads_for(vectors), 1, 0, true};
-    while (s.blocks < MAX_BLOCKS && ((vectors + s.blocks - 1) / s.blocks > SHARE ||
-                                     (N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * VPT < vectors))) ++s.blocks;
+    constexpr long long SM_BYTES = 227 * 1024, OWN = 5 * 1024;   // of an SM; what a block takes beside its share
+    Shape s{128, MAX_BLOCKS, 0, true};
+    long long best = 0;
+    for (int b = MAX_BLOCKS; b >= 1; --b) {
+        const long long share = (vectors + b - 1) / b * 16, resident = SM_BYTES / (share + OWN);
+        const long long used = (resident < 16 ? resident : 16) * share;
+        if (resident < 3 || used <= best || (b > 1 && share < 16 * 1024)) continue;
+        best = used;
+        s.blocks = b;
+    }
+    while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * 4 < vectors) ++s.blocks;
     const long long share = (vectors + s.blocks - 1) / s.blocks;
+    s.nt = share <= 256 ? 32 : share <= 512 ? 64 : share <= 2048 ? 128 : MAX_THREADS;
     s.keep = share <= SHARE_MOST;
     s.smem = s.keep ? 16 * (size_t)share : 0;
     return s;
 }
 
 template <class K>
-cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, cudaStream_t st) {
+cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaStream_t st) {
     a.blocks = s.blocks;
     if (s.smem > 32 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
@@ -848,60 +945,51 @@ cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, cudaStream_t st) {
         attr.val.clusterDim.x = (unsigned)s.blocks;
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
-        cfg.numAttrs = s.blocks > 1 ? 1 : 0;
+        cfg.numAttrs = cluster && s.blocks > 1 ? 1 : 0;
         const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
-// the backward calls: independent blocks, each with up to VG vectors per thread of its row
-struct GradShape { int nt, vg, blocks; };
-GradShape grad_shape(int64_t V, int size) {
-    const long long n = most_vectors(V, size);
-    if (n <= 128 * 2) return GradShape{128, 2, 1};
-    if (n <= 128 * 4) return GradShape{128, 4, 1};
-    return GradShape{256, 4, (int)((n + 256 * 4 - 1) / (256 * 4))};
-}
-template <class K>
-cudaError_t launch_grad(K kernel, const GradShape& s, RowArgs a, cudaStream_t st) {
-    a.blocks = s.blocks;
-    const long long most = 0x7fffffffll / s.blocks;              // rows per launch
-    for (a.row0 = 0; a.row0 < a.N; a.row0 += most) {
-        const long long rows = a.N - a.row0 < most ? a.N - a.row0 : most;
-        kernel<<<(unsigned)(rows * s.blocks), s.nt, 0, st>>>(a);
-        const cudaError_t e = cudaPeekAtLastError();
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+// The backward calls: independent blocks, each with some sixteen vectors per thread of its row, or four where there are few
+// rows
+Shape grad_shape(int64_t N, long long vectors) {
+    Shape s{vectors <= 2048 ? 64 : MAX_THREADS, 1, 0, false};
+    const long long most = (vectors + s.nt * 16 - 1) / (s.nt * 16), fine = (vectors + s.nt * 4 - 1) / (s.nt * 4);
+    long long blocks = most;
+    while (blocks < fine && N * blocks < 8 * SMS) blocks *= 2;
+    s.blocks = (int)(blocks < fine ? blocks : fine);
+    return s;
 }
 
 template <class T>
 cudaError_t launch_token_logp(RowArgs a, cudaStream_t st) {
-    const Shape s = stream_shape(a.N, most_vectors(a.V, sizeof(T)));
-    // maxima per warp that bound the K-th alternative: about four for each alternative asked for
-    a.groups = 1;
-    while (a.groups < 32 && s.nt / 32 * a.groups < 4 * a.K) a.groups *= 2;
-    return launch_rows(a.K > 0 ? token_logp_kernel<T, true> : token_logp_kernel<T, false>, s, a, st);
+    Shape s = stream_shape(a.N, most_vectors(a.V, sizeof(T)), a.K);
+    if (a.K > 0) {
+        const long long share = (most_vectors(a.V, sizeof(T)) + s.blocks - 1) / s.blocks, batches = (share + s.nt * VPT - 1) / (s.nt * VPT);
+        a.per = (int)((batches + SLOTS - 1) / SLOTS);
+        // (a slot more: the loop may close the last one)
+        s.smem = (s.blocks > 1 ? sizeof(unsigned long long) * CANDS : 0) + sizeof(float) * s.nt * ((batches + a.per - 1) / a.per + 1);
+    }
+    return launch_rows(a.K > 0 ? token_logp_kernel<T, true> : token_logp_kernel<T, false>, s, a, true, st);
 }
 template <class T>
 cudaError_t launch_token_logp_grad(const RowArgs& a, cudaStream_t st) {
-    const GradShape s = grad_shape(a.V, sizeof(T));
-    const bool ent = a.g2 != nullptr;
-    if (s.vg == 2) return launch_grad(ent ? token_logp_grad_kernel<T, 2, true> : token_logp_grad_kernel<T, 2, false>, s, a, st);
-    return launch_grad(ent ? token_logp_grad_kernel<T, 4, true> : token_logp_grad_kernel<T, 4, false>, s, a, st);
+    const Shape s = grad_shape(a.N, most_vectors(a.V, sizeof(T)));
+    return launch_rows(a.g2 ? token_logp_grad_kernel<T, true> : token_logp_grad_kernel<T, false>, s, a, false, st);
 }
 template <class T>
 cudaError_t launch_distill(const RowArgs& a, bool tail, cudaStream_t st) {
-    const Shape s = keep_shape(a.N, most_vectors(a.V, sizeof(T)));
-    if (s.keep) return launch_rows(tail ? distill_kernel<T, true, true> : distill_kernel<T, true, false>, s, a, st);
-    return launch_rows(tail ? distill_kernel<T, false, true> : distill_kernel<T, false, false>, s, a, st);
+    const long long vectors = most_vectors(a.V, sizeof(T));
+    const Shape s = keep_shape(a.N, vectors);
+    if (s.keep) return launch_rows(tail ? distill_kernel<T, true, true> : distill_kernel<T, true, false>, s, a, true, st);
+    return launch_rows(tail ? distill_kernel<T, false, true> : distill_kernel<T, false, false>, s, a, true, st);
 }
 template <class T>
 cudaError_t launch_distill_grad(const RowArgs& a, bool tail, cudaStream_t st) {
-    const GradShape s = grad_shape(a.V, sizeof(T));
-    if (s.vg == 2) return launch_grad(tail ? distill_grad_kernel<T, 2, true> : distill_grad_kernel<T, 2, false>, s, a, st);
-    return launch_grad(tail ? distill_grad_kernel<T, 4, true> : distill_grad_kernel<T, 4, false>, s, a, st);
+    const Shape s = grad_shape(a.N, most_vectors(a.V, sizeof(T)));
+    return launch_rows(tail ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>, s, a, false, st);
 }
 
 int status_of(cudaError_t e) {

@@ -201,15 +201,51 @@ __device__ __forceinline__ void load_share(const Share<T>& r, int base, int nt, 
     }
 }
 
-// one vector of results; `wide`: the row's vectors have the same places in memory as the logits'
-template <class T>
-__device__ __forceinline__ void store_vec(const Share<T>& r, T* out, int vec, const uint4& q, bool wide) {
-    if (wide && r.whole(vec)) {
-        __stcs(reinterpret_cast<uint4*>(out - r.head) + vec, q);
-        return;
+// calls f(q, vec, more) for the share's vectors, nt apart from vec on: batches of VPT per thread, then the rest in one
+// batch (`more`: vectors at or past w1 are no vectors, -inf), then those that are not whole
+struct Full { static constexpr bool value = false; };
+struct Rest { static constexpr bool value = true; };
+template <class T, int VPT, class F>
+__device__ __forceinline__ void each_batch(const Share<T>& r, F f) {
+    const int nt = blockDim.x;
+    const uint4* p = r.vectors();
+    int base = r.w0;
+    for (; base + nt * VPT <= r.w1; base += nt * VPT) {
+        const int vec = base + (int)threadIdx.x;
+        uint4 q[VPT];
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) q[j] = __ldcs(p + vec + j * nt);
+        f(q, vec, Full());
     }
+    if (base + nt < r.w1) {
+        const int vec = base + (int)threadIdx.x;
+        uint4 q[VPT];
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            q[j] = all_lowest<T>();
+            if (vec + j * nt < r.w1) q[j] = __ldcs(p + vec + j * nt);
+        }
+        f(q, vec, Rest());
+    } else if (base + (int)threadIdx.x < r.w1) {
+        const int vec = base + (int)threadIdx.x;
+        uint4 q[1] = {__ldcs(p + vec)};
+        f(q, vec, Full());
+    }
+    if (threadIdx.x == 0 && r.w0 > r.v0) {
+        uint4 q[1] = {r.edge(r.v0)};
+        f(q, r.v0, Full());
+    }
+    if ((int)threadIdx.x == nt - 1 && r.w1 < r.v1) {
+        uint4 q[1] = {r.edge(r.w1)};
+        f(q, r.w1, Full());
+    }
+}
+
+// one vector of results, element by element: one that is not whole, or rows that do not lie like the logits' rows
+template <class T>
+__device__ __noinline__ void store_edge(const Share<T>& r, T* out, int vec, uint4 q) {
     const int e0 = r.first(vec);
-    const uint32_t* w = &q.x;
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int i = 0; i < Vec<T>::E; ++i) {
         if (e0 + i < 0 || e0 + i >= r.V) continue;
@@ -234,39 +270,50 @@ __device__ __forceinline__ float warp_sum(float v) {
 // the shift that a part's exponents take: its maximum, or 0 where everything is masked
 __device__ __forceinline__ float shift_of(float m) { return m == neg_inf() ? 0.0f : m; }
 
-// The exponentials of a batch of vectors relative to m: s += sum e, u += sum e d.  One multiply-add per pair gives
-// d + delta = z c2 - fl(m c2); the rounding error delta of m c2 is the same in all places and is taken out of the
-// sums.  False where this form does not serve: u turns to NaN where a place is masked (0 times -inf), and m c2 may be
-// out of range
-template <class T, int VPT, bool ENT>
-__device__ __forceinline__ bool add_exps(const uint4 (&q)[VPT], float m, float c2, float& s_all, float& u_all) {
-    const float ref = m * c2;
+// A part's sums are held relative to 2^ref with ref = fl(m c2), so that an exponent is one multiply-add, d = z c2 - ref;
+// that rounding of m c2 is the same in every term, and final_stat takes it out at the end.  Beyond the range in which
+// ref has fractions enough (a row at a mask of the lowest value), exponents are (z - m) c2 instead.
+constexpr float REF_RANGE = 65536.0f;
+__device__ __forceinline__ bool in_range(float m, float c2) { return fabsf(m * c2) < REF_RANGE; }
+// distance of two references
+__device__ __forceinline__ float ref_diff(float a, float b, float c2) {
+    return in_range(a, c2) && in_range(b, c2) ? a * c2 - b * c2 : (a - b) * c2;
+}
+
+// The exponentials of a batch: s += sum e, u += sum e d.  FLOOR: exponents are kept finite, for a batch with places that
+// hold nothing.  False where this form does not serve: u turns to NaN where a
+// place is masked (0 times -inf), and m c2 may be out of range
+template <class T, int VPT, bool ENT, bool FLOOR>
+__device__ __forceinline__ bool add_exps(const uint4 (&q)[VPT], float ref, float c2, float& s_all, float& u_all) {
     const f2 minus = make_f2(-ref, -ref), c = make_f2(c2, c2);
     f2 s = make_f2(0.0f, 0.0f), u = s;
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int i = 0; i < Vec<T>::E / 2; ++i) {
-            const f2 d = fma2(Vec<T>::pair(q[j], i), c, minus), e = ex2_2(d);
+            f2 d = fma2(Vec<T>::pair(q[j], i), c, minus);
+            if (FLOOR) d = floor2(d);
+            const f2 e = ex2_2(d);
             s = add2(s, e);
             if (ENT) u = fma2(e, d, u);
         }
     const float2 ps = parts(s), pu = parts(u);
-    const float delta = fmaf(m, c2, -ref), w = ex2(-delta);
-    const float sum = (ps.x + ps.y) * w, sum_d = ENT ? fmaf(-delta, sum, (pu.x + pu.y) * w) : 0.0f;
-    if (!(fabsf(ref) < 65536.0f) || (ENT && !(sum_d == sum_d))) return false;
-    s_all += sum;
+    const float sum_d = pu.x + pu.y;
+    if (!(fabsf(ref) < REF_RANGE) || (ENT && !(sum_d == sum_d))) return false;
+    s_all += ps.x + ps.y;
     if (ENT) u_all += sum_d;
     return true;
 }
-// the same for one vector in a form that serves always: z - m first, masked places and overflow made finite
+// the same for one vector in a form that serves always: masked places and overflow made finite
 template <class T>
 __device__ __noinline__ float2 add_exps_exact(uint4 q, float m, float c2) {
-    const f2 minus = make_f2(-m, -m), c = make_f2(c2, c2);
+    const bool far = !in_range(m, c2);
+    const float ref = m * c2;
+    const f2 minus = far ? make_f2(-m, -m) : make_f2(-ref, -ref), c = make_f2(c2, c2);
     f2 s = make_f2(0.0f, 0.0f), u = s;
 #pragma unroll
     for (int i = 0; i < Vec<T>::E / 2; ++i) {
-        const f2 d = floor2(mul2(add2(Vec<T>::pair(q, i), minus), c)), e = ex2_2(d);
+        const f2 z = Vec<T>::pair(q, i), d = floor2(far ? mul2(add2(z, minus), c) : fma2(z, c, minus)), e = ex2_2(d);
         s = add2(s, e);
         u = fma2(e, d, u);
     }
@@ -277,8 +324,14 @@ __device__ __noinline__ float2 add_exps_exact(uint4 q, float m, float c2) {
 // the larger maximum takes over
 __device__ __forceinline__ Stat rescale(Stat a, float m, float c2) {
     if (a.m == neg_inf()) return Stat{m, a.s, a.u};              // a masked part: s = u = 0 (or NaN)
-    const float d = fmaxf((a.m - m) * c2, LOW_EXP), w = ex2(d);
+    const float d = fmaxf(ref_diff(a.m, m, c2), LOW_EXP), w = ex2(d);
     return Stat{m, a.s * w, w * fmaf(a.s, d, a.u)};
+}
+// sums relative to the maximum itself
+__device__ __forceinline__ Stat final_stat(Stat a, float c2) {
+    if (a.m == neg_inf() || !in_range(a.m, c2)) return a;
+    const float delta = fmaf(a.m, c2, -(a.m * c2)), w = ex2(-delta), s = a.s * w;
+    return Stat{a.m, s, fmaf(-delta, s, a.u * w)};
 }
 
 template <class T, int VPT>
@@ -293,14 +346,14 @@ __device__ __forceinline__ float thread_max_of(const uint4 (&q)[VPT]) {
 // moves when the exponents would pass 2^REACH, so that most batches need no new scale; the reach is small because the
 // entropy's u loses REACH units in the last place when it moves on to the row's maximum at the end
 constexpr float REACH = 3.0f;
-template <class T, int VPT, bool ENT>
+template <class T, int VPT, bool ENT, bool FLOOR>
 __device__ __forceinline__ void take(Stat& st, const uint4 (&q)[VPT], float m, float c2) {
     if (!((m - st.m) * c2 <= REACH) && m > st.m) st = rescale(st, m, c2);
-    const float ref = shift_of(st.m);
-    if (add_exps<T, VPT, ENT>(q, ref, c2, st.s, st.u)) return;
+    const float at = shift_of(st.m);
+    if (add_exps<T, VPT, ENT, FLOOR && ENT>(q, at * c2, c2, st.s, st.u)) return;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-        const float2 x = add_exps_exact<T>(q[j], ref, c2);
+        const float2 x = add_exps_exact<T>(q[j], at, c2);
         st.s += x.x;
         if (ENT) st.u += x.y;
     }
