@@ -902,24 +902,26 @@ Shape stream_shape(int64_t N, long long vectors, int K) {
     while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * VPT < vectors) s.blocks *= 2;
     return s;
 }
-// The loss with its gradient: the row is cut into as many shares as leave the most of an SM's shared memory in use by
-// resident blocks (2 shares of 50 KB for a row of 100 KB, four blocks to an SM: 184 us where 3 shares take 199; 8 of 32 KB
-// for one of 256 KB: 227 us, with 4 shares 244).  Few rows are split further, down to a batch per block
+// The loss with its gradient: the row is cut into as many shares as keep the most of an SM's shared memory in use, the
+// smaller shares where two counts do as well (2 shares of 50 KB for a row of 100 KB, four blocks to an SM: 184 us where
+// 4 shares take 199; 8 of 32 KB for one of 256 KB: 227 us, with 4 shares 244; 3, 5 or 7 blocks fit the chip's groups of SMs
+// worse, 239 to 249).  Few rows are split further, down to half a batch per thread
 constexpr int SHARE_MOST = 200 * 1024 / 16;
+int keep_threads(long long share) { return share <= 256 ? 32 : share <= 512 ? 64 : share <= 2048 ? 128 : MAX_THREADS; }
 Shape keep_shape(int64_t N, long long vectors) {
     constexpr long long SM_BYTES = 227 * 1024, OWN = 5 * 1024;   // of an SM; what a block takes beside its share
     Shape s{128, MAX_BLOCKS, 0, true};
     long long best = 0;
-    for (int b = MAX_BLOCKS; b >= 1; --b) {
-        const long long share = (vectors + b - 1) / b * 16, resident = SM_BYTES / (share + OWN);
-        const long long used = (resident < 16 ? resident : 16) * share;
-        if (resident < 3 || used <= best || (b > 1 && share < 16 * 1024)) continue;
+    for (int b = MAX_BLOCKS; b >= 1; b /= 2) {
+        const long long share = (vectors + b - 1) / b, fit = SM_BYTES / (16 * share + OWN), threads = 1024 / keep_threads(share);
+        const long long used = (fit < threads ? fit : threads) * share;
+        if (fit < 3 || used <= best || (b > 1 && share < 1024)) continue;
         best = used;
         s.blocks = b;
     }
-    while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * s.nt * 4 < vectors) ++s.blocks;
+    while (s.blocks < MAX_BLOCKS && N * s.blocks < 6 * SMS && (long long)s.blocks * 512 < vectors) s.blocks *= 2;
     const long long share = (vectors + s.blocks - 1) / s.blocks;
-    s.nt = share <= 256 ? 32 : share <= 512 ? 64 : share <= 2048 ? 128 : MAX_THREADS;
+    s.nt = keep_threads(share);
     s.keep = share <= SHARE_MOST;
     s.smem = s.keep ? 16 * (size_t)share : 0;
     return s;

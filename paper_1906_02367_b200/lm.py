@@ -8,7 +8,6 @@ device) and nothing waits for the GPU.  Tensors made on other streams are the ca
 torch call.  `status`, where taken, is an int32 CUDA tensor of one element, zero before the call, that receives
 QS_INVALID_ARG if an id lies past the last row or column.
 """
-import contextlib
 from collections import namedtuple
 
 import torch
@@ -20,7 +19,8 @@ Distill = namedtuple("Distill", "loss lse log_tail grad")
 
 _TYPE = {torch.float32: QS_F32, torch.bfloat16: QS_BF16, torch.float16: QS_F16}
 _ID = {torch.int32: QS_I32, torch.int64: QS_I64}
-_HERE = contextlib.nullcontext()
+# a serving loop's calls are as short as their marshalling: the stream's handle without a Stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _type(t, what, table=_TYPE):
@@ -31,21 +31,26 @@ def _type(t, what, table=_TYPE):
 
 
 def _on(first, *rest):
-    """All tensors on the current CUDA device."""
-    dev = first.device
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors must be on the current CUDA device, not on {dev}")
+    """The CUDA device of all the tensors, which must be the current one."""
+    device = first.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"tensors must be on the current CUDA device, not on {first.device}")
     for t in rest:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+    return device
 
 
-def _stream(stream):
-    """(stream handle, context in which results are allocated so that they belong to that stream)."""
-    cur = torch.cuda.current_stream()
-    if stream is None or stream == cur:
-        return cur.cuda_stream, _HERE
-    return stream.cuda_stream, torch.cuda.stream(stream)
+def _allocate(stream, shape, dtype, device):
+    """A tensor that belongs to `stream` (None: the current one)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _handle(stream, device):
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 def _ptr(t):
@@ -59,17 +64,13 @@ def _done(rc, what):
 
 def _rows(t, what):
     """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one."""
-    if t.dim() < 2 or (t.stride(-1) != 1 and t.shape[-1] > 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 2 or (stride[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{what} needs rows with unit stride")
-    step = t.stride(-2)
-    for i in range(t.dim() - 3, -1, -1):
-        if t.shape[i] > 1 and t.stride(i) != _step_of(t, i):
+    for i in range(len(shape) - 3, -1, -1):
+        if shape[i] > 1 and stride[i] != stride[i + 1] * shape[i + 1]:
             raise ValueError(f"{what}: leading dimensions must flatten into rows of one stride")
-    return step if t.shape[-2] > 1 or t.dim() > 2 else max(step, t.shape[-1])
-
-
-def _step_of(t, i):
-    return t.stride(i + 1) * t.shape[i + 1]
+    return stride[-2] if shape[-2] > 1 or len(shape) > 2 else max(stride[-2], shape[-1])
 
 
 def _vector(t, n, what, dtype=torch.float32):
@@ -77,24 +78,16 @@ def _vector(t, n, what, dtype=torch.float32):
         raise ValueError(f"{what} needs {n} contiguous elements of {dtype}")
 
 
-def _result(out, shape, dtype, device, what):
-    """`out` checked, or a new tensor."""
-    if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if out.shape != torch.Size(shape) or out.dtype != dtype:
-        raise ValueError(f"{what} must be {tuple(shape)} of {dtype}")
-    return out
-
-
 def _table(t, R, what):
     """(vocabulary, width, worker stride, row stride) of a (V, D) or (R, V, D) table."""
-    if t.dim() not in (2, 3) or (t.dim() == 3 and t.shape[0] != R):
+    shape, stride = t.shape, t.stride()
+    if len(shape) not in (2, 3) or (len(shape) == 3 and shape[0] != R):
         raise ValueError(f"{what} must be (V, D), or (R, V, D) for R workers' tokens")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    V, D = shape[-2], shape[-1]
+    if stride[-1] != 1 and D > 1:
         raise ValueError(f"{what} needs rows with unit stride")
-    V, D = t.shape[-2], t.shape[-1]
-    row = t.stride(-2) if V > 1 else max(t.stride(-2), D)
-    return V, D, (t.stride(0) if t.dim() == 3 and R > 1 else 0), row
+    row = stride[-2] if V > 1 else max(stride[-2], D)
+    return V, D, (stride[0] if len(shape) == 3 and R > 1 else 0), row
 
 
 def _tokens(tokens, workers):
@@ -112,22 +105,26 @@ def _tokens(tokens, workers):
 def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=None):
     """scale * table[tokens] (qs_embed): tokens (.., N) with a (V, D) table, or (R, .., N) with (R, V, D), one table
     per worker.  Negative tokens give zeros.  Returns tokens.shape + (D,) in `dtype` (default the table's)."""
-    _on(tokens, table, out, status)
+    device = _on(tokens, table, out, status)
     R, N = _tokens(tokens, table.dim() == 3)
     V, D, ws, rs = _table(table, R, "table")
-    st, where = _stream(stream)
-    with where:
-        out = _result(out, (*tokens.shape, D), dtype or (out.dtype if out is not None else table.dtype), table.device, "out")
-    os_ = _rows(out, "out") if out.dim() > 1 else D
+    shape = (*tokens.shape, D)
+    if out is None:
+        out = _allocate(stream, shape, dtype or table.dtype, device)
+        step = D
+    else:
+        if out.shape != shape or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"out must be {shape}" + (f" of {dtype}" if dtype else ""))
+        step = _rows(out, "out") if len(shape) > 1 else D
     _done(lib().qs_embed(R, N, V, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), table.data_ptr(), _type(table, "table"), ws, rs,
-                         scale, out.data_ptr(), _type(out, "out"), os_, _ptr(status), st), "qs_embed")
+                         scale, out.data_ptr(), _type(out, "out"), step, _ptr(status), _handle(stream, device)), "qs_embed")
     return out
 
 
 def embed_grad_work(workers, tokens, vocab, width, device=None):
     """Scratch of embed_grad for `tokens` tokens per worker."""
     n = lib().qs_embed_grad_bytes(workers, tokens, vocab, width)
-    _done(min(n, 0), "qs_embed_grad_bytes")
+    _done(n, "qs_embed_grad_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device or "cuda")
 
 
@@ -136,7 +133,7 @@ def embed_grad(tokens, grad_out, vocab, scale=1.0, workers=None, accumulate=Fals
     workers (default: tokens have more than one dimension, or out has three): a table per entry of the tokens' first
     dimension, result (R, vocab, D); otherwise one table, (vocab, D).  `out` may be a strided view, a stretch of
     the rows of a gradient batch; with accumulate it is added to and rows no token names stay untouched."""
-    _on(tokens, grad_out, out, work, status)
+    device = _on(tokens, grad_out, out, work, status)
     if workers is None:
         workers = out.dim() == 3 if out is not None else tokens.dim() > 1
     R, N = _tokens(tokens, workers)
@@ -145,15 +142,22 @@ def embed_grad(tokens, grad_out, vocab, scale=1.0, workers=None, accumulate=Fals
         raise ValueError(f"grad_out {tuple(grad_out.shape)} does not belong to tokens {tuple(tokens.shape)}")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    st, where = _stream(stream)
-    with where:
-        out = _result(out, (R, vocab, D) if workers else (vocab, D), torch.float32, grad_out.device, "out")
-        if work is None:
-            work = embed_grad_work(R, N, vocab, D, grad_out.device)
+    shape = (R, vocab, D) if workers else (vocab, D)
+    if out is None:
+        out = _allocate(stream, shape, torch.float32, device)
+    elif out.shape != shape or out.dtype != torch.float32:
+        raise ValueError(f"out must be {shape} of torch.float32")
+    L = lib()
+    if work is None:
+        need = L.qs_embed_grad_bytes(R, N, vocab, D)
+        _done(need, "qs_embed_grad_bytes")
+        work = _allocate(stream, need, torch.uint8, device)
+    else:
+        need = work.numel() * work.element_size()
     _, _, ws, rs = _table(out, R, "out")
-    _done(lib().qs_embed_grad(R, N, vocab, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), grad_out.data_ptr(),
-                              _type(grad_out, "grad_out"), _rows(grad_out, "grad_out"), scale, int(accumulate), out.data_ptr(), ws, rs,
-                              work.data_ptr(), work.numel() * work.element_size(), _ptr(status), st), "qs_embed_grad")
+    _done(L.qs_embed_grad(R, N, vocab, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), grad_out.data_ptr(),
+                          _type(grad_out, "grad_out"), _rows(grad_out, "grad_out"), scale, int(accumulate), out.data_ptr(), ws, rs,
+                          work.data_ptr(), need, _ptr(status), _handle(stream, device)), "qs_embed_grad")
     return out
 
 
@@ -167,7 +171,7 @@ def token_logp(logits, tokens=None, scale=1.0, top=0, status=None, stream=None):
     """Log probabilities of `tokens` (N) under softmax(scale * logits) (qs_token_logp), with the log of the sum, the
     entropy, and the `top` largest logits' columns and log probabilities (equal logits: lower index first).
     tokens None: no logp, and top_ids are int64.  Returns TokenLogp; fields not asked for are None."""
-    _on(logits, tokens, status)
+    device = _on(logits, tokens, status)
     N, V, step = _logits(logits)
     if not 0 <= top <= min(QS_MAX_TOP, V):
         raise ValueError(f"top must be between 0 and {min(QS_MAX_TOP, V)}")
@@ -176,16 +180,15 @@ def token_logp(logits, tokens=None, scale=1.0, top=0, status=None, stream=None):
         id_type = tokens.dtype
         _type(tokens, "tokens", _ID)
         _vector(tokens, N, "tokens", id_type)
-    st, where = _stream(stream)
-    dev = logits.device
-    with where:
-        stats = torch.empty((3, N), dtype=torch.float32, device=dev)
-        ids = torch.empty((N, top), dtype=id_type, device=dev) if top else None
-        top_logp = torch.empty((N, top), dtype=torch.float32, device=dev) if top else None
+    stats = _allocate(stream, (3, N), torch.float32, device)
+    ids = top_logp = None
+    if top:
+        ids = _allocate(stream, (N, top), id_type, device)
+        top_logp = _allocate(stream, (N, top), torch.float32, device)
     base = stats.data_ptr()
     _done(lib().qs_token_logp(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens), _ID[id_type], scale, top,
-                              base if tokens is not None else None, base + 4 * N, base + 8 * N, _ptr(ids), _ptr(top_logp), _ptr(status), st),
-          "qs_token_logp")
+                              base if tokens is not None else None, base + 4 * N, base + 8 * N, _ptr(ids), _ptr(top_logp), _ptr(status),
+                              _handle(stream, device)), "qs_token_logp")
     logp, lse, entropy = stats.unbind(0)
     return TokenLogp(logp if tokens is not None else None, lse, entropy, ids, top_logp)
 
@@ -208,7 +211,7 @@ def _weights(w, n, what):
 def token_logp_grad(logits, tokens, lse, grad_logp=1.0, scale=1.0, entropy=None, grad_entropy=None, out=None, status=None, stream=None):
     """Gradient of sum(grad_logp * logp + grad_entropy * entropy) with respect to the logits (qs_token_logp_grad).
     grad_logp: (N) or a number; grad_entropy: (N) or None.  out may be the logits themselves."""
-    _on(logits, tokens, lse, entropy, grad_entropy, out, status)
+    device = _on(logits, tokens, lse, entropy, grad_entropy, out, status)
     N, V, step = _logits(logits)
     if tokens is not None:
         _vector(tokens, N, "tokens", tokens.dtype)
@@ -219,12 +222,12 @@ def token_logp_grad(logits, tokens, lse, grad_logp=1.0, scale=1.0, entropy=None,
     if isinstance(grad_logp, torch.Tensor):
         _on(logits, grad_logp)
     g, g_all = _weights(grad_logp, N, "grad_logp")
-    st, where = _stream(stream)
-    with where:
-        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    if out is None:
+        out = _allocate(stream, (N, V), logits.dtype, device)
     _done(lib().qs_token_logp_grad(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens),
                                    _type(tokens, "tokens", _ID) if tokens is not None else QS_I64, scale, lse.data_ptr(), _ptr(entropy), g, g_all,
-                                   _ptr(grad_entropy), out.data_ptr(), _gradient(logits, out), _ptr(status), st), "qs_token_logp_grad")
+                                   _ptr(grad_entropy), out.data_ptr(), _gradient(logits, out), _ptr(status), _handle(stream, device)),
+          "qs_token_logp_grad")
     return out
 
 
@@ -242,7 +245,7 @@ def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weig
     there, renormalised, or with `tail` its log probabilities and the rest of its mass as one more class.  token_logp's
     top_ids and top_logp are such entries.  weight (N) or a number: the gradient of sum(weight * loss) with
     respect to the logits as well, from the same pass; out receives it and may be the logits themselves."""
-    _on(logits, ids, teacher, out, status)
+    device = _on(logits, ids, teacher, out, status)
     N, V, step = _logits(logits)
     K = _entries(ids, teacher, N)
     w, w_all = None, 0.0
@@ -252,16 +255,14 @@ def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weig
         w, w_all = _weights(weight, N, "weight")
     elif out is not None:
         raise ValueError("a gradient needs weight")
-    st, where = _stream(stream)
-    with where:
-        stats = torch.empty((3 if tail else 2, N), dtype=torch.float32, device=logits.device)
-        if weight is not None and out is None:
-            out = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    stats = _allocate(stream, (3 if tail else 2, N), torch.float32, device)
+    if weight is not None and out is None:
+        out = _allocate(stream, (N, V), logits.dtype, device)
     base = stats.data_ptr()
     _done(lib().qs_distill(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
                            teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), base, base + 4 * N,
                            base + 8 * N if tail else None, w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _ptr(status),
-                           st), "qs_distill")
+                           _handle(stream, device)), "qs_distill")
     parts = stats.unbind(0)
     return Distill(parts[0], parts[1], parts[2] if tail else None, out)
 
@@ -269,7 +270,7 @@ def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weig
 def distill_grad(logits, ids, teacher, lse, weight, scale=1.0, teacher_scale=1.0, tail=False, log_tail=None, out=None, status=None,
                  stream=None):
     """Gradient of sum(weight * loss) on its own (qs_distill_grad), from what distill returned."""
-    _on(logits, ids, teacher, lse, log_tail, out, status)
+    device = _on(logits, ids, teacher, lse, log_tail, out, status)
     N, V, step = _logits(logits)
     K = _entries(ids, teacher, N)
     _vector(lse, N, "lse")
@@ -279,10 +280,10 @@ def distill_grad(logits, ids, teacher, lse, weight, scale=1.0, teacher_scale=1.0
     if isinstance(weight, torch.Tensor):
         _on(logits, weight)
     w, w_all = _weights(weight, N, "weight")
-    st, where = _stream(stream)
-    with where:
-        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device) if out is None else out
+    if out is None:
+        out = _allocate(stream, (N, V), logits.dtype, device)
     _done(lib().qs_distill_grad(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
                                 teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), lse.data_ptr(), _ptr(log_tail),
-                                w, w_all, out.data_ptr(), _gradient(logits, out), _ptr(status), st), "qs_distill_grad")
+                                w, w_all, out.data_ptr(), _gradient(logits, out), _ptr(status), _handle(stream, device)),
+          "qs_distill_grad")
     return out
