@@ -58,7 +58,8 @@ struct EmbedArgs {
     long long out_stride;
     int* status;
     long long rows;                        // R x N
-    uint32_t units;                        // 8-column units per row (wide), 256-column tiles per row (else)
+    uint32_t units;                        // 256-column tiles per row
+    int lanes;                             // log2 of the lanes that share a row (wide)
 };
 
 // where a place's row comes from; null: it names none
@@ -93,49 +94,43 @@ template <> __device__ __forceinline__ void store_eight<float>(float* p, const f
     __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(f[4], f[5], f[6], f[7]));
 }
 
-constexpr int UNITS = 4;                       // units per thread, their loads in flight together
+constexpr int UNITS = 4;                       // 8-column units per lane in flight together
 
-// rows 16-byte aligned on both sides
+// Rows 16-byte aligned on both sides.  1 << a.lanes lanes share a row, so that a warp takes a long row or several short
+// ones: one token and one address per lane, 24 to 64 bytes of table in flight per unit
 template <class TW, class TO>
 __global__ void __launch_bounds__(256) embed_wide_kernel(const EmbedArgs a) {
-    const unsigned long long total = (unsigned long long)a.rows * a.units, first = (unsigned long long)blockIdx.x * (256 * UNITS) + threadIdx.x;
-    long long row[UNITS], col[UNITS], t[UNITS];
-    Eight<TW> e[UNITS];
+    const int lane = (int)(threadIdx.x & ((1u << a.lanes) - 1u));
+    const long long row = ((long long)blockIdx.x * 256 + threadIdx.x) >> a.lanes;
+    if (row >= a.rows) return;
+    const long long t = a.tok.at(row);
+    const TW* src = source_row<TW>(a, row, t);
+    TO* out = static_cast<TO*>(a.out) + row * a.out_stride;
+    const float none = t < 0 ? 0.0f : quiet_nan();
+    if (t >= a.V && lane == 0) flag_status(a.status, QS_INVALID_ARG);
+    const int step = 8 << a.lanes, D = (int)a.D;
+    for (int c0 = lane * 8; c0 < D; c0 += UNITS * step) {
+        Eight<TW> e[UNITS];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const unsigned long long id = first + 256 * i;
-        row[i] = -1;
-        if (id >= total) continue;
-        // (a 64-bit division costs several 32-bit ones)
-        row[i] = total >> 32 ? (long long)(id / a.units) : (long long)((uint32_t)id / a.units);
-        col[i] = (long long)(id - (unsigned long long)row[i] * a.units) * 8;
-        t[i] = a.tok.at(row[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        if (row[i] < 0) continue;
-        const TW* src = source_row<TW>(a, row[i], t[i]);
-        if (src && col[i] + 8 <= a.D) {
-            const uint4* p = reinterpret_cast<const uint4*>(src + col[i]);
+        for (int i = 0; i < UNITS; ++i) {
+            const int c = c0 + i * step;
+            if (!src || c + 8 > D) continue;
+            const uint4* p = reinterpret_cast<const uint4*>(src + c);
 #pragma unroll
             for (int w = 0; w < (int)sizeof(TW) / 2; ++w) e[i].q[w] = __ldg(p + w);
         }
-    }
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        if (row[i] < 0) continue;
-        TO* out = static_cast<TO*>(a.out) + row[i] * a.out_stride + col[i];
-        const TW* src = source_row<TW>(a, row[i], t[i]);
-        const float none = t[i] < 0 ? 0.0f : quiet_nan();
-        if (t[i] >= a.V && col[i] == 0) flag_status(a.status, QS_INVALID_ARG);
-        if (col[i] + 8 <= a.D) {
-            float f[8];
-            eight_to_float<TW>(e[i], f);
+        for (int i = 0; i < UNITS; ++i) {
+            const int c = c0 + i * step;
+            if (c + 8 <= D) {
+                float f[8];
+                eight_to_float<TW>(e[i], f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = src ? f[j] * a.scale : none;
-            store_eight<TO>(out, f);
-        } else {
-            for (int j = 0; j < (int)(a.D - col[i]); ++j) out[j] = from_float<TO>(src ? to_float(src[col[i] + j]) * a.scale : none);
+                for (int j = 0; j < 8; ++j) f[j] = src ? f[j] * a.scale : none;
+                store_eight<TO>(out + c, f);
+            } else {
+                for (int x = c; x < D; ++x) out[x] = from_float<TO>(src ? to_float(src[x]) * a.scale : none);
+            }
         }
     }
 }
@@ -166,14 +161,21 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
 
 template <class TW, class TO>
 void launch_embed(EmbedArgs a, bool wide, cudaStream_t st) {
-    const long long per = wide ? 256 * UNITS : 8;
-    a.units = (uint32_t)((a.D + (wide ? 7 : COLS - 1)) / (wide ? 8 : COLS));
-    const unsigned grid = (unsigned)((a.rows * a.units + per - 1) / per);
-    if (wide) embed_wide_kernel<TW, TO><<<grid, 256, 0, st>>>(a);
-    else embed_kernel<TW, TO><<<grid, 256, 0, st>>>(a);
+    if (wide) {
+        while (a.lanes < 5 && (8ll << a.lanes) < a.D) ++a.lanes;
+        embed_wide_kernel<TW, TO><<<(unsigned)(((a.rows << a.lanes) + 255) / 256), 256, 0, st>>>(a);
+    } else {
+        a.units = (uint32_t)((a.D + COLS - 1) / COLS);
+        embed_kernel<TW, TO><<<(unsigned)((a.rows * a.units + 7) / 8), 256, 0, st>>>(a);
+    }
 }
 
 // ------------------------------------------------------------------ gradient: sort by token
+// The kernels of one call follow one another without a gap: each is launched while the one before still runs, and waits
+// here for its end before it reads or writes anything
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 constexpr int SORT_THREADS = 1024;
 constexpr int SORT_MAX_BITS = 9;
 constexpr int SORT_MAX_ITEMS = 8;          // places per thread and tile
@@ -261,6 +263,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_count_kernel(const GradArgs
     __shared__ uint32_t hist[1 << SORT_MAX_BITS];
     __shared__ uint32_t seen[SEEN];                      // tokens the block has marked, by their low bits
     const int r = blockIdx.y, bins = 1 << a.bits;
+    next_may_start();
     for (int b = threadIdx.x; b < bins; b += SORT_THREADS) hist[b] = 0;
     for (int b = threadIdx.x; b < SEEN; b += SORT_THREADS) seen[b] = 0;
     __syncthreads();
@@ -333,8 +336,10 @@ __device__ uint32_t stable_place(SortShared& s, uint32_t d, int bins) {
 }
 
 // One pass of the sort: blocks [0, R x tiles) scatter a tile each, the others set rows to zero meanwhile
-__global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const GradArgs a, int pass) {
+__global__ void __launch_bounds__(SORT_THREADS, 2) sort_scatter_kernel(const GradArgs a, int pass) {
     __shared__ SortShared s;
+    wait_for_previous();
+    next_may_start();
     const int sorters = a.R * a.tiles;
     if ((int)blockIdx.x >= sorters) {
         zero_rows(a, pass, a.passes, blockIdx.x - sorters, gridDim.x - sorters);
@@ -382,10 +387,15 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_one_tile_kernel(const GradA
     const int r = blockIdx.x, bins = 1 << a.bits, i = threadIdx.x;
     const bool in = i < a.N;
     uint32_t k = 0, p = i;
-    if (in) {
-        k = key_of(a, r * a.N + i);
-        if (!a.accumulate) mark_row(a, r, k);
+    if (in) k = key_of(a, r * a.N + i);
+    if (r == 0 && i == 0) a.joins[0] = 0;
+    if (!a.accumulate) {
+        uint32_t* marks = reinterpret_cast<uint32_t*>(a.named + r * a.padded);
+        for (long long w = i; w < a.padded / 4; w += SORT_THREADS) marks[w] = 0;
+        __syncthreads();
+        if (in) mark_row(a, r, k);
     }
+    next_may_start();
     for (int pass = 0; pass < a.passes; ++pass) {
         const uint32_t d = in ? (k >> (pass * a.bits)) & (bins - 1) : (uint32_t)bins;
         for (int b = i; b < bins; b += SORT_THREADS) s.total[b] = 0;
@@ -499,6 +509,8 @@ constexpr int SUM_THREADS = 128;
 template <class T, bool WIDE>
 __global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
     constexpr int AHEAD = sizeof(T) == 4 || !WIDE ? 2 : 4;         // rows in a batch; two batches are in flight
+    wait_for_previous();
+    next_may_start();
     if (blockIdx.x >= sum_blocks) {
         zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
         return;
@@ -594,6 +606,7 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
     __shared__ float sums[8][COLS];
     __shared__ long long length[8];                // chunks of the long runs met in this round
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    wait_for_previous();
     const long long all = (long long)a.joins[0] * a.col_tiles;
     // a run's column tiles follow one another: neighbours go to different blocks, so that a long run's do not queue up in one
     for (long long id0 = blockIdx.x; id0 < all; id0 += (long long)gridDim.x * 8) {
@@ -650,11 +663,25 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
 // rows of zeros alone (no tokens)
 __global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_rows(a, 0, 1, blockIdx.x, gridDim.x); }
 
+template <class... P, class... A>
+void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, kernel, args...);           // (an error stays for launch_status)
+}
+
 template <class T, bool WIDE>
 void launch_sums(const GradArgs& a, bool zero_here, int sms, cudaStream_t st) {
     const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + SUM_THREADS / 32 - 1) / (SUM_THREADS / 32));
-    run_sum_kernel<T, WIDE><<<sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, 0, st>>>(a, sum_blocks);
-    run_join_kernel<sizeof(T), WIDE><<<sms * 4, 256, 0, st>>>(a);
+    launch_after(run_sum_kernel<T, WIDE>, sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, st, a, sum_blocks);
+    launch_after(run_join_kernel<sizeof(T), WIDE>, sms * 4, 256, st, a);
 }
 
 int bits_for(long long v) {
@@ -681,7 +708,7 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     s.tiles = (int)((N + tile - 1) / tile);
     s.col_tiles = (int)((D + COLS - 1) / COLS);
     // chunks as long as 64 places while they give every SM some 16 warps
-    s.chunk = 16;
+    s.chunk = 8;
     while (s.chunk < 64 && R * N / (2 * s.chunk) * s.col_tiles >= 148 * 16) s.chunk *= 2;
     s.chunks = (int)((N + s.chunk - 1) / s.chunk);
     s.count = 4 * R * N;
@@ -723,7 +750,7 @@ int qs_embed(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int tok
     if (N == 0) return QS_OK;
     if (!tokens || !table || !out || !aligned_to(tokens, token_type == QS_I64 ? 8 : 4) || !aligned_to(table, size_of_type(table_type)) ||
         !aligned_to(out, size_of_type(out_type)) || !aligned_to(status, 4)) return QS_INVALID_ARG;
-    EmbedArgs a{N, V, D, Ids{tokens, token_type == QS_I64}, table, worker_stride, row_stride, scale, out, out_stride, status, R * N, 0};
+    EmbedArgs a{N, V, D, Ids{tokens, token_type == QS_I64}, table, worker_stride, row_stride, scale, out, out_stride, status, R * N, 0, 0};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (table_type == QS_F32) launch_embed_to<float>(a, out_type, st);
     else if (table_type == QS_BF16) launch_embed_to<__nv_bfloat16>(a, out_type, st);
@@ -771,7 +798,8 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     a.unit = 32;
     while (a.unit > 1 && a.unit * D > 2048) a.unit /= 2;
     if (N == 0 && accumulate) return QS_OK;
-    if (cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
+    // (the one-tile sort sets its own marks to zero)
+    if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
     if (N == 0) {
         zero_all_kernel<<<sms * 8, 256, 0, st>>>(a);
         return launch_status();
@@ -783,7 +811,7 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
         // as many blocks as fit beside the sort's two to an SM, so that none of them starts late with a full share
         const int zero_blocks = accumulate ? 0 : R * p.tiles < sms ? 2 * sms - R * p.tiles : sms;
         for (int pass = 0; pass < p.passes; ++pass)
-            sort_scatter_kernel<<<R * p.tiles + zero_blocks, SORT_THREADS, 0, st>>>(a, pass);
+            launch_after(sort_scatter_kernel, (unsigned)(R * p.tiles + zero_blocks), SORT_THREADS, st, a, pass);
     }
     const int size = size_of_type(grad_type);
     const bool zero_here = p.one_tile && !accumulate;
