@@ -206,6 +206,7 @@ struct GradArgs {
     int col_tiles;
     int side;                              // where the sorted list ends up
     int unit;                              // rows a warp sets to zero at a time
+    int swept;                             // or: tables of 16-byte units side by side
 };
 
 __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
@@ -231,10 +232,45 @@ __device__ __forceinline__ void warp_zero(float* dst, long long n) {
     if (tail + lane < n) dst[tail + lane] = 0.0f;
 }
 
+// Tables of 16-byte units side by side: all blocks sweep over a worker's table together, a unit per thread, so that the
+// writes go through memory in order (7.0 TB/s; a warp on 8 KB of its own, 5.9)
+__device__ void zero_swept(const GradArgs& a, int part, int parts, long long block, long long blocks) {
+    constexpr int AHEAD = 4;
+    const uint32_t d4 = (uint32_t)(a.D / 4), all = (uint32_t)(a.V * d4);
+    const uint32_t lo = (uint32_t)((unsigned long long)all * part / parts), hi = (uint32_t)((unsigned long long)all * (part + 1) / parts);
+    const uint32_t stride = (uint32_t)blocks * blockDim.x, rows = stride / d4, rest = stride % d4;
+    for (int r = 0; r < a.R; ++r) {
+        const uint8_t* named = a.named + r * a.padded;
+        float4* table = reinterpret_cast<float4*>(a.grad + r * a.worker_stride);
+        uint32_t at = lo + (uint32_t)block * blockDim.x + threadIdx.x, row = at / d4, in = at % d4;
+        while (at < hi) {
+            bool zero[AHEAD];
+            uint32_t where[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                where[u] = at;
+                zero[u] = at < hi && !named[row];
+                at += stride;
+                row += rows;
+                in += rest;
+                if (in >= d4) { in -= d4; ++row; }
+                if (row >= a.V) row = 0;           // (past the end: not used)
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (zero[u]) __stcs(table + where[u], make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        }
+    }
+}
+
 // Rows that no token names, part `part` of `parts` of them, by `blocks` blocks of which this is number `block`.  A warp
 // takes `unit` rows at a time (a power of two up to 32, about 8 KB: short enough to spread the work evenly);
 // neighbours without a name are one stretch where rows lie side by side
 __device__ void zero_rows(const GradArgs& a, int part, int parts, long long block, long long blocks) {
+    if (a.swept) {
+        zero_swept(a, part, parts, block, blocks);
+        return;
+    }
     const int unit = a.unit, lane = threadIdx.x & 31;
     const long long per = a.padded / unit, all = per * a.R, lo = all * part / parts, hi = all * (part + 1) / parts;
     const long long warps = blocks * (blockDim.x >> 5);
@@ -448,67 +484,92 @@ __device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0,
     }
 }
 
-template <class T, bool WIDE>
-struct Piece {                             // a lane's 8 columns of one row of g
-    uint4 q[sizeof(T) / 2];
-    float f[WIDE ? 1 : 8];
+// A warp's chunk of the sorted places and 256 columns of it
+struct Chunk {
+    long long ch, r, i0;                   // chunk, worker, first place
+    int c0, n;                             // first column, places
+    const uint32_t* key;
+    const uint32_t* pos;
+    uint32_t prev, next;                   // tokens beside the chunk
+    bool there;
 
-    __device__ __forceinline__ void load(const GradArgs& a, const T* row, int c0, bool on) {
-        const int lane = threadIdx.x & 31;
-        if (WIDE) {
-            constexpr int E = 16 / sizeof(T);
-#pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-                const int c = c0 + col_of<sizeof(T), true>(lane, h * E);
-                q[h] = make_uint4(0, 0, 0, 0);
-                if (on && c + E <= a.D) q[h] = __ldcs(reinterpret_cast<const uint4*>(row + c));
-                else if (on && c < a.D) {                  // the last columns
-                    uint32_t* w = &q[h].x;
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        if (c + j >= a.D) continue;
-                        if (sizeof(T) == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[c + j];
-                        else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[c + j] << (16 * (j & 1));
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = c0 + lane + 32 * j;
-                f[WIDE ? 0 : j] = on && c < a.D ? to_float(row[c]) : 0.0f;
-            }
-        }
+    __device__ __forceinline__ Chunk(const GradArgs& a, long long id) {
+        there = id < (long long)a.R * a.chunks * a.col_tiles;
+        if (!there) return;
+        ch = id / a.col_tiles;
+        c0 = (int)(id - ch * a.col_tiles) * COLS;
+        r = ch / a.chunks;
+        i0 = (ch - r * a.chunks) * a.chunk;
+        n = (int)min((long long)a.chunk, a.N - i0);
+        key = a.key[a.side] + r * a.N + i0;
+        pos = a.pos[a.side] + r * a.N + i0;
+        prev = i0 > 0 ? key[-1] : 0xffffffffu;
+        next = i0 + n < a.N ? key[n] : 0xffffffffu;
     }
-    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
-        if (WIDE) {
-            float x[8];
-            if (sizeof(T) == 4) {
-                const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[sizeof(T) / 2 - 1].x, q[sizeof(T) / 2 - 1].y, q[sizeof(T) / 2 - 1].z, q[sizeof(T) / 2 - 1].w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
-            } else {
-                widen_if(x);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += x[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += f[WIDE ? 0 : j];
-        }
-    }
-    __device__ __forceinline__ void widen_if(float* x) const;
 };
-template <class T, bool WIDE> __device__ __forceinline__ void Piece<T, WIDE>::widen_if(float* x) const { widen(q[0], x, T()); }
-template <> __device__ __forceinline__ void Piece<float, true>::widen_if(float*) const {}
-template <> __device__ __forceinline__ void Piece<float, false>::widen_if(float*) const {}
 
-constexpr int SUM_THREADS = 128;
+// the run being summed
+template <bool WIDE, int SIZE>
+struct Run {
+    uint32_t cur;
+    bool first;                            // of its chunk
+    float sum[8];
 
-// A warp per chunk and 256 columns; blocks past those set rows to zero (one-tile sorts: nothing ran beside them)
-template <class T, bool WIDE>
-__global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
-    constexpr int AHEAD = sizeof(T) == 4 || !WIDE ? 2 : 4;         // rows in a batch; two batches are in flight
+    __device__ __forceinline__ void start(uint32_t k) {
+        cur = k;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    }
+    // on: it goes on in the next chunk
+    __device__ __forceinline__ void flush(const GradArgs& a, const Chunk& c, bool on) {
+        if (cur >= (uint32_t)a.V) return;
+        const int lane = threadIdx.x & 31;
+        const bool from = first && cur == c.prev;
+        if (!from && !on) {
+            write_sum<WIDE, SIZE>(a, a.grad + c.r * a.worker_stride + (long long)cur * a.row_stride, c.c0, sum);
+        } else {                                   // part of a run that crosses chunks
+            float4* p = reinterpret_cast<float4*>(a.part + (c.ch * 2 + (from ? 0 : 1)) * ((long long)a.col_tiles * COLS) + c.c0 + lane * 8);
+            p[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            p[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            if (!from && c.c0 == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1u)] = (uint32_t)c.ch;
+        }
+    }
+    __device__ __forceinline__ void meet(const GradArgs& a, const Chunk& c, uint32_t k) {
+        if (k == cur) return;
+        flush(a, c, false);
+        first = false;
+        start(k);
+    }
+};
+
+// adds a lane's 8 columns of a row
+__device__ __forceinline__ void add_pieces(const uint4* q, float (&sum)[8], float) {
+    const uint32_t w[8] = {q[0].x, q[0].y, q[0].z, q[0].w, q[1].x, q[1].y, q[1].z, q[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += __uint_as_float(w[j]);
+}
+template <class T>
+__device__ __forceinline__ void add_pieces(const uint4* q, float (&sum)[8], T type) {
+    float x[8];
+    widen(q[0], x, type);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += x[j];
+}
+
+// Wide rows: a warp per chunk and 256 columns, its rows on their way through a ring of its own in shared memory, 16 (or 8
+// of fp32) ahead of the sums: each lane copies and reads its own 16 bytes, so that no barrier is needed
+constexpr int RING_WARPS = 8, RING_BYTES = 8192;           // per warp
+
+__device__ __forceinline__ void copy16(uint4* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <class T>
+__global__ void __launch_bounds__(RING_WARPS * 32, 3) run_sum_wide_kernel(const GradArgs a, unsigned sum_blocks) {
+    constexpr int E = 16 / sizeof(T), PIECES = sizeof(T) / 2, DEPTH = RING_BYTES / (512 * PIECES);
+    extern __shared__ __align__(16) uint4 ring_of_all[];
     wait_for_previous();
     next_may_start();
     if (blockIdx.x >= sum_blocks) {
@@ -516,72 +577,99 @@ __global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs 
         return;
     }
     const int lane = threadIdx.x & 31;
-    const long long id = (long long)blockIdx.x * (SUM_THREADS / 32) + (threadIdx.x >> 5);
-    if (id >= (long long)a.R * a.chunks * a.col_tiles) return;
-    const long long ch = id / a.col_tiles;
-    const int c0 = (int)(id - ch * a.col_tiles) * COLS;
-    const long long r = ch / a.chunks, i0 = (ch - r * a.chunks) * a.chunk;
-    const int n = (int)min((long long)a.chunk, a.N - i0);
-    const uint32_t* key = a.key[a.side] + r * a.N + i0;
-    const uint32_t* pos = a.pos[a.side] + r * a.N + i0;
-    const T* g = static_cast<const T*>(a.g) + r * a.N * a.g_stride;
+    uint4* ring = ring_of_all + (threadIdx.x >> 5) * (RING_BYTES / 16) + lane;         // slot s, piece h: ring[(s * PIECES + h) * 32]
+    const Chunk c(a, (long long)blockIdx.x * RING_WARPS + (threadIdx.x >> 5));
+    if (!c.there) return;
     const uint32_t none = 0xffffffffu, V = (uint32_t)a.V;
-    const uint32_t prev = i0 > 0 ? key[-1] : none, next = i0 + n < a.N ? key[n] : none;
-    float sum[8];
+    const uint32_t k0 = lane < c.n ? c.key[lane] : none, k1 = lane + 32 < c.n ? c.key[lane + 32] : none;
+    const uint32_t p0 = lane < c.n ? c.pos[lane] : 0u, p1 = lane + 32 < c.n ? c.pos[lane + 32] : 0u;
+    const int n = __popc(__ballot_sync(~0u, k0 < V)) + __popc(__ballot_sync(~0u, k1 < V));     // places past these name no row
+    if (n == 0) return;
+    const T* g = static_cast<const T*>(a.g) + c.r * a.N * a.g_stride;
+    int col[PIECES];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
-    uint32_t cur = key[0];
-    bool first = true;
-    auto flush = [&](bool last) {
-        if (cur >= V) return;
-        const bool from = first && cur == prev, on = last && cur == next;
-        if (!from && !on) {
-            write_sum<WIDE, sizeof(T)>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
-        } else {                                   // part of a run that crosses chunks
-            float* p = a.part + (ch * 2 + (from ? 0 : 1)) * ((long long)a.col_tiles * COLS) + c0 + lane * 8;
-            reinterpret_cast<float4*>(p)[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
-            if (!from && c0 == 0 && lane == 0) a.joins[1 + atomicAdd(a.joins, 1u)] = (uint32_t)ch;
-        }
-    };
-    for (int b = 0; b < n; b += 32) {
-        const int left = min(32, n - b);
-        const uint32_t k = lane < left ? key[b + lane] : none, p = lane < left ? pos[b + lane] : 0u;
-        if (__all_sync(~0u, k >= V) && cur >= V) break;            // only places that name no row are left
-        Piece<T, WIDE> row[2][AHEAD];
-        auto fetch = [&](Piece<T, WIDE> (&to)[AHEAD], int i) {
+    for (int h = 0; h < PIECES; ++h) col[h] = c.c0 + col_of<sizeof(T), true>(lane, h * E);
+    auto issue = [&](int i) {
+        if (i < n) {
+            const uint32_t at = __shfl_sync(~0u, i < 32 ? p0 : p1, i & 31);
+            const T* row = g + (long long)at * a.g_stride;
+            uint4* slot = ring + (i % DEPTH) * PIECES * 32;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31), pu = __shfl_sync(~0u, p, (i + u) & 31);
-                to[u].load(a, g + (long long)pu * a.g_stride, c0, i + u < left && ku < V);
-            }
-        };
-        auto add = [&](const Piece<T, WIDE> (&from)[AHEAD], int i) {
+            for (int h = 0; h < PIECES; ++h) {
+                if (col[h] + E <= a.D) copy16(slot + h * 32, row + col[h]);
+                else if (col[h] < a.D) {                   // the last columns
+                    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const uint32_t ku = __shfl_sync(~0u, k, (i + u) & 31);
-                if (i + u < left) {
-                    if (ku != cur) {
-                        flush(false);
-                        first = false;
-                        cur = ku;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+                    for (int j = 0; j < E; ++j) {
+                        if (col[h] + j >= a.D) continue;
+                        if (sizeof(T) == 4) w[j] = reinterpret_cast<const uint32_t*>(row)[col[h] + j];
+                        else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col[h] + j] << (16 * (j & 1));
                     }
-                    from[u].add_to(sum);
+                    slot[h * 32] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-        };
-        fetch(row[0], 0);
-        for (int i = 0; i < left; i += 2 * AHEAD) {
-            if (i + AHEAD < left) fetch(row[1], i + AHEAD);
-            add(row[0], i);
-            if (i + AHEAD >= left) break;
-            if (i + 2 * AHEAD < left) fetch(row[0], i + 2 * AHEAD);
-            add(row[1], i + AHEAD);
         }
+        copy_commit();
+    };
+#pragma unroll 1
+    for (int i = 0; i < DEPTH; ++i) issue(i);
+    Run<true, sizeof(T)> run;
+    run.first = true;
+    run.start(__shfl_sync(~0u, k0, 0));
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        copy_wait<DEPTH - 1>();
+        run.meet(a, c, __shfl_sync(~0u, i < 32 ? k0 : k1, i & 31));
+        uint4 q[PIECES];
+#pragma unroll
+        for (int h = 0; h < PIECES; ++h) q[h] = ring[((i % DEPTH) * PIECES + h) * 32];
+        add_pieces(q, run.sum, T());
+        issue(i + DEPTH);
     }
-    flush(true);
+    run.flush(a, c, n == c.n && run.cur == c.next);
+}
+
+// Rows of any alignment: the same with single-element loads, side by side across the warp.  Blocks past the chunks set rows
+// to zero (one-tile sorts: nothing ran beside them)
+constexpr int SUM_THREADS = 128;
+
+template <class T>
+__global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs a, unsigned sum_blocks) {
+    constexpr int AHEAD = 4;                       // rows in flight
+    wait_for_previous();
+    next_may_start();
+    if (blockIdx.x >= sum_blocks) {
+        zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
+        return;
+    }
+    const int lane = threadIdx.x & 31;
+    const Chunk c(a, (long long)blockIdx.x * (SUM_THREADS / 32) + (threadIdx.x >> 5));
+    if (!c.there) return;
+    const T* g = static_cast<const T*>(a.g) + c.r * a.N * a.g_stride + c.c0 + lane;
+    const int cols = (int)min(a.D - c.c0 - lane, (long long)COLS);     // the lane's columns are 32 apart below it
+    Run<false, sizeof(T)> run;
+    run.first = true;
+    run.start(c.key[0]);
+    for (int i = 0; i < c.n; i += AHEAD) {
+        float f[AHEAD][8];
+        uint32_t k[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            k[u] = i + u < c.n ? c.key[i + u] : 0xffffffffu;
+            const T* row = g + (long long)(k[u] < (uint32_t)a.V ? c.pos[i + u] : 0u) * a.g_stride;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[u][j] = k[u] < (uint32_t)a.V && 32 * j < cols ? to_float(row[32 * j]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i + u >= c.n) break;
+            run.meet(a, c, k[u]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) run.sum[j] += f[u][j];
+        }
+        if (run.cur >= (uint32_t)a.V) return;      // only places that name no row are left
+    }
+    run.flush(a, c, run.cur == c.next);
 }
 
 // Runs that cross chunks: their partial sums are added in order.  A warp per run and 256 columns; a run of more than
@@ -664,10 +752,11 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
 __global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_rows(a, 0, 1, blockIdx.x, gridDim.x); }
 
 template <class... P, class... A>
-void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, cudaStream_t st, A... args) {
+void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, unsigned smem, cudaStream_t st, A... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -679,9 +768,15 @@ void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, cudaStr
 
 template <class T, bool WIDE>
 void launch_sums(const GradArgs& a, bool zero_here, int sms, cudaStream_t st) {
-    const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + SUM_THREADS / 32 - 1) / (SUM_THREADS / 32));
-    launch_after(run_sum_kernel<T, WIDE>, sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, st, a, sum_blocks);
-    launch_after(run_join_kernel<sizeof(T), WIDE>, sms * 4, 256, st, a);
+    if (WIDE) {
+        const unsigned blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + RING_WARPS - 1) / RING_WARPS);
+        cudaFuncSetAttribute(run_sum_wide_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_WARPS * RING_BYTES);
+        launch_after(run_sum_wide_kernel<T>, blocks + (zero_here ? sms * 3 : 0), RING_WARPS * 32, RING_WARPS * RING_BYTES, st, a, blocks);
+    } else {
+        const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + SUM_THREADS / 32 - 1) / (SUM_THREADS / 32));
+        launch_after(run_sum_kernel<T>, sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, 0, st, a, sum_blocks);
+    }
+    launch_after(run_join_kernel<sizeof(T), WIDE>, sms * 4, 256, 0, st, a);
 }
 
 int bits_for(long long v) {
@@ -797,6 +892,8 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     a.chunk = p.chunk; a.chunks = p.chunks; a.col_tiles = p.col_tiles; a.side = p.passes & 1;
     a.unit = 32;
     while (a.unit > 1 && a.unit * D > 2048) a.unit /= 2;
+    // (32-bit counters with a stride to spare)
+    a.swept = aligned_to(grad_table, 16) && D % 4 == 0 && row_stride == D && worker_stride % 4 == 0 && V * (D / 4) < (1ll << 31);
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)
     if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
@@ -811,7 +908,7 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
         // as many blocks as fit beside the sort's two to an SM, so that none of them starts late with a full share
         const int zero_blocks = accumulate ? 0 : R * p.tiles < sms ? 2 * sms - R * p.tiles : sms;
         for (int pass = 0; pass < p.passes; ++pass)
-            launch_after(sort_scatter_kernel, (unsigned)(R * p.tiles + zero_blocks), SORT_THREADS, st, a, pass);
+            launch_after(sort_scatter_kernel, (unsigned)(R * p.tiles + zero_blocks), SORT_THREADS, 0, st, a, pass);
     }
     const int size = size_of_type(grad_type);
     const bool zero_here = p.one_tile && !accumulate;

@@ -65,6 +65,8 @@ def _done(rc, what):
 def _rows(t, what):
     """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one."""
     shape, stride = t.shape, t.stride()
+    if t.numel() == 0 and len(shape) >= 2:
+        return shape[-1]
     if len(shape) < 2 or (stride[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{what} needs rows with unit stride")
     for i in range(len(shape) - 3, -1, -1):
