@@ -61,7 +61,7 @@ def teacher_entries(teacher, tokens, top):
     return r.top_ids, r.top_logp
 
 
-def run(R=4, vocab=1000, width=64, tokens=256, top=16, steps=60, sync_every=2, eta=2.0, seed=0, log=None):
+def run(R=4, vocab=1000, width=64, tokens=256, top=16, steps=60, sync_every=2, eta=20.0, seed=0, log=None):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     student = Student(vocab, width)
     teacher = torch.randn((vocab, vocab), generator=gen, device="cuda") * 2.5

@@ -41,12 +41,18 @@ def _on(first, *rest):
     return device
 
 
+_empty = {}
+
+
 def _allocate(stream, shape, dtype, device):
-    """A tensor that belongs to `stream` (None: the current one)."""
+    """A tensor that belongs to `stream` (None: the current one); shape: a tuple, or a number of elements."""
+    like = _empty.get((dtype, device))
+    if like is None:                                     # (new_empty takes half of torch.empty's time on the host)
+        like = _empty[dtype, device] = torch.empty(0, dtype=dtype, device=device)
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape)
 
 
 def _handle(stream, device):
@@ -182,17 +188,17 @@ def token_logp(logits, tokens=None, scale=1.0, top=0, status=None, stream=None):
         id_type = tokens.dtype
         _type(tokens, "tokens", _ID)
         _vector(tokens, N, "tokens", id_type)
-    stats = _allocate(stream, (3, N), torch.float32, device)
+    f32 = torch.float32
+    logp = _allocate(stream, N, f32, device) if tokens is not None else None
+    lse, entropy = _allocate(stream, N, f32, device), _allocate(stream, N, f32, device)
     ids = top_logp = None
     if top:
         ids = _allocate(stream, (N, top), id_type, device)
-        top_logp = _allocate(stream, (N, top), torch.float32, device)
-    base = stats.data_ptr()
+        top_logp = _allocate(stream, (N, top), f32, device)
     _done(lib().qs_token_logp(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens), _ID[id_type], scale, top,
-                              base if tokens is not None else None, base + 4 * N, base + 8 * N, _ptr(ids), _ptr(top_logp), _ptr(status),
+                              _ptr(logp), lse.data_ptr(), entropy.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(status),
                               _handle(stream, device)), "qs_token_logp")
-    logp, lse, entropy = stats.unbind(0)
-    return TokenLogp(logp if tokens is not None else None, lse, entropy, ids, top_logp)
+    return TokenLogp(logp, lse, entropy, ids, top_logp)
 
 
 def _gradient(logits, out):
@@ -257,16 +263,15 @@ def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weig
         w, w_all = _weights(weight, N, "weight")
     elif out is not None:
         raise ValueError("a gradient needs weight")
-    stats = _allocate(stream, (3 if tail else 2, N), torch.float32, device)
+    loss, lse = _allocate(stream, N, torch.float32, device), _allocate(stream, N, torch.float32, device)
+    log_tail = _allocate(stream, N, torch.float32, device) if tail else None
     if weight is not None and out is None:
         out = _allocate(stream, (N, V), logits.dtype, device)
-    base = stats.data_ptr()
     _done(lib().qs_distill(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
-                           teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), base, base + 4 * N,
-                           base + 8 * N if tail else None, w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _ptr(status),
+                           teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), loss.data_ptr(), lse.data_ptr(),
+                           _ptr(log_tail), w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _ptr(status),
                            _handle(stream, device)), "qs_distill")
-    parts = stats.unbind(0)
-    return Distill(parts[0], parts[1], parts[2] if tail else None, out)
+    return Distill(loss, lse, log_tail, out)
 
 
 def distill_grad(logits, ids, teacher, lse, weight, scale=1.0, teacher_scale=1.0, tail=False, log_tail=None, out=None, status=None,
