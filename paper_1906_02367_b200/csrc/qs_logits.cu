@@ -50,7 +50,7 @@ struct RowArgs {
     float g_all;                           // where g1 is null
     void* grad; long long grad_stride;
     int wide;                              // the gradient's rows lie like the logits' rows within 16 bytes
-    int blocks;                            // blocks per row
+    int parts;                             // log2 of the blocks per row
     int per;                               // batches per stretch whose maximum is kept
     int* status;
 };
@@ -287,18 +287,18 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 5 : 6) token_logp_kernel(co
     __shared__ TopShared top[1];                   // (no room where it is not used)
     // TOP: the stretches' maxima (slots x threads), and what a cluster's blocks have left, block b's at b * CANDS / blocks
     extern __shared__ unsigned long long merged[];
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = 1 << a.parts;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-    const long long n = a.row0 + blockIdx.x / blocks;
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
     const float c2 = a.scale * LOG2E;
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
-    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
     Stat st{neg_inf(), 0.0f, 0.0f};
     float mine = neg_inf();                        // the thread's largest
     float* slot_max = reinterpret_cast<float*>(merged + (blocks > 1 ? CANDS : 0)) + threadIdx.x;
     float stretch = neg_inf();
     int batch = 0, slot = 0;
-    each_batch<T, VPT>(r, [&](auto& q, int vec, auto more) {
+    each_batch<T, VPT, TOP>(r, [&](auto& q, int vec, auto more) {
         constexpr int P = sizeof(q) / sizeof(uint4);
         const float m = thread_max_of<T, P>(q);
         take<T, P, true, decltype(more)::value>(st, q, m, c2);
@@ -415,8 +415,8 @@ __device__ __forceinline__ void map_row(const Share<T>& r, T* out, bool wide, F 
 
 template <class T, bool ENT>
 __global__ void __launch_bounds__(MAX_THREADS) token_logp_grad_kernel(const RowArgs a) {
-    const long long n = a.row0 + blockIdx.x / a.blocks;
-    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
+    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x & ((1u << a.parts) - 1u)), a.parts);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const long long t = a.tok.p ? a.tok.at(n) : -1;
     const float lse = a.in_lse[n];
@@ -622,12 +622,12 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     __shared__ float row_m, row_by;                // maximum, one over the sum
     __shared__ Slope row;
     __shared__ uint32_t marks[KEEP || !TAIL ? 1 : 256];        // vectors that an id may name, by their low bits
-    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = a.blocks;
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = 1 << a.parts;
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
-    const long long n = a.row0 + blockIdx.x / blocks;
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
     const float c2 = a.scale * LOG2E;
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
-    const Share<T> r(a.logits, a.stride, n, a.V, rank, blocks);
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
     if (KEEP) {
         if (threadIdx.x == 0) {
             const uint32_t bytes = r.w1 > r.w0 ? (uint32_t)(r.w1 - r.w0) * 16u : 0u;
@@ -838,8 +838,8 @@ __global__ void __launch_bounds__(MAX_THREADS) distill_grad_kernel(const RowArgs
     constexpr int E = Vec<T>::E;
     __shared__ TeacherShared t;
     const int nt = blockDim.x;
-    const long long n = a.row0 + blockIdx.x / a.blocks;
-    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x % a.blocks), a.blocks);
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
+    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x & ((1u << a.parts) - 1u)), a.parts);
     const float lse = a.in_lse[n], log_tail = TAIL ? a.in_log_tail[n] : 0.0f;
     if (threadIdx.x < 32) {
         Entries e;
@@ -929,7 +929,8 @@ Shape keep_shape(int64_t N, long long vectors) {
 
 template <class K>
 cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaStream_t st) {
-    a.blocks = s.blocks;
+    a.parts = 0;
+    while ((1 << a.parts) < s.blocks) ++a.parts;
     if (s.smem > 32 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
         if (e != cudaSuccess) return e;
@@ -958,10 +959,7 @@ cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaS
 // rows
 Shape grad_shape(int64_t N, long long vectors) {
     Shape s{vectors <= 2048 ? 64 : MAX_THREADS, 1, 0, false};
-    const long long most = (vectors + s.nt * 16 - 1) / (s.nt * 16), fine = (vectors + s.nt * 4 - 1) / (s.nt * 4);
-    long long blocks = most;
-    while (blocks < fine && N * blocks < 8 * SMS) blocks *= 2;
-    s.blocks = (int)(blocks < fine ? blocks : fine);
+    while ((long long)s.blocks * s.nt * 16 < vectors || (N * s.blocks < 8 * SMS && (long long)s.blocks * s.nt * 4 < vectors)) s.blocks *= 2;
     return s;
 }
 

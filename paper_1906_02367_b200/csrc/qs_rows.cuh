@@ -146,11 +146,11 @@ struct Share {
     int v0, v1;                // the block's vectors
     int w0, w1;                // those of them that are whole
 
-    __device__ __forceinline__ Share(const void* logits, long long stride, long long n, long long len, int part, int nparts) {
+    __device__ __forceinline__ Share(const void* logits, long long stride, long long n, long long len, int part, int log_parts) {
         z = static_cast<const T*>(logits) + n * stride;
         V = (int)len;
         head = (int)((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
-        const int nvec = (V + head + Vec<T>::E - 1) / Vec<T>::E, per = (nvec + nparts - 1) / nparts;
+        const int nvec = (V + head + Vec<T>::E - 1) / Vec<T>::E, per = (nvec + (1 << log_parts) - 1) >> log_parts;
         v0 = min(part * per, nvec);
         v1 = min(v0 + per, nvec);
         w0 = v0 < v1 && !whole(v0) ? v0 + 1 : v0;
@@ -202,10 +202,11 @@ __device__ __forceinline__ void load_share(const Share<T>& r, int base, int nt, 
 }
 
 // calls f(q, vec, more) for the share's vectors, nt apart from vec on: batches of VPT per thread, then the rest in one
-// batch (`more`: vectors at or past w1 are no vectors, -inf), then those that are not whole
+// batch (`more`: vectors at or past w1 are no vectors, -inf), then those that are not whole.  AGAIN: some will be read again soon
 struct Full { static constexpr bool value = false; };
 struct Rest { static constexpr bool value = true; };
-template <class T, int VPT, class F>
+template <bool AGAIN> __device__ __forceinline__ uint4 read_vec(const uint4* p) { return AGAIN ? __ldcg(p) : __ldcs(p); }
+template <class T, int VPT, bool AGAIN, class F>
 __device__ __forceinline__ void each_batch(const Share<T>& r, F f) {
     const int nt = blockDim.x;
     const uint4* p = r.vectors();
@@ -214,7 +215,7 @@ __device__ __forceinline__ void each_batch(const Share<T>& r, F f) {
         const int vec = base + (int)threadIdx.x;
         uint4 q[VPT];
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) q[j] = __ldcs(p + vec + j * nt);
+        for (int j = 0; j < VPT; ++j) q[j] = read_vec<AGAIN>(p + vec + j * nt);
         f(q, vec, Full());
     }
     if (base + nt < r.w1) {
@@ -223,12 +224,12 @@ __device__ __forceinline__ void each_batch(const Share<T>& r, F f) {
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             q[j] = all_lowest<T>();
-            if (vec + j * nt < r.w1) q[j] = __ldcs(p + vec + j * nt);
+            if (vec + j * nt < r.w1) q[j] = read_vec<AGAIN>(p + vec + j * nt);
         }
         f(q, vec, Rest());
     } else if (base + (int)threadIdx.x < r.w1) {
         const int vec = base + (int)threadIdx.x;
-        uint4 q[1] = {__ldcs(p + vec)};
+        uint4 q[1] = {read_vec<AGAIN>(p + vec)};
         f(q, vec, Full());
     }
     if (threadIdx.x == 0 && r.w0 > r.v0) {
