@@ -491,16 +491,19 @@ struct Entries {
         }
     }
     // the row's probabilities into shared memory
+    // (how many of them name a column)
     template <bool TAIL>
-    __device__ void finish(const RowArgs& a, TeacherShared& s, bool tell) {
+    __device__ int finish(const RowArgs& a, TeacherShared& s, bool tell) {
         const int lane = threadIdx.x & 31;
         bool bad = false;
+        int entries = 0;
         float m = neg_inf();
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int k = lane + 32 * i;
             const bool named = id[i] >= 0 && id[i] < a.V;
             bad |= id[i] >= a.V;
+            entries += __popc(__ballot_sync(~0u, named));
             u[i] = named ? u[i] * a.teacher_scale : neg_inf();
             if (k < a.K) s.id[k] = named ? (uint32_t)id[i] : NO_ID;
             m = fmaxf(m, u[i]);
@@ -535,6 +538,7 @@ struct Entries {
             if (bad && tell) flag_status(a.status, QS_INVALID_ARG);
         }
         __syncwarp();
+        return entries;
     }
 };
 
@@ -614,7 +618,7 @@ template <class T, bool KEEP, bool TAIL>
 __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a) {
     constexpr int E = Vec<T>::E, PER = (QS_MAX_TOP + 31) / 32;
     extern __shared__ __align__(128) uint4 kept[];
-    __shared__ uint64_t landed;
+    __shared__ uint64_t landed, met;               // the share's copy; what the row's blocks send to one another
     __shared__ float4 part[PARTS];
     __shared__ float4 in_part[MAX_BLOCKS];         // tail: the statistics of the ids' own columns, block by block
     __shared__ float z_at[QS_MAX_TOP];             // first block: logits at the ids
@@ -626,13 +630,17 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     const int rank = blocks == 1 ? 0 : (int)cluster_rank();
     const long long n = a.row0 + (blockIdx.x >> a.parts);
     const float c2 = a.scale * LOG2E;
+    if (threadIdx.x == 0) {
+        mbar_init(&landed, 1);
+        mbar_init(&met, 1);
+        fence_async_smem();
+        if (blocks > 1) fence_barrier_init();
+    }
     if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
     const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
     if (KEEP) {
         if (threadIdx.x == 0) {
             const uint32_t bytes = r.w1 > r.w0 ? (uint32_t)(r.w1 - r.w0) * 16u : 0u;
-            mbar_init(&landed, 1);
-            fence_async_smem();
             mbar_expect(&landed, bytes);
             if (bytes) bulk_load(kept + (r.w0 - r.v0), r.vectors() + r.w0, bytes, &landed);
         }
@@ -641,10 +649,13 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     }
     if (!KEEP && TAIL)
         for (int i = threadIdx.x; i < 256; i += nt) marks[i] = 0;
+    const int readers = a.grad ? blocks : 1;       // blocks that need the row's statistics
     if (warp == 0) {
         Entries e;
         e.load(a, n);
-        e.finish<TAIL>(a, t, rank == 0);
+        const int entries = e.finish<TAIL>(a, t, rank == 0);
+        if (lane == 0 && blocks > 1 && rank < readers)
+            mbar_expect(&met, blocks * (warps + (TAIL ? 1 : 0)) * (uint32_t)sizeof(float4) + (rank == 0 ? entries * (uint32_t)sizeof(float) : 0u));
     }
     __syncthreads();
     if (blocks > 1) cluster_wait();
@@ -661,8 +672,8 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         const int place = (int)t.id[k] + r.head;
         const float z = to_float(KEEP ? flat[place - r.v0 * E] : r.z[t.id[k]]);
         t.z[k] = z;
-        if (rank != 0) remote_store(remote_addr(&z_at[k], 0), __float_as_uint(z));
-        else z_at[k] = z;
+        if (blocks == 1) z_at[k] = z;
+        else send(remote_addr(&z_at[k], 0), z, remote_addr(&met, 0));
         if (!KEEP && TAIL) atomicOr(&marks[(place / E & 8191) >> 5], 1u << (place / E & 31));
     }
     if (TAIL) {                                    // these places leave the sum; their own statistics join later
@@ -693,13 +704,12 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         take<T, VK, false, false>(st, q, most, c2);
         largest = fmaxf(largest, most);
     }
-    const int readers = a.grad ? blocks : 1;       // blocks that need the row's statistics
     const Stat w = join_warp<false>(st, largest, c2);
     const float4 sent = make_float4(w.m, w.s, 0.0f, 0.0f);
     if (blocks == 1) {
         if (lane == 0) part[warp] = sent;
     } else if (lane < readers) {
-        remote_store(remote_addr(&part[rank * warps + warp], lane), sent);
+        send(remote_addr(&part[rank * warps + warp], lane), sent, remote_addr(&met, lane));
     }
     if (TAIL && warp == 0) {
         float z[Entries::PER], m = neg_inf(), s = 0.0f;
@@ -724,19 +734,18 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         if (blocks == 1) {
             if (lane == 0) in_part[0] = v;
         } else if (lane < readers) {
-            remote_store(remote_addr(&in_part[rank], lane), v);
+            send(remote_addr(&in_part[rank], lane), v, remote_addr(&met, lane));
         }
-    }
-    if (!ok) {                                     // the copy never came (2 s): the row's results are void
-        flag_status(a.status, QS_TIMEOUT);
-        mbar_wait(&landed, 0);                     // once more, before the memory goes to another block
     }
     if (blocks == 1) {
         __syncthreads();
     } else {
-        cluster_arrive();
-        if (!a.grad && rank != 0) return;          // nothing is written into this block's memory
-        cluster_wait();
+        if (rank >= readers) return;               // nothing is sent to this block
+        ok &= mbar_wait(&met, 0);
+    }
+    if (!ok) {                                     // a copy never came (2 s): the row's results are void
+        flag_status(a.status, QS_TIMEOUT);
+        if (KEEP) mbar_wait(&landed, 0);           // once more, before the memory goes to another block
     }
     Stat v{};
     float log_tail = 0.0f, lse = 0.0f, ls = 0.0f;
