@@ -12,7 +12,10 @@
 // equal length whatever the lengths of the runs, and a warp sums a chunk's runs for 256 columns.  A
 // run that crosses chunks (a frequent token's) leaves one partial sum per chunk, and these are
 // joined in order.  The rows that no token names are known after the first look at the tokens (a byte
-// per row), so they are set to zero by blocks that run beside the sort's, which is bound by latency.
+// per row); they are set to zero by blocks beside those that sum, so that reads and writes share the
+// memory, and, as far as there is time, beside those that sort.  At 8 workers x 4096 tokens, tables of
+// 32000 x 1024, bf16 in: 188 us, 5.9 TB/s of what has to be read and written; 65536 tokens, 128000 x
+// 2048: 248 us, 5.3 TB/s.
 #include "qs_lm.cuh"
 
 namespace {
@@ -199,6 +202,7 @@ struct GradArgs {
     uint32_t* count[4];                    // per pass: R x tiles x bins
     uint8_t* named;                        // R x padded: 1 for a row that some token names
     long long padded;                      // V up to a multiple of 32
+    uint32_t* turns;                       // pieces of the tables handed out
     uint32_t* joins;                       // [0] runs that cross chunks, then the chunk each of them starts in
     float* part;                           // R x chunks x 2 x padded D: partial sums of such runs
     int passes, bits, tiles, items, tile;  // bits per digit, tiles per worker, places per thread, places per tile
@@ -206,7 +210,7 @@ struct GradArgs {
     int col_tiles;
     int side;                              // where the sorted list ends up
     int unit;                              // rows a warp sets to zero at a time
-    int swept;                             // or: tables of 16-byte units side by side
+    int pieces;                            // or: tables of 16-byte units side by side, in pieces
 };
 
 __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
@@ -232,50 +236,51 @@ __device__ __forceinline__ void warp_zero(float* dst, long long n) {
     if (tail + lane < n) dst[tail + lane] = 0.0f;
 }
 
-// Tables of 16-byte units side by side: all blocks sweep over a worker's table together, a unit per thread, so that the
-// writes go through memory in order (7.0 TB/s; a warp on 8 KB of its own, 5.9)
-__device__ void zero_swept(const GradArgs& a, int part, int parts, long long block, long long blocks) {
-    constexpr int AHEAD = 4;
-    const uint32_t d4 = (uint32_t)(a.D / 4), all = (uint32_t)(a.V * d4);
-    const uint32_t lo = (uint32_t)((unsigned long long)all * part / parts), hi = (uint32_t)((unsigned long long)all * (part + 1) / parts);
-    const uint32_t stride = (uint32_t)blocks * blockDim.x, rows = stride / d4, rest = stride % d4;
-    for (int r = 0; r < a.R; ++r) {
+// Rows that no token names become zero.  Tables of 16-byte units side by side: pieces of 32 KB are handed out in order
+// (`most` at most to a block), so that the writes go through memory in order and no block is left with more than its
+// share: 7.2 TB/s, where a warp on 8 KB of its own writes 5.9
+constexpr int PIECE = 2048;                // 16-byte units
+template <int NT>
+__device__ void zero_pieces(const GradArgs& a, int most) {
+    constexpr int U = PIECE / NT;
+    __shared__ uint32_t turn;
+    const uint32_t d4 = (uint32_t)(a.D / 4), all = (uint32_t)(a.V * d4), per = (all + PIECE - 1) / PIECE;
+    const unsigned long long pieces = (unsigned long long)per * a.R;
+    const uint32_t rows = NT / d4, rest = NT - rows * d4;
+    uint32_t mine = threadIdx.x == 0 ? atomicAdd(a.turns, 1u) : 0u;
+    for (int done = 1;; ++done) {
+        if (threadIdx.x == 0) turn = mine;
+        __syncthreads();
+        const uint32_t piece = turn;
+        __syncthreads();
+        if (piece >= pieces) return;
+        if (done < most && threadIdx.x == 0) mine = atomicAdd(a.turns, 1u);            // known by the time it is needed
+        const uint32_t r = piece / per, first = (piece - r * per) * PIECE + threadIdx.x;
         const uint8_t* named = a.named + r * a.padded;
         float4* table = reinterpret_cast<float4*>(a.grad + r * a.worker_stride);
-        uint32_t at = lo + (uint32_t)block * blockDim.x + threadIdx.x, row = at / d4, in = at % d4;
-        while (at < hi) {
-            bool zero[AHEAD];
-            uint32_t where[AHEAD];
+        uint32_t row = first / d4, in = first - row * d4;
+        bool zero[U];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                where[u] = at;
-                zero[u] = at < hi && !named[row];
-                at += stride;
-                row += rows;
-                in += rest;
-                if (in >= d4) { in -= d4; ++row; }
-                if (row >= a.V) row = 0;           // (past the end: not used)
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (zero[u]) __stcs(table + where[u], make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        for (int u = 0; u < U; ++u) {
+            zero[u] = first + u * NT < all && !named[row];
+            row += rows;
+            in += rest;
+            if (in >= d4) { in -= d4; ++row; }
         }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (zero[u]) __stcs(table + first + u * NT, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+        if (done == most) return;
     }
 }
 
-// Rows that no token names, part `part` of `parts` of them, by `blocks` blocks of which this is number `block`.  A warp
-// takes `unit` rows at a time (a power of two up to 32, about 8 KB: short enough to spread the work evenly);
-// neighbours without a name are one stretch where rows lie side by side
-__device__ void zero_rows(const GradArgs& a, int part, int parts, long long block, long long blocks) {
-    if (a.swept) {
-        zero_swept(a, part, parts, block, blocks);
-        return;
-    }
+// Other tables, by `blocks` blocks of which this is number `block`: a warp takes `unit` rows at a time (a power of two up to
+// 32, about 8 KB); neighbours without a name are one stretch where rows lie side by side
+__device__ void zero_rows(const GradArgs& a, long long block, long long blocks) {
     const int unit = a.unit, lane = threadIdx.x & 31;
-    const long long per = a.padded / unit, all = per * a.R, lo = all * part / parts, hi = all * (part + 1) / parts;
-    const long long warps = blocks * (blockDim.x >> 5);
+    const long long per = a.padded / unit, all = per * a.R, warps = blocks * (blockDim.x >> 5);
     const bool side_by_side = a.row_stride == a.D;
-    for (long long i = lo + block * (blockDim.x >> 5) + (threadIdx.x >> 5); i < hi; i += warps) {
+    for (long long i = block * (blockDim.x >> 5) + (threadIdx.x >> 5); i < all; i += warps) {
         const long long r = i / per, v0 = (i - r * per) * unit;
         uint32_t left = ~__ballot_sync(~0u, lane < unit && a.named[r * a.padded + v0 + lane]);
         const long long rows = min((long long)unit, a.V - v0);
@@ -290,6 +295,11 @@ __device__ void zero_rows(const GradArgs& a, int part, int parts, long long bloc
             left &= b + len >= 32 ? 0u : ~0u << (b + len);
         }
     }
+}
+template <int NT>
+__device__ __forceinline__ void zero_all(const GradArgs& a, long long block, long long blocks) {
+    if (a.pieces) zero_pieces<NT>(a, 0x7fffffff);
+    else zero_rows(a, block, blocks);
 }
 
 constexpr int SEEN = 2048;
@@ -371,14 +381,17 @@ __device__ uint32_t stable_place(SortShared& s, uint32_t d, int bins) {
     return to;
 }
 
-// One pass of the sort: blocks [0, R x tiles) scatter a tile each, the others set rows to zero meanwhile
+// One pass of the sort: blocks [0, R x tiles) scatter a tile each, the others meanwhile set as many pieces to zero as the
+// sorting, bound by latency, leaves time for (65536 tokens, 128000 rows of 2048: 251 us with 1 piece each, 248 with 4, 258
+// with 16)
+constexpr int BESIDE = 4;
 __global__ void __launch_bounds__(SORT_THREADS, 2) sort_scatter_kernel(const GradArgs a, int pass) {
     __shared__ SortShared s;
     wait_for_previous();
     next_may_start();
     const int sorters = a.R * a.tiles;
     if ((int)blockIdx.x >= sorters) {
-        zero_rows(a, pass, a.passes, blockIdx.x - sorters, gridDim.x - sorters);
+        zero_pieces<SORT_THREADS>(a, BESIDE);
         return;
     }
     const int r = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, bins = 1 << a.bits, shift = pass * a.bits;
@@ -424,7 +437,7 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_one_tile_kernel(const GradA
     const bool in = i < a.N;
     uint32_t k = 0, p = i;
     if (in) k = key_of(a, r * a.N + i);
-    if (r == 0 && i == 0) a.joins[0] = 0;
+    if (r == 0 && i == 0) a.joins[0] = a.turns[0] = 0;
     if (!a.accumulate) {
         uint32_t* marks = reinterpret_cast<uint32_t*>(a.named + r * a.padded);
         for (long long w = i; w < a.padded / 4; w += SORT_THREADS) marks[w] = 0;
@@ -573,7 +586,7 @@ __global__ void __launch_bounds__(RING_WARPS * 32, 3) run_sum_wide_kernel(const 
     wait_for_previous();
     next_may_start();
     if (blockIdx.x >= sum_blocks) {
-        zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
+        zero_all<RING_WARPS * 32>(a, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
         return;
     }
     const int lane = threadIdx.x & 31;
@@ -639,7 +652,7 @@ __global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs 
     wait_for_previous();
     next_may_start();
     if (blockIdx.x >= sum_blocks) {
-        zero_rows(a, 0, 1, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
+        zero_all<SUM_THREADS>(a, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
         return;
     }
     const int lane = threadIdx.x & 31;
@@ -749,7 +762,7 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
 }
 
 // rows of zeros alone (no tokens)
-__global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_rows(a, 0, 1, blockIdx.x, gridDim.x); }
+__global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_all<256>(a, blockIdx.x, gridDim.x); }
 
 template <class... P, class... A>
 void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, unsigned smem, cudaStream_t st, A... args) {
@@ -789,7 +802,7 @@ int bits_for(long long v) {
 struct SortPlan {
     int passes, bits, tiles, items, chunk, chunks, col_tiles;
     bool one_tile;
-    int64_t count, named, joins, zeroed, part, words;    // first words; [count, zeroed) starts at zero
+    int64_t count, named, turns, joins, zeroed, part, words;    // first words; [count, zeroed) starts at zero
 };
 SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     SortPlan s;
@@ -808,7 +821,8 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     s.chunks = (int)((N + s.chunk - 1) / s.chunk);
     s.count = 4 * R * N;
     s.named = s.count + (s.one_tile ? 0 : (int64_t)s.passes * R * s.tiles << s.bits);
-    s.joins = s.named + R * ((V + 31) / 32 * 32) / 4;
+    s.turns = s.named + R * ((V + 31) / 32 * 32) / 4;
+    s.joins = s.turns + 1;
     s.zeroed = s.joins + 1;
     s.part = (s.zeroed + (int64_t)R * s.chunks + 3) / 4 * 4;
     s.words = s.part + (int64_t)R * s.chunks * 2 * s.col_tiles * COLS;
@@ -887,13 +901,13 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     a.worker_stride = worker_stride; a.row_stride = row_stride; a.status = status;
     a.key[0] = w; a.key[1] = w + m; a.pos[0] = w + 2 * m; a.pos[1] = w + 3 * m;
     for (int i = 0; i < p.passes; ++i) a.count[i] = w + p.count + ((int64_t)i * R * p.tiles << p.bits);
-    a.named = reinterpret_cast<uint8_t*>(w + p.named); a.padded = (V + 31) / 32 * 32; a.joins = w + p.joins; a.part = reinterpret_cast<float*>(w + p.part);
+    a.named = reinterpret_cast<uint8_t*>(w + p.named); a.padded = (V + 31) / 32 * 32; a.turns = w + p.turns; a.joins = w + p.joins; a.part = reinterpret_cast<float*>(w + p.part);
     a.passes = p.passes; a.bits = p.bits; a.tiles = p.tiles; a.items = p.items; a.tile = p.items * SORT_THREADS;
     a.chunk = p.chunk; a.chunks = p.chunks; a.col_tiles = p.col_tiles; a.side = p.passes & 1;
     a.unit = 32;
     while (a.unit > 1 && a.unit * D > 2048) a.unit /= 2;
-    // (32-bit counters with a stride to spare)
-    a.swept = aligned_to(grad_table, 16) && D % 4 == 0 && row_stride == D && worker_stride % 4 == 0 && V * (D / 4) < (1ll << 31);
+    // (counters of 32 bits, with a block's last turn each to spare)
+    a.pieces = aligned_to(grad_table, 16) && D % 4 == 0 && row_stride == D && worker_stride % 4 == 0 && V * (D / 4) < (1ll << 31) - PIECE;
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)
     if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
@@ -905,13 +919,11 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
         sort_one_tile_kernel<<<R, SORT_THREADS, 0, st>>>(a);
     } else {
         sort_count_kernel<<<dim3(p.tiles, R), SORT_THREADS, 0, st>>>(a);
-        // as many blocks as fit beside the sort's two to an SM, so that none of them starts late with a full share
-        const int zero_blocks = accumulate ? 0 : R * p.tiles < sms ? 2 * sms - R * p.tiles : sms;
-        for (int pass = 0; pass < p.passes; ++pass)
-            launch_after(sort_scatter_kernel, (unsigned)(R * p.tiles + zero_blocks), SORT_THREADS, 0, st, a, pass);
+        const int sorters = R * p.tiles, beside = accumulate || !a.pieces || sorters > 2 * sms ? 0 : 2 * sms - sorters;
+        for (int pass = 0; pass < p.passes; ++pass) launch_after(sort_scatter_kernel, (unsigned)(sorters + beside), SORT_THREADS, 0, st, a, pass);
     }
     const int size = size_of_type(grad_type);
-    const bool zero_here = p.one_tile && !accumulate;
+    const bool zero_here = !accumulate;
     // 16-byte accesses need every row on a 16-byte boundary
     const bool wide = aligned_to(grad_out, 16) && grad_stride * size % 16 == 0 && aligned_to(grad_table, 16) && row_stride % 4 == 0 && worker_stride % 4 == 0;
     if (grad_type == QS_F32) wide ? launch_sums<float, true>(a, zero_here, sms, st) : launch_sums<float, false>(a, zero_here, sms, st);
