@@ -210,7 +210,7 @@ struct GradArgs {
     int col_tiles;
     int side;                              // where the sorted list ends up
     int unit;                              // rows a warp sets to zero at a time
-    int pieces;                            // or: tables of 16-byte units side by side, in pieces
+    int pieces;                            // or: rows side by side, in pieces (1), of whole 16-byte units (2)
 };
 
 __device__ __forceinline__ uint32_t key_of(const GradArgs& a, long long i) {
@@ -236,17 +236,22 @@ __device__ __forceinline__ void warp_zero(float* dst, long long n) {
     if (tail + lane < n) dst[tail + lane] = 0.0f;
 }
 
-// Rows that no token names become zero.  Tables of 16-byte units side by side: pieces of 32 KB are handed out in order
-// (`most` at most to a block), so that the writes go through memory in order and no block is left with more than its
-// share: 7.2 TB/s, where a warp on 8 KB of its own writes 5.9
+// Rows that no token names become zero.  Rows side by side: the table is cut into 16-byte units, and pieces of 32 KB are
+// handed out in order (`most` at most to a block), so that the writes go through memory in order and no block is left with
+// more than its share: 7.2 TB/s, where a warp on 8 KB of its own writes 5.9.  Rows that are no whole units (EVEN false)
+// have the units counted from the 16-byte boundary at or before the table, `lead` floats off; one that two rows share is
+// written by elements unless both become zero, as are the table's first and last
 constexpr int PIECE = 2048;                // 16-byte units
-template <int NT>
+template <int NT, bool EVEN>
 __device__ void zero_pieces(const GradArgs& a, int most) {
     constexpr int U = PIECE / NT;
     __shared__ uint32_t turn;
-    const uint32_t d4 = (uint32_t)(a.D / 4), all = (uint32_t)(a.V * d4), per = (all + PIECE - 1) / PIECE;
+    // places in a table: units, or floats
+    constexpr uint32_t STEP = EVEN ? 1 : 4;
+    const uint32_t D = (uint32_t)(EVEN ? a.D / 4 : a.D), all = (uint32_t)a.V * D;
+    const uint32_t per = ((EVEN ? all : (all + 6) / 4) + PIECE - 1) / PIECE;
     const unsigned long long pieces = (unsigned long long)per * a.R;
-    const uint32_t rows = NT / d4, rest = NT - rows * d4;
+    const uint32_t rows = STEP * NT / D, rest = STEP * NT - rows * D;
     uint32_t mine = threadIdx.x == 0 ? atomicAdd(a.turns, 1u) : 0u;
     for (int done = 1;; ++done) {
         if (threadIdx.x == 0) turn = mine;
@@ -255,21 +260,40 @@ __device__ void zero_pieces(const GradArgs& a, int most) {
         __syncthreads();
         if (piece >= pieces) return;
         if (done < most && threadIdx.x == 0) mine = atomicAdd(a.turns, 1u);            // known by the time it is needed
-        const uint32_t r = piece / per, first = (piece - r * per) * PIECE + threadIdx.x;
+        const uint32_t r = piece / per;
         const uint8_t* named = a.named + r * a.padded;
-        float4* table = reinterpret_cast<float4*>(a.grad + r * a.worker_stride);
-        uint32_t row = first / d4, in = first - row * d4;
-        bool zero[U];
+        float* table = a.grad + r * a.worker_stride;
+        const uint32_t lead = EVEN ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(table) & 15u) / 4;
+        const uint32_t first = ((piece - r * per) * PIECE + threadIdx.x) * STEP;
+        float4* units = reinterpret_cast<float4*>(table - lead) + first / STEP;
+        if (EVEN || (first >= lead && first + STEP * NT * (U - 1) + 4 <= all + lead)) {
+            uint32_t row = (first - lead) / D, in = first - lead - row * D;
+            int zero[U];                               // 1: the unit, 2: some of its elements
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            zero[u] = first + u * NT < all && !named[row];
-            row += rows;
-            in += rest;
-            if (in >= d4) { in -= d4; ++row; }
+            for (int u = 0; u < U; ++u) {
+                if (EVEN) zero[u] = first + u * NT < all && !named[row];
+                else {
+                    const bool here = !named[row], next = in + 3 >= D ? !named[row + 1] : here;
+                    zero[u] = here && next ? 1 : here || next ? 2 : 0;
+                }
+                row += rows;
+                in += rest;
+                if (in >= D) { in -= D; ++row; }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (zero[u] == 1) __stcs(units + u * NT, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+                if (!EVEN && zero[u] == 2)
+                    for (uint32_t e = 0, f = first - lead + u * STEP * NT; e < 4; ++e)
+                        if (!named[(f + e) / D]) table[f + e] = 0.0f;
+            }
+        } else if constexpr (!EVEN) {                  // a table's first or last piece
+            for (int u = 0; u < U; ++u)
+                for (uint32_t e = 0; e < 4; ++e) {
+                    const uint32_t f = first + u * STEP * NT + e;
+                    if (f >= lead && f < all + lead && !named[(f - lead) / D]) table[f - lead] = 0.0f;
+                }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (zero[u]) __stcs(table + first + u * NT, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
         if (done == most) return;
     }
 }
@@ -298,7 +322,8 @@ __device__ void zero_rows(const GradArgs& a, long long block, long long blocks) 
 }
 template <int NT>
 __device__ __forceinline__ void zero_all(const GradArgs& a, long long block, long long blocks) {
-    if (a.pieces) zero_pieces<NT>(a, 0x7fffffff);
+    if (a.pieces == 2) zero_pieces<NT, true>(a, 0x7fffffff);
+    else if (a.pieces) zero_pieces<NT, false>(a, 0x7fffffff);
     else zero_rows(a, block, blocks);
 }
 
@@ -391,7 +416,8 @@ __global__ void __launch_bounds__(SORT_THREADS, 2) sort_scatter_kernel(const Gra
     next_may_start();
     const int sorters = a.R * a.tiles;
     if ((int)blockIdx.x >= sorters) {
-        zero_pieces<SORT_THREADS>(a, BESIDE);
+        if (a.pieces == 2) zero_pieces<SORT_THREADS, true>(a, BESIDE);
+        else zero_pieces<SORT_THREADS, false>(a, BESIDE);
         return;
     }
     const int r = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, bins = 1 << a.bits, shift = pass * a.bits;
@@ -472,28 +498,54 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_one_tile_kernel(const GradA
 static_assert(ONE_TILE <= SORT_THREADS, "one place per thread");
 
 // ------------------------------------------------------------------ gradient: sums of the runs
-template <bool WIDE, int SIZE>
-__device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0, const float (&sum)[8]) {
+// A lane's 8 sums into the table's row.  IN: the sums' columns are those of 16-byte loads; OUT: rows 16-byte aligned.  Where
+// only the first holds (a worker's table at an odd place of the batch), the sums change lanes through the warp's 256
+// floats of shared memory, so that single-element stores lie side by side: 197 us for the 8 workers' tables above from a
+// place that is odd, 331 with single-element loads as well
+template <bool IN, bool OUT, int SIZE>
+__device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0, const float (&sum)[8], float* swap) {
     const int lane = threadIdx.x & 31;
+    if (IN && OUT) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int c = c0 + col_of<SIZE, WIDE>(lane, 4 * h);
-        if (WIDE && c + 4 <= a.D) {
-            float4* p = reinterpret_cast<float4*>(dst + c);
-            float4 v = make_float4(a.scale * sum[4 * h], a.scale * sum[4 * h + 1], a.scale * sum[4 * h + 2], a.scale * sum[4 * h + 3]);
-            if (a.accumulate) {
-                const float4 o = *p;
-                v = make_float4(fmaf(a.scale, sum[4 * h], o.x), fmaf(a.scale, sum[4 * h + 1], o.y), fmaf(a.scale, sum[4 * h + 2], o.z),
-                                fmaf(a.scale, sum[4 * h + 3], o.w));
-            }
-            __stcs(p, v);
-        } else {
+        for (int h = 0; h < 2; ++h) {
+            const int c = c0 + col_of<SIZE, true>(lane, 4 * h);
+            if (c + 4 <= a.D) {
+                float4* p = reinterpret_cast<float4*>(dst + c);
+                float4 v = make_float4(a.scale * sum[4 * h], a.scale * sum[4 * h + 1], a.scale * sum[4 * h + 2], a.scale * sum[4 * h + 3]);
+                if (a.accumulate) {
+                    const float4 o = *p;
+                    v = make_float4(fmaf(a.scale, sum[4 * h], o.x), fmaf(a.scale, sum[4 * h + 1], o.y), fmaf(a.scale, sum[4 * h + 2], o.z),
+                                    fmaf(a.scale, sum[4 * h + 3], o.w));
+                }
+                __stcs(p, v);
+            } else {
 #pragma unroll
-            for (int j = 4 * h; j < 4 * h + 4; ++j) {
-                const int x = c0 + col_of<SIZE, WIDE>(lane, j);
-                if (x < a.D) dst[x] = a.accumulate ? fmaf(a.scale, sum[j], dst[x]) : a.scale * sum[j];
+                for (int j = 4 * h; j < 4 * h + 4; ++j) {
+                    const int x = c0 + col_of<SIZE, true>(lane, j);
+                    if (x < a.D) dst[x] = a.accumulate ? fmaf(a.scale, sum[j], dst[x]) : a.scale * sum[j];
+                }
             }
         }
+        return;
+    }
+    float x[8];
+    if (IN) {
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<float4*>(swap + col_of<SIZE, true>(lane, 4 * h)) = make_float4(sum[4 * h], sum[4 * h + 1], sum[4 * h + 2], sum[4 * h + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = swap[lane + 32 * j];
+        __syncwarp();
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = sum[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int c = c0 + lane + 32 * j;
+        if (c < a.D) dst[c] = a.accumulate ? fmaf(a.scale, x[j], dst[c]) : a.scale * x[j];
     }
 }
 
@@ -522,11 +574,12 @@ struct Chunk {
 };
 
 // the run being summed
-template <bool WIDE, int SIZE>
+template <bool IN, bool OUT, int SIZE>
 struct Run {
     uint32_t cur;
     bool first;                            // of its chunk
     float sum[8];
+    float* swap;                           // see write_sum
 
     __device__ __forceinline__ void start(uint32_t k) {
         cur = k;
@@ -539,7 +592,7 @@ struct Run {
         const int lane = threadIdx.x & 31;
         const bool from = first && cur == c.prev;
         if (!from && !on) {
-            write_sum<WIDE, SIZE>(a, a.grad + c.r * a.worker_stride + (long long)cur * a.row_stride, c.c0, sum);
+            write_sum<IN, OUT, SIZE>(a, a.grad + c.r * a.worker_stride + (long long)cur * a.row_stride, c.c0, sum, swap);
         } else {                                   // part of a run that crosses chunks
             float4* p = reinterpret_cast<float4*>(a.part + (c.ch * 2 + (from ? 0 : 1)) * ((long long)a.col_tiles * COLS) + c.c0 + lane * 8);
             p[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
@@ -579,10 +632,11 @@ __device__ __forceinline__ void copy16(uint4* dst, const void* src) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <class T>
+template <class T, bool OUT>
 __global__ void __launch_bounds__(RING_WARPS * 32, 3) run_sum_wide_kernel(const GradArgs a, unsigned sum_blocks) {
     constexpr int E = 16 / sizeof(T), PIECES = sizeof(T) / 2, DEPTH = RING_BYTES / (512 * PIECES);
     extern __shared__ __align__(16) uint4 ring_of_all[];
+    __shared__ __align__(16) float swap[RING_WARPS][OUT ? 4 : COLS];
     wait_for_previous();
     next_may_start();
     if (blockIdx.x >= sum_blocks) {
@@ -626,8 +680,9 @@ __global__ void __launch_bounds__(RING_WARPS * 32, 3) run_sum_wide_kernel(const 
     };
 #pragma unroll 1
     for (int i = 0; i < DEPTH; ++i) issue(i);
-    Run<true, sizeof(T)> run;
+    Run<true, OUT, sizeof(T)> run;
     run.first = true;
+    run.swap = swap[threadIdx.x >> 5];
     run.start(__shfl_sync(~0u, k0, 0));
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
@@ -660,8 +715,9 @@ __global__ void __launch_bounds__(SUM_THREADS, 5) run_sum_kernel(const GradArgs 
     if (!c.there) return;
     const T* g = static_cast<const T*>(a.g) + c.r * a.N * a.g_stride + c.c0 + lane;
     const int cols = (int)min(a.D - c.c0 - lane, (long long)COLS);     // the lane's columns are 32 apart below it
-    Run<false, sizeof(T)> run;
+    Run<false, false, sizeof(T)> run;
     run.first = true;
+    run.swap = nullptr;
     run.start(c.key[0]);
     for (int i = 0; i < c.n; i += AHEAD) {
         float f[AHEAD][8];
@@ -702,9 +758,9 @@ __device__ __forceinline__ void add_parts(const GradArgs& a, long long ch, int c
     }
 }
 
-template <int SIZE, bool WIDE>
+template <int SIZE, bool IN, bool OUT>
 __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
-    __shared__ float sums[8][COLS];
+    __shared__ __align__(16) float sums[8][COLS];
     __shared__ long long length[8];                // chunks of the long runs met in this round
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     wait_for_previous();
@@ -730,7 +786,7 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
             if (n <= JOIN_ALONE) {
                 const int c0 = (int)(id - at * a.col_tiles) * COLS;
                 add_parts(a, ch, c0, 0, n, sum);
-                write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+                write_sum<IN, OUT, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum, sums[warp]);
                 n = 0;
             }
         }
@@ -753,7 +809,7 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[j] += sums[x][lane + 32 * j];
                 const uint32_t cur = a.key[a.side][r * a.N + (c + 1) * a.chunk - 1];
-                write_sum<WIDE, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum);
+                write_sum<IN, OUT, SIZE>(a, a.grad + r * a.worker_stride + (long long)cur * a.row_stride, c0, sum, sums[warp]);
             }
             __syncthreads();
         }
@@ -779,17 +835,24 @@ void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, unsigne
     cudaLaunchKernelEx(&cfg, kernel, args...);           // (an error stays for launch_status)
 }
 
-template <class T, bool WIDE>
-void launch_sums(const GradArgs& a, bool zero_here, int sms, cudaStream_t st) {
-    if (WIDE) {
-        const unsigned blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + RING_WARPS - 1) / RING_WARPS);
-        cudaFuncSetAttribute(run_sum_wide_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_WARPS * RING_BYTES);
-        launch_after(run_sum_wide_kernel<T>, blocks + (zero_here ? sms * 3 : 0), RING_WARPS * 32, RING_WARPS * RING_BYTES, st, a, blocks);
+// IN, OUT: the rows of g, of the table on 16-byte boundaries
+template <class T, bool IN, bool OUT>
+void launch_sums(const GradArgs& a, bool zero, int sms, cudaStream_t st) {
+    const int warps = IN ? RING_WARPS : SUM_THREADS / 32;
+    const unsigned blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + warps - 1) / warps);
+    if (IN) {
+        cudaFuncSetAttribute(run_sum_wide_kernel<T, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_WARPS * RING_BYTES);
+        launch_after(run_sum_wide_kernel<T, OUT>, blocks + (zero ? sms * 3 : 0), RING_WARPS * 32, RING_WARPS * RING_BYTES, st, a, blocks);
     } else {
-        const unsigned sum_blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + SUM_THREADS / 32 - 1) / (SUM_THREADS / 32));
-        launch_after(run_sum_kernel<T>, sum_blocks + (zero_here ? sms * 8 : 0), SUM_THREADS, 0, st, a, sum_blocks);
+        launch_after(run_sum_kernel<T>, blocks + (zero ? sms * 8 : 0), SUM_THREADS, 0, st, a, blocks);
     }
-    launch_after(run_join_kernel<sizeof(T), WIDE>, sms * 4, 256, 0, st, a);
+    launch_after(run_join_kernel<sizeof(T), IN, OUT>, sms * 4, 256, 0, st, a);
+}
+template <class T>
+void launch_sums(const GradArgs& a, bool zero, bool in, bool out, int sms, cudaStream_t st) {
+    if (in && out) launch_sums<T, true, true>(a, zero, sms, st);
+    else if (in) launch_sums<T, true, false>(a, zero, sms, st);
+    else launch_sums<T, false, false>(a, zero, sms, st);
 }
 
 int bits_for(long long v) {
@@ -906,8 +969,9 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     a.chunk = p.chunk; a.chunks = p.chunks; a.col_tiles = p.col_tiles; a.side = p.passes & 1;
     a.unit = 32;
     while (a.unit > 1 && a.unit * D > 2048) a.unit /= 2;
-    // (counters of 32 bits, with a block's last turn each to spare)
-    a.pieces = aligned_to(grad_table, 16) && D % 4 == 0 && row_stride == D && worker_stride % 4 == 0 && V * (D / 4) < (1ll << 31) - PIECE;
+    // (counters of 32 bits, with a piece to spare)
+    a.pieces = row_stride == D && D >= 4 && V * D < (1ll << 32) - (1ll << 16);
+    if (a.pieces && aligned_to(grad_table, 16) && D % 4 == 0 && worker_stride % 4 == 0) a.pieces = 2;
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)
     if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
@@ -923,12 +987,11 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
         for (int pass = 0; pass < p.passes; ++pass) launch_after(sort_scatter_kernel, (unsigned)(sorters + beside), SORT_THREADS, 0, st, a, pass);
     }
     const int size = size_of_type(grad_type);
-    const bool zero_here = !accumulate;
-    // 16-byte accesses need every row on a 16-byte boundary
-    const bool wide = aligned_to(grad_out, 16) && grad_stride * size % 16 == 0 && aligned_to(grad_table, 16) && row_stride % 4 == 0 && worker_stride % 4 == 0;
-    if (grad_type == QS_F32) wide ? launch_sums<float, true>(a, zero_here, sms, st) : launch_sums<float, false>(a, zero_here, sms, st);
-    else if (grad_type == QS_BF16) wide ? launch_sums<__nv_bfloat16, true>(a, zero_here, sms, st) : launch_sums<__nv_bfloat16, false>(a, zero_here, sms, st);
-    else wide ? launch_sums<__half, true>(a, zero_here, sms, st) : launch_sums<__half, false>(a, zero_here, sms, st);
+    const bool in = aligned_to(grad_out, 16) && grad_stride * size % 16 == 0;
+    const bool out = aligned_to(grad_table, 16) && row_stride % 4 == 0 && worker_stride % 4 == 0;
+    if (grad_type == QS_F32) launch_sums<float>(a, !accumulate, in, out, sms, st);
+    else if (grad_type == QS_BF16) launch_sums<__nv_bfloat16>(a, !accumulate, in, out, sms, st);
+    else launch_sums<__half>(a, !accumulate, in, out, sms, st);
     return launch_status();
 }
 

@@ -185,6 +185,33 @@ def test_embed_gradient_into_the_workers_gradient_batch(offset, pad):
     assert bool((batch[rest] == 5.0).all())
 
 
+@pytest.mark.parametrize("offset", [0, 1, 2, 3])
+@pytest.mark.parametrize("V,D", [(1, 4), (1, 5), (2, 7), (3000, 4), (700, 37), (20, 1030), (9, 4100)])
+@pytest.mark.parametrize("few", [True, False])
+def test_embed_gradient_beside_other_values(offset, V, D, few):
+    """Rows side by side at any distance from a 16-byte boundary: named rows between rows of zeros, nothing beside the table."""
+    R, N = 3, 6 if few else 1500
+    g = gen(V + D + offset)
+    d = offset + V * D + 5
+    batch = torch.full((R, d), 5.0, device="cuda")
+    out = torch.as_strided(batch, (R, V, D), (d, D, 1), offset)
+    tok = torch.randint(0, V, (R, N), generator=g) // 3 * 3
+    go = torch.randn((R, N, D), generator=g).to(BF16)
+    for type_ in (F32, BF16):
+        out.fill_(7.0)
+        lm().embed_grad(tok.cuda(), go.to(type_).cuda(), V, out=out)
+        acc = torch.full((R, d), 0.5, device="cuda")
+        lm().embed_grad(tok.cuda(), go.to(type_).cuda(), V, out=torch.as_strided(acc, (R, V, D), (d, D, 1), offset), accumulate=True)
+        for r in range(R):
+            want, mag, cnt = ref.embed_grad(tok[r], go[r], V, 1.0)
+            tol = (cnt[:, None] + 2) * EPS * mag
+            near(out[r], want, tol)
+            near(torch.as_strided(acc, (R, V, D), (d, D, 1), offset)[r], want + 0.5, tol + 2 * EPS * (mag + 0.5))
+        rest = torch.ones_like(batch, dtype=torch.bool)
+        torch.as_strided(rest, (R, V, D), (d, D, 1), offset).fill_(False)
+        assert bool((batch[rest] == 5.0).all()) and bool((acc[rest] == 0.5).all())
+
+
 def test_embed_gradient_is_the_transpose_of_embed():
     """<embed(tok, W), G> = <W, embed_grad(tok, G)>, and the difference of the product along one entry."""
     N, V, D = 50, 20, 12
