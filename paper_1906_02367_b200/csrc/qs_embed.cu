@@ -240,7 +240,7 @@ __device__ __forceinline__ void warp_zero(float* dst, long long n) {
 // handed out in order (`most` at most to a block), so that the writes go through memory in order and no block is left with
 // more than its share: 7.2 TB/s, where a warp on 8 KB of its own writes 5.9.  Rows that are no whole units (EVEN false)
 // have the units counted from the 16-byte boundary at or before the table, `lead` floats off; one that two rows share is
-// written by elements unless both become zero, as are the table's first and last
+// written by elements unless both become zero
 constexpr int PIECE = 2048;                // 16-byte units
 template <int NT, bool EVEN>
 __device__ void zero_pieces(const GradArgs& a, int most) {
@@ -266,33 +266,43 @@ __device__ void zero_pieces(const GradArgs& a, int most) {
         const uint32_t lead = EVEN ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(table) & 15u) / 4;
         const uint32_t first = ((piece - r * per) * PIECE + threadIdx.x) * STEP;
         float4* units = reinterpret_cast<float4*>(table - lead) + first / STEP;
+        uint32_t zero[U];                              // a bit per element (EVEN: for the unit)
         if (EVEN || (first >= lead && first + STEP * NT * (U - 1) + 4 <= all + lead)) {
             uint32_t row = (first - lead) / D, in = first - lead - row * D;
-            int zero[U];                               // 1: the unit, 2: some of its elements
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (EVEN) zero[u] = first + u * NT < all && !named[row];
                 else {
-                    const bool here = !named[row], next = in + 3 >= D ? !named[row + 1] : here;
-                    zero[u] = here && next ? 1 : here || next ? 2 : 0;
+                    const uint32_t here = in + 3 < D ? 15u : (1u << (D - in)) - 1u;
+                    const uint8_t one = named[row], other = named[here == 15u ? row : row + 1];        // (no branch between the loads)
+                    zero[u] = (one ? 0u : here) | (other ? 0u : 15u ^ here);
                 }
                 row += rows;
                 in += rest;
                 if (in >= D) { in -= D; ++row; }
             }
+        } else if constexpr (!EVEN) {                  // a table's first or last units are among the thread's
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (zero[u] == 1) __stcs(units + u * NT, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
-                if (!EVEN && zero[u] == 2)
-                    for (uint32_t e = 0, f = first - lead + u * STEP * NT; e < 4; ++e)
-                        if (!named[(f + e) / D]) table[f + e] = 0.0f;
+                const uint32_t f = first + u * STEP * NT, off = f < lead ? lead - f : 0u;          // `off` elements lie before the table
+                zero[u] = 0;
+                if (f >= all + lead) continue;
+                const uint32_t row = (f + off - lead) / D, end = off + D - (f + off - lead - row * D);
+                const uint32_t there = f + 4 <= all + lead ? 15u : (1u << (all + lead - f)) - 1u, here = end < 4 ? (1u << end) - 1u : 15u;
+                zero[u] = named[row] ? 0u : here & there;
+                if ((there & ~here) && !named[row + 1]) zero[u] |= there & ~here;
+                zero[u] &= 15u << off;
             }
-        } else if constexpr (!EVEN) {                  // a table's first or last piece
-            for (int u = 0; u < U; ++u)
-                for (uint32_t e = 0; e < 4; ++e) {
-                    const uint32_t f = first + u * STEP * NT + e;
-                    if (f >= lead && f < all + lead && !named[(f - lead) / D]) table[f - lead] = 0.0f;
-                }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (zero[u] == (EVEN ? 1u : 15u)) __stcs(units + u * NT, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+            else if (!EVEN && zero[u]) {
+                float* p = reinterpret_cast<float*>(units + u * NT);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (zero[u] >> e & 1u) p[e] = 0.0f;
+            }
         }
         if (done == most) return;
     }
@@ -500,7 +510,7 @@ static_assert(ONE_TILE <= SORT_THREADS, "one place per thread");
 // ------------------------------------------------------------------ gradient: sums of the runs
 // A lane's 8 sums into the table's row.  IN: the sums' columns are those of 16-byte loads; OUT: rows 16-byte aligned.  Where
 // only the first holds (a worker's table at an odd place of the batch), the sums change lanes through the warp's 256
-// floats of shared memory, so that single-element stores lie side by side: 197 us for the 8 workers' tables above from a
+// floats of shared memory, so that single-element stores lie side by side: 208 us for the 8 workers' tables above from a
 // place that is odd, 331 with single-element loads as well
 template <bool IN, bool OUT, int SIZE>
 __device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0, const float (&sum)[8], float* swap) {
@@ -972,6 +982,9 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     // (counters of 32 bits, with a piece to spare)
     a.pieces = row_stride == D && D >= 4 && V * D < (1ll << 32) - (1ll << 16);
     if (a.pieces && aligned_to(grad_table, 16) && D % 4 == 0 && worker_stride % 4 == 0) a.pieces = 2;
+    // (without whole units, where there is no longer sort to be beside, the pieces' start costs more than their order gains below
+    // 128 MB: 509 tokens, fp32, 8191 x 257: 14.3 us in pieces, 13.1 by rows; 100000 x 2049: 130 and 148)
+    else if (a.pieces && p.one_tile && R * V * D < 1ll << 25) a.pieces = 0;
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)
     if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
