@@ -63,6 +63,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _word(status):
+    """Address of the status word: four bytes that the device writes."""
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.numel() == 0:
+        raise ValueError(f"status must be one element of torch.int32, not {status.numel()} of {status.dtype}")
+    return status.data_ptr()
+
+
 def _done(rc, what):
     if rc < 0:
         raise QsError(rc, what + (": arguments refused" if rc == -1 else " failed"))
@@ -125,7 +134,7 @@ def embed(tokens, table, scale=1.0, dtype=None, out=None, status=None, stream=No
             raise ValueError(f"out must be {shape}" + (f" of {dtype}" if dtype else ""))
         step = _rows(out, "out") if len(shape) > 1 else D
     _done(lib().qs_embed(R, N, V, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), table.data_ptr(), _type(table, "table"), ws, rs,
-                         scale, out.data_ptr(), _type(out, "out"), step, _ptr(status), _handle(stream, device)), "qs_embed")
+                         scale, out.data_ptr(), _type(out, "out"), step, _word(status), _handle(stream, device)), "qs_embed")
     return out
 
 
@@ -165,7 +174,7 @@ def embed_grad(tokens, grad_out, vocab, scale=1.0, workers=None, accumulate=Fals
     _, _, ws, rs = _table(out, R, "out")
     _done(L.qs_embed_grad(R, N, vocab, D, tokens.data_ptr(), _type(tokens, "tokens", _ID), grad_out.data_ptr(),
                           _type(grad_out, "grad_out"), _rows(grad_out, "grad_out"), scale, int(accumulate), out.data_ptr(), ws, rs,
-                          work.data_ptr(), need, _ptr(status), _handle(stream, device)), "qs_embed_grad")
+                          work.data_ptr(), need, _word(status), _handle(stream, device)), "qs_embed_grad")
     return out
 
 
@@ -196,7 +205,7 @@ def token_logp(logits, tokens=None, scale=1.0, top=0, status=None, stream=None):
         ids = _allocate(stream, (N, top), id_type, device)
         top_logp = _allocate(stream, (N, top), f32, device)
     _done(lib().qs_token_logp(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens), _ID[id_type], scale, top,
-                              _ptr(logp), lse.data_ptr(), entropy.data_ptr(), _ptr(ids), _ptr(top_logp), _ptr(status),
+                              _ptr(logp), lse.data_ptr(), entropy.data_ptr(), _ptr(ids), _ptr(top_logp), _word(status),
                               _handle(stream, device)), "qs_token_logp")
     return TokenLogp(logp, lse, entropy, ids, top_logp)
 
@@ -234,7 +243,7 @@ def token_logp_grad(logits, tokens, lse, grad_logp=1.0, scale=1.0, entropy=None,
         out = _allocate(stream, (N, V), logits.dtype, device)
     _done(lib().qs_token_logp_grad(N, V, logits.data_ptr(), _type(logits, "logits"), step, _ptr(tokens),
                                    _type(tokens, "tokens", _ID) if tokens is not None else QS_I64, scale, lse.data_ptr(), _ptr(entropy), g, g_all,
-                                   _ptr(grad_entropy), out.data_ptr(), _gradient(logits, out), _ptr(status), _handle(stream, device)),
+                                   _ptr(grad_entropy), out.data_ptr(), _gradient(logits, out), _word(status), _handle(stream, device)),
           "qs_token_logp_grad")
     return out
 
@@ -269,7 +278,7 @@ def distill(logits, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False, weig
         out = _allocate(stream, (N, V), logits.dtype, device)
     _done(lib().qs_distill(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
                            teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), loss.data_ptr(), lse.data_ptr(),
-                           _ptr(log_tail), w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _ptr(status),
+                           _ptr(log_tail), w, w_all, _ptr(out), _gradient(logits, out) if out is not None else 0, _word(status),
                            _handle(stream, device)), "qs_distill")
     return Distill(loss, lse, log_tail, out)
 
@@ -291,6 +300,6 @@ def distill_grad(logits, ids, teacher, lse, weight, scale=1.0, teacher_scale=1.0
         out = _allocate(stream, (N, V), logits.dtype, device)
     _done(lib().qs_distill_grad(N, V, K, logits.data_ptr(), _type(logits, "logits"), step, ids.data_ptr(), _type(ids, "ids", _ID),
                                 teacher.data_ptr(), _type(teacher, "teacher"), scale, teacher_scale, int(tail), lse.data_ptr(), _ptr(log_tail),
-                                w, w_all, out.data_ptr(), _gradient(logits, out), _ptr(status), _handle(stream, device)),
+                                w, w_all, out.data_ptr(), _gradient(logits, out), _word(status), _handle(stream, device)),
           "qs_distill_grad")
     return out

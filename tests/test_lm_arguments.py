@@ -1,0 +1,52 @@
+"""What the language-model operators' torch functions hand to the library, checked on the host with a stand-in for it:
+pointers, strides and sizes, and what is refused before anything is enqueued."""
+import pytest
+import torch
+
+from paper_1906_02367_b200 import lm
+
+
+class Recorder:
+    """Takes the place of the library: keeps the arguments of every call and reports success."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 4096 if name == "qs_embed_grad_bytes" else 0
+        return call
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(lm, "lib", lambda: rec)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(lm, "_allocate", lambda stream, shape, dtype, device: torch.zeros(shape, dtype=dtype))
+    monkeypatch.setattr(lm, "_handle", lambda stream, device: 0)
+    return rec.calls
+
+
+def operators(status):
+    """Every function that takes a status word."""
+    tok, table, z, u = torch.zeros(4, dtype=torch.int64), torch.zeros(10, 8), torch.zeros(4, 10), torch.zeros(4, 2)
+    ids, lse = torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4)
+    return [lambda: lm.embed(tok, table, status=status), lambda: lm.embed_grad(tok, torch.zeros(4, 8), 10, status=status),
+            lambda: lm.token_logp(z, tok, status=status), lambda: lm.token_logp_grad(z, tok, lse, status=status),
+            lambda: lm.distill(z, ids, u, status=status), lambda: lm.distill_grad(z, ids, u, lse, 1.0, status=status)]
+
+
+@pytest.mark.parametrize("status", [torch.zeros(1, dtype=torch.int8), torch.zeros(1, dtype=torch.int64), torch.zeros(0, dtype=torch.int32),
+                                    torch.zeros(1, dtype=torch.float32)])
+def test_a_status_word_is_one_int32(calls, status):
+    """The device writes four bytes there: anything else would be written past its end, or read back as another number."""
+    for call in operators(status):
+        del calls[:]
+        with pytest.raises(ValueError):
+            call()
+        assert all(name == "qs_embed_grad_bytes" for name, _ in calls)
+    for call in operators(torch.zeros(1, dtype=torch.int32)) + operators(torch.zeros((), dtype=torch.int32)):
+        call()
