@@ -169,6 +169,8 @@ def embed_grad(tokens, grad_out, vocab, scale=1.0, workers=None, accumulate=Fals
         need = L.qs_embed_grad_bytes(R, N, vocab, D)
         _done(need, "qs_embed_grad_bytes")
         work = _allocate(stream, need, torch.uint8, device)
+    elif not work.is_contiguous():
+        raise ValueError("work must be contiguous")
     else:
         need = work.numel() * work.element_size()
     _, _, ws, rs = _table(out, R, "out")

@@ -50,3 +50,17 @@ def test_a_status_word_is_one_int32(calls, status):
         assert all(name == "qs_embed_grad_bytes" for name, _ in calls)
     for call in operators(torch.zeros(1, dtype=torch.int32)) + operators(torch.zeros((), dtype=torch.int32)):
         call()
+
+
+def test_a_workspace_is_one_stretch_of_memory(calls):
+    """Its size is counted from its elements, so they have to lie side by side: every other byte of a buffer would be
+    taken for all of it."""
+    tok, go = torch.zeros(4, dtype=torch.int64), torch.zeros(4, 8)
+    buf = torch.zeros(8192, dtype=torch.uint8)
+    for work in (buf[::2], torch.zeros(1, dtype=torch.uint8).expand(8192), torch.zeros(64, 64).t()):
+        with pytest.raises(ValueError):
+            lm.embed_grad(tok, go, 10, work=work)
+    assert not calls
+    lm.embed_grad(tok, go, 10, work=buf)
+    lm.embed_grad(tok, go, 10, work=torch.zeros(64, 32))
+    assert [c[1][15] for c in calls] == [8192, 8192]
