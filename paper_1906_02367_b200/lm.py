@@ -80,14 +80,15 @@ def _done(rc, what):
 def _rows(t, what):
     """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one."""
     shape, stride = t.shape, t.stride()
-    if t.numel() == 0 and len(shape) >= 2:
+    if t.numel() == 0:
         return shape[-1]
-    if len(shape) < 2 or (stride[-1] != 1 and shape[-1] > 1):
+    if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{what} needs rows with unit stride")
-    for i in range(len(shape) - 3, -1, -1):
-        if shape[i] > 1 and stride[i] != stride[i + 1] * shape[i + 1]:
+    outer = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n > 1]       # (a dimension of one element has no stride)
+    for (_, s), (n, inner) in zip(outer, outer[1:]):
+        if s != inner * n:
             raise ValueError(f"{what}: leading dimensions must flatten into rows of one stride")
-    return stride[-2] if shape[-2] > 1 or len(shape) > 2 else max(stride[-2], shape[-1])
+    return outer[-1][1] if outer else (shape[-1] + 15) // 16 * 16            # (a single row: none is used; one that keeps wide accesses)
 
 
 def _vector(t, n, what, dtype=torch.float32):

@@ -64,3 +64,35 @@ def test_a_workspace_is_one_stretch_of_memory(calls):
     lm.embed_grad(tok, go, 10, work=buf)
     lm.embed_grad(tok, go, 10, work=torch.zeros(64, 32))
     assert [c[1][15] for c in calls] == [8192, 8192]
+
+
+def strides_of(calls, name):
+    """(table's worker and row stride, out's row stride) of qs_embed; grad_out's row stride of qs_embed_grad."""
+    args = [a for n, a in calls if n == name][-1]
+    return (args[8], args[9], args[13]) if name == "qs_embed" else args[8]
+
+
+def test_dimensions_of_one_element_have_no_stride(calls):
+    """The last position of each of several sequences, (B, 1, D) of (B, S, D): rows one sequence apart; and a single row,
+    whatever strides its dimensions of one element carry."""
+    B, S, D = 3, 5, 8
+    hidden, tok, table = torch.zeros(B, S, D), torch.zeros((B, 1), dtype=torch.int64), torch.zeros(10, D)
+    lm.embed(tok, table, out=hidden[:, -1:, :])
+    assert strides_of(calls, "qs_embed") == (0, D, S * D)
+    lm.embed_grad(tok, hidden[:, -1:, :], 10, workers=False)
+    assert strides_of(calls, "qs_embed_grad") == S * D
+    lm.embed(tok, table, out=torch.as_strided(hidden, (B, 1, D), (S * D, 1, 1)))
+    assert strides_of(calls, "qs_embed") == (0, D, S * D)
+    lm.embed(tok[:1], table, out=torch.as_strided(hidden, (1, 1, D), (1, 1, 1)))
+    assert strides_of(calls, "qs_embed")[2] >= D
+    lm.embed_grad(tok[0, 0], hidden[0, 0], 10)           # one token without a dimension
+    assert strides_of(calls, "qs_embed_grad") >= D
+    lm.embed(torch.zeros((2, 1, 4), dtype=torch.int64), table, out=torch.as_strided(hidden, (2, 1, 4, D), (4 * D, 1, D, 1)))
+    assert strides_of(calls, "qs_embed") == (0, D, D)
+    z = torch.as_strided(torch.zeros(64), (1, 10), (1, 1))
+    lm.token_logp(z, torch.zeros(1, dtype=torch.int64))
+    assert calls[-1][1][4] >= 10
+    with pytest.raises(ValueError):                      # every other element
+        lm.embed(tok, table, out=torch.zeros(B, 1, 2 * D)[..., ::2])
+    with pytest.raises(ValueError):                      # rows whose two dimensions do not flatten
+        lm.embed(torch.zeros((2, 2), dtype=torch.int64), table, out=torch.zeros(2, 3, D)[:, :2])
