@@ -1,0 +1,228 @@
+"""Language-model operators at the edges of their types and sizes: rows whose lse has lost its fractions, or passes the
+largest number; NaN and infinities; paths that only long lists and long rows take; calls from several threads.
+Tolerances as in test_gpu_lm.py: EPS is half a unit in the last place of fp32, an exponential is off by 2^-21, a sum of n
+terms by n EPS of their magnitudes."""
+import math
+
+import pytest
+import torch
+
+from tests import lm_reference as ref
+from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, _near_distill, _near_logp_grad, gen, near, sum_tol
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+@pytest.fixture(autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def lm():
+    from paper_1906_02367_b200 import lm as module
+    return module
+
+
+def clip(t, most):
+    return torch.where(torch.isfinite(t), t.abs().clamp_max(most), torch.zeros((), dtype=t.dtype))
+
+
+# ------------------------------------------------------------------ long lists of tokens
+def sums_by_token(tok, go, V, scale):
+    out = torch.zeros((V + 1, go.shape[1]), dtype=torch.float64)
+    mag, cnt = torch.zeros_like(out), torch.zeros(V + 1, dtype=torch.int64)
+    at = torch.where(tok < 0, V, tok).long()
+    out.index_add_(0, at, scale * go.double())
+    mag.index_add_(0, at, abs(scale) * go.double().abs())
+    cnt.index_add_(0, at, torch.ones_like(at))
+    return out[:V], mag[:V], cnt[:V]
+
+
+LONG = [(1, 20000, 700, 2048, "zipf"), (1, 20000, 700, 2048, "runs"), (1, 20001, 90, 2049, "uniform"), (2, 40000, 50, 1030, "runs"), (1, 65537, 1000, 3, "uniform"),
+        (1, 140001, 30000, 5, "zipf"), (1, 140001, 300, 4, "runs"), (1, 600011, 70001, 1, "uniform"), (8, 40000, 5000, 8, "zipf"), (3, 131073, 513, 2, "runs")]
+
+
+@pytest.mark.parametrize("R,N,V,D,kind", LONG)
+@pytest.mark.parametrize("type_", [F32, BF16])
+def test_embed_gradient_of_long_lists(R, N, V, D, kind, type_):
+    """Chunks of 64 places, tiles of several places per thread, more tiles than blocks fit: sizes that short lists do not
+    reach."""
+    g = gen(N + D)
+    if kind == "runs":                           # of lengths that end at every place of a chunk
+        tok = torch.stack([(torch.cumsum((torch.rand(N, generator=g) < 0.03).long(), 0) * 7) % V for _ in range(R)])
+    elif kind == "zipf":
+        tok = torch.clamp((torch.rand((R, N), generator=g) * math.log(V + 1)).exp().long() - 1, 0, V - 1)
+    else:
+        tok = torch.randint(-1, V, (R, N), generator=g)
+    go = torch.randn((R, N, D), generator=g).to(type_)
+    td, gd = tok.cuda(), go.cuda()
+    got = lm().embed_grad(td, gd, V, scale=0.75)
+    assert torch.equal(got, lm().embed_grad(td, gd, V, scale=0.75))
+    base = torch.randn((R, V, D), generator=g)
+    acc = lm().embed_grad(td, gd, V, scale=0.75, accumulate=True, out=base.cuda())
+    for r in range(R):
+        want, mag, cnt = sums_by_token(tok[r], go[r], V, 0.75)
+        tol = (cnt[:, None] + 2) * EPS * mag
+        near(got[r], want, tol)
+        near(acc[r], want + base[r].double(), tol + 2 * EPS * (mag + base[r].abs()))
+        assert torch.equal(acc[r].cpu()[cnt == 0], base[r][cnt == 0])
+
+
+def test_embed_gradient_of_seventeen_million_tokens():
+    N, V = 17_000_001, 1000
+    tok = torch.randint(0, V, (N,), generator=gen(1), dtype=torch.int32)
+    go = torch.randn((N, 1), generator=gen(2))
+    got = lm().embed_grad(tok.cuda(), go.cuda(), V)
+    want, mag, cnt = sums_by_token(tok, go, V, 1.0)
+    near(got, want, (cnt[:, None] + 2) * EPS * mag)
+
+
+def test_embed_gradient_with_a_workspace_of_the_callers():
+    N, V, D = 3000, 500, 40
+    tok, go = torch.randint(0, V, (N,), generator=gen(1)), torch.randn((N, D), generator=gen(2))
+    want = lm().embed_grad(tok.cuda(), go.cuda(), V)
+    work = lm().embed_grad_work(1, N, V, D)
+    work.fill_(255)
+    more = torch.full((work.numel() // 4 + 100,), -1, dtype=torch.int32, device="cuda")
+    for w in (work, work, more):
+        out = torch.full((V, D), 7.0, device="cuda")
+        assert lm().embed_grad(tok.cuda(), go.cuda(), V, out=out, work=w) is out and torch.equal(out, want)
+    assert bool((more[work.numel() // 4:] == -1).all())          # nothing past what is asked for
+
+
+def test_embed_gradient_of_several_tiles_in_a_graph():
+    N, V, D = 5000, 800, 24
+    tok, go = torch.randint(0, V, (N,), generator=gen(1)).cuda(), torch.randn((N, D), generator=gen(2)).cuda()
+    out = torch.empty((V, D), device="cuda")
+    want = lm().embed_grad(tok, go, V)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lm().embed_grad(tok, go, V, out=out)
+    for _ in range(3):
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    tok.fill_(3)                                 # other tokens, the same launches
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, lm().embed_grad(tok, go, V)) and float(out[4:].abs().sum()) == 0.0
+
+
+# ------------------------------------------------------------------ long rows by one block
+@pytest.mark.parametrize("N,V,type_,top", [(900, 256001, F32, 64), (900, 256000, F32, 8), (1100, 256003, BF16, 128), (900, 150001, F16, 20), (890, 140000, BF16, 1)])
+def test_alternatives_of_long_rows_by_one_block(N, V, type_, top):
+    """Rows of more batches than there are stretches, so that a stretch is several batches."""
+    z = torch.empty((N, V), device="cuda").normal_(0.0, 3.0, generator=torch.Generator(device="cuda").manual_seed(V))
+    z[1] = torch.round(z[1])                     # ties everywhere
+    z[2] = torch.linspace(-8, 8, V, device="cuda")
+    z[3] = torch.linspace(8, -8, V, device="cuda")
+    z[4, :] = torch.finfo(type_).min
+    z[4, V - 5:] = 1.0
+    z[5, V // 2: V // 2 + 300] += 40.0           # the largest side by side
+    z[6] = 0.5
+    z = z.to(type_)
+    tok = torch.randint(0, V, (N,), generator=gen(3))
+    r = lm().token_logp(z, tok.cuda(), top=top)
+    rows = torch.tensor([0, 1, 2, 3, 4, 5, 6, N // 2, N - 1])
+    zr = z[rows.cuda()].cpu()
+    logp, lse, ent, ids, tl = ref.token_logp(zr, tok[rows], 1.0, top)
+    s = sum_tol(V)
+    pick = lambda t: t[rows.cuda()]  # noqa: E731
+    assert torch.equal(pick(r.top_ids).cpu(), ids)
+    near(pick(r.top_logp), tl, s + 8 * EPS * clip(tl, INF))
+    near(pick(r.logp), logp, s + 8 * EPS * clip(logp, INF))
+    near(pick(r.lse), lse, s + 4 * EPS * lse.abs())
+    near(pick(r.entropy), ent, s * (4 + 2 * math.log(V + 1)))
+
+
+# ------------------------------------------------------------------ NaN and infinities
+@pytest.mark.parametrize("V", [5, 1000, 40009, 140001])
+@pytest.mark.parametrize("type_", [F32, BF16, F16])
+@pytest.mark.parametrize("tail", [False, True])
+def test_nan_and_infinity_in_the_logits(V, type_, tail):
+    """A NaN or +inf anywhere in a row makes its results NaN and leaves the other rows' alone."""
+    N, K = 5, 3
+    z = (torch.randn((N, V), generator=gen(V)) * 2).to(type_)
+    z[1, V // 2] = NAN
+    z[2, V - 1] = INF
+    z[3] = NEG
+    z[3, 0] = NAN
+    bad = torch.tensor([False, True, True, True, False])
+    ids, u = torch.stack([torch.randperm(V, generator=gen(i))[:K] for i in range(N)]), torch.log_softmax(torch.randn((N, K), generator=gen(2)), 1) - 0.2
+    tok, w = torch.randint(0, V, (N,), generator=gen(3)), torch.ones(N)
+    r = lm().token_logp(z.cuda(), tok.cuda())
+    assert torch.equal(torch.isnan(r.lse.cpu()), bad)
+    for extra in ({}, dict(entropy=r.entropy, grad_entropy=w.cuda())):
+        got = lm().token_logp_grad(z.cuda(), tok.cuda(), r.lse, 1.0, **extra).cpu()
+        assert torch.equal(torch.isnan(got).all(1), bad) and torch.equal(torch.isnan(got).any(1), bad)
+        _near_logp_grad(got[~bad], z[~bad], tok[~bad], 1.0, w[:2], w[:2] if extra else 0 * w[:2])
+    d = lm().distill(z.cuda(), ids.cuda(), u.cuda(), tail=tail, weight=1.0)
+    back = lm().distill_grad(z.cuda(), ids.cuda(), u.cuda(), d.lse, 1.0, tail=tail, log_tail=d.log_tail).cpu()
+    for t in (d.loss.cpu()[:, None], d.lse.cpu()[:, None], d.grad.cpu(), back):
+        assert torch.equal(torch.isnan(t).all(1), bad) and torch.equal(torch.isnan(t).any(1), bad)
+    keep = [i for i in range(N) if not bad[i]]
+    rows = type(d)(d.loss[keep], d.lse[keep], d.log_tail[keep] if tail else None, d.grad[keep])
+    _near_distill(rows, z[keep], ids[keep], u[keep], 1.0, 1.0, tail, w[:2])
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_nan_in_the_teachers_values(tail):
+    N, V, K = 3, 777, 5
+    z, ids = torch.randn((N, V), generator=gen(1)), torch.stack([torch.randperm(V, generator=gen(i))[:K] for i in range(N)])
+    u = torch.log_softmax(torch.randn((N, K), generator=gen(2)), 1) - 0.2
+    u[1, 2] = NAN
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), tail=tail, weight=1.0)
+    back = lm().distill_grad(z.cuda(), ids.cuda(), u.cuda(), got.lse, 1.0, tail=tail, log_tail=got.log_tail).cpu()
+    for t in (got.loss.cpu()[:, None], got.grad.cpu(), back):
+        assert torch.isnan(t).all(1).tolist() == [False, True, False] and torch.isnan(t).any(1).tolist() == [False, True, False]
+    ids[1, 2] = -1                               # a place that names nothing: its value is not looked at
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), tail=tail, weight=1.0)
+    u[1, 2] = 0.0
+    _near_distill(got, z, ids, u, 1.0, 1.0, tail, torch.ones(N))
+
+
+# ------------------------------------------------------------------ types and results
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V,K,type_", [(1000, 8, F32), (33001, 64, BF16)])
+def test_a_teacher_in_fp16(V, K, type_, tail):
+    N = 4
+    z = (torch.randn((N, V), generator=gen(1)) * 2).to(type_)
+    ids = torch.stack([torch.randperm(V, generator=gen(i))[:K] for i in range(N)])
+    u = (torch.log_softmax(torch.randn((N, K), generator=gen(2)), 1) - 0.2).to(F16)
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), tail=tail, weight=1.0)
+    _near_distill(got, z, ids, u, 1.0, 1.0, tail, torch.ones(N))
+    back = lm().distill_grad(z.cuda(), ids.cuda(), u.cuda(), got.lse, 1.0, tail=tail, log_tail=got.log_tail)
+    near(back, got.grad.double().cpu(), 1e-5 + 2 * HALF[type_] * got.grad.double().cpu().abs())
+
+
+def test_results_that_are_not_asked_for():
+    """NULL for any of logp, lse, entropy, loss, log_tail in the C calls: the others are the same."""
+    from paper_1906_02367_b200 import binding as B
+    L, N, V, K = B.lib(), 4, 3001, 3
+    st = torch.cuda.current_stream().cuda_stream
+    z, tok = torch.randn((N, V), generator=gen(1)).cuda(), torch.arange(N).cuda()
+    full = lm().token_logp(z, tok, top=K)
+    for skip in range(3):
+        for top in (0, K):
+            out = [torch.full((N,), 7.0, device="cuda") for _ in range(3)]
+            ids, tl = torch.full((N, K), 7, dtype=torch.int64, device="cuda"), torch.full((N, K), 7.0, device="cuda")
+            ptr = [None if i == skip else t.data_ptr() for i, t in enumerate(out)]
+            assert L.qs_token_logp(N, V, z.data_ptr(), B.QS_F32, V, tok.data_ptr() if skip else None, B.QS_I64, 1.0, top, *ptr,
+                                   ids.data_ptr() if top else None, tl.data_ptr() if top else None, None, st) == 0
+            for i, t in enumerate(out):
+                assert bool((t == 7.0).all()) if i == skip else torch.equal(t, full[i])
+            assert torch.equal(ids, full.top_ids) if top else bool((ids == 7).all())
+    ids, u = torch.randint(0, V, (N, K), generator=gen(2)).cuda(), torch.full((N, K), -2.0).cuda()
+    want = lm().distill(z, ids, u, tail=True, weight=0.5)
+    for skip in range(3):
+        out, grad = [torch.full((N,), 7.0, device="cuda") for _ in range(3)], torch.empty_like(z)
+        ptr = [None if i == skip else t.data_ptr() for i, t in enumerate(out)]
+        assert L.qs_distill(N, V, K, z.data_ptr(), B.QS_F32, V, ids.data_ptr(), B.QS_I64, u.data_ptr(), B.QS_F32, 1.0, 1.0, 1, *ptr, None, 0.5,
+                            grad.data_ptr(), V, None, st) == 0
+        for i, t in enumerate(out):
+            assert bool((t == 7.0).all()) if i == skip else torch.equal(t, want[i])
+        assert torch.equal(grad, want.grad)
