@@ -5,9 +5,9 @@
 // the row and are read one by one, their other places counting as -inf.  A row belongs to one block or to a cluster
 // of blocks, each with a contiguous share of the vectors.
 //
-// Statistics: with y = scale * z, a part of a row is held as (m, s, u): m = max z, s = sum e and
-// u = sum e * d with d = (z - m) * scale * log2(e) and e = 2^d.  Parts join exactly up to rounding; the
-// difference z - m is formed first, so that a row at the type's lowest value loses nothing.
+// Statistics: with y = scale * z, a part of a row is held as (m, s, u): m = max z, s = sum e and u = sum e * d with
+// e = 2^d and d = z c2 - fl(m c2), c2 = scale * log2(e): one multiply-add.  Where m c2 is too large for that, as in a row
+// at the type's lowest value, d = (z - m) c2, so that nothing is lost.  Parts join exactly up to rounding.
 #pragma once
 #include "qs_bulk.cuh"
 #include "qs_lm.cuh"
@@ -276,9 +276,12 @@ __device__ __forceinline__ float shift_of(float m) { return m == neg_inf() ? 0.0
 // ref has fractions enough (a row at a mask of the lowest value), exponents are (z - m) c2 instead.
 constexpr float REF_RANGE = 65536.0f;
 __device__ __forceinline__ bool in_range(float m, float c2) { return fabsf(m * c2) < REF_RANGE; }
-// distance of two references
+// distance of two references: where only one of them is a rounded product, with what its rounding left out (up to 2^-9 at
+// the end of the range)
+__device__ __forceinline__ float left_out(float m, float c2) { return in_range(m, c2) ? fmaf(m, c2, -(m * c2)) : 0.0f; }
 __device__ __forceinline__ float ref_diff(float a, float b, float c2) {
-    return in_range(a, c2) && in_range(b, c2) ? a * c2 - b * c2 : (a - b) * c2;
+    if (in_range(a, c2) && in_range(b, c2)) return a * c2 - b * c2;
+    return (a - b) * c2 - left_out(a, c2) + left_out(b, c2);
 }
 
 // The exponentials of a batch: s += sum e, u += sum e d.  FLOOR: exponents are kept finite, for a batch with places that

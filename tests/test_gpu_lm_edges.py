@@ -29,6 +29,26 @@ def clip(t, most):
     return torch.where(torch.isfinite(t), t.abs().clamp_max(most), torch.zeros((), dtype=t.dtype))
 
 
+# ------------------------------------------------------------------ statistics on both sides of the range of one multiply-add
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("rising", [False, True])
+@pytest.mark.parametrize("N,V", [(2, 5000), (3, 40009), (1, 130001), (900, 3000)])
+def test_rows_on_both_sides_of_the_exponents_range(N, V, rising, sign):
+    """Logits around 65536 ln 2: some blocks', threads' or batches' exponents are relative to a rounded product, others' to
+    the difference."""
+    z = torch.linspace(-1.0, 1.0, V).expand(N, V) + 0.05 * torch.rand((N, V), generator=gen(V))
+    z = (45426.0 + (z if rising else -z)) * sign
+    tok = torch.randint(0, V, (N,), generator=gen(1))
+    logp, lse, ent, ids, tl = ref.token_logp(z, tok, 1.0, 4)
+    r = lm().token_logp(z.cuda(), tok.cuda(), top=4)
+    s = sum_tol(V) + 8 * EPS * math.log(V)
+    near(r.logp, logp, s)
+    near(r.entropy, ent, s * (4 + 2 * math.log(V)))
+    near(r.top_logp, tl, s)
+    d = lm().distill(z.cuda(), tok[:, None].cuda(), torch.zeros(N, 1).cuda(), weight=1.0)
+    near(d.loss, -logp, s + 2 ** -19)
+
+
 # ------------------------------------------------------------------ long lists of tokens
 def sums_by_token(tok, go, V, scale):
     out = torch.zeros((V + 1, go.shape[1]), dtype=torch.float64)
