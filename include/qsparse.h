@@ -442,7 +442,9 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
  * top_ids are of token_type.
  *   A column at -inf has p = 0 and is no alternative: places left over hold id -1 and -inf.  A row
  *   of nothing else has lse = logp = -inf and entropy 0.  A NaN or +inf in a row makes its lse,
- *   logp, entropy and top_logp NaN and its top_ids -1.
+ *   logp, entropy and top_logp NaN and its top_ids -1.  An lse of a row with live columns that
+ *   passes the largest fp32 number (scale above 1, a row at its type's lowest value) is that
+ *   number with its sign; logp and entropy are not taken from it.
  *   A negative token gives logp = 0, one >= V gives NaN.
  * logits: rows row_stride >= V apart.  N, V <= 2^30, else QS_TOO_LARGE.
  */
@@ -480,7 +482,8 @@ int qs_token_logp_grad(int64_t N, int64_t V, const void* logits, int type, int64
  * sum_n weight[n] loss[n] (weight NULL: weight_all for every row) in their type:
  *   weight scale ( p_v (Q + q_T) - [v outside the ids] p_v q_T / p_T - q_v ),   Q = sum q.
  * ids, teacher: N x K, contiguous; an id given twice counts as two entries of one class.
- *   loss, lse, log_tail (log p_T; written when tail != 0), each N or NULL.
+ *   loss, lse, log_tail (log p_T; written when tail != 0), each N or NULL; a loss or log_tail that
+ *   passes the largest fp32 number without a column at -inf is that number with its sign.
  *   A row without entries (tail == 0) has loss 0 and gradient 0; q_k > 0 on a column at -inf gives
  *   loss +inf; a row of logits at -inf has gradient 0.  An id >= V makes the row's loss and
  *   gradient NaN.  grad and its overlap as in qs_token_logp_grad.

@@ -350,8 +350,8 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 5 : 6) token_logp_kernel(co
     }
     if (warp == warps - 1) {
         const Stat v = final_stat(join_parts(part, warps * blocks, c2), c2);
-        const bool empty = v.m == neg_inf() && v.s == 0.0f;
-        const float ls = logf(v.s), lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
+        const bool empty = is_empty(v);
+        const float ls = logf(v.s), lse = lse_of(v, a.scale, ls);
         if (lane == 31) {                          // the thread that holds the token
             if (a.lse) a.lse[n] = lse;
             if (a.entropy) a.entropy[n] = empty ? 0.0f : ls - LN2 * (v.u / v.s);
@@ -552,7 +552,7 @@ struct Slope {
     int thin, empty;
 };
 template <bool TAIL>
-__device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, float lse, float log_tail) {
+__device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, bool empty, float log_tail) {
     Slope s;
     s.w = w;
     s.in = t.bad ? quiet_nan() : t.Q + t.rest;
@@ -560,7 +560,7 @@ __device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, float
     s.log_tail = log_tail;
     s.thin = TAIL && t.rest > 0.0f && log_tail < -60.0f;
     s.out = !TAIL ? s.in : s.thin ? s.in : s.in - (t.rest > 0.0f ? t.rest * ex2(-log_tail * LOG2E) : t.rest);
-    s.empty = lse == neg_inf();
+    s.empty = empty;
     return s;
 }
 
@@ -750,7 +750,8 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         if (KEEP) mbar_wait(&landed, 0);           // once more, before the memory goes to another block
     }
     Stat v{};
-    float log_tail = 0.0f, lse = 0.0f, ls = 0.0f;
+    float log_tail = 0.0f, out_gap = 0.0f, lse = 0.0f, ls = 0.0f;
+    bool empty = false;
     if (warp == 0) {
         v = join_parts(part, warps * blocks, c2);
         if (TAIL) {
@@ -760,18 +761,19 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             const float s = x.s + y.s;
             // log of the share outside: near 1 the difference of two logs would cancel
             const float out_s = final_stat(v, c2).s;
-            const bool none = v.m == neg_inf() && v.s == 0.0f;
-            const float out_m = v.m;
+            const bool none = is_empty(v);
+            out_gap = v.m - m;
             v = final_stat(Stat{m, s, 0.0f}, c2);
-            log_tail = none ? neg_inf() : fmaf(out_m - m, a.scale, logf(out_s) - logf(v.s));
+            log_tail = none ? neg_inf() : fmaf(out_gap, a.scale, logf(out_s) - logf(v.s));
+            if (!none && log_tail == neg_inf()) log_tail = -FLT_MAX;           // as for lse
             if (log_tail > -0.5f) log_tail = -log1pf(y.s / x.s);
         } else {
             v = final_stat(v, c2);
         }
-        const bool empty = v.m == neg_inf() && v.s == 0.0f;
+        empty = is_empty(v);
         ls = logf(v.s);
-        lse = empty ? neg_inf() : fmaf(v.m, a.scale, ls);
-        const Slope s = slope_of<TAIL>(t.w, t, lse, log_tail);
+        lse = lse_of(v, a.scale, ls);
+        const Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
         if (lane == 0) {
             row_m = shift_of(v.m);
             row_by = empty ? 0.0f : 1.0f / v.s;
@@ -784,14 +786,19 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         bool beyond = false;                       // an entry where the student has no mass at all
         for (int k = lane; k < a.K; k += 32) {
             if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
-            const float lp = lse == neg_inf() ? neg_inf() : fmaf(z_at[k] - v.m, a.scale, -ls);
-            beyond |= lp == neg_inf();
-            loss = fmaf(t.q[k], t.logq[k] - lp, loss);
+            const float gap = z_at[k] - v.m, lp = empty ? neg_inf() : fmaf(gap, a.scale, -ls);
+            beyond |= empty || z_at[k] == neg_inf();
+            // (a log p beyond the largest number, of a column that is not masked: its product with q need not be)
+            loss = !empty && lp == neg_inf() && gap > lp ? fmaf(-t.q[k] * a.scale, gap, loss) : fmaf(t.q[k], t.logq[k] - lp, loss);
         }
         loss = warp_sum(loss);
-        // a mean of log p at a mask of the lowest value: only its rounding passes the largest number
-        if (!__any_sync(~0u, beyond) && loss == -neg_inf()) loss = FLT_MAX;
-        if (TAIL && t.rest != 0.0f) loss = fmaf(t.rest, logf(t.rest) - log_tail, loss);
+        // a mean of log p at masks of the lowest value that passes the largest number is that number
+        const bool masked = __any_sync(~0u, beyond);
+        if (!masked && loss == -neg_inf()) loss = FLT_MAX;
+        if (TAIL && t.rest != 0.0f) {
+            loss = log_tail == -FLT_MAX ? fmaf(-t.rest * a.scale, out_gap, loss) : fmaf(t.rest, logf(t.rest) - log_tail, loss);
+            if (!masked && log_tail > neg_inf() && loss == -neg_inf()) loss = FLT_MAX;
+        }
         if (lane == 0) {
             if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
             if (a.lse) a.lse[n] = lse;
@@ -861,7 +868,7 @@ __global__ void __launch_bounds__(MAX_THREADS) distill_grad_kernel(const RowArgs
     for (int k = threadIdx.x; k < a.K; k += nt)
         if (t.id[k] != NO_ID && r.holds((int)t.id[k])) t.z[k] = to_float(r.z[t.id[k]]);
     __syncthreads();                               // the gradient may take the logits' place
-    const Slope s = slope_of<TAIL>(t.w, t, lse, log_tail);
+    const Slope s = slope_of<TAIL>(t.w, t, lse == neg_inf(), log_tail);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const float shift = s.empty ? LOW_EXP : -lse, f = factor(s, 1.0f);
     const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);

@@ -338,6 +338,15 @@ __device__ __forceinline__ Stat final_stat(Stat a, float c2) {
     return Stat{a.m, s, fmaf(-delta, s, a.u * w)};
 }
 
+// whether a row has no live column at all (a NaN is one)
+__device__ __forceinline__ bool is_empty(Stat a) { return a.m == neg_inf() && a.s == 0.0f; }
+// lse = m scale + ls of final statistics.  -inf says that the row is empty: one that merely passes the largest number (a
+// row at the type's lowest value, a scale above 1) is that number
+__device__ __forceinline__ float lse_of(Stat a, float scale, float ls) {
+    const float lse = fmaf(a.m, scale, ls);
+    return is_empty(a) ? neg_inf() : isinf(lse) ? copysignf(FLT_MAX, lse) : lse;
+}
+
 template <class T, int VPT>
 __device__ __forceinline__ float thread_max_of(const uint4 (&q)[VPT]) {
     uint32_t m = max_of_words<T>(q[0]);

@@ -8,10 +8,11 @@ import pytest
 import torch
 
 from tests import lm_reference as ref
-from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, _near_distill, _near_logp_grad, gen, near, sum_tol
+from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, TINY, _near_distill, _near_logp_grad, gen, near, sum_tol
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
+SAVED = 256.0                                    # an lse up to here is taken as it is: off by EPS of it
 
 
 @pytest.fixture(autouse=True)
@@ -27,6 +28,91 @@ def lm():
 
 def clip(t, most):
     return torch.where(torch.isfinite(t), t.abs().clamp_max(most), torch.zeros((), dtype=t.dtype))
+
+
+# ------------------------------------------------------------------ an lse beyond the largest number
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V,type_", [(50, F32), (3001, BF16), (40001, BF16), (140001, F32)])
+def test_rows_at_the_lowest_value_with_a_scale_above_one(V, type_, tail):
+    """scale * lowest is no finite fp32 number, but the row has live columns: every one of them has the share 1 / V."""
+    N, K, scale = 3, 5, 1.25
+    g = gen(V)
+    z = torch.randn((N, V), generator=g)
+    z[0] = torch.finfo(type_).min
+    z[1] = NEG
+    z = z.to(type_)
+    tok = torch.tensor([V // 2, 0, 1])
+    r = lm().token_logp(z.cuda(), tok.cuda(), scale=scale, top=2)
+    assert float(r.lse[0]) == -torch.finfo(F32).max and float(r.lse[1]) == NEG
+    s = sum_tol(V) + 8 * EPS * math.log(V)
+    assert abs(float(r.logp[0]) + math.log(V)) <= s and abs(float(r.entropy[0]) - math.log(V)) <= 4 * s
+    assert r.top_ids[:2].tolist() == [[0, 1], [-1, -1]]
+    ids = torch.arange(K).expand(N, K).contiguous() * (V // K)
+    u = torch.log_softmax(torch.randn((N, K), generator=g), 1) - 0.3
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), scale=scale, tail=tail, weight=2.0)
+    assert float(got.lse[0]) == -torch.finfo(F32).max
+    q, rest = ref.teacher(ids, u, 1.0, tail)
+    want = float((q[0] * (q[0].log() + math.log(V))).sum())
+    if tail:
+        want += float(rest[0] * (rest[0].log() - math.log((V - K) / V)))
+    assert abs(float(got.loss[0]) - want) <= 2 * s + 2 ** -17
+    want, tol = far_distill_grad(z, ids, u, scale, tail, torch.full((N,), 2.0))
+    near(got.grad, want, tol)
+    assert float(got.loss[1]) == INF and bool((got.grad[1] == 0).all())
+
+
+@pytest.mark.parametrize("type_", [F32, BF16])
+@pytest.mark.parametrize("V", [40, 5001])
+def test_losses_at_columns_of_the_lowest_value(V, type_):
+    """log p = scale * lowest is no fp32 number, its product with a small share is; a loss that is none is the largest one,
+    and only a column at -inf makes it infinite."""
+    low, most, scale = torch.finfo(type_).min, torch.finfo(F32).max, 1.25
+    z = torch.full((3, V), low).to(type_)
+    z[:, 0] = 0.0
+    z[2, 7] = NEG
+    ids = torch.tensor([[0, 5], [5, -1], [0, 7]])
+    u = torch.tensor([[0.9, 0.1], [1.0, 1.0], [0.9, 0.1]]).log()
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), scale=scale, weight=1.0)
+    want = -0.1 * scale * low
+    assert abs(float(got.loss[0]) - want) <= 2 ** -20 * want and got.loss[1:].tolist() == [most, INF]
+    assert got.lse.tolist() == [0.0] * 3
+    # the rest of the teacher's mass on columns at the lowest value
+    got = lm().distill(z.cuda(), ids[:, :1].contiguous().cuda(), torch.tensor([[0.9], [1.0], [0.9]]).log().cuda(), scale=scale, tail=True, weight=1.0)
+    assert abs(float(got.loss[0]) - want) <= 2 ** -20 * want and float(got.log_tail[0]) == -most
+    assert float(got.loss[1]) == most and abs(float(got.loss[2]) - want) <= 2 ** -20 * want
+
+
+# ------------------------------------------------------------------ backward calls where lse has lost its fractions
+
+
+
+
+def far_distill_grad(z, ids, u, scale, tail, weight):
+    """The gradient with the share outside the ids taken from the largest logit there: nothing is lost at any size."""
+    lp, lse = ref.log_softmax(z, scale)
+    p = lp.exp()
+    q, rest = ref.teacher(ids, u, 1.0, tail)
+    want, terms = torch.zeros_like(p), torch.zeros_like(p)
+    for i in range(z.shape[0]):
+        if lse[i] == NEG:
+            continue
+        qv, inside = torch.zeros(z.shape[1], dtype=torch.float64), torch.zeros(z.shape[1], dtype=torch.bool)
+        for j in range(ids.shape[1]):
+            if ids[i, j] >= 0:
+                qv[ids[i, j]] += q[i, j]
+                inside[ids[i, j]] = True
+        d, mag = p[i] * q[i].sum() - qv, p[i] * (1 + q[i].sum()) + qv
+        if tail and float(rest[i]) > 0:
+            y = torch.where(inside, torch.full((), NEG, dtype=torch.float64), z[i].double() * scale)
+            share = torch.zeros_like(y)
+            if float(y.max()) > NEG:
+                e = (y - y.max()).exp()
+                share = e / e.sum()
+            d = d + rest[i] * (p[i] - share)
+            mag = mag + share * (rest[i] + 1)
+        want[i], terms[i] = weight[i].double() * scale * d, mag
+    rel = sum_tol(z.shape[1]) + 8 * EPS * (clip(lp, 200.0) + clip(lse, SAVED)[:, None] + clip(u.double(), 200.0).amax(1)[:, None] + 4) + 2 ** -20
+    return want, weight.double().abs()[:, None] * scale * rel * terms * 4 + HALF[z.dtype] * want.abs() + TINY[z.dtype] + 1e-30
 
 
 # ------------------------------------------------------------------ statistics on both sides of the range of one multiply-add
