@@ -545,10 +545,12 @@ struct Entries {
 };
 
 // What turns a row's probabilities into its gradient: outside the ids f p with f = w (Q + q_T - q_T / p_T), or, where
-// p_T is too small for the quotient, w p (Q + q_T) - w q_T exp(log p - log p_T)
+// p_T is too small for the quotient, w p (Q + q_T) - w q_T share with the column's share of p_T.  That share is taken from
+// the statistics of the columns outside: log p - log p_T would be the difference of two large numbers
 struct Slope {
     float w, in, out;                      // weight * scale, Q + q_T, and out = f / w
     float rest, log_tail;
+    float out_m, out_by;                   // largest logit outside the ids; one over the sum relative to it, 0 if there is none
     int thin, empty;
 };
 template <bool TAIL>
@@ -585,6 +587,20 @@ __device__ __noinline__ uint4 thin_vec(const f2* d, const Slope& s, float norm) 
     for (int i = 0; i < P; ++i) {
         const float2 x = parts(d[i]);
         const float a = c == 0.0f ? 0.0f : c * ex2(x.x - sub), b = c == 0.0f ? 0.0f : c * ex2(x.y - sub);
+        g[i] = make_f2(fmaf(f, ex2(x.x), a), fmaf(f, ex2(x.y), b));
+    }
+    return Vec<T>::pack(g);
+}
+// the same from the shares
+template <class T>
+__device__ __noinline__ uint4 share_vec(const uint4& q, const f2* d, const Slope& s, float norm, float c2) {
+    constexpr int P = Vec<T>::E / 2;
+    f2 g[P];
+    const float f = factor(s, norm), c = s.out_by > 0.0f ? -s.w * s.rest * s.out_by : 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const float2 x = parts(d[i]), z = parts(Vec<T>::pair(q, i));
+        const float a = c == 0.0f ? 0.0f : c * ex2((z.x - s.out_m) * c2), b = c == 0.0f ? 0.0f : c * ex2((z.y - s.out_m) * c2);
         g[i] = make_f2(fmaf(f, ex2(x.x), a), fmaf(f, ex2(x.y), b));
     }
     return Vec<T>::pack(g);
@@ -750,7 +766,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         if (KEEP) mbar_wait(&landed, 0);           // once more, before the memory goes to another block
     }
     Stat v{};
-    float log_tail = 0.0f, out_gap = 0.0f, lse = 0.0f, ls = 0.0f;
+    float log_tail = 0.0f, out_m = 0.0f, out_s = 0.0f, out_gap = 0.0f, lse = 0.0f, ls = 0.0f;
     bool empty = false;
     if (warp == 0) {
         v = join_parts(part, warps * blocks, c2);
@@ -760,7 +776,8 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
             const float s = x.s + y.s;
             // log of the share outside: near 1 the difference of two logs would cancel
-            const float out_s = final_stat(v, c2).s;
+            out_s = final_stat(v, c2).s;
+            out_m = v.m;
             const bool none = is_empty(v);
             out_gap = v.m - m;
             v = final_stat(Stat{m, s, 0.0f}, c2);
@@ -773,7 +790,9 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         empty = is_empty(v);
         ls = logf(v.s);
         lse = lse_of(v, a.scale, ls);
-        const Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
+        Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
+        s.out_m = shift_of(out_m);
+        s.out_by = out_s == 0.0f ? 0.0f : 1.0f / out_s;
         if (lane == 0) {
             row_m = shift_of(v.m);
             row_by = empty ? 0.0f : 1.0f / v.s;
@@ -838,7 +857,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
                 const f2 z = Vec<T>::pair(q, i);
                 d[i] = far ? mul2(add2(z, minus), c2s) : fma2(z, c2s, minus);
             }
-            const uint4 g = thin ? thin_vec<T>(d, s, norm) : slope_vec<T>(d, f);
+            const uint4 g = thin ? share_vec<T>(q, d, s, norm, c2) : slope_vec<T>(d, f);
             if (a.wide && whole) __stcs(to + vec, g);
             else store_edge(r, out, vec, g);
         }

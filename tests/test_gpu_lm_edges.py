@@ -82,6 +82,26 @@ def test_losses_at_columns_of_the_lowest_value(V, type_):
     assert float(got.loss[1]) == most and abs(float(got.loss[2]) - want) <= 2 ** -20 * want
 
 
+@pytest.mark.parametrize("type_,value", [(F32, -1e9), (F32, torch.finfo(F32).min), (F32, -300.0), (BF16, -1e9), (F16, -60000.0)])
+@pytest.mark.parametrize("V", [40, 5001, 300007])
+@pytest.mark.parametrize("scale", [1.0, 1.25])
+def test_gradient_outside_ids_that_are_all_live(V, type_, value, scale):
+    """The student's mass outside the ids is next to nothing, at columns masked with a finite value: the teacher's rest of the
+    mass pulls at each of them by its share of that nothing."""
+    z = torch.full((2, V), value).to(type_)
+    z[:, 0] = 0.0
+    z[1, V // 2:] = NEG
+    ids, u = torch.zeros((2, 1), dtype=torch.int64), torch.full((2, 1), math.log(0.9))
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), scale=scale, tail=True, weight=1.0)
+    rest = 1.0 - float(u[0, 0].double().exp())
+    for i, live in enumerate((V - 1, V // 2 - 1)):
+        grad = torch.zeros(V, dtype=torch.float64)
+        grad[1:live + 1] = -rest * scale / live
+        grad[0] = rest * scale
+        # q_T is 1 - q, q off by 2^-21 of it
+        near(got.grad[i], grad, (2 ** -21 / rest + sum_tol(V) + 2 ** -20 + 2 * HALF[type_]) * grad.abs() + TINY[type_])
+
+
 # ------------------------------------------------------------------ backward calls where lse has lost its fractions
 
 
