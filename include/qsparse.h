@@ -460,7 +460,8 @@ int qs_token_logp(int64_t N, int64_t V, const void* logits, int type, int64_t ro
  *   scale * ( g (1[v = t] - p_v) - h p_v (log p_v + entropy) ),   0 where p_v = 0 and v != t.
  *   grad_logp NULL: grad_logp_all for every row.  grad_entropy NULL: none (entropy is not read).
  *   tokens NULL or a negative token: no part from logp; one >= V: a row of NaN.
- *   A row whose lse is -inf gets zeros.
+ *   A row whose lse is -inf gets zeros.  Where |lse| > 256, 32 bits have lost too much of it: the
+ *   row's statistics are taken again from the logits, which are then read twice.
  *   grad: rows grad_stride >= V apart; it may be the logits themselves (same stride), any other
  *   overlap is QS_INVALID_ARG.
  */
@@ -496,7 +497,8 @@ int qs_distill(int64_t N, int64_t V, int K, const void* logits, int type, int64_
 
 /*
  * qs_distill_grad — the same gradient on its own, from the lse (and, for tail != 0, log_tail) that
- * qs_distill gave, for weights that are known only after the loss.
+ * qs_distill gave, for weights that are known only after the loss.  |lse| > 256 as in
+ * qs_token_logp_grad; also rows with log_tail < -60 and q_T > 0 are read twice.
  */
 int qs_distill_grad(int64_t N, int64_t V, int K, const void* logits, int type, int64_t row_stride,
                     const void* ids, int id_type, const void* teacher, int teacher_type,

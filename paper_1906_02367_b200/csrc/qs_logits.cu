@@ -54,6 +54,7 @@ struct RowArgs {
     int wide;                              // the gradient's rows lie like the logits' rows within 16 bytes
     int parts;                             // log2 of the blocks per row
     int per;                               // batches per stretch whose maximum is kept
+    int rows;                              // backward calls: which rows this launch is for
     int* status;
 };
 
@@ -391,73 +392,61 @@ __global__ void __launch_bounds__(MAX_THREADS, TOP ? 5 : 6) token_logp_kernel(co
 }
 
 // One pass over the row: f(q) turns a vector of logits into its gradient.  Four loads in flight; each vector is read and
-// written by one thread, so that the gradient may take the logits' place
-template <class T, class F>
-__device__ __forceinline__ void map_row(const Share<T>& r, T* out, bool wide, F f) {
+// written by one thread, so that the gradient may take the logits' place.  `skip`: this row is not for it (false is
+// returned).  That depends on a number from memory, and the first loads do not wait for it (40000 rows of 1000 fp32: 64 us
+// where they do, 58 so)
+__device__ __forceinline__ uint4 read_now(const uint4* p) {
+    uint4 q;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(p));
+    return q;
+}
+template <class T, bool WIDE, class F>
+__device__ __forceinline__ bool map_row(const Share<T>& r, T* out, bool skip, F f) {
     const int nt = blockDim.x;
     const uint4* p = r.vectors();
+    auto put = [&](int vec, const uint4& g) {
+        if (WIDE) __stcs(reinterpret_cast<uint4*>(out - r.head) + vec, g);
+        else store_whole(out + r.first(vec), g);
+    };
+    int vec = r.w0 + (int)threadIdx.x;
+    uint4 q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (vec + j * nt < r.w1) q[j] = read_now(p + vec + j * nt);
+    if (skip) return false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (vec + j * nt < r.w1) put(vec + j * nt, f(q[j], vec + j * nt));
+    for (vec += 4 * nt; vec + 3 * nt < r.w1; vec += 4 * nt) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = __ldcs(p + vec + j * nt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) put(vec + j * nt, f(q[j], vec + j * nt));
+    }
+    for (; vec < r.w1; vec += nt) put(vec, f(__ldcs(p + vec), vec));
+    if (threadIdx.x == 0 && r.w0 > r.v0) store_edge(r, out, r.v0, f(r.edge(r.v0), r.v0));
+    if ((int)threadIdx.x == nt - 1 && r.w1 < r.v1) store_edge(r, out, r.w1, f(r.edge(r.w1), r.w1));
+    return true;
+}
+template <class T, class F>
+__device__ __forceinline__ bool map_row(const Share<T>& r, T* out, bool wide, bool skip, F f) {
+    return wide ? map_row<T, true>(r, out, skip, f) : map_row<T, false>(r, out, skip, f);
+}
+
+// the same, one vector at a time: rows that are rare
+template <class T, class F>
+__device__ __forceinline__ void map_row_again(const Share<T>& r, T* out, bool wide, F f) {
     uint4* to = reinterpret_cast<uint4*>(out - r.head);
-    if (wide) {
-        int vec = r.w0 + (int)threadIdx.x;
-        for (; vec + 3 * nt < r.w1; vec += 4 * nt) {
-            uint4 q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = __ldcs(p + vec + j * nt);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) __stcs(to + vec + j * nt, f(q[j], vec + j * nt));
-        }
-        for (; vec < r.w1; vec += nt) __stcs(to + vec, f(__ldcs(p + vec), vec));
-        if (threadIdx.x == 0 && r.w0 > r.v0) store_edge(r, out, r.v0, f(r.edge(r.v0), r.v0));
-        if ((int)threadIdx.x == nt - 1 && r.w1 < r.v1) store_edge(r, out, r.w1, f(r.edge(r.w1), r.w1));
-    } else {
-        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt)
-            store_edge(r, out, vec, f(vec >= r.w0 && vec < r.w1 ? __ldcs(p + vec) : r.edge(vec), vec));
+#pragma unroll 1
+    for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += blockDim.x) {
+        const bool whole = vec >= r.w0 && vec < r.w1;
+        const uint4 g = f(whole ? __ldcs(r.vectors() + vec) : r.edge(vec), vec);
+        if (wide && whole) __stcs(to + vec, g);
+        else store_edge(r, out, vec, g);
     }
 }
 
-template <class T, bool ENT>
-__global__ void __launch_bounds__(MAX_THREADS) token_logp_grad_kernel(const RowArgs a) {
-    const long long n = a.row0 + (blockIdx.x >> a.parts);
-    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x & ((1u << a.parts) - 1u)), a.parts);
-    T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
-    const long long t = a.tok.p ? a.tok.at(n) : -1;
-    const float lse = a.in_lse[n];
-    const bool empty = lse == neg_inf();
-    float g = t < 0 ? 0.0f : t >= a.V ? quiet_nan() : a.g1 ? a.g1[n] : a.g_all;
-    float h = ENT ? a.g2[n] : 0.0f, shift = -lse;
-    if (t >= a.V && threadIdx.x == 0) flag_status(a.status, QS_INVALID_ARG);
-    if (empty) {                                   // zeros, unless the token makes the row NaN
-        h = 0.0f;
-        if (t < a.V) g = 0.0f;
-        shift = LOW_EXP;
-    }
-    const float at_one = (g + h * (ENT ? a.in_entropy[n] : 0.0f)) * a.scale;
-    const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);
-    const f2 slope = make_f2(-h * a.scale, -h * a.scale), offset = make_f2(-at_one, -at_one);
-    const int hot = t >= 0 && t < a.V ? (int)((t + r.head) / Vec<T>::E) : -1;
-    const float hot_g = g * a.scale;
-    map_row<T>(r, out, a.wide, [&](const uint4& q, int vec) {
-        f2 d[Vec<T>::E / 2];
-#pragma unroll
-        for (int i = 0; i < Vec<T>::E / 2; ++i) {
-            // log p; p times minus (g + h (log p + entropy))
-            f2 lp = fma2(Vec<T>::pair(q, i), scale, minus);
-            if (ENT) lp = floor2(lp);
-            d[i] = mul2(ex2_2(mul2(lp, l2e)), ENT ? fma2(lp, slope, offset) : offset);
-        }
-        if (vec == hot) {
-            const int e = (int)t + r.head - vec * Vec<T>::E;
-#pragma unroll
-            for (int i = 0; i < Vec<T>::E / 2; ++i) {
-                const float2 p = parts(d[i]);
-                d[i] = make_f2(2 * i == e ? p.x + hot_g : p.x, 2 * i + 1 == e ? p.y + hot_g : p.y);
-            }
-        }
-        return Vec<T>::pack(d);
-    });
-}
-
-// ------------------------------------------------------------------ distillation
+// ------------------------------------------------------------------ gradients from a saved lse
 constexpr uint32_t NO_ID = 0xffffffffu;
 
 struct TeacherShared {
@@ -468,6 +457,189 @@ struct TeacherShared {
     int bad;                               // an id past the last column
 };
 
+// the statistics of the ids that lie in the block's share, by one warp (an id given twice is one column)
+template <class T>
+__device__ __forceinline__ float4 ids_stat(const RowArgs& a, const TeacherShared& t, const Share<T>& r, float c2) {
+    constexpr int PER = QS_MAX_TOP / 32;
+    const int lane = threadIdx.x & 31;
+    float z[PER], m = neg_inf(), s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = lane + 32 * i;
+        z[i] = neg_inf();
+        if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
+        bool first = true;
+        for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
+        if (first) z[i] = t.z[k];
+        m = fmaxf(m, z[i]);
+    }
+    m = warp_max(m);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const float at = shift_of(m);
+        s += ex2(in_range(at, c2) ? fmaf(z[i], c2, -(at * c2)) : (z[i] - at) * c2);
+    }
+    return make_float4(m, warp_sum(s), 0.0f, 0.0f);
+}
+// vectors that an id may name, by their low bits; and those places of a vector dropped
+__device__ __forceinline__ void mark_id(uint32_t* marks, int vec) { atomicOr(&marks[(vec & 8191) >> 5], 1u << (vec & 31)); }
+template <class T>
+__device__ __forceinline__ void drop_ids(uint4& q, int vec, const uint32_t* marks, const TeacherShared& t, int K, int head) {
+    constexpr int E = Vec<T>::E;
+    if (!(marks[(vec & 8191) >> 5] >> (vec & 31) & 1)) return;
+    for (int k = 0; k < K; ++k)
+        if (t.id[k] != NO_ID && ((int)t.id[k] + head) / E == vec) drop<T>(q, ((int)t.id[k] + head) % E);
+}
+
+// An lse of 32 bits is off by half its last place, and so is every p by that factor: 2^-17 at 256, all of it where the log of
+// the sum is lost beside a maximum of -1e9.  Rows beyond that, and rows whose share outside the ids needs the statistics there,
+// take them again, in a cluster that first reads all of the row (the gradient may lie in the logits' place).  A row of
+// more blocks than a cluster holds is left out by the launch that has them (SAVED), and a second launch, of clusters, takes
+// such rows alone (AGAIN): in most calls none.  The clusters cost the other rows up to 1.5 % (4096 rows of 50003: 76.0 us
+// and 76.9), a second launch in place of them some 3 us a call
+constexpr float LSE_RANGE = 256.0f;
+enum { ROWS_ALL = 0, ROWS_SAVED = 1, ROWS_AGAIN = 2 };
+__device__ __forceinline__ bool lse_far(float lse) { return fabsf(lse) > LSE_RANGE && lse != neg_inf(); }
+
+constexpr int AGAIN_BLOCKS = 16;               // of such a row's cluster
+struct Again {
+    float4 part[AGAIN_BLOCKS * MAX_WARPS], in_part[AGAIN_BLOCKS];
+    uint32_t marks[256];
+};
+struct RowStats { Stat all, out; };            // of the row, and (TAIL) of its columns outside the ids
+// All threads of the row's blocks.  TAIL: t.z holds the logits at the share's ids
+template <class T, bool TAIL>
+__device__ __forceinline__ RowStats stats_again(const RowArgs& a, const Share<T>& r, const TeacherShared* t, Again& sh, int rank) {
+    const int nt = blockDim.x, warps = nt >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = 1 << a.parts;
+    const float c2 = a.scale * LOG2E;
+    if (blocks > 1) cluster_arrive();              // the blocks have started: their shared memory may be written
+    if (TAIL) {
+        for (int i = threadIdx.x; i < 256; i += nt) sh.marks[i] = 0;
+        __syncthreads();
+        for (int k = threadIdx.x; k < a.K; k += nt)
+            if (t->id[k] != NO_ID && r.holds((int)t->id[k])) mark_id(sh.marks, ((int)t->id[k] + r.head) / Vec<T>::E);
+        __syncthreads();
+    }
+    Stat st{neg_inf(), 0.0f, 0.0f};
+    float largest = neg_inf();
+    for (int base = r.v0; base < r.v1; base += nt * VPT) {
+        uint4 q[VPT];
+        load_share<T, VPT>(r, base, nt, q);
+        if (TAIL) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+                if (base + j * nt + (int)threadIdx.x < r.v1) drop_ids<T>(q[j], base + j * nt + (int)threadIdx.x, sh.marks, *t, a.K, r.head);
+        }
+        const float most = thread_max_of<T, VPT>(q);
+        take<T, VPT, false, false>(st, q, most, c2);
+        largest = fmaxf(largest, most);
+    }
+    const Stat w = join_warp<false>(st, largest, c2);
+    const float4 sent = make_float4(w.m, w.s, 0.0f, 0.0f), in = TAIL && warp == 0 ? ids_stat<T>(a, *t, r, c2) : sent;
+    if (blocks == 1) {
+        if (lane == 0) {
+            sh.part[warp] = sent;
+            if (TAIL && warp == 0) sh.in_part[0] = in;
+        }
+        __syncthreads();
+    } else {
+        cluster_wait();
+        if (lane < blocks) {
+            remote_store(remote_addr(&sh.part[rank * warps + warp], lane), sent);
+            if (TAIL && warp == 0) remote_store(remote_addr(&sh.in_part[rank], lane), in);
+        }
+        cluster_arrive();
+        cluster_wait();                            // all of the row has been read; nothing is written to another block after this
+    }
+    const Stat v = join_parts(sh.part, warps * blocks, c2);
+    RowStats x{final_stat(v, c2), Stat{}};
+    if (TAIL) {
+        const Stat y = join_parts(sh.in_part, blocks, c2);
+        const float m = fmaxf(v.m, y.m);
+        x.out = x.all;
+        x.all = final_stat(Stat{m, rescale(v, m, c2).s + rescale(y, m, c2).s, 0.0f}, c2);
+    }
+    return x;
+}
+
+// What turns a row's log p into its gradient: p times minus (g + h (log p + entropy)), and g at the token
+template <class T, bool ENT>
+struct LogpSlope {
+    long long t;
+    int hot;                               // the token's vector
+    float hot_g, shift;                    // g scale; minus lse
+    f2 scale, slope, offset;
+
+    __device__ __forceinline__ LogpSlope(const RowArgs& a, const Share<T>& r, long long n, float lse, bool tell) {
+        t = a.tok.p ? a.tok.at(n) : -1;
+        float g = t < 0 ? 0.0f : t >= a.V ? quiet_nan() : a.g1 ? a.g1[n] : a.g_all, h = ENT ? a.g2[n] : 0.0f;
+        shift = -lse;
+        if (t >= a.V && tell) flag_status(a.status, QS_INVALID_ARG);
+        if (lse == neg_inf()) {                    // an empty row: zeros, unless the token makes it NaN
+            h = 0.0f;
+            if (t < a.V) g = 0.0f;
+            shift = LOW_EXP;
+        }
+        const float at_one = (g + h * (ENT ? a.in_entropy[n] : 0.0f)) * a.scale;
+        scale = make_f2(a.scale, a.scale);
+        slope = make_f2(-h * a.scale, -h * a.scale);
+        offset = make_f2(-at_one, -at_one);
+        hot = t >= 0 && t < a.V ? (int)((t + r.head) / Vec<T>::E) : -1;
+        hot_g = g * a.scale;
+    }
+    // log_p: of a pair of logits
+    template <class F>
+    __device__ __forceinline__ uint4 vec_of(const uint4& q, int vec, int head, F log_p) const {
+        const f2 l2e = make_f2(LOG2E, LOG2E);
+        f2 d[Vec<T>::E / 2];
+#pragma unroll
+        for (int i = 0; i < Vec<T>::E / 2; ++i) {
+            f2 lp = log_p(Vec<T>::pair(q, i));
+            if (ENT) lp = floor2(lp);
+            d[i] = mul2(ex2_2(mul2(lp, l2e)), ENT ? fma2(lp, slope, offset) : offset);
+        }
+        if (vec == hot) {
+            const int e = (int)t + head - vec * Vec<T>::E;
+#pragma unroll
+            for (int i = 0; i < Vec<T>::E / 2; ++i) {
+                const float2 p = parts(d[i]);
+                d[i] = make_f2(2 * i == e ? p.x + hot_g : p.x, 2 * i + 1 == e ? p.y + hot_g : p.y);
+            }
+        }
+        return Vec<T>::pack(d);
+    }
+};
+template <class T, bool ENT>
+__device__ __noinline__ void token_logp_grad_again(const RowArgs& a, Again& sh) {
+    const int rank = (int)(blockIdx.x & ((1u << a.parts) - 1u));
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
+    const LogpSlope<T, ENT> s(a, r, n, a.in_lse[n], false);
+    const Stat v = stats_again<T, false>(a, r, nullptr, sh, rank).all;
+    const float m = -shift_of(v.m), ls = -logf(v.s);
+    const f2 mm = make_f2(m, m), mls = make_f2(ls, ls);
+    map_row_again<T>(r, static_cast<T*>(a.grad) + n * a.grad_stride, a.wide, [&](const uint4& q, int vec) {
+        return s.vec_of(q, vec, r.head, [&](f2 z) { return fma2(add2(z, mm), s.scale, mls); });
+    });
+}
+
+// (six blocks of 40 registers an SM; without the bound the path of rows taken again would have 64 for itself and all others)
+template <class T, bool ENT>
+__global__ void __launch_bounds__(MAX_THREADS, 6) token_logp_grad_kernel(const __grid_constant__ RowArgs a) {
+    __shared__ Again sh;
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
+    const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x & ((1u << a.parts) - 1u)), a.parts);
+    const float lse = a.in_lse[n];
+    const LogpSlope<T, ENT> s(a, r, n, lse, threadIdx.x == 0);
+    const f2 minus = make_f2(s.shift, s.shift);
+    if (!map_row<T>(r, static_cast<T*>(a.grad) + n * a.grad_stride, a.wide, lse_far(lse) || a.rows == ROWS_AGAIN, [&](const uint4& q, int vec) {
+            return s.vec_of(q, vec, r.head, [&](f2 z) { return fma2(z, s.scale, minus); });
+        })) {
+        if (lse_far(lse) && a.rows != ROWS_SAVED) token_logp_grad_again<T, ENT>(a, sh);
+    }
+}
+
+// ------------------------------------------------------------------ distillation
 __device__ __forceinline__ float teacher_at(const RowArgs& a, long long i) {
     return a.teacher_type == QS_F32 ? static_cast<const float*>(a.teacher)[i]
          : a.teacher_type == QS_BF16 ? to_float(static_cast<const __nv_bfloat16*>(a.teacher)[i])
@@ -549,9 +721,14 @@ struct Entries {
 // the statistics of the columns outside: log p - log p_T would be the difference of two large numbers
 struct Slope {
     float w, in, out;                      // weight * scale, Q + q_T, and out = f / w
-    float rest, log_tail;
+    float rest;
     float out_m, out_by;                   // largest logit outside the ids; one over the sum relative to it, 0 if there is none
     int thin, empty;
+
+    __device__ __forceinline__ void set_out(float m, float sum) {
+        out_m = shift_of(m);
+        out_by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    }
 };
 template <bool TAIL>
 __device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, bool empty, float log_tail) {
@@ -559,7 +736,7 @@ __device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, bool 
     s.w = w;
     s.in = t.bad ? quiet_nan() : t.Q + t.rest;
     s.rest = t.rest;
-    s.log_tail = log_tail;
+    s.out_m = s.out_by = 0.0f;
     s.thin = TAIL && t.rest > 0.0f && log_tail < -60.0f;
     s.out = !TAIL ? s.in : s.thin ? s.in : s.in - (t.rest > 0.0f ? t.rest * ex2(-log_tail * LOG2E) : t.rest);
     s.empty = empty;
@@ -577,21 +754,7 @@ __device__ __forceinline__ float at_id(const TeacherShared& t, int K, int k, con
 __device__ __forceinline__ float factor(const Slope& s, float norm) {
     return s.empty ? (s.in == s.in ? 0.0f : s.in) : s.w * s.out * norm;
 }
-// rows whose p_T is too small for a quotient: what is left of the gradient, exponents first
-template <class T>
-__device__ __noinline__ uint4 thin_vec(const f2* d, const Slope& s, float norm) {
-    constexpr int P = Vec<T>::E / 2;
-    f2 g[P];
-    const float f = factor(s, norm), sub = s.log_tail * LOG2E - log2f(norm), c = s.log_tail > neg_inf() ? -s.w * s.rest : 0.0f;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const float2 x = parts(d[i]);
-        const float a = c == 0.0f ? 0.0f : c * ex2(x.x - sub), b = c == 0.0f ? 0.0f : c * ex2(x.y - sub);
-        g[i] = make_f2(fmaf(f, ex2(x.x), a), fmaf(f, ex2(x.y), b));
-    }
-    return Vec<T>::pack(g);
-}
-// the same from the shares
+// rows whose p_T is too small for the quotient: the shares instead
 template <class T>
 __device__ __noinline__ uint4 share_vec(const uint4& q, const f2* d, const Slope& s, float norm, float c2) {
     constexpr int P = Vec<T>::E / 2;
@@ -692,7 +855,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         t.z[k] = z;
         if (blocks == 1) z_at[k] = z;
         else send(remote_addr(&z_at[k], 0), z, remote_addr(&met, 0));
-        if (!KEEP && TAIL) atomicOr(&marks[(place / E & 8191) >> 5], 1u << (place / E & 31));
+        if (!KEEP && TAIL) mark_id(marks, place / E);
     }
     if (TAIL) {                                    // these places leave the sum; their own statistics join later
         __syncthreads();                           // (an id given twice is read twice)
@@ -713,9 +876,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
 #pragma unroll
             for (int j = 0; j < VK; ++j) {
                 const int vec = base + j * nt + (int)threadIdx.x;
-                if (vec < r.v1 && marks[(vec & 8191) >> 5] >> (vec & 31) & 1)
-                    for (int k = 0; k < a.K; ++k)
-                        if (t.id[k] != NO_ID && ((int)t.id[k] + r.head) / E == vec) drop<T>(q[j], ((int)t.id[k] + r.head) % E);
+                if (vec < r.v1) drop_ids<T>(q[j], vec, marks, t, a.K, r.head);
             }
         }
         const float most = thread_max_of<T, VK>(q);
@@ -730,25 +891,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         send(remote_addr(&part[rank * warps + warp], lane), sent, remote_addr(&met, lane));
     }
     if (TAIL && warp == 0) {
-        float z[Entries::PER], m = neg_inf(), s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < Entries::PER; ++i) {
-            const int k = lane + 32 * i;
-            z[i] = neg_inf();
-            if (k >= a.K || t.id[k] == NO_ID || !r.holds((int)t.id[k])) continue;
-            bool first = true;                     // an id given twice is one column
-            for (int j = 0; j < k; ++j) first &= t.id[j] != t.id[k];
-            if (first) z[i] = t.z[k];
-            m = fmaxf(m, z[i]);
-        }
-        m = warp_max(m);
-#pragma unroll
-        for (int i = 0; i < Entries::PER; ++i) {
-            const float at = shift_of(m);
-            s += ex2(in_range(at, c2) ? fmaf(z[i], c2, -(at * c2)) : (z[i] - at) * c2);
-        }
-        s = warp_sum(s);
-        const float4 v = make_float4(m, s, 0.0f, 0.0f);
+        const float4 v = ids_stat<T>(a, t, r, c2);
         if (blocks == 1) {
             if (lane == 0) in_part[0] = v;
         } else if (lane < readers) {
@@ -791,8 +934,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         ls = logf(v.s);
         lse = lse_of(v, a.scale, ls);
         Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
-        s.out_m = shift_of(out_m);
-        s.out_by = out_s == 0.0f ? 0.0f : 1.0f / out_s;
+        s.set_out(out_m, out_s);
         if (lane == 0) {
             row_m = shift_of(v.m);
             row_by = empty ? 0.0f : 1.0f / v.s;
@@ -871,9 +1013,34 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
 }
 
 template <class T, bool TAIL>
-__global__ void __launch_bounds__(MAX_THREADS) distill_grad_kernel(const RowArgs a) {
+__device__ __noinline__ void distill_grad_again(const RowArgs& a, const TeacherShared& t, Again& sh) {
+    constexpr int E = Vec<T>::E;
+    const int rank = (int)(blockIdx.x & ((1u << a.parts) - 1u));
+    const long long n = a.row0 + (blockIdx.x >> a.parts);
+    const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
+    T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
+    const RowStats x = stats_again<T, TAIL>(a, r, &t, sh, rank);
+    Slope s = slope_of<TAIL>(t.w, t, is_empty(x.all), TAIL ? a.in_log_tail[n] : 0.0f);
+    if (TAIL) s.set_out(x.out.m, x.out.s);
+    const bool thin = TAIL && s.thin && !s.empty;
+    const float m = shift_of(x.all.m), ls = s.empty ? -LOW_EXP : logf(x.all.s), f = factor(s, 1.0f), c2 = a.scale * LOG2E;
+    const f2 scale = make_f2(a.scale, a.scale), l2e = make_f2(LOG2E, LOG2E), mm = make_f2(-m, -m), mls = make_f2(-ls, -ls);
+    map_row_again<T>(r, out, a.wide, [&](const uint4& q, int) {
+        f2 d[E / 2];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) d[i] = mul2(fma2(add2(Vec<T>::pair(q, i), mm), scale, mls), l2e);
+        return thin ? share_vec<T>(q, d, s, 1.0f, c2) : slope_vec<T>(d, f);
+    });
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.K; k += blockDim.x)
+        if (t.id[k] != NO_ID && r.holds((int)t.id[k])) out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2(fmaf(t.z[k] - m, a.scale, -ls) * LOG2E)));
+}
+
+template <class T, bool TAIL>
+__global__ void __launch_bounds__(MAX_THREADS, 6) distill_grad_kernel(const __grid_constant__ RowArgs a) {
     constexpr int E = Vec<T>::E;
     __shared__ TeacherShared t;
+    __shared__ Again sh;
     const int nt = blockDim.x;
     const long long n = a.row0 + (blockIdx.x >> a.parts);
     const Share<T> r(a.logits, a.stride, n, a.V, (int)(blockIdx.x & ((1u << a.parts) - 1u)), a.parts);
@@ -889,30 +1056,21 @@ __global__ void __launch_bounds__(MAX_THREADS) distill_grad_kernel(const RowArgs
     __syncthreads();                               // the gradient may take the logits' place
     const Slope s = slope_of<TAIL>(t.w, t, lse == neg_inf(), log_tail);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
+    const bool again = lse_far(lse) || (TAIL && s.thin && !s.empty);
     const float shift = s.empty ? LOW_EXP : -lse, f = factor(s, 1.0f);
     const f2 scale = make_f2(a.scale, a.scale), minus = make_f2(shift, shift), l2e = make_f2(LOG2E, LOG2E);
-    auto exponents = [&](const uint4& q, f2* d) {
+    if (!map_row<T>(r, out, a.wide, again || a.rows == ROWS_AGAIN, [&](const uint4& q, int) {
+            f2 d[E / 2];
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) d[i] = mul2(fma2(Vec<T>::pair(q, i), scale, minus), l2e);
-    };
-    if (TAIL && s.thin && !s.empty) {
-#pragma unroll 1
-        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt) {
-            f2 d[E / 2];
-            exponents(vec >= r.w0 && vec < r.w1 ? __ldcs(r.vectors() + vec) : r.edge(vec), d);
-            store_edge(r, out, vec, thin_vec<T>(d, s, 1.0f));
-        }
-    } else {
-        map_row<T>(r, out, a.wide, [&](const uint4& q, int) {
-            f2 d[E / 2];
-            exponents(q, d);
+            for (int i = 0; i < E / 2; ++i) d[i] = mul2(fma2(Vec<T>::pair(q, i), scale, minus), l2e);
             return slope_vec<T>(d, f);
-        });
+        })) {
+        if (again && a.rows != ROWS_SAVED) distill_grad_again<T, TAIL>(a, t, sh);
+        return;
     }
     __syncthreads();
     for (int k = threadIdx.x; k < a.K; k += nt)
-        if (t.id[k] != NO_ID && r.holds((int)t.id[k]))
-            out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2(fmaf(t.z[k], a.scale, -lse) * LOG2E)));
+        if (t.id[k] != NO_ID && r.holds((int)t.id[k])) out[t.id[k]] = from_float<T>(at_id(t, a.K, k, s, ex2(fmaf(t.z[k], a.scale, -lse) * LOG2E)));
 }
 
 // ------------------------------------------------------------------ launches
@@ -968,6 +1126,10 @@ template <class K>
 cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaStream_t st) {
     a.parts = 0;
     while ((1 << a.parts) < s.blocks) ++a.parts;
+    if (cluster && s.blocks > 8) {                 // (more than every GPU has to offer: this one does)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     if (s.smem > 32 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
         if (e != cudaSuccess) return e;
@@ -992,12 +1154,23 @@ cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaS
     return cudaSuccess;
 }
 
-// The backward calls: independent blocks, each with some sixteen vectors per thread of its row, or four where there are few
-// rows
+// The backward calls: blocks with some sixteen vectors per thread of their row, or four where there are few rows
 Shape grad_shape(int64_t N, long long vectors) {
     Shape s{vectors <= 2048 ? 64 : MAX_THREADS, 1, 0, false};
-    while ((long long)s.blocks * s.nt * 16 < vectors || (N * s.blocks < 8 * SMS && (long long)s.blocks * s.nt * 4 < vectors)) s.blocks *= 2;
+    while ((long long)s.blocks * s.nt * 16 < vectors ||
+           (s.blocks < AGAIN_BLOCKS && N * s.blocks < 8 * SMS && (long long)s.blocks * s.nt * 4 < vectors)) s.blocks *= 2;
     return s;
+}
+// a row in a cluster, or in more blocks than one holds: then the rows whose statistics are taken again follow (see LSE_RANGE)
+template <class K>
+cudaError_t launch_grad(K kernel, RowArgs a, long long vectors, cudaStream_t st) {
+    Shape s = grad_shape(a.N, vectors);
+    a.rows = s.blocks <= AGAIN_BLOCKS ? ROWS_ALL : ROWS_SAVED;
+    const cudaError_t e = launch_rows(kernel, s, a, a.rows == ROWS_ALL, st);
+    if (e != cudaSuccess || a.rows == ROWS_ALL) return e;
+    s.blocks = AGAIN_BLOCKS;
+    a.rows = ROWS_AGAIN;
+    return launch_rows(kernel, s, a, true, st);
 }
 
 template <class T>
@@ -1013,8 +1186,7 @@ cudaError_t launch_token_logp(RowArgs a, cudaStream_t st) {
 }
 template <class T>
 cudaError_t launch_token_logp_grad(const RowArgs& a, cudaStream_t st) {
-    const Shape s = grad_shape(a.N, most_vectors(a.V, sizeof(T)));
-    return launch_rows(a.g2 ? token_logp_grad_kernel<T, true> : token_logp_grad_kernel<T, false>, s, a, false, st);
+    return launch_grad(a.g2 ? token_logp_grad_kernel<T, true> : token_logp_grad_kernel<T, false>, a, most_vectors(a.V, sizeof(T)), st);
 }
 template <class T>
 cudaError_t launch_distill(const RowArgs& a, bool tail, cudaStream_t st) {
@@ -1025,8 +1197,7 @@ cudaError_t launch_distill(const RowArgs& a, bool tail, cudaStream_t st) {
 }
 template <class T>
 cudaError_t launch_distill_grad(const RowArgs& a, bool tail, cudaStream_t st) {
-    const Shape s = grad_shape(a.N, most_vectors(a.V, sizeof(T)));
-    return launch_rows(tail ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>, s, a, false, st);
+    return launch_grad(tail ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>, a, most_vectors(a.V, sizeof(T)), st);
 }
 
 int status_of(cudaError_t e) {

@@ -255,6 +255,17 @@ __device__ __noinline__ void store_edge(const Share<T>& r, T* out, int vec, uint
     }
 }
 
+// a whole vector of results where rows do not lie like the logits' rows
+template <class T>
+__device__ __forceinline__ void store_whole(T* out, const uint4& q) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 16 / (int)sizeof(T); ++i) {
+        if (sizeof(T) == 4) reinterpret_cast<uint32_t*>(out)[i] = w[i];
+        else reinterpret_cast<uint16_t*>(out)[i] = (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
+    }
+}
+
 // ------------------------------------------------------------------ statistics
 struct Stat { float m, s, u; };
 

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from tests import lm_reference as ref
-from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, TINY, _near_distill, _near_logp_grad, gen, near, sum_tol
+from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, TINY, _near_distill, _near_logp_grad, gen, near, sum_tol, view
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -61,6 +61,26 @@ def test_rows_at_the_lowest_value_with_a_scale_above_one(V, type_, tail):
     assert float(got.loss[1]) == INF and bool((got.grad[1] == 0).all())
 
 
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V,type_", [(50, F32), (3001, BF16), (40001, BF16), (140001, F32)])
+def test_backward_calls_at_the_lowest_value_with_a_scale_above_one(V, type_, tail):
+    N, K, scale = 3, 5, 1.25
+    g = gen(V)
+    z = torch.randn((N, V), generator=g)
+    z[0] = torch.finfo(type_).min
+    z[1] = NEG
+    z = z.to(type_)
+    tok = torch.tensor([V // 2, 0, 1])
+    ids = torch.arange(K).expand(N, K).contiguous() * (V // K)
+    u = torch.log_softmax(torch.randn((N, K), generator=g), 1) - 0.3
+    want, tol = far_distill_grad(z, ids, u, scale, tail, torch.full((N,), 2.0))
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), scale=scale, tail=tail)
+    near(lm().distill_grad(z.cuda(), ids.cuda(), u.cuda(), got.lse, 2.0, scale=scale, tail=tail, log_tail=got.log_tail), want, tol)
+    r, gl = lm().token_logp(z.cuda(), tok.cuda(), scale=scale), torch.ones(N)
+    want, tol = far_logp_grad(z, tok, scale, gl, gl)
+    near(lm().token_logp_grad(z.cuda(), tok.cuda(), r.lse, 1.0, scale=scale, entropy=r.entropy, grad_entropy=gl.cuda()), want, tol)
+
+
 @pytest.mark.parametrize("type_", [F32, BF16])
 @pytest.mark.parametrize("V", [40, 5001])
 def test_losses_at_columns_of_the_lowest_value(V, type_):
@@ -103,8 +123,66 @@ def test_gradient_outside_ids_that_are_all_live(V, type_, value, scale):
 
 
 # ------------------------------------------------------------------ backward calls where lse has lost its fractions
+FAR = ["masked", "lowest", "high", "low", "flat", "plain", "empty", "one", "thin"]
 
 
+def far_rows(V, type_, g):
+    """A row of each kind; `where` masks are finite: -1e9 (fp16: its lowest value)."""
+    mask = torch.finfo(type_).min if type_ == F16 else -1e9
+    z = torch.randn((len(FAR), V), generator=g) * 2
+    z[0] = mask                                  # everything masked: uniform
+    z[1] = torch.finfo(type_).min
+    z[2] += 9000.0
+    z[3] -= 9000.0
+    z[4] = 3000.0
+    z[6] = NEG
+    z[7] = mask
+    z[7, V // 3] = -5.0                          # one live column
+    z[8] = mask                                  # the first four live
+    z[8, :4] = torch.tensor([1.0, 2.0, 0.5, 0.0])
+    return z.to(type_)
+
+
+def far_logp_grad(z, tok, scale, gl, ge):
+    want = ref.token_logp_grad(z, tok, scale, gl, ge)
+    lp, lse = ref.log_softmax(z, scale)
+    p = lp.exp()
+    l0 = torch.where(p > 0, clip(lp, 1e4), torch.zeros(()).double())
+    ent = (p * l0).sum(1, keepdim=True)
+    rel = sum_tol(z.shape[1]) + 8 * EPS * (l0 + clip(lse, SAVED)[:, None] + 1)
+    terms = scale * p * (gl.double().abs()[:, None] + ge.double().abs()[:, None] * (l0 + ent + 1))
+    hot = torch.zeros_like(p)
+    for i, t in enumerate(tok.tolist()):
+        if t >= 0:
+            hot[i, t] = abs(float(gl[i])) * scale
+    return want, rel * terms * 4 + 4 * EPS * hot + HALF[z.dtype] * want.abs() + TINY[z.dtype] + 1e-30
+
+
+FAR_SIZES = [(37, F32), (3001, BF16), (5003, F16), (50003, BF16), (140001, F32), (300007, BF16), (270011, F32)]
+
+
+@pytest.mark.parametrize("V,type_", FAR_SIZES)
+@pytest.mark.parametrize("entropy", [False, True])
+def test_token_logp_gradient_where_lse_is_large(V, type_, entropy):
+    g = gen(V)
+    z = far_rows(V, type_, g)
+    N, scale = z.shape[0], 1.0
+    tok = torch.randint(0, V, (N,), generator=g)
+    tok[7] = V // 3
+    gl, ge = torch.randn(N, generator=g), torch.randn(N, generator=g) if entropy else torch.zeros(N)
+    zd, _ = view(z, 3, 1)
+    r = lm().token_logp(zd, tok.cuda(), scale=scale)
+    extra = dict(entropy=r.entropy, grad_entropy=ge.cuda()) if entropy else {}
+    want, tol = far_logp_grad(z, tok, scale, gl, ge)
+    got = lm().token_logp_grad(zd, tok.cuda(), r.lse, gl.cuda(), scale=scale, **extra)
+    near(got, want, tol)
+    near(lm().token_logp_grad(zd, tok.cuda(), r.lse, gl.cuda(), scale=scale, out=zd, **extra), want, tol)     # in place
+    # one row at a time: as many blocks as a row takes
+    for i in (0, 8):
+        zi = z[i:i + 1].cuda()
+        one = lm().token_logp_grad(zi, tok[i:i + 1].cuda(), r.lse[i:i + 1], gl[i:i + 1].cuda(), scale=scale, out=zi,
+                                   **({k: v[i:i + 1] for k, v in extra.items()}))
+        near(one, want[i:i + 1], tol[i:i + 1])
 
 
 def far_distill_grad(z, ids, u, scale, tail, weight):
@@ -133,6 +211,31 @@ def far_distill_grad(z, ids, u, scale, tail, weight):
         want[i], terms[i] = weight[i].double() * scale * d, mag
     rel = sum_tol(z.shape[1]) + 8 * EPS * (clip(lp, 200.0) + clip(lse, SAVED)[:, None] + clip(u.double(), 200.0).amax(1)[:, None] + 4) + 2 ** -20
     return want, weight.double().abs()[:, None] * scale * rel * terms * 4 + HALF[z.dtype] * want.abs() + TINY[z.dtype] + 1e-30
+
+
+@pytest.mark.parametrize("V,type_", FAR_SIZES)
+@pytest.mark.parametrize("tail", [False, True])
+def test_distillation_gradient_where_lse_is_large(V, type_, tail):
+    g = gen(V)
+    z = far_rows(V, type_, g)
+    N, K = z.shape[0], 6
+    ids = torch.stack([torch.randperm(V, generator=g)[:K] for _ in range(N)])
+    ids[8] = torch.arange(K)                     # all live columns are named: the student's mass outside is exp(-1e9)
+    ids[5, K - 1] = ids[5, 0]
+    u = torch.log_softmax(torch.randn((N, K), generator=g), 1) - 0.3
+    w = torch.rand(N, generator=g) + 0.5
+    want, tol = far_distill_grad(z, ids, u, 1.0, tail, w)
+    zd, _ = view(z, 3, 1)
+    got = lm().distill(zd, ids.cuda(), u.cuda(), tail=tail, weight=w.cuda())
+    near(got.grad, want, tol)
+    back = lm().distill_grad(zd, ids.cuda(), u.cuda(), got.lse, w.cuda(), tail=tail, log_tail=got.log_tail)
+    near(back, want, tol)
+    near(lm().distill_grad(zd, ids.cuda(), u.cuda(), got.lse, w.cuda(), tail=tail, log_tail=got.log_tail, out=zd), want, tol)
+    for i in (0, 8):
+        zi = z[i:i + 1].cuda()
+        one = lm().distill_grad(zi, ids[i:i + 1].cuda(), u[i:i + 1].cuda(), got.lse[i:i + 1], w[i:i + 1].cuda(), tail=tail,
+                                log_tail=got.log_tail[i:i + 1] if tail else None, out=zi)
+        near(one, want[i:i + 1], tol[i:i + 1])
 
 
 # ------------------------------------------------------------------ statistics on both sides of the range of one multiply-add
