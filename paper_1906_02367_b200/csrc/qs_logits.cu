@@ -756,7 +756,7 @@ __device__ __forceinline__ float factor(const Slope& s, float norm) {
 }
 // rows whose p_T is too small for the quotient: the shares instead
 template <class T>
-__device__ __noinline__ uint4 share_vec(const uint4& q, const f2* d, const Slope& s, float norm, float c2) {
+__device__ __noinline__ uint4 share_vec(uint4 q, const f2* d, const Slope& s, float norm, float c2) {
     constexpr int P = Vec<T>::E / 2;
     f2 g[P];
     const float f = factor(s, norm), c = s.out_by > 0.0f ? -s.w * s.rest * s.out_by : 0.0f;
@@ -989,20 +989,24 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         if ((int)threadIdx.x == nt - 2 && r.w1 < r.v1) store_edge(r, out, r.w1, grad_of(kept[r.w1 - r.v0]));
     } else {
         const f2 minus = far ? make_f2(-m, -m) : make_f2(-ref, -ref);
+        auto each = [&](auto grad_of) {
 #pragma unroll 1
-        for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt) {
-            const bool whole = vec >= r.w0 && vec < r.w1;
-            const uint4 q = KEEP ? kept[vec - r.v0] : whole ? __ldcs(r.vectors() + vec) : r.edge(vec);
-            f2 d[E / 2];
+            for (int vec = r.v0 + (int)threadIdx.x; vec < r.v1; vec += nt) {
+                const bool whole = vec >= r.w0 && vec < r.w1;
+                const uint4 q = KEEP ? kept[vec - r.v0] : whole ? __ldcs(r.vectors() + vec) : r.edge(vec);
+                f2 d[E / 2];
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                const f2 z = Vec<T>::pair(q, i);
-                d[i] = far ? mul2(add2(z, minus), c2s) : fma2(z, c2s, minus);
+                for (int i = 0; i < E / 2; ++i) {
+                    const f2 z = Vec<T>::pair(q, i);
+                    d[i] = far ? mul2(add2(z, minus), c2s) : fma2(z, c2s, minus);
+                }
+                const uint4 g = grad_of(q, d);
+                if (a.wide && whole) __stcs(to + vec, g);
+                else store_edge(r, out, vec, g);
             }
-            const uint4 g = thin ? share_vec<T>(q, d, s, norm, c2) : slope_vec<T>(d, f);
-            if (a.wide && whole) __stcs(to + vec, g);
-            else store_edge(r, out, vec, g);
-        }
+        };
+        if (thin) each([&](const uint4& q, const f2* d) { return share_vec<T>(q, d, s, norm, c2); });
+        else each([&](const uint4&, const f2* d) { return slope_vec<T>(d, f); });
     }
     __syncthreads();                               // the ids' places are written last
 #pragma unroll
