@@ -485,6 +485,9 @@ int qs_token_logp_grad(int64_t N, int64_t V, const void* logits, int type, int64
  * ids, teacher: N x K, contiguous; an id given twice counts as two entries of one class.
  *   loss, lse, log_tail (log p_T; written when tail != 0), each N or NULL; a loss or log_tail that
  *   passes the largest fp32 number without a column at -inf is that number with its sign.
+ *   A block waits two seconds at most for its copies and its cluster (QSPARSE_WAIT_LIMIT_NS lowers
+ *   that; 0 gives up at once); a row for which they did not come is NaN in loss, lse, log_tail and
+ *   gradient, and *status becomes QS_TIMEOUT.
  *   A row without entries (tail == 0) has loss 0 and gradient 0; q_k > 0 on a column at -inf gives
  *   loss +inf; a row of logits at -inf has gradient 0.  An id >= V makes the row's loss and
  *   gradient NaN.  grad and its overlap as in qs_token_logp_grad.

@@ -17,6 +17,9 @@
 // are one pass per vector.  bf16 rows of 128000: statistics alone 374 us for 8192 rows (5.6 TB/s), the loss and its gradient
 // 650 us for 6144 (4.8 TB/s; the two halves of a block's life, read and write, overlap only with other blocks' halves);
 // 64 alternatives, 4096 rows of 50003: 131 us (3.1 TB/s; finding and ranking them takes as long as reading).
+#include <algorithm>
+#include <cstdlib>
+
 #include "qs_rows.cuh"
 
 namespace {
@@ -55,6 +58,7 @@ struct RowArgs {
     int parts;                             // log2 of the blocks per row
     int per;                               // batches per stretch whose maximum is kept
     int rows;                              // backward calls: which rows this launch is for
+    unsigned long long wait_ns;            // limit of a wait
     int* status;
 };
 
@@ -841,7 +845,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     __syncthreads();
     if (blocks > 1) cluster_wait();
     bool ok = true;
-    if (KEEP) ok = mbar_wait(&landed, 0);
+    if (KEEP) ok = mbar_wait(&landed, 0, a.wait_ns);
     // logits at the ids of the share
     T* flat = reinterpret_cast<T*>(kept);
     bool named[PER];
@@ -866,7 +870,8 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             __syncthreads();
         }
     }
-    Stat st{neg_inf(), 0.0f, 0.0f};
+    // a share that has not come (see below) makes the row's sums NaN, and so all of its results in every block
+    Stat st{neg_inf(), ok ? 0.0f : quiet_nan(), 0.0f};
     float largest = neg_inf();
     // (one loop for all vectors: a second copy of its body for the rest costs more in instruction misses than it saves)
     for (int base = r.v0; base < r.v1; base += nt * VK) {
@@ -898,21 +903,20 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             send(remote_addr(&in_part[rank], lane), v, remote_addr(&met, lane));
         }
     }
-    if (blocks == 1) {
-        __syncthreads();
-    } else {
-        if (rank >= readers) return;               // nothing is sent to this block
-        ok &= mbar_wait(&met, 0);
-    }
-    if (!ok) {                                     // a copy never came (2 s): the row's results are void
-        flag_status(a.status, QS_TIMEOUT);
+    if (blocks == 1) __syncthreads();
+    else if (rank < readers) ok &= mbar_wait(&met, 0, a.wait_ns);
+    if (!ok) {                                     // a copy or a block's sums did not come in time: the row's results are NaN
+        if (a.status) atomicExch(a.status, QS_TIMEOUT);
         if (KEEP) mbar_wait(&landed, 0);           // once more, before the memory goes to another block
+        if (rank < readers && blocks > 1) mbar_wait(&met, 0);
     }
+    if (rank >= readers) return;                   // nothing is sent to this block
     Stat v{};
     float log_tail = 0.0f, out_m = 0.0f, out_s = 0.0f, out_gap = 0.0f, lse = 0.0f, ls = 0.0f;
     bool empty = false;
     if (warp == 0) {
         v = join_parts(part, warps * blocks, c2);
+        if (!ok) v.s = quiet_nan();
         if (TAIL) {
             const Stat in = join_parts(in_part, blocks, c2);
             const float m = fmaxf(v.m, in.m);
@@ -961,7 +965,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             if (!masked && log_tail > neg_inf() && loss == -neg_inf()) loss = FLT_MAX;
         }
         if (lane == 0) {
-            if (a.loss) a.loss[n] = t.bad ? quiet_nan() : loss;
+            if (a.loss) a.loss[n] = t.bad || !ok ? quiet_nan() : loss;
             if (a.lse) a.lse[n] = lse;
             if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
         }
@@ -1204,6 +1208,15 @@ cudaError_t launch_distill_grad(const RowArgs& a, bool tail, cudaStream_t st) {
     return launch_grad(tail ? distill_grad_kernel<T, true> : distill_grad_kernel<T, false>, a, most_vectors(a.V, sizeof(T)), st);
 }
 
+// Two seconds, or less: QSPARSE_WAIT_LIMIT_NS, read once; 0 gives up at once (a test of what follows)
+unsigned long long wait_limit() {
+    static const unsigned long long ns = [] {
+        const char* e = std::getenv("QSPARSE_WAIT_LIMIT_NS");
+        return e ? std::min(std::strtoull(e, nullptr, 10), WAIT_LIMIT_NS) : WAIT_LIMIT_NS;
+    }();
+    return ns;
+}
+
 int status_of(cudaError_t e) {
     if (e == cudaSuccess) return QS_OK;
     cudaGetLastError();
@@ -1285,7 +1298,7 @@ int qs_distill(int64_t N, int64_t V, int K, const void* logits, int type, int64_
     RowArgs a{};
     a.N = N; a.V = V; a.logits = logits; a.stride = row_stride; a.scale = scale;
     a.tok = Ids{ids, id_type == QS_I64}; a.K = K; a.teacher = teacher; a.teacher_type = teacher_type; a.teacher_scale = teacher_scale;
-    a.loss = loss; a.lse = lse; a.log_tail = log_tail; a.g1 = weight; a.g_all = weight_all;
+    a.loss = loss; a.lse = lse; a.log_tail = log_tail; a.g1 = weight; a.g_all = weight_all; a.wait_ns = wait_limit();
     a.grad = grad; a.grad_stride = grad_stride; a.status = status;
     a.wide = grad && lie_alike(logits, row_stride, grad, grad_stride, size);
     return QS_BY_TYPE(launch_distill, type, a, tail != 0, static_cast<cudaStream_t>(cuda_stream));

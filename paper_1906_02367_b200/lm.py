@@ -6,7 +6,8 @@ include/qsparse.h, which says what each computes; the arithmetic is in the CUDA 
 enqueued on `stream` (default: the current stream of the tensors' device, which must be the current
 device) and nothing waits for the GPU.  Tensors made on other streams are the caller's to order, as with any
 torch call.  `status`, where taken, is an int32 CUDA tensor of one element, zero before the call, that receives
-QS_INVALID_ARG if an id lies past the last row or column.
+QS_INVALID_ARG if an id lies past the last row or column, and QS_TIMEOUT if a wait on the device ran out (distill; the
+rows concerned are NaN with or without it).
 """
 from collections import namedtuple
 

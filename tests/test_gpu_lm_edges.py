@@ -3,6 +3,9 @@ largest number; NaN and infinities; paths that only long lists and long rows tak
 Tolerances as in test_gpu_lm.py: EPS is half a unit in the last place of fp32, an exponential is off by 2^-21, a sum of n
 terms by n EPS of their magnitudes."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -11,6 +14,7 @@ from tests import lm_reference as ref
 from tests.test_gpu_lm import BF16, EPS, F16, F32, HALF, NAN, NEG, TINY, _near_distill, _near_logp_grad, gen, near, sum_tol, view
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 INF = float("inf")
 SAVED = 256.0                                    # an lse up to here is taken as it is: off by EPS of it
 
@@ -256,6 +260,45 @@ def test_rows_on_both_sides_of_the_exponents_range(N, V, rising, sign):
     near(r.top_logp, tl, s)
     d = lm().distill(z.cuda(), tok[:, None].cuda(), torch.zeros(N, 1).cuda(), weight=1.0)
     near(d.loss, -logp, s + 2 ** -19)
+
+
+# ------------------------------------------------------------------ calls beside other calls
+
+
+def child(code, **env):
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, env={**os.environ, **env}, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
+    return r.stdout
+
+
+def test_a_wait_that_runs_out_leaves_nan():
+    """With no time to wait at all, every row that needs a copy or another block's sums is NaN, with a status or without; the
+    memory of the copies is not given up before they have come."""
+    child("""
+import torch
+from paper_1906_02367_b200 import binding as B, lm
+for N, V, type_ in ((3, 1000, torch.float32), (2, 50003, torch.bfloat16), (900, 40000, torch.bfloat16), (2, 600000, torch.float32)):
+    z = torch.randn(N, V, device="cuda").to(type_)
+    ids, u = torch.randint(0, V, (N, 4), device="cuda"), torch.full((N, 4), -2.0, device="cuda")
+    ids[1] = torch.tensor([-1, -1, -1, V])                    # an id past the end does not hide it
+    for tail in (False, True):
+        for weight in (None, 1.0):
+            status = torch.zeros(1, dtype=torch.int32, device="cuda")
+            lm.distill(z, ids, u, tail=tail, weight=weight)
+            d = lm.distill(z, ids, u, tail=tail, weight=weight, status=status)
+            assert int(status) == B.QS_TIMEOUT
+            for t in (d.loss, d.lse, d.log_tail, d.grad):
+                assert t is None or bool(torch.isnan(t).all())
+    r = lm.token_logp(z, ids[:, 0].contiguous(), top=2)       # the calls that wait for nothing go on
+    assert bool(torch.isfinite(r.lse).all())
+""", QSPARSE_WAIT_LIMIT_NS="0")
+    child("""
+import torch
+from paper_1906_02367_b200 import lm
+z = torch.randn(2, 50003, device="cuda")
+d = lm.distill(z, torch.zeros(2, 1, dtype=torch.int64, device="cuda"), torch.zeros(2, 1, device="cuda"), tail=True, weight=1.0)
+assert bool(torch.isfinite(d.loss).all()) and bool(torch.isfinite(d.grad).all())
+""", QSPARSE_WAIT_LIMIT_NS="1000000000")
 
 
 # ------------------------------------------------------------------ long lists of tokens
