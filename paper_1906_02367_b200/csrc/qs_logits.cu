@@ -1138,8 +1138,8 @@ cudaError_t launch_rows(K kernel, const Shape& s, RowArgs a, bool cluster, cudaS
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
     }
-    if (s.smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)s.smem);
+    if (s.smem > 32 * 1024) {                      // (the limit is the function's, for all threads: every call sets the same one)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16 * SHARE_MOST);
         if (e != cudaSuccess) return e;
     }
     const long long most = 0x7fffffffll / s.blocks;              // rows per launch

@@ -6,6 +6,7 @@ import math
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 import torch
@@ -263,6 +264,33 @@ def test_rows_on_both_sides_of_the_exponents_range(N, V, rising, sign):
 
 
 # ------------------------------------------------------------------ calls beside other calls
+def test_calls_from_several_threads():
+    """Threads distil at vocabularies whose shares of shared memory differ: no call may see another's size."""
+    from paper_1906_02367_b200 import binding as B
+    L, N, K, calls, codes, work = B.lib(), 890, 4, 2000, [], []
+    for V in (18000, 40000, 90000, 33000):
+        z = torch.randn((N, V), generator=gen(V)).to(BF16).cuda()
+        ids, u = torch.randint(0, V, (N, K), generator=gen(1)).cuda(), torch.zeros(N, K).cuda()
+        loss, grad = torch.empty(N, device="cuda"), torch.empty_like(z)
+        work.append((z, ids, u, loss, grad, lm().distill(z, ids, u, weight=1.0), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    start = threading.Barrier(len(work))
+
+    def run(z, ids, u, loss, grad, _, stream):
+        args = (N, z.shape[1], K, z.data_ptr(), B.QS_BF16, z.shape[1], ids.data_ptr(), B.QS_I64, u.data_ptr(), B.QS_F32, 1.0, 1.0, 0, loss.data_ptr(),
+                None, None, None, 1.0, grad.data_ptr(), z.shape[1], None, stream.cuda_stream)
+        start.wait()
+        codes.extend(L.qs_distill(*args) for _ in range(calls))
+
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert len(codes) == calls * len(work) and not any(codes)
+    for _, _, _, loss, grad, want, _ in work:
+        assert torch.equal(loss, want.loss) and torch.equal(grad, want.grad)
 
 
 def child(code, **env):
