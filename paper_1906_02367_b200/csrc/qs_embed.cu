@@ -163,14 +163,13 @@ __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
 }
 
 template <class TW, class TO>
-void launch_embed(EmbedArgs a, bool wide, cudaStream_t st) {
+cudaError_t launch_embed(EmbedArgs a, bool wide, cudaStream_t st) {
     if (wide) {
         while (a.lanes < 5 && (8ll << a.lanes) < a.D) ++a.lanes;
-        embed_wide_kernel<TW, TO><<<(unsigned)(((a.rows << a.lanes) + 255) / 256), 256, 0, st>>>(a);
-    } else {
-        a.units = (uint32_t)((a.D + COLS - 1) / COLS);
-        embed_kernel<TW, TO><<<(unsigned)((a.rows * a.units + 7) / 8), 256, 0, st>>>(a);
+        return launch(false, embed_wide_kernel<TW, TO>, (unsigned)(((a.rows << a.lanes) + 255) / 256), 256, 0, st, a);
     }
+    a.units = (uint32_t)((a.D + COLS - 1) / COLS);
+    return launch(false, embed_kernel<TW, TO>, (unsigned)((a.rows * a.units + 7) / 8), 256, 0, st, a);
 }
 
 // ------------------------------------------------------------------ gradient: sort by token
@@ -830,39 +829,25 @@ __global__ void __launch_bounds__(256) run_join_kernel(const GradArgs a) {
 // rows of zeros alone (no tokens)
 __global__ void __launch_bounds__(256) zero_all_kernel(const GradArgs a) { zero_all<256>(a, blockIdx.x, gridDim.x); }
 
-template <class... P, class... A>
-void launch_after(void (*kernel)(P...), unsigned grid, unsigned threads, unsigned smem, cudaStream_t st, A... args) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, kernel, args...);           // (an error stays for launch_status)
-}
-
 // IN, OUT: the rows of g, of the table on 16-byte boundaries
 template <class T, bool IN, bool OUT>
-void launch_sums(const GradArgs& a, bool zero, int sms, cudaStream_t st) {
+cudaError_t launch_sums(const GradArgs& a, bool zero, int sms, cudaStream_t st) {
     const int warps = IN ? RING_WARPS : SUM_THREADS / 32;
     const unsigned blocks = (unsigned)(((long long)a.R * a.chunks * a.col_tiles + warps - 1) / warps);
+    cudaError_t e;
     if (IN) {
-        cudaFuncSetAttribute(run_sum_wide_kernel<T, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_WARPS * RING_BYTES);
-        launch_after(run_sum_wide_kernel<T, OUT>, blocks + (zero ? sms * 3 : 0), RING_WARPS * 32, RING_WARPS * RING_BYTES, st, a, blocks);
+        e = cudaFuncSetAttribute(run_sum_wide_kernel<T, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_WARPS * RING_BYTES);
+        if (e == cudaSuccess) e = launch(true, run_sum_wide_kernel<T, OUT>, blocks + (zero ? sms * 3 : 0), RING_WARPS * 32, RING_WARPS * RING_BYTES, st, a, blocks);
     } else {
-        launch_after(run_sum_kernel<T>, blocks + (zero ? sms * 8 : 0), SUM_THREADS, 0, st, a, blocks);
+        e = launch(true, run_sum_kernel<T>, blocks + (zero ? sms * 8 : 0), SUM_THREADS, 0, st, a, blocks);
     }
-    launch_after(run_join_kernel<sizeof(T), IN, OUT>, sms * 4, 256, 0, st, a);
+    return e != cudaSuccess ? e : launch(true, run_join_kernel<sizeof(T), IN, OUT>, sms * 4, 256, 0, st, a);
 }
 template <class T>
-void launch_sums(const GradArgs& a, bool zero, bool in, bool out, int sms, cudaStream_t st) {
-    if (in && out) launch_sums<T, true, true>(a, zero, sms, st);
-    else if (in) launch_sums<T, true, false>(a, zero, sms, st);
-    else launch_sums<T, false, false>(a, zero, sms, st);
+cudaError_t launch_sums(const GradArgs& a, bool zero, bool in, bool out, int sms, cudaStream_t st) {
+    if (in && out) return launch_sums<T, true, true>(a, zero, sms, st);
+    if (in) return launch_sums<T, true, false>(a, zero, sms, st);
+    return launch_sums<T, false, false>(a, zero, sms, st);
 }
 
 int bits_for(long long v) {
@@ -903,14 +888,13 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
 }
 
 template <class TW>
-void launch_embed_to(const EmbedArgs& a, int out_type, cudaStream_t st) {
+cudaError_t launch_embed_to(const EmbedArgs& a, int out_type, cudaStream_t st) {
     const int out_size = out_type == QS_F32 ? 4 : 2, size = (int)sizeof(TW);
     // 16-byte accesses need every row on a 16-byte boundary
     const bool wide = aligned_to(a.table, 16) && a.row_stride * size % 16 == 0 && a.worker_stride * size % 16 == 0 && aligned_to(a.out, 16) &&
                       a.out_stride * out_size % 16 == 0;
-    if (out_type == QS_F32) launch_embed<TW, float>(a, wide, st);
-    else if (out_type == QS_BF16) launch_embed<TW, __nv_bfloat16>(a, wide, st);
-    else launch_embed<TW, __half>(a, wide, st);
+    if (out_type == QS_F32) return launch_embed<TW, float>(a, wide, st);
+    return out_type == QS_BF16 ? launch_embed<TW, __nv_bfloat16>(a, wide, st) : launch_embed<TW, __half>(a, wide, st);
 }
 
 bool bad_shape(int R, int64_t N, int64_t V, int64_t D) { return R < 1 || R > 32 || N < 0 || V < 1 || D < 1; }
@@ -934,10 +918,8 @@ int qs_embed(int R, int64_t N, int64_t V, int64_t D, const void* tokens, int tok
         !aligned_to(out, size_of_type(out_type)) || !aligned_to(status, 4)) return QS_INVALID_ARG;
     EmbedArgs a{N, V, D, Ids{tokens, token_type == QS_I64}, table, worker_stride, row_stride, scale, out, out_stride, status, R * N, 0, 0};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (table_type == QS_F32) launch_embed_to<float>(a, out_type, st);
-    else if (table_type == QS_BF16) launch_embed_to<__nv_bfloat16>(a, out_type, st);
-    else launch_embed_to<__half>(a, out_type, st);
-    return launch_status();
+    return status_of(table_type == QS_F32 ? launch_embed_to<float>(a, out_type, st) : table_type == QS_BF16 ? launch_embed_to<__nv_bfloat16>(a, out_type, st)
+                                                                                                            : launch_embed_to<__half>(a, out_type, st));
 }
 
 int64_t qs_embed_grad_bytes(int R, int64_t N, int64_t V, int64_t D) {
@@ -987,25 +969,23 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     else if (a.pieces && p.one_tile && R * V * D < 1ll << 25) a.pieces = 0;
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)
-    if ((N == 0 || !p.one_tile) && cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st) != cudaSuccess) { cudaGetLastError(); return QS_CUDA; }
-    if (N == 0) {
-        zero_all_kernel<<<sms * 8, 256, 0, st>>>(a);
-        return launch_status();
-    }
+    cudaError_t e = cudaSuccess;
+    if (N == 0 || !p.one_tile) e = cudaMemsetAsync(w + p.count, 0, 4 * (p.zeroed - p.count), st);
+    if (N == 0) return status_of(e != cudaSuccess ? e : launch(false, zero_all_kernel, sms * 8, 256, 0, st, a));
     if (p.one_tile) {
-        sort_one_tile_kernel<<<R, SORT_THREADS, 0, st>>>(a);
+        e = launch(false, sort_one_tile_kernel, R, SORT_THREADS, 0, st, a);
     } else {
-        sort_count_kernel<<<dim3(p.tiles, R), SORT_THREADS, 0, st>>>(a);
+        if (e == cudaSuccess) e = launch(false, sort_count_kernel, dim3(p.tiles, R), SORT_THREADS, 0, st, a);
         const int sorters = R * p.tiles, beside = accumulate || !a.pieces || sorters > 2 * sms ? 0 : 2 * sms - sorters;
-        for (int pass = 0; pass < p.passes; ++pass) launch_after(sort_scatter_kernel, (unsigned)(sorters + beside), SORT_THREADS, 0, st, a, pass);
+        for (int pass = 0; pass < p.passes && e == cudaSuccess; ++pass)
+            e = launch(true, sort_scatter_kernel, (unsigned)(sorters + beside), SORT_THREADS, 0, st, a, pass);
     }
+    if (e != cudaSuccess) return status_of(e);
     const int size = size_of_type(grad_type);
     const bool in = aligned_to(grad_out, 16) && grad_stride * size % 16 == 0;
     const bool out = aligned_to(grad_table, 16) && row_stride % 4 == 0 && worker_stride % 4 == 0;
-    if (grad_type == QS_F32) launch_sums<float>(a, !accumulate, in, out, sms, st);
-    else if (grad_type == QS_BF16) launch_sums<__nv_bfloat16>(a, !accumulate, in, out, sms, st);
-    else launch_sums<__half>(a, !accumulate, in, out, sms, st);
-    return launch_status();
+    return status_of(grad_type == QS_F32 ? launch_sums<float>(a, !accumulate, in, out, sms, st)
+                     : grad_type == QS_BF16 ? launch_sums<__nv_bfloat16>(a, !accumulate, in, out, sms, st) : launch_sums<__half>(a, !accumulate, in, out, sms, st));
 }
 
 }  // extern "C"

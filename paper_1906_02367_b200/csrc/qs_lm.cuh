@@ -48,10 +48,26 @@ __device__ __forceinline__ float ex2(float x) {
 inline int size_of_type(int type) { return type == QS_F32 ? 4 : (type == QS_BF16 || type == QS_F16) ? 2 : 0; }
 inline bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 inline bool is_id_type(int t) { return t == QS_I32 || t == QS_I64; }
-inline int launch_status() {
-    if (cudaPeekAtLastError() == cudaSuccess) return QS_OK;
+// of a call's own launches and copies: an error that another call left is not looked at
+inline int status_of(cudaError_t e) {
+    if (e == cudaSuccess) return QS_OK;
     cudaGetLastError();
     return QS_CUDA;
+}
+// AFTER: the kernel may start while the one before it still runs (it waits for that one's end itself)
+template <class... P, class... A>
+cudaError_t launch(bool after, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = after ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace qs

@@ -1217,11 +1217,6 @@ unsigned long long wait_limit() {
     return ns;
 }
 
-int status_of(cudaError_t e) {
-    if (e == cudaSuccess) return QS_OK;
-    cudaGetLastError();
-    return QS_CUDA;
-}
 #define QS_BY_TYPE(launch, type, ...) \
     status_of((type) == QS_F32 ? launch<float>(__VA_ARGS__) : (type) == QS_BF16 ? launch<__nv_bfloat16>(__VA_ARGS__) : launch<__half>(__VA_ARGS__))
 

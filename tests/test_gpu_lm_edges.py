@@ -299,6 +299,34 @@ def child(code, **env):
     return r.stdout
 
 
+def test_an_error_that_another_call_left_is_not_reported():
+    """A call that fails on the host (waiting for a stream that is being captured) leaves its error with the runtime; the
+    operators' calls after it do their work and say so."""
+    child("""
+import torch
+from paper_1906_02367_b200 import binding as B, lm
+side = torch.cuda.Stream()
+ctx = B.Context(1, 64, 4, 1, stream=side)
+table, tok = torch.randn(10, 8, device="cuda"), torch.arange(5, device="cuda")
+z = torch.randn(5, 10, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+try:
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        code = ctx.sync_status()
+        graph.capture_end()
+except RuntimeError:
+    pass
+assert code == B.QS_CUDA
+assert torch.equal(lm.embed(tok, table), table[:5])
+grad = lm.embed_grad(tok, torch.ones(5, 8, device="cuda"), 10)
+assert grad.sum().item() == 40.0
+assert lm.embed_grad(tok[:0], torch.ones(0, 8, device="cuda"), 10).sum().item() == 0.0
+assert torch.isfinite(lm.token_logp(z, tok).logp).all()
+""")
+
+
 def test_a_wait_that_runs_out_leaves_nan():
     """With no time to wait at all, every row that needs a copy or another block's sums is NaN, with a status or without; the
     memory of the copies is not given up before they have come."""
