@@ -462,8 +462,8 @@ int qs_token_logp(int64_t N, int64_t V, const void* logits, int type, int64_t ro
  *   tokens NULL or a negative token: no part from logp; one >= V: a row of NaN.
  *   A row whose lse is -inf gets zeros.  Where |lse| > 256, 32 bits have lost too much of it: the
  *   row's statistics are taken again from the logits, which are then read twice.
- *   grad: rows grad_stride >= V apart; it may be the logits themselves (same stride), any other
- *   overlap is QS_INVALID_ARG.
+ *   grad: rows grad_stride >= V apart; it may be the logits themselves, or other columns of the
+ *   same rows (same stride); memory that both name is QS_INVALID_ARG otherwise.
  */
 int qs_token_logp_grad(int64_t N, int64_t V, const void* logits, int type, int64_t row_stride,
                        const void* tokens, int token_type, float scale, const float* lse,

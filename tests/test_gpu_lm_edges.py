@@ -263,6 +263,30 @@ def test_rows_on_both_sides_of_the_exponents_range(N, V, rising, sign):
     near(d.loss, -logp, s + 2 ** -19)
 
 
+# ------------------------------------------------------------------ gradients beside the logits
+def test_gradients_in_other_columns_of_the_logits_buffer():
+    """Logits and gradient in two halves of the same rows share no element."""
+    N, V, K = 5, 203, 3
+    z = torch.randn((N, V), generator=gen(1))
+    buf = torch.full((N, 2 * V + 2), 77.0, device="cuda")
+    for at, out_at in ((0, V + 1), (V + 2, 1)):
+        zd, out = buf[:, at:at + V], buf[:, out_at:out_at + V]
+        zd.copy_(z)
+        tok = torch.arange(N)
+        r = lm().token_logp(zd, tok.cuda())
+        lm().token_logp_grad(zd, tok.cuda(), r.lse, 1.0, out=out)
+        _near_logp_grad(out, z, tok, 1.0, torch.ones(N), torch.zeros(N))
+        assert torch.equal(zd.cpu(), z)
+        ids, u = torch.randint(0, V, (N, K), generator=gen(2)), torch.randn((N, K), generator=gen(3))
+        got = lm().distill(zd, ids.cuda(), u.cuda(), weight=1.0, out=out)
+        _near_distill(got, z, ids, u, 1.0, 1.0, False, torch.ones(N))
+        assert torch.equal(zd.cpu(), z)
+    from paper_1906_02367_b200 import binding as B
+    for at in (1, V - 1, V + 3):                 # one element at least is shared, within a row or with the next
+        with pytest.raises(B.QsError):
+            lm().token_logp_grad(buf[:N - 1, :V], tok[:N - 1].cuda(), r.lse[:N - 1], 1.0, out=torch.as_strided(buf, (N - 1, V), (2 * V + 2, 1), at))
+
+
 # ------------------------------------------------------------------ calls beside other calls
 def test_calls_from_several_threads():
     """Threads distil at vocabularies whose shares of shared memory differ: no call may see another's size."""
