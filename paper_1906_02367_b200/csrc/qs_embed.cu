@@ -180,7 +180,8 @@ __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.
 
 constexpr int SORT_THREADS = 1024;
 constexpr int SORT_MAX_BITS = 9;
-constexpr int SORT_MAX_ITEMS = 8;          // places per thread and tile
+constexpr int SORT_ITEMS = 8;              // places per thread and tile, as long as a worker's tiles are no more than
+constexpr int MOST_TILES = 2048;           // (each tile reads the counts of all: 131072 of them for 2^30 tokens would be 30 TB)
 constexpr int ONE_TILE = 1024;             // places per worker that one block sorts in its shared memory
 constexpr int WARPS = SORT_THREADS / 32;
 
@@ -869,7 +870,7 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     s.bits = (total + s.passes - 1) / s.passes;
     s.one_tile = N <= ONE_TILE;
     s.items = 1;                                         // tiles of 1024 places while 64 of them cover the list: every block reads all tiles' counts
-    while (s.items < SORT_MAX_ITEMS && N > 64ll * SORT_THREADS * s.items) s.items *= 2;
+    while (N > 64ll * SORT_THREADS * s.items && (s.items < SORT_ITEMS || N > (long long)MOST_TILES * SORT_THREADS * s.items)) s.items *= 2;
     const int64_t tile = (int64_t)s.items * SORT_THREADS;
     s.tiles = (int)((N + tile - 1) / tile);
     s.col_tiles = (int)((D + COLS - 1) / COLS);

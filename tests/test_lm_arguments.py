@@ -96,3 +96,14 @@ def test_dimensions_of_one_element_have_no_stride(calls):
         lm.embed(tok, table, out=torch.zeros(B, 1, 2 * D)[..., ::2])
     with pytest.raises(ValueError):                      # rows whose two dimensions do not flatten
         lm.embed(torch.zeros((2, 2), dtype=torch.int64), table, out=torch.zeros(2, 3, D)[:, :2])
+
+
+def test_tiles_of_a_long_list_are_few():
+    """Every tile of the sort reads the counts of all tiles: their number has a bound, up to the most tokens that are taken.
+    The workspace shows it: 16 bytes a token, the partial sums of chunks of 64, and the rest."""
+    from paper_1906_02367_b200 import binding as B
+    L = B.lib()
+    for R, N in ((1, 1 << 30), (1, 20_000_000), (32, 1 << 25), (8, 3_000_000)):
+        chunks = R * (N // 64 + 1)
+        rest = L.qs_embed_grad_bytes(R, N, 128000, 1) - 16 * R * N - chunks * (2 * 256 * 4 + 4) - R * 128000
+        assert rest <= 2 * R * 2048 * 512 * 4 + 1024, (R, N, rest)
