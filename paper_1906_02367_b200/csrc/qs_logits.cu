@@ -912,7 +912,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     }
     if (rank >= readers) return;                   // nothing is sent to this block
     Stat v{};
-    float log_tail = 0.0f, out_m = 0.0f, out_s = 0.0f, out_gap = 0.0f, lse = 0.0f, ls = 0.0f;
+    float log_tail = 0.0f, out_m = 0.0f, out_s = 0.0f, out_gap = 0.0f;
     bool empty = false;
     if (warp == 0) {
         v = join_parts(part, warps * blocks, c2);
@@ -935,10 +935,8 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             v = final_stat(v, c2);
         }
         empty = is_empty(v);
-        ls = logf(v.s);
-        lse = lse_of(v, a.scale, ls);
         Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
-        s.set_out(out_m, out_s);
+        if (TAIL) s.set_out(out_m, out_s);
         if (lane == 0) {
             row_m = shift_of(v.m);
             row_by = empty ? 0.0f : 1.0f / v.s;
@@ -947,18 +945,27 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     }
     if (a.grad) __syncthreads();
     if (warp == 0 && rank == 0) {                  // while the other warps go on
+        const float ls = logf(v.s);
         float loss = 0.0f;
-        bool beyond = false;                       // an entry where the student has no mass at all
+        bool beyond = false, masked = false;       // an entry whose log p is no number; where the student has no mass at all
         for (int k = lane; k < a.K; k += 32) {
             if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
-            const float gap = z_at[k] - v.m, lp = empty ? neg_inf() : fmaf(gap, a.scale, -ls);
-            beyond |= empty || z_at[k] == neg_inf();
-            // (a log p beyond the largest number, of a column that is not masked: its product with q need not be)
-            loss = !empty && lp == neg_inf() && gap > lp ? fmaf(-t.q[k] * a.scale, gap, loss) : fmaf(t.q[k], t.logq[k] - lp, loss);
+            const float lp = empty ? neg_inf() : fmaf(z_at[k] - v.m, a.scale, -ls);
+            beyond |= lp == neg_inf();
+            loss = fmaf(t.q[k], t.logq[k] - lp, loss);
+        }
+        if (__any_sync(~0u, beyond)) {             // a log p beyond the largest number, of a column at a lowest value: its product with q need not be
+            loss = 0.0f;
+            for (int k = lane; k < a.K; k += 32) {
+                if (t.id[k] == NO_ID || t.q[k] == 0.0f) continue;
+                const float gap = z_at[k] - v.m, lp = fmaf(gap, a.scale, -ls);
+                masked |= empty || z_at[k] == neg_inf();
+                loss = !empty && lp == neg_inf() && gap > lp ? fmaf(-t.q[k] * a.scale, gap, loss) : fmaf(t.q[k], t.logq[k] - (empty ? neg_inf() : lp), loss);
+            }
+            masked = __any_sync(~0u, masked);
         }
         loss = warp_sum(loss);
         // a mean of log p at masks of the lowest value that passes the largest number is that number
-        const bool masked = __any_sync(~0u, beyond);
         if (!masked && loss == -neg_inf()) loss = FLT_MAX;
         if (TAIL && t.rest != 0.0f) {
             loss = log_tail == -FLT_MAX ? fmaf(-t.rest * a.scale, out_gap, loss) : fmaf(t.rest, logf(t.rest) - log_tail, loss);
@@ -966,7 +973,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
         }
         if (lane == 0) {
             if (a.loss) a.loss[n] = t.bad || !ok ? quiet_nan() : loss;
-            if (a.lse) a.lse[n] = lse;
+            if (a.lse) a.lse[n] = lse_of(v, a.scale, ls);
             if (TAIL && a.log_tail) a.log_tail[n] = log_tail;
         }
     }
