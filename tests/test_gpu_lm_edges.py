@@ -243,6 +243,22 @@ def test_distillation_gradient_where_lse_is_large(V, type_, tail):
         near(one, want[i:i + 1], tol[i:i + 1])
 
 
+@pytest.mark.parametrize("V", [12, 128])
+@pytest.mark.parametrize("type_", [F32, BF16])
+def test_backward_call_where_every_column_is_named(V, type_):
+    """No column is left outside the ids: log p_T is -inf, and the rest of the teacher's mass pulls at none."""
+    N = 3
+    z = torch.randn((N, V), generator=gen(V)).to(type_)
+    z[2, V // 2:] = NEG
+    ids = torch.stack([torch.randperm(V, generator=gen(i)) for i in range(N)])
+    u, w = torch.log_softmax(torch.randn((N, V), generator=gen(4)), 1) + math.log(0.9), torch.ones(N)
+    got = lm().distill(z.cuda(), ids.cuda(), u.cuda(), tail=True, weight=1.0)
+    assert bool((got.log_tail == NEG).all()) and bool((got.loss == INF).all())
+    want, tol = far_distill_grad(z, ids, u, 1.0, True, w)
+    near(got.grad, want, tol)
+    near(lm().distill_grad(z.cuda(), ids.cuda(), u.cuda(), got.lse, 1.0, tail=True, log_tail=got.log_tail), want, tol)
+
+
 # ------------------------------------------------------------------ statistics on both sides of the range of one multiply-add
 @pytest.mark.parametrize("sign", [1.0, -1.0])
 @pytest.mark.parametrize("rising", [False, True])
