@@ -1097,10 +1097,13 @@ constexpr int SMS = 148;
 struct Shape { int nt, blocks; size_t smem; bool keep; };
 
 // Threads of a row's block: few enough that a thread has some eight vectors at least (its share of the row's last steps is
-// dear: 65536 rows of 1000 take 102 us with 128 threads, 55 with 32), and as many as bound the K-th alternative well
+// dear: 65536 rows of 1000 take 102 us with 128 threads, 55 with 32), and a quarter more than alternatives, whose K-th the
+// K-th largest of the threads' maxima bounds: with as many threads as alternatives it is the smallest of the maxima, and
+// far too many elements reach it.  16384 rows of 4000 bf16, us with 64, 128 and 256 threads: K = 20 84, 105, 191; 48
+// 140, 141, 211; 64 272, 181, 244; 100 -, 232, 316; 128 -, 447, 396
 int threads_for(long long vectors, int K) {
-    const int least = K == 0 ? 32 : K <= 20 ? 64 : K <= 64 ? 128 : MAX_THREADS;
-    int nt = MAX_THREADS;
+    int least = K == 0 ? 32 : 64, nt = MAX_THREADS;
+    while (least < K + K / 4) least *= 2;
     while (nt > least && vectors <= nt * 8) nt /= 2;
     return nt;
 }
