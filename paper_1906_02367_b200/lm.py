@@ -79,17 +79,25 @@ def _done(rc, what):
 
 
 def _rows(t, what):
-    """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one."""
+    """Stride between the rows of a tensor whose last dimension is contiguous and whose others flatten into one.
+    (Dimensions of one element have no stride; a single row uses none, and gets one that keeps wide accesses.)"""
     shape, stride = t.shape, t.stride()
+    D = shape[-1]
+    if len(shape) == 2 and stride[1] == 1 and D:
+        return stride[0] if shape[0] > 1 else (D + 15) // 16 * 16
     if t.numel() == 0:
-        return shape[-1]
-    if stride[-1] != 1 and shape[-1] > 1:
+        return D
+    if stride[-1] != 1 and D > 1:
         raise ValueError(f"{what} needs rows with unit stride")
-    outer = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n > 1]       # (a dimension of one element has no stride)
-    for (_, s), (n, inner) in zip(outer, outer[1:]):
-        if s != inner * n:
-            raise ValueError(f"{what}: leading dimensions must flatten into rows of one stride")
-    return outer[-1][1] if outer else (shape[-1] + 15) // 16 * 16            # (a single row: none is used; one that keeps wide accesses)
+    row = outer = None                                   # the rows' stride; the one that the next dimension has to have
+    for i in range(len(shape) - 2, -1, -1):
+        if shape[i] > 1:
+            if row is None:
+                row = outer = stride[i]
+            elif stride[i] != outer:
+                raise ValueError(f"{what}: leading dimensions must flatten into rows of one stride")
+            outer *= shape[i]
+    return (D + 15) // 16 * 16 if row is None else row
 
 
 def _vector(t, n, what, dtype=torch.float32):

@@ -94,6 +94,10 @@ def test_dimensions_of_one_element_have_no_stride(calls):
     assert calls[-1][1][4] >= 10
     with pytest.raises(ValueError):                      # every other element
         lm.embed(tok, table, out=torch.zeros(B, 1, 2 * D)[..., ::2])
+    # expanded dimensions: rows of stride 0 are the library's to refuse, they are not taken for rows side by side
+    assert lm._rows(torch.zeros(1, 1, D).expand(2, 3, D), "rows") == 0
+    with pytest.raises(ValueError):
+        lm._rows(torch.zeros(2, 1, D).expand(2, 3, D), "rows")
     with pytest.raises(ValueError):                      # rows whose two dimensions do not flatten
         lm.embed(torch.zeros((2, 2), dtype=torch.int64), table, out=torch.zeros(2, 3, D)[:, :2])
 
