@@ -111,3 +111,22 @@ def test_tiles_of_a_long_list_are_few():
         chunks = R * (N // 64 + 1)
         rest = L.qs_embed_grad_bytes(R, N, 128000, 1) - 16 * R * N - chunks * (2 * 256 * 4 + 4) - R * 128000
         assert rest <= 2 * R * 2048 * 512 * 4 + 1024, (R, N, rest)
+
+
+def test_strides_of_rows_address_the_same_elements():
+    """Whatever stride is taken for a tensor of any shape and strides, the rows found with it are the tensor's."""
+    g, base, taken = torch.Generator().manual_seed(3), torch.arange(4000), 0
+    pick = lambda values: values[int(torch.randint(0, len(values), (1,), generator=g))]  # noqa: E731
+    for _ in range(3000):
+        dims = pick((1, 2, 3, 4))
+        shape, stride = [pick((1, 1, 2, 3)) for _ in range(dims)], [pick((0, 1, 2, 3, 4, 6, 9, 12, 18)) for _ in range(dims)]
+        stride[-1] = pick((1, 1, stride[-1]))
+        t = torch.as_strided(base, shape, stride)
+        try:
+            step = lm._rows(t, "rows")
+        except ValueError:
+            continue
+        flat = t.reshape(-1, shape[-1])
+        assert torch.equal(flat, torch.stack([base[i * step:i * step + shape[-1]] for i in range(len(flat))])), (shape, stride, step)
+        taken += 1
+    assert taken > 1000
