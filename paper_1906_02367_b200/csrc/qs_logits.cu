@@ -726,13 +726,13 @@ struct Entries {
 struct Slope {
     float w, in, out;                      // weight * scale, Q + q_T, and out = f / w
     float rest;
-    float out_m, out_by;                   // largest logit outside the ids; one over the sum relative to it, 0 if there is none
     int thin, empty;
+};
+// with what the shares take: the largest logit outside the ids; one over the sum relative to it, 0 if there is none
+struct Shares : Slope {
+    float out_m, out_by;
 
-    __device__ __forceinline__ void set_out(float m, float sum) {
-        out_m = shift_of(m);
-        out_by = sum == 0.0f ? 0.0f : 1.0f / sum;
-    }
+    __device__ __forceinline__ Shares(const Slope& s, Stat out) : Slope(s), out_m(shift_of(out.m)), out_by(out.s == 0.0f ? 0.0f : 1.0f / out.s) {}
 };
 template <bool TAIL>
 __device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, bool empty, float log_tail) {
@@ -740,7 +740,6 @@ __device__ __forceinline__ Slope slope_of(float w, const TeacherShared& t, bool 
     s.w = w;
     s.in = t.bad ? quiet_nan() : t.Q + t.rest;
     s.rest = t.rest;
-    s.out_m = s.out_by = 0.0f;
     s.thin = TAIL && t.rest > 0.0f && log_tail < -60.0f;
     s.out = !TAIL ? s.in : s.thin ? s.in : s.in - (t.rest > 0.0f ? t.rest * ex2(-log_tail * LOG2E) : t.rest);
     s.empty = empty;
@@ -760,7 +759,7 @@ __device__ __forceinline__ float factor(const Slope& s, float norm) {
 }
 // rows whose p_T is too small for the quotient: the shares instead
 template <class T>
-__device__ __noinline__ uint4 share_vec(uint4 q, const f2* d, const Slope& s, float norm, float c2) {
+__device__ __noinline__ uint4 share_vec(uint4 q, const f2* d, const Shares& s, float norm, float c2) {
     constexpr int P = Vec<T>::E / 2;
     f2 g[P];
     const float f = factor(s, norm), c = s.out_by > 0.0f ? -s.w * s.rest * s.out_by : 0.0f;
@@ -912,7 +911,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
     }
     if (rank >= readers) return;                   // nothing is sent to this block
     Stat v{};
-    float log_tail = 0.0f, out_m = 0.0f, out_s = 0.0f, out_gap = 0.0f;
+    float log_tail = 0.0f, out_gap = 0.0f;
     bool empty = false;
     if (warp == 0) {
         v = join_parts(part, warps * blocks, c2);
@@ -923,8 +922,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             const Stat x = rescale(v, m, c2), y = rescale(in, m, c2);
             const float s = x.s + y.s;
             // log of the share outside: near 1 the difference of two logs would cancel
-            out_s = final_stat(v, c2).s;
-            out_m = v.m;
+            const float out_s = final_stat(v, c2).s;
             const bool none = is_empty(v);
             out_gap = v.m - m;
             v = final_stat(Stat{m, s, 0.0f}, c2);
@@ -935,8 +933,7 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
             v = final_stat(v, c2);
         }
         empty = is_empty(v);
-        Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
-        if (TAIL) s.set_out(out_m, out_s);
+        const Slope s = slope_of<TAIL>(t.w, t, empty, log_tail);
         if (lane == 0) {
             row_m = shift_of(v.m);
             row_by = empty ? 0.0f : 1.0f / v.s;
@@ -1016,8 +1013,10 @@ __global__ void __launch_bounds__(MAX_THREADS, 4) distill_kernel(const RowArgs a
                 else store_edge(r, out, vec, g);
             }
         };
-        if (thin) each([&](const uint4& q, const f2* d) { return share_vec<T>(q, d, s, norm, c2); });
-        else each([&](const uint4&, const f2* d) { return slope_vec<T>(d, f); });
+        if (thin) {
+            const Shares by_share(s, final_stat(join_parts(part, warps * blocks, c2), c2));
+            each([&](const uint4& q, const f2* d) { return share_vec<T>(q, d, by_share, norm, c2); });
+        } else each([&](const uint4&, const f2* d) { return slope_vec<T>(d, f); });
     }
     __syncthreads();                               // the ids' places are written last
 #pragma unroll
@@ -1035,8 +1034,7 @@ __device__ __noinline__ void distill_grad_again(const RowArgs& a, const TeacherS
     const Share<T> r(a.logits, a.stride, n, a.V, rank, a.parts);
     T* out = static_cast<T*>(a.grad) + n * a.grad_stride;
     const RowStats x = stats_again<T, TAIL>(a, r, &t, sh, rank);
-    Slope s = slope_of<TAIL>(t.w, t, is_empty(x.all), TAIL ? a.in_log_tail[n] : 0.0f);
-    if (TAIL) s.set_out(x.out.m, x.out.s);
+    const Shares s(slope_of<TAIL>(t.w, t, is_empty(x.all), TAIL ? a.in_log_tail[n] : 0.0f), x.out);
     const bool thin = TAIL && s.thin && !s.empty;
     const float m = shift_of(x.all.m), ls = s.empty ? -LOW_EXP : logf(x.all.s), f = factor(s, 1.0f), c2 = a.scale * LOG2E;
     const f2 scale = make_f2(a.scale, a.scale), l2e = make_f2(LOG2E, LOG2E), mm = make_f2(-m, -m), mls = make_f2(-ls, -ls);
