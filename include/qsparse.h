@@ -395,6 +395,7 @@ void qs_destroy(qs_ctx* ctx);
  *     *status (device, one int the caller has set to 0, or NULL).
  *   - Pointers are aligned to their element type; strides are counted in elements.  16-byte
  *     aligned rows of equal phase are the fast case; every other one is correct.
+ *   - What a call writes overlaps nothing else that it reads or writes, except where it says so.
  *   - Results do not depend on the order in which blocks run.
  */
 enum { QS_F32 = 0, QS_BF16 = 1, QS_F16 = 2 };

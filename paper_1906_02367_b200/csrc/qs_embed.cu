@@ -14,8 +14,9 @@
 // joined in order.  The rows that no token names are known after the first look at the tokens (a byte
 // per row); they are set to zero by blocks beside those that sum, so that reads and writes share the
 // memory, and, as far as there is time, beside those that sort.  At 8 workers x 4096 tokens, tables of
-// 32000 x 1024, bf16 in: 188 us, 5.9 TB/s of what has to be read and written; 65536 tokens, 128000 x
-// 2048: 248 us, 5.3 TB/s.
+// 32000 x 1024, bf16 in: 187 us, 6.0 TB/s of what has to be read and written; 65536 tokens, 128000 x
+// 2048: 249 us, 5.3 TB/s.  Added to what is there (29 us' worth of bytes in the first case), nothing hides the sort and
+// the joins: 88 us.
 #include "qs_lm.cuh"
 
 namespace {
@@ -100,7 +101,8 @@ template <> __device__ __forceinline__ void store_eight<float>(float* p, const f
 constexpr int UNITS = 4;                       // 8-column units per lane in flight together
 
 // Rows 16-byte aligned on both sides.  1 << a.lanes lanes share a row, so that a warp takes a long row or several short
-// ones: one token and one address per lane, 24 to 64 bytes of table in flight per unit
+// ones: one token and one address per lane, 64 (2-byte types) or 128 bytes of table in flight per lane.  8 x 4096 rows of 1024
+// fp32 to bf16: 25 us; rows of any alignment, by the kernel after this one, 39
 template <class TW, class TO>
 __global__ void __launch_bounds__(256) embed_wide_kernel(const EmbedArgs a) {
     const int lane = (int)(threadIdx.x & ((1u << a.lanes) - 1u));
@@ -240,7 +242,9 @@ __device__ __forceinline__ void warp_zero(float* dst, long long n) {
 // handed out in order (`most` at most to a block), so that the writes go through memory in order and no block is left with
 // more than its share: 7.2 TB/s, where a warp on 8 KB of its own writes 5.9.  Rows that are no whole units (EVEN false)
 // have the units counted from the 16-byte boundary at or before the table, `lead` floats off; one that two rows share is
-// written by elements unless both become zero
+// written by elements unless both become zero, by a mask of its elements (16384 tokens, 50000 x 257: 33.0 us, 35.3 with a
+// second look at the names of such units only; where such units are few that is the faster one: 8 x 4096 tokens,
+// 32000 x 1024 at an odd place, 197 us against 208)
 constexpr int PIECE = 2048;                // 16-byte units
 template <int NT, bool EVEN>
 __device__ void zero_pieces(const GradArgs& a, int most) {
@@ -510,8 +514,8 @@ static_assert(ONE_TILE <= SORT_THREADS, "one place per thread");
 // ------------------------------------------------------------------ gradient: sums of the runs
 // A lane's 8 sums into the table's row.  IN: the sums' columns are those of 16-byte loads; OUT: rows 16-byte aligned.  Where
 // only the first holds (a worker's table at an odd place of the batch), the sums change lanes through the warp's 256
-// floats of shared memory, so that single-element stores lie side by side: 208 us for the 8 workers' tables above from a
-// place that is odd, 331 with single-element loads as well
+// floats of shared memory, so that single-element stores lie side by side: 211 us for the 8 workers' tables above from a
+// place that is odd (188 from an aligned one), 331 with single-element loads as well
 template <bool IN, bool OUT, int SIZE>
 __device__ __forceinline__ void write_sum(const GradArgs& a, float* dst, int c0, const float (&sum)[8], float* swap) {
     const int lane = threadIdx.x & 31;
@@ -874,7 +878,7 @@ SortPlan sort_plan(int R, int64_t N, int64_t V, int64_t D) {
     const int64_t tile = (int64_t)s.items * SORT_THREADS;
     s.tiles = (int)((N + tile - 1) / tile);
     s.col_tiles = (int)((D + COLS - 1) / COLS);
-    // chunks as long as 64 places while they give every SM some 16 warps
+    // chunks as long as 64 places while they give every SM of a B200 some 16 warps (the size of the workspace asks no device)
     s.chunk = 8;
     while (s.chunk < 64 && R * N / (2 * s.chunk) * s.col_tiles >= 148 * 16) s.chunk *= 2;
     s.chunks = (int)((N + s.chunk - 1) / s.chunk);
@@ -965,8 +969,9 @@ int qs_embed_grad(int R, int64_t N, int64_t V, int64_t D, const void* tokens, in
     // (counters of 32 bits, with a piece to spare)
     a.pieces = row_stride == D && D >= 4 && V * D < (1ll << 32) - (1ll << 16);
     if (a.pieces && aligned_to(grad_table, 16) && D % 4 == 0 && worker_stride % 4 == 0) a.pieces = 2;
-    // (without whole units, where there is no longer sort to be beside, the pieces' start costs more than their order gains below
-    // 128 MB: 509 tokens, fp32, 8191 x 257: 14.3 us in pieces, 13.1 by rows; 100000 x 2049: 130 and 148)
+    // (without whole units, where there is no longer sort to be beside, the pieces' start costs more than their order gains in
+    // small tables.  509 tokens, fp32, rows of 1025, us in pieces and by rows: 32 MB 20.6, 18.5; 128 MB 35.1, 34.7; 192 MB 45.1,
+    // 46.7; 800 MB 139, 169.  Of 257 columns: 128 MB 38.3, 37.1; 256 MB 60.1, 59.9; 800 MB 155, 165)
     else if (a.pieces && p.one_tile && R * V * D < 1ll << 25) a.pieces = 0;
     if (N == 0 && accumulate) return QS_OK;
     // (the one-tile sort sets its own marks to zero)

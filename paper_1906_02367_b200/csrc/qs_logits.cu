@@ -11,12 +11,12 @@
 //
 // All of these are bound by the memory that holds the logits: each must read the row, and the gradients write
 // one.  So a row is read once.  Statistics and alternatives are taken as the vectors come by, with plain loads of
-// many resident warps (64 warps of 32 registers read 6.8 TB/s with all the arithmetic; the same loop behind a ring of
-// bulk copies and 24 warps, 4.5).  The loss that also gives its gradient keeps the row in the shared memory of a cluster's
-// blocks, one bulk copy each, until the statistics are joined.  The backward calls, which start from a saved lse,
-// are one pass per vector.  bf16 rows of 128000: statistics alone 374 us for 8192 rows (5.6 TB/s), the loss and its gradient
-// 650 us for 6144 (4.8 TB/s; the two halves of a block's life, read and write, overlap only with other blocks' halves);
-// 64 alternatives, 4096 rows of 50003: 131 us (3.1 TB/s; finding and ranking them takes as long as reading).
+// many resident warps (48 an SM of 40 registers, 40 of 48 with alternatives; the same loop behind a ring of bulk copies and
+// 24 warps took 480 us where this took 363).  The loss that also gives its gradient keeps the row in the shared memory of a
+// cluster's blocks, one bulk copy each, until the statistics are joined.  The backward calls, which start from a saved
+// lse, are one pass per vector.  bf16 rows of 128000: statistics alone 389 us for 8192 rows (5.4 TB/s), the loss and its
+// gradient 692 us for 6144 (4.5 TB/s; a block reads, computes and writes in turn, and only other blocks fill the gaps);
+// 64 alternatives, 4096 rows of 50003: 133 us (3.1 TB/s; finding and ranking them takes as long as reading).
 #include <algorithm>
 #include <cstdlib>
 
