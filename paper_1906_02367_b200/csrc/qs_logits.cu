@@ -722,7 +722,8 @@ struct Entries {
 
 // What turns a row's probabilities into its gradient: outside the ids f p with f = w (Q + q_T - q_T / p_T), or, where
 // p_T is too small for the quotient, w p (Q + q_T) - w q_T share with the column's share of p_T.  That share is taken from
-// the statistics of the columns outside: log p - log p_T would be the difference of two large numbers
+// the statistics of the columns outside: log p - log p_T would be the difference of two large numbers.  At the bound, e^-60,
+// a p below the smallest normal number, which counts as 0, would have had 1e-12 of the weight
 struct Slope {
     float w, in, out;                      // weight * scale, Q + q_T, and out = f / w
     float rest;
