@@ -398,7 +398,7 @@ void qs_destroy(qs_ctx* ctx);
  *   - What a call writes overlaps nothing else that it reads or writes, except where it says so.
  *   - Results do not depend on the order in which blocks run.
  */
-enum { QS_F32 = 0, QS_BF16 = 1, QS_F16 = 2 };
+enum { QS_F32 = 0, QS_BF16 = 1, QS_F16 = 2, QS_E4M3 = 3 };
 enum { QS_I32 = 0, QS_I64 = 1 };
 
 /*
@@ -509,6 +509,119 @@ int qs_distill_grad(int64_t N, int64_t V, int K, const void* logits, int type, i
                     float scale, float teacher_scale, int tail, const float* lse,
                     const float* log_tail, const float* weight, float weight_all, void* grad,
                     int64_t grad_stride, int* status, void* cuda_stream);
+
+/*
+ * Operators between the two ends: what a residual block of a network computes, for R workers with
+ * weights of their own (stretches of the rows of the R x d batch) or one set for all, under the
+ * rules above.  Rows of activations are R N of them, worker r's N after worker r - 1's.  QS_E4M3
+ * is an 8-bit float (1 sign, 4 exponent, 3 fraction bits; largest 448) that stands for itself
+ * times its row's scale; it is a type only where a call says so.
+ *
+ * qs_rms_norm — root-mean-square norm of rows of D, with the residual's addition in front:
+ *   h = x + residual, rounded to the type of x and written to hidden (residual and hidden both
+ *   NULL: h = x);  rstd = 1 / sqrt(mean h^2 + eps);  out = h rstd w_r.
+ *   weight (NULL: ones): worker r's D at weight + r weight_worker_stride, of fp32 or of type.
+ *   out_type: type, or QS_E4M3: then with y = h rstd w (fp32) and s = max(max |y| / 448, 2^-126)
+ *   out = y / s rounded to 8 bits and scale[row] = s; a row with a NaN or an infinity in y has a
+ *   scale of NaN.  rstd: one per row, or NULL.
+ *   eps > 0.  Squares are summed in fp32: an h beyond 1.8e19 makes its row's sum infinite, rstd 0.
+ *   hidden may take the place of x or residual, out that of x or residual (row for row, the same
+ *   stride), or other columns of their rows.
+ * qs_quantize_rows — rows into 8 bits with a scale per row, as above with y = x.
+ */
+int qs_rms_norm(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_stride,
+                const void* residual, int64_t residual_stride, const void* weight, int weight_type,
+                int64_t weight_worker_stride, float eps, void* hidden, int64_t hidden_stride,
+                void* out, int out_type, int64_t out_stride, float* scale, float* rstd,
+                void* cuda_stream);
+int qs_quantize_rows(int64_t N, int64_t D, const void* x, int type, int64_t x_stride, void* out,
+                     int64_t out_stride, float* scale, void* cuda_stream);
+
+/*
+ * qs_rms_norm_grad — gradient of qs_rms_norm (its output not in 8 bits) with n = hidden rstd:
+ *   out = grad_hidden + rstd (w g - n mean(w g n)),  the gradient of h, so of x and of residual;
+ *   grad_weight_r = sum over worker r's rows of g n  (fp32; accumulate != 0: added to it).
+ *   grad_hidden (NULL: none): what arrives at h by the residual stream.  grad_weight may be NULL;
+ *   it takes qs_rms_norm_grad_bytes(R, N, D) of 16-byte aligned work, and its sums' order depends
+ *   on the sizes alone.  out may take the place of grad, hidden or grad_hidden.
+ */
+int64_t qs_rms_norm_grad_bytes(int R, int64_t N, int64_t D);
+int qs_rms_norm_grad(int R, int64_t N, int64_t D, const void* grad, int type, int64_t grad_stride,
+                     const void* hidden, int64_t hidden_stride, const float* rstd,
+                     const void* weight, int weight_type, int64_t weight_worker_stride,
+                     const void* grad_hidden, int64_t grad_hidden_stride, void* out,
+                     int64_t out_stride, float* grad_weight, int64_t grad_weight_worker_stride,
+                     int accumulate, void* work, int64_t work_bytes, void* cuda_stream);
+
+/*
+ * qs_dropout — out = residual + (word >= floor(p 2^32) ? x c : 0), c = fl(1 / (1 - p)), 0 <= p < 1;
+ * residual may be NULL.  A dropped element counts as 0 whatever it holds.  Element e = n D + d of
+ * worker r draws word e & 3 of Philox4x32-10 with key = seed and counter = (e >> 2, worker + r,
+ * round's low 32 bits, layer << 16 | round >> 32 << 8 | 2): the generator and keying of the
+ * sparsifier and the quantizer, in a stream of its own.  No mask is kept: the gradient with
+ * respect to x is the same call on the gradient, without a residual.
+ *   round < 2^40, 0 <= layer < 2^16, N D <= 2^34.  out may take the place of x or of residual.
+ */
+int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_stride,
+               const void* residual, int64_t residual_stride, double p, uint64_t seed,
+               uint64_t round, int worker, int layer, void* out, int64_t out_stride,
+               void* cuda_stream);
+
+/*
+ * qs_linear — z = x w_r^T + bias_r;  out = act(z) + residual;  pre = z where it is not NULL.
+ *   x: R M rows of K; w: N rows of K per worker, at w + r w_worker_stride (0: one for all);
+ *   out, residual (NULL: none), pre (NULL: not wanted): R M rows of N, all of out_type.
+ *   x_type QS_F32, QS_BF16, QS_F16: w of the same type or QS_F32, which is then rounded to x_type;
+ *   out_type is x_type or QS_F32.  x_type QS_E4M3: w too, x_scale (R M) and w_scale (R N, or N with
+ *   one w for all) multiply the sums, out_type any other.  The scales are NULL otherwise.
+ *   bias (NULL: none): N of bias_type per worker.  Sums, bias and activation are fp32, rounded once.
+ *   Products of 16- and 8-bit elements are exact.  fp32 operands are cut into three parts of 8
+ *   bits of significand, and products of parts below 2^-24 of the whole are left out; with an
+ *   infinity among them, the results that it enters are not finite (some NaN where the sum would be
+ *   infinite).  Small products (under a million operations) are plain fp32.
+ *   activation: QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU z / (1 + e^-z), QS_ACT_GELU z Phi(z).
+ *   work: 256-byte aligned, qs_linear_bytes(...) bytes for the same arguments (their alignment
+ *   counts: operands off 16-byte boundaries are laid out anew), else QS_CAPACITY; may be NULL for 0.
+ *   residual may be out itself.  A wait on the device is bounded as in qs_distill; what depends on
+ *   one that ran out is NaN, and *status becomes QS_TIMEOUT.
+ * qs_linear_grad_input  — out = dz w_r      (R M rows of K, of type), dz: R M rows of N.
+ * qs_linear_grad_weight — out_r = dz_r^T x_r (N rows of K per worker, fp32 or type; accumulate:
+ *   added to it).  Workers' results must not overlap.
+ * qs_activation_grad    — out = grad act'(pre), rounded to type (NULL: not wanted), and
+ *   grad_bias_r = the sum over worker r's rows of grad act'(pre) before that rounding (NULL: not
+ *   wanted; accumulate: added to it; takes 16-byte aligned work).  relu has slope 0 at 0.
+ *   out may take the place of grad or pre.
+ * M <= 2^28 in all, N, K <= 2^24, workers x tiles of 128 x 128 <= 2^24, else QS_TOO_LARGE.
+ */
+enum { QS_ACT_NONE = 0, QS_ACT_RELU = 1, QS_ACT_SILU = 2, QS_ACT_GELU = 3 };
+int64_t qs_linear_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type,
+                        int64_t x_stride, const void* w, int w_type, int64_t w_worker_stride,
+                        int64_t w_stride);
+int qs_linear(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride,
+              const float* x_scale, const void* w, int w_type, int64_t w_worker_stride,
+              int64_t w_stride, const float* w_scale, const void* bias, int bias_type,
+              int64_t bias_worker_stride, int activation, const void* residual,
+              int64_t residual_stride, void* pre, int64_t pre_stride, void* out, int out_type,
+              int64_t out_stride, void* work, int64_t work_bytes, int* status, void* cuda_stream);
+int64_t qs_linear_grad_input_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
+                                   int64_t dz_stride, const void* w, int w_type,
+                                   int64_t w_worker_stride, int64_t w_stride);
+int qs_linear_grad_input(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
+                         int64_t dz_stride, const void* w, int w_type, int64_t w_worker_stride,
+                         int64_t w_stride, void* out, int64_t out_stride, void* work,
+                         int64_t work_bytes, int* status, void* cuda_stream);
+int64_t qs_linear_grad_weight_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
+                                    int64_t dz_stride, const void* x, int64_t x_stride);
+int qs_linear_grad_weight(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
+                          int64_t dz_stride, const void* x, int64_t x_stride, void* out,
+                          int out_type, int64_t out_worker_stride, int64_t out_stride,
+                          int accumulate, void* work, int64_t work_bytes, int* status,
+                          void* cuda_stream);
+int64_t qs_activation_grad_bytes(int R, int64_t M, int64_t N);
+int qs_activation_grad(int R, int64_t M, int64_t N, const void* grad, int type, int64_t grad_stride,
+                       const void* pre, int64_t pre_stride, int activation, void* out,
+                       int64_t out_stride, float* grad_bias, int64_t grad_bias_worker_stride,
+                       int accumulate, void* work, int64_t work_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ QS_STATIC_MAX_D = 1 << 20
 QS_TOPK, QS_RANDK = 0, 1
 QS_QSGD, QS_QSGD_SCALED, QS_SIGN_L1, QS_NONE, QS_SIGN_L2, QS_MINMAX = 0, 1, 2, 3, 4, 5
 QS_ROUND_AUTO = 2**64 - 1
-QS_F32, QS_BF16, QS_F16 = 0, 1, 2
+QS_F32, QS_BF16, QS_F16, QS_E4M3 = 0, 1, 2, 3
+QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU, QS_ACT_GELU = 0, 1, 2, 3
 QS_I32, QS_I64 = 0, 1
 QS_MAX_TOP = 128
 
@@ -31,6 +32,9 @@ EXPORTS = [
     "qs_get_stats", "qs_enable_phase_timing", "qs_get_phase_timing", "qs_get_stage_trace", "qs_unpack_accumulate_static",
     "qs_gap_words", "qs_recode_gaps", "qs_decode_gaps", "qs_destroy",
     "qs_embed", "qs_embed_grad", "qs_embed_grad_bytes", "qs_token_logp", "qs_token_logp_grad", "qs_distill", "qs_distill_grad",
+    "qs_rms_norm", "qs_quantize_rows", "qs_rms_norm_grad_bytes", "qs_rms_norm_grad", "qs_dropout", "qs_linear_bytes", "qs_linear",
+    "qs_linear_grad_input_bytes", "qs_linear_grad_input", "qs_linear_grad_weight_bytes", "qs_linear_grad_weight",
+    "qs_activation_grad_bytes", "qs_activation_grad",
 ]
 
 _lib = None
@@ -92,6 +96,23 @@ def lib():
         L.qs_token_logp_grad.argtypes = [i64, i64, vp, i32, i64, vp, i32, f32, vp, vp, vp, f32, vp, vp, i64, vp, vp]
         L.qs_distill.argtypes = [i64, i64, i32, vp, i32, i64, vp, i32, vp, i32, f32, f32, i32, vp, vp, vp, vp, f32, vp, i64, vp, vp]
         L.qs_distill_grad.argtypes = [i64, i64, i32, vp, i32, i64, vp, i32, vp, i32, f32, f32, i32, vp, vp, vp, f32, vp, i64, vp, vp]
+        L.qs_rms_norm.argtypes = [i32, i64, i64, vp, i32, i64, vp, i64, vp, i32, i64, f32, vp, i64, vp, i32, i64, vp, vp, vp]
+        L.qs_quantize_rows.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, vp]
+        L.qs_rms_norm_grad_bytes.argtypes = [i32, i64, i64]
+        L.qs_rms_norm_grad.argtypes = [i32, i64, i64, vp, i32, i64, vp, i64, vp, vp, i32, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp]
+        L.qs_dropout.argtypes = [i32, i64, i64, vp, i32, i64, vp, i64, C.c_double, u64, u64, i32, i32, vp, i64, vp]
+        operands = [i32, i64, i64, i64, vp, i32, i64, vp, i32, i64, i64]
+        L.qs_linear_bytes.argtypes = operands
+        L.qs_linear.argtypes = [i32, i64, i64, i64, vp, i32, i64, vp, vp, i32, i64, i64, vp, vp, i32, i64, i32, vp, i64, vp, i64, vp, i32, i64,
+                                vp, i64, vp, vp]
+        L.qs_linear_grad_input_bytes.argtypes = operands
+        L.qs_linear_grad_input.argtypes = operands + [vp, i64, vp, i64, vp, vp]
+        L.qs_linear_grad_weight_bytes.argtypes = [i32, i64, i64, i64, vp, i32, i64, vp, i64]
+        L.qs_linear_grad_weight.argtypes = [i32, i64, i64, i64, vp, i32, i64, vp, i64, vp, i32, i64, i64, i32, vp, i64, vp, vp]
+        L.qs_activation_grad_bytes.argtypes = [i32, i64, i64]
+        L.qs_activation_grad.argtypes = [i32, i64, i64, vp, i32, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp]
+        for f in (L.qs_rms_norm_grad_bytes, L.qs_linear_bytes, L.qs_linear_grad_input_bytes, L.qs_linear_grad_weight_bytes, L.qs_activation_grad_bytes):
+            f.restype = i64
         L.qs_destroy.argtypes = [vp]
         L.qs_destroy.restype = None
         _lib = L

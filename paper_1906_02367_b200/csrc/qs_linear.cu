@@ -1,0 +1,856 @@
+// Matrix products of a network's layers, with bias, activation and residual in the same kernel, and their gradients:
+//
+//   z = x w^T (+ bias);  out = act(z) (+ residual);  dx = dz w;  dw = dz^T x;  dz = g act'(z)
+//
+// All three products are one kernel's: D[m, n] = sum over k of A[m, k] B[n, k], per worker, where an operand lies along k
+// or across it (w in dx, both in dw): the tensor maps and the matrix unit's descriptors take either.
+#include <algorithm>
+#include <cstdlib>
+
+#include "qs_parts.cuh"
+
+namespace qs {
+namespace {
+
+typedef __nv_bfloat16 bf16;
+
+// ------------------------------------------------------------------ what follows the sums
+struct Finish {
+    long long M, N;                                  // of one worker
+    const void* bias; int bias_type; long long bias_worker;
+    int act;
+    const void* res; long long res_stride;           // rows of all workers, one after the other
+    void* pre; long long pre_stride;
+    void* out; int type; long long out_stride, out_worker;
+    const float* a_scale; const float* b_scale;      // per row and per column, of 8-bit operands
+    int accumulate;                                  // added to what `out` holds
+    int vec;                                         // rows of 16-byte vectors all around
+};
+
+__device__ __forceinline__ float rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float logistic(float z) { return rcp(1.0f + ex2(-LOG2E * z)); }
+__device__ __forceinline__ float activate(int act, float z) {
+    if (act == QS_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (act == QS_ACT_SILU) return z * logistic(z);
+    if (act == QS_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+    return z;
+}
+__device__ __forceinline__ float slope(int act, float z) {
+    if (act == QS_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (act == QS_ACT_SILU) {
+        const float p = logistic(z);
+        return p * __fmaf_rn(z, 1.0f - p, 1.0f);
+    }
+    if (act == QS_ACT_GELU) return __fmaf_rn(z * 0.39894228f, ex2(-0.5f * LOG2E * z * z), 0.5f * (1.0f + erff(z * 0.70710678f)));
+    return 1.0f;
+}
+
+__device__ __forceinline__ float element(const void* p, int type, long long i) {
+    return type == QS_F32 ? static_cast<const float*>(p)[i] : type == QS_BF16 ? to_float(static_cast<const bf16*>(p)[i]) : to_float(static_cast<const __half*>(p)[i]);
+}
+
+template <int V, class T>
+__device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, long long n, float (&v)[V]) {
+    const long long row = r * f.M + m;
+    if (f.pre) store_vec<V>(static_cast<T*>(f.pre) + row * f.pre_stride + n, v);
+    if (f.act != QS_ACT_NONE)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = activate(f.act, v[i]);
+    if (f.res) {
+        float t[V];
+        load_vec<V>(t, static_cast<const T*>(f.res) + row * f.res_stride + n);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += t[i];
+    }
+    T* out = static_cast<T*>(f.out) + r * f.out_worker + m * f.out_stride + n;
+    if (f.accumulate) {
+        float t[V];
+        load_vec<V>(t, out);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += t[i];
+    }
+    store_vec<V>(out, v);
+}
+// V columns from n on of row m: the sums in v, and what belongs to the columns
+template <int V> struct Columns { float bias[V], scale[V]; };
+template <int V>
+__device__ __forceinline__ void load_columns(const Finish& f, int r, long long n, Columns<V>& c) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const bool in = n + i < f.N;
+        c.bias[i] = f.bias && in ? element(f.bias, f.bias_type, r * f.bias_worker + n + i) : 0.0f;
+        c.scale[i] = f.b_scale && in ? f.b_scale[r * f.N + n + i] : 1.0f;
+    }
+}
+template <int V>
+__device__ __forceinline__ void finish(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c) {
+    if (f.a_scale) {
+        const float s = f.a_scale[r * f.M + m];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = v[i] * s * c.scale[i];
+    }
+    if (f.bias)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += c.bias[i];
+    if (f.type == QS_F32) finish_as<V, float>(f, r, m, n, v);
+    else if (f.type == QS_BF16) finish_as<V, bf16>(f, r, m, n, v);
+    else finish_as<V, __half>(f, r, m, n, v);
+}
+
+// ------------------------------------------------------------------ operands for the matrix unit
+// Operands that the tensor maps cannot take as they lie (another type, rows off the 16-byte boundary) are laid out in the
+// workspace: fp32 rounded to the other operand's 16 bits, or cut into three bf16 parts x = x0 + x1 + x2, each the rest of
+// the ones before it rounded: 24 bits in all.
+struct LayArgs {
+    const void* src; int src_type; long long src_stride, src_worker;
+    void* dst; int dst_type, planes; long long ld;   // (workers, planes, rows, ld)
+    long long rows, cols; int vec;
+};
+__device__ __forceinline__ bf16 part_of(float& v) {
+    bf16 p = __float2bfloat16_rn(v);
+    if (isinf(__bfloat162float(p)) && !isinf(v)) p = __float2bfloat16_rz(v);
+    const float f = __bfloat162float(p);
+    v = isinf(f) ? 0.0f : v - f;                     // (exact; a NaN stays one)
+    return p;
+}
+__global__ void __launch_bounds__(256) lay_kernel(const LayArgs a) {
+    const int size = a.dst_type == QS_E4M3 ? 1 : 2;
+    const long long units = a.ld / 8, r = blockIdx.y, items = a.rows * units;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
+        const long long row = i / units, c = (i - row * units) * 8, from = r * a.src_worker + row * a.src_stride + c;
+        if (size == 1) {
+            Pack<uint8_t, 8> q;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q.e[j] = c + j < a.cols ? static_cast<const uint8_t*>(a.src)[from + j] : 0;
+            *reinterpret_cast<Pack<uint8_t, 8>*>(static_cast<uint8_t*>(a.dst) + (r * a.rows + row) * a.ld + c) = q;
+            continue;
+        }
+        if (a.src_type != QS_F32) {                  // 16 bits as they are
+            Pack<uint16_t, 8> q;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q.e[j] = c + j < a.cols ? static_cast<const uint16_t*>(a.src)[from + j] : 0;
+            *reinterpret_cast<Pack<uint16_t, 8>*>(static_cast<uint16_t*>(a.dst) + (r * a.rows + row) * a.ld + c) = q;
+            continue;
+        }
+        float v[8];
+        if (a.vec && c + 8 <= a.cols) load_floats<8>(v, static_cast<const float*>(a.src) + from);
+        else
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = c + j < a.cols ? static_cast<const float*>(a.src)[from + j] : 0.0f;
+        if (a.dst_type == QS_F16) {
+            store_vec<8>(static_cast<__half*>(a.dst) + (r * a.rows + row) * a.ld + c, v);
+        } else {
+            for (int p = 0; p < a.planes; ++p) {
+                Pack<bf16, 8> q;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q.e[j] = a.planes == 1 ? __float2bfloat16_rn(v[j]) : part_of(v[j]);
+                *reinterpret_cast<Pack<bf16, 8>*>(static_cast<bf16*>(a.dst) + ((r * a.planes + p) * a.rows + row) * a.ld + c) = q;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ the product
+constexpr int TILE_M = 128;                          // rows of a block's part of a tile: the lanes of tensor memory
+constexpr int STAGES = 6;
+constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
+constexpr int PASS_BYTES = 8 * 4096;                 // 32 x 32 sums on their way from lanes to rows, per finishing warp
+
+struct GemmArgs {
+    int R;
+    long long M, N;
+    int tiles_m, tiles_n, splits, units;             // units of work: workers x splits x tiles
+    int k_blocks, k_step, pairs, iters;              // blocks of 128 bytes along k; pairs of parts; their product
+    int a_across, b_across;                          // operand lies across k
+    int a_worker, b_worker;                          // 0: one operand for all workers
+    int eight;                                       // 8-bit operands
+    uint32_t idesc;
+    float* part; long long part_ld;                  // splits > 1: (splits, R, M, part_ld) sums instead of results
+    unsigned long long limit;
+    int* status;
+    Finish f;
+};
+
+// parts of the operands whose products are added, the small ones first: what is left out is 2^-24 of the whole
+__device__ __forceinline__ int part_a(int pairs, int p) { return pairs == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
+__device__ __forceinline__ int part_b(int pairs, int p) { return pairs == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
+
+struct Unit { int r, split, tm, tn, it0, it1; };
+__device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
+    Unit t;
+    const int tiles = g.tiles_m * g.tiles_n;
+    const int rs = u / tiles;
+    int i = u - rs * tiles;
+    t.split = rs % g.splits;
+    t.r = rs / g.splits;
+    // bands of eight tile rows, so that the blocks at work share operands in the L2
+    const int band = i / (8 * g.tiles_n), rows = min(8, g.tiles_m - band * 8);
+    i -= band * 8 * g.tiles_n;
+    t.tn = i / rows;
+    t.tm = band * 8 + (i - t.tn * rows);
+    t.it0 = (int)((long long)g.iters * t.split / g.splits);
+    t.it1 = (int)((long long)g.iters * (t.split + 1) / g.splits);
+    return t;
+}
+
+template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return TILE_M * 128 + BN / CG * 128; }
+template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return STAGES * stage_bytes<CG, BN>() + PASS_BYTES + 1024; }
+
+// A tile of TILE_M CG x BN per cluster of CG blocks.  Copies (one thread per block) keep a ring of STAGES tiles of both
+// operands filling; one thread of the leading block issues the products into one of two accumulators; eight warps per
+// block take the other one out: they turn 32 x 32 sums through shared memory so that rows leave in whole sectors.
+template <int CG, int BN>
+__global__ void __launch_bounds__(GEMM_THREADS, 1)
+gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmArgs g) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_at;
+    constexpr int A_BYTES = TILE_M * 128, B_ROWS = BN / CG, STAGE = stage_bytes<CG, BN>();
+    uint8_t* ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 8 * CG);
+        mbar_init(&drained, 1);
+        fence_barrier_init();
+    }
+    if (warp == 2) tmem_alloc<CG>(&tmem_at, 2 * BN);
+    tc_fence_before();
+    if (CG == 2) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+    after_launch();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int c = 0;
+            bool fine = g.limit != 0;
+            for (int u = cluster; u < g.units && fine; u += clusters) {
+                const Unit t = unit_of(g, u);
+                const int m0 = (t.tm * CG + (int)rank) * TILE_M, n0 = t.tn * BN + (int)rank * B_ROWS;
+                for (int it = t.it0; it < t.it1; ++it, ++c) {
+                    const int slot = c % STAGES;
+                    if (c >= STAGES && !mbar_wait_cluster(&empty[slot], (c / STAGES - 1) & 1, g.limit)) {
+                        fine = false;
+                        break;
+                    }
+                    if (rank == 0) mbar_expect(&full[slot], STAGE * CG);
+                    const uint32_t bar = CG == 2 ? in_block(smem_addr(&full[slot]), 0) : smem_addr(&full[slot]);
+                    const uint32_t a = smem_addr(ring + slot * STAGE), b = a + A_BYTES;
+                    const int p = it / g.k_blocks, k0 = (it - p * g.k_blocks) * g.k_step;
+                    const int pa = part_a(g.pairs, p), pb = part_b(g.pairs, p), ra = t.r * g.a_worker, rb = t.r * g.b_worker;
+                    if (g.a_across) {
+                        for (int j = 0; j < TILE_M / 64; ++j) tile_load<CG>(a + j * 8192, &map_a, bar, m0 + j * 64, k0, pa, ra);
+                    } else {
+                        tile_load<CG>(a, &map_a, bar, k0, m0, pa, ra);
+                    }
+                    if (g.b_across) {
+                        for (int j = 0; j < B_ROWS / 64; ++j) tile_load<CG>(b + j * 8192, &map_b, bar, n0 + j * 64, k0, pb, rb);
+                    } else {
+                        tile_load<CG>(b, &map_b, bar, k0, n0, pb, rb);
+                    }
+                }
+            }
+            if (fine) {
+                // the last products' arrivals, which may come from the other block, are in before this one ends
+                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_cluster(&empty[i % STAGES], (i / STAGES) & 1, g.limit);
+            } else if (c > 0 && rank == 0) {
+                // after a wait that ran out: the copies under way (of both blocks: they count here) land before the memory is given up
+                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_cluster(&full[i % STAGES], (i / STAGES) & 1, WAIT_LIMIT_NS);
+            } else if (c > 0) {
+                // (the second block's count at the first: it cannot look, and gives them far more time than a copy takes)
+                const unsigned long long t0 = global_ns();
+                while (global_ns() - t0 < 10000000ull) {}
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0 && g.limit != 0) {
+            int c = 0, n = 0;
+            bool fine = true;
+            const uint32_t step_a = g.a_across ? 2048 : 32, step_b = g.b_across ? 2048 : 32;
+            for (int u = cluster; u < g.units && fine; u += clusters, ++n) {
+                const Unit t = unit_of(g, u);
+                const int buf = n & 1;
+                if (!(fine = mbar_wait_cluster(&acc_empty[buf], ((n >> 1) & 1) ^ 1, g.limit))) break;
+                tc_fence_after();
+                for (int it = t.it0; it < t.it1; ++it, ++c) {
+                    const int slot = c % STAGES;
+                    if (!(fine = mbar_wait_cluster(&full[slot], (c / STAGES) & 1, g.limit))) break;
+                    tc_fence_after();
+                    const uint32_t a = smem_addr(ring + slot * STAGE), b = a + A_BYTES;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint64_t da = tile_descriptor(a + k * step_a, 8192), db = tile_descriptor(b + k * step_b, 8192);
+                        if (g.eight) mma<CG, true>(tmem + buf * BN, da, db, g.idesc, it > t.it0 || k);
+                        else mma<CG, false>(tmem + buf * BN, da, db, g.idesc, it > t.it0 || k);
+                    }
+                    mma_commit<CG>(&empty[slot]);
+                }
+                if (fine) mma_commit<CG>(&acc_full[buf]);
+            }
+            // the products under way are done before their tensor memory is given up
+            mma_commit_here<CG>(&drained);
+            mbar_wait_cluster(&drained, 0, WAIT_LIMIT_NS);
+        }
+    } else if (warp >= 4) {
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        float* pass = reinterpret_cast<float*>(ring + STAGES * STAGE) + (warp - 4) * 1024;
+        const uint32_t leader[2] = {CG == 2 ? in_block(smem_addr(&acc_empty[0]), 0) : smem_addr(&acc_empty[0]),
+                                    CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
+        int n = 0;
+        bool fine = g.limit != 0;
+        for (int u = cluster; u < g.units; u += clusters, ++n) {
+            const Unit t = unit_of(g, u);
+            const int buf = n & 1;
+            if (fine) fine = __all_sync(~0u, mbar_wait_cluster(&acc_full[buf], (n >> 1) & 1, g.limit));
+            if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
+            tc_fence_after();
+            const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + half * (BN / 2);
+#pragma unroll 1
+            for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+                uint32_t v[32];
+                if (fine) {
+                    tmem_load32(v, tmem + ((uint32_t)(q * 32) << 16) + buf * BN + half * (BN / 2) + c0);
+                    tmem_wait_load();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = 0x7fffffff;
+                }
+                if (c0 + 32 == BN / 2 && fine) {     // the accumulator is free once its last columns are in registers
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_at(leader[buf]);
+                }
+                const long long n1 = n0 + c0;
+                if (m0 >= g.M || n1 >= g.N) continue;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<uint4*>(pass + lane * 32 + (j ^ (lane & 7)) * 4) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                __syncwarp();
+                const int rows = (int)min((long long)32, g.M - m0);
+                if (g.splits > 1) {
+                    float* p = g.part + (((long long)t.split * g.R + t.r) * g.M + m0) * g.part_ld + n1;
+                    const int j = lane & 7;
+                    if (n1 + 4 * j < g.part_ld)
+                        for (int i = lane >> 3; i < rows; i += 4)
+                            *reinterpret_cast<float4*>(p + i * g.part_ld + 4 * j) = *reinterpret_cast<float4*>(pass + i * 32 + (j ^ (i & 7)) * 4);
+                } else if (g.f.vec && n1 + 32 <= g.N) {
+                    const int j = lane & 3;
+                    Columns<8> c;
+                    load_columns(g.f, t.r, n1 + 8 * j, c);
+                    for (int i = lane >> 2; i < rows; i += 8) {
+                        float w[8];
+                        const float4 x = *reinterpret_cast<float4*>(pass + i * 32 + ((2 * j) ^ (i & 7)) * 4);
+                        const float4 y = *reinterpret_cast<float4*>(pass + i * 32 + ((2 * j + 1) ^ (i & 7)) * 4);
+                        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
+                        finish(g.f, t.r, m0 + i, n1 + 8 * j, w, c);
+                    }
+                } else if (n1 + lane < g.N) {
+                    Columns<1> c;
+                    load_columns(g.f, t.r, n1 + lane, c);
+                    for (int i = 0; i < rows; ++i) {
+                        float w[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
+                        finish(g.f, t.r, m0 + i, n1 + lane, w, c);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    tc_fence_after();
+    if (warp == 2) tmem_free<CG>(tmem, 2 * BN);
+}
+
+// The splits' sums, joined in order, and what follows
+template <int V>
+__global__ void __launch_bounds__(256) join_splits_kernel(const float* part, long long ld, int splits, int R, const Finish f) {
+    after_launch();
+    const long long units = (f.N + V - 1) / V, items = R * f.M * units, plane = R * f.M * ld;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
+        const long long row = i / units, n = (i - row * units) * V;
+        const float* p = part + row * ld + n;
+        float v[V];
+        load_floats<V>(v, p);
+        for (int s = 1; s < splits; ++s) {
+            float t[V];
+            load_floats<V>(t, p + s * plane);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] += t[j];
+        }
+        const int r = (int)(row / f.M);
+        Columns<V> c;
+        load_columns(f, r, n, c);
+        finish(f, r, row - r * f.M, n, v, c);
+    }
+}
+
+// ------------------------------------------------------------------ small products, in fp32 on the ordinary units
+struct Side { const void* p; int type, as; long long row, k, worker; };   // element (row, k) of a worker; rounded to `as`
+__device__ __forceinline__ float side_at(const Side& s, long long i) {
+    if (s.type == QS_E4M3) {
+        const __half_raw h = __nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(s.p)[i], __NV_E4M3);
+        return __half2float(__half(h));
+    }
+    const float v = element(s.p, s.type, i);
+    if (s.type != QS_F32 || s.as == QS_F32) return v;
+    return s.as == QS_BF16 ? to_float(__float2bfloat16_rn(v)) : to_float(__float2half_rn(v));
+}
+// 64 x 64 results per block of 256 threads, 16 of the contraction at a time
+__global__ void __launch_bounds__(256) small_kernel(const Side a, const Side b, long long K, const Finish f) {
+    __shared__ float sa[16][68], sb[16][68];
+    const int r = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const long long n0 = (long long)blockIdx.x * 64;
+    for (long long m0 = (long long)blockIdx.y * 64; m0 < f.M; m0 += (long long)gridDim.y * 64) {
+    float acc[4][4] = {};
+    for (long long k0 = 0; k0 < K; k0 += 16) {
+        for (int side = 0; side < 2; ++side) {
+            const Side& s = side ? b : a;
+            float (*to)[68] = side ? sb : sa;
+            const long long first = side ? n0 : m0, most = side ? f.N : f.M;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = threadIdx.x + 256 * i;
+                const int row = s.k == 1 ? e >> 4 : e & 63, k = s.k == 1 ? e & 15 : e >> 6;
+                to[k][row] = first + row < most && k0 + k < K ? side_at(s, r * s.worker + (first + row) * s.row + (k0 + k) * s.k) : 0.0f;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const float4 x = *reinterpret_cast<float4*>(&sa[k][ty * 4]), y = *reinterpret_cast<float4*>(&sb[k][tx * 4]);
+            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(xs[i], ys[j], acc[i][j]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const long long n = n0 + tx * 4 + j;
+        if (n >= f.N) continue;
+        Columns<1> c;
+        load_columns(f, r, n, c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v[1] = {acc[i][j]};
+            if (m0 + ty * 4 + i < f.M) finish(f, r, m0 + ty * 4 + i, n, v, c);
+        }
+    }
+    }
+}
+
+// ------------------------------------------------------------------ host
+struct Operand {
+    const void* p; int type;
+    long long rows;                                  // of the result's side
+    long long ld, worker;                            // between rows in memory, between workers (0: one for all)
+    int across;                                      // memory rows run along k
+};
+struct Product {
+    int R; long long M, N, K; int type;              // type: what both operands are multiplied as
+    Operand a, b;
+};
+
+struct Plan {
+    bool small, lay_a, lay_b;
+    int cg, bn, planes, splits;
+    long long ld_a, ld_b, part_ld;
+    long long off_b, off_part, bytes;
+};
+
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+int bytes_of(int type) { return type == QS_E4M3 ? 1 : size_of_type(type); }
+
+long long memory_rows(const Product& p, const Operand& o) { return o.across ? p.K : o.rows; }
+long long memory_cols(const Product& p, const Operand& o) { return o.across ? o.rows : p.K; }
+bool taken_as_it_lies(const Product& p, const Operand& o) {
+    const int size = bytes_of(o.type);
+    return o.type == p.type && p.type != QS_F32 && aligned_to(o.p, 16) && (memory_rows(p, o) == 1 || (o.ld * size % 16 == 0 && o.ld < 1ll << 36)) &&
+           (p.R == 1 || (o.worker * size % 16 == 0 && o.worker < 1ll << 36));       // (a map's strides end at 2^40 bytes)
+}
+
+Plan plan_of(const Product& p, int sms) {
+    Plan q{};
+    q.planes = p.type == QS_F32 ? 3 : 1;
+    q.splits = 1;
+    const double work = 2.0 * p.R * p.M * p.N * p.K;
+    q.small = p.K == 0 || work < 1e6;
+    if (q.small) return q;
+    const int size = p.type == QS_E4M3 ? 1 : 2;
+    q.lay_a = !taken_as_it_lies(p, p.a);
+    q.lay_b = !taken_as_it_lies(p, p.b);
+    q.ld_a = round_up(memory_cols(p, p.a), 16);
+    q.ld_b = round_up(memory_cols(p, p.b), 16);
+    const long long t2 = p.R * ((p.M + 255) / 256) * ((p.N + 255) / 256), t1 = p.R * ((p.M + 127) / 128) * ((p.N + 127) / 128);
+    const double c2 = 2.0 * ((t2 + sms / 2 - 1) / (sms / 2)), c1 = 1.25 * ((t1 + sms - 1) / sms);
+    q.cg = c2 <= c1 ? 2 : 1;
+    q.bn = q.cg == 2 ? 256 : 128;
+    const long long tiles = q.cg == 2 ? t2 : t1, slots = sms / q.cg;
+    const long long iters = (p.K + 128 / size - 1) / (128 / size) * (q.planes == 3 ? 6 : 1);
+    q.splits = (int)std::max<long long>(1, std::min<long long>({slots / std::max<long long>(1, tiles), iters / 4, 64}));
+    long long at = 0;
+    const long long wa = p.a.worker || p.R == 1 ? p.R : 1, wb = p.b.worker || p.R == 1 ? p.R : 1;
+    if (q.lay_a) at += round_up(wa * q.planes * memory_rows(p, p.a) * q.ld_a * size, 256);
+    q.off_b = at;
+    if (q.lay_b) at += round_up(wb * q.planes * memory_rows(p, p.b) * q.ld_b * size, 256);
+    q.off_part = at;
+    q.part_ld = round_up(p.N, 8);
+    if (q.splits > 1) at += 4ll * q.splits * p.R * p.M * q.part_ld;
+    q.bytes = at;
+    return q;
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+    static const EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeFn>(f);
+    }();
+    return fn;
+}
+// (inner, outer, plane, worker) in boxes of 128 bytes by `box` rows
+bool encode(CUtensorMap* map, const void* p, int type, long long inner, long long outer, int planes, long long workers, long long ld, long long plane,
+            long long worker, int box) {
+    const int size = type == QS_E4M3 ? 1 : 2;
+    const EncodeFn fn = encoder();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)outer, (cuuint64_t)planes, (cuuint64_t)workers};
+    // (a dimension of one element has no stride: any that is allowed)
+    const long long row = outer > 1 ? ld * size : round_up(inner * size, 16);
+    const cuuint64_t strides[3] = {(cuuint64_t)row, (cuuint64_t)(planes > 1 ? plane * size : row), (cuuint64_t)(workers > 1 ? worker * size : row)};
+    const cuuint32_t boxes[4] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1, 1}, ones[4] = {1, 1, 1, 1};
+    const CUtensorMapDataType t = type == QS_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : type == QS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return fn(map, t, 4, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+unsigned long long wait_limit() {
+    static const unsigned long long ns = [] {
+        const char* e = std::getenv("QSPARSE_WAIT_LIMIT_NS");
+        return e ? std::min(std::strtoull(e, nullptr, 10), WAIT_LIMIT_NS) : WAIT_LIMIT_NS;
+    }();
+    return ns;
+}
+
+cudaError_t lay_out(const Product& p, const Operand& o, void* dst, int dst_type, int planes, long long ld, cudaStream_t st) {
+    LayArgs a{};
+    const long long workers = o.worker || p.R == 1 ? p.R : 1;
+    a.src = o.p; a.src_type = o.type; a.src_stride = o.ld; a.src_worker = o.worker;
+    a.dst = dst; a.dst_type = dst_type; a.planes = planes; a.ld = ld; a.rows = memory_rows(p, o); a.cols = memory_cols(p, o);
+    a.vec = o.type == QS_F32 && aligned_to(o.p, 16) && (a.rows == 1 || o.ld % 4 == 0) && (workers == 1 || o.worker % 4 == 0);
+    const long long items = a.rows * (ld / 8);
+    return launch(false, lay_kernel, dim3((unsigned)std::min<long long>((items + 255) / 256, 1 << 16), (unsigned)workers), 256, 0, st, a);
+}
+
+template <int CG, int BN>
+cudaError_t launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& g, bool after, int sms, cudaStream_t st) {
+    constexpr int smem = gemm_smem<CG, BN>();
+    cudaError_t e = cudaFuncSetAttribute(gemm_kernel<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min(g.units, sms / CG) * CG);
+    cfg.blockDim = dim3(GEMM_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, gemm_kernel<CG, BN>, ma, mb, g);
+}
+
+int run_product(const Product& p, const Finish& f, void* work, int64_t work_bytes, int* status, cudaStream_t st) {
+    const int sms = sm_count();
+    if (!sms) return QS_CUDA;
+    const Plan q = plan_of(p, sms);
+    if (q.small) {
+        const auto side = [&](const Operand& o) { return Side{o.p, o.type, p.type, o.across ? 1 : o.ld, o.across ? o.ld : 1, o.worker}; };
+        return status_of(launch(false, small_kernel, dim3((unsigned)((p.N + 63) / 64), (unsigned)std::min<long long>((p.M + 63) / 64, 65535), (unsigned)p.R), 256, 0, st, side(p.a), side(p.b),
+                                (long long)p.K, f));
+    }
+    if (q.bytes > 0 && (!work || !aligned_to(work, 256))) return QS_INVALID_ARG;
+    if (work_bytes < q.bytes) return QS_CAPACITY;
+    uint8_t* w = static_cast<uint8_t*>(work);
+    const int type = p.type == QS_F32 ? QS_BF16 : p.type, size = type == QS_E4M3 ? 1 : 2;
+    GemmArgs g{};
+    CUtensorMap map[2];
+    bool after = false;
+    for (int i = 0; i < 2; ++i) {
+        const Operand& o = i ? p.b : p.a;
+        const bool lay = i ? q.lay_b : q.lay_a;
+        const long long rows = memory_rows(p, o), cols = memory_cols(p, o), workers = o.worker || p.R == 1 ? p.R : 1;
+        const long long ld = lay ? (i ? q.ld_b : q.ld_a) : o.ld;
+        const void* at = lay ? w + (i ? q.off_b : 0) : o.p;
+        if (lay) {
+            const cudaError_t e = lay_out(p, o, w + (i ? q.off_b : 0), type, q.planes, ld, st);
+            if (e != cudaSuccess) return status_of(e);
+            after = true;
+        }
+        (i ? g.b_worker : g.a_worker) = workers > 1;
+        (i ? g.b_across : g.a_across) = o.across;
+        const int box = o.across ? 64 : i ? q.bn / q.cg : TILE_M;
+        if (!encode(&map[i], at, type, cols, rows, q.planes, workers, ld, rows * ld, lay ? q.planes * rows * ld : o.worker, box)) return QS_CUDA;
+    }
+    g.R = p.R; g.M = p.M; g.N = p.N;
+    g.tiles_m = (int)((p.M + TILE_M * q.cg - 1) / (TILE_M * q.cg));
+    g.tiles_n = (int)((p.N + q.bn - 1) / q.bn);
+    g.splits = q.splits;
+    g.units = p.R * g.tiles_m * g.tiles_n * g.splits;
+    g.k_step = 128 / size;
+    g.k_blocks = (int)((p.K + g.k_step - 1) / g.k_step);
+    g.pairs = q.planes == 3 ? 6 : 1;
+    g.iters = g.k_blocks * g.pairs;
+    g.eight = type == QS_E4M3;
+    // sums in fp32; operand types (e4m3 and fp16 are 0, bf16 is 1); which lie across k; the tile
+    const uint32_t t = type == QS_BF16 ? 1 : 0;
+    g.idesc = 1u << 4 | t << 7 | t << 10 | (uint32_t)g.a_across << 15 | (uint32_t)g.b_across << 16 | (uint32_t)(q.bn / 8) << 17 | (uint32_t)(TILE_M * q.cg / 16) << 24;
+    g.part = reinterpret_cast<float*>(w + q.off_part);
+    g.part_ld = q.part_ld;
+    g.limit = wait_limit();
+    g.status = status;
+    g.f = f;
+    cudaError_t e = q.cg == 2 ? launch_gemm<2, 256>(map[0], map[1], g, after, sms, st) : launch_gemm<1, 128>(map[0], map[1], g, after, sms, st);
+    if (e != cudaSuccess || q.splits == 1) return status_of(e);
+    const long long items = p.R * p.M * (f.vec ? (p.N + 7) / 8 : p.N);
+    const dim3 grid((unsigned)std::min<long long>((items + 255) / 256, 1 << 20));
+    e = f.vec && p.N % 8 == 0 ? launch(true, join_splits_kernel<8>, grid, 256, 0, st, (const float*)g.part, g.part_ld, q.splits, p.R, f)
+                              : launch(true, join_splits_kernel<1>, grid, 256, 0, st, (const float*)g.part, g.part_ld, q.splits, p.R, f);
+    return status_of(e);
+}
+
+bool is_act(int act) { return act >= QS_ACT_NONE && act <= QS_ACT_GELU; }
+bool bad_sizes(int R, int64_t M, int64_t N, int64_t K) { return R < 1 || R > 32 || M < 0 || N < 1 || K < 1; }
+// (tile and block counts fit 31 bits, and so do the tensor maps' coordinates)
+bool sizes_too_large(int R, int64_t M, int64_t N, int64_t K) {
+    return M > (1ll << 28) || N > (1ll << 24) || K > (1ll << 24) || R * M > (1ll << 28) || R * ((M + 127) / 128) * ((N + 127) / 128) > (1ll << 24);
+}
+bool bad_matrix(const void* p, int64_t stride, int64_t width, int size) { return !p || stride < width || !aligned_to(p, size); }
+bool workers_overlap(int R, int64_t worker, int64_t rows, int64_t stride, int64_t width) {
+    return R > 1 && worker < (rows - 1) * stride + width && (worker < width || stride < (R - 1) * worker + width);
+}
+
+// ------------------------------------------------------------------ gradient in front of the activation
+struct ActGradArgs {
+    int R; long long M, N;
+    const void* g; long long g_stride;
+    const void* z; long long z_stride; int act;
+    void* out; long long out_stride;
+    float* part; int parts;                          // (R, parts, N): column sums of the rows of a block, or null
+};
+// 8 warps of rows, 32 V columns per block; block (x, p, r) takes rows p * 8 + warp, + 8 parts, ..
+template <class T, int V>
+__global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a) {
+    __shared__ float sh[8][32 * V + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.z;
+    const long long n = ((long long)blockIdx.x * 32 + lane) * V;
+    float sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+    if (n < a.N)
+#pragma unroll 2
+        for (long long m = blockIdx.y * 8 + warp; m < a.M; m += a.parts * 8) {
+            const long long row = r * a.M + m;
+            float g[V];
+            load_vec<V>(g, static_cast<const T*>(a.g) + row * a.g_stride + n);
+            if (a.act != QS_ACT_NONE) {
+                float z[V];
+                load_vec<V>(z, static_cast<const T*>(a.z) + row * a.z_stride + n);
+#pragma unroll
+                for (int j = 0; j < V; ++j) g[j] *= slope(a.act, z[j]);
+            }
+            if (a.out) store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + n, g);
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum[j] += g[j];
+        }
+    if (!a.part) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) sh[warp][lane * V + j] = sum[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * V; i += 256) {
+        const long long c = (long long)blockIdx.x * 32 * V + i;
+        if (c >= a.N) break;
+        float s = sh[0][i];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) s += sh[w][i];
+        a.part[((long long)r * a.parts + blockIdx.y) * a.N + c] = s;
+    }
+}
+int act_parts(int R, int64_t M, int64_t N) {
+    const long long columns = R * ((N + 255) / 256);
+    return (int)std::max<long long>(1, std::min<long long>((M + 31) / 32, (148 * 12 + columns - 1) / columns));
+}
+template <class T>
+cudaError_t launch_act_grad(const ActGradArgs& a, bool vec, cudaStream_t st) {
+    constexpr int V = wide_of<T>();
+    const int v = vec ? V : 1;
+    const dim3 grid((unsigned)((a.N + 32 * v - 1) / (32 * v)), (unsigned)a.parts, (unsigned)a.R);
+    return vec ? launch(false, act_grad_kernel<T, V>, grid, 256, 0, st, a) : launch(false, act_grad_kernel<T, 1>, grid, 256, 0, st, a);
+}
+
+Product forward_of(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const void* w, int w_type, int64_t w_worker, int64_t w_stride) {
+    return {R, M, N, K, x_type, {x, x_type, M, x_stride, R > 1 ? M * x_stride : 0, 0}, {w, w_type, N, w_stride, w_worker, 0}};
+}
+// dx (M x K) = sum over n of dz[m, n] w[n, k]
+Product input_of(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* w, int w_type, int64_t w_worker, int64_t w_stride) {
+    return {R, M, K, N, type, {dz, type, M, dz_stride, R > 1 ? M * dz_stride : 0, 0}, {w, w_type, K, w_stride, w_worker, 1}};
+}
+// dw (N x K) = sum over m of dz[m, n] x[m, k]
+Product weight_of(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride) {
+    return {R, N, K, M, type, {dz, type, N, dz_stride, R > 1 ? M * dz_stride : 0, 1}, {x, type, K, x_stride, R > 1 ? M * x_stride : 0, 1}};
+}
+int64_t bytes_for(const Product& p) {
+    const int sms = sm_count();
+    return sms ? plan_of(p, sms).bytes : (int64_t)QS_CUDA;
+}
+bool weight_type_ok(int type, int w_type) { return type == QS_E4M3 ? w_type == QS_E4M3 : size_of_type(type) && (w_type == type || w_type == QS_F32); }
+
+}  // namespace
+}  // namespace qs
+
+using namespace qs;
+
+extern "C" {
+
+int64_t qs_linear_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const void* w, int w_type,
+                        int64_t w_worker_stride, int64_t w_stride) {
+    if (bad_sizes(R, M, N, K) || !weight_type_ok(x_type, w_type)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K)) return QS_TOO_LARGE;
+    return M ? bytes_for(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride)) : 0;
+}
+
+int qs_linear(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const float* x_scale, const void* w, int w_type,
+              int64_t w_worker_stride, int64_t w_stride, const float* w_scale, const void* bias, int bias_type, int64_t bias_worker_stride,
+              int activation, const void* residual, int64_t residual_stride, void* pre, int64_t pre_stride, void* out, int out_type,
+              int64_t out_stride, void* work, int64_t work_bytes, int* status, void* cuda_stream) {
+    if (bad_sizes(R, M, N, K) || !weight_type_ok(x_type, w_type) || !is_act(activation)) return QS_INVALID_ARG;
+    const bool eight = x_type == QS_E4M3;
+    const int size = size_of_type(out_type);
+    if (!size || (!eight && out_type != x_type && out_type != QS_F32) || eight != (x_scale != nullptr) || eight != (w_scale != nullptr)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K)) return QS_TOO_LARGE;
+    if (M == 0) return QS_OK;
+    if (bad_matrix(x, x_stride, K, bytes_of(x_type)) || bad_matrix(w, w_stride, K, bytes_of(w_type)) || w_worker_stride < 0 ||
+        (w_worker_stride && workers_overlap(R, w_worker_stride, N, w_stride, K)) || bad_matrix(out, out_stride, N, size) ||
+        (residual && bad_matrix(residual, residual_stride, N, size)) || (pre && bad_matrix(pre, pre_stride, N, size)) || !aligned_to(x_scale, 4) ||
+        !aligned_to(w_scale, 4) || !aligned_to(status, 4) ||
+        (bias && (!size_of_type(bias_type) || !aligned_to(bias, size_of_type(bias_type)) || bias_worker_stride < 0))) return QS_INVALID_ARG;
+    const int64_t rows = R * M, bytes = span(rows, out_stride, N, size), pre_bytes = pre ? span(rows, pre_stride, N, size) : 0;
+    const int64_t x_bytes = span(rows, x_stride, K, bytes_of(x_type)), w_bytes = (R - 1) * w_worker_stride * bytes_of(w_type) + span(N, w_stride, K, bytes_of(w_type));
+    if (!apart(out, bytes, x, x_bytes) || !apart(out, bytes, w, w_bytes) || !apart(pre, pre_bytes, x, x_bytes) || !apart(pre, pre_bytes, w, w_bytes) ||
+        !beside(residual, residual_stride, out, out_stride, rows, N, size) || (pre && (pre == out || pre == residual)) ||
+        !beside(residual, residual_stride, pre, pre_stride, rows, N, size) || !beside(pre, pre_stride, out, out_stride, rows, N, size)) return QS_INVALID_ARG;
+    Finish f{};
+    f.M = M; f.N = N; f.bias = bias; f.bias_type = bias_type; f.bias_worker = bias_worker_stride; f.act = activation;
+    f.res = residual; f.res_stride = residual_stride; f.pre = pre; f.pre_stride = pre_stride;
+    f.out = out; f.type = out_type; f.out_stride = out_stride; f.out_worker = M * out_stride; f.a_scale = x_scale; f.b_scale = w_scale;
+    f.vec = rows_aligned(out, out_stride, rows, size, 16) && rows_aligned(residual, residual_stride, rows, size, 16) && rows_aligned(pre, pre_stride, rows, size, 16);
+    return run_product(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride), f, work, work_bytes, status,
+                       static_cast<cudaStream_t>(cuda_stream));
+}
+
+int64_t qs_linear_grad_input_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* w, int w_type,
+                                   int64_t w_worker_stride, int64_t w_stride) {
+    if (bad_sizes(R, M, N, K) || !size_of_type(type) || !weight_type_ok(type, w_type)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K) || sizes_too_large(R, M, K, N)) return QS_TOO_LARGE;
+    return M ? bytes_for(input_of(R, M, N, K, dz, type, dz_stride, w, w_type, w_worker_stride, w_stride)) : 0;
+}
+
+int qs_linear_grad_input(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* w, int w_type,
+                         int64_t w_worker_stride, int64_t w_stride, void* out, int64_t out_stride, void* work, int64_t work_bytes, int* status,
+                         void* cuda_stream) {
+    if (bad_sizes(R, M, N, K) || !size_of_type(type) || !weight_type_ok(type, w_type)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K) || sizes_too_large(R, M, K, N)) return QS_TOO_LARGE;
+    if (M == 0) return QS_OK;
+    const int size = size_of_type(type);
+    if (bad_matrix(dz, dz_stride, N, size) || bad_matrix(w, w_stride, K, size_of_type(w_type)) || bad_matrix(out, out_stride, K, size) || w_worker_stride < 0 ||
+        (w_worker_stride && workers_overlap(R, w_worker_stride, N, w_stride, K)) || !aligned_to(status, 4)) return QS_INVALID_ARG;
+    const int64_t rows = R * M, bytes = span(rows, out_stride, K, size);
+    if (!apart(out, bytes, dz, span(rows, dz_stride, N, size)) ||
+        !apart(out, bytes, w, (R - 1) * w_worker_stride * size_of_type(w_type) + span(N, w_stride, K, size_of_type(w_type)))) return QS_INVALID_ARG;
+    Finish f{};
+    f.M = M; f.N = K; f.out = out; f.type = type; f.out_stride = out_stride; f.out_worker = M * out_stride;
+    f.vec = rows_aligned(out, out_stride, rows, size, 16);
+    return run_product(input_of(R, M, N, K, dz, type, dz_stride, w, w_type, w_worker_stride, w_stride), f, work, work_bytes, status,
+                       static_cast<cudaStream_t>(cuda_stream));
+}
+
+int64_t qs_linear_grad_weight_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride) {
+    if (bad_sizes(R, M, N, K) || !size_of_type(type)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K) || sizes_too_large(R, N, K, 1)) return QS_TOO_LARGE;
+    return M ? bytes_for(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride)) : 0;
+}
+
+int qs_linear_grad_weight(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride, void* out,
+                          int out_type, int64_t out_worker_stride, int64_t out_stride, int accumulate, void* work, int64_t work_bytes, int* status,
+                          void* cuda_stream) {
+    const int size = size_of_type(type), out_size = size_of_type(out_type);
+    if (bad_sizes(R, M, N, K) || !size || (out_type != type && out_type != QS_F32)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K) || sizes_too_large(R, N, K, 1)) return QS_TOO_LARGE;
+    if (bad_matrix(out, out_stride, K, out_size) || workers_overlap(R, out_worker_stride, N, out_stride, K) || !aligned_to(status, 4)) return QS_INVALID_ARG;
+    if (M == 0 && accumulate) return QS_OK;
+    if (M && (bad_matrix(dz, dz_stride, N, size) || bad_matrix(x, x_stride, K, size))) return QS_INVALID_ARG;
+    const int64_t bytes = ((R - 1) * out_worker_stride + (N - 1) * out_stride + K) * out_size;
+    if (M && (!apart(out, bytes, dz, span(R * M, dz_stride, N, size)) || !apart(out, bytes, x, span(R * M, x_stride, K, size)))) return QS_INVALID_ARG;
+    Finish f{};
+    f.M = N; f.N = K; f.out = out; f.type = out_type; f.out_stride = out_stride; f.out_worker = R > 1 ? out_worker_stride : 0;
+    f.accumulate = accumulate;
+    f.vec = rows_aligned(out, out_stride, N, out_size, 16) && (R == 1 || out_worker_stride * out_size % 16 == 0);
+    return run_product(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride), f, work, work_bytes, status, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int64_t qs_activation_grad_bytes(int R, int64_t M, int64_t N) {
+    if (bad_sizes(R, M, N, 1)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, 1)) return QS_TOO_LARGE;
+    return 4 * (int64_t)R * act_parts(R, M, N) * N;
+}
+
+int qs_activation_grad(int R, int64_t M, int64_t N, const void* grad, int type, int64_t grad_stride, const void* pre, int64_t pre_stride, int activation,
+                       void* out, int64_t out_stride, float* grad_bias, int64_t grad_bias_worker_stride, int accumulate, void* work, int64_t work_bytes,
+                       void* cuda_stream) {
+    const int size = size_of_type(type);
+    if (bad_sizes(R, M, N, 1) || !size || !is_act(activation) || (!out && !grad_bias)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, 1)) return QS_TOO_LARGE;
+    if (grad_bias && (!aligned_to(grad_bias, 4) || (R > 1 && grad_bias_worker_stride < N))) return QS_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (M == 0) return !grad_bias || accumulate ? QS_OK : status_of(launch_join(false, nullptr, 0, R, N, grad_bias, grad_bias_worker_stride, 0, st));
+    const int64_t rows = R * M;
+    const bool act = activation != QS_ACT_NONE;
+    if (bad_matrix(grad, grad_stride, N, size) || (act && bad_matrix(pre, pre_stride, N, size)) || (out && bad_matrix(out, out_stride, N, size))) return QS_INVALID_ARG;
+    if (!beside(grad, grad_stride, out, out_stride, rows, N, size) || (act && !beside(pre, pre_stride, out, out_stride, rows, N, size))) return QS_INVALID_ARG;
+    if (grad_bias && (!work || !aligned_to(work, 16))) return QS_INVALID_ARG;
+    if (grad_bias && work_bytes < 4 * (int64_t)R * act_parts(R, M, N) * N) return QS_CAPACITY;
+    ActGradArgs a{};
+    a.R = R; a.M = M; a.N = N; a.g = grad; a.g_stride = grad_stride; a.z = pre; a.z_stride = pre_stride; a.act = activation; a.out = out; a.out_stride = out_stride;
+    a.part = grad_bias ? static_cast<float*>(work) : nullptr;
+    a.parts = act_parts(R, M, N);
+    const int V = 16 / size;
+    const bool vec = N % V == 0 && rows_aligned(grad, grad_stride, rows, size, 16) && rows_aligned(act ? pre : nullptr, pre_stride, rows, size, 16) &&
+                     rows_aligned(out, out_stride, rows, size, 16);
+    const cudaError_t e = type == QS_F32 ? launch_act_grad<float>(a, vec, st) : type == QS_BF16 ? launch_act_grad<bf16>(a, vec, st) : launch_act_grad<__half>(a, vec, st);
+    if (e != cudaSuccess || !grad_bias) return status_of(e);
+    return status_of(launch_join(true, a.part, a.parts, R, N, grad_bias, grad_bias_worker_stride, accumulate, st));
+}
+
+}  // extern "C"

@@ -54,6 +54,17 @@ inline int status_of(cudaError_t e) {
     cudaGetLastError();
     return QS_CUDA;
 }
+// A result may take an input's own place, row for row, or other columns of the same rows; any other overlap is refused
+inline bool overlap(const void* z, int64_t stride, const void* g, int64_t g_stride, int64_t N, int64_t V, int size) {
+    typedef __int128 wide;
+    const wide z0 = reinterpret_cast<uintptr_t>(z), g0 = reinterpret_cast<uintptr_t>(g), row = (wide)stride * size, len = (wide)V * size;
+    if (z0 == g0 && stride == g_stride) return false;
+    const wide z1 = z0 + (N - 1) * row + len, g1 = g0 + (N - 1) * (wide)g_stride * size + len;
+    if (z1 <= g0 || g1 <= z0) return false;
+    if (stride != g_stride) return true;
+    const wide apart = ((g0 - z0) % row + row) % row;            // from a row of z to the next row of g
+    return apart < len || apart + len > row;
+}
 // AFTER: the kernel may start while the one before it still runs (it waits for that one's end itself)
 template <class... P, class... A>
 cudaError_t launch(bool after, void (*kernel)(P...), dim3 grid, unsigned threads, unsigned smem, cudaStream_t st, A... args) {

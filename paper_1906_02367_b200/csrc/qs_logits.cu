@@ -1240,18 +1240,6 @@ bool bad_rows(int64_t N, int64_t V, int type, int64_t stride, float scale) {
 bool rows_too_large(int64_t N, int64_t V) { return N > (1ll << 30) || V > (1ll << 30); }
 bool ok_floats(const void* p) { return aligned_to(p, 4); }
 
-// the gradient may take the logits' own place, row for row, or other columns of the same rows; any other overlap is refused
-bool overlap(const void* z, int64_t stride, const void* g, int64_t g_stride, int64_t N, int64_t V, int size) {
-    typedef __int128 wide;
-    const wide z0 = reinterpret_cast<uintptr_t>(z), g0 = reinterpret_cast<uintptr_t>(g), row = (wide)stride * size, len = (wide)V * size;
-    if (z0 == g0 && stride == g_stride) return false;
-    const wide z1 = z0 + (N - 1) * row + len, g1 = g0 + (N - 1) * (wide)g_stride * size + len;
-    if (z1 <= g0 || g1 <= z0) return false;
-    if (stride != g_stride) return true;
-    const wide apart = ((g0 - z0) % row + row) % row;            // from a row of logits to the next row of results
-    return apart < len || apart + len > row;
-}
-
 }  // namespace
 
 extern "C" {
