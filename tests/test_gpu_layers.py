@@ -287,6 +287,23 @@ def test_linear(L, dtype, M, N, K):
     check_linear(L, rand((M, K), dtype, 1), rand((N, K), dtype, 2, K ** -0.5))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("R,M,N,K", [(1, 4000, 2100, 200), (1, 8192, 4096, 136), (2, 1500, 3001, 257), (5, 900, 1100, 64)])
+def test_linear_of_many_tiles(L, dtype, R, M, N, K):
+    """More tiles than blocks, in both directions: every accumulator and every slot of the ring is used again."""
+    x, w, g = rand((R, M, K), dtype, 1), rand((R, N, K), dtype, 2, K ** -0.5), rand((R, M, N), dtype, 3, 0.1)
+    check_linear(L, x, w, rand((R, N), F32, 3), "relu", rand((R, M, N), dtype, 4))
+    r = L.linear_grad(g, x, w, dtype=dtype)
+    dx, size = ref.product(g, w.transpose(1, 2))
+    near(r.x, dx, ((N + 8) * E * 1.05 + 4 * E) * size, dtype)
+    dw, size = ref.product(g.transpose(1, 2), x.transpose(1, 2))
+    near(r.weight, dw, ((M + 8) * E * 1.05 + 4 * E) * size, dtype)
+    v, u = L.quantize(x[0].float()), L.quantize(w[0].float())
+    z, size = ref.product(v.values.float(), u.values.float())
+    s = v.scale.double()[:, None] * u.scale.double()
+    near(L.linear(v.values, u.values, x_scale=v.scale, weight_scale=u.scale, dtype=dtype).out, z * s, ((K + 8) * E + 4 * E) * size * s, dtype)
+
+
 @pytest.mark.parametrize("activation", [None, "relu", "silu", "gelu"])
 @pytest.mark.parametrize("M,N,K", [(5, 24, 33), (200, 264, 192), (190, 261, 130)])
 @pytest.mark.parametrize("dtype,w_dtype,out", [(BF16, F32, BF16), (F16, F16, F32), (F32, F32, F32)])
