@@ -23,6 +23,7 @@ struct Finish {
     void* pre; long long pre_stride;
     void* out; int type; long long out_stride, out_worker;
     const float* a_scale; const float* b_scale;      // per row and per column, of 8-bit operands
+    long long b_scale_worker;
     int accumulate;                                  // added to what `out` holds
     int vec;                                         // rows of 16-byte vectors all around
 };
@@ -33,19 +34,36 @@ __device__ __forceinline__ float rcp(float x) {
     return r;
 }
 __device__ __forceinline__ float logistic(float z) { return rcp(1.0f + ex2(-LOG2E * z)); }
-__device__ __forceinline__ float activate(int act, float z) {
-    if (act == QS_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == QS_ACT_SILU) return z * logistic(z);
-    if (act == QS_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+// Phi(z) = erfc(-z / sqrt 2) / 2 by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (error below
+// 1.5e-7 in erf), and e^(-z^2 / 2) on the way.  (erff has two branches: 8192 x 16384 results in bf16 take 30 us longer with it)
+struct Normal { float phi, density; };
+__device__ __forceinline__ Normal normal(float z) {
+    const float x = fabsf(z) * 0.70710678f, t = rcp(__fmaf_rn(0.3275911f, x, 1.0f)), e = ex2(-LOG2E * x * x);
+    float p = __fmaf_rn(1.061405429f, t, -1.453152027f);
+    p = __fmaf_rn(p, t, 1.421413741f);
+    p = __fmaf_rn(p, t, -0.284496736f);
+    p = __fmaf_rn(p, t, 0.254829592f);
+    const float half = 0.5f * p * t * e;
+    return {z < 0.0f ? half : 1.0f - half, e};
+}
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if (ACT == QS_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (ACT == QS_ACT_SILU) return z * logistic(z);
+    if (ACT == QS_ACT_GELU) return z * normal(z).phi;
     return z;
 }
-__device__ __forceinline__ float slope(int act, float z) {
-    if (act == QS_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (act == QS_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+    if (ACT == QS_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == QS_ACT_SILU) {
         const float p = logistic(z);
         return p * __fmaf_rn(z, 1.0f - p, 1.0f);
     }
-    if (act == QS_ACT_GELU) return __fmaf_rn(z * 0.39894228f, ex2(-0.5f * LOG2E * z * z), 0.5f * (1.0f + erff(z * 0.70710678f)));
+    if (ACT == QS_ACT_GELU) {
+        const Normal n = normal(z);
+        return __fmaf_rn(z * 0.39894228f, n.density, n.phi);
+    }
     return 1.0f;
 }
 
@@ -53,52 +71,69 @@ __device__ __forceinline__ float element(const void* p, int type, long long i) {
     return type == QS_F32 ? static_cast<const float*>(p)[i] : type == QS_BF16 ? to_float(static_cast<const bf16*>(p)[i]) : to_float(static_cast<const __half*>(p)[i]);
 }
 
-template <int V, class T>
-__device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, long long n, float (&v)[V]) {
-    const long long row = r * f.M + m;
-    if (f.pre) store_vec<V>(static_cast<T*>(f.pre) + row * f.pre_stride + n, v);
-    if (f.act != QS_ACT_NONE)
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = activate(f.act, v[i]);
-    if (f.res) {
-        float t[V];
-        load_vec<V>(t, static_cast<const T*>(f.res) + row * f.res_stride + n);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += t[i];
-    }
-    T* out = static_cast<T*>(f.out) + r * f.out_worker + m * f.out_stride + n;
-    if (f.accumulate) {
-        float t[V];
-        load_vec<V>(t, out);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += t[i];
-    }
-    store_vec<V>(out, v);
-}
-// V columns from n on of row m: the sums in v, and what belongs to the columns
+// V columns from n on of a row: what belongs to the columns
 template <int V> struct Columns { float bias[V], scale[V]; };
 template <int V>
 __device__ __forceinline__ void load_columns(const Finish& f, int r, long long n, Columns<V>& c) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool in = n + i < f.N;
-        c.bias[i] = f.bias && in ? element(f.bias, f.bias_type, r * f.bias_worker + n + i) : 0.0f;
-        c.scale[i] = f.b_scale && in ? f.b_scale[r * f.N + n + i] : 1.0f;
+    for (int i = 0; i < V; ++i) c.bias[i] = 0.0f, c.scale[i] = 1.0f;
+    if (f.bias) {
+        const long long at = r * f.bias_worker + n;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (n + i < f.N) c.bias[i] = element(f.bias, f.bias_type, at + i);
     }
+    if (f.b_scale)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (n + i < f.N) c.scale[i] = f.b_scale[r * f.b_scale_worker + n + i];
+}
+// Sums of row m (of worker r), columns n on, on their way to the result.  add: to what the result holds; raw: nothing but that
+enum { ADD = 1, RAW = 2 };
+template <int ACT, int V, class T>
+__device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
+    const long long row = r * f.M + m;
+    T* out = static_cast<T*>(f.out) + r * f.out_worker + m * f.out_stride + n;
+    float t[V];
+    if (how & ADD) {
+        load_vec<V>(t, out);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += t[i];
+    }
+    if (!(how & RAW)) {
+        if (f.a_scale) {
+            const float s = f.a_scale[row];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = v[i] * s * c.scale[i];
+        }
+        if (f.bias)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += c.bias[i];
+        if (f.pre) store_vec<V>(static_cast<T*>(f.pre) + row * f.pre_stride + n, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = activate<ACT>(v[i]);
+        if (f.res) {
+            load_vec<V>(t, static_cast<const T*>(f.res) + row * f.res_stride + n);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += t[i];
+        }
+    }
+    store_vec<V>(out, v);
+}
+template <int ACT, int V>
+__device__ __forceinline__ void finish(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
+    if (f.type == QS_F32) finish_as<ACT, V, float>(f, r, m, n, v, c, how);
+    else if (f.type == QS_BF16) finish_as<ACT, V, bf16>(f, r, m, n, v, c, how);
+    else finish_as<ACT, V, __half>(f, r, m, n, v, c, how);
 }
 template <int V>
-__device__ __forceinline__ void finish(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c) {
-    if (f.a_scale) {
-        const float s = f.a_scale[r * f.M + m];
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = v[i] * s * c.scale[i];
+__device__ __forceinline__ void finish_any(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
+    switch (f.act) {
+    case QS_ACT_RELU: return finish<QS_ACT_RELU>(f, r, m, n, v, c, how);
+    case QS_ACT_SILU: return finish<QS_ACT_SILU>(f, r, m, n, v, c, how);
+    case QS_ACT_GELU: return finish<QS_ACT_GELU>(f, r, m, n, v, c, how);
+    default: return finish<QS_ACT_NONE>(f, r, m, n, v, c, how);
     }
-    if (f.bias)
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += c.bias[i];
-    if (f.type == QS_F32) finish_as<V, float>(f, r, m, n, v);
-    else if (f.type == QS_BF16) finish_as<V, bf16>(f, r, m, n, v);
-    else finish_as<V, __half>(f, r, m, n, v);
 }
 
 // ------------------------------------------------------------------ operands for the matrix unit
@@ -158,13 +193,17 @@ __global__ void __launch_bounds__(256) lay_kernel(const LayArgs a) {
 constexpr int TILE_M = 128;                          // rows of a block's part of a tile: the lanes of tensor memory
 constexpr int STAGES = 6;
 constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
+// The matrix unit cuts what lies below 2^-24 of a sum at every addition, always towards zero: 8e-10 of the result per element
+// summed.  Results in fp32 are therefore added up from sums over this many blocks of 128 bytes (4096 elements of 16 bits: 3e-6).
+constexpr int CHUNK_BLOCKS = 64;
 constexpr int PASS_BYTES = 8 * 4096;                 // 32 x 32 sums on their way from lanes to rows, per finishing warp
 
 struct GemmArgs {
     int R;
     long long M, N;
     int tiles_m, tiles_n, splits, units;             // units of work: workers x splits x tiles
-    int k_blocks, k_step, pairs, iters;              // blocks of 128 bytes along k; pairs of parts; their product
+    int k_blocks, k_step, pairs;                     // blocks of 128 bytes along k; pairs of parts
+    int chunk;                                       // blocks along k that are summed by the matrix unit before they are added up
     int a_across, b_across;                          // operand lies across k
     int a_worker, b_worker;                          // 0: one operand for all workers
     int eight;                                       // 8-bit operands
@@ -179,7 +218,7 @@ struct GemmArgs {
 __device__ __forceinline__ int part_a(int pairs, int p) { return pairs == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
 __device__ __forceinline__ int part_b(int pairs, int p) { return pairs == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
 
-struct Unit { int r, split, tm, tn, it0, it1; };
+struct Unit { int r, split, tm, tn, kb0, kb1; };      // blocks [kb0, kb1) along k of one tile
 __device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
     Unit t;
     const int tiles = g.tiles_m * g.tiles_n;
@@ -192,9 +231,33 @@ __device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
     i -= band * 8 * g.tiles_n;
     t.tn = i / rows;
     t.tm = band * 8 + (i - t.tn * rows);
-    t.it0 = (int)((long long)g.iters * t.split / g.splits);
-    t.it1 = (int)((long long)g.iters * (t.split + 1) / g.splits);
+    t.kb0 = (int)((long long)g.k_blocks * t.split / g.splits);
+    t.kb1 = (int)((long long)g.k_blocks * (t.split + 1) / g.splits);
     return t;
+}
+
+// 32 x 32 sums in shared memory (row i's group j of four columns at place j ^ (i & 7)): eight columns of a row per lane, or,
+// where rows cannot be written so, a column per lane
+template <int ACT>
+__device__ __forceinline__ void finish_block(const Finish& f, int r, long long m0, long long n1, int rows, const float* pass, int lane, int how) {
+    if (f.vec && n1 + 32 <= f.N) {
+        const int j = lane & 3;
+        Columns<8> c;
+        load_columns(f, r, n1 + 8 * j, c);
+        for (int i = lane >> 2; i < rows; i += 8) {
+            const float4 x = *reinterpret_cast<const float4*>(pass + i * 32 + ((2 * j) ^ (i & 7)) * 4);
+            const float4 y = *reinterpret_cast<const float4*>(pass + i * 32 + ((2 * j + 1) ^ (i & 7)) * 4);
+            float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            finish<ACT>(f, r, m0 + i, n1 + 8 * j, w, c, how);
+        }
+    } else if (n1 + lane < f.N) {
+        Columns<1> c;
+        load_columns(f, r, n1 + lane, c);
+        for (int i = 0; i < rows; ++i) {
+            float w[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
+            finish<ACT>(f, r, m0 + i, n1 + lane, w, c, how);
+        }
+    }
 }
 
 template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return TILE_M * 128 + BN / CG * 128; }
@@ -236,35 +299,36 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             for (int u = cluster; u < g.units && fine; u += clusters) {
                 const Unit t = unit_of(g, u);
                 const int m0 = (t.tm * CG + (int)rank) * TILE_M, n0 = t.tn * BN + (int)rank * B_ROWS;
-                for (int it = t.it0; it < t.it1; ++it, ++c) {
-                    const int slot = c % STAGES;
-                    if (c >= STAGES && !mbar_wait_cluster(&empty[slot], (c / STAGES - 1) & 1, g.limit)) {
-                        fine = false;
-                        break;
-                    }
-                    if (rank == 0) mbar_expect(&full[slot], STAGE * CG);
-                    const uint32_t bar = CG == 2 ? in_block(smem_addr(&full[slot]), 0) : smem_addr(&full[slot]);
-                    const uint32_t a = smem_addr(ring + slot * STAGE), b = a + A_BYTES;
-                    const int p = it / g.k_blocks, k0 = (it - p * g.k_blocks) * g.k_step;
-                    const int pa = part_a(g.pairs, p), pb = part_b(g.pairs, p), ra = t.r * g.a_worker, rb = t.r * g.b_worker;
-                    if (g.a_across) {
-                        for (int j = 0; j < TILE_M / 64; ++j) tile_load<CG>(a + j * 8192, &map_a, bar, m0 + j * 64, k0, pa, ra);
-                    } else {
-                        tile_load<CG>(a, &map_a, bar, k0, m0, pa, ra);
-                    }
-                    if (g.b_across) {
-                        for (int j = 0; j < B_ROWS / 64; ++j) tile_load<CG>(b + j * 8192, &map_b, bar, n0 + j * 64, k0, pb, rb);
-                    } else {
-                        tile_load<CG>(b, &map_b, bar, k0, n0, pb, rb);
+                for (int kb0 = t.kb0; kb0 < t.kb1 && fine; kb0 += g.chunk) {
+                    const int kb1 = min(t.kb1, kb0 + g.chunk);
+                    for (int p = 0; p < g.pairs && fine; ++p) {
+                        const int pa = part_a(g.pairs, p), pb = part_b(g.pairs, p), ra = t.r * g.a_worker, rb = t.r * g.b_worker;
+                        for (int kb = kb0; kb < kb1; ++kb, ++c) {
+                            const int slot = c % STAGES, k0 = kb * g.k_step;
+                            if (c >= STAGES && !(fine = mbar_wait_asleep(&empty[slot], (c / STAGES - 1) & 1, g.limit))) break;
+                            if (rank == 0) mbar_expect(&full[slot], STAGE * CG);
+                            const uint32_t bar = CG == 2 ? in_block(smem_addr(&full[slot]), 0) : smem_addr(&full[slot]);
+                            const uint32_t a = smem_addr(ring + slot * STAGE), b = a + A_BYTES;
+                            if (g.a_across) {
+                                for (int j = 0; j < TILE_M / 64; ++j) tile_load<CG>(a + j * 8192, &map_a, bar, m0 + j * 64, k0, pa, ra);
+                            } else {
+                                tile_load<CG>(a, &map_a, bar, k0, m0, pa, ra);
+                            }
+                            if (g.b_across) {
+                                for (int j = 0; j < B_ROWS / 64; ++j) tile_load<CG>(b + j * 8192, &map_b, bar, n0 + j * 64, k0, pb, rb);
+                            } else {
+                                tile_load<CG>(b, &map_b, bar, k0, n0, pb, rb);
+                            }
+                        }
                     }
                 }
             }
             if (fine) {
                 // the last products' arrivals, which may come from the other block, are in before this one ends
-                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_cluster(&empty[i % STAGES], (i / STAGES) & 1, g.limit);
+                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_asleep(&empty[i % STAGES], (i / STAGES) & 1, g.limit);
             } else if (c > 0 && rank == 0) {
                 // after a wait that ran out: the copies under way (of both blocks: they count here) land before the memory is given up
-                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_cluster(&full[i % STAGES], (i / STAGES) & 1, WAIT_LIMIT_NS);
+                for (int i = c > STAGES ? c - STAGES : 0; i < c; ++i) mbar_wait_asleep(&full[i % STAGES], (i / STAGES) & 1, WAIT_LIMIT_NS);
             } else if (c > 0) {
                 // (the second block's count at the first: it cannot look, and gives them far more time than a copy takes)
                 const unsigned long long t0 = global_ns();
@@ -275,30 +339,32 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (lane == 0 && rank == 0 && g.limit != 0) {
             int c = 0, n = 0;
             bool fine = true;
-            const uint32_t step_a = g.a_across ? 2048 : 32, step_b = g.b_across ? 2048 : 32;
-            for (int u = cluster; u < g.units && fine; u += clusters, ++n) {
+            const uint64_t step_a = (g.a_across ? 2048 : 32) >> 4, step_b = (g.b_across ? 2048 : 32) >> 4;   // 16 (8 bits: 32) along k
+            for (int u = cluster; u < g.units && fine; u += clusters) {
                 const Unit t = unit_of(g, u);
-                const int buf = n & 1;
-                if (!(fine = mbar_wait_cluster(&acc_empty[buf], ((n >> 1) & 1) ^ 1, g.limit))) break;
-                tc_fence_after();
-                for (int it = t.it0; it < t.it1; ++it, ++c) {
-                    const int slot = c % STAGES;
-                    if (!(fine = mbar_wait_cluster(&full[slot], (c / STAGES) & 1, g.limit))) break;
+                for (int kb0 = t.kb0; kb0 < t.kb1 && fine; kb0 += g.chunk, ++n) {
+                    const int buf = n & 1, todo = (min(t.kb1, kb0 + g.chunk) - kb0) * g.pairs;
+                    if (!(fine = mbar_wait_asleep(&acc_empty[buf], ((n >> 1) & 1) ^ 1, g.limit))) break;
                     tc_fence_after();
-                    const uint32_t a = smem_addr(ring + slot * STAGE), b = a + A_BYTES;
+                    for (int it = 0; it < todo; ++it, ++c) {
+                        const int slot = c % STAGES;
+                        if (!(fine = mbar_wait_asleep(&full[slot], (c / STAGES) & 1, g.limit))) break;
+                        tc_fence_after();
+                        const uint32_t a = smem_addr(ring + slot * STAGE);
+                        uint64_t da = tile_descriptor(a, 8192), db = tile_descriptor(a + A_BYTES, 8192);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint64_t da = tile_descriptor(a + k * step_a, 8192), db = tile_descriptor(b + k * step_b, 8192);
-                        if (g.eight) mma<CG, true>(tmem + buf * BN, da, db, g.idesc, it > t.it0 || k);
-                        else mma<CG, false>(tmem + buf * BN, da, db, g.idesc, it > t.it0 || k);
+                        for (int k = 0; k < 4; ++k, da += step_a, db += step_b) {
+                            if (g.eight) mma<CG, true>(tmem + buf * BN, da, db, g.idesc, it || k);
+                            else mma<CG, false>(tmem + buf * BN, da, db, g.idesc, it || k);
+                        }
+                        mma_commit<CG>(&empty[slot]);
                     }
-                    mma_commit<CG>(&empty[slot]);
+                    if (fine) mma_commit<CG>(&acc_full[buf]);
                 }
-                if (fine) mma_commit<CG>(&acc_full[buf]);
             }
             // the products under way are done before their tensor memory is given up
             mma_commit_here<CG>(&drained);
-            mbar_wait_cluster(&drained, 0, WAIT_LIMIT_NS);
+            mbar_wait_asleep(&drained, 0, WAIT_LIMIT_NS);
         }
     } else if (warp >= 4) {
         const int q = warp & 3, half = (warp - 4) >> 2;
@@ -307,61 +373,52 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                                     CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
         int n = 0;
         bool fine = g.limit != 0;
-        for (int u = cluster; u < g.units; u += clusters, ++n) {
+        for (int u = cluster; u < g.units; u += clusters) {
             const Unit t = unit_of(g, u);
-            const int buf = n & 1;
-            if (fine) fine = __all_sync(~0u, mbar_wait_cluster(&acc_full[buf], (n >> 1) & 1, g.limit));
-            if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
-            tc_fence_after();
             const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + half * (BN / 2);
+            for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += g.chunk, ++n) {
+                const int buf = n & 1, how = (g.f.accumulate || kb0 > t.kb0 ? ADD : 0) | (kb0 + g.chunk < t.kb1 ? RAW : 0);
+                if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, g.limit));
+                if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
+                tc_fence_after();
 #pragma unroll 1
-            for (int c0 = 0; c0 < BN / 2; c0 += 32) {
-                uint32_t v[32];
-                if (fine) {
-                    tmem_load32(v, tmem + ((uint32_t)(q * 32) << 16) + buf * BN + half * (BN / 2) + c0);
-                    tmem_wait_load();
-                } else {
+                for (int c0 = 0; c0 < BN / 2; c0 += 32) {
+                    uint32_t v[32];
+                    if (fine) {
+                        tmem_load32(v, tmem + ((uint32_t)(q * 32) << 16) + buf * BN + half * (BN / 2) + c0);
+                        tmem_wait_load();
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = 0x7fffffff;
-                }
-                if (c0 + 32 == BN / 2 && fine) {     // the accumulator is free once its last columns are in registers
-                    tc_fence_before();
+                        for (int i = 0; i < 32; ++i) v[i] = 0x7fffffff;
+                    }
+                    if (c0 + 32 == BN / 2 && fine) { // the accumulator is free once its last columns are in registers
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_at(leader[buf]);
+                    }
+                    const long long n1 = n0 + c0;
+                    if (m0 >= g.M || n1 >= g.N) continue;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4*>(pass + lane * 32 + (j ^ (lane & 7)) * 4) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_at(leader[buf]);
-                }
-                const long long n1 = n0 + c0;
-                if (m0 >= g.M || n1 >= g.N) continue;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<uint4*>(pass + lane * 32 + (j ^ (lane & 7)) * 4) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                __syncwarp();
-                const int rows = (int)min((long long)32, g.M - m0);
-                if (g.splits > 1) {
-                    float* p = g.part + (((long long)t.split * g.R + t.r) * g.M + m0) * g.part_ld + n1;
-                    const int j = lane & 7;
-                    if (n1 + 4 * j < g.part_ld)
-                        for (int i = lane >> 3; i < rows; i += 4)
-                            *reinterpret_cast<float4*>(p + i * g.part_ld + 4 * j) = *reinterpret_cast<float4*>(pass + i * 32 + (j ^ (i & 7)) * 4);
-                } else if (g.f.vec && n1 + 32 <= g.N) {
-                    const int j = lane & 3;
-                    Columns<8> c;
-                    load_columns(g.f, t.r, n1 + 8 * j, c);
-                    for (int i = lane >> 2; i < rows; i += 8) {
-                        float w[8];
-                        const float4 x = *reinterpret_cast<float4*>(pass + i * 32 + ((2 * j) ^ (i & 7)) * 4);
-                        const float4 y = *reinterpret_cast<float4*>(pass + i * 32 + ((2 * j + 1) ^ (i & 7)) * 4);
-                        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
-                        finish(g.f, t.r, m0 + i, n1 + 8 * j, w, c);
+                    const int rows = (int)min((long long)32, g.M - m0);
+                    if (g.splits > 1) {
+                        float* p = g.part + (((long long)t.split * g.R + t.r) * g.M + m0) * g.part_ld + n1;
+                        const int j = lane & 7;
+                        if (n1 + 4 * j < g.part_ld)
+                            for (int i = lane >> 3; i < rows; i += 4)
+                                *reinterpret_cast<float4*>(p + i * g.part_ld + 4 * j) = *reinterpret_cast<float4*>(pass + i * 32 + (j ^ (i & 7)) * 4);
+                    } else {
+                        switch (g.f.act) {
+                        case QS_ACT_RELU: finish_block<QS_ACT_RELU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
+                        case QS_ACT_SILU: finish_block<QS_ACT_SILU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
+                        case QS_ACT_GELU: finish_block<QS_ACT_GELU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
+                        default: finish_block<QS_ACT_NONE>(g.f, t.r, m0, n1, rows, pass, lane, how);
+                        }
                     }
-                } else if (n1 + lane < g.N) {
-                    Columns<1> c;
-                    load_columns(g.f, t.r, n1 + lane, c);
-                    for (int i = 0; i < rows; ++i) {
-                        float w[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
-                        finish(g.f, t.r, m0 + i, n1 + lane, w, c);
-                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
     }
@@ -391,7 +448,7 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, lon
         const int r = (int)(row / f.M);
         Columns<V> c;
         load_columns(f, r, n, c);
-        finish(f, r, row - r * f.M, n, v, c);
+        finish_any(f, r, row - r * f.M, n, v, c, f.accumulate ? ADD : 0);
     }
 }
 
@@ -446,7 +503,7 @@ __global__ void __launch_bounds__(256) small_kernel(const Side a, const Side b, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float v[1] = {acc[i][j]};
-            if (m0 + ty * 4 + i < f.M) finish(f, r, m0 + ty * 4 + i, n, v, c);
+            if (m0 + ty * 4 + i < f.M) finish_any(f, r, m0 + ty * 4 + i, n, v, c, f.accumulate ? ADD : 0);
         }
     }
     }
@@ -499,8 +556,9 @@ Plan plan_of(const Product& p, int sms) {
     q.cg = c2 <= c1 ? 2 : 1;
     q.bn = q.cg == 2 ? 256 : 128;
     const long long tiles = q.cg == 2 ? t2 : t1, slots = sms / q.cg;
-    const long long iters = (p.K + 128 / size - 1) / (128 / size) * (q.planes == 3 ? 6 : 1);
+    const long long k_blocks = (p.K + 128 / size - 1) / (128 / size), iters = k_blocks;
     q.splits = (int)std::max<long long>(1, std::min<long long>({slots / std::max<long long>(1, tiles), iters / 4, 64}));
+    if (q.splits > 1) q.splits = (int)std::max<long long>(q.splits, (k_blocks + CHUNK_BLOCKS - 1) / CHUNK_BLOCKS);
     long long at = 0;
     const long long wa = p.a.worker || p.R == 1 ? p.R : 1, wb = p.b.worker || p.R == 1 ? p.R : 1;
     if (q.lay_a) at += round_up(wa * q.planes * memory_rows(p, p.a) * q.ld_a * size, 256);
@@ -622,7 +680,8 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.k_step = 128 / size;
     g.k_blocks = (int)((p.K + g.k_step - 1) / g.k_step);
     g.pairs = q.planes == 3 ? 6 : 1;
-    g.iters = g.k_blocks * g.pairs;
+    // (the sums so far lie in the result, so it has to hold fp32 and be nothing that is still to be read)
+    g.chunk = q.splits == 1 && f.type == QS_F32 && f.res != f.out ? CHUNK_BLOCKS : g.k_blocks;
     g.eight = type == QS_E4M3;
     // sums in fp32; operand types (e4m3 and fp16 are 0, bf16 is 1); which lie across k; the tile
     const uint32_t t = type == QS_BF16 ? 1 : 0;
@@ -661,7 +720,7 @@ struct ActGradArgs {
     float* part; int parts;                          // (R, parts, N): column sums of the rows of a block, or null
 };
 // 8 warps of rows, 32 V columns per block; block (x, p, r) takes rows p * 8 + warp, + 8 parts, ..
-template <class T, int V>
+template <class T, int V, int ACT>
 __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a) {
     __shared__ float sh[8][32 * V + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.z;
@@ -675,11 +734,11 @@ __global__ void __launch_bounds__(256) act_grad_kernel(const ActGradArgs a) {
             const long long row = r * a.M + m;
             float g[V];
             load_vec<V>(g, static_cast<const T*>(a.g) + row * a.g_stride + n);
-            if (a.act != QS_ACT_NONE) {
+            if (ACT != QS_ACT_NONE) {
                 float z[V];
                 load_vec<V>(z, static_cast<const T*>(a.z) + row * a.z_stride + n);
 #pragma unroll
-                for (int j = 0; j < V; ++j) g[j] *= slope(a.act, z[j]);
+                for (int j = 0; j < V; ++j) g[j] *= slope<ACT>(z[j]);
             }
             if (a.out) store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + n, g);
 #pragma unroll
@@ -702,12 +761,19 @@ int act_parts(int R, int64_t M, int64_t N) {
     const long long columns = R * ((N + 255) / 256);
     return (int)std::max<long long>(1, std::min<long long>((M + 31) / 32, (148 * 12 + columns - 1) / columns));
 }
+template <class T, int V>
+cudaError_t launch_act_grad_of(const ActGradArgs& a, cudaStream_t st) {
+    const dim3 grid((unsigned)((a.N + 32 * V - 1) / (32 * V)), (unsigned)a.parts, (unsigned)a.R);
+    switch (a.act) {
+    case QS_ACT_RELU: return launch(false, act_grad_kernel<T, V, QS_ACT_RELU>, grid, 256, 0, st, a);
+    case QS_ACT_SILU: return launch(false, act_grad_kernel<T, V, QS_ACT_SILU>, grid, 256, 0, st, a);
+    case QS_ACT_GELU: return launch(false, act_grad_kernel<T, V, QS_ACT_GELU>, grid, 256, 0, st, a);
+    default: return launch(false, act_grad_kernel<T, V, QS_ACT_NONE>, grid, 256, 0, st, a);
+    }
+}
 template <class T>
 cudaError_t launch_act_grad(const ActGradArgs& a, bool vec, cudaStream_t st) {
-    constexpr int V = wide_of<T>();
-    const int v = vec ? V : 1;
-    const dim3 grid((unsigned)((a.N + 32 * v - 1) / (32 * v)), (unsigned)a.parts, (unsigned)a.R);
-    return vec ? launch(false, act_grad_kernel<T, V>, grid, 256, 0, st, a) : launch(false, act_grad_kernel<T, 1>, grid, 256, 0, st, a);
+    return vec ? launch_act_grad_of<T, wide_of<T>()>(a, st) : launch_act_grad_of<T, 1>(a, st);
 }
 
 Product forward_of(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const void* w, int w_type, int64_t w_worker, int64_t w_stride) {
@@ -765,6 +831,7 @@ int qs_linear(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type,
     f.M = M; f.N = N; f.bias = bias; f.bias_type = bias_type; f.bias_worker = bias_worker_stride; f.act = activation;
     f.res = residual; f.res_stride = residual_stride; f.pre = pre; f.pre_stride = pre_stride;
     f.out = out; f.type = out_type; f.out_stride = out_stride; f.out_worker = M * out_stride; f.a_scale = x_scale; f.b_scale = w_scale;
+    f.b_scale_worker = w_worker_stride ? N : 0;
     f.vec = rows_aligned(out, out_stride, rows, size, 16) && rows_aligned(residual, residual_stride, rows, size, 16) && rows_aligned(pre, pre_stride, rows, size, 16);
     return run_product(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride), f, work, work_bytes, status,
                        static_cast<cudaStream_t>(cuda_stream));
