@@ -18,6 +18,12 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// one lane of a warp that is all here, always the same one
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -80,11 +86,10 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 
 // D (tensor memory) = A B + (keep ? D : 0); A and B by their descriptors
 template <int CG, bool EIGHT>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool keep) {
-    const uint32_t k = keep;
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t keep) {
 #define QS_MMA(group, kind)                                                                                                  \
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, p;\n\t}" ::"r"(d), \
-                 "l"(a), "l"(b), "r"(idesc), "r"(k)                                                                           \
+                 "l"(a), "l"(b), "r"(idesc), "r"(keep)                                                                          \
                  : "memory")
     if (CG == 2) {
         if (EIGHT) QS_MMA("2", "f8f6f4");
