@@ -66,6 +66,13 @@ __device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, 
                      : "memory");
 }
 
+// a tile of shared memory into a tensor map's place; what lies outside of the tensor is not written
+__device__ __forceinline__ void tile_store(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2),
+                 "r"(c3)
+                 : "memory");
+}
+
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t* dst, uint32_t columns) {
     if (CG == 2) asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(columns) : "memory");

@@ -88,10 +88,10 @@ __device__ __forceinline__ void load_columns(const Finish& f, int r, long long n
         for (int i = 0; i < V; ++i)
             if (n + i < f.N) c.scale[i] = f.b_scale[r * f.b_scale_worker + n + i];
 }
-// Sums of row m (of worker r), columns n on, on their way to the result.  add: to what the result holds; raw: nothing but that
+// Sums of row m (of worker r), columns n on, on their way to the result.  ADD: to what the result holds; RAW: nothing but that
 enum { ADD = 1, RAW = 2 };
 template <int ACT, int V, class T>
-__device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
+__device__ __forceinline__ void finish(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
     const long long row = r * f.M + m;
     T* out = static_cast<T*>(f.out) + r * f.out_worker + m * f.out_stride + n;
     float t[V];
@@ -106,9 +106,8 @@ __device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, l
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = v[i] * s * c.scale[i];
         }
-        if (f.bias)
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += c.bias[i];
+        for (int i = 0; i < V; ++i) v[i] += c.bias[i];
         if (f.pre) store_vec<V>(static_cast<T*>(f.pre) + row * f.pre_stride + n, v);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = activate<ACT>(v[i]);
@@ -120,19 +119,100 @@ __device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, l
     }
     store_vec<V>(out, v);
 }
-template <int ACT, int V>
-__device__ __forceinline__ void finish(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
-    if (f.type == QS_F32) finish_as<ACT, V, float>(f, r, m, n, v, c, how);
-    else if (f.type == QS_BF16) finish_as<ACT, V, bf16>(f, r, m, n, v, c, how);
-    else finish_as<ACT, V, __half>(f, r, m, n, v, c, how);
+template <int V, class T>
+__device__ __forceinline__ void finish_as(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
+    switch (f.act) {
+    case QS_ACT_RELU: return finish<QS_ACT_RELU, V, T>(f, r, m, n, v, c, how);
+    case QS_ACT_SILU: return finish<QS_ACT_SILU, V, T>(f, r, m, n, v, c, how);
+    case QS_ACT_GELU: return finish<QS_ACT_GELU, V, T>(f, r, m, n, v, c, how);
+    default: return finish<QS_ACT_NONE, V, T>(f, r, m, n, v, c, how);
+    }
 }
 template <int V>
 __device__ __forceinline__ void finish_any(const Finish& f, int r, long long m, long long n, float (&v)[V], const Columns<V>& c, int how) {
-    switch (f.act) {
-    case QS_ACT_RELU: return finish<QS_ACT_RELU>(f, r, m, n, v, c, how);
-    case QS_ACT_SILU: return finish<QS_ACT_SILU>(f, r, m, n, v, c, how);
-    case QS_ACT_GELU: return finish<QS_ACT_GELU>(f, r, m, n, v, c, how);
-    default: return finish<QS_ACT_NONE>(f, r, m, n, v, c, how);
+    if (f.type == QS_F32) finish_as<V, float>(f, r, m, n, v, c, how);
+    else if (f.type == QS_BF16) finish_as<V, bf16>(f, r, m, n, v, c, how);
+    else finish_as<V, __half>(f, r, m, n, v, c, how);
+}
+
+// The same for 32 x 32 sums, one row per lane, on their way to a tile of shared memory that a copy takes to the result (and
+// another to `pre`): rows of 128 bytes, pieces of 16 bytes at place piece ^ (row & 7).
+template <class T> struct Raw32 { uint4 a[2 * sizeof(T)]; };                 // 32 elements
+// (whole pieces alone: where there is anything to read, rows end with one.  FRESH: what this kernel's copies wrote is not
+// looked for in the L1)
+template <class T, bool FRESH>
+__device__ __forceinline__ void load_raw(Raw32<T>& q, const T* p, int left) {
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
+        q.a[k] = make_uint4(0, 0, 0, 0);
+        const uint4* at = reinterpret_cast<const uint4*>(p) + k;
+        if (k * W < left) q.a[k] = FRESH ? __ldcg(at) : *at;
+    }
+}
+template <class T>
+__device__ __forceinline__ void add_raw(float (&v)[32], const Raw32<T>& q) {
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
+        const Pack<T, W> e = *reinterpret_cast<const Pack<T, W>*>(&q.a[k]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[k * W + i] += to_float(e.e[i]);
+    }
+}
+template <class T>
+__device__ __forceinline__ void put_row(uint8_t* tile, int lane, int first, const float (&v)[32]) {
+    constexpr int W = 16 / sizeof(T);
+#pragma unroll
+    for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
+        Pack<T, W> e;
+#pragma unroll
+        for (int i = 0; i < W; ++i) e.e[i] = from_float<T>(v[k * W + i]);
+        *reinterpret_cast<uint4*>(tile + lane * 128 + (((first + k) ^ (lane & 7)) << 4)) = *reinterpret_cast<uint4*>(&e);
+    }
+}
+// `first`: the row's pieces in front of these; bias, scale: of the 32 columns; left: columns that there are
+template <int ACT, class T>
+__device__ __forceinline__ void finish_row(const Finish& f, float (&v)[32], const T* out, const T* res, int left, float a_scale, const float* bias,
+                                           const float* scale, uint8_t* out_tile, uint8_t* pre_tile, int first, int lane, int how) {
+    Raw32<T> q;
+    if (how & ADD) {
+        load_raw<T, true>(q, out, left);
+        add_raw<T>(v, q);
+    }
+    if (!(how & RAW)) {
+        if (res) load_raw<T, false>(q, res, left);
+        if (f.a_scale) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const float4 s = *reinterpret_cast<const float4*>(scale + i);
+                v[i] = v[i] * a_scale * s.x, v[i + 1] = v[i + 1] * a_scale * s.y, v[i + 2] = v[i + 2] * a_scale * s.z, v[i + 3] = v[i + 3] * a_scale * s.w;
+            }
+        }
+        if (f.bias) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const float4 b = *reinterpret_cast<const float4*>(bias + i);
+                v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+            }
+        }
+        if (f.pre) put_row<T>(pre_tile, lane, first, v);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = activate<ACT>(v[i]);
+        if (res) add_raw<T>(v, q);
+    }
+    put_row<T>(out_tile, lane, first, v);
+}
+// Where rows are not on 16-byte boundaries: the sums in shared memory (row i's group j of four columns at place j ^ (i & 7)), a
+// column per lane
+template <int ACT, class T>
+__device__ __forceinline__ void finish_columns(const Finish& f, int r, long long m0, long long n, int rows, const float* pass, int lane, int how) {
+    Columns<1> c;
+    load_columns(f, r, n, c);
+#pragma unroll 8
+    for (int i = 0; i < rows; ++i) {
+        float v[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
+        finish<ACT, 1, T>(f, r, m0 + i, n, v, c, how);
     }
 }
 
@@ -191,12 +271,12 @@ __global__ void __launch_bounds__(256) lay_kernel(const LayArgs a) {
 
 // ------------------------------------------------------------------ the product
 constexpr int TILE_M = 128;                          // rows of a block's part of a tile: the lanes of tensor memory
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
 // The matrix unit cuts what lies below 2^-24 of a sum at every addition, always towards zero: 8e-10 of the result per element
 // summed.  Results in fp32 are therefore added up from sums over this many blocks of 128 bytes (4096 elements of 16 bits: 3e-6).
 constexpr int CHUNK_BLOCKS = 64;
-constexpr int PASS_BYTES = 8 * 4096;                 // 32 x 32 sums on their way from lanes to rows, per finishing warp
+constexpr int PASS_BYTES = 8 * 2 * 4096;             // two tiles of 32 rows of 128 bytes on their way out, per finishing warp
 
 struct GemmArgs {
     int R;
@@ -208,7 +288,7 @@ struct GemmArgs {
     int a_worker, b_worker;                          // 0: one operand for all workers
     int eight;                                       // 8-bit operands
     uint32_t idesc;
-    float* part; long long part_ld;                  // splits > 1: (splits, R, M, part_ld) sums instead of results
+    int columns;                                     // there is a bias or a scale of the columns
     unsigned long long limit;
     int* status;
     Finish f;
@@ -236,44 +316,27 @@ __device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
     return t;
 }
 
-// 32 x 32 sums in shared memory (row i's group j of four columns at place j ^ (i & 7)): eight columns of a row per lane, or,
-// where rows cannot be written so, a column per lane
-template <int ACT>
-__device__ __forceinline__ void finish_block(const Finish& f, int r, long long m0, long long n1, int rows, const float* pass, int lane, int how) {
-    if (f.vec && n1 + 32 <= f.N) {
-        const int j = lane & 3;
-        Columns<8> c;
-        load_columns(f, r, n1 + 8 * j, c);
-        for (int i = lane >> 2; i < rows; i += 8) {
-            const float4 x = *reinterpret_cast<const float4*>(pass + i * 32 + ((2 * j) ^ (i & 7)) * 4);
-            const float4 y = *reinterpret_cast<const float4*>(pass + i * 32 + ((2 * j + 1) ^ (i & 7)) * 4);
-            float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-            finish<ACT>(f, r, m0 + i, n1 + 8 * j, w, c, how);
-        }
-    } else if (n1 + lane < f.N) {
-        Columns<1> c;
-        load_columns(f, r, n1 + lane, c);
-        for (int i = 0; i < rows; ++i) {
-            float w[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
-            finish<ACT>(f, r, m0 + i, n1 + lane, w, c, how);
-        }
-    }
-}
-
 template <int CG, int BN> __host__ __device__ constexpr int stage_bytes() { return TILE_M * 128 + BN / CG * 128; }
-template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return STAGES * stage_bytes<CG, BN>() + PASS_BYTES + 1024; }
+struct Small {                                       // beside the ring and the tiles on their way out
+    float bias[256], scale[256];                     // of the columns at hand, per half of the finishing warps
+    uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem_at;
+};
+template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return STAGES * stage_bytes<CG, BN>() + PASS_BYTES + (int)sizeof(Small); }
 
 // A tile of TILE_M CG x BN per cluster of CG blocks.  Copies (one thread per block) keep a ring of STAGES tiles of both
 // operands filling; one thread of the leading block issues the products into one of two accumulators; eight warps per
 // block take the other one out: they turn 32 x 32 sums through shared memory so that rows leave in whole sectors.
-template <int CG, int BN>
+template <int CG, int BN, class T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
-gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const GemmArgs g) {
-    extern __shared__ uint8_t raw[];
-    __shared__ uint64_t full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drained;
-    __shared__ uint32_t tmem_at;
+gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+            const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GemmArgs g) {
+    extern __shared__ __align__(1024) uint8_t ring[];
     constexpr int A_BYTES = TILE_M * 128, B_ROWS = BN / CG, STAGE = stage_bytes<CG, BN>();
-    uint8_t* ring = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    Small& small = *reinterpret_cast<Small*>(ring + STAGES * STAGE + PASS_BYTES);
+    uint64_t *full = small.full, *empty = small.empty, *acc_full = small.acc_full, *acc_empty = small.acc_empty;
+    // (tiles are swizzled by their addresses: off the 1024-byte boundary nothing is begun, as with a wait that runs out at once)
+    const unsigned long long limit = smem_addr(ring) & 1023 ? 0 : g.limit;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
@@ -281,15 +344,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 8 * CG);
-        mbar_init(&drained, 1);
+        mbar_init(&small.drained, 1);
         fence_barrier_init();
     }
-    if (warp == 2) tmem_alloc<CG>(&tmem_at, 2 * BN);
+    if (warp == 2) tmem_alloc<CG>(&small.tmem_at, 2 * BN);
     tc_fence_before();
     if (CG == 2) cluster_sync();
     else __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = small.tmem_at;
     after_launch();
 
     // (Both of these warps run as one: a single lane's loop around the products left the matrix unit idle for 300 of 810 cycles
@@ -298,7 +361,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const bool me = elected();
         int slot = 0, count = 0;
         uint32_t phase = 1;                          // (of a new barrier: the phase before counts as over)
-        bool fine = g.limit != 0;
+        bool fine = limit != 0;
         for (int u = cluster; u < g.units && fine; u += clusters) {
             const Unit t = unit_of(g, u);
             const int m0 = (t.tm * CG + (int)rank) * TILE_M, n0 = t.tn * BN + (int)rank * B_ROWS, ra = t.r * g.a_worker, rb = t.r * g.b_worker;
@@ -307,7 +370,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 for (int p = 0; p < g.pairs && fine; ++p) {
                     const int pa = part_a(g.pairs, p), pb = part_b(g.pairs, p);
                     for (int kb = kb0; kb < kb1; ++kb) {
-                        if (!(fine = mbar_wait_asleep(&empty[slot], phase, g.limit))) break;
+                        if (!(fine = mbar_wait_asleep(&empty[slot], phase, limit))) break;
                         if (me) {
                             const int k0 = kb * g.k_step;
                             if (rank == 0) mbar_expect(&full[slot], STAGE * CG);
@@ -331,11 +394,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 }
             }
         }
-        if (g.limit == 0) count = 0;
+        if (limit == 0) count = 0;
         if (fine) {
             // the last products' arrivals, which may come from the other block, are in before this one ends
             for (int i = 0; i < STAGES; ++i) {
-                if (count >= STAGES || slot < count) mbar_wait_asleep(&empty[slot], phase, g.limit);
+                if (count >= STAGES || slot < count) mbar_wait_asleep(&empty[slot], phase, limit);
                 if (++slot == STAGES) slot = 0, phase ^= 1;
             }
         } else if (count > 0 && rank == 0) {
@@ -347,7 +410,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             while (global_ns() - t0 < 10000000ull) {}
         }
     } else if (warp == 1) {
-        if (rank == 0 && g.limit != 0) {
+        if (rank == 0 && limit != 0) {
             const bool me = elected();
             int n = 0, slot = 0;
             uint32_t phase = 0;
@@ -358,18 +421,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 const Unit t = unit_of(g, u);
                 for (int kb0 = t.kb0; kb0 < t.kb1 && fine; kb0 += g.chunk, ++n) {
                     const uint32_t d = tmem + (n & 1) * BN;
-                    if (!(fine = mbar_wait_asleep(&acc_empty[n & 1], ((n >> 1) & 1) ^ 1, g.limit))) break;
+                    if (!(fine = mbar_wait_asleep(&acc_empty[n & 1], ((n >> 1) & 1) ^ 1, limit))) break;
                     tc_fence_after();
                     const int todo = (min(t.kb1, kb0 + g.chunk) - kb0) * g.pairs;
                     for (int it = 0; it < todo; ++it) {
-                        if (!(fine = mbar_wait_asleep(&full[slot], phase, g.limit))) break;
+                        if (!(fine = mbar_wait_asleep(&full[slot], phase, limit))) break;
                         tc_fence_after();
                         if (me) {
                             const uint64_t da = first + slot * (STAGE >> 4), db = da + (A_BYTES >> 4);
+                            // (four in a row behind one branch: with a branch at each, 649 cycles per slot in 16 bits, not 516)
+                            if (g.eight) {
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if (g.eight) mma<CG, true>(d, da + k * step_a, db + k * step_b, g.idesc, it | k);
-                                else mma<CG, false>(d, da + k * step_a, db + k * step_b, g.idesc, it | k);
+                                for (int k = 0; k < 4; ++k) mma<CG, true>(d, da + k * step_a, db + k * step_b, g.idesc, it | k);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) mma<CG, false>(d, da + k * step_a, db + k * step_b, g.idesc, it | k);
                             }
                             mma_commit<CG>(&empty[slot]);
                         }
@@ -381,65 +447,114 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 }
             }
             // the products under way are done before their tensor memory is given up
-            if (me) mma_commit_here<CG>(&drained);
+            if (me) mma_commit_here<CG>(&small.drained);
             __syncwarp();
-            mbar_wait_asleep(&drained, 0, WAIT_LIMIT_NS);
+            mbar_wait_asleep(&small.drained, 0, WAIT_LIMIT_NS);
         }
     } else if (warp >= 4) {
+        constexpr int HALF = BN / 2, WIDE = 128 / sizeof(T);                 // columns of a warp; of a tile on its way out
         const int q = warp & 3, half = (warp - 4) >> 2;
-        float* pass = reinterpret_cast<float*>(ring + STAGES * STAGE) + (warp - 4) * 1024;
+        uint8_t* pass = ring + STAGES * STAGE + (warp - 4) * 8192;
+        float *bias = small.bias + half * HALF, *scale = small.scale + half * HALF;
         const uint32_t leader[2] = {CG == 2 ? in_block(smem_addr(&acc_empty[0]), 0) : smem_addr(&acc_empty[0]),
                                     CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
-        int n = 0;
-        bool fine = g.limit != 0;
+        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + half * HALF;
+        int n = 0, out_buf = 0;
+        bool fine = limit != 0;
         for (int u = cluster; u < g.units; u += clusters) {
             const Unit t = unit_of(g, u);
-            const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + half * (BN / 2);
+            const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + half * HALF;
+            const long long m = m0 + lane, row = t.r * g.M + m;
+            const bool in = m < g.M;
+            if (g.columns) {                         // (uniform) what belongs to the columns, for the four warps of this half
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                const int i = q * 32 + lane;
+                if (i < HALF) {
+                    const bool there = n0 + i < g.N;
+                    bias[i] = g.f.bias && there ? element(g.f.bias, g.f.bias_type, t.r * g.f.bias_worker + n0 + i) : 0.0f;
+                    scale[i] = g.f.b_scale && there ? g.f.b_scale[t.r * g.f.b_scale_worker + n0 + i] : 1.0f;
+                }
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+            }
+            const float a_scale = g.f.a_scale && in ? g.f.a_scale[row] : 1.0f;
             for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += g.chunk, ++n) {
-                const int buf = n & 1, how = (g.f.accumulate || kb0 > t.kb0 ? ADD : 0) | (kb0 + g.chunk < t.kb1 ? RAW : 0);
-                if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, g.limit));
+                const int buf = n & 1, how = (g.f.accumulate || kb0 > t.kb0 ? ADD : 0) | (kb0 + g.chunk < t.kb1 || g.splits > 1 ? RAW : 0);
+                if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, limit));
                 if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
                 tc_fence_after();
-#pragma unroll 1
-                for (int c0 = 0; c0 < BN / 2; c0 += 32) {
-                    uint32_t v[32];
-                    if (fine) {
-                        tmem_load32(v, tmem + ((uint32_t)(q * 32) << 16) + buf * BN + half * (BN / 2) + c0);
-                        tmem_wait_load();
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = 0x7fffffff;
-                    }
-                    if (c0 + 32 == BN / 2 && fine) { // the accumulator is free once its last columns are in registers
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_at(leader[buf]);
-                    }
-                    const long long n1 = n0 + c0;
-                    if (m0 >= g.M || n1 >= g.N) continue;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4*>(pass + lane * 32 + (j ^ (lane & 7)) * 4) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                // sums of the chunks before have arrived where they are read again
+                if (how & ADD) {
+                    bulk_wait_all();
                     __syncwarp();
-                    const int rows = (int)min((long long)32, g.M - m0);
-                    if (g.splits > 1) {
-                        float* p = g.part + (((long long)t.split * g.R + t.r) * g.M + m0) * g.part_ld + n1;
-                        const int j = lane & 7;
-                        if (n1 + 4 * j < g.part_ld)
-                            for (int i = lane >> 3; i < rows; i += 4)
-                                *reinterpret_cast<float4*>(p + i * g.part_ld + 4 * j) = *reinterpret_cast<float4*>(pass + i * 32 + (j ^ (i & 7)) * 4);
-                    } else {
-                        switch (g.f.act) {
-                        case QS_ACT_RELU: finish_block<QS_ACT_RELU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
-                        case QS_ACT_SILU: finish_block<QS_ACT_SILU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
-                        case QS_ACT_GELU: finish_block<QS_ACT_GELU>(g.f, t.r, m0, n1, rows, pass, lane, how); break;
-                        default: finish_block<QS_ACT_NONE>(g.f, t.r, m0, n1, rows, pass, lane, how);
+                }
+#pragma unroll 1
+                for (int c0 = 0; c0 < HALF; c0 += WIDE) {
+                    const long long n1 = n0 + c0;
+                    const bool some = m0 < g.M && n1 < g.N;
+                    uint8_t* tile = pass + (g.f.pre ? 0 : out_buf * 4096);
+                    if (some && g.f.vec) {           // the tile's last copy has been read
+                        if (g.f.pre) bulk_wait_read<0>();
+                        else bulk_wait_read<1>();
+                        __syncwarp();
+                    }
+#pragma unroll 1
+                    for (int c = 0; c < WIDE; c += 32) {
+                        uint32_t raw[32];
+                        float v[32];
+                        if (fine) {
+                            tmem_load32(raw, from + buf * BN + c0 + c);
+                            tmem_wait_load();
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = fine ? __uint_as_float(raw[i]) : quiet_nan();
+                        if (c0 + c + 32 == HALF && fine) {           // the accumulator is free once its last columns are in registers
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_at(leader[buf]);
+                        }
+                        if (!some) continue;
+                        if (g.f.vec) {
+                            const T* out = static_cast<const T*>(g.f.out) + t.r * g.f.out_worker + m * g.f.out_stride + n1 + c;
+                            const T* res = g.f.res ? static_cast<const T*>(g.f.res) + row * g.f.res_stride + n1 + c : nullptr;
+                            const int left = in ? (int)max(0ll, min(32ll, g.N - n1 - c)) : 0, first = c * (int)sizeof(T) / 16;
+                            switch (g.f.act) {
+                            case QS_ACT_RELU: finish_row<QS_ACT_RELU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
+                            case QS_ACT_SILU: finish_row<QS_ACT_SILU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
+                            case QS_ACT_GELU: finish_row<QS_ACT_GELU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
+                            default: finish_row<QS_ACT_NONE, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how);
+                            }
+                        } else {
+                            float* turn = reinterpret_cast<float*>(pass);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(turn + lane * 32 + (j ^ (lane & 7)) * 4) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                            __syncwarp();
+                            const int rows = (int)min((long long)32, g.M - m0);
+                            const long long col = n1 + c + lane;
+                            if (col < g.N) {
+                                switch (g.f.act) {
+                                case QS_ACT_RELU: finish_columns<QS_ACT_RELU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
+                                case QS_ACT_SILU: finish_columns<QS_ACT_SILU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
+                                case QS_ACT_GELU: finish_columns<QS_ACT_GELU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
+                                default: finish_columns<QS_ACT_NONE, T>(g.f, t.r, m0, col, rows, turn, lane, how);
+                                }
+                            }
+                            __syncwarp();
                         }
                     }
-                    __syncwarp();
+                    if (some && g.f.vec) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tile_store(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
+                            if (g.f.pre && !(how & RAW)) tile_store(&map_pre, smem_addr(pass + 4096), (int)n1, (int)m0, 0, t.r);
+                            bulk_commit();
+                        }
+                        out_buf ^= 1;
+                    }
                 }
             }
         }
+        bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
@@ -452,10 +567,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 template <int V>
 __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, long long ld, int splits, int R, const Finish f) {
     after_launch();
-    const long long units = (f.N + V - 1) / V, items = R * f.M * units, plane = R * f.M * ld;
+    const long long units = (f.N + V - 1) / V, items = R * f.M * units, plane = f.M * ld;      // part: (R, splits, M, ld)
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
         const long long row = i / units, n = (i - row * units) * V;
-        const float* p = part + row * ld + n;
+        const int r = (int)(row / f.M);
+        const float* p = part + (row + r * (splits - 1) * f.M) * ld + n;
         float v[V];
         load_floats<V>(v, p);
         for (int s = 1; s < splits; ++s) {
@@ -464,7 +580,6 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, lon
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] += t[j];
         }
-        const int r = (int)(row / f.M);
         Columns<V> c;
         load_columns(f, r, n, c);
         finish_any(f, r, row - r * f.M, n, v, c, f.accumulate ? ADD : 0);
@@ -607,7 +722,7 @@ EncodeFn encoder() {
 // (inner, outer, plane, worker) in boxes of 128 bytes by `box` rows
 bool encode(CUtensorMap* map, const void* p, int type, long long inner, long long outer, int planes, long long workers, long long ld, long long plane,
             long long worker, int box) {
-    const int size = type == QS_E4M3 ? 1 : 2;
+    const int size = bytes_of(type);
     const EncodeFn fn = encoder();
     if (!fn) return false;
     const cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)outer, (cuuint64_t)planes, (cuuint64_t)workers};
@@ -615,9 +730,17 @@ bool encode(CUtensorMap* map, const void* p, int type, long long inner, long lon
     const long long row = outer > 1 ? ld * size : round_up(inner * size, 16);
     const cuuint64_t strides[3] = {(cuuint64_t)row, (cuuint64_t)(planes > 1 ? plane * size : row), (cuuint64_t)(workers > 1 ? worker * size : row)};
     const cuuint32_t boxes[4] = {(cuuint32_t)(128 / size), (cuuint32_t)box, 1, 1}, ones[4] = {1, 1, 1, 1};
-    const CUtensorMapDataType t = type == QS_E4M3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : type == QS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const CUtensorMapDataType t = type == QS_E4M3  ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                  : type == QS_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                  : type == QS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                   : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     return fn(map, t, 4, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// a result, written in tiles of 32 rows
+bool encode_out(CUtensorMap* map, const void* p, int type, long long N, long long M, int planes, long long workers, long long ld, long long plane, long long worker) {
+    return encode(map, p, type, N, M, planes, workers, ld, plane, worker, 32);
 }
 
 unsigned long long wait_limit() {
@@ -638,10 +761,10 @@ cudaError_t lay_out(const Product& p, const Operand& o, void* dst, int dst_type,
     return launch(false, lay_kernel, dim3((unsigned)std::min<long long>((items + 255) / 256, 1 << 16), (unsigned)workers), 256, 0, st, a);
 }
 
-template <int CG, int BN>
-cudaError_t launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& g, bool after, int sms, cudaStream_t st) {
+template <int CG, int BN, class T>
+cudaError_t launch_gemm_as(const CUtensorMap (&map)[4], const GemmArgs& g, bool after, int sms, cudaStream_t st) {
     constexpr int smem = gemm_smem<CG, BN>();
-    cudaError_t e = cudaFuncSetAttribute(gemm_kernel<CG, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaError_t e = cudaFuncSetAttribute(gemm_kernel<CG, BN, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min(g.units, sms / CG) * CG);
@@ -656,7 +779,13 @@ cudaError_t launch_gemm(const CUtensorMap& ma, const CUtensorMap& mb, const Gemm
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = after ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, gemm_kernel<CG, BN>, ma, mb, g);
+    return cudaLaunchKernelEx(&cfg, gemm_kernel<CG, BN, T>, map[0], map[1], map[2], map[3], g);
+}
+template <int CG, int BN>
+cudaError_t launch_gemm(const CUtensorMap (&map)[4], const GemmArgs& g, bool after, int sms, cudaStream_t st) {
+    // (sums of splits are written in fp32 whatever the result's type: one form is enough)
+    if (g.f.type == QS_F32 || g.splits > 1) return launch_gemm_as<CG, BN, float>(map, g, after, sms, st);
+    return g.f.type == QS_BF16 ? launch_gemm_as<CG, BN, bf16>(map, g, after, sms, st) : launch_gemm_as<CG, BN, __half>(map, g, after, sms, st);
 }
 
 int run_product(const Product& p, const Finish& f, void* work, int64_t work_bytes, int* status, cudaStream_t st) {
@@ -673,7 +802,7 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     uint8_t* w = static_cast<uint8_t*>(work);
     const int type = p.type == QS_F32 ? QS_BF16 : p.type, size = type == QS_E4M3 ? 1 : 2;
     GemmArgs g{};
-    CUtensorMap map[2];
+    CUtensorMap map[4] = {};
     bool after = false;
     for (int i = 0; i < 2; ++i) {
         const Operand& o = i ? p.b : p.a;
@@ -705,17 +834,26 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     // sums in fp32; operand types (e4m3 and fp16 are 0, bf16 is 1); which lie across k; the tile
     const uint32_t t = type == QS_BF16 ? 1 : 0;
     g.idesc = 1u << 4 | t << 7 | t << 10 | (uint32_t)g.a_across << 15 | (uint32_t)g.b_across << 16 | (uint32_t)(q.bn / 8) << 17 | (uint32_t)(TILE_M * q.cg / 16) << 24;
-    g.part = reinterpret_cast<float*>(w + q.off_part);
-    g.part_ld = q.part_ld;
     g.limit = wait_limit();
     g.status = status;
     g.f = f;
-    cudaError_t e = q.cg == 2 ? launch_gemm<2, 256>(map[0], map[1], g, after, sms, st) : launch_gemm<1, 128>(map[0], map[1], g, after, sms, st);
+    g.columns = q.splits == 1 && (f.bias || f.b_scale);
+    if ((f.res || f.accumulate || g.chunk < g.k_blocks) && p.N * size_of_type(f.type) % 16) g.f.vec = 0;
+    float* part = reinterpret_cast<float*>(w + q.off_part);
+    if (q.splits > 1) {                              // sums instead of results: (R, splits, M, part_ld)
+        g.f = Finish{};
+        g.f.M = p.M; g.f.N = p.N; g.f.type = QS_F32; g.f.vec = 1;
+        if (!encode_out(&map[2], part, QS_F32, p.N, p.M, q.splits, p.R, q.part_ld, p.M * q.part_ld, q.splits * p.M * q.part_ld)) return QS_CUDA;
+    } else if (g.f.vec) {
+        if (!encode_out(&map[2], f.out, f.type, p.N, p.M, 1, p.R, f.out_stride, 0, f.out_worker) ||
+            (f.pre && !encode_out(&map[3], f.pre, f.type, p.N, p.M, 1, p.R, f.pre_stride, 0, p.M * f.pre_stride))) return QS_CUDA;
+    }
+    cudaError_t e = q.cg == 2 ? launch_gemm<2, 256>(map, g, after, sms, st) : launch_gemm<1, 128>(map, g, after, sms, st);
     if (e != cudaSuccess || q.splits == 1) return status_of(e);
     const long long items = p.R * p.M * (f.vec ? (p.N + 7) / 8 : p.N);
     const dim3 grid((unsigned)std::min<long long>((items + 255) / 256, 1 << 20));
-    e = f.vec && p.N % 8 == 0 ? launch(true, join_splits_kernel<8>, grid, 256, 0, st, (const float*)g.part, g.part_ld, q.splits, p.R, f)
-                              : launch(true, join_splits_kernel<1>, grid, 256, 0, st, (const float*)g.part, g.part_ld, q.splits, p.R, f);
+    e = f.vec && p.N % 8 == 0 ? launch(true, join_splits_kernel<8>, grid, 256, 0, st, (const float*)part, q.part_ld, q.splits, p.R, f)
+                              : launch(true, join_splits_kernel<1>, grid, 256, 0, st, (const float*)part, q.part_ld, q.splits, p.R, f);
     return status_of(e);
 }
 
