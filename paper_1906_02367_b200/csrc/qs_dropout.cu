@@ -4,11 +4,11 @@
 //
 // with one Philox4x32-10 word per element: key = the seed, counter = (element >> 2, worker, round's low half,
 // layer << 16 | round's bits 32 to 39 << 8 | 2), word = out[element & 3]; 2 is this operator's stream beside those of
-// the sparsifier and the quantizer.  A row is read and written once by vectors of 16 bytes (two or one draws of four words
-// each); the generator's ten rounds keep about half of the issue slots busy while memory sets the pace.
+// the sparsifier and the quantizer.  A row is read and written once by vectors of 16 bytes, each with one or two draws of four
+// words.  In fp32 memory sets the pace (6.7 TB/s); in 16 bits the generator does as much: ten rounds are about 20 of the 25
+// instructions per element, and the multipliers and the logic units are each about half busy (4.6 to 5.0 TB/s).
 #include <algorithm>
 
-#include "qs_common.cuh"
 #include "qs_vec.cuh"
 
 namespace qs {
@@ -19,72 +19,75 @@ struct DropArgs {
     const void* x; long long x_stride;
     const void* res; long long res_stride;
     void* out; long long out_stride;
-    uint32_t seed_lo, seed_hi, round_lo, word3, worker, threshold;
+    uint2 key[10];                                   // of the rounds
+    uint32_t round_lo, word3, worker, threshold;
     float c;
-    long long vecs;                                  // work items of a row (vectors), or of a worker (groups of four)
+    long long vecs, items;                           // work items of a row (vectors), or of a worker (groups of four); of all
 };
 
+// Philox4x32-10 with the ten round keys at hand: two wide products and two xors a round
 __device__ __forceinline__ uint4 words_of(const DropArgs& a, uint32_t worker, uint32_t quad) {
-    return philox4x32_10(make_uint4(quad, a.worker + worker, a.round_lo, a.word3), make_uint2(a.seed_lo, a.seed_hi));
+    uint4 c = make_uint4(quad, a.worker + worker, a.round_lo, a.word3);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const unsigned long long p0 = (unsigned long long)0xD2511F53u * c.x, p1 = (unsigned long long)0xCD9E8D57u * c.z;
+        c = make_uint4((uint32_t)(p1 >> 32) ^ c.y ^ a.key[i].x, (uint32_t)p1, (uint32_t)(p0 >> 32) ^ c.w ^ a.key[i].y, (uint32_t)p0);
+    }
+    return c;
 }
 __device__ __forceinline__ float dropped(const DropArgs& a, float x, uint32_t word) { return word >= a.threshold ? x * a.c : 0.0f; }
 
 // Rows whose elements come in vectors of V, the first of each at a multiple of four elements of its worker
-template <class T, int V, int U, bool RES>
-__global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
-    const long long items = a.rows * a.vecs, step = (long long)gridDim.x * 256;
-    for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < items; i0 += step * U) {
-        float x[U][V], res[U][V];
-        long long row[U], at[U];
+// FLAT: one row.  A vector per thread: what is in flight comes from many resident warps, and 32 registers let all of them in (8192 x
+// 4096 in bf16 with a residual: 44.0 us with eight blocks an SM, 46.2 with six; two vectors a thread 51; blocks that stay, with the
+// next vector on its way, 75)
+template <class T, int V, bool RES, bool FLAT>
+__global__ void __launch_bounds__(256, 8) dropout_kernel(const DropArgs a) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.items) return;
+    const long long row = FLAT ? 0 : i / a.vecs, at = (FLAT ? i : i - row * a.vecs) * V, w = FLAT || a.per == 1 ? row : row / a.per;
+    const T* p = static_cast<const T*>(a.x) + row * a.x_stride + at;
+    const T* q = static_cast<const T*>(a.res) + row * a.res_stride + at;
+    T* o = static_cast<T*>(a.out) + row * a.out_stride + at;
+    const bool whole = at + V <= a.D;
+    Pack<T, V> x, res;
+    if (whole) {
+        x = *reinterpret_cast<const Pack<T, V>*>(p);
+        if (RES) res = *reinterpret_cast<const Pack<T, V>*>(q);
+    } else {                                         // the row's last elements
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = i0 + u * step;
-            row[u] = a.rows == 1 ? 0 : i / a.vecs;
-            at[u] = (i - row[u] * a.vecs) * V;
-            if (i >= items || at[u] + V > a.D) continue;
-            load_vec<V>(x[u], static_cast<const T*>(a.x) + row[u] * a.x_stride + at[u]);
-            if (RES) load_vec<V>(res[u], static_cast<const T*>(a.res) + row[u] * a.res_stride + at[u]);
+        for (int j = 0; j < V; ++j) {
+            x.e[j] = at + j < a.D ? p[j] : from_float<T>(0.0f);
+            if (RES) res.e[j] = at + j < a.D ? q[j] : from_float<T>(0.0f);
         }
+    }
+    const uint32_t quad = (uint32_t)(((FLAT ? 0 : (row - w * a.per) * a.D) + at) >> 2);
+    float v[V];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (i0 + u * step >= items) break;
-            const long long w = a.per == 1 ? row[u] : row[u] / a.per, e = (row[u] - w * a.per) * a.D + at[u];
-            const bool whole = at[u] + V <= a.D;
-            if (!whole) {                            // the row's last elements
-                const T* p = static_cast<const T*>(a.x) + row[u] * a.x_stride + at[u];
+    for (int j = 0; j < V / 4; ++j) {
+        const uint4 r = words_of(a, (uint32_t)w, quad + j);
+        const uint32_t word[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    x[u][j] = at[u] + j < a.D ? to_float(p[j]) : 0.0f;
-                    if (RES) res[u][j] = at[u] + j < a.D ? to_float(static_cast<const T*>(a.res)[row[u] * a.res_stride + at[u] + j]) : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                const uint4 r = words_of(a, (uint32_t)w, (uint32_t)((e + j) >> 2));
-                const uint32_t word[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float v = dropped(a, x[u][j + k], word[k]);
-                    x[u][j + k] = RES ? v + res[u][j + k] : v;
-                }
-            }
-            T* o = static_cast<T*>(a.out) + row[u] * a.out_stride + at[u];
-            if (whole) {
-                store_vec<V>(o, x[u]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (at[u] + j < a.D) o[j] = from_float<T>(x[u][j]);
-            }
+        for (int k = 0; k < 4; ++k) {
+            v[4 * j + k] = dropped(a, to_float(x.e[4 * j + k]), word[k]);
+            if (RES) v[4 * j + k] += to_float(res.e[4 * j + k]);
         }
+    }
+    if (whole) {
+        store_vec<V>(o, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (at + j < a.D) o[j] = from_float<T>(v[j]);
     }
 }
 
 // Any rows: a thread per draw of four words, whose elements may lie in two rows or more
 template <class T, bool RES>
 __global__ void __launch_bounds__(256) dropout_loose_kernel(const DropArgs a) {
-    const long long workers = a.rows / a.per, items = workers * a.vecs, count = a.per * a.D;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
+    const long long items = a.items, count = a.per * a.D;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < items) {
         const long long w = i / a.vecs, e = (i - w * a.vecs) * 4;
         long long row = e / a.D, d = e - row * a.D;
         row += w * a.per;
@@ -112,11 +115,12 @@ cudaError_t launch_dropout(DropArgs a, cudaStream_t st) {
     const bool vec = rows_aligned(a.x, a.x_stride, a.rows, size, 16) && rows_aligned(a.res, a.res_stride, a.rows, size, 16) &&
                      rows_aligned(a.out, a.out_stride, a.rows, size, 16) && (a.per == 1 || a.D % 4 == 0);
     a.vecs = vec ? (a.D + V - 1) / V : (a.per * a.D + 3) / 4;
-    const long long items = vec ? a.rows * a.vecs : a.rows / a.per * a.vecs;
-    constexpr int U = 2;
-    const long long blocks = std::min<long long>((items + 255) / 256, 148 * 64);
-    const dim3 grid((unsigned)blocks);
-    if (vec) return a.res ? launch(false, dropout_kernel<T, V, U, true>, grid, 256, 0, st, a) : launch(false, dropout_kernel<T, V, U, false>, grid, 256, 0, st, a);
+    a.items = vec ? a.rows * a.vecs : a.rows / a.per * a.vecs;
+    const dim3 grid((unsigned)((a.items + 255) / 256));                       // (2^34 elements a worker, 32 workers: 2^29 blocks)
+    if (vec && a.rows == 1)
+        return a.res ? launch(false, dropout_kernel<T, V, true, true>, grid, 256, 0, st, a) : launch(false, dropout_kernel<T, V, false, true>, grid, 256, 0, st, a);
+    if (vec)
+        return a.res ? launch(false, dropout_kernel<T, V, true, false>, grid, 256, 0, st, a) : launch(false, dropout_kernel<T, V, false, false>, grid, 256, 0, st, a);
     return a.res ? launch(false, dropout_loose_kernel<T, true>, grid, 256, 0, st, a) : launch(false, dropout_loose_kernel<T, false>, grid, 256, 0, st, a);
 }
 
@@ -141,7 +145,8 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
     DropArgs a{};
     a.rows = rows; a.per = N; a.D = D; a.x = x; a.x_stride = x_stride; a.res = residual; a.res_stride = residual_stride; a.out = out;
     a.out_stride = out_stride;
-    a.seed_lo = (uint32_t)seed; a.seed_hi = (uint32_t)(seed >> 32); a.round_lo = (uint32_t)round;
+    for (uint32_t i = 0; i < 10; ++i) a.key[i] = make_uint2((uint32_t)seed + i * 0x9E3779B9u, (uint32_t)(seed >> 32) + i * 0xBB67AE85u);
+    a.round_lo = (uint32_t)round;
     a.word3 = (uint32_t)layer << 16 | (uint32_t)(round >> 32) << 8 | 2u;
     a.worker = (uint32_t)worker; a.threshold = (uint32_t)(p * 4294967296.0); a.c = (float)(1.0 / (1.0 - p));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

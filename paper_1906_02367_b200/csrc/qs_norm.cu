@@ -16,106 +16,79 @@ constexpr float E4M3_MAX = 448.0f;
 constexpr float LEAST_SCALE = 1.17549435e-38f;       // 2^-126: its reciprocal is finite
 
 struct NormArgs {
-    long long rows, N, D;                            // R N rows
+    int R; long long N, D;                           // R workers, N rows each
     const void* x; long long x_stride;
     const void* res; long long res_stride;
     const void* w; long long w_worker; int w_float;  // weights in fp32, or of the rows' type
-    float eps;
+    float eps, by_width;
     int norm;                                        // 0: rows are only put into 8 bits
     void* hidden; long long h_stride;
     void* out; long long out_stride;
     float* scale; float* rstd;
 };
 
-// Sum (or maximum) over the group that owns a row: a warp, or the block by way of `sh` (two halves used in turn, so that
-// one barrier per sum is enough)
+// Sum (or maximum) over the threads that own a row: a warp, or the block by way of `sh` (two halves used in turn, so that one
+// barrier per sum is enough)
 template <bool WARP, bool MAX>
-__device__ __forceinline__ float over_row(float v, float* sh, int& turn) {
+__device__ __forceinline__ float over_row(float v, float (*sh)[16], int& turn) {
     v = MAX ? warp_max_f(v) : warp_sum_f(v);
     if (WARP) return v;
-    float* s = sh + (turn ^= 32);
-    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) s[threadIdx.x >> 5] = v;
+    float* s = sh[turn ^= 1];
+    const int warps = blockDim.x >> 5;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = lane < warps ? s[lane] : 0.0f;               // (a maximum of magnitudes)
-    return MAX ? warp_max_f(v) : warp_sum_f(v);
+    v = s[0];
+    for (int i = 1; i < warps; ++i) v = MAX ? max_nan(v, s[i]) : v + s[i];
+    return v;
 }
 
-template <class T, int V>
-__device__ __forceinline__ void load_weight(float (&v)[V], const void* w, int w_float, long long at) {
-    if (!w) {
+// the weights' type, as a constant for the code behind it (a branch per element, or all three forms and a choice, cost more than
+// the norm's own arithmetic)
+enum { NO_WEIGHT, FLOATS, LIKE_ROWS };
+template <int W, class T, int V>
+__device__ __forceinline__ void load_weight(float (&v)[V], const void* w, long long at) {
+    if (W == NO_WEIGHT)
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = 1.0f;
-    } else if (w_float) {
-        load_floats<V>(v, static_cast<const float*>(w) + at);
+    else if (W == FLOATS) load_floats<V>(v, static_cast<const float*>(w) + at);
+    else load_vec<V>(v, static_cast<const T*>(w) + at);
+}
+#define QS_BY_WEIGHT(args, call)                                      \
+    do {                                                              \
+        if (!(args).w) call(NO_WEIGHT);                               \
+        else if ((args).w_float) call(FLOATS);                        \
+        else call(LIKE_ROWS);                                         \
+    } while (0)
+template <class T, int V> __device__ __forceinline__ Pack<T, V> load_streamed(const T* p) {      // read once: not kept in the L1
+    Pack<T, V> q;
+    if constexpr (sizeof(T) * V == 16) {
+        const uint4 u = __ldcs(reinterpret_cast<const uint4*>(p));
+        q = *reinterpret_cast<const Pack<T, V>*>(&u);
     } else {
-        load_vec<V>(v, static_cast<const T*>(w) + at);
+        q.e[0] = __ldcs(p);
     }
+    return q;
 }
 
-// U vectors of V elements per thread; WARP: a row per warp, else a row per block
-template <class T, int V, int U, bool WARP, bool QUANT>
-__global__ void __launch_bounds__(WARP ? 128 : 512) norm_kernel(const NormArgs a) {
-    __shared__ float sh[64];
-    int turn = 0;
-    const int group = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
-    const long long row = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
-    if (row >= a.rows) return;                       // (whole warps, where a row is a warp's)
-    const long long vecs = a.D / V;
-    float h[U][V], r[U][V];
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long i = t + (long long)u * group;
-        if (i < vecs) load_vec<V>(h[u], x + i * V);
-    }
-    if (a.res) {
-        const T* res = static_cast<const T*>(a.res) + row * a.res_stride;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs) load_vec<V>(r[u], res + i * V);
-        }
-        T* hid = static_cast<T*>(a.hidden) + row * a.h_stride;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) h[u][j] = to_float(from_float<T>(h[u][j] + r[u][j]));
-                store_vec<V>(hid + i * V, h[u]);
-            }
-        }
-    }
-    float f = 1.0f;
-    if (a.norm) {
-        float ss = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (t + (long long)u * group < vecs) {
-                float part = 0.0f;
-#pragma unroll
-                for (int j = 0; j < V; ++j) part = __fmaf_rn(h[u][j], h[u][j], part);
-                ss += part;
-            }
-        ss = over_row<WARP, false>(ss, sh, turn);
-        f = 1.0f / sqrtf(ss / (float)a.D + a.eps);
-        if (a.rstd && t == 0) a.rstd[row] = f;
-    }
-    const long long w0 = a.w ? row / a.N * a.w_worker : 0;
+// What follows the row's factor f: y = h f w, stored, or put into 8 bits
+template <int W, class T, int V, int U, bool WARP, bool QUANT>
+__device__ __forceinline__ void write_row(const NormArgs& a, const Pack<T, V> (&h)[U], float f, long long row, int t, int group, int vecs, float (*sh)[16], int& turn) {
+    const long long w0 = blockIdx.y * a.w_worker;
+    T* out = static_cast<T*>(a.out) + row * a.out_stride;
     float most = 0.0f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long i = t + (long long)u * group;
+        const int i = t + u * group;
         if (i < vecs) {
-            float w[V];
-            load_weight<T, V>(w, a.w, a.w_float, w0 + i * V);
+            float v[V], w[V];
+            load_weight<W, T, V>(w, a.w, w0 + i * V);
+            unpack(v, h[u]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if (a.norm) h[u][j] = h[u][j] * f * w[j];
-                if (QUANT) most = max_nan(most, fabsf(h[u][j]));
+                v[j] = v[j] * f * w[j];
+                if (QUANT) most = max_nan(most, fabsf(v[j]));
             }
-            if (!QUANT) store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + i * V, h[u]);
+            if (!QUANT) store_vec<V>(out + i * V, v);
         }
     }
     if (!QUANT) return;
@@ -124,31 +97,114 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_kernel(const NormArgs a
     const float s = most < __int_as_float(0x7f800000) ? fmaxf(most / E4M3_MAX, LEAST_SCALE) : quiet_nan();
     if (t == 0) a.scale[row] = s;
     const float inv = 1.0f / s;
-    uint8_t* out = static_cast<uint8_t*>(a.out) + row * a.out_stride;
+    uint8_t* bytes = static_cast<uint8_t*>(a.out) + row * a.out_stride;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long i = t + (long long)u * group;
+        const int i = t + u * group;
         if (i < vecs) {
+            float v[V], w[V];
+            load_weight<W, T, V>(w, a.w, w0 + i * V);
+            unpack(v, h[u]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) h[u][j] *= inv;
-            store_e4m3<V>(out + i * V, h[u]);
+            for (int j = 0; j < V; ++j) v[j] = v[j] * f * w[j] * inv;
+            store_e4m3<V>(bytes + i * V, v);
         }
     }
 }
 
-// Rows too long for the registers of a block: read again for each step (from the L2, mostly), every element by one thread
-template <class T, int V, bool QUANT>
-__global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a) {
-    __shared__ float sh[64];
+// A row per warp (four in a block) or per block, U vectors of V elements per thread, kept as they are stored until they are used
+template <class T, int V, int U, bool WARP, bool QUANT>
+__global__ void __launch_bounds__(WARP ? 128 : 512) norm_kernel(const NormArgs a) {
+    __shared__ float sh[2][16];
     int turn = 0;
-    const long long vecs = a.D / V, w_step = a.w_worker;
-    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int group = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const long long n = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    if (n >= a.N) return;                            // (whole warps, where a row is a warp's)
+    const long long row = blockIdx.y * a.N + n;
+    const int vecs = (int)(a.D / V);
+    Pack<T, V> h[U];
+    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (t + u * group < vecs) h[u] = load_streamed<T, V>(x + (t + u * group) * V);
+    if (a.res) {
+        Pack<T, V> q[U];
+        const T* res = static_cast<const T*>(a.res) + row * a.res_stride;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + u * group < vecs) q[u] = load_streamed<T, V>(res + (t + u * group) * V);
+        T* hid = static_cast<T*>(a.hidden) + row * a.h_stride;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + u * group < vecs) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) h[u].e[j] = from_float<T>(to_float(h[u].e[j]) + to_float(q[u].e[j]));
+                *reinterpret_cast<Pack<T, V>*>(hid + (t + u * group) * V) = h[u];
+            }
+    }
+    float f = 1.0f;
+    if (a.norm) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + u * group < vecs) {
+                float v[V], part = 0.0f;
+                unpack(v, h[u]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) part = __fmaf_rn(v[j], v[j], part);
+                ss += part;
+            }
+        f = rsqrtf(__fmaf_rn(over_row<WARP, false>(ss, sh, turn), a.by_width, a.eps));
+        if (a.rstd && t == 0) a.rstd[row] = f;
+    }
+#define QS_WRITE(W) write_row<W, T, V, U, WARP, QUANT>(a, h, f, row, t, group, vecs, sh, turn)
+    QS_BY_WEIGHT(a, QS_WRITE);
+#undef QS_WRITE
+}
+
+// Rows too long for the registers of a block: read again for each step (from the L2, mostly), every element by one thread
+template <int W, class T, int V, bool QUANT>
+__device__ __forceinline__ void write_long_row(const NormArgs& a, const T* h_row, float f, long long row, float (*sh)[16], int& turn) {
+    const long long vecs = a.D / V, w0 = blockIdx.y * a.w_worker;
+    float inv = 1.0f;
+    for (int pass = QUANT ? 0 : 1; pass < 2; ++pass) {
+        float most = 0.0f;
+        for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
+            float h[V], w[V];
+            load_vec<V>(h, h_row + i * V);
+            load_weight<W, T, V>(w, a.w, w0 + i * V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                h[j] = h[j] * f * w[j];
+                if (QUANT && pass == 0) most = max_nan(most, fabsf(h[j]));
+                if (QUANT) h[j] *= inv;
+            }
+            if (pass == 0) continue;
+            if (QUANT) store_e4m3<V>(static_cast<uint8_t*>(a.out) + row * a.out_stride + i * V, h);
+            else store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + i * V, h);
+        }
+        if (pass == 0) {
+            most = over_row<false, true>(most, sh, turn);
+            const float s = most < __int_as_float(0x7f800000) ? fmaxf(most / E4M3_MAX, LEAST_SCALE) : quiet_nan();
+            if (threadIdx.x == 0) a.scale[row] = s;
+            inv = 1.0f / s;
+        }
+    }
+}
+template <class T, int V, bool QUANT>
+__global__ void __launch_bounds__(512) norm_long_kernel(const NormArgs a) {
+    __shared__ float sh[2][16];
+    int turn = 0;
+    const long long vecs = a.D / V;
+    for (long long n = blockIdx.x; n < a.N; n += gridDim.x) {
+        const long long row = blockIdx.y * a.N + n;
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         const T* h_row = x;
         float ss = 0.0f;
         if (a.res) {
             const T* res = static_cast<const T*>(a.res) + row * a.res_stride;
             T* hid = static_cast<T*>(a.hidden) + row * a.h_stride;
+#pragma unroll 4
             for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
                 float h[V], r[V];
                 load_vec<V>(h, x + i * V);
@@ -162,6 +218,7 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a) {
             }
             h_row = hid;
         } else if (a.norm) {
+#pragma unroll 4
             for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
                 float h[V];
                 load_vec<V>(h, x + i * V);
@@ -171,35 +228,12 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs a) {
         }
         float f = 1.0f;
         if (a.norm) {
-            f = 1.0f / sqrtf(over_row<false, false>(ss, sh, turn) / (float)a.D + a.eps);
+            f = rsqrtf(__fmaf_rn(over_row<false, false>(ss, sh, turn), a.by_width, a.eps));
             if (a.rstd && threadIdx.x == 0) a.rstd[row] = f;
         }
-        const long long w0 = a.w ? row / a.N * w_step : 0;
-        float s = 1.0f, inv = 1.0f;
-        for (int pass = QUANT ? 0 : 1; pass < 2; ++pass) {
-            float most = 0.0f;
-            for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
-                float h[V], w[V];
-                load_vec<V>(h, h_row + i * V);
-                load_weight<T, V>(w, a.w, a.w_float, w0 + i * V);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if (a.norm) h[j] = h[j] * f * w[j];
-                    most = max_nan(most, fabsf(h[j]));
-                    if (QUANT) h[j] *= inv;
-                }
-                if (pass == 0) continue;
-                if (QUANT) store_e4m3<V>(static_cast<uint8_t*>(a.out) + row * a.out_stride + i * V, h);
-                else store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + i * V, h);
-            }
-            if (pass == 0) {
-                most = over_row<false, true>(most, sh, turn);
-                s = most < __int_as_float(0x7f800000) ? fmaxf(most / E4M3_MAX, LEAST_SCALE) : quiet_nan();
-                if (threadIdx.x == 0) a.scale[row] = s;
-                inv = 1.0f / s;
-            }
-        }
-        __syncthreads();                             // (the sums' halves are used again)
+#define QS_WRITE(W) write_long_row<W, T, V, QUANT>(a, h_row, f, row, sh, turn)
+        QS_BY_WEIGHT(a, QS_WRITE);
+#undef QS_WRITE
     }
 }
 
@@ -213,135 +247,146 @@ struct NormGradArgs {
     const void* w; long long w_worker; int w_float;
     const void* gh; long long gh_stride;
     void* out; long long out_stride;
+    float by_width;
     float* part;                                     // (R, parts, D) sums of g n over some of the rows, or null
     int parts;
     float* dw; long long dw_worker; int accumulate;
 };
 
-// Blocks stay: block (b, r) takes worker r's rows b, b + gridDim.x, .. (WARP: a warp each four-th of them) and keeps its
-// columns' sums of the weights' gradient in registers; one row of partial sums per block.
+// Blocks stay: block (b, r) takes rows of worker r in turn (WARP: a row per warp) and keeps its columns' sums of the weights'
+// gradient in registers; it leaves one row of partial sums.
+template <int W, class T, int V, int U, bool WARP>
+__device__ __forceinline__ void norm_grad_rows_of(const NormGradArgs& a, float (&dw)[U][V], float (*sh)[16], int t, int group, int vecs) {
+    int turn = 0;
+    const long long w0 = blockIdx.y * a.w_worker, first = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    for (long long n = first; n < a.N; n += WARP ? (long long)gridDim.x * 4 : gridDim.x) {
+        const long long row = blockIdx.y * a.N + n;
+        Pack<T, V> h[U], g[U], gh[U];
+        const float rstd = a.rstd[row];
+        const T* hp = static_cast<const T*>(a.h) + row * a.h_stride;
+        const T* gp = static_cast<const T*>(a.g) + row * a.g_stride;
+        const T* ghp = static_cast<const T*>(a.gh) + row * a.gh_stride;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + u * group < vecs) {
+                h[u] = load_streamed<T, V>(hp + (t + u * group) * V);
+                g[u] = load_streamed<T, V>(gp + (t + u * group) * V);
+            }
+        if (a.gh)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (t + u * group < vecs) gh[u] = load_streamed<T, V>(ghp + (t + u * group) * V);
+        float dot = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = t + u * group;
+            if (i < vecs) {
+                float w[V], hv[V], gv[V];
+                load_weight<W, T, V>(w, a.w, w0 + i * V);
+                unpack(hv, h[u]);
+                unpack(gv, g[u]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float gn = gv[j] * (hv[j] * rstd);
+                    dw[u][j] += gn;
+                    dot = __fmaf_rn(gn, w[j], dot);
+                }
+            }
+        }
+        const float along = over_row<WARP, false>(dot, sh, turn) * a.by_width * rstd * rstd;
+        T* op = static_cast<T*>(a.out) + row * a.out_stride;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = t + u * group;
+            if (i < vecs) {
+                float w[V], hv[V], gv[V];
+                load_weight<W, T, V>(w, a.w, w0 + i * V);
+                unpack(hv, h[u]);
+                unpack(gv, g[u]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) gv[j] = __fmaf_rn(-along, hv[j], gv[j] * w[j] * rstd);
+                if (a.gh) {
+                    unpack(hv, gh[u]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) gv[j] += hv[j];
+                }
+                store_vec<V>(op + i * V, gv);
+            }
+        }
+    }
+}
 template <class T, int V, int U, bool WARP>
 __global__ void __launch_bounds__(WARP ? 128 : 512) norm_grad_kernel(const NormGradArgs a) {
-    __shared__ float sh[64];
-    extern __shared__ float warps_dw[];              // WARP: (4, D) of the block's warps
-    int turn = 0;
-    const int group = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x, r = blockIdx.y;
-    const long long vecs = a.D / V;
-    const long long first = WARP ? (long long)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x, step = WARP ? (long long)gridDim.x * 4 : gridDim.x;
+    __shared__ float sh[2][16];
+    extern __shared__ float joined[];                // WARP: (4, D) of the block's warps
+    const int group = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const int vecs = (int)(a.D / V);
     float dw[U][V];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int j = 0; j < V; ++j) dw[u][j] = 0.0f;
-    const float by_width = 1.0f / (float)a.D;
-    for (long long n = first; n < a.N; n += step) {
-        const long long row = r * a.N + n;
-        float h[U][V], g[U][V];
-        const float rstd = a.rstd[row];
-        const T* hp = static_cast<const T*>(a.h) + row * a.h_stride;
-        const T* gp = static_cast<const T*>(a.g) + row * a.g_stride;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs) {
-                load_vec<V>(h[u], hp + i * V);
-                load_vec<V>(g[u], gp + i * V);
-            }
-        }
-        float dot = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs) {
-                float w[V];
-                load_weight<T, V>(w, a.w, a.w_float, r * a.w_worker + i * V);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    h[u][j] *= rstd;
-                    dw[u][j] = __fmaf_rn(g[u][j], h[u][j], dw[u][j]);
-                    g[u][j] *= w[j];
-                    dot = __fmaf_rn(g[u][j], h[u][j], dot);
-                }
-            }
-        }
-        const float mean = over_row<WARP, false>(dot, sh, turn) * by_width;
-        T* op = static_cast<T*>(a.out) + row * a.out_stride;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs) {
-                float gh[V];
-                if (a.gh) load_vec<V>(gh, static_cast<const T*>(a.gh) + row * a.gh_stride + i * V);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = rstd * (g[u][j] - h[u][j] * mean);
-                    g[u][j] = a.gh ? d + gh[j] : d;
-                }
-                store_vec<V>(op + i * V, g[u]);
-            }
-        }
-    }
+#define QS_ROWS(W) norm_grad_rows_of<W, T, V, U, WARP>(a, dw, sh, t, group, vecs)
+    QS_BY_WEIGHT(a, QS_ROWS);
+#undef QS_ROWS
     if (!a.part) return;
-    float* part = a.part + ((long long)r * a.parts + blockIdx.x) * a.D;
-    if (WARP) {
-        float* mine = warps_dw + (threadIdx.x >> 5) * a.D;
+    float* part = a.part + ((long long)blockIdx.y * a.parts + blockIdx.x) * a.D;
+    float* to = WARP ? joined + (threadIdx.x >> 5) * a.D : part;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * 32;
-            if (i < vecs)
+    for (int u = 0; u < U; ++u) {
+        const int i = t + u * group;
+        if (i < vecs)
 #pragma unroll
-                for (int j = 0; j < V; ++j) mine[i * V + j] = dw[u][j];
-        }
-        __syncthreads();
-        for (long long i = threadIdx.x; i < a.D; i += 128)
-            part[i] = (warps_dw[i] + warps_dw[a.D + i]) + (warps_dw[2 * a.D + i] + warps_dw[3 * a.D + i]);
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const long long i = t + (long long)u * group;
-            if (i < vecs)
-#pragma unroll
-                for (int j = 0; j < V; ++j) part[i * V + j] = dw[u][j];
-        }
+            for (int j = 0; j < V; ++j) to[i * V + j] = dw[u][j];
     }
+    if (!WARP) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < (int)a.D; i += 128) part[i] = (joined[i] + joined[a.D + i]) + (joined[2 * a.D + i] + joined[3 * a.D + i]);
 }
 
 // Long rows, read twice
-template <class T, int V>
-__global__ void __launch_bounds__(1024) norm_grad_long_kernel(const NormGradArgs a) {
-    __shared__ float sh[64];
+template <int W, class T, int V>
+__device__ __forceinline__ void norm_grad_long_rows(const NormGradArgs& a, float (*sh)[16]) {
     int turn = 0;
-    const long long vecs = a.D / V;
-    const float by_width = 1.0f / (float)a.D;
-    for (long long row = blockIdx.x; row < a.R * a.N; row += gridDim.x) {
-        const long long w0 = row / a.N * a.w_worker;
+    const long long vecs = a.D / V, w0 = blockIdx.y * a.w_worker;
+    for (long long n = blockIdx.x; n < a.N; n += gridDim.x) {
+        const long long row = blockIdx.y * a.N + n;
         const T* hp = static_cast<const T*>(a.h) + row * a.h_stride;
         const T* gp = static_cast<const T*>(a.g) + row * a.g_stride;
         const float rstd = a.rstd[row];
         float dot = 0.0f;
+#pragma unroll 4
         for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
             float h[V], g[V], w[V];
             load_vec<V>(h, hp + i * V);
             load_vec<V>(g, gp + i * V);
-            load_weight<T, V>(w, a.w, a.w_float, w0 + i * V);
+            load_weight<W, T, V>(w, a.w, w0 + i * V);
 #pragma unroll
             for (int j = 0; j < V; ++j) dot = __fmaf_rn(g[j] * w[j], h[j] * rstd, dot);
         }
-        const float mean = over_row<false, false>(dot, sh, turn) * by_width;
+        const float along = over_row<false, false>(dot, sh, turn) * a.by_width * rstd * rstd;
         for (long long i = threadIdx.x; i < vecs; i += blockDim.x) {
-            float h[V], g[V], w[V], gh[V];
+            float h[V], g[V], w[V];
             load_vec<V>(h, hp + i * V);
             load_vec<V>(g, gp + i * V);
-            load_weight<T, V>(w, a.w, a.w_float, w0 + i * V);
-            if (a.gh) load_vec<V>(gh, static_cast<const T*>(a.gh) + row * a.gh_stride + i * V);
+            load_weight<W, T, V>(w, a.w, w0 + i * V);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = rstd * (g[j] * w[j] - h[j] * rstd * mean);
-                g[j] = a.gh ? d + gh[j] : d;
+            for (int j = 0; j < V; ++j) g[j] = __fmaf_rn(-along, h[j], g[j] * w[j] * rstd);
+            if (a.gh) {
+                load_vec<V>(h, static_cast<const T*>(a.gh) + row * a.gh_stride + i * V);
+#pragma unroll
+                for (int j = 0; j < V; ++j) g[j] += h[j];
             }
             store_vec<V>(static_cast<T*>(a.out) + row * a.out_stride + i * V, g);
         }
     }
+}
+template <class T, int V>
+__global__ void __launch_bounds__(512) norm_grad_long_kernel(const NormGradArgs a) {
+    __shared__ float sh[2][16];
+#define QS_ROWS(W) norm_grad_long_rows<W, T, V>(a, sh)
+    QS_BY_WEIGHT(a, QS_ROWS);
+#undef QS_ROWS
 }
 // and the weights' gradient of such rows: a thread per column, block (x, p, r) the rows p, p + parts, ..
 template <class T>
@@ -359,35 +404,40 @@ __global__ void __launch_bounds__(256) norm_dw_kernel(const NormGradArgs a) {
 }
 
 // ------------------------------------------------------------------ launches
-// A row in registers: `group` threads with `per` vectors each; 0 vectors: too long.  Two vectors a thread keep enough loads
-// in flight with blocks small enough that several share an SM.
+// A row in the registers of `group` threads with up to `per` vectors each; 0: too long.  (32: a warp's, else a block's)
 struct RowShape { int group, per; };
-RowShape row_shape(long long vecs, int most_per) {
-    if (vecs <= 32) return {32, 1};
-    if (vecs <= 64) return {32, 2};
+RowShape row_shape(long long vecs, int least, int most) {
+    if (vecs <= 32 * least) return {32, vecs <= 32 * (least / 2) ? (vecs <= 32 * (least / 4) && least == 4 ? 1 : least / 2) : least};
     int g = 64;
-    while (g < 512 && 2 * g < vecs) g *= 2;
-    int per = 1;
-    while (per < most_per && (long long)per * g < vecs) per *= 2;
+    while (g < 512 && (long long)least * g < vecs) g *= 2;
+    int per = least;
+    while (per < most && (long long)per * g < vecs) per *= 2;
     return {g, (long long)per * g < vecs ? 0 : per};
 }
+// Loads in flight against registers: four vectors a thread for the norm, two for its gradient, which keeps sums as well (8192 x
+// 4096 in bf16, us with 1, 2, 4 vectors: norm 40, 30, 26; with the residual 57, 49, 47; gradient 69, 66, 86).  Element by element
+// what a row costs per thread counts most: eight.
+template <int V> RowShape norm_shape(long long vecs) { return V == 1 ? row_shape(vecs, 8, 16) : row_shape(vecs, 4, 4); }
+template <int V> RowShape grad_shape(long long vecs) { return V == 1 ? row_shape(vecs, 8, 16) : row_shape(vecs, 2, 4); }
 
+template <class T, int V, bool QUANT, int U>
+cudaError_t norm_by(const NormArgs& a, int group, cudaStream_t st) {
+    if (group == 32) return launch(false, norm_kernel<T, V, U, true, QUANT>, dim3((unsigned)((a.N + 3) / 4), (unsigned)a.R), 128, 0, st, a);
+    return launch(false, norm_kernel<T, V, U, false, QUANT>, dim3((unsigned)a.N, (unsigned)a.R), group, 0, st, a);
+}
 template <class T, int V, bool QUANT>
 cudaError_t norm_of(const NormArgs& a, cudaStream_t st) {
-    const RowShape s = row_shape(a.D / V, V == 1 ? 8 : 4);
-    if (s.per && s.group == 32) {
-        const dim3 grid((unsigned)((a.rows + 3) / 4));
-        return s.per == 1 ? launch(false, norm_kernel<T, V, 1, true, QUANT>, grid, 128, 0, st, a)
-                          : launch(false, norm_kernel<T, V, 2, true, QUANT>, grid, 128, 0, st, a);
+    const RowShape s = norm_shape<V>(a.D / V);
+    if constexpr (V == 1) {
+        if (s.per == 4) return norm_by<T, V, QUANT, 4>(a, s.group, st);
+        if (s.per == 8) return norm_by<T, V, QUANT, 8>(a, s.group, st);
+        if (s.per == 16) return norm_by<T, V, QUANT, 16>(a, s.group, st);
+    } else {
+        if (s.per == 1) return norm_by<T, V, QUANT, 1>(a, s.group, st);
+        if (s.per == 2) return norm_by<T, V, QUANT, 2>(a, s.group, st);
+        if (s.per == 4) return norm_by<T, V, QUANT, 4>(a, s.group, st);
     }
-    const dim3 grid((unsigned)a.rows);
-    switch (s.per) {
-    case 1: return launch(false, norm_kernel<T, V, 1, false, QUANT>, grid, s.group, 0, st, a);
-    case 2: return launch(false, norm_kernel<T, V, 2, false, QUANT>, grid, s.group, 0, st, a);
-    case 4: return launch(false, norm_kernel<T, V, 4, false, QUANT>, grid, s.group, 0, st, a);
-    case 8: return launch(false, norm_kernel<T, 1, 8, false, QUANT>, grid, s.group, 0, st, a);
-    }
-    return launch(false, norm_long_kernel<T, V, QUANT>, dim3((unsigned)std::min<long long>(a.rows, 1 << 20)), 1024, 0, st, a);
+    return launch(false, norm_long_kernel<T, V, QUANT>, dim3((unsigned)std::min<long long>(a.N, 1 << 20), (unsigned)a.R), 512, 0, st, a);
 }
 template <class T>
 cudaError_t launch_norm(const NormArgs& a, bool vec, bool quant, cudaStream_t st) {
@@ -396,35 +446,42 @@ cudaError_t launch_norm(const NormArgs& a, bool vec, bool quant, cudaStream_t st
     return vec ? norm_of<T, V, false>(a, st) : norm_of<T, 1, false>(a, st);
 }
 
-// Partial sums per worker: enough blocks to fill the GPU, no more than there are rows (or groups of four)
+// Partial sums per worker: no more than there are rows, blocks that fit the GPU together, or 128 MB of them
+constexpr int GRAD_BLOCKS = 148 * 16;
 int grad_parts(int R, int64_t N, int64_t D) {
-    const long long want = (148 * 8 + R - 1) / R;
-    return (int)std::max<long long>(1, std::min<long long>(N, std::min<long long>(want, std::max<long long>(1, (32ll << 20) / (R * D)))));
+    return (int)std::max<long long>(1, std::min<long long>({N, (GRAD_BLOCKS + R - 1) / R, std::max<long long>(1, (32ll << 20) / (R * D))}));
+}
+
+template <class T, int V, int U, bool WARP>
+cudaError_t norm_grad_by(NormGradArgs& a, int group, int sms, cudaStream_t st) {
+    const int threads = WARP ? 128 : group;
+    const unsigned smem = WARP ? (unsigned)(16 * a.D) : 0;
+    int per_sm = 0;
+    cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, norm_grad_kernel<T, V, U, WARP>, threads, smem);
+    if (e != cudaSuccess) return e;
+    // blocks that are there together
+    const long long rows = WARP ? (a.N + 3) / 4 : a.N, there = ((long long)sms * std::max(1, per_sm) + a.R - 1) / a.R;
+    a.parts = (int)std::max<long long>(1, std::min<long long>({rows, (long long)a.parts, there}));
+    return launch(false, norm_grad_kernel<T, V, U, WARP>, dim3((unsigned)a.parts, (unsigned)a.R), threads, smem, st, a);
+}
+template <class T, int V, int U>
+cudaError_t norm_grad_rows(NormGradArgs& a, int group, int sms, cudaStream_t st) {
+    return group == 32 ? norm_grad_by<T, V, U, true>(a, group, sms, st) : norm_grad_by<T, V, U, false>(a, group, sms, st);
 }
 
 template <class T, int V>
 cudaError_t norm_grad_of(NormGradArgs a, int sms, cudaStream_t st) {
-    const RowShape s = row_shape(a.D / V, V == 1 ? 8 : 4);
-    const int most = a.parts;
-    cudaError_t e;
+    const RowShape s = grad_shape<V>(a.D / V);
+    cudaError_t e = cudaSuccess;
     if (s.per) {
-        // blocks that fit the GPU together: more would only make more partial sums
-        const bool warp = s.group == 32;
-        const int threads = warp ? 128 : s.group, per_sm = std::max(1, 1024 / threads);
-        const long long rows = warp ? (a.N + 3) / 4 : a.N;
-        a.parts = (int)std::max<long long>(1, std::min<long long>({rows, (long long)most, (long long)(sms * per_sm + a.R - 1) / a.R}));
-        const dim3 grid((unsigned)a.parts, (unsigned)a.R);
-        const unsigned smem = warp ? (unsigned)(16 * a.D) : 0;
-        if (warp) e = s.per == 1 ? launch(false, norm_grad_kernel<T, V, 1, true>, grid, 128, smem, st, a) : launch(false, norm_grad_kernel<T, V, 2, true>, grid, 128, smem, st, a);
-        else if (s.per == 1) e = launch(false, norm_grad_kernel<T, V, 1, false>, grid, s.group, 0, st, a);
-        else if (s.per == 2) e = launch(false, norm_grad_kernel<T, V, 2, false>, grid, s.group, 0, st, a);
-        else if (s.per == 4) e = launch(false, norm_grad_kernel<T, V, 4, false>, grid, s.group, 0, st, a);
-        else e = launch(false, norm_grad_kernel<T, 1, 8, false>, grid, s.group, 0, st, a);
+        if constexpr (V == 1)
+            e = s.per == 4 ? norm_grad_rows<T, V, 4>(a, s.group, sms, st) : s.per == 8 ? norm_grad_rows<T, V, 8>(a, s.group, sms, st) : norm_grad_rows<T, V, 16>(a, s.group, sms, st);
+        else
+            e = s.per == 1 ? norm_grad_rows<T, V, 1>(a, s.group, sms, st) : s.per == 2 ? norm_grad_rows<T, V, 2>(a, s.group, sms, st) : norm_grad_rows<T, V, 4>(a, s.group, sms, st);
     } else {
         // the weights' sums first: the rows' gradient may take g's place
-        e = cudaSuccess;
         if (a.part) e = launch(false, norm_dw_kernel<T>, dim3((unsigned)((a.D + 255) / 256), (unsigned)a.parts, (unsigned)a.R), 256, 0, st, a);
-        if (e == cudaSuccess) e = launch(false, norm_grad_long_kernel<T, V>, dim3((unsigned)std::min<long long>(a.R * a.N, 1 << 20)), 1024, 0, st, a);
+        if (e == cudaSuccess) e = launch(false, norm_grad_long_kernel<T, V>, dim3((unsigned)std::min<long long>(a.N, 1 << 20), (unsigned)a.R), 512, 0, st, a);
     }
     if (e != cudaSuccess || !a.part) return e;
     return launch_join(true, a.part, a.parts, a.R, a.D, a.dw, a.dw_worker, a.accumulate, st);
@@ -478,7 +535,7 @@ int qs_rms_norm(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_
         return QS_INVALID_ARG;
     }
     NormArgs a{};
-    a.rows = rows; a.N = N; a.D = D;
+    a.R = R; a.N = N; a.D = D; a.by_width = 1.0f / (float)D;
     a.x = x; a.x_stride = x_stride; a.res = residual; a.res_stride = residual_stride;
     a.w = weight; a.w_worker = weight_worker_stride; a.w_float = weight_type == QS_F32;
     a.eps = eps; a.norm = 1; a.hidden = hidden; a.h_stride = hidden_stride; a.out = out; a.out_stride = out_stride; a.scale = scale; a.rstd = rstd;
@@ -498,7 +555,7 @@ int qs_quantize_rows(int64_t N, int64_t D, const void* x, int type, int64_t x_st
     if (!x || !out || !scale || bad_rows(x, x_stride, D, size) || out_stride < D || !aligned_to(scale, 4) ||
         !apart(out, span(N, out_stride, D, 1), x, span(N, x_stride, D, size))) return QS_INVALID_ARG;
     NormArgs a{};
-    a.rows = N; a.N = N; a.D = D; a.x = x; a.x_stride = x_stride; a.out = out; a.out_stride = out_stride; a.scale = scale;
+    a.R = 1; a.N = N; a.D = D; a.x = x; a.x_stride = x_stride; a.out = out; a.out_stride = out_stride; a.scale = scale;
     const int V = 16 / size;
     const bool vec = D % V == 0 && rows_aligned(x, x_stride, N, size, 16) && rows_aligned(out, out_stride, N, 1, V);
     return QS_NORM_BY_TYPE(launch_norm, type, a, vec, true, static_cast<cudaStream_t>(cuda_stream));
@@ -533,7 +590,7 @@ int qs_rms_norm_grad(int R, int64_t N, int64_t D, const void* grad, int type, in
     const int sms = sm_count();
     if (!sms) return QS_CUDA;
     NormGradArgs a{};
-    a.R = R; a.N = N; a.D = D; a.g = grad; a.g_stride = grad_stride; a.h = hidden; a.h_stride = hidden_stride; a.rstd = rstd;
+    a.R = R; a.N = N; a.D = D; a.by_width = 1.0f / (float)D; a.g = grad; a.g_stride = grad_stride; a.h = hidden; a.h_stride = hidden_stride; a.rstd = rstd;
     a.w = weight; a.w_worker = weight_worker_stride; a.w_float = weight_type == QS_F32; a.gh = grad_hidden; a.gh_stride = grad_hidden_stride;
     a.out = out; a.out_stride = out_stride; a.part = grad_weight ? static_cast<float*>(work) : nullptr; a.parts = grad_parts(R, N, D);
     a.dw = grad_weight; a.dw_worker = grad_weight_worker_stride; a.accumulate = accumulate;

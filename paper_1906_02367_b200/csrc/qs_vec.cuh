@@ -32,6 +32,10 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[V]) {
         *reinterpret_cast<Pack<T, W>*>(p + i) = q;
     }
 }
+template <class T, int V> __device__ __forceinline__ void unpack(float (&v)[V], const Pack<T, V>& q) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = to_float(q.e[j]);
+}
 template <int V> __device__ __forceinline__ void load_floats(float (&v)[V], const float* p) { load_vec<V>(v, p); }
 // e4m3, rounded to nearest, magnitudes above 448 to 448, NaN kept
 template <int V>
