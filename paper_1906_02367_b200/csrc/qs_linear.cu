@@ -223,7 +223,7 @@ __device__ __forceinline__ void finish_columns(const Finish& f, int r, long long
 struct LayArgs {
     const void* src; int src_type; long long src_stride, src_worker;
     void* dst; int dst_type, planes; long long ld;   // (workers, planes, rows, ld)
-    long long rows, cols; int vec;
+    long long rows, cols; int workers, vec;
 };
 __device__ __forceinline__ bf16 part_of(float& v) {
     bf16 p = __float2bfloat16_rn(v);
@@ -232,7 +232,14 @@ __device__ __forceinline__ bf16 part_of(float& v) {
     v = isinf(f) ? 0.0f : v - f;                     // (exact; a NaN stays one)
     return p;
 }
-__global__ void __launch_bounds__(256) lay_kernel(const LayArgs a) {
+// parts of the operands whose products are added, the small ones first: what is left out is 2^-24 of the whole
+__device__ __forceinline__ int part_a(int pairs, int p) { return pairs == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
+__device__ __forceinline__ int part_b(int pairs, int p) { return pairs == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
+
+struct LayBoth { LayArgs side[2]; };
+__global__ void __launch_bounds__(256) lay_kernel(const LayBoth both) {
+    const LayArgs& a = both.side[blockIdx.z];
+    if (blockIdx.y >= a.workers) return;
     const int size = a.dst_type == QS_E4M3 ? 1 : 2;
     const long long units = a.ld / 8, r = blockIdx.y, items = a.rows * units;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
@@ -294,10 +301,6 @@ struct GemmArgs {
     Finish f;
 };
 
-// parts of the operands whose products are added, the small ones first: what is left out is 2^-24 of the whole
-__device__ __forceinline__ int part_a(int pairs, int p) { return pairs == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
-__device__ __forceinline__ int part_b(int pairs, int p) { return pairs == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
-
 struct Unit { int r, split, tm, tn, kb0, kb1; };      // blocks [kb0, kb1) along k of one tile
 __device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
     Unit t;
@@ -333,6 +336,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GemmArgs g) {
     extern __shared__ __align__(1024) uint8_t ring[];
     constexpr int A_BYTES = TILE_M * 128, B_ROWS = BN / CG, STAGE = stage_bytes<CG, BN>();
+    // Tiles of 64 columns: the two halves of the finishing warps take accumulators in turn (each unit is one sum then), else half of
+    // the columns of each
+    constexpr bool TURNS = BN == 64;
     Small& small = *reinterpret_cast<Small*>(ring + STAGES * STAGE + PASS_BYTES);
     uint64_t *full = small.full, *empty = small.empty, *acc_full = small.acc_full, *acc_empty = small.acc_empty;
     // (tiles are swizzled by their addresses: off the 1024-byte boundary nothing is begun, as with a wait that runs out at once)
@@ -343,7 +349,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
-        for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], 8 * CG);
+        for (int i = 0; i < 2; ++i) mbar_init(&acc_full[i], 1), mbar_init(&acc_empty[i], (TURNS ? 4 : 8) * CG);
         mbar_init(&small.drained, 1);
         fence_barrier_init();
     }
@@ -452,18 +458,22 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             mbar_wait_asleep(&small.drained, 0, WAIT_LIMIT_NS);
         }
     } else if (warp >= 4) {
-        constexpr int HALF = BN / 2, WIDE = 128 / sizeof(T);                 // columns of a warp; of a tile on its way out
+        constexpr int HALF = TURNS ? BN : BN / 2, WIDE = 128 / sizeof(T);    // columns of a warp; of a tile on its way out
         const int q = warp & 3, half = (warp - 4) >> 2;
         uint8_t* pass = ring + STAGES * STAGE + (warp - 4) * 8192;
         float *bias = small.bias + half * HALF, *scale = small.scale + half * HALF;
         const uint32_t leader[2] = {CG == 2 ? in_block(smem_addr(&acc_empty[0]), 0) : smem_addr(&acc_empty[0]),
                                     CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
-        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + half * HALF;
+        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (TURNS ? 0 : half * HALF);
         int n = 0, out_buf = 0;
         bool fine = limit != 0;
         for (int u = cluster; u < g.units; u += clusters) {
             const Unit t = unit_of(g, u);
-            const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + half * HALF;
+            const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + (TURNS ? 0 : half * HALF);
+            if (TURNS && (n & 1) != half) {
+                ++n;
+                continue;
+            }
             const long long m = m0 + lane, row = t.r * g.M + m;
             const bool in = m < g.M;
             if (g.columns) {                         // (uniform) what belongs to the columns, for the four warps of this half
@@ -587,59 +597,252 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, lon
 }
 
 // ------------------------------------------------------------------ small products, in fp32 on the ordinary units
-struct Side { const void* p; int type, as; long long row, k, worker; };   // element (row, k) of a worker; rounded to `as`
-__device__ __forceinline__ float side_at(const Side& s, long long i) {
-    if (s.type == QS_E4M3) {
-        const __half_raw h = __nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(s.p)[i], __NV_E4M3);
-        return __half2float(__half(h));
-    }
-    const float v = element(s.p, s.type, i);
-    if (s.type != QS_F32 || s.as == QS_F32) return v;
-    return s.as == QS_BF16 ? to_float(__float2bfloat16_rn(v)) : to_float(__float2half_rn(v));
+struct Side { const void* p; long long row, k, worker; };                // element (row, k) of a worker
+__device__ __forceinline__ float e4m3_at(const void* p, long long i) {
+    const __half_raw h = __nv_cvt_fp8_to_halfraw(static_cast<const uint8_t*>(p)[i], __NV_E4M3);
+    return __half2float(__half(h));
 }
-// 64 x 64 results per block of 256 threads, 16 of the contraction at a time
-__global__ void __launch_bounds__(256) small_kernel(const Side a, const Side b, long long K, const Finish f) {
-    __shared__ float sa[16][68], sb[16][68];
-    const int r = blockIdx.z, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const long long n0 = (long long)blockIdx.x * 64;
-    for (long long m0 = (long long)blockIdx.y * 64; m0 < f.M; m0 += (long long)gridDim.y * 64) {
-    float acc[4][4] = {};
-    for (long long k0 = 0; k0 < K; k0 += 16) {
-        for (int side = 0; side < 2; ++side) {
-            const Side& s = side ? b : a;
-            float (*to)[68] = side ? sb : sa;
-            const long long first = side ? n0 : m0, most = side ? f.N : f.M;
+// TYPE: as stored; AS: what it is multiplied as (fp32 weights of 16-bit rows are rounded)
+template <int TYPE, int AS>
+__device__ __forceinline__ float side_at(const Side& s, long long i) {
+    if (TYPE == QS_E4M3) return e4m3_at(s.p, i);
+    const float v = element(s.p, TYPE, i);
+    return TYPE == QS_F32 && AS == QS_BF16 ? to_float(__float2bfloat16_rn(v)) : TYPE == QS_F32 && AS == QS_F16 ? to_float(__float2half_rn(v)) : v;
+}
+// 32 x 32 results per block.  Four groups of 64 threads each take a quarter of the contraction, 16 at a time, the next 16 on
+// their way to registers while these are multiplied; their sums are joined in order.
+template <int TA, int TB>
+__global__ void __launch_bounds__(256, 3) small_kernel(const Side a, const Side b, int K, const Finish f) {
+    __shared__ float4 tiles[4][2][16][9];            // (group, operand, k, rows by four; one place of padding)
+    const int r = blockIdx.z, group = threadIdx.x >> 6, t = threadIdx.x & 63, tx = t & 7, ty = t >> 3;
+    const int per = ((K + 3) / 4 + 15) / 16 * 16, k0 = min(K, group * per), k1 = min(K, k0 + per);
+    const long long n0 = (long long)blockIdx.x * 32;
+    for (long long m0 = (long long)blockIdx.y * 32; m0 < f.M; m0 += (long long)gridDim.y * 32) {
+        float acc[4][4] = {}, next[2][8];
+        const auto fetch = [&](int k) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = threadIdx.x + 256 * i;
-                const int row = s.k == 1 ? e >> 4 : e & 63, k = s.k == 1 ? e & 15 : e >> 6;
-                to[k][row] = first + row < most && k0 + k < K ? side_at(s, r * s.worker + (first + row) * s.row + (k0 + k) * s.k) : 0.0f;
+            for (int o = 0; o < 2; ++o) {
+                const Side& s = o ? b : a;
+                const long long first = o ? n0 : m0, most = o ? f.N : f.M;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int e = t + 64 * i, row = s.k == 1 ? e >> 4 : e & 31, kk = s.k == 1 ? e & 15 : e >> 5;
+                    next[o][i] = first + row < most && k + kk < k1 ? (o ? side_at<TB, TA>(s, r * s.worker + (first + row) * s.row + (k + kk) * s.k) : side_at<TA, TA>(s, r * s.worker + (first + row) * s.row + (k + kk) * s.k)) : 0.0f;
+                }
+            }
+        };
+        if (k0 < k1) fetch(k0);
+        for (int k = k0; k < k0 + per; k += 16) {    // (all groups take as many steps: the barriers are the block's)
+            __syncthreads();
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const Side& s = o ? b : a;
+                float* to = reinterpret_cast<float*>(tiles[group][o]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int e = t + 64 * i, row = s.k == 1 ? e >> 4 : e & 31, kk = s.k == 1 ? e & 15 : e >> 5;
+                    to[kk * 36 + row] = k < k1 ? next[o][i] : 0.0f;
+                }
+            }
+            __syncthreads();
+            if (k + 16 < k1) fetch(k + 16);
+#pragma unroll
+            for (int kk = 0; kk < 16; ++kk) {
+                const float4 x = tiles[group][0][kk][ty], y = tiles[group][1][kk][tx];
+                const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(xs[i], ys[j], acc[i][j]);
             }
         }
         __syncthreads();
+        float* sums = reinterpret_cast<float*>(tiles);                       // (group, m, n) of 32 x 33
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const float4 x = *reinterpret_cast<float4*>(&sa[k][ty * 4]), y = *reinterpret_cast<float4*>(&sb[k][tx * 4]);
-            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(xs[i], ys[j], acc[i][j]);
+            for (int j = 0; j < 4; ++j) sums[(group * 32 + ty * 4 + i) * 33 + tx * 4 + j] = acc[i][j];
+        __syncthreads();
+        const int col = threadIdx.x & 31;
+        if (n0 + col < f.N) {
+            Columns<1> c;
+            load_columns(f, r, n0 + col, c);
+            for (int i = threadIdx.x >> 5; i < 32 && m0 + i < f.M; i += 8) {
+                const float* q = sums + i * 33 + col;
+                float v[1] = {(q[0] + q[32 * 33]) + (q[2 * 32 * 33] + q[3 * 32 * 33])};
+                finish_any(f, r, m0 + i, n0 + col, v, c, f.accumulate ? ADD : 0);
+            }
         }
         __syncthreads();
     }
+}
+
+// ------------------------------------------------------------------ few rows: the weights go by once
+// Decoding: up to 32 rows of x, so the weights' bytes are all there is.  A block takes 16 or 32 rows of the weights (the matrix
+// instruction's 16 rows), its eight warps stretches of 64 along k in turn; their sums are joined in order.  The order along k
+// within a stretch is free, so a lane's four places in two products are eight neighbours in memory: one load of 16 bytes per row
+// and two products.  fp32 weights are rounded, or cut in three, on the way: nothing is laid out first.  (us, one row of x, 8192 x 8192
+// weights: bf16 28, 4.8 TB/s; e4m3 12.4.  Streaming hints on the loads: 31 to 35, and 18: the halves of a line are read by two
+// loads.  8 x 2048 x 8192, weights in the L2: 6.3; 16 rows 8.5; the same from fp32 weights 9.1)
+constexpr int FEW = 32;                              // rows of x
+struct FewArgs {
+    const void* x; long long x_stride, x_worker;
+    const void* w; long long w_stride, w_worker;
+    int K;
+    Finish f;
+};
+struct Eight { uint32_t v[4]; };                     // eight elements of 16 bits
+template <bool HALF>
+__device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
+    if (HALF) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Elements [k, k + 8) of a row (BITS 8: sixteen, [2 k, 2 k + 16)); those at K and beyond are zero.  BITS: of an element; VEC: rows on 16-byte
+// boundaries
+template <bool VEC>
+__device__ __forceinline__ void floats_at(float (&v)[8], const float* p, int k, int K) {
+    if (VEC && k + 8 <= K) return load_floats<8>(v, p + k);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const long long n = n0 + tx * 4 + j;
-        if (n >= f.N) continue;
-        Columns<1> c;
-        load_columns(f, r, n, c);
+    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? p[k + i] : 0.0f;
+}
+template <int BITS, bool HALF, bool VEC>
+__device__ __forceinline__ Eight eight_at(const void* p, long long row, int k, int K) {
+    Eight e = {};
+    if (BITS == 8) k *= 2;
+    if (k >= K) return e;
+    if (VEC && k + (BITS == 8 ? 16 : 8) <= K) {
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p) + (row + k) * (BITS / 8));
+        const uint4 a = *q;
+        if (BITS == 32) {
+            const uint4 b = q[1];
+            e.v[0] = pair_of<HALF>(__uint_as_float(a.x), __uint_as_float(a.y)), e.v[1] = pair_of<HALF>(__uint_as_float(a.z), __uint_as_float(a.w));
+            e.v[2] = pair_of<HALF>(__uint_as_float(b.x), __uint_as_float(b.y)), e.v[3] = pair_of<HALF>(__uint_as_float(b.z), __uint_as_float(b.w));
+        } else {
+            e.v[0] = a.x, e.v[1] = a.y, e.v[2] = a.z, e.v[3] = a.w;
+        }
+        return e;
+    }
+    if (BITS == 32) {
+        float v[8];
+        floats_at<false>(v, static_cast<const float*>(p) + row, k, K);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.v[i] = pair_of<HALF>(v[2 * i], v[2 * i + 1]);
+    } else if (BITS == 16) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (k + i < K) e.v[i / 2] |= (uint32_t)static_cast<const uint16_t*>(p)[row + k + i] << (i % 2 * 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (k + i < K) e.v[i / 4] |= (uint32_t)static_cast<const uint8_t*>(p)[row + k + i] << (i % 4 * 8);
+    }
+    return e;
+}
+template <int BITS, bool HALF>
+__device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+#define QS_MMA(shape)                                                                                                              \
+    asm volatile("mma.sync.aligned." shape " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"                        \
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1))
+    if (BITS == 8) QS_MMA("m16n8k32.row.col.f32.e4m3.e4m3.f32");
+    else if (HALF) QS_MMA("m16n8k16.row.col.f32.f16.f16.f32");
+    else QS_MMA("m16n8k16.row.col.f32.bf16.bf16.f32");
+#undef QS_MMA
+}
+// fp32 in its three parts
+template <bool VEC>
+__device__ __forceinline__ void parts_at(Eight (&e)[3], const void* p, long long row, bool ok, int k, int K) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    if (ok && k < K) floats_at<VEC>(v, static_cast<const float*>(p) + row, k, K);
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float v[1] = {acc[i][j]};
-            if (m0 + ty * 4 + i < f.M) finish_any(f, r, m0 + ty * 4 + i, n, v, c, f.accumulate ? ADD : 0);
+            const bf16 lo = part_of(v[2 * i]), hi = part_of(v[2 * i + 1]);
+            e[q].v[i] = (uint32_t)__bfloat16_as_ushort(lo) | (uint32_t)__bfloat16_as_ushort(hi) << 16;
         }
+}
+// MT x 16 rows of the weights per block, NT x 8 rows of x; PARTS 3: both in fp32
+template <int MT, int NT, int WBITS, bool HALF, bool VEC, int PARTS>
+__global__ void __launch_bounds__(256) few_kernel(const FewArgs a) {
+    __shared__ float sums[8][NT * 8][MT * 16 + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, r = blockIdx.y;
+    const long long n0 = (long long)blockIdx.x * (MT * 16);
+    float acc[MT][NT][4] = {};
+    long long wrow[MT][2], xrow[NT];
+    bool wok[MT][2], xok[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const long long n = n0 + i * 16 + h * 8 + g;
+            wok[i][h] = n < a.f.N;
+            wrow[i][h] = r * a.w_worker + (wok[i][h] ? n : 0) * a.w_stride;
+        }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        xok[j] = j * 8 + g < a.f.M;
+        xrow[j] = r * a.x_worker + (xok[j] ? j * 8 + g : 0) * a.x_stride;
     }
+    const auto product = [&](float (&d)[4], const Eight& w0, const Eight& w1, const Eight& x) {
+        mma_16x8<WBITS, HALF>(d, w0.v[0], w1.v[0], w0.v[1], w1.v[1], x.v[0], x.v[1]);
+        mma_16x8<WBITS, HALF>(d, w0.v[2], w1.v[2], w0.v[3], w1.v[3], x.v[2], x.v[3]);
+    };
+    const auto stretch = [&](int k) {
+        if constexpr (PARTS == 3) {
+            Eight w[MT][2][3], x[NT][3];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) parts_at<VEC>(w[i][h], a.w, wrow[i][h], wok[i][h], k, a.K);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) parts_at<VEC>(x[j], a.x, xrow[j], xok[j], k, a.K);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int p = 0; p < 6; ++p) product(acc[i][j], w[i][0][part_a(6, p)], w[i][1][part_a(6, p)], x[j][part_b(6, p)]);
+        } else {
+            Eight w[MT][2], x[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) w[i][h] = wok[i][h] ? eight_at<WBITS, HALF, VEC>(a.w, wrow[i][h], k, a.K) : Eight{};
+#pragma unroll
+            for (int j = 0; j < NT; ++j) x[j] = xok[j] ? eight_at<WBITS == 8 ? 8 : 16, HALF, VEC>(a.x, xrow[j], k, a.K) : Eight{};
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) product(acc[i][j], w[i][0], w[i][1], x[j]);
+        }
+    };
+    const int places = WBITS == 8 ? (a.K + 1) / 2 : a.K;     // pairs of 8 bits take the place of 16
+#pragma unroll(NT == 1 ? 2 : 1)
+    for (int k = warp * 64; k < places; k += 512) stretch(k + t * 8), stretch(k + 32 + t * 8);
+    // lane (g, t) holds rows g and g + 8 of the weights, rows 2 t and 2 t + 1 of x
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[warp][j * 8 + 2 * t + (e & 1)][i * 16 + g + (e >> 1) * 8] = acc[i][j][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 8 * MT * 16; i += 256) {
+        const int m = i / (MT * 16), c = i - m * (MT * 16);
+        const long long n = n0 + c;
+        if (m >= a.f.M || n >= a.f.N) continue;
+        float v[1] = {sums[0][m][c]};
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v[0] += sums[w][m][c];
+        Columns<1> cols;
+        load_columns(a.f, r, n, cols);
+        finish_any(a.f, r, m, n, v, cols, a.f.accumulate ? ADD : 0);
     }
 }
 
@@ -656,7 +859,7 @@ struct Product {
 };
 
 struct Plan {
-    bool small, lay_a, lay_b;
+    bool small, few, lay_a, lay_b;
     int cg, bn, planes, splits;
     long long ld_a, ld_b, part_ld;
     long long off_b, off_part, bytes;
@@ -673,26 +876,41 @@ bool taken_as_it_lies(const Product& p, const Operand& o) {
            (p.R == 1 || (o.worker * size % 16 == 0 && o.worker < 1ll << 36));       // (a map's strides end at 2^40 bytes)
 }
 
+// Tiles of 256 x 256 by two blocks, of 128 x 128 and 128 x 64 by one.  Measured in bf16 (us; each form with the splits that suit it best):
+// 512 x 4096 x 4096 24.1, 21.0, 33.7; 2048 x 2048 x 2048 19.5, 21.8, 35.6; 1024 x 1024 x 1024 13.4, 10.2, 9.7; 64 x 4096 x 4096 16.1, 12.2
+// (four splits; one 19.7), 14.9
+constexpr double FORM_BASE[3] = {8.5, 6.2, 6.2}, FORM_BLOCK[3] = {0.29, 0.22, 0.20};
 Plan plan_of(const Product& p, int sms) {
     Plan q{};
     q.planes = p.type == QS_F32 ? 3 : 1;
     q.splits = 1;
     const double work = 2.0 * p.R * p.M * p.N * p.K;
-    q.small = p.K == 0 || work < 1e6;
+    // (us, plain and on the matrix unit: fp32, which is laid out first, 64 x 64 x 64 4.7, 10.5; 33 x 200 x 300 12.6, 16.5; 509 x 1000 x 257
+    // 34, 20.  bf16 64 x 64 x 64 5.7, 5.5; 33 x 200 x 300 24, 9)
+    q.small = p.K == 0 || work < (p.type == QS_F32 ? 5e6 : 5e5);
     if (q.small) return q;
+    q.few = p.M <= FEW && !p.a.across && !p.b.across;
+    if (q.few) return q;
     const int size = p.type == QS_E4M3 ? 1 : 2;
     q.lay_a = !taken_as_it_lies(p, p.a);
     q.lay_b = !taken_as_it_lies(p, p.b);
     q.ld_a = round_up(memory_cols(p, p.a), 16);
     q.ld_b = round_up(memory_cols(p, p.b), 16);
-    const long long t2 = p.R * ((p.M + 255) / 256) * ((p.N + 255) / 256), t1 = p.R * ((p.M + 127) / 128) * ((p.N + 127) / 128);
-    const double c2 = 2.0 * ((t2 + sms / 2 - 1) / (sms / 2)), c1 = 1.25 * ((t1 + sms - 1) / sms);
-    q.cg = c2 <= c1 ? 2 : 1;
-    q.bn = q.cg == 2 ? 256 : 128;
-    const long long tiles = q.cg == 2 ? t2 : t1, slots = sms / q.cg;
-    const long long k_blocks = (p.K + 128 / size - 1) / (128 / size), iters = k_blocks;
-    q.splits = (int)std::max<long long>(1, std::min<long long>({slots / std::max<long long>(1, tiles), iters / 4, 64}));
-    if (q.splits > 1) q.splits = (int)std::max<long long>(q.splits, (k_blocks + CHUNK_BLOCKS - 1) / CHUNK_BLOCKS);
+    // What a tile and a split would take, in us: launch, first loads and last stores; a block along k (latency of the copies, where few
+    // blocks are at work, as much as the products); the join of the splits
+    const long long k_blocks = (p.K + 128 / size - 1) / (128 / size), pairs = q.planes == 3 ? 6 : 1;
+    double best = 0;
+    for (int form = 0; form < 3; ++form) {
+        const int cg = form == 0 ? 2 : 1, bn = form == 0 ? 256 : form == 1 ? 128 : 64;
+        const long long tiles = p.R * ((p.M + cg * TILE_M - 1) / (cg * TILE_M)) * ((p.N + bn - 1) / bn), slots = sms / cg;
+        for (long long splits = 1; splits <= 64 && (splits == 1 || k_blocks >= 2 * splits); splits *= 2) {
+            if ((splits > 1 && tiles >= slots) || ((splits > 1 || bn == 64) && k_blocks > splits * CHUNK_BLOCKS)) continue;
+            const long long rounds = (tiles * splits + slots - 1) / slots;
+            double us = FORM_BASE[form] + rounds * ((double)((k_blocks + splits - 1) / splits) * pairs * FORM_BLOCK[form] + 0.5);
+            if (splits > 1) us += 2.0 + 1e-6 * splits * p.R * p.M * p.N;
+            if (best == 0 || us < best) best = us, q.cg = cg, q.bn = bn, q.splits = (int)splits;
+        }
+    }
     long long at = 0;
     const long long wa = p.a.worker || p.R == 1 ? p.R : 1, wb = p.b.worker || p.R == 1 ? p.R : 1;
     if (q.lay_a) at += round_up(wa * q.planes * memory_rows(p, p.a) * q.ld_a * size, 256);
@@ -751,14 +969,21 @@ unsigned long long wait_limit() {
     return ns;
 }
 
-cudaError_t lay_out(const Product& p, const Operand& o, void* dst, int dst_type, int planes, long long ld, cudaStream_t st) {
+LayArgs lay_args(const Product& p, const Operand& o, void* dst, int dst_type, int planes, long long ld) {
     LayArgs a{};
-    const long long workers = o.worker || p.R == 1 ? p.R : 1;
+    a.workers = o.worker || p.R == 1 ? p.R : 1;
     a.src = o.p; a.src_type = o.type; a.src_stride = o.ld; a.src_worker = o.worker;
     a.dst = dst; a.dst_type = dst_type; a.planes = planes; a.ld = ld; a.rows = memory_rows(p, o); a.cols = memory_cols(p, o);
-    a.vec = o.type == QS_F32 && aligned_to(o.p, 16) && (a.rows == 1 || o.ld % 4 == 0) && (workers == 1 || o.worker % 4 == 0);
-    const long long items = a.rows * (ld / 8);
-    return launch(false, lay_kernel, dim3((unsigned)std::min<long long>((items + 255) / 256, 1 << 16), (unsigned)workers), 256, 0, st, a);
+    a.vec = o.type == QS_F32 && aligned_to(o.p, 16) && (a.rows == 1 || o.ld % 4 == 0) && (a.workers == 1 || o.worker % 4 == 0);
+    return a;
+}
+cudaError_t lay_out(const LayBoth& both, int sides, cudaStream_t st) {
+    long long items = 0, workers = 0;
+    for (int i = 0; i < sides; ++i) {
+        items = std::max(items, both.side[i].rows * (both.side[i].ld / 8));
+        workers = std::max<long long>(workers, both.side[i].workers);
+    }
+    return launch(false, lay_kernel, dim3((unsigned)std::min<long long>((items + 255) / 256, 1 << 16), (unsigned)workers, (unsigned)sides), 256, 0, st, both);
 }
 
 template <int CG, int BN, class T>
@@ -788,22 +1013,63 @@ cudaError_t launch_gemm(const CUtensorMap (&map)[4], const GemmArgs& g, bool aft
     return g.f.type == QS_BF16 ? launch_gemm_as<CG, BN, bf16>(map, g, after, sms, st) : launch_gemm_as<CG, BN, __half>(map, g, after, sms, st);
 }
 
+template <int WBITS, bool HALF, bool VEC, int PARTS>
+cudaError_t launch_few_as(const Product& p, const FewArgs& a, cudaStream_t st) {
+    // 32 rows of the weights per block where that still gives every SM one: x is read once per block
+    const bool wide = PARTS == 1 && p.M > 8 && p.R * p.N >= 32 * 148;
+    const dim3 grid((unsigned)((p.N + (wide ? 31 : 15)) / (wide ? 32 : 16)), (unsigned)p.R);
+    if constexpr (PARTS == 1)
+        if (wide)
+            return p.M <= 16 ? launch(false, few_kernel<2, 2, WBITS, HALF, VEC, 1>, grid, 256, 0, st, a)
+                             : launch(false, few_kernel<2, 4, WBITS, HALF, VEC, 1>, grid, 256, 0, st, a);
+    return p.M <= 8    ? launch(false, few_kernel<1, 1, WBITS, HALF, VEC, PARTS>, grid, 256, 0, st, a)
+           : p.M <= 16 ? launch(false, few_kernel<1, 2, WBITS, HALF, VEC, PARTS>, grid, 256, 0, st, a)
+                       : launch(false, few_kernel<1, 4, WBITS, HALF, VEC, PARTS>, grid, 256, 0, st, a);
+}
+cudaError_t launch_few(const Product& p, const FewArgs& a, bool vec, cudaStream_t st) {
+    if (p.type == QS_E4M3) return vec ? launch_few_as<8, true, true, 1>(p, a, st) : launch_few_as<8, true, false, 1>(p, a, st);
+    if (p.type == QS_F32) return vec ? launch_few_as<32, false, true, 3>(p, a, st) : launch_few_as<32, false, false, 3>(p, a, st);
+    const bool wide = p.b.type == QS_F32;
+    if (p.type == QS_F16)
+        return wide ? (vec ? launch_few_as<32, true, true, 1>(p, a, st) : launch_few_as<32, true, false, 1>(p, a, st))
+                    : (vec ? launch_few_as<16, true, true, 1>(p, a, st) : launch_few_as<16, true, false, 1>(p, a, st));
+    return wide ? (vec ? launch_few_as<32, false, true, 1>(p, a, st) : launch_few_as<32, false, false, 1>(p, a, st))
+                : (vec ? launch_few_as<16, false, true, 1>(p, a, st) : launch_few_as<16, false, false, 1>(p, a, st));
+}
+
 int run_product(const Product& p, const Finish& f, void* work, int64_t work_bytes, int* status, cudaStream_t st) {
     const int sms = sm_count();
     if (!sms) return QS_CUDA;
     const Plan q = plan_of(p, sms);
     if (q.small) {
-        const auto side = [&](const Operand& o) { return Side{o.p, o.type, p.type, o.across ? 1 : o.ld, o.across ? o.ld : 1, o.worker}; };
-        return status_of(launch(false, small_kernel, dim3((unsigned)((p.N + 63) / 64), (unsigned)std::min<long long>((p.M + 63) / 64, 65535), (unsigned)p.R), 256, 0, st, side(p.a), side(p.b),
-                                (long long)p.K, f));
+        const auto side = [&](const Operand& o) { return Side{o.p, o.across ? 1 : o.ld, o.across ? o.ld : 1, o.worker}; };
+        const bool same = p.b.type == p.type;
+        const auto kernel = p.type == QS_E4M3   ? small_kernel<QS_E4M3, QS_E4M3>
+                            : p.type == QS_F32  ? small_kernel<QS_F32, QS_F32>
+                            : p.type == QS_BF16 ? (same ? small_kernel<QS_BF16, QS_BF16> : small_kernel<QS_BF16, QS_F32>)
+                                                : (same ? small_kernel<QS_F16, QS_F16> : small_kernel<QS_F16, QS_F32>);
+        return status_of(launch(false, kernel, dim3((unsigned)((p.N + 31) / 32), (unsigned)std::min<long long>((p.M + 31) / 32, 65535), (unsigned)p.R), 256, 0, st,
+                                side(p.a), side(p.b), (int)p.K, f));
     }
-    if (q.bytes > 0 && (!work || !aligned_to(work, 256))) return QS_INVALID_ARG;
-    if (work_bytes < q.bytes) return QS_CAPACITY;
+    if (q.few) {
+        FewArgs a{};
+        a.x = p.a.p; a.x_stride = p.a.ld; a.x_worker = p.a.worker;
+        a.w = p.b.p; a.w_stride = p.b.ld; a.w_worker = p.b.worker;
+        a.K = (int)p.K; a.f = f;
+        const auto vec = [&](const Operand& o) {
+            const int size = bytes_of(o.type);
+            return aligned_to(o.p, 16) && (o.rows == 1 || o.ld * size % 16 == 0) && (p.R == 1 || o.worker * size % 16 == 0);
+        };
+        return status_of(launch_few(p, a, vec(p.a) && vec(p.b), st));
+    }
+    if (q.bytes > 0 && work && !aligned_to(work, 256)) return QS_INVALID_ARG;
+    if ((work ? work_bytes : 0) < q.bytes) return QS_CAPACITY;
     uint8_t* w = static_cast<uint8_t*>(work);
     const int type = p.type == QS_F32 ? QS_BF16 : p.type, size = type == QS_E4M3 ? 1 : 2;
     GemmArgs g{};
     CUtensorMap map[4] = {};
-    bool after = false;
+    LayBoth both{};
+    int sides = 0;
     for (int i = 0; i < 2; ++i) {
         const Operand& o = i ? p.b : p.a;
         const bool lay = i ? q.lay_b : q.lay_a;
@@ -811,9 +1077,7 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
         const long long ld = lay ? (i ? q.ld_b : q.ld_a) : o.ld;
         const void* at = lay ? w + (i ? q.off_b : 0) : o.p;
         if (lay) {
-            const cudaError_t e = lay_out(p, o, w + (i ? q.off_b : 0), type, q.planes, ld, st);
-            if (e != cudaSuccess) return status_of(e);
-            after = true;
+            both.side[sides++] = lay_args(p, o, w + (i ? q.off_b : 0), type, q.planes, ld);
         }
         (i ? g.b_worker : g.a_worker) = workers > 1;
         (i ? g.b_across : g.a_across) = o.across;
@@ -848,7 +1112,10 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
         if (!encode_out(&map[2], f.out, f.type, p.N, p.M, 1, p.R, f.out_stride, 0, f.out_worker) ||
             (f.pre && !encode_out(&map[3], f.pre, f.type, p.N, p.M, 1, p.R, f.pre_stride, 0, p.M * f.pre_stride))) return QS_CUDA;
     }
-    cudaError_t e = q.cg == 2 ? launch_gemm<2, 256>(map, g, after, sms, st) : launch_gemm<1, 128>(map, g, after, sms, st);
+    cudaError_t e = sides ? lay_out(both, sides, st) : cudaSuccess;
+    if (e != cudaSuccess) return status_of(e);
+    const bool after = sides > 0;
+    e = q.cg == 2 ? launch_gemm<2, 256>(map, g, after, sms, st) : q.bn == 128 ? launch_gemm<1, 128>(map, g, after, sms, st) : launch_gemm<1, 64>(map, g, after, sms, st);
     if (e != cudaSuccess || q.splits == 1) return status_of(e);
     const long long items = p.R * p.M * (f.vec ? (p.N + 7) / 8 : p.N);
     const dim3 grid((unsigned)std::min<long long>((items + 255) / 256, 1 << 20));
