@@ -576,9 +576,9 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
  *   one w for all) multiply the sums, out_type any other.  The scales are NULL otherwise.
  *   bias (NULL: none): N of bias_type per worker.  Sums, bias and activation are fp32, rounded once.
  *   Products of 16- and 8-bit elements are exact.  fp32 operands are cut into three parts of 8
- *   bits of significand, and products of parts below 2^-24 of the whole are left out; with an
- *   infinity among them, the results that it enters are not finite (some NaN where the sum would be
- *   infinite).  Small products (under a million operations) are plain fp32.
+ *   bits of significand, and the products of their last parts, below 2^-21 of the whole, are left
+ *   out; results that an infinity enters are NaN.  Small products of them (under five million
+ *   operations) are plain fp32.
  *   activation: QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU z / (1 + e^-z), QS_ACT_GELU z Phi(z).
  *   work: 256-byte aligned, qs_linear_bytes(...) bytes for the same arguments (their alignment
  *   counts: operands off 16-byte boundaries are laid out anew), else QS_CAPACITY; may be NULL for 0.

@@ -73,6 +73,13 @@ __device__ __forceinline__ void tile_store(const CUtensorMap* map, uint32_t src,
                  : "memory");
 }
 
+// the same, added to what is there in fp32 (by the L2)
+__device__ __forceinline__ void tile_add(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+    asm volatile("cp.reduce.async.bulk.tensor.4d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1),
+                 "r"(c2), "r"(c3)
+                 : "memory");
+}
+
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t* dst, uint32_t columns) {
     if (CG == 2) asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst)), "r"(columns) : "memory");

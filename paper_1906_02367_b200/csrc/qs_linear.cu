@@ -218,21 +218,23 @@ __device__ __forceinline__ void finish_columns(const Finish& f, int r, long long
 
 // ------------------------------------------------------------------ operands for the matrix unit
 // Operands that the tensor maps cannot take as they lie (another type, rows off the 16-byte boundary) are laid out in the
-// workspace: fp32 rounded to the other operand's 16 bits, or cut into three bf16 parts x = x0 + x1 + x2, each the rest of
-// the ones before it rounded: 24 bits in all.
+// workspace: fp32 rounded to the other operand's 16 bits, or cut into three bf16 parts x = x0 + x1 + x2, the first eight bits of what
+// the ones before left: 24 bits in all, exactly.
 struct LayArgs {
     const void* src; int src_type; long long src_stride, src_worker;
     void* dst; int dst_type, planes; long long ld;   // (workers, planes, rows, ld)
     long long rows, cols; int workers, vec;
 };
-__device__ __forceinline__ bf16 part_of(float& v) {
-    bf16 p = __float2bfloat16_rn(v);
-    if (isinf(__bfloat162float(p)) && !isinf(v)) p = __float2bfloat16_rz(v);
-    const float f = __bfloat162float(p);
-    v = isinf(f) ? 0.0f : v - f;                     // (exact; a NaN stays one)
-    return p;
+// the next eight bits of two numbers, cut off, as a pair of bf16; v keeps the rest (exactly)
+__device__ __forceinline__ uint32_t parts_of(float& v0, float& v1) {
+    const uint32_t a = __float_as_uint(v0), b = __float_as_uint(v1);
+    v0 -= __uint_as_float(a & 0xffff0000u);
+    v1 -= __uint_as_float(b & 0xffff0000u);
+    return __byte_perm(a, b, 0x7632);
 }
-// parts of the operands whose products are added, the small ones first: what is left out is 2^-24 of the whole
+
+// parts of the operands whose products are added, the small ones first: x1 y2, x2 y1 and x2 y2 are left out, 2^-21 of a product at
+// most, 2^-23 as a rule
 __device__ __forceinline__ int part_a(int pairs, int p) { return pairs == 1 ? 0 : (0x010120 >> (4 * p)) & 15; }
 __device__ __forceinline__ int part_b(int pairs, int p) { return pairs == 1 ? 0 : (0x001102 >> (4 * p)) & 15; }
 
@@ -266,12 +268,11 @@ __global__ void __launch_bounds__(256) lay_kernel(const LayBoth both) {
         if (a.dst_type == QS_F16) {
             store_vec<8>(static_cast<__half*>(a.dst) + (r * a.rows + row) * a.ld + c, v);
         } else {
-            for (int p = 0; p < a.planes; ++p) {
-                Pack<bf16, 8> q;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q.e[j] = a.planes == 1 ? __float2bfloat16_rn(v[j]) : part_of(v[j]);
-                *reinterpret_cast<Pack<bf16, 8>*>(static_cast<bf16*>(a.dst) + ((r * a.planes + p) * a.rows + row) * a.ld + c) = q;
-            }
+            if (a.planes == 1) store_vec<8>(static_cast<bf16*>(a.dst) + (r * a.rows + row) * a.ld + c, v);
+            else
+                for (int p = 0; p < 3; ++p)
+                    *reinterpret_cast<uint4*>(static_cast<bf16*>(a.dst) + ((r * 3 + p) * a.rows + row) * a.ld + c) =
+                        make_uint4(parts_of(v[0], v[1]), parts_of(v[2], v[3]), parts_of(v[4], v[5]), parts_of(v[6], v[7]));
         }
     }
 }
@@ -281,8 +282,9 @@ constexpr int TILE_M = 128;                          // rows of a block's part o
 constexpr int STAGES = 5;
 constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
 // The matrix unit cuts what lies below 2^-24 of a sum at every addition, always towards zero: 8e-10 of the result per element
-// summed.  Results in fp32 are therefore added up from sums over this many blocks of 128 bytes (4096 elements of 16 bits: 3e-6).
-constexpr int CHUNK_BLOCKS = 64;
+// summed.  Results in fp32 are therefore added up, rounded to nearest, from sums over this many blocks of 128 bytes (1024 elements
+// of 16 bits: 8e-7).  (Weights' gradient of 8 x 4096 rows, 4096 x 1024: 205 us with 64 blocks, 3e-6 off; 218 with 32; 243 with 16)
+constexpr int CHUNK_BLOCKS = 16;
 constexpr int PASS_BYTES = 8 * 2 * 4096;             // two tiles of 32 rows of 128 bytes on their way out, per finishing warp
 
 struct GemmArgs {
@@ -296,6 +298,7 @@ struct GemmArgs {
     int eight;                                       // 8-bit operands
     uint32_t idesc;
     int columns;                                     // there is a bias or a scale of the columns
+    int l2_adds;                                     // nothing but sums, in fp32: the copies out add what is to be added
     unsigned long long limit;
     int* status;
     Finish f;
@@ -336,8 +339,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             const __grid_constant__ CUtensorMap map_pre, const __grid_constant__ GemmArgs g) {
     extern __shared__ __align__(1024) uint8_t ring[];
     constexpr int A_BYTES = TILE_M * 128, B_ROWS = BN / CG, STAGE = stage_bytes<CG, BN>();
-    // Tiles of 64 columns: the two halves of the finishing warps take accumulators in turn (each unit is one sum then), else half of
-    // the columns of each
+    // Tiles of 64 columns: the two halves of the finishing warps take units in turn, else half of the columns of each
     constexpr bool TURNS = BN == 64;
     Small& small = *reinterpret_cast<Small*>(ring + STAGES * STAGE + PASS_BYTES);
     uint64_t *full = small.full, *empty = small.empty, *acc_full = small.acc_full, *acc_empty = small.acc_empty;
@@ -465,13 +467,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         const uint32_t leader[2] = {CG == 2 ? in_block(smem_addr(&acc_empty[0]), 0) : smem_addr(&acc_empty[0]),
                                     CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
         const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (TURNS ? 0 : half * HALF);
-        int n = 0, out_buf = 0;
+        int n = 0, out_buf = 0, turn = 0;
         bool fine = limit != 0;
         for (int u = cluster; u < g.units; u += clusters) {
             const Unit t = unit_of(g, u);
             const long long m0 = (long long)(t.tm * CG + (int)rank) * TILE_M + q * 32, n0 = (long long)t.tn * BN + (TURNS ? 0 : half * HALF);
-            if (TURNS && (n & 1) != half) {
-                ++n;
+            if (TURNS && (turn++ & 1) != half) {
+                n += (t.kb1 - t.kb0 + g.chunk - 1) / g.chunk;
                 continue;
             }
             const long long m = m0 + lane, row = t.r * g.M + m;
@@ -488,12 +490,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             }
             const float a_scale = g.f.a_scale && in ? g.f.a_scale[row] : 1.0f;
             for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += g.chunk, ++n) {
-                const int buf = n & 1, how = (g.f.accumulate || kb0 > t.kb0 ? ADD : 0) | (kb0 + g.chunk < t.kb1 || g.splits > 1 ? RAW : 0);
+                const bool more = g.f.accumulate || kb0 > t.kb0, added = more && g.l2_adds;
+                const int buf = n & 1, how = (more && !added ? ADD : 0) | (kb0 + g.chunk < t.kb1 || g.splits > 1 ? RAW : 0);
                 if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, limit));
                 if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
                 tc_fence_after();
-                // sums of the chunks before have arrived where they are read again
-                if (how & ADD) {
+                // sums of the chunks before have arrived where they are read again or added to, in this order
+                if (more) {
                     bulk_wait_all();
                     __syncwarp();
                 }
@@ -555,7 +558,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            tile_store(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
+                            if (added) tile_add(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
+                            else tile_store(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
                             if (g.f.pre && !(how & RAW)) tile_store(&map_pre, smem_addr(pass + 4096), (int)n1, (int)m0, 0, t.r);
                             bulk_commit();
                         }
@@ -762,10 +766,7 @@ __device__ __forceinline__ void parts_at(Eight (&e)[3], const void* p, long long
 #pragma unroll
     for (int q = 0; q < 3; ++q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bf16 lo = part_of(v[2 * i]), hi = part_of(v[2 * i + 1]);
-            e[q].v[i] = (uint32_t)__bfloat16_as_ushort(lo) | (uint32_t)__bfloat16_as_ushort(hi) << 16;
-        }
+        for (int i = 0; i < 4; ++i) e[q].v[i] = parts_of(v[2 * i], v[2 * i + 1]);
 }
 // MT x 16 rows of the weights per block, NT x 8 rows of x; PARTS 3: both in fp32
 template <int MT, int NT, int WBITS, bool HALF, bool VEC, int PARTS>
@@ -904,7 +905,7 @@ Plan plan_of(const Product& p, int sms) {
         const int cg = form == 0 ? 2 : 1, bn = form == 0 ? 256 : form == 1 ? 128 : 64;
         const long long tiles = p.R * ((p.M + cg * TILE_M - 1) / (cg * TILE_M)) * ((p.N + bn - 1) / bn), slots = sms / cg;
         for (long long splits = 1; splits <= 64 && (splits == 1 || k_blocks >= 2 * splits); splits *= 2) {
-            if ((splits > 1 && tiles >= slots) || ((splits > 1 || bn == 64) && k_blocks > splits * CHUNK_BLOCKS)) continue;
+            if (splits > 1 && tiles >= slots) continue;
             const long long rounds = (tiles * splits + slots - 1) / slots;
             double us = FORM_BASE[form] + rounds * ((double)((k_blocks + splits - 1) / splits) * pairs * FORM_BLOCK[form] + 0.5);
             if (splits > 1) us += 2.0 + 1e-6 * splits * p.R * p.M * p.N;
@@ -1093,7 +1094,7 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.k_blocks = (int)((p.K + g.k_step - 1) / g.k_step);
     g.pairs = q.planes == 3 ? 6 : 1;
     // (the sums so far lie in the result, so it has to hold fp32 and be nothing that is still to be read)
-    g.chunk = q.splits == 1 && f.type == QS_F32 && f.res != f.out ? CHUNK_BLOCKS : g.k_blocks;
+    g.chunk = f.type == QS_F32 && (q.splits > 1 || f.res != f.out) ? CHUNK_BLOCKS : g.k_blocks;
     g.eight = type == QS_E4M3;
     // sums in fp32; operand types (e4m3 and fp16 are 0, bf16 is 1); which lie across k; the tile
     const uint32_t t = type == QS_BF16 ? 1 : 0;
@@ -1102,11 +1103,13 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.status = status;
     g.f = f;
     g.columns = q.splits == 1 && (f.bias || f.b_scale);
-    if ((f.res || f.accumulate || g.chunk < g.k_blocks) && p.N * size_of_type(f.type) % 16) g.f.vec = 0;
+    g.l2_adds = f.vec && f.type == QS_F32 && q.splits == 1 && f.act == QS_ACT_NONE && !f.bias && !f.res && !f.pre && !f.a_scale;
+    if ((f.res || ((f.accumulate || g.chunk < g.k_blocks) && !g.l2_adds)) && p.N * size_of_type(f.type) % 16) g.f.vec = 0;
     float* part = reinterpret_cast<float*>(w + q.off_part);
     if (q.splits > 1) {                              // sums instead of results: (R, splits, M, part_ld)
         g.f = Finish{};
         g.f.M = p.M; g.f.N = p.N; g.f.type = QS_F32; g.f.vec = 1;
+        g.l2_adds = 1;
         if (!encode_out(&map[2], part, QS_F32, p.N, p.M, q.splits, p.R, q.part_ld, p.M * q.part_ld, q.splits * p.M * q.part_ld)) return QS_CUDA;
     } else if (g.f.vec) {
         if (!encode_out(&map[2], f.out, f.type, p.N, p.M, 1, p.R, f.out_stride, 0, f.out_worker) ||

@@ -32,8 +32,13 @@ def _act(activation):
 
 def _like(t, shape, dtype, what):
     """Checks a tensor that goes with another: its shape and type."""
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+    if t is not None and (t.shape != shape or t.dtype != dtype):
         raise ValueError(f"{what} must be {tuple(shape)} of {dtype}, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _pitch(t, D, what):
+    """Elements between the rows of D of a tensor (None: 0)."""
+    return 0 if t is None else D if t.is_contiguous() else _rows(t, what)
 
 
 def _counted(t, n, what):
@@ -58,7 +63,7 @@ def _vector_of(t, R, n, workers, what):
     """Worker stride of a vector of n per worker, (R, n), or of one for all, (n)."""
     if t is None:
         return 0
-    if tuple(t.shape) != ((R, n) if workers else (n,)) or (n > 1 and t.stride(-1) != 1):
+    if t.shape != ((R, n) if workers else (n,)) or (n > 1 and t.stride(-1) != 1):
         raise ValueError(f"{what} must be {(R, n) if workers else (n,)} with unit stride, not {tuple(t.shape)}")
     return t.stride(0) if workers and R > 1 else (n if workers else 0)
 
@@ -99,35 +104,35 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, quantize=False, out=None, 
         raise ValueError(f"weight must be of {x.dtype} or torch.float32, not {weight.dtype}")
     if not eps > 0.0:
         raise ValueError("eps must be positive")
-    _like(residual, x.shape, x.dtype, "residual")
+    shape = x.shape
+    _like(residual, shape, x.dtype, "residual")
     if residual is None:
         if hidden is not None:
             raise ValueError("hidden needs a residual")
     elif hidden is None:
-        hidden = _allocate(stream, tuple(x.shape), x.dtype, device)
+        hidden = _allocate(stream, shape, x.dtype, device)
     else:
-        _like(hidden, x.shape, x.dtype, "hidden")
+        _like(hidden, shape, x.dtype, "hidden")
     out_type = E4M3 if quantize else x.dtype
     if out is None:
-        out = _allocate(stream, tuple(x.shape), out_type, device)
+        out = _allocate(stream, shape, out_type, device)
     else:
-        _like(out, x.shape, out_type, "out")
-    n = R * N
+        _like(out, shape, out_type, "out")
     if quantize:
         if scale is None:
-            scale = _allocate(stream, tuple(x.shape[:-1]), torch.float32, device)
-        _counted(scale, n, "scale")
+            scale = _allocate(stream, shape[:-1], torch.float32, device)
+        _counted(scale, R * N, "scale")
     elif scale is not None:
         raise ValueError("scale belongs to quantize")
     if rstd is None:
-        rstd = _allocate(stream, tuple(x.shape[:-1]), torch.float32, device)
+        rstd = _allocate(stream, shape[:-1], torch.float32, device)
     elif rstd is False:
         rstd = None
-    _counted(rstd, n, "rstd")
-    _done(lib().qs_rms_norm(R, N, D, x.data_ptr(), code, _rows(x, "x"), _ptr(residual), _rows(residual, "residual") if residual is not None else 0,
-                            _ptr(weight), _type(weight, "weight") if weight is not None else code, w_step, eps, _ptr(hidden),
-                            _rows(hidden, "hidden") if hidden is not None else 0, out.data_ptr(), _ALL[out_type], _rows(out, "out"), _ptr(scale),
-                            _ptr(rstd), _handle(stream, device)), "qs_rms_norm")
+    else:
+        _counted(rstd, R * N, "rstd")
+    _done(lib().qs_rms_norm(R, N, D, x.data_ptr(), code, _pitch(x, D, "x"), _ptr(residual), _pitch(residual, D, "residual"), _ptr(weight),
+                            code if weight is None else _TYPE[weight.dtype], w_step, eps, _ptr(hidden), _pitch(hidden, D, "hidden"), out.data_ptr(),
+                            _ALL[out_type], _pitch(out, D, "out"), _ptr(scale), _ptr(rstd), _handle(stream, device)), "qs_rms_norm")
     return RmsNorm(out, x if residual is None else hidden, rstd, scale)
 
 
@@ -138,12 +143,12 @@ def quantize(x, out=None, scale=None, stream=None):
     R, N, D = _activations(x, False, "x")
     code = _type(x, "x")
     if out is None:
-        out = _allocate(stream, tuple(x.shape), E4M3, device)
+        out = _allocate(stream, x.shape, E4M3, device)
     _like(out, x.shape, E4M3, "out")
     if scale is None:
-        scale = _allocate(stream, tuple(x.shape[:-1]), torch.float32, device)
+        scale = _allocate(stream, x.shape[:-1], torch.float32, device)
     _counted(scale, N, "scale")
-    _done(lib().qs_quantize_rows(N, D, x.data_ptr(), code, _rows(x, "x"), out.data_ptr(), _rows(out, "out"), scale.data_ptr(),
+    _done(lib().qs_quantize_rows(N, D, x.data_ptr(), code, _pitch(x, D, "x"), out.data_ptr(), _pitch(out, D, "out"), scale.data_ptr(),
                                  _handle(stream, device)), "qs_quantize_rows")
     return Quantized(out, scale)
 
@@ -165,7 +170,7 @@ def rms_norm_grad(grad_out, hidden, rstd, weight=None, grad_hidden=None, out=Non
     if accumulate and out_weight is None:
         raise ValueError("accumulate needs out_weight")
     if out is None:
-        out = _allocate(stream, tuple(hidden.shape), hidden.dtype, device)
+        out = _allocate(stream, hidden.shape, hidden.dtype, device)
     _like(out, hidden.shape, hidden.dtype, "out")
     dw_step, ptr, size, keep = 0, None, 0, None
     if weight is None:
@@ -173,14 +178,13 @@ def rms_norm_grad(grad_out, hidden, rstd, weight=None, grad_hidden=None, out=Non
             raise ValueError("out_weight needs weight")
     else:
         if out_weight is None:
-            out_weight = _allocate(stream, tuple(weight.shape), torch.float32, device)
+            out_weight = _allocate(stream, weight.shape, torch.float32, device)
         _like(out_weight, weight.shape, torch.float32, "out_weight")
         dw_step = _vector_of(out_weight, R, D, workers, "out_weight")
         ptr, size, keep = _work(work, lib().qs_rms_norm_grad_bytes(R, N, D), "qs_rms_norm_grad_bytes", stream, device)
-    _done(lib().qs_rms_norm_grad(R, N, D, grad_out.data_ptr(), code, _rows(grad_out, "grad_out"), hidden.data_ptr(), _rows(hidden, "hidden"),
-                                 rstd.data_ptr(), _ptr(weight), _type(weight, "weight") if weight is not None else code, w_step,
-                                 _ptr(grad_hidden), _rows(grad_hidden, "grad_hidden") if grad_hidden is not None else 0, out.data_ptr(),
-                                 _rows(out, "out"), _ptr(out_weight), dw_step, int(accumulate), ptr, size, _handle(stream, device)),
+    _done(lib().qs_rms_norm_grad(R, N, D, grad_out.data_ptr(), code, _pitch(grad_out, D, "grad_out"), hidden.data_ptr(), _pitch(hidden, D, "hidden"),
+                                 rstd.data_ptr(), _ptr(weight), code if weight is None else _TYPE[weight.dtype], w_step, _ptr(grad_hidden),
+                                 _pitch(grad_hidden, D, "grad_hidden"), out.data_ptr(), _pitch(out, D, "out"), _ptr(out_weight), dw_step, int(accumulate), ptr, size, _handle(stream, device)),
           "qs_rms_norm_grad")
     return RmsNormGrad(out, out_weight)
 
@@ -200,11 +204,11 @@ def dropout(x, p, seed, round=0, layer=0, worker=0, workers=False, residual=None
     if not 0 <= round < 1 << 40 or not 0 <= layer < 1 << 16 or not 0 <= worker < 1 << 31:
         raise ValueError("round must be below 2^40, layer below 2^16, worker below 2^31, none negative")
     if out is None:
-        out = _allocate(stream, tuple(x.shape), x.dtype, device)
+        out = _allocate(stream, x.shape, x.dtype, device)
     else:
         _like(out, x.shape, x.dtype, "out")
-    _done(lib().qs_dropout(R, N, D, x.data_ptr(), code, _rows(x, "x"), _ptr(residual), _rows(residual, "residual") if residual is not None else 0,
-                           p, seed & 0xFFFFFFFFFFFFFFFF, round, worker, layer, out.data_ptr(), _rows(out, "out"), _handle(stream, device)), "qs_dropout")
+    _done(lib().qs_dropout(R, N, D, x.data_ptr(), code, _pitch(x, D, "x"), _ptr(residual), _pitch(residual, D, "residual"), p,
+                           seed & 0xFFFFFFFFFFFFFFFF, round, worker, layer, out.data_ptr(), _pitch(out, D, "out"), _handle(stream, device)), "qs_dropout")
     return out
 
 
@@ -254,13 +258,12 @@ def linear(x, weight, bias=None, activation=None, residual=None, x_scale=None, w
         pre = _allocate(stream, shape, dtype, device)
     _like(pre, shape, dtype, "pre")
     L = lib()
-    x_row, w_code = _rows(x, "x"), _type(weight, "weight", _ALL)
+    x_row, w_code = _pitch(x, K, "x"), _ALL[weight.dtype]
     ptr, size, keep = _work(work, L.qs_linear_bytes(R, M, N, K, x.data_ptr(), x_code, x_row, weight.data_ptr(), w_code, w_worker, w_row),
                             "qs_linear_bytes", stream, device)
     _done(L.qs_linear(R, M, N, K, x.data_ptr(), x_code, x_row, _ptr(x_scale), weight.data_ptr(), w_code, w_worker, w_row, _ptr(weight_scale),
-                      _ptr(bias), bias_type, bias_step, act, _ptr(residual), _rows(residual, "residual") if residual is not None else 0,
-                      _ptr(pre), _rows(pre, "pre") if pre is not None else 0, out.data_ptr(), _TYPE[dtype], _rows(out, "out"), ptr, size,
-                      _word(status), _handle(stream, device)), "qs_linear")
+                      _ptr(bias), bias_type, bias_step, act, _ptr(residual), _pitch(residual, N, "residual"), _ptr(pre), _pitch(pre, N, "pre"),
+                      out.data_ptr(), _TYPE[dtype], _pitch(out, N, "out"), ptr, size, _word(status), _handle(stream, device)), "qs_linear")
     return Linear(out, pre)
 
 
@@ -277,7 +280,7 @@ def activation_grad(grad_out, pre=None, activation=None, out=None, bias=False, o
             raise ValueError("the gradient of an activation needs pre")
         _like(pre, grad_out.shape, grad_out.dtype, "pre")
         if out is None:
-            out = _allocate(stream, tuple(grad_out.shape), grad_out.dtype, device)
+            out = _allocate(stream, grad_out.shape, grad_out.dtype, device)
         _like(out, grad_out.shape, grad_out.dtype, "out")
     elif out is not None:
         raise ValueError("without an activation there is nothing to write into out")
@@ -293,49 +296,58 @@ def activation_grad(grad_out, pre=None, activation=None, out=None, bias=False, o
         ptr, size, keep = _work(work, lib().qs_activation_grad_bytes(R, M, N), "qs_activation_grad_bytes", stream, device)
     elif out is None:
         return grad_out, None
-    _done(lib().qs_activation_grad(R, M, N, grad_out.data_ptr(), code, _rows(grad_out, "grad_out"), _ptr(pre) if act else None,
-                                   _rows(pre, "pre") if act else 0, act, _ptr(out), _rows(out, "out") if out is not None else 0, _ptr(out_bias), step,
-                                   int(accumulate), ptr, size, _handle(stream, device)), "qs_activation_grad")
+    _done(lib().qs_activation_grad(R, M, N, grad_out.data_ptr(), code, _pitch(grad_out, N, "grad_out"), _ptr(pre) if act else None,
+                                   _pitch(pre, N, "pre") if act else 0, act, _ptr(out), _pitch(out, N, "out"), _ptr(out_bias), step, int(accumulate), ptr, size, _handle(stream, device)), "qs_activation_grad")
     return (grad_out if out is None else out), out_bias
 
 
 def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, need_weight=True, bias=False, dtype=torch.float32, out=None,
-                out_weight=None, out_bias=None, accumulate=False, status=None, stream=None):
+                out_weight=None, out_bias=None, accumulate=False, work=None, status=None, stream=None):
     """Gradients of act(x weight^T + bias) from that of its result (qs_activation_grad, qs_linear_grad_input,
     qs_linear_grad_weight); the residual's is grad_out itself.  pre: what linear saved (not needed without an activation).
     The gradient in front of the activation is rounded to grad_out's type, which is x's.  The weight's gradient is of `dtype`
     (fp32 or x's type), the bias's fp32; out_weight and out_bias may be stretches of a gradient batch, and accumulate adds
     to them.  Returns LinearGrad(x, weight, bias, pre): None for what was not asked for; pre is the gradient in front of the
     activation."""
-    device = _on(x, weight, grad_out, pre, out, out_weight, out_bias, status)
+    device = _on(x, weight, grad_out, pre, out, out_weight, out_bias, work, status)
     workers, R, M, N, K, w_worker, w_row = _operands(x, weight)
-    code = _type(x, "x")
+    code, act = _type(x, "x"), _act(activation)
     _like(grad_out, (*x.shape[:-1], N), x.dtype, "grad_out")
     if not need_x and out is not None or not need_weight and out_weight is not None:
         raise ValueError("out and out_weight belong to gradients that are asked for")
     if accumulate and (need_weight and out_weight is None or bias and out_bias is None):
         raise ValueError("accumulate needs out_weight and out_bias for what it is to be added to")
-    dz, db = activation_grad(grad_out, pre, activation, bias=bias, out_bias=out_bias, workers=workers, accumulate=accumulate and out_bias is not None,
-                             stream=stream)
-    L, dz_row, x_row = lib(), _rows(dz, "grad_out"), _rows(x, "x")
-    if need_x:
-        if out is None:
-            out = _allocate(stream, tuple(x.shape), x.dtype, device)
-        _like(out, x.shape, x.dtype, "out")
-        w_code = _type(weight, "weight")
-        args = (R, M, N, K, dz.data_ptr(), code, dz_row, weight.data_ptr(), w_code, w_worker, w_row)
-        ptr, size, keep = _work(None, L.qs_linear_grad_input_bytes(*args), "qs_linear_grad_input_bytes", stream, device)
-        _done(L.qs_linear_grad_input(*args, out.data_ptr(), _rows(out, "out"), ptr, size, _word(status), _handle(stream, device)), "qs_linear_grad_input")
     if need_weight:
         if out_weight is None:
             if dtype not in (x.dtype, torch.float32):
                 raise ValueError(f"the weight's gradient cannot be of {dtype}")
-            out_weight = _allocate(stream, tuple(weight.shape), dtype, device)
+            out_weight = _allocate(stream, weight.shape, dtype, device)
         elif out_weight.dtype not in (x.dtype, torch.float32) or out_weight.shape != weight.shape:
             raise ValueError(f"out_weight must be {tuple(weight.shape)} of {x.dtype} or torch.float32")
         _, _, g_worker, g_row = _matrix_of(out_weight, R, workers, "out_weight")
-        args = (R, M, N, K, dz.data_ptr(), code, dz_row, x.data_ptr(), x_row)
-        ptr, size, keep = _work(None, L.qs_linear_grad_weight_bytes(*args), "qs_linear_grad_weight_bytes", stream, device)
-        _done(L.qs_linear_grad_weight(*args, out_weight.data_ptr(), _TYPE[out_weight.dtype], g_worker, g_row, int(accumulate), ptr, size, _word(status),
-                                      _handle(stream, device)), "qs_linear_grad_weight")
+    if need_x:
+        if out is None:
+            out = _allocate(stream, x.shape, x.dtype, device)
+        _like(out, x.shape, x.dtype, "out")
+    L, bias = lib(), bias or out_bias is not None
+    dz = grad_out if act == QS_ACT_NONE else _allocate(stream, grad_out.shape, grad_out.dtype, device)
+    dz_row, x_row = _pitch(dz, N, "grad_out"), _pitch(x, K, "x")
+    to_x = (R, M, N, K, dz.data_ptr(), code, dz_row, weight.data_ptr(), _TYPE[weight.dtype], w_worker, w_row)
+    to_weight = (R, M, N, K, dz.data_ptr(), code, dz_row, x.data_ptr(), x_row)
+    # one scratch for the three calls, which follow one another
+    need = [L.qs_activation_grad_bytes(R, M, N) if bias else 0, L.qs_linear_grad_input_bytes(*to_x) if need_x else 0,
+            L.qs_linear_grad_weight_bytes(*to_weight) if need_weight else 0]
+    for n, what in zip(need, ("qs_activation_grad_bytes", "qs_linear_grad_input_bytes", "qs_linear_grad_weight_bytes")):
+        _done(n, what)
+    ptr, size, work = _work(work, max(need), "scratch", stream, device)
+    db = None
+    if bias or act != QS_ACT_NONE:
+        _, db = activation_grad(grad_out, pre, activation, out=dz if act != QS_ACT_NONE else None, bias=bias, out_bias=out_bias, workers=workers,
+                                accumulate=accumulate and out_bias is not None, work=work if bias else None, stream=stream)
+    word, handle = _word(status), _handle(stream, device)
+    if need_x:
+        _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), _pitch(out, K, "out"), ptr, size, word, handle), "qs_linear_grad_input")
+    if need_weight:
+        _done(L.qs_linear_grad_weight(*to_weight, out_weight.data_ptr(), _TYPE[out_weight.dtype], g_worker, g_row, int(accumulate), ptr, size, word, handle),
+              "qs_linear_grad_weight")
     return LinearGrad(out, out_weight, db, dz)
