@@ -207,12 +207,49 @@ __device__ __forceinline__ void finish_row(const Finish& f, float (&v)[32], cons
 // column per lane
 template <int ACT, class T>
 __device__ __forceinline__ void finish_columns(const Finish& f, int r, long long m0, long long n, int rows, const float* pass, int lane, int how) {
+    const long long row = r * f.M + m0;
+    T* out = static_cast<T*>(f.out) + r * f.out_worker + m0 * f.out_stride + n;
+    const T* res = static_cast<const T*>(f.res) + row * f.res_stride + n;
+    T* pre = static_cast<T*>(f.pre) + row * f.pre_stride + n;
     Columns<1> c;
     load_columns(f, r, n, c);
-#pragma unroll 8
-    for (int i = 0; i < rows; ++i) {
-        float v[1] = {pass[i * 32 + ((lane >> 2) ^ (i & 7)) * 4 + (lane & 3)]};
-        finish<ACT, 1, T>(f, r, m0 + i, n, v, c, how);
+#pragma unroll 1
+    for (int i = 0; i < rows; i += 8) {              // (eight rows under way together)
+        float v[8];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) v[p] = pass[(i + p) * 32 + ((lane >> 2) ^ p) * 4 + (lane & 3)];
+        if (how & ADD) {
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (i + p < rows) v[p] += to_float(out[p * f.out_stride]);
+        }
+        if (!(how & RAW)) {
+            if (f.a_scale) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    if (i + p < rows) v[p] = v[p] * f.a_scale[row + i + p] * c.scale[0];
+            }
+#pragma unroll
+            for (int p = 0; p < 8; ++p) v[p] += c.bias[0];
+            if (f.pre) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    if (i + p < rows) pre[p * f.pre_stride] = from_float<T>(v[p]);
+                pre += 8 * f.pre_stride;
+            }
+#pragma unroll
+            for (int p = 0; p < 8; ++p) v[p] = activate<ACT>(v[p]);
+            if (f.res) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    if (i + p < rows) v[p] += to_float(res[p * f.res_stride]);
+                res += 8 * f.res_stride;
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < 8; ++p)
+            if (i + p < rows) out[p * f.out_stride] = from_float<T>(v[p]);
+        out += 8 * f.out_stride;
     }
 }
 
@@ -730,6 +767,22 @@ __device__ __forceinline__ Eight eight_at(const void* p, long long row, int k, i
         }
         return e;
     }
+    if (BITS != 32 && k + (BITS == 8 ? 16 : 8) <= K) {
+        // off the boundary: the two aligned pieces that hold these 16 bytes, and what lies between (each piece holds some of the row)
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p) + (uintptr_t)(row + k) * (BITS / 8);
+        const uint4* q = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+        const uint4 a = q[0], b = at & 15 ? q[1] : a;
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        if (at & 8)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+        if (at & 4)
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.v[i] = __funnelshift_r(w[i], w[i + 1], (uint32_t)(at & 3) * 8);
+        return e;
+    }
     if (BITS == 32) {
         float v[8];
         floats_at<false>(v, static_cast<const float*>(p) + row, k, K);
@@ -794,7 +847,8 @@ __global__ void __launch_bounds__(256) few_kernel(const FewArgs a) {
         mma_16x8<WBITS, HALF>(d, w0.v[0], w1.v[0], w0.v[1], w1.v[1], x.v[0], x.v[1]);
         mma_16x8<WBITS, HALF>(d, w0.v[2], w1.v[2], w0.v[3], w1.v[3], x.v[2], x.v[3]);
     };
-    const auto stretch = [&](int k) {
+    // (the matrix instruction cuts its sums as the large one does: two stretches, then they are added up rounded)
+    const auto stretch = [&](float (&acc)[MT][NT][4], int k) {
         if constexpr (PARTS == 3) {
             Eight w[MT][2][3], x[NT][3];
 #pragma unroll
@@ -825,7 +879,17 @@ __global__ void __launch_bounds__(256) few_kernel(const FewArgs a) {
     };
     const int places = WBITS == 8 ? (a.K + 1) / 2 : a.K;     // pairs of 8 bits take the place of 16
 #pragma unroll(NT == 1 ? 2 : 1)
-    for (int k = warp * 64; k < places; k += 512) stretch(k + t * 8), stretch(k + 32 + t * 8);
+    for (int k = warp * 64; k < places; k += 512) {
+        float two[MT][NT][4] = {};
+        stretch(two, k + t * 8);
+        stretch(two, k + 32 + t * 8);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += two[i][j][e];
+    }
     // lane (g, t) holds rows g and g + 8 of the weights, rows 2 t and 2 t + 1 of x
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -845,6 +909,61 @@ __global__ void __launch_bounds__(256) few_kernel(const FewArgs a) {
         load_columns(a.f, r, n, cols);
         finish_any(a.f, r, m, n, v, cols, a.f.accumulate ? ADD : 0);
     }
+}
+
+// fp32 by few rows of fp32: ordinary multiply-adds keep up with memory.  Four rows of the weights per block, stretches of 128 along k
+// by its eight warps in turn, RM rows of x; their sums are joined in order.  (8 workers, one row, 6912 x 5696: 1.26 GB; by the matrix
+// instruction in three parts 367 us)
+template <int RM, bool VEC>
+__global__ void __launch_bounds__(256, RM <= 4 ? 3 : 2) few_floats_kernel(const FewArgs a) {
+    __shared__ float sums[8][4][RM];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = blockIdx.y;
+    const long long n0 = (long long)blockIdx.x * 4;
+    const float *w[4], *x[RM];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = static_cast<const float*>(a.w) + r * a.w_worker + min(n0 + i, a.f.N - 1) * a.w_stride;
+#pragma unroll
+    for (int j = 0; j < RM; ++j) x[j] = static_cast<const float*>(a.x) + r * a.x_worker + min((long long)j, a.f.M - 1) * a.x_stride;
+    float acc[4][RM] = {};
+#pragma unroll(RM <= 2 ? 2 : 1)
+    for (int k = warp * 128; k < a.K; k += 1024) {
+        float wv[4][4], xv[RM][4];
+        const auto four = [&](float (&v)[4], const float* p) {
+            const int at = k + lane * 4;
+            if (VEC && at + 4 <= a.K) return load_floats<4>(v, p + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = VEC ? at + e : k + 32 * e + lane;
+                v[e] = i < a.K ? p[i] : 0.0f;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) four(wv[i], w[i]);
+#pragma unroll
+        for (int j = 0; j < RM; ++j) four(xv[j], x[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < RM; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j] = __fmaf_rn(wv[i][e], xv[j][e], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < RM; ++j) {
+            const float s = warp_sum_f(acc[i][j]);
+            if (lane == 0) sums[warp][i][j] = s;
+        }
+    __syncthreads();
+    const int i = threadIdx.x & 3, j = threadIdx.x >> 2;
+    if (j >= RM || j >= a.f.M || n0 + i >= a.f.N) return;
+    float v[1] = {sums[0][i][j]};
+#pragma unroll
+    for (int q = 1; q < 8; ++q) v[0] += sums[q][i][j];
+    Columns<1> c;
+    load_columns(a.f, r, n0 + i, c);
+    finish_any(a.f, r, j, n0 + i, v, c, a.f.accumulate ? ADD : 0);
 }
 
 // ------------------------------------------------------------------ host
@@ -1029,6 +1148,14 @@ cudaError_t launch_few_as(const Product& p, const FewArgs& a, cudaStream_t st) {
 }
 cudaError_t launch_few(const Product& p, const FewArgs& a, bool vec, cudaStream_t st) {
     if (p.type == QS_E4M3) return vec ? launch_few_as<8, true, true, 1>(p, a, st) : launch_few_as<8, true, false, 1>(p, a, st);
+    if (p.type == QS_F32 && p.M <= 8) {
+        const dim3 grid((unsigned)((p.N + 3) / 4), (unsigned)p.R);
+        const auto kernel = p.M == 1   ? (vec ? few_floats_kernel<1, true> : few_floats_kernel<1, false>)
+                            : p.M == 2 ? (vec ? few_floats_kernel<2, true> : few_floats_kernel<2, false>)
+                            : p.M <= 4 ? (vec ? few_floats_kernel<4, true> : few_floats_kernel<4, false>)
+                                       : (vec ? few_floats_kernel<8, true> : few_floats_kernel<8, false>);
+        return launch(false, kernel, grid, 256, 0, st, a);
+    }
     if (p.type == QS_F32) return vec ? launch_few_as<32, false, true, 3>(p, a, st) : launch_few_as<32, false, false, 3>(p, a, st);
     const bool wide = p.b.type == QS_F32;
     if (p.type == QS_F16)
