@@ -55,23 +55,24 @@ __global__ void __launch_bounds__(256, 8) dropout_kernel(const DropArgs a) {
         x = *reinterpret_cast<const Pack<T, V>*>(p);
         if (RES) res = *reinterpret_cast<const Pack<T, V>*>(q);
     } else {                                         // the row's last elements
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            x.e[j] = at + j < a.D ? p[j] : from_float<T>(0.0f);
-            if (RES) res.e[j] = at + j < a.D ? q[j] : from_float<T>(0.0f);
-        }
+        x = pack_some<T, V>(p, a.D - at);
+        if (RES) res = pack_some<T, V>(q, a.D - at);
     }
     const uint32_t quad = (uint32_t)(((FLAT ? 0 : (row - w * a.per) * a.D) + at) >> 2);
     float v[V];
+    unpack(v, x);
 #pragma unroll
     for (int j = 0; j < V / 4; ++j) {
         const uint4 r = words_of(a, (uint32_t)w, quad + j);
         const uint32_t word[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[4 * j + k] = dropped(a, to_float(x.e[4 * j + k]), word[k]);
-            if (RES) v[4 * j + k] += to_float(res.e[4 * j + k]);
-        }
+        for (int k = 0; k < 4; ++k) v[4 * j + k] = dropped(a, v[4 * j + k], word[k]);
+    }
+    if (RES) {
+        float t[V];
+        unpack(t, res);
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] += t[j];
     }
     if (whole) {
         store_vec<V>(o, v);

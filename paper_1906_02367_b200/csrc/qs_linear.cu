@@ -155,51 +155,63 @@ __device__ __forceinline__ void add_raw(float (&v)[32], const Raw32<T>& q) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
     for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
-        const Pack<T, W> e = *reinterpret_cast<const Pack<T, W>*>(&q.a[k]);
+        float t[W];
+        unpack<T, W>(t, *reinterpret_cast<const Pack<T, W>*>(&q.a[k]));
 #pragma unroll
-        for (int i = 0; i < W; ++i) v[k * W + i] += to_float(e.e[i]);
+        for (int i = 0; i < W; ++i) v[k * W + i] += t[i];
     }
 }
+__device__ __forceinline__ void store_shared(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ float4 load_shared(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
 template <class T>
-__device__ __forceinline__ void put_row(uint8_t* tile, int lane, int first, const float (&v)[32]) {
+__device__ __forceinline__ void put_row(uint32_t row, int lane, int first, const float (&v)[32]) {
     constexpr int W = 16 / sizeof(T);
 #pragma unroll
     for (int k = 0; k < 2 * (int)sizeof(T); ++k) {
-        Pack<T, W> e;
-#pragma unroll
-        for (int i = 0; i < W; ++i) e.e[i] = from_float<T>(v[k * W + i]);
-        *reinterpret_cast<uint4*>(tile + lane * 128 + (((first + k) ^ (lane & 7)) << 4)) = *reinterpret_cast<uint4*>(&e);
+        const Pack<T, W> q = pack_of<T, W>(v + k * W);
+        store_shared(row + (((first + k) ^ (lane & 7)) << 4), *reinterpret_cast<const uint4*>(&q));
     }
+}
+// What there is to do, in one register: looking at the arguments for each of 32 columns cost more than the arithmetic
+enum { SCALED = 4, BIASED = 8, KEPT = 16, ADDED_RES = 32 };
+__device__ __forceinline__ int todo_of(const Finish& f) {
+    return (f.a_scale ? SCALED : 0) | (f.bias ? BIASED : 0) | (f.pre ? KEPT : 0) | (f.res ? ADDED_RES : 0);
 }
 // `first`: the row's pieces in front of these; bias, scale: of the 32 columns; left: columns that there are
 template <int ACT, class T>
-__device__ __forceinline__ void finish_row(const Finish& f, float (&v)[32], const T* out, const T* res, int left, float a_scale, const float* bias,
-                                           const float* scale, uint8_t* out_tile, uint8_t* pre_tile, int first, int lane, int how) {
+__device__ __forceinline__ void finish_row(int todo, float (&v)[32], const T* out, const T* res, int left, float a_scale, uint32_t bias, uint32_t scale,
+                                           uint32_t out_tile, uint32_t pre_tile, int first, int lane) {
     Raw32<T> q;
-    if (how & ADD) {
+    if (todo & ADD) {
         load_raw<T, true>(q, out, left);
         add_raw<T>(v, q);
     }
-    if (!(how & RAW)) {
-        if (res) load_raw<T, false>(q, res, left);
-        if (f.a_scale) {
+    if (!(todo & RAW)) {
+        if (todo & ADDED_RES) load_raw<T, false>(q, res, left);
+        if (todo & SCALED) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
-                const float4 s = *reinterpret_cast<const float4*>(scale + i);
+                const float4 s = load_shared(scale + 4 * i);
                 v[i] = v[i] * a_scale * s.x, v[i + 1] = v[i + 1] * a_scale * s.y, v[i + 2] = v[i + 2] * a_scale * s.z, v[i + 3] = v[i + 3] * a_scale * s.w;
             }
         }
-        if (f.bias) {
+        if (todo & BIASED) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
-                const float4 b = *reinterpret_cast<const float4*>(bias + i);
+                const float4 b = load_shared(bias + 4 * i);
                 v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
             }
         }
-        if (f.pre) put_row<T>(pre_tile, lane, first, v);
+        if (todo & KEPT) put_row<T>(pre_tile, lane, first, v);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = activate<ACT>(v[i]);
-        if (res) add_raw<T>(v, q);
+        if (todo & ADDED_RES) add_raw<T>(v, q);
     }
     put_row<T>(out_tile, lane, first, v);
 }
@@ -257,10 +269,26 @@ __device__ __forceinline__ void finish_columns(const Finish& f, int r, long long
 // Operands that the tensor maps cannot take as they lie (another type, rows off the 16-byte boundary) are laid out in the
 // workspace: fp32 rounded to the other operand's 16 bits, or cut into three bf16 parts x = x0 + x1 + x2, the first eight bits of what
 // the ones before left: 24 bits in all, exactly.
+// 16 bytes from any address, of which the first and the last are there: by the aligned pieces that hold them
+__device__ __forceinline__ uint4 bytes_at(uintptr_t at) {
+    const uint4* q = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+    const uint4 a = q[0];
+    if ((at & 15) == 0) return a;
+    const uint4 b = q[1];
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (at & 8)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (at & 4)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+    const uint32_t s = (uint32_t)(at & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], s), __funnelshift_r(w[1], w[2], s), __funnelshift_r(w[2], w[3], s), __funnelshift_r(w[3], w[4], s));
+}
 struct LayArgs {
     const void* src; int src_type; long long src_stride, src_worker;
     void* dst; int dst_type, planes; long long ld;   // (workers, planes, rows, ld)
-    long long rows, cols; int workers, vec;
+    long long rows, cols; int workers;
 };
 // the next eight bits of two numbers, cut off, as a pair of bf16; v keeps the rest (exactly)
 __device__ __forceinline__ uint32_t parts_of(float& v0, float& v1) {
@@ -279,29 +307,37 @@ struct LayBoth { LayArgs side[2]; };
 __global__ void __launch_bounds__(256) lay_kernel(const LayBoth both) {
     const LayArgs& a = both.side[blockIdx.z];
     if (blockIdx.y >= a.workers) return;
-    const int size = a.dst_type == QS_E4M3 ? 1 : 2;
-    const long long units = a.ld / 8, r = blockIdx.y, items = a.rows * units;
+    const int size = a.dst_type == QS_E4M3 ? 1 : 2, n = 16 / size, from_size = a.src_type == QS_F32 ? 4 : size;      // n elements a unit
+    const long long units = a.ld / n, r = blockIdx.y, items = a.rows * units;
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
-        const long long row = i / units, c = (i - row * units) * 8, from = r * a.src_worker + row * a.src_stride + c;
-        if (size == 1) {
-            Pack<uint8_t, 8> q;
+        const long long row = i / units, c = (i - row * units) * n, from = r * a.src_worker + row * a.src_stride + c;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(a.src) + (uintptr_t)from * from_size;
+        const bool whole = c + n <= a.cols;
+        if (from_size != 4) {                        // as they are
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (whole) {
+                q = bytes_at(at);
+            } else {
+                uint32_t w[4] = {};
+                const int left = (int)max(0ll, a.cols - c) * size;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q.e[j] = c + j < a.cols ? static_cast<const uint8_t*>(a.src)[from + j] : 0;
-            *reinterpret_cast<Pack<uint8_t, 8>*>(static_cast<uint8_t*>(a.dst) + (r * a.rows + row) * a.ld + c) = q;
-            continue;
-        }
-        if (a.src_type != QS_F32) {                  // 16 bits as they are
-            Pack<uint16_t, 8> q;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q.e[j] = c + j < a.cols ? static_cast<const uint16_t*>(a.src)[from + j] : 0;
-            *reinterpret_cast<Pack<uint16_t, 8>*>(static_cast<uint16_t*>(a.dst) + (r * a.rows + row) * a.ld + c) = q;
+                for (int b = 0; b < 16; ++b)
+                    if (b < left) w[b / 4] |= (uint32_t)reinterpret_cast<const uint8_t*>(at)[b] << (b % 4 * 8);
+                q = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.dst) + ((r * a.rows + row) * a.ld + c) * size) = q;
             continue;
         }
         float v[8];
-        if (a.vec && c + 8 <= a.cols) load_floats<8>(v, static_cast<const float*>(a.src) + from);
-        else
+        if (whole) {
+            const uint4 q0 = bytes_at(at), q1 = bytes_at(at + 16);
+            const uint32_t w[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+        } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = c + j < a.cols ? static_cast<const float*>(a.src)[from + j] : 0.0f;
+        }
         if (a.dst_type == QS_F16) {
             store_vec<8>(static_cast<__half*>(a.dst) + (r * a.rows + row) * a.ld + c, v);
         } else {
@@ -329,6 +365,7 @@ struct GemmArgs {
     long long M, N;
     int tiles_m, tiles_n, splits, units;             // units of work: workers x splits x tiles
     int k_blocks, k_step, pairs;                     // blocks of 128 bytes along k; pairs of parts
+    int per_split, more;                             // blocks along k of a split; the first `more` take one more
     int chunk;                                       // blocks along k that are summed by the matrix unit before they are added up
     int a_across, b_across;                          // operand lies across k
     int a_worker, b_worker;                          // 0: one operand for all workers
@@ -344,18 +381,19 @@ struct GemmArgs {
 struct Unit { int r, split, tm, tn, kb0, kb1; };      // blocks [kb0, kb1) along k of one tile
 __device__ __forceinline__ Unit unit_of(const GemmArgs& g, int u) {
     Unit t;
-    const int tiles = g.tiles_m * g.tiles_n;
-    const int rs = u / tiles;
-    int i = u - rs * tiles;
-    t.split = rs % g.splits;
-    t.r = rs / g.splits;
+    const unsigned tiles = g.tiles_m * g.tiles_n, n = g.tiles_n;
+    const unsigned rs = (unsigned)u / tiles;
+    unsigned i = (unsigned)u - rs * tiles;
+    t.r = rs, t.split = 0;
+    if (g.splits > 1) t.r = rs / (unsigned)g.splits, t.split = rs - t.r * g.splits;
     // bands of eight tile rows, so that the blocks at work share operands in the L2
-    const int band = i / (8 * g.tiles_n), rows = min(8, g.tiles_m - band * 8);
-    i -= band * 8 * g.tiles_n;
-    t.tn = i / rows;
+    const unsigned band = i / (8 * n), rows = min(8u, g.tiles_m - band * 8);
+    i -= band * 8 * n;
+    t.tn = rows == 8 ? i >> 3 : i / rows;
     t.tm = band * 8 + (i - t.tn * rows);
-    t.kb0 = (int)((long long)g.k_blocks * t.split / g.splits);
-    t.kb1 = (int)((long long)g.k_blocks * (t.split + 1) / g.splits);
+    // the first `more` splits take one block along k more than the others
+    t.kb0 = t.split * g.per_split + min(t.split, g.more);
+    t.kb1 = t.kb0 + g.per_split + (t.split < g.more);
     return t;
 }
 
@@ -503,7 +541,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         float *bias = small.bias + half * HALF, *scale = small.scale + half * HALF;
         const uint32_t leader[2] = {CG == 2 ? in_block(smem_addr(&acc_empty[0]), 0) : smem_addr(&acc_empty[0]),
                                     CG == 2 ? in_block(smem_addr(&acc_empty[1]), 0) : smem_addr(&acc_empty[1])};
+        const uint32_t bias_at = smem_addr(bias), scale_at = smem_addr(scale), row_at = smem_addr(pass) + lane * 128;
         const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (TURNS ? 0 : half * HALF);
+        const int has = todo_of(g.f), act = g.f.act, vec = g.f.vec, splits = g.splits, chunk = g.chunk;
         int n = 0, out_buf = 0, turn = 0;
         bool fine = limit != 0;
         for (int u = cluster; u < g.units; u += clusters) {
@@ -525,10 +565,13 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 }
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
             }
-            const float a_scale = g.f.a_scale && in ? g.f.a_scale[row] : 1.0f;
-            for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += g.chunk, ++n) {
+            const float a_scale = has & SCALED && in ? g.f.a_scale[row] : 1.0f;
+            const T* out_row = static_cast<const T*>(g.f.out) + t.r * g.f.out_worker + m * g.f.out_stride + n0;
+            const T* res_row = static_cast<const T*>(g.f.res) + row * g.f.res_stride + n0;
+            const int cols = (int)max(0ll, min((long long)HALF, g.N - n0)), rows = (int)max(0ll, min(32ll, g.M - m0));
+            for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += chunk, ++n) {
                 const bool more = g.f.accumulate || kb0 > t.kb0, added = more && g.l2_adds;
-                const int buf = n & 1, how = (more && !added ? ADD : 0) | (kb0 + g.chunk < t.kb1 || g.splits > 1 ? RAW : 0);
+                const int buf = n & 1, how = (more && !added ? ADD : 0) | (kb0 + chunk < t.kb1 || splits > 1 ? RAW : 0), todo = has | how;
                 if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, limit));
                 if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
                 tc_fence_after();
@@ -539,11 +582,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 }
 #pragma unroll 1
                 for (int c0 = 0; c0 < HALF; c0 += WIDE) {
-                    const long long n1 = n0 + c0;
-                    const bool some = m0 < g.M && n1 < g.N;
-                    uint8_t* tile = pass + (g.f.pre ? 0 : out_buf * 4096);
-                    if (some && g.f.vec) {           // the tile's last copy has been read
-                        if (g.f.pre) bulk_wait_read<0>();
+                    const bool some = rows > 0 && c0 < cols;
+                    uint8_t* tile = pass + (has & KEPT ? 0 : out_buf * 4096);
+                    if (some && vec) {               // the tile's last copy has been read
+                        if (has & KEPT) bulk_wait_read<0>();
                         else bulk_wait_read<1>();
                         __syncwarp();
                     }
@@ -554,50 +596,52 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         if (fine) {
                             tmem_load32(raw, from + buf * BN + c0 + c);
                             tmem_wait_load();
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) raw[i] = 0x7fffffff;
                         }
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = fine ? __uint_as_float(raw[i]) : quiet_nan();
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
                         if (c0 + c + 32 == HALF && fine) {           // the accumulator is free once its last columns are in registers
                             tc_fence_before();
                             __syncwarp();
                             if (lane == 0) mbar_arrive_at(leader[buf]);
                         }
                         if (!some) continue;
-                        if (g.f.vec) {
-                            const T* out = static_cast<const T*>(g.f.out) + t.r * g.f.out_worker + m * g.f.out_stride + n1 + c;
-                            const T* res = g.f.res ? static_cast<const T*>(g.f.res) + row * g.f.res_stride + n1 + c : nullptr;
-                            const int left = in ? (int)max(0ll, min(32ll, g.N - n1 - c)) : 0, first = c * (int)sizeof(T) / 16;
-                            switch (g.f.act) {
-                            case QS_ACT_RELU: finish_row<QS_ACT_RELU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
-                            case QS_ACT_SILU: finish_row<QS_ACT_SILU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
-                            case QS_ACT_GELU: finish_row<QS_ACT_GELU, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how); break;
-                            default: finish_row<QS_ACT_NONE, T>(g.f, v, out, res, left, a_scale, bias + c0 + c, scale + c0 + c, tile, pass + 4096, first, lane, how);
+                        const int at = c0 + c;
+                        if (vec) {
+                            const int left = in ? max(0, min(32, cols - at)) : 0, first = c * (int)sizeof(T) / 16;
+                            switch (act) {
+                            case QS_ACT_RELU: finish_row<QS_ACT_RELU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
+                            case QS_ACT_SILU: finish_row<QS_ACT_SILU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
+                            case QS_ACT_GELU: finish_row<QS_ACT_GELU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
+                            default: finish_row<QS_ACT_NONE, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane);
                             }
                         } else {
-                            float* turn = reinterpret_cast<float*>(pass);
+                            float* turned = reinterpret_cast<float*>(pass);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(turn + lane * 32 + (j ^ (lane & 7)) * 4) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                            for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(turned + lane * 32 + (j ^ (lane & 7)) * 4) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                             __syncwarp();
-                            const int rows = (int)min((long long)32, g.M - m0);
-                            const long long col = n1 + c + lane;
-                            if (col < g.N) {
-                                switch (g.f.act) {
-                                case QS_ACT_RELU: finish_columns<QS_ACT_RELU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
-                                case QS_ACT_SILU: finish_columns<QS_ACT_SILU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
-                                case QS_ACT_GELU: finish_columns<QS_ACT_GELU, T>(g.f, t.r, m0, col, rows, turn, lane, how); break;
-                                default: finish_columns<QS_ACT_NONE, T>(g.f, t.r, m0, col, rows, turn, lane, how);
+                            if (at + lane < cols) {
+                                const long long col = n0 + at + lane;
+                                switch (act) {
+                                case QS_ACT_RELU: finish_columns<QS_ACT_RELU, T>(g.f, t.r, m0, col, rows, turned, lane, how); break;
+                                case QS_ACT_SILU: finish_columns<QS_ACT_SILU, T>(g.f, t.r, m0, col, rows, turned, lane, how); break;
+                                case QS_ACT_GELU: finish_columns<QS_ACT_GELU, T>(g.f, t.r, m0, col, rows, turned, lane, how); break;
+                                default: finish_columns<QS_ACT_NONE, T>(g.f, t.r, m0, col, rows, turned, lane, how);
                                 }
                             }
                             __syncwarp();
                         }
                     }
-                    if (some && g.f.vec) {
+                    if (some && vec) {
                         fence_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            if (added) tile_add(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
-                            else tile_store(&map_out, smem_addr(tile), (int)n1, (int)m0, t.split, t.r);
-                            if (g.f.pre && !(how & RAW)) tile_store(&map_pre, smem_addr(pass + 4096), (int)n1, (int)m0, 0, t.r);
+                            const int n1 = (int)n0 + c0;
+                            if (added) tile_add(&map_out, smem_addr(tile), n1, (int)m0, t.split, t.r);
+                            else tile_store(&map_out, smem_addr(tile), n1, (int)m0, t.split, t.r);
+                            if (has & KEPT && !(how & RAW)) tile_store(&map_pre, smem_addr(pass + 4096), n1, (int)m0, 0, t.r);
                             bulk_commit();
                         }
                         out_buf ^= 1;
@@ -735,12 +779,7 @@ struct FewArgs {
 struct Eight { uint32_t v[4]; };                     // eight elements of 16 bits
 template <bool HALF>
 __device__ __forceinline__ uint32_t pair_of(float lo, float hi) {
-    if (HALF) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
+    return HALF ? pack_two<__half>(lo, hi) : pack_two<bf16>(lo, hi);
 }
 // Elements [k, k + 8) of a row (BITS 8: sixteen, [2 k, 2 k + 16)); those at K and beyond are zero.  BITS: of an element; VEC: rows on 16-byte
 // boundaries
@@ -768,19 +807,8 @@ __device__ __forceinline__ Eight eight_at(const void* p, long long row, int k, i
         return e;
     }
     if (BITS != 32 && k + (BITS == 8 ? 16 : 8) <= K) {
-        // off the boundary: the two aligned pieces that hold these 16 bytes, and what lies between (each piece holds some of the row)
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p) + (uintptr_t)(row + k) * (BITS / 8);
-        const uint4* q = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-        const uint4 a = q[0], b = at & 15 ? q[1] : a;
-        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-        if (at & 8)
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-        if (at & 4)
-#pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e.v[i] = __funnelshift_r(w[i], w[i + 1], (uint32_t)(at & 3) * 8);
+        const uint4 a = bytes_at(reinterpret_cast<uintptr_t>(p) + (uintptr_t)(row + k) * (BITS / 8));
+        e.v[0] = a.x, e.v[1] = a.y, e.v[2] = a.z, e.v[3] = a.w;
         return e;
     }
     if (BITS == 32) {
@@ -1094,7 +1122,6 @@ LayArgs lay_args(const Product& p, const Operand& o, void* dst, int dst_type, in
     a.workers = o.worker || p.R == 1 ? p.R : 1;
     a.src = o.p; a.src_type = o.type; a.src_stride = o.ld; a.src_worker = o.worker;
     a.dst = dst; a.dst_type = dst_type; a.planes = planes; a.ld = ld; a.rows = memory_rows(p, o); a.cols = memory_cols(p, o);
-    a.vec = o.type == QS_F32 && aligned_to(o.p, 16) && (a.rows == 1 || o.ld % 4 == 0) && (a.workers == 1 || o.worker % 4 == 0);
     return a;
 }
 cudaError_t lay_out(const LayBoth& both, int sides, cudaStream_t st) {
@@ -1220,6 +1247,8 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.k_step = 128 / size;
     g.k_blocks = (int)((p.K + g.k_step - 1) / g.k_step);
     g.pairs = q.planes == 3 ? 6 : 1;
+    g.per_split = g.k_blocks / q.splits;
+    g.more = g.k_blocks % q.splits;
     // (the sums so far lie in the result, so it has to hold fp32 and be nothing that is still to be read)
     g.chunk = f.type == QS_F32 && (q.splits > 1 || f.res != f.out) ? CHUNK_BLOCKS : g.k_blocks;
     g.eight = type == QS_E4M3;

@@ -137,8 +137,12 @@ __global__ void __launch_bounds__(WARP ? 128 : 512) norm_kernel(const NormArgs a
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (t + u * group < vecs) {
+                float v[V], r[V];
+                unpack(v, h[u]);
+                unpack(r, q[u]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) h[u].e[j] = from_float<T>(to_float(h[u].e[j]) + to_float(q[u].e[j]));
+                for (int j = 0; j < V; ++j) v[j] += r[j];
+                h[u] = pack_of<T, V>(v);
                 *reinterpret_cast<Pack<T, V>*>(hid + (t + u * group) * V) = h[u];
             }
     }
