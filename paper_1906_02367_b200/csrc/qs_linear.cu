@@ -405,9 +405,15 @@ struct Small {                                       // beside the ring and the 
 };
 template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return STAGES * stage_bytes<CG, BN>() + PASS_BYTES + (int)sizeof(Small); }
 
-// A tile of TILE_M CG x BN per cluster of CG blocks.  Copies (one thread per block) keep a ring of STAGES tiles of both
-// operands filling; one thread of the leading block issues the products into one of two accumulators; eight warps per
-// block take the other one out: they turn 32 x 32 sums through shared memory so that rows leave in whole sectors.
+// A tile of TILE_M CG x BN per cluster of CG blocks.  One warp per block keeps a ring of STAGES tiles of both operands filling; one
+// of the leading block issues the products into one of two accumulators; eight warps per block take the other one out, a row
+// per lane, finish it and leave it in tiles of shared memory that bulk copies take to the result (rows off the 16-byte boundary
+// are turned there and stored a column per lane).  Bound by the products for long sums: 516 of 512 cycles per slot in bf16 and in
+// e4m3 (8192 x 8192 x 8192: 732 us, 1503 TFLOP/s under the power limit; e4m3 371 us, 2960); for short ones by the finishing warps' instructions
+// (8 x 4096 x 4096 x 1024: 198 us, 223 with silu, 246 with the saved values too).
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit) {
+    return __all_sync(~0u, mbar_wait_asleep(bar, parity, limit));                // (the lanes give up together)
+}
 template <int CG, int BN, class T>
 __global__ void __launch_bounds__(GEMM_THREADS, 1)
 gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
@@ -453,7 +459,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 for (int p = 0; p < g.pairs && fine; ++p) {
                     const int pa = part_a(g.pairs, p), pb = part_b(g.pairs, p);
                     for (int kb = kb0; kb < kb1; ++kb) {
-                        if (!(fine = mbar_wait_asleep(&empty[slot], phase, limit))) break;
+                        if (!(fine = warp_wait(&empty[slot], phase, limit))) break;
                         if (me) {
                             const int k0 = kb * g.k_step;
                             if (rank == 0) mbar_expect(&full[slot], STAGE * CG);
@@ -481,12 +487,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if (fine) {
             // the last products' arrivals, which may come from the other block, are in before this one ends
             for (int i = 0; i < STAGES; ++i) {
-                if (count >= STAGES || slot < count) mbar_wait_asleep(&empty[slot], phase, limit);
+                if (count >= STAGES || slot < count) warp_wait(&empty[slot], phase, limit);
                 if (++slot == STAGES) slot = 0, phase ^= 1;
             }
         } else if (count > 0 && rank == 0) {
             // after a wait that ran out: the copies under way (of both blocks: they count here) land before the memory is given up
-            for (int i = max(0, count - STAGES); i < count; ++i) mbar_wait_asleep(&full[i % STAGES], (i / STAGES) & 1, WAIT_LIMIT_NS);
+            for (int i = max(0, count - STAGES); i < count; ++i) warp_wait(&full[i % STAGES], (i / STAGES) & 1, WAIT_LIMIT_NS);
         } else if (count > 0) {
             // (the second block's count at the first: it cannot look, and gives them far more time than a copy takes)
             const unsigned long long t0 = global_ns();
@@ -504,11 +510,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 const Unit t = unit_of(g, u);
                 for (int kb0 = t.kb0; kb0 < t.kb1 && fine; kb0 += g.chunk, ++n) {
                     const uint32_t d = tmem + (n & 1) * BN;
-                    if (!(fine = mbar_wait_asleep(&acc_empty[n & 1], ((n >> 1) & 1) ^ 1, limit))) break;
+                    if (!(fine = warp_wait(&acc_empty[n & 1], ((n >> 1) & 1) ^ 1, limit))) break;
                     tc_fence_after();
                     const int todo = (min(t.kb1, kb0 + g.chunk) - kb0) * g.pairs;
                     for (int it = 0; it < todo; ++it) {
-                        if (!(fine = mbar_wait_asleep(&full[slot], phase, limit))) break;
+                        if (!(fine = warp_wait(&full[slot], phase, limit))) break;
                         tc_fence_after();
                         if (me) {
                             const uint64_t da = first + slot * (STAGE >> 4), db = da + (A_BYTES >> 4);
@@ -532,7 +538,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             // the products under way are done before their tensor memory is given up
             if (me) mma_commit_here<CG>(&small.drained);
             __syncwarp();
-            mbar_wait_asleep(&small.drained, 0, WAIT_LIMIT_NS);
+            warp_wait(&small.drained, 0, WAIT_LIMIT_NS);
         }
     } else if (warp >= 4) {
         constexpr int HALF = TURNS ? BN : BN / 2, WIDE = 128 / sizeof(T);    // columns of a warp; of a tile on its way out
@@ -572,7 +578,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             for (int kb0 = t.kb0; kb0 < t.kb1; kb0 += chunk, ++n) {
                 const bool more = g.f.accumulate || kb0 > t.kb0, added = more && g.l2_adds;
                 const int buf = n & 1, how = (more && !added ? ADD : 0) | (kb0 + chunk < t.kb1 || splits > 1 ? RAW : 0), todo = has | how;
-                if (fine) fine = __all_sync(~0u, mbar_wait_asleep(&acc_full[buf], (n >> 1) & 1, limit));
+                if (fine) fine = warp_wait(&acc_full[buf], (n >> 1) & 1, limit);
                 if (!fine && lane == 0) flag_status(g.status, QS_TIMEOUT);
                 tc_fence_after();
                 // sums of the chunks before have arrived where they are read again or added to, in this order
@@ -611,12 +617,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         const int at = c0 + c;
                         if (vec) {
                             const int left = in ? max(0, min(32, cols - at)) : 0, first = c * (int)sizeof(T) / 16;
+                            const uint32_t to = row_at + (has & KEPT ? 0 : out_buf * 4096);
+#define QS_FINISH(ACT) finish_row<ACT, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, to, row_at + 4096, first, lane)
                             switch (act) {
-                            case QS_ACT_RELU: finish_row<QS_ACT_RELU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
-                            case QS_ACT_SILU: finish_row<QS_ACT_SILU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
-                            case QS_ACT_GELU: finish_row<QS_ACT_GELU, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane); break;
-                            default: finish_row<QS_ACT_NONE, T>(todo, v, out_row + at, res_row + at, left, a_scale, bias_at + 4 * at, scale_at + 4 * at, row_at + (has & KEPT ? 0 : out_buf * 4096), row_at + 4096, first, lane);
+                            case QS_ACT_RELU: QS_FINISH(QS_ACT_RELU); break;
+                            case QS_ACT_SILU: QS_FINISH(QS_ACT_SILU); break;
+                            case QS_ACT_GELU: QS_FINISH(QS_ACT_GELU); break;
+                            default: QS_FINISH(QS_ACT_NONE);
                             }
+#undef QS_FINISH
                         } else {
                             float* turned = reinterpret_cast<float*>(pass);
 #pragma unroll
@@ -1033,12 +1042,11 @@ Plan plan_of(const Product& p, int sms) {
     q.planes = p.type == QS_F32 ? 3 : 1;
     q.splits = 1;
     const double work = 2.0 * p.R * p.M * p.N * p.K;
+    q.few = p.M <= FEW && !p.a.across && !p.b.across;
     // (us, plain and on the matrix unit: fp32, which is laid out first, 64 x 64 x 64 4.7, 10.5; 33 x 200 x 300 12.6, 16.5; 509 x 1000 x 257
     // 34, 20.  bf16 64 x 64 x 64 5.7, 5.5; 33 x 200 x 300 24, 9)
-    q.small = p.K == 0 || work < (p.type == QS_F32 ? 5e6 : 5e5);
-    if (q.small) return q;
-    q.few = p.M <= FEW && !p.a.across && !p.b.across;
-    if (q.few) return q;
+    q.small = !q.few && (p.K == 0 || work < (p.type == QS_F32 ? 5e6 : 5e5));
+    if (q.few || q.small) return q;
     const int size = p.type == QS_E4M3 ? 1 : 2;
     q.lay_a = !taken_as_it_lies(p, p.a);
     q.lay_b = !taken_as_it_lies(p, p.b);

@@ -149,6 +149,29 @@ def test_long_sums_keep_32_bits(L, M, N, K):
     assert float(((L.linear(f, v).out.double() - z) / z).abs().max()) < 64 * E + (K / 1024 + 2) * E + 2.0 ** -21
 
 
+@pytest.mark.parametrize("M,N,K", [(2000, 520, 3000), (150, 264, 2500), (2000, 519, 1100)])
+def test_fp32_results_in_several_sums_with_all_that_follows(L, M, N, K):
+    x, w, b, res = rand((M, K), BF16, 1), rand((N, K), BF16, 2, K ** -0.5), rand((N,), F32, 3), rand((M, N), F32, 4)
+    r = L.linear(x, w, b, activation="gelu", residual=res, save=True, dtype=F32)
+    z, size = ref.product(x, w)
+    z, slack = z + b.double(), (K + 8) * E * size + 2 * E * b.double().abs()
+    near(r.pre, z, slack, F32)
+    near(r.out, ref.activate(z, "gelu") + res.double(), 1.13 * slack + 8 * E * (z.abs() + 1) + 2 * E * res.double().abs(), F32)
+    L.linear(x, w, b, activation="gelu", residual=res, out=res)
+    near(res, r.out, 2 * (1.13 * slack + 8 * E * (z.abs() + 1) + 2 * E * r.out.double().abs()), F32)
+
+
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F16, F16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("M,N,K", [(3000, 264, 520), (100, 1300, 1096), (300, 65, 130), (40, 8, 8)])
+def test_weight_gradients_added_to_what_is_there(L, dtype, out, M, N, K):
+    g, x, held = rand((M, N), dtype, 1, 0.1), rand((M, K), dtype, 2), rand((N, K), out, 3)
+    w = torch.zeros((N, K), device="cuda", dtype=dtype)
+    want, size = ref.product(g.t(), x.t())
+    got = held.clone()
+    L.linear_grad(g, x, w, need_x=False, out_weight=got, accumulate=True)
+    near(got, want + held.double(), ((M + 8) * E * 1.05 + 4 * E) * size + 2 * E * held.double().abs(), out)
+
+
 def test_a_callers_workspace(L):
     from paper_1906_02367_b200.binding import QS_CAPACITY, QsError
     x, w = rand((300, 257), F32, 1), rand((200, 257), F32, 2)
