@@ -6,7 +6,7 @@
 // layer << 16 | round's bits 32 to 39 << 8 | 2), word = out[element & 3]; 2 is this operator's stream beside those of
 // the sparsifier and the quantizer.  A row is read and written once by vectors of 16 bytes, each with one or two draws of four
 // words.  In fp32 memory sets the pace (6.7 TB/s); in 16 bits the generator does as much: ten rounds are about 20 of the 25
-// instructions per element, and the multipliers and the logic units are each about half busy (4.6 to 5.0 TB/s).
+// instructions per element, and the multipliers and the logic units are each about half busy (5.0 to 5.3 TB/s).
 #include <algorithm>
 
 #include "qs_vec.cuh"
@@ -39,8 +39,8 @@ __device__ __forceinline__ float dropped(const DropArgs& a, float x, uint32_t wo
 
 // Rows whose elements come in vectors of V, the first of each at a multiple of four elements of its worker
 // FLAT: one row.  A vector per thread: what is in flight comes from many resident warps, and 32 registers let all of them in (8192 x
-// 4096 in bf16 with a residual: 44.0 us with eight blocks an SM, 46.2 with six; two vectors a thread 51; blocks that stay, with the
-// next vector on its way, 75)
+// 4096 in bf16 with a residual, words taken apart by elements: 44.0 us with eight blocks an SM, 46.2 with six; two vectors a thread 51;
+// blocks that stay, with the next vector on its way, 75.  By pairs 41)
 template <class T, int V, bool RES, bool FLAT>
 __global__ void __launch_bounds__(256, 8) dropout_kernel(const DropArgs a) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;

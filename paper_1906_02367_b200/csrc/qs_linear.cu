@@ -35,7 +35,7 @@ __device__ __forceinline__ float rcp(float x) {
 }
 __device__ __forceinline__ float logistic(float z) { return rcp(1.0f + ex2(-LOG2E * z)); }
 // Phi(z) = erfc(-z / sqrt 2) / 2 by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (error below
-// 1.5e-7 in erf), and e^(-z^2 / 2) on the way.  (erff has two branches: 8192 x 16384 results in bf16 take 30 us longer with it)
+// 1.5e-7 in erf), and e^(-z^2 / 2) on the way.  (erff has two branches; with it a 16-slot sum's finishing took three times silu's)
 struct Normal { float phi, density; };
 __device__ __forceinline__ Normal normal(float z) {
     const float x = fabsf(z) * 0.70710678f, t = rcp(__fmaf_rn(0.3275911f, x, 1.0f)), e = ex2(-LOG2E * x * x);
@@ -356,7 +356,7 @@ constexpr int STAGES = 5;
 constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
 // The matrix unit cuts what lies below 2^-24 of a sum at every addition, always towards zero: 8e-10 of the result per element
 // summed.  Results in fp32 are therefore added up, rounded to nearest, from sums over this many blocks of 128 bytes (1024 elements
-// of 16 bits: 8e-7).  (Weights' gradient of 8 x 4096 rows, 4096 x 1024: 205 us with 64 blocks, 3e-6 off; 218 with 32; 243 with 16)
+// of 16 bits: 8e-7).  (Weights' gradient of 8 x 4096 rows, 4096 x 1024: 205 us with 64 blocks, 3e-6 off; 218 with 32; 240 with 16)
 constexpr int CHUNK_BLOCKS = 16;
 constexpr int PASS_BYTES = 8 * 2 * 4096;             // two tiles of 32 rows of 128 bytes on their way out, per finishing warp
 
@@ -409,8 +409,8 @@ template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return
 // of the leading block issues the products into one of two accumulators; eight warps per block take the other one out, a row
 // per lane, finish it and leave it in tiles of shared memory that bulk copies take to the result (rows off the 16-byte boundary
 // are turned there and stored a column per lane).  Bound by the products for long sums: 516 of 512 cycles per slot in bf16 and in
-// e4m3 (8192 x 8192 x 8192: 732 us, 1503 TFLOP/s under the power limit; e4m3 371 us, 2960); for short ones by the finishing warps' instructions
-// (8 x 4096 x 4096 x 1024: 198 us, 223 with silu, 246 with the saved values too).
+// e4m3 (8192 x 8192 x 8192: 725 us, 1516 TFLOP/s under the power limit; e4m3 365 us, 3014); for short ones by the finishing warps' instructions
+// (8 x 4096 x 4096 x 1024: 203 us, 227 with silu, 248 with the saved values too).
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit) {
     return __all_sync(~0u, mbar_wait_asleep(bar, parity, limit));                // (the lanes give up together)
 }
