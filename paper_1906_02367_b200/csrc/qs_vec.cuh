@@ -120,7 +120,5 @@ inline int64_t span(int64_t rows, int64_t stride, int64_t width, int size) { ret
 inline bool beside(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t rows, int64_t width, int size) {
     return !in || !out || rows <= 0 || width <= 0 || !overlap(in, in_stride, out, out_stride, rows, width, size);
 }
-// a pitch of one row says nothing: one that keeps wide accesses
-inline int64_t pitch_of(int64_t rows, int64_t stride, int64_t width) { return rows > 1 ? stride : (width + 15) / 16 * 16; }
 
 }  // namespace qs

@@ -401,6 +401,24 @@ def test_linear_grad_of_workers_into_a_gradient_batch(L):
     assert bool((dw == 0).all()) and bool((db == 0).all()) and r.x.shape == (R, 0, K) and bool((grad[:, :shift] == 5).all())
 
 
+@pytest.mark.parametrize("activation", [None, "silu", "gelu"])
+def test_linear_gradients_against_differences(L, activation):
+    M, N, K, step = 6, 9, 40, 1e-5
+    x, w, b, g = rand((M, K), F32, 1), rand((N, K), F32, 2, K ** -0.5), rand((N,), F32, 3), rand((M, N), F32, 4)
+    y = L.linear(x, w, b, activation=activation, save=True)
+    got = L.linear_grad(g, x, w, y.pre, activation, bias=True)
+    loss = lambda x_, w_, b_: float((ref.activate(x_ @ w_.t() + b_, activation) * g.double()).sum())  # noqa: E731
+    at = [t.double() for t in (x, w, b)]
+    for which, grad in ((0, got.x), (1, got.weight), (2, got.bias)):
+        for i in range(0, grad.numel(), 7):
+            d = torch.zeros(grad.numel(), device="cuda", dtype=torch.float64)
+            d[i] = step
+            up, down = list(at), list(at)
+            up[which], down[which] = at[which] + d.view(at[which].shape), at[which] - d.view(at[which].shape)
+            # (third derivatives below 10, step^2 / 6 of them; fp32 sums of up to 40 terms of size 1)
+            assert abs((loss(*up) - loss(*down)) / (2 * step) - float(grad.view(-1)[i])) < 2e-5
+
+
 def test_linear_of_no_rows(L):
     assert L.linear(torch.zeros((0, 64), device="cuda"), torch.zeros((8, 64), device="cuda")).out.shape == (0, 8)
 
