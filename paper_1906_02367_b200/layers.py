@@ -246,6 +246,8 @@ def linear(x, weight, bias=None, activation=None, residual=None, x_scale=None, w
             raise ValueError("8-bit operands need x_scale and weight_scale")
         _counted(x_scale, R * M, "x_scale")
         _counted(weight_scale, (R if workers else 1) * N, "weight_scale")
+        if workers and R > 1 and w_worker == 0:
+            raise ValueError("8-bit weights that all workers share are (N, K), with one scale per row")
     elif x_scale is not None or weight_scale is not None:
         raise ValueError("scales belong to 8-bit operands")
     bias_step = _vector_of(bias, R, N, workers, "bias")

@@ -83,6 +83,7 @@ REFUSED = {
     "8 bits without scales": lambda: L.linear(X.to(E4M3), W.to(E4M3)),
     "8 bits with fp32 weights": lambda: L.linear(X.to(E4M3), W, x_scale=torch.zeros(4), weight_scale=torch.zeros(5)),
     "short scales": lambda: L.linear(X.to(E4M3), W.to(E4M3), x_scale=torch.zeros(3), weight_scale=torch.zeros(5)),
+    "one 8-bit weight as many": lambda: L.linear(torch.zeros(3, 4, 6).to(E4M3), W.to(E4M3).expand(3, 5, 6), x_scale=torch.zeros(3, 4), weight_scale=torch.zeros(3, 5)),
     "status": lambda: L.linear(X, W, status=torch.zeros(1, dtype=torch.int64)),
     "workspace in pieces": lambda: L.linear(X, W, work=torch.zeros(8192, dtype=torch.uint8)[::2]),
     "gradient of a product of another shape": lambda: L.linear_grad(torch.zeros(4, 6), X, W),
