@@ -78,6 +78,22 @@ def _matrix_of(t, R, workers, what):
     return N, K, (t.stride(0) if workers and R > 1 else 0), (t.stride(-2) if N > 1 else max(t.stride(-2), K))
 
 
+def _meet(a, b, width=None):
+    """Whether the memory of two tensors (None: no) meets: what lies between their first and last elements, or with a width of
+    their rows those rows' columns."""
+    if a is None or b is None or not a.numel() or not b.numel():
+        return False
+    size, other = a.element_size(), b.element_size()
+    at, to = a.data_ptr(), b.data_ptr()
+    end = [p + s * (1 + sum((n - 1) * d for n, d in zip(t.shape, t.stride()))) for t, p, s in ((a, at, size), (b, to, other))]
+    if end[0] <= to or end[1] <= at:
+        return False
+    if width is None or size != other:
+        return True
+    row = _pitch(a, width, "")
+    return row != _pitch(b, width, "") or not width * size <= (to - at) % (row * size) <= (row - width) * size
+
+
 def _work(work, need, what, stream, device):
     """(pointer, bytes) of the scratch: the caller's, or new."""
     _done(need, what)
@@ -309,7 +325,7 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
     qs_linear_grad_weight); the residual's is grad_out itself.  pre: what linear saved (not needed without an activation).
     The gradient in front of the activation is rounded to grad_out's type, which is x's.  The weight's gradient is of `dtype`
     (fp32 or x's type), the bias's fp32; out_weight and out_bias may be stretches of a gradient batch, and accumulate adds
-    to them.  Returns LinearGrad(x, weight, bias, pre): None for what was not asked for; pre is the gradient in front of the
+    to them.  out may take x's place, or out_weight weight's, not both.  Returns LinearGrad(x, weight, bias, pre): None for what was not asked for; pre is the gradient in front of the
     activation."""
     device = _on(x, weight, grad_out, pre, out, out_weight, out_bias, work, status)
     workers, R, M, N, K, w_worker, w_row = _operands(x, weight)
@@ -327,10 +343,15 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
         elif out_weight.dtype not in (x.dtype, torch.float32) or out_weight.shape != weight.shape:
             raise ValueError(f"out_weight must be {tuple(weight.shape)} of {x.dtype} or torch.float32")
         _, _, g_worker, g_row = _matrix_of(out_weight, R, workers, "out_weight")
+    weight_first = False
     if need_x:
         if out is None:
             out = _allocate(stream, x.shape, x.dtype, device)
-        _like(out, x.shape, x.dtype, "out")
+        else:
+            _like(out, x.shape, x.dtype, "out")
+            weight_first = need_weight and _meet(out, x, K)
+    if weight_first and _meet(out_weight, weight):
+        raise ValueError("out in x's place and out_weight in weight's: each gradient needs what the other would be written over")
     L, bias = lib(), bias or out_bias is not None
     dz = grad_out if act == QS_ACT_NONE else _allocate(stream, grad_out.shape, grad_out.dtype, device)
     dz_row, x_row = _pitch(dz, N, "grad_out"), _pitch(x, K, "x")
@@ -347,9 +368,11 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
         _, db = activation_grad(grad_out, pre, activation, out=dz if act != QS_ACT_NONE else None, bias=bias, out_bias=out_bias, workers=workers,
                                 accumulate=accumulate and out_bias is not None, work=work if bias else None, stream=stream)
     word, handle = _word(status), _handle(stream, device)
-    if need_x:
-        _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), _pitch(out, K, "out"), ptr, size, word, handle), "qs_linear_grad_input")
-    if need_weight:
-        _done(L.qs_linear_grad_weight(*to_weight, out_weight.data_ptr(), _TYPE[out_weight.dtype], g_worker, g_row, int(accumulate), ptr, size, word, handle),
-              "qs_linear_grad_weight")
+    # each reads what the other may be written over: the weight's comes first where out takes x's place
+    for product in ("weight", "x") if weight_first else ("x", "weight"):
+        if product == "x" and need_x:
+            _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), _pitch(out, K, "out"), ptr, size, word, handle), "qs_linear_grad_input")
+        if product == "weight" and need_weight:
+            _done(L.qs_linear_grad_weight(*to_weight, out_weight.data_ptr(), _TYPE[out_weight.dtype], g_worker, g_row, int(accumulate), ptr, size, word,
+                                          handle), "qs_linear_grad_weight")
     return LinearGrad(out, out_weight, db, dz)

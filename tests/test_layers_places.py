@@ -1,0 +1,51 @@
+"""Results in their inputs' places, on the host with a stand-in for the library: the order of a call's parts, and refusals that come
+before anything is enqueued."""
+import pytest
+import torch
+
+from paper_1906_02367_b200 import layers as L
+from test_layers_arguments import calls  # noqa: F401
+
+
+def names(calls):  # noqa: F811
+    return [n for n, _ in calls if not n.endswith("_bytes")]
+
+
+def test_the_weights_gradient_reads_x_before_its_place_is_taken(calls):  # noqa: F811
+    x, w, g = torch.zeros(4, 6), torch.zeros(5, 6), torch.zeros(4, 5)
+    order = ["qs_linear_grad_weight", "qs_linear_grad_input"]
+    r = L.linear_grad(g, x, w, out=x)
+    assert names(calls) == order and r.x is x
+    calls.clear()
+    L.linear_grad(g, x, w, out=x.view(2, 2, 6).view(4, 6), bias=True)
+    assert names(calls) == ["qs_activation_grad"] + order
+    calls.clear()
+    L.linear_grad(g, x, w, out=x, need_weight=False)
+    assert names(calls) == order[1:]
+    # the weight's place is free once the input's gradient is there
+    calls.clear()
+    L.linear_grad(g, x, w, out_weight=w)
+    L.linear_grad(g, x, w)
+    assert names(calls) == order[::-1] * 2
+    # other columns of the same rows are no place of x's; one that reaches into them is
+    wide = torch.zeros(4, 20)
+    calls.clear()
+    L.linear_grad(g, wide[:, :6], w, out=wide[:, 6:12])
+    assert names(calls) == order[::-1]
+    calls.clear()
+    L.linear_grad(g, wide[:, :6], w, out=wide[:, 5:11])
+    assert names(calls) == order
+    long = torch.zeros(60)
+    calls.clear()
+    L.linear_grad(g, long[:24].view(4, 6), w, out=long[24:48].view(4, 6))
+    assert names(calls) == order[::-1]
+    calls.clear()
+    L.linear_grad(g, long[:24].view(4, 6), w, out=long[18:42].view(4, 6))
+    assert names(calls) == order
+
+
+def test_both_places_at_once_are_refused(calls):  # noqa: F811
+    x, w, g = torch.zeros(4, 6), torch.zeros(5, 6), torch.zeros(4, 5)
+    with pytest.raises(ValueError):
+        L.linear_grad(g, x, w, out=x, out_weight=w, bias=True)
+    assert names(calls) == []
