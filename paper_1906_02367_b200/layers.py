@@ -110,7 +110,8 @@ def _work(work, need, what, stream, device):
 def rms_norm(x, weight=None, residual=None, eps=1e-6, quantize=False, out=None, hidden=None, scale=None, rstd=None, stream=None):
     """h = x + residual, h / sqrt(mean h^2 + eps) * weight (qs_rms_norm).  x (.., D); weight (D), or (R, D) for x (R, .., D), in
     fp32 or x's type.  quantize: the result in 8 bits (torch.float8_e4m3fn) with a scale per row.  Returns RmsNorm(out, hidden,
-    rstd, scale): hidden is h, in x's type (x itself without a residual); scale is None unless quantize.  rstd False: not wanted."""
+    rstd, scale): hidden is h, in x's type (x itself without a residual, None where out has taken x's place); scale is None unless
+    quantize.  rstd False: not wanted."""
     device = _on(x, weight, residual, out, hidden, scale, rstd if isinstance(rstd, torch.Tensor) else None)
     workers = weight is not None and weight.dim() == 2
     R, N, D = _activations(x, workers, "x")
@@ -129,11 +130,13 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, quantize=False, out=None, 
         hidden = _allocate(stream, shape, x.dtype, device)
     else:
         _like(hidden, shape, x.dtype, "hidden")
-    out_type = E4M3 if quantize else x.dtype
+    out_type, kept = E4M3 if quantize else x.dtype, x if residual is None else hidden
     if out is None:
         out = _allocate(stream, shape, out_type, device)
     else:
         _like(out, shape, out_type, "out")
+        if residual is None and _meet(out, x, D):
+            kept = None
     if quantize:
         if scale is None:
             scale = _allocate(stream, shape[:-1], torch.float32, device)
@@ -149,7 +152,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, quantize=False, out=None, 
     _done(lib().qs_rms_norm(R, N, D, x.data_ptr(), code, _pitch(x, D, "x"), _ptr(residual), _pitch(residual, D, "residual"), _ptr(weight),
                             code if weight is None else _TYPE[weight.dtype], w_step, eps, _ptr(hidden), _pitch(hidden, D, "hidden"), out.data_ptr(),
                             _ALL[out_type], _pitch(out, D, "out"), _ptr(scale), _ptr(rstd), _handle(stream, device)), "qs_rms_norm")
-    return RmsNorm(out, x if residual is None else hidden, rstd, scale)
+    return RmsNorm(out, kept, rstd, scale)
 
 
 def quantize(x, out=None, scale=None, stream=None):
@@ -173,6 +176,8 @@ def rms_norm_grad(grad_out, hidden, rstd, weight=None, grad_hidden=None, out=Non
     """Gradient of rms_norm (qs_rms_norm_grad) from its hidden and rstd: with respect to hidden (so to x and to residual;
     grad_hidden, what arrives by the residual stream, is added), and to the weight, fp32 (out_weight may be a stretch of
     the rows of a gradient batch; accumulate adds to it).  Returns RmsNormGrad(hidden, weight); weight None: none."""
+    if hidden is None:
+        raise ValueError("hidden is needed: a norm's result that took x's place left none")
     device = _on(hidden, grad_out, rstd, weight, grad_hidden, out, out_weight, work)
     workers = weight is not None and weight.dim() == 2
     R, N, D = _activations(hidden, workers, "hidden")

@@ -41,3 +41,20 @@ def test_gradient_of_x_in_its_place(L, dtype, R, M, N, K, activation):
     over = w.clone()
     got = L.linear_grad(g, x, over, z, activation, out_weight=over)
     assert torch.equal(over, want.weight) and torch.equal(got.x, want.x)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,width", [(3, 64), (9, 257), (2, 20000)])
+def test_norm_in_its_inputs_place(L, dtype, rows, width):
+    """Without a residual h is x itself: there is no hidden to hand out once the result lies there."""
+    x, w = rand((rows, width), dtype, 1, 2.0), rand((width,), F32, 2, 0.2, 1.0)
+    want = L.rms_norm(x, w)
+    assert want.hidden is x
+    place = x.clone()
+    r = L.rms_norm(place, w, out=place)
+    assert r.out is place and torch.equal(place, want.out) and torch.equal(r.rstd, want.rstd)
+    assert r.hidden is None
+    place = x.clone()
+    assert L.rms_norm(place, w, out=place.view(rows, width)).hidden is None
+    with pytest.raises((ValueError, AttributeError)):
+        L.rms_norm_grad(x, r.hidden, r.rstd, w)

@@ -49,3 +49,15 @@ def test_both_places_at_once_are_refused(calls):  # noqa: F811
     with pytest.raises(ValueError):
         L.linear_grad(g, x, w, out=x, out_weight=w, bias=True)
     assert names(calls) == []
+
+
+def test_a_norm_in_its_inputs_place_hands_out_no_hidden(calls):  # noqa: F811
+    x, w = torch.zeros(4, 6), torch.zeros(6)
+    assert L.rms_norm(x, w).hidden is x
+    assert L.rms_norm(x, w, out=x).hidden is None and L.rms_norm(x, w, out=x.view(4, 6)).hidden is None
+    res = torch.zeros(4, 6)
+    assert L.rms_norm(x, w, res, hidden=res, out=x).hidden is res and L.rms_norm(x, w, res, out=x).hidden is not None
+    wide = torch.zeros(4, 20)
+    assert L.rms_norm(wide[:, :6], w, out=wide[:, 6:12]).hidden is not None
+    with pytest.raises(ValueError):
+        L.rms_norm_grad(x, None, torch.zeros(4), w)
