@@ -10,7 +10,7 @@ from collections import namedtuple
 
 import torch
 
-from .binding import QS_ACT_GELU, QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU, QS_E4M3, lib
+from .binding import QS_ACT_GELU, QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU, QS_CAPACITY, QS_E4M3, QsError, lib
 from .lm import _TYPE, _allocate, _done, _handle, _on, _ptr, _rows, _type, _word
 
 RmsNorm = namedtuple("RmsNorm", "out hidden rstd scale")
@@ -38,7 +38,14 @@ def _like(t, shape, dtype, what):
 
 def _pitch(t, D, what):
     """Elements between the rows of D of a tensor (None: 0)."""
-    return 0 if t is None else D if t.is_contiguous() else _rows(t, what)
+    if t is None:
+        return 0
+    if t.is_contiguous():
+        return D
+    row = _rows(t, what)
+    if row < D:
+        raise ValueError(f"{what}: rows must not share memory")
+    return row
 
 
 def _counted(t, n, what):
@@ -348,6 +355,8 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
         elif out_weight.dtype not in (x.dtype, torch.float32) or out_weight.shape != weight.shape:
             raise ValueError(f"out_weight must be {tuple(weight.shape)} of {x.dtype} or torch.float32")
         _, _, g_worker, g_row = _matrix_of(out_weight, R, workers, "out_weight")
+        if g_row < K or R > 1 and g_worker < (N - 1) * g_row + K and (g_worker < K or g_row < (R - 1) * g_worker + K):
+            raise ValueError("out_weight's rows must not share memory")
     weight_first = False
     if need_x:
         if out is None:
@@ -357,9 +366,15 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
             weight_first = need_weight and _meet(out, x, K)
     if weight_first and _meet(out_weight, weight):
         raise ValueError("out in x's place and out_weight in weight's: each gradient needs what the other would be written over")
+    # (all that one of the three calls would refuse, before another has added to a gradient)
+    read = grad_out if act == QS_ACT_NONE else None
+    if _meet(out, read) or _meet(out, weight) or _meet(out_weight, read) or _meet(out_weight, x):
+        raise ValueError("out and out_weight must lie apart from the operands of their products")
+    if need_x and w_row < K:
+        raise ValueError("weight's rows must not share memory")
     L, bias = lib(), bias or out_bias is not None
     dz = grad_out if act == QS_ACT_NONE else _allocate(stream, grad_out.shape, grad_out.dtype, device)
-    dz_row, x_row = _pitch(dz, N, "grad_out"), _pitch(x, K, "x")
+    dz_row, x_row, out_row = _pitch(dz, N, "grad_out"), _pitch(x, K, "x") if need_weight else K, _pitch(out, K, "out")
     to_x = (R, M, N, K, dz.data_ptr(), code, dz_row, weight.data_ptr(), _TYPE[weight.dtype], w_worker, w_row)
     to_weight = (R, M, N, K, dz.data_ptr(), code, dz_row, x.data_ptr(), x_row)
     # one scratch for the three calls, which follow one another
@@ -367,16 +382,21 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
             L.qs_linear_grad_weight_bytes(*to_weight) if need_weight else 0]
     for n, what in zip(need, ("qs_activation_grad_bytes", "qs_linear_grad_input_bytes", "qs_linear_grad_weight_bytes")):
         _done(n, what)
+    given = work is not None
     ptr, size, work = _work(work, max(need), "scratch", stream, device)
+    if given and size < max(need):
+        raise QsError(QS_CAPACITY, f"work holds {size} bytes of {max(need)}")
+    if given and ptr % (256 if max(need[1:]) else 16):
+        raise ValueError("work must lie on a boundary of 256 bytes")
+    word, handle = _word(status), _handle(stream, device)
     db = None
     if bias or act != QS_ACT_NONE:
         _, db = activation_grad(grad_out, pre, activation, out=dz if act != QS_ACT_NONE else None, bias=bias, out_bias=out_bias, workers=workers,
                                 accumulate=accumulate and out_bias is not None, work=work if bias else None, stream=stream)
-    word, handle = _word(status), _handle(stream, device)
     # each reads what the other may be written over: the weight's comes first where out takes x's place
     for product in ("weight", "x") if weight_first else ("x", "weight"):
         if product == "x" and need_x:
-            _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), _pitch(out, K, "out"), ptr, size, word, handle), "qs_linear_grad_input")
+            _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), out_row, ptr, size, word, handle), "qs_linear_grad_input")
         if product == "weight" and need_weight:
             _done(L.qs_linear_grad_weight(*to_weight, out_weight.data_ptr(), _TYPE[out_weight.dtype], g_worker, g_row, int(accumulate), ptr, size, word,
                                           handle), "qs_linear_grad_weight")

@@ -3,6 +3,7 @@ before anything is enqueued."""
 import pytest
 import torch
 
+from paper_1906_02367_b200 import binding as B
 from paper_1906_02367_b200 import layers as L
 from test_layers_arguments import calls  # noqa: F401
 
@@ -61,3 +62,43 @@ def test_a_norm_in_its_inputs_place_hands_out_no_hidden(calls):  # noqa: F811
     assert L.rms_norm(wide[:, :6], w, out=wide[:, 6:12]).hidden is not None
     with pytest.raises(ValueError):
         L.rms_norm_grad(x, None, torch.zeros(4), w)
+
+
+BAD = {
+    "status": lambda x, w, g, dw, db: dict(status=torch.zeros(1)),
+    "short work": lambda x, w, g, dw, db: dict(work=torch.zeros(4095, dtype=torch.uint8)),
+    "work off its boundary": lambda x, w, g, dw, db: dict(work=torch.zeros(8192, dtype=torch.uint8)[1:]),
+    "out in grad_out's place": lambda x, w, g, dw, db: dict(out=g),
+    "out in weight's place": lambda x, w, g, dw, db: dict(out=w),
+    "out_weight in x's place": lambda x, w, g, dw, db: dict(out_weight=x),
+    "out_weight in grad_out's place": lambda x, w, g, dw, db: dict(out_weight=g),
+    "out_weight that its rows share": lambda x, w, g, dw, db: dict(out_weight=dw[:1].expand(6, 6)),
+    "rows of out that overlap": lambda x, w, g, dw, db: dict(out=torch.zeros(36).as_strided((6, 6), (5, 1))),
+}
+
+
+@pytest.mark.parametrize("what", list(BAD))
+def test_gradients_are_refused_before_any_is_added_to(calls, what):  # noqa: F811
+    x, w, g, dw, db = torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6)
+    good = dict(out_weight=dw, out_bias=db, accumulate=True)
+    L.linear_grad(g, x, w, **good)
+    assert len(names(calls)) == 3
+    calls.clear()
+    with pytest.raises((ValueError, B.QsError)):
+        L.linear_grad(g, x, w, **{**good, **BAD[what](x, w, g, dw, db)})
+    assert names(calls) == []
+
+
+@pytest.mark.parametrize("what", ["x", "grad_out", "weight"])
+def test_operands_that_share_rows_are_refused_before_any_gradient_is_added_to(calls, what):  # noqa: F811
+    t = dict(x=torch.zeros(6, 6), grad_out=torch.zeros(6, 6), weight=torch.zeros(6, 6))
+    t[what] = t[what][:1].expand(6, 6)
+    with pytest.raises((ValueError, B.QsError)):
+        L.linear_grad(t["grad_out"], t["x"], t["weight"], out_weight=torch.zeros(6, 6), out_bias=torch.zeros(6), accumulate=True)
+    assert names(calls) == []
+
+
+def test_the_gradient_behind_an_activation_may_take_grad_outs_place(calls):  # noqa: F811
+    x, w, g, z = torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6)
+    r = L.linear_grad(g, x, w, z, "relu", out=g)
+    assert r.x is g and len(names(calls)) == 3
