@@ -582,7 +582,10 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
  *   activation: QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU z / (1 + e^-z), QS_ACT_GELU z Phi(z).
  *   work: 256-byte aligned, qs_linear_bytes(...) bytes for the same arguments (their alignment
  *   counts: operands off 16-byte boundaries are laid out anew), else QS_CAPACITY; may be NULL for 0.
- *   residual may be out itself.  A wait on the device is bounded as in qs_distill; what depends on
+ *   That is enough for any out_type and residual; qs_linear_call_bytes gives what one call takes,
+ *   by its out_type and whether residual is out itself (in_place), which is less for long sums.
+ *   residual may be out itself; then sums of more than 1024 elements of 16 bits into fp32 are kept
+ *   in work, with the result that another place of out gives.  A wait on the device is bounded as in qs_distill; what depends on
  *   one that ran out is NaN, and *status becomes QS_TIMEOUT.
  * qs_linear_grad_input  — out = dz w_r      (R M rows of K, of type), dz: R M rows of N.
  * qs_linear_grad_weight — out_r = dz_r^T x_r (N rows of K per worker, fp32 or type; accumulate:
@@ -597,6 +600,9 @@ enum { QS_ACT_NONE = 0, QS_ACT_RELU = 1, QS_ACT_SILU = 2, QS_ACT_GELU = 3 };
 int64_t qs_linear_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type,
                         int64_t x_stride, const void* w, int w_type, int64_t w_worker_stride,
                         int64_t w_stride);
+int64_t qs_linear_call_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type,
+                             int64_t x_stride, const void* w, int w_type, int64_t w_worker_stride,
+                             int64_t w_stride, int out_type, int in_place);
 int qs_linear(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride,
               const float* x_scale, const void* w, int w_type, int64_t w_worker_stride,
               int64_t w_stride, const float* w_scale, const void* bias, int bias_type,

@@ -667,7 +667,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     if (warp == 2) tmem_free<CG>(tmem, 2 * BN);
 }
 
-// The splits' sums, joined in order, and what follows
+// Sums out of the workspace, those of splits joined in order, and what follows
 template <int V>
 __global__ void __launch_bounds__(256) join_splits_kernel(const float* part, long long ld, int splits, int R, const Finish f) {
     after_launch();
@@ -1017,7 +1017,9 @@ struct Product {
 
 struct Plan {
     bool small, few, lay_a, lay_b;
+    bool kept;                                       // sums in the workspace: of splits, or where the result has no room for them
     int cg, bn, planes, splits;
+    long long k_blocks, chunk;                       // blocks along k: in all, and summed by the matrix unit in one go
     long long ld_a, ld_b, part_ld;
     long long off_b, off_part, bytes;
 };
@@ -1037,7 +1039,8 @@ bool taken_as_it_lies(const Product& p, const Operand& o) {
 // 512 x 4096 x 4096 24.1, 21.0, 33.7; 2048 x 2048 x 2048 19.5, 21.8, 35.6; 1024 x 1024 x 1024 13.4, 10.2, 9.7; 64 x 4096 x 4096 16.1, 12.2
 // (four splits; one 19.7), 14.9
 constexpr double FORM_BASE[3] = {8.5, 6.2, 6.2}, FORM_BLOCK[3] = {0.29, 0.22, 0.20};
-Plan plan_of(const Product& p, int sms) {
+// in_place: the result lies where something is still to be read
+Plan plan_of(const Product& p, int sms, int out_type, bool in_place) {
     Plan q{};
     q.planes = p.type == QS_F32 ? 3 : 1;
     q.splits = 1;
@@ -1074,7 +1077,10 @@ Plan plan_of(const Product& p, int sms) {
     if (q.lay_b) at += round_up(wb * q.planes * memory_rows(p, p.b) * q.ld_b * size, 256);
     q.off_part = at;
     q.part_ld = round_up(p.N, 8);
-    if (q.splits > 1) at += 4ll * q.splits * p.R * p.M * q.part_ld;
+    q.k_blocks = k_blocks;
+    q.chunk = out_type == QS_F32 ? CHUNK_BLOCKS : k_blocks;
+    q.kept = q.splits > 1 || (k_blocks > q.chunk && in_place);
+    if (q.kept) at += 4ll * q.splits * p.R * p.M * q.part_ld;
     q.bytes = at;
     return q;
 }
@@ -1163,8 +1169,8 @@ cudaError_t launch_gemm_as(const CUtensorMap (&map)[4], const GemmArgs& g, bool 
 }
 template <int CG, int BN>
 cudaError_t launch_gemm(const CUtensorMap (&map)[4], const GemmArgs& g, bool after, int sms, cudaStream_t st) {
-    // (sums of splits are written in fp32 whatever the result's type: one form is enough)
-    if (g.f.type == QS_F32 || g.splits > 1) return launch_gemm_as<CG, BN, float>(map, g, after, sms, st);
+    // (sums that are kept are written in fp32 whatever the result's type: one form is enough)
+    if (g.f.type == QS_F32) return launch_gemm_as<CG, BN, float>(map, g, after, sms, st);
     return g.f.type == QS_BF16 ? launch_gemm_as<CG, BN, bf16>(map, g, after, sms, st) : launch_gemm_as<CG, BN, __half>(map, g, after, sms, st);
 }
 
@@ -1203,7 +1209,7 @@ cudaError_t launch_few(const Product& p, const FewArgs& a, bool vec, cudaStream_
 int run_product(const Product& p, const Finish& f, void* work, int64_t work_bytes, int* status, cudaStream_t st) {
     const int sms = sm_count();
     if (!sms) return QS_CUDA;
-    const Plan q = plan_of(p, sms);
+    const Plan q = plan_of(p, sms, f.type, f.res && f.res == f.out);
     if (q.small) {
         const auto side = [&](const Operand& o) { return Side{o.p, o.across ? 1 : o.ld, o.across ? o.ld : 1, o.worker}; };
         const bool same = p.b.type == p.type;
@@ -1253,12 +1259,11 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.splits = q.splits;
     g.units = p.R * g.tiles_m * g.tiles_n * g.splits;
     g.k_step = 128 / size;
-    g.k_blocks = (int)((p.K + g.k_step - 1) / g.k_step);
+    g.k_blocks = (int)q.k_blocks;
     g.pairs = q.planes == 3 ? 6 : 1;
     g.per_split = g.k_blocks / q.splits;
     g.more = g.k_blocks % q.splits;
-    // (the sums so far lie in the result, so it has to hold fp32 and be nothing that is still to be read)
-    g.chunk = f.type == QS_F32 && (q.splits > 1 || f.res != f.out) ? CHUNK_BLOCKS : g.k_blocks;
+    g.chunk = (int)q.chunk;
     g.eight = type == QS_E4M3;
     // sums in fp32; operand types (e4m3 and fp16 are 0, bf16 is 1); which lie across k; the tile
     const uint32_t t = type == QS_BF16 ? 1 : 0;
@@ -1266,11 +1271,11 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     g.limit = wait_limit();
     g.status = status;
     g.f = f;
-    g.columns = q.splits == 1 && (f.bias || f.b_scale);
-    g.l2_adds = f.vec && f.type == QS_F32 && q.splits == 1 && f.act == QS_ACT_NONE && !f.bias && !f.res && !f.pre && !f.a_scale;
+    g.columns = !q.kept && (f.bias || f.b_scale);
+    g.l2_adds = f.vec && f.type == QS_F32 && !q.kept && f.act == QS_ACT_NONE && !f.bias && !f.res && !f.pre && !f.a_scale;
     if ((f.res || ((f.accumulate || g.chunk < g.k_blocks) && !g.l2_adds)) && p.N * size_of_type(f.type) % 16) g.f.vec = 0;
     float* part = reinterpret_cast<float*>(w + q.off_part);
-    if (q.splits > 1) {                              // sums instead of results: (R, splits, M, part_ld)
+    if (q.kept) {                                    // sums instead of results: (R, splits, M, part_ld)
         g.f = Finish{};
         g.f.M = p.M; g.f.N = p.N; g.f.type = QS_F32; g.f.vec = 1;
         g.l2_adds = 1;
@@ -1283,7 +1288,7 @@ int run_product(const Product& p, const Finish& f, void* work, int64_t work_byte
     if (e != cudaSuccess) return status_of(e);
     const bool after = sides > 0;
     e = q.cg == 2 ? launch_gemm<2, 256>(map, g, after, sms, st) : q.bn == 128 ? launch_gemm<1, 128>(map, g, after, sms, st) : launch_gemm<1, 64>(map, g, after, sms, st);
-    if (e != cudaSuccess || q.splits == 1) return status_of(e);
+    if (e != cudaSuccess || !q.kept) return status_of(e);
     const long long items = p.R * p.M * (f.vec ? (p.N + 7) / 8 : p.N);
     const dim3 grid((unsigned)std::min<long long>((items + 255) / 256, 1 << 20));
     e = f.vec && p.N % 8 == 0 ? launch(true, join_splits_kernel<8>, grid, 256, 0, st, (const float*)part, q.part_ld, q.splits, p.R, f)
@@ -1378,9 +1383,9 @@ Product input_of(int R, int64_t M, int64_t N, int64_t K, const void* dz, int typ
 Product weight_of(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride) {
     return {R, N, K, M, type, {dz, type, N, dz_stride, R > 1 ? M * dz_stride : 0, 1}, {x, type, K, x_stride, R > 1 ? M * x_stride : 0, 1}};
 }
-int64_t bytes_for(const Product& p) {
+int64_t bytes_for(const Product& p, int out_type, bool in_place) {
     const int sms = sm_count();
-    return sms ? plan_of(p, sms).bytes : (int64_t)QS_CUDA;
+    return sms ? plan_of(p, sms, out_type, in_place).bytes : (int64_t)QS_CUDA;
 }
 bool weight_type_ok(int type, int w_type) { return type == QS_E4M3 ? w_type == QS_E4M3 : size_of_type(type) && (w_type == type || w_type == QS_F32); }
 
@@ -1395,7 +1400,15 @@ int64_t qs_linear_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, i
                         int64_t w_worker_stride, int64_t w_stride) {
     if (bad_sizes(R, M, N, K) || !weight_type_ok(x_type, w_type)) return QS_INVALID_ARG;
     if (sizes_too_large(R, M, N, K)) return QS_TOO_LARGE;
-    return M ? bytes_for(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride)) : 0;
+    // (a result in fp32 in its residual's place keeps sums where any other does: enough for all)
+    return M ? bytes_for(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride), QS_F32, true) : 0;
+}
+
+int64_t qs_linear_call_bytes(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const void* w, int w_type,
+                             int64_t w_worker_stride, int64_t w_stride, int out_type, int in_place) {
+    if (bad_sizes(R, M, N, K) || !weight_type_ok(x_type, w_type) || !size_of_type(out_type)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K)) return QS_TOO_LARGE;
+    return M ? bytes_for(forward_of(R, M, N, K, x, x_type, x_stride, w, w_type, w_worker_stride, w_stride), out_type, in_place) : 0;
 }
 
 int qs_linear(int R, int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t x_stride, const float* x_scale, const void* w, int w_type,
@@ -1432,7 +1445,7 @@ int64_t qs_linear_grad_input_bytes(int R, int64_t M, int64_t N, int64_t K, const
                                    int64_t w_worker_stride, int64_t w_stride) {
     if (bad_sizes(R, M, N, K) || !size_of_type(type) || !weight_type_ok(type, w_type)) return QS_INVALID_ARG;
     if (sizes_too_large(R, M, N, K) || sizes_too_large(R, M, K, N)) return QS_TOO_LARGE;
-    return M ? bytes_for(input_of(R, M, N, K, dz, type, dz_stride, w, w_type, w_worker_stride, w_stride)) : 0;
+    return M ? bytes_for(input_of(R, M, N, K, dz, type, dz_stride, w, w_type, w_worker_stride, w_stride), type, false) : 0;
 }
 
 int qs_linear_grad_input(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* w, int w_type,
@@ -1457,7 +1470,7 @@ int qs_linear_grad_input(int R, int64_t M, int64_t N, int64_t K, const void* dz,
 int64_t qs_linear_grad_weight_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride) {
     if (bad_sizes(R, M, N, K) || !size_of_type(type)) return QS_INVALID_ARG;
     if (sizes_too_large(R, M, N, K) || sizes_too_large(R, N, K, 1)) return QS_TOO_LARGE;
-    return M ? bytes_for(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride)) : 0;
+    return M ? bytes_for(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride), type, false) : 0;
 }
 
 int qs_linear_grad_weight(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride, void* out,

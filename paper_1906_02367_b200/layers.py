@@ -288,9 +288,9 @@ def linear(x, weight, bias=None, activation=None, residual=None, x_scale=None, w
         pre = _allocate(stream, shape, dtype, device)
     _like(pre, shape, dtype, "pre")
     L = lib()
-    x_row, w_code = _pitch(x, K, "x"), _ALL[weight.dtype]
-    ptr, size, keep = _work(work, L.qs_linear_bytes(R, M, N, K, x.data_ptr(), x_code, x_row, weight.data_ptr(), w_code, w_worker, w_row),
-                            "qs_linear_bytes", stream, device)
+    x_row, w_code, in_place = _pitch(x, K, "x"), _ALL[weight.dtype], residual is not None and residual.data_ptr() == out.data_ptr()
+    ptr, size, keep = _work(work, L.qs_linear_call_bytes(R, M, N, K, x.data_ptr(), x_code, x_row, weight.data_ptr(), w_code, w_worker, w_row,
+                                                         _TYPE[dtype], int(in_place)), "qs_linear_call_bytes", stream, device)
     _done(L.qs_linear(R, M, N, K, x.data_ptr(), x_code, x_row, _ptr(x_scale), weight.data_ptr(), w_code, w_worker, w_row, _ptr(weight_scale),
                       _ptr(bias), bias_type, bias_step, act, _ptr(residual), _pitch(residual, N, "residual"), _ptr(pre), _pitch(pre, N, "pre"),
                       out.data_ptr(), _TYPE[dtype], _pitch(out, N, "out"), ptr, size, _word(status), _handle(stream, device)), "qs_linear")
@@ -337,8 +337,8 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
     qs_linear_grad_weight); the residual's is grad_out itself.  pre: what linear saved (not needed without an activation).
     The gradient in front of the activation is rounded to grad_out's type, which is x's.  The weight's gradient is of `dtype`
     (fp32 or x's type), the bias's fp32; out_weight and out_bias may be stretches of a gradient batch, and accumulate adds
-    to them.  out may take x's place, or out_weight weight's, not both.  Returns LinearGrad(x, weight, bias, pre): None for what was not asked for; pre is the gradient in front of the
-    activation."""
+    to them.  out may take x's place, or out_weight weight's, not both.  Returns LinearGrad(x, weight, bias, pre): None for what
+    was not asked for; pre is the gradient in front of the activation."""
     device = _on(x, weight, grad_out, pre, out, out_weight, out_bias, work, status)
     workers, R, M, N, K, w_worker, w_row = _operands(x, weight)
     code, act = _type(x, "x"), _act(activation)
