@@ -589,7 +589,8 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
  *   one that ran out is NaN, and *status becomes QS_TIMEOUT.
  * qs_linear_grad_input  — out = dz w_r      (R M rows of K, of type), dz: R M rows of N.
  * qs_linear_grad_weight — out_r = dz_r^T x_r (N rows of K per worker, fp32 or type; accumulate:
- *   added to it).  Workers' results must not overlap.
+ *   added to it).  Workers' results must not overlap.  qs_linear_grad_weight_bytes is enough for
+ *   either type; qs_linear_grad_weight_call_bytes gives what one call takes.
  * qs_activation_grad    — out = grad act'(pre), rounded to type (NULL: not wanted), and
  *   grad_bias_r = the sum over worker r's rows of grad act'(pre) before that rounding (NULL: not
  *   wanted; accumulate: added to it; takes 16-byte aligned work).  relu has slope 0 at 0.
@@ -618,6 +619,9 @@ int qs_linear_grad_input(int R, int64_t M, int64_t N, int64_t K, const void* dz,
                          int64_t work_bytes, int* status, void* cuda_stream);
 int64_t qs_linear_grad_weight_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
                                     int64_t dz_stride, const void* x, int64_t x_stride);
+int64_t qs_linear_grad_weight_call_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz,
+                                         int type, int64_t dz_stride, const void* x,
+                                         int64_t x_stride, int out_type);
 int qs_linear_grad_weight(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type,
                           int64_t dz_stride, const void* x, int64_t x_stride, void* out,
                           int out_type, int64_t out_worker_stride, int64_t out_stride,

@@ -33,7 +33,8 @@ EXPORTS = [
     "qs_gap_words", "qs_recode_gaps", "qs_decode_gaps", "qs_destroy",
     "qs_embed", "qs_embed_grad", "qs_embed_grad_bytes", "qs_token_logp", "qs_token_logp_grad", "qs_distill", "qs_distill_grad",
     "qs_rms_norm", "qs_quantize_rows", "qs_rms_norm_grad_bytes", "qs_rms_norm_grad", "qs_dropout", "qs_linear_bytes",
-    "qs_linear_call_bytes", "qs_linear", "qs_linear_grad_input_bytes", "qs_linear_grad_input", "qs_linear_grad_weight_bytes", "qs_linear_grad_weight",
+    "qs_linear_call_bytes", "qs_linear", "qs_linear_grad_input_bytes", "qs_linear_grad_input", "qs_linear_grad_weight_bytes",
+    "qs_linear_grad_weight_call_bytes", "qs_linear_grad_weight",
     "qs_activation_grad_bytes", "qs_activation_grad",
 ]
 
@@ -109,11 +110,12 @@ def lib():
         L.qs_linear_grad_input_bytes.argtypes = operands
         L.qs_linear_grad_input.argtypes = operands + [vp, i64, vp, i64, vp, vp]
         L.qs_linear_grad_weight_bytes.argtypes = [i32, i64, i64, i64, vp, i32, i64, vp, i64]
+        L.qs_linear_grad_weight_call_bytes.argtypes = L.qs_linear_grad_weight_bytes.argtypes + [i32]
         L.qs_linear_grad_weight.argtypes = [i32, i64, i64, i64, vp, i32, i64, vp, i64, vp, i32, i64, i64, i32, vp, i64, vp, vp]
         L.qs_activation_grad_bytes.argtypes = [i32, i64, i64]
         L.qs_activation_grad.argtypes = [i32, i64, i64, vp, i32, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp]
         for f in (L.qs_rms_norm_grad_bytes, L.qs_linear_bytes, L.qs_linear_call_bytes, L.qs_linear_grad_input_bytes, L.qs_linear_grad_weight_bytes,
-                  L.qs_activation_grad_bytes):
+                  L.qs_linear_grad_weight_call_bytes, L.qs_activation_grad_bytes):
             f.restype = i64
         L.qs_destroy.argtypes = [vp]
         L.qs_destroy.restype = None

@@ -354,10 +354,14 @@ __global__ void __launch_bounds__(256) lay_kernel(const LayBoth both) {
 constexpr int TILE_M = 128;                          // rows of a block's part of a tile: the lanes of tensor memory
 constexpr int STAGES = 5;
 constexpr int GEMM_THREADS = 384;                    // warps: copies, products, tensor memory, (none), eight that finish
-// The matrix unit cuts what lies below 2^-24 of a sum at every addition, always towards zero: 8e-10 of the result per element
-// summed.  Results in fp32 are therefore added up, rounded to nearest, from sums over this many blocks of 128 bytes (1024 elements
-// of 16 bits: 8e-7).  (Weights' gradient of 8 x 4096 rows, 4096 x 1024: 205 us with 64 blocks, 3e-6 off; 218 with 32; 240 with 16)
-constexpr int CHUNK_BLOCKS = 16;
+// The matrix unit cuts what lies below the last bits of a sum at every addition, always towards zero: less than 2^-23 of the sum so
+// far for every 8 elements of 16 bits or 16 of 8.  Of the result that is, in the mean, for sums of mixed signs 8.6e-7 after 1024
+// elements of 16 bits, 7.9e-6 after 8192, 6.6e-5 after 65536; of one sign in bf16 2.2e-6, 3.5e-5, 3.9e-4, in fp16 6.1e-6, 5.3e-5, 4.3e-4, in
+// e4m3 1.7e-7, 3.5e-6, 5.7e-5.  Sums are therefore added up, rounded to nearest, from those over this many blocks of 128 bytes:
+// results in fp32 from 1024 elements of 16 bits (weights' gradient of 8 x 4096 rows, 4096 x 1024: 205 us with 64 blocks, 218 with
+// 32; 240 with 16); those in 16 bits, which are rounded by 2^-9 (bf16) or 2^-12 (fp16) of their size at most, from 16384 and 8192: the cut is a
+// quarter of that at most.  (4096 x 4096 x 32768 in bf16 5 to 15 % longer than in one sum, 4096 x 4096 x 16384 in fp16 10 to 20 %)
+constexpr int CHUNK_BLOCKS = 16, CHUNK_BF16 = 256, CHUNK_F16 = 128;
 constexpr int PASS_BYTES = 8 * 2 * 4096;             // two tiles of 32 rows of 128 bytes on their way out, per finishing warp
 
 struct GemmArgs {
@@ -1039,7 +1043,7 @@ bool taken_as_it_lies(const Product& p, const Operand& o) {
 // 512 x 4096 x 4096 24.1, 21.0, 33.7; 2048 x 2048 x 2048 19.5, 21.8, 35.6; 1024 x 1024 x 1024 13.4, 10.2, 9.7; 64 x 4096 x 4096 16.1, 12.2
 // (four splits; one 19.7), 14.9
 constexpr double FORM_BASE[3] = {8.5, 6.2, 6.2}, FORM_BLOCK[3] = {0.29, 0.22, 0.20};
-// in_place: the result lies where something is still to be read
+// in_place: the result lies where something is still to be read.  Sums of several chunks need a place in fp32: the result's, or their own
 Plan plan_of(const Product& p, int sms, int out_type, bool in_place) {
     Plan q{};
     q.planes = p.type == QS_F32 ? 3 : 1;
@@ -1078,8 +1082,8 @@ Plan plan_of(const Product& p, int sms, int out_type, bool in_place) {
     q.off_part = at;
     q.part_ld = round_up(p.N, 8);
     q.k_blocks = k_blocks;
-    q.chunk = out_type == QS_F32 ? CHUNK_BLOCKS : k_blocks;
-    q.kept = q.splits > 1 || (k_blocks > q.chunk && in_place);
+    q.chunk = out_type == QS_F32 ? CHUNK_BLOCKS : out_type == QS_F16 ? CHUNK_F16 : CHUNK_BF16;
+    q.kept = q.splits > 1 || (k_blocks > q.chunk && (in_place || out_type != QS_F32));
     if (q.kept) at += 4ll * q.splits * p.R * p.M * q.part_ld;
     q.bytes = at;
     return q;
@@ -1471,6 +1475,13 @@ int64_t qs_linear_grad_weight_bytes(int R, int64_t M, int64_t N, int64_t K, cons
     if (bad_sizes(R, M, N, K) || !size_of_type(type)) return QS_INVALID_ARG;
     if (sizes_too_large(R, M, N, K) || sizes_too_large(R, N, K, 1)) return QS_TOO_LARGE;
     return M ? bytes_for(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride), type, false) : 0;
+}
+
+int64_t qs_linear_grad_weight_call_bytes(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x,
+                                         int64_t x_stride, int out_type) {
+    if (bad_sizes(R, M, N, K) || !size_of_type(type) || (out_type != type && out_type != QS_F32)) return QS_INVALID_ARG;
+    if (sizes_too_large(R, M, N, K) || sizes_too_large(R, N, K, 1)) return QS_TOO_LARGE;
+    return M ? bytes_for(weight_of(R, M, N, K, dz, type, dz_stride, x, x_stride), out_type, false) : 0;
 }
 
 int qs_linear_grad_weight(int R, int64_t M, int64_t N, int64_t K, const void* dz, int type, int64_t dz_stride, const void* x, int64_t x_stride, void* out,

@@ -379,8 +379,8 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
     to_weight = (R, M, N, K, dz.data_ptr(), code, dz_row, x.data_ptr(), x_row)
     # one scratch for the three calls, which follow one another
     need = [L.qs_activation_grad_bytes(R, M, N) if bias else 0, L.qs_linear_grad_input_bytes(*to_x) if need_x else 0,
-            L.qs_linear_grad_weight_bytes(*to_weight) if need_weight else 0]
-    for n, what in zip(need, ("qs_activation_grad_bytes", "qs_linear_grad_input_bytes", "qs_linear_grad_weight_bytes")):
+            L.qs_linear_grad_weight_call_bytes(*to_weight, _TYPE[out_weight.dtype]) if need_weight else 0]
+    for n, what in zip(need, ("qs_activation_grad_bytes", "qs_linear_grad_input_bytes", "qs_linear_grad_weight_call_bytes")):
         _done(n, what)
     given = work is not None
     ptr, size, work = _work(work, max(need), "scratch", stream, device)
