@@ -55,3 +55,51 @@ def test_quantized_rows_to_the_last_bit(L, dtype):
     x = rand((256, 512), F32, 5) * torch.pow(2.0, torch.arange(-140, 116, device="cuda").float())[:, None]
     q = L.quantize(x)
     check_bits(q.values, q.scale, x)
+
+
+# ------------------------------------------------------------------ activations
+def by_bias(L, z, M, K, activation, dtype, out):
+    """act(z) through a product whose sums are zero: z is the bias, the same for every row."""
+    x, w = torch.zeros((M, K), device="cuda", dtype=dtype), rand((z.numel(), K), dtype, 2)
+    return L.linear(x, w, z, activation=activation, dtype=out, save=True)
+
+
+# few rows, small products, one tile in a row and several, 64 and 256 columns, in splits (with K), off the boundary
+FORMS = [(1, 1024, 64), (20, 1024, 64), (40, 40, 16), (300, 1024, 64), (130, 64, 4096), (3000, 1280, 64), (140, 1023, 100)]
+
+
+@pytest.mark.parametrize("M,N,K", FORMS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gelu_in_32_bits_over_its_range(L, M, N, K, dtype):
+    """Relative to the value, where the normal distribution's tail makes it small too: z^2, log2(e) / 2 and their product, each
+    rounded, are 0.6 z^2 2^-23 in the exponential, which is good to 2 steps of 2^-23; the reciprocal, the polynomial, the
+    products of the two and of z to 4."""
+    z = torch.linspace(-12.5, 6.0, N, device="cuda")
+    r = by_bias(L, z, M, K, "gelu", dtype, F32)
+    assert torch.equal(r.pre, z.expand(M, N))
+    y = ref.activate(z.double(), "gelu").expand(M, N)
+    near(r.out, y, (6 + 0.6 * z.double() ** 2) * E * y.abs(), F32)
+
+
+@pytest.mark.parametrize("M,N,K", FORMS)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_gelu_in_16_bits_over_its_range(L, M, N, K, dtype):
+    """Half a step of the type and what fp32 leaves: z^2 rounded in an exponent, about ten more roundings."""
+    z = torch.linspace(-12.5, 6.0, N, device="cuda")
+    r = by_bias(L, z, M, K, "gelu", dtype, dtype)
+    y = ref.activate(z.double(), "gelu")
+    near(r.out, y.expand(M, N), ((10 + 2 * z.double() ** 2) * E * y.abs()).expand(M, N), dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_slope_of_gelu_over_its_range(L, dtype):
+    """slope = Phi + z phi: in fp32 6 + 0.6 z^2 steps of either, in 16 bits about ten and more in the exponent."""
+    z = torch.linspace(-12.5, 6.0, 4096, device="cuda").to(dtype).repeat(9, 1)
+    z64 = z.double()
+    phi = torch.exp(-z64 * z64 / 2) * 0.3989422804014327
+    cdf = 0.5 * torch.special.erfc(-z64 * 0.7071067811865476)
+    steps = 6 + 0.6 * z64 ** 2 if dtype == F32 else 10 + 2 * z64 ** 2
+    got = L.activation_grad(torch.ones_like(z), z, "gelu", bias=True)
+    slack = steps * E * (cdf + (z64 * phi).abs())
+    near(got[0], cdf + z64 * phi, slack, dtype)
+    near(got[1], 9 * (cdf + z64 * phi)[0], 9 * (slack[0] + 9 * E * (cdf + z64 * phi).abs()[0]), F32)
