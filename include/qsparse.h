@@ -575,10 +575,10 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
  *   out_type is x_type or QS_F32.  x_type QS_E4M3: w too, x_scale (R M) and w_scale (R N, or N with
  *   one w for all) multiply the sums, out_type any other.  The scales are NULL otherwise.
  *   bias (NULL: none): N of bias_type per worker.  Sums, bias and activation are fp32, rounded once.
- *   Products of 16- and 8-bit elements are exact.  fp32 operands are cut into three parts of 8
- *   bits of significand, and the products of their last parts, below 2^-21 of the whole, are left
- *   out; results that an infinity enters are NaN.  Small products of them (under five million
- *   operations) are plain fp32.
+ *   Products of 16- and 8-bit elements are exact.  fp32 operands are taken apart into three
+ *   rounded parts of 8 bits of significand, and the products of their last parts, below 2^-25 of
+ *   the whole, are left out; results that an infinity enters are NaN.  Small products of them (under
+ *   five million operations) are plain fp32.
  *   activation: QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU z / (1 + e^-z), QS_ACT_GELU z Phi(z).
  *   work: 256-byte aligned, qs_linear_bytes(...) bytes for the same arguments (their alignment
  *   counts: operands off 16-byte boundaries are laid out anew), else QS_CAPACITY; may be NULL for 0.

@@ -103,3 +103,31 @@ def test_slope_of_gelu_over_its_range(L, dtype):
     slack = steps * E * (cdf + (z64 * phi).abs())
     near(got[0], cdf + z64 * phi, slack, dtype)
     near(got[1], 9 * (cdf + z64 * phi)[0], 9 * (slack[0] + 9 * E * (cdf + z64 * phi).abs()[0]), F32)
+
+
+# ------------------------------------------------------------------ fp32 operands in parts
+@pytest.mark.parametrize("M,N,K", [(16, 2048, 16), (1024, 1024, 16), (600, 1029, 32)])
+def test_parts_of_fp32_leave_little_out(L, M, N, K):
+    """Operands just below 1 + 2^-7, whose bits behind the first eight are all ones: cut off instead of rounded, the products
+    of their last parts are 2^-21 of the whole.  Rounded parts leave out 2^-25 at most; the matrix unit's sums of 16 terms cut
+    off 2^-23 twice at most (in the last two of six products, the others are below 2^-8)."""
+    one = 1 + 2.0 ** -7 - 2.0 ** -23
+    x, w = rand((M, K), F32, 1).mul_(2.0 ** -16).abs_().neg_().add_(one), torch.full((N, K), one, device="cuda")
+    z, _ = ref.product(x, w)
+    off = ((L.linear(x, w).out.double() - z) / z).abs().max()
+    assert float(off) < (K / 16) * 2 * E + 2.0 ** -25, float(off)
+
+
+def test_parts_of_the_largest_numbers(L):
+    """Numbers that round past the largest bf16 are cut off; NaN and infinities make their rows NaN, and no others."""
+    x, w = torch.zeros((600, 64), device="cuda"), torch.zeros((1100, 64), device="cuda")
+    x[:, 3], w[:, 3] = torch.finfo(F32).max, 0.5
+    x[5, 3], x[6, 3], x[7, 3] = -torch.finfo(F32).max, float("nan"), float("inf")
+    y = L.linear(x, w).out
+    want = torch.full((600, 1100), torch.finfo(F32).max / 2, device="cuda")
+    want[5] *= -1
+    keep = [i for i in range(600) if i not in (6, 7)]
+    near(y[keep], want[keep].double(), 4 * E * want[keep].double().abs(), F32)
+    assert bool(torch.isnan(y[6:8]).all())
+    # up to 32 rows by the small instruction, parts on the way
+    assert bool(torch.isnan(L.linear(x[:16], w).out[6:8]).all()) and torch.equal(L.linear(x[:16], w).out[:6], y[:6])
