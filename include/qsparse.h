@@ -542,8 +542,9 @@ int qs_quantize_rows(int64_t N, int64_t D, const void* x, int type, int64_t x_st
  *   out = grad_hidden + rstd (w g - n mean(w g n)),  the gradient of h, so of x and of residual;
  *   grad_weight_r = sum over worker r's rows of g n  (fp32; accumulate != 0: added to it).
  *   grad_hidden (NULL: none): what arrives at h by the residual stream.  grad_weight may be NULL;
- *   it takes qs_rms_norm_grad_bytes(R, N, D) of 16-byte aligned work, and its sums' order depends
- *   on the sizes alone.  out may take the place of grad, hidden or grad_hidden.
+ *   it takes qs_rms_norm_grad_bytes(R, N, D) of 16-byte aligned work.  Its sums' order depends on
+ *   the sizes, the type, whether rows lie on 16-byte boundaries, and the device.  out may take the
+ *   place of grad, hidden or grad_hidden.
  */
 int64_t qs_rms_norm_grad_bytes(int R, int64_t N, int64_t D);
 int qs_rms_norm_grad(int R, int64_t N, int64_t D, const void* grad, int type, int64_t grad_stride,
@@ -577,15 +578,19 @@ int qs_dropout(int R, int64_t N, int64_t D, const void* x, int type, int64_t x_s
  *   bias (NULL: none): N of bias_type per worker.  Sums, bias and activation are fp32, rounded once.
  *   Products of 16- and 8-bit elements are exact.  fp32 operands are taken apart into three
  *   rounded parts of 8 bits of significand, and the products of their last parts, below 2^-25 of
- *   the whole, are left out; results that an infinity enters are NaN.  Small products of them (under
- *   five million operations) are plain fp32.
+ *   the whole, are left out; results that an infinity enters are NaN.  Products of up to 8 rows of
+ *   x and small ones (under five million operations) are plain fp32, where an infinity stays one.
+ *   Otherwise sums are rounded after every 1024 elements of 16 bits (2048 of 8) into fp32, 16384
+ *   into bf16 and 8192 into fp16, and cut off towards zero before: sums of 1024 bf16 by 9e-7 of the
+ *   result where signs are mixed and 2e-6 where all are alike, of fp16 by 1e-6 and 6e-6; of 8192
+ *   ten times as much.
  *   activation: QS_ACT_NONE, QS_ACT_RELU, QS_ACT_SILU z / (1 + e^-z), QS_ACT_GELU z Phi(z).
  *   work: 256-byte aligned, qs_linear_bytes(...) bytes for the same arguments (their alignment
  *   counts: operands off 16-byte boundaries are laid out anew), else QS_CAPACITY; may be NULL for 0.
  *   That is enough for any out_type and residual; qs_linear_call_bytes gives what one call takes,
  *   by its out_type and whether residual is out itself (in_place), which is less for long sums.
- *   residual may be out itself; then sums of more than 1024 elements of 16 bits into fp32 are kept
- *   in work, with the result that another place of out gives.  A wait on the device is bounded as in qs_distill; what depends on
+ *   residual may be out itself; then long sums into fp32 are kept in work, with the result that
+ *   another place of out gives.  A wait on the device is bounded as in qs_distill; what depends on
  *   one that ran out is NaN, and *status becomes QS_TIMEOUT.
  * qs_linear_grad_input  — out = dz w_r      (R M rows of K, of type), dz: R M rows of N.
  * qs_linear_grad_weight — out_r = dz_r^T x_r (N rows of K per worker, fp32 or type; accumulate:
