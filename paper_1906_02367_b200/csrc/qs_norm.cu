@@ -316,9 +316,9 @@ __device__ __forceinline__ void norm_grad_rows_of(const NormGradArgs& a, float (
                 unpack(gv, g[u]);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float gn = gv[j] * (hv[j] * rstd);
-                    dw[u][j] += gn;
-                    dot = __fmaf_rn(gn, w[u][j], dot);
+                    const float n = hv[j] * rstd;
+                    dw[u][j] = __fmaf_rn(gv[j], n, dw[u][j]);
+                    dot = __fmaf_rn(gv[j] * w[u][j], n, dot);
                 }
             }
         }

@@ -131,3 +131,18 @@ def test_parts_of_the_largest_numbers(L):
     assert bool(torch.isnan(y[6:8]).all())
     # up to 32 rows by the small instruction, parts on the way
     assert bool(torch.isnan(L.linear(x[:16], w).out[6:8]).all()) and torch.equal(L.linear(x[:16], w).out[:6], y[:6])
+
+
+# ------------------------------------------------------------------ sums over rows
+@pytest.mark.parametrize("R,M,N", [(1, 509, 257), (1, 5000, 1024), (2, 3000, 333), (1, 64, 4096)])
+def test_sums_over_rows_round_like_trees(L, R, M, N):
+    """A rounding is 0.41 2^-24 of its sum in the mean of squares.  In a tree over rows of mixed signs every level leaves as much: 13
+    levels, or stretches of as many rows, and two products' roundings come to 1.6 2^-24 of the result; a chain of 32 partial sums
+    alone is worth 16 levels."""
+    h, g, w = rand((R, M, N), F32, 1, 2.0), rand((R, M, N), F32, 2, 0.01), rand((R, N), F32, 3, 0.1, 1.0)
+    rstd = ref.rms_norm(h, w, None, 1e-6)[2].float()
+    _, dw, _ = ref.rms_norm_grad(g, h, rstd, w, None)
+    off = L.rms_norm_grad(g, h, rstd, w).weight.double() - dw
+    assert float(off.norm() / dw.norm()) < 2 * 2.0 ** -24, float(off.norm() / dw.norm())
+    db = L.activation_grad(g, bias=True, workers=True)[1].double() - g.double().sum(1)
+    assert float(db.norm() / g.double().sum(1).norm()) < 2 * 2.0 ** -24
