@@ -85,20 +85,26 @@ def _matrix_of(t, R, workers, what):
     return N, K, (t.stride(0) if workers and R > 1 else 0), (t.stride(-2) if N > 1 else max(t.stride(-2), K))
 
 
-def _meet(a, b, width=None):
-    """Whether the memory of two tensors (None: no) meets: what lies between their first and last elements, or with a width of
-    their rows those rows' columns."""
-    if a is None or b is None or not a.numel() or not b.numel():
+def _span(t):
+    """The addresses of a tensor's first element and behind its last (None or empty: none)."""
+    if t is None or not t.numel():
+        return 0, 0
+    at = t.data_ptr()
+    if t.is_contiguous():
+        return at, at + t.nbytes
+    return at, at + t.element_size() * (1 + sum((n - 1) * d for n, d in zip(t.shape, t.stride())))
+
+
+def _cross(a, b):
+    return a[0] < b[1] and b[0] < a[1]
+
+
+def _share(a, b, width):
+    """Whether two tensors of rows of one type and width share memory: other columns of the same rows do not."""
+    if not _cross(_span(a), _span(b)):
         return False
-    size, other = a.element_size(), b.element_size()
-    at, to = a.data_ptr(), b.data_ptr()
-    end = [p + s * (1 + sum((n - 1) * d for n, d in zip(t.shape, t.stride()))) for t, p, s in ((a, at, size), (b, to, other))]
-    if end[0] <= to or end[1] <= at:
-        return False
-    if width is None or size != other:
-        return True
-    row = _pitch(a, width, "")
-    return row != _pitch(b, width, "") or not width * size <= (to - at) % (row * size) <= (row - width) * size
+    row, size = _pitch(a, width, "out"), a.element_size()
+    return row != _pitch(b, width, "x") or not width * size <= (b.data_ptr() - a.data_ptr()) % (row * size) <= (row - width) * size
 
 
 def _work(work, need, what, stream, device):
@@ -142,7 +148,7 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, quantize=False, out=None, 
         out = _allocate(stream, shape, out_type, device)
     else:
         _like(out, shape, out_type, "out")
-        if residual is None and _meet(out, x, D):
+        if residual is None and not quantize and _share(out, x, D):
             kept = None
     if quantize:
         if scale is None:
@@ -347,6 +353,7 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
         raise ValueError("out and out_weight belong to gradients that are asked for")
     if accumulate and (need_weight and out_weight is None or bias and out_bias is None):
         raise ValueError("accumulate needs out_weight and out_bias for what it is to be added to")
+    place, weight_place = out, out_weight                # (of the caller's: what is made here meets nothing)
     if need_weight:
         if out_weight is None:
             if dtype not in (x.dtype, torch.float32):
@@ -357,19 +364,22 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
         _, _, g_worker, g_row = _matrix_of(out_weight, R, workers, "out_weight")
         if g_row < K or R > 1 and g_worker < (N - 1) * g_row + K and (g_worker < K or g_row < (R - 1) * g_worker + K):
             raise ValueError("out_weight's rows must not share memory")
-    weight_first = False
     if need_x:
         if out is None:
             out = _allocate(stream, x.shape, x.dtype, device)
-        else:
-            _like(out, x.shape, x.dtype, "out")
-            weight_first = need_weight and _meet(out, x, K)
-    if weight_first and _meet(out_weight, weight):
-        raise ValueError("out in x's place and out_weight in weight's: each gradient needs what the other would be written over")
-    # (all that one of the three calls would refuse, before another has added to a gradient)
-    read = grad_out if act == QS_ACT_NONE else None
-    if _meet(out, read) or _meet(out, weight) or _meet(out_weight, read) or _meet(out_weight, x):
-        raise ValueError("out and out_weight must lie apart from the operands of their products")
+        _like(out, x.shape, x.dtype, "out")
+    # all that one of the three calls would refuse, before another has added to a gradient; each of the two products reads what the
+    # other may be written over, so the weight's comes first where out takes x's place
+    weight_first = False
+    if place is not None or weight_place is not None:
+        to, to_w, of, of_w, read = _span(place), _span(weight_place), _span(x), _span(weight), _span(grad_out if act == QS_ACT_NONE else None)
+        if _cross(to, read) or _cross(to, of_w):
+            raise ValueError("out must lie apart from grad_out and weight")
+        if _cross(to_w, read) or _cross(to_w, of):
+            raise ValueError("out_weight must lie apart from grad_out and x")
+        weight_first = need_weight and _cross(to, of) and _share(place, x, K)
+        if weight_first and _cross(to_w, of_w):
+            raise ValueError("out in x's place and out_weight in weight's: each gradient needs what the other would be written over")
     if need_x and w_row < K:
         raise ValueError("weight's rows must not share memory")
     L, bias = lib(), bias or out_bias is not None
@@ -393,7 +403,6 @@ def linear_grad(grad_out, x, weight, pre=None, activation=None, need_x=True, nee
     if bias or act != QS_ACT_NONE:
         _, db = activation_grad(grad_out, pre, activation, out=dz if act != QS_ACT_NONE else None, bias=bias, out_bias=out_bias, workers=workers,
                                 accumulate=accumulate and out_bias is not None, work=work if bias else None, stream=stream)
-    # each reads what the other may be written over: the weight's comes first where out takes x's place
     for product in ("weight", "x") if weight_first else ("x", "weight"):
         if product == "x" and need_x:
             _done(L.qs_linear_grad_input(*to_x, out.data_ptr(), out_row, ptr, size, word, handle), "qs_linear_grad_input")
