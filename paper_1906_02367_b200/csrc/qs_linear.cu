@@ -444,8 +444,8 @@ template <int CG, int BN> __host__ __device__ constexpr int gemm_smem() { return
 // of the leading block issues the products into one of two accumulators; eight warps per block take the other one out, a row
 // per lane, finish it and leave it in tiles of shared memory that bulk copies take to the result (rows off the 16-byte boundary
 // are turned there and stored a column per lane).  Bound by the products for long sums: 516 of 512 cycles per slot in bf16 and in
-// e4m3 (8192 x 8192 x 8192: 725 us, 1516 TFLOP/s under the power limit; e4m3 365 us, 3014); for short ones by the finishing warps' instructions
-// (8 x 4096 x 4096 x 1024: 203 us, 227 with silu, 248 with the saved values too).
+// e4m3 (8192 x 8192 x 8192 in short loops: 725 us, 1516 TFLOP/s under the power limit; e4m3 365 us, 3014.  8192 x 16384 x 4096 in e4m3 takes 400
+// us so, 473 to 496 in a loop of seconds); for short ones by the finishing warps' instructions (8 x 4096 x 4096 x 1024: 203 us, 222 with silu, 248 with the saved values too).
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, unsigned long long limit) {
     return __all_sync(~0u, mbar_wait_asleep(bar, parity, limit));                // (the lanes give up together)
 }
@@ -1071,7 +1071,7 @@ bool taken_as_it_lies(const Product& p, const Operand& o) {
            (p.R == 1 || (o.worker * size % 16 == 0 && o.worker < 1ll << 36));       // (a map's strides end at 2^40 bytes)
 }
 
-// Tiles of 256 x 256 by two blocks, of 128 x 128 and 128 x 64 by one.  Measured in bf16 (us; each form with the splits that suit it best):
+// Tiles of 256 x 256 by two blocks, of 128 x 128 and 128 x 64 by one.  Measured in bf16, and used for all types (us; each form with the splits that suit it best):
 // 512 x 4096 x 4096 24.1, 21.0, 33.7; 2048 x 2048 x 2048 19.5, 21.8, 35.6; 1024 x 1024 x 1024 13.4, 10.2, 9.7; 64 x 4096 x 4096 16.1, 12.2
 // (four splits; one 19.7), 14.9
 constexpr double FORM_BASE[3] = {8.5, 6.2, 6.2}, FORM_BLOCK[3] = {0.29, 0.22, 0.20};
