@@ -102,3 +102,29 @@ def test_the_gradient_behind_an_activation_may_take_grad_outs_place(calls):  # n
     x, w, g, z = torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6), torch.zeros(6, 6)
     r = L.linear_grad(g, x, w, z, "relu", out=g)
     assert r.x is g and len(names(calls)) == 3
+
+
+def test_the_workspace_goes_by_the_results_type_and_place(calls):  # noqa: F811
+    x, w, r = torch.zeros(4, 6, dtype=torch.bfloat16), torch.zeros(5, 6), torch.zeros(4, 5)
+    L.linear(x, w, residual=r, out=r)
+    assert [a[-2:] for n, a in calls if n == "qs_linear_call_bytes"] == [(B.QS_F32, 1)]
+    calls.clear()
+    L.linear(x, w, residual=r, dtype=torch.float32)
+    L.linear(x, w)
+    assert [a[-2:] for n, a in calls if n == "qs_linear_call_bytes"] == [(B.QS_F32, 0), (B.QS_BF16, 0)]
+    calls.clear()
+    L.linear_grad(torch.zeros(4, 5, dtype=torch.bfloat16), x, w, dtype=torch.bfloat16)
+    L.linear_grad(torch.zeros(4, 5, dtype=torch.bfloat16), x, w)
+    assert [a[-1] for n, a in calls if n == "qs_linear_grad_weight_call_bytes"] == [B.QS_BF16, B.QS_F32]
+
+
+def test_workspace_sizes_are_refused_as_the_calls_are():
+    P, lib = 1 << 20, B.lib()
+    of = lambda **kw: lib.qs_linear_call_bytes(*{**dict(R=1, M=4, N=5, K=8, x=P, xt=1, xs=8, w=P, wt=0, ww=0, ws=8, ot=0, at=0), **kw}.values())  # noqa: E731
+    for kw in (dict(R=0), dict(K=0), dict(ot=3), dict(ot=9), dict(wt=2), dict(M=-1)):
+        assert of(**kw) == -1, kw
+    assert of(N=1 << 25) == B.QS_TOO_LARGE and of(M=0) == 0
+    of = lambda **kw: lib.qs_linear_grad_weight_call_bytes(*{**dict(R=1, M=4, N=5, K=8, dz=P, t=1, dzs=5, x=P, xs=8, ot=0), **kw}.values())  # noqa: E731
+    for kw in (dict(R=33), dict(N=0), dict(ot=2), dict(t=3, ot=3), dict(t=0, ot=1)):
+        assert of(**kw) == -1, kw
+    assert of(M=1 << 29) == B.QS_TOO_LARGE and of(M=0) == 0
